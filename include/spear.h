@@ -356,6 +356,117 @@ spear_status_t spear_group_launches(int32_t n, const spear_layer_call_t* calls, 
 spear_status_t spear_w4ec_linear_group(int32_t n, const spear_layer_call_t* calls, void* workspace,
                                        size_t workspace_bytes, void* hip_stream);
 
+/* ---- Low-rank adapters of many requests --------------------------------------
+ * The tokens of a serving batch share the 4-bit weights and may each belong to
+ * a request with a low-rank adapter of its own. Beside the shared product, and
+ * the EC where there is one, a token m with adapter a = ids[m] gets
+ *
+ *     Y[m] += scale[a] * (X[m] . A_a^T) . B_a^T
+ *
+ * The adapters lie in slots of equal size: slot a holds A_a [rank][K] at
+ * A + a * a_stride and B_a [N][rank] at B + a * b_stride (elements), of which
+ * the first ranks[a] rows of A_a and columns of B_a count; what lies beyond
+ * them may hold anything. ids, ranks and scale are read on the device when the
+ * kernels run, so that a captured call follows their contents. */
+typedef struct {
+  int32_t n_adapters;   /* slots, >= 0                                        */
+  int32_t rank;         /* r of the slots, 0..256                             */
+  const void* A;        /* slots of [r][K] act dtype                          */
+  const void* B;        /* slots of [N][r] act dtype                          */
+  int64_t a_stride;     /* elements between slots: 0 = r K; else a multiple of
+                           8 (SPEAR_E_ALIGN) that is at least r K             */
+  int64_t b_stride;     /* 0 = N r; else at least N r                         */
+  const int32_t* ranks; /* [n_adapters] rank of each slot, clamped to 0..r;
+                           NULL: all r                                        */
+  const float* scale;   /* [n_adapters] fp32; NULL: all 1                     */
+  const int32_t* ids;   /* [M] slot of each token; any value outside
+                           [0, n_adapters): no adapter                        */
+} spear_adapters_t;
+
+/* Workspace bytes of the calls below for n members (n = 1: the single call):
+ * what spear_group_workspace gives, then each member's adapter data. Of calls[i]
+ * prob and whether ec is NULL are read, of adapters[i] (NULL: a member without
+ * adapters) n_adapters and rank. Host-only. Errors as in spear_group_workspace,
+ * and SPEAR_E_SHAPE for n_adapters < 0, rank outside 0..256 or a product of
+ * rank with M, N or K of 2^30 elements or more. */
+spear_status_t spear_adapters_workspace(int32_t n, const spear_layer_call_t* calls,
+                                        const spear_adapters_t* const* adapters, size_t* out_bytes);
+
+/* spear_w4ec_linear (ec NULL: spear_w4_linear) with adapters, followed by the
+ * post-EC tail if tail is not NULL. Y = the layer + the adapters' term + the
+ * tail's residual: the term and the residual are summed in fp32, rounded once
+ * to the act dtype and added to the layer's fp32 sums before Y's rounding. A
+ * token without an adapter gets what the call without adapters writes, and no
+ * token's result depends on another token's adapter or values. The workspace
+ * follows the rules of the other calls and may be shared with them in stream
+ * order. Errors as for spear_w4ec_linear_tail and spear_adapters_workspace,
+ * plus SPEAR_E_NULL for missing adapters, A, B or ids, SPEAR_E_ALIGN for a
+ * misaligned pointer or a_stride, SPEAR_E_SHAPE for a stride smaller than its
+ * slot, SPEAR_E_ALIAS for an output overlapping an adapter buffer. */
+spear_status_t spear_w4ec_linear_adapters(const spear_problem_t* prob, const void* x,
+                                          const spear_w4_t* w, const spear_ec_t* ec,
+                                          const spear_adapters_t* adapters, const spear_tail_t* tail,
+                                          void* y, void* workspace, size_t workspace_bytes,
+                                          void* hip_stream);
+
+/* spear_w4ec_linear_group with adapters: adapters[i] belongs to calls[i] (NULL:
+ * none). The adapters' terms of all members share their launches, and each
+ * member's Y is exactly (bit for bit) what its own spear_w4ec_linear_adapters
+ * call writes. Errors as for the group and the call above; SPEAR_E_NULL for a
+ * NULL array. */
+spear_status_t spear_w4ec_linear_adapters_group(int32_t n, const spear_layer_call_t* calls,
+                                                const spear_adapters_t* const* adapters,
+                                                void* workspace, size_t workspace_bytes,
+                                                void* hip_stream);
+
+/* ---- Norms around a block ----------------------------------------------------
+ * Between a block's output projection and the next block's input, in one pass
+ * over the rows (M tokens of N features):
+ *
+ *     o  = y                or  RMSNorm(y; post_w)       (norm after the block)
+ *     h' = stream_scale * h + branch_scale * act(gate) (.) o
+ *     x  = RMSNorm(h'; pre_w)                            (norm before the next)
+ *
+ * with RMSNorm(v; w)[n] = v[n] (w_offset + w[n]) / sqrt(mean_n v[n]^2 + eps),
+ * all in fp32; h' is rounded once to the stream's type, and x is computed from
+ * the rounded h' and rounded once to the act dtype. Where the layer needs no
+ * norm after the block, gate or scale, spear_w4ec_linear_tail does it inside
+ * the layer's call. */
+enum { SPEAR_BLOCK_GATE_MUL = 0, SPEAR_BLOCK_GATE_TANH = 1, SPEAR_BLOCK_GATE_SIGMOID = 2 };
+enum { SPEAR_STREAM_ACT = 0, SPEAR_STREAM_F32 = 1 };
+
+typedef struct {
+  int64_t M, N;           /* >= 0 (0 is a no-op)                              */
+  int32_t act_dtype;      /* SPEAR_F16 or SPEAR_BF16: y, weights, gate, x     */
+  int32_t stream_dtype;   /* h and h_out: SPEAR_STREAM_ACT (the act dtype) or
+                             SPEAR_STREAM_F32                                 */
+  const void* y;          /* [M][N] the block's output                        */
+  const void* post_w;     /* [N] weight of the norm after the block; NULL: none */
+  const void* gate;       /* [n_gates][N] rows; NULL: no gate                 */
+  const int32_t* gate_ids;/* [M] gate row of each token, any value outside
+                             [0, n_gates): no gate for it; NULL: row m, or the
+                             one row there is                                 */
+  const void* h;          /* [M][N] the residual stream; NULL: none (h = 0)   */
+  void* h_out;            /* [M][N] h'; may be h itself with the same rows    */
+  const void* pre_w;      /* [N] weight of the norm before the next block;
+                             NULL: none, x is not written                     */
+  void* x;                /* [M][N] the next block's input                    */
+  int64_t y_ld, gate_ld, h_ld, h_out_ld, x_ld; /* elements between rows, at
+                             least N; 0 = N                                   */
+  int32_t n_gates;        /* gate rows: >= 1; without gate_ids 1 or M         */
+  int32_t gate_kind;      /* SPEAR_BLOCK_GATE_*                               */
+  float stream_scale, branch_scale, w_offset, eps; /* finite; eps >= 0        */
+} spear_block_norm_t;
+
+/* One launch; needs no workspace. SPEAR_E_NULL for a missing argument, y, h_out,
+ * or x with pre_w; SPEAR_E_SHAPE for sizes, row strides, n_gates, scales or eps
+ * outside the above, or 2^31 rows or 2^30 features or more; SPEAR_E_DTYPE for
+ * an unknown type; SPEAR_E_UNSUPPORTED for an unknown gate kind; SPEAR_E_ALIGN
+ * for a pointer off 16 bytes (row strides may be any); SPEAR_E_ALIAS where h_out
+ * or x overlaps another buffer (from its first row to the end of its last),
+ * except h_out being h. */
+spear_status_t spear_block_norm(const spear_block_norm_t* args, void* hip_stream);
+
 /* Diagnostic of the dequantisation the kernels use: writes
  * w_out[n][k] = RNE_act((q[n][k] - z[n][k/G]) * s[n][k/G]) as a dense [N][K]
  * act-dtype matrix, the exact product rounded once to nearest even

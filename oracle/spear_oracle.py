@@ -322,3 +322,47 @@ def tolerance_check(y, y_ref, rel_frob: float = 5e-3, max_rel: float = 1e-2):
     bound = max_rel * float(np.abs(y_ref).max(initial=0.0))
     ok = (relf <= rel_frob) and (mx <= bound if bound > 0 else mx == 0.0)
     return ok, relf, mx, bound
+
+
+# ---------------------------------------------------------------------------
+# adapters of many requests, norms around a block (float64)
+# ---------------------------------------------------------------------------
+
+def adapters_term(x, A, B, ids, ranks=None, scale=None) -> np.ndarray:
+    """The adapters' term [M][N]: scale[a] (x[m] A_a^T) B_a^T with a = ids[m],
+    over the first ranks[a] rows of A_a [r][K] and columns of B_a [N][r]; zero
+    for an id outside [0, L)."""
+    x, A, B = (np.asarray(v, np.float64) for v in (x, A, B))
+    L, r, _ = A.shape
+    out = np.zeros((x.shape[0], B.shape[1]))
+    for m, a in enumerate(np.asarray(ids).tolist()):
+        if not 0 <= a < L:
+            continue
+        n = r if ranks is None else min(max(int(ranks[a]), 0), r)
+        s = 1.0 if scale is None else float(scale[a])
+        out[m] = s * (B[a, :, :n] @ (A[a, :n] @ x[m]))
+    return out
+
+
+def rms_norm(v, w, eps, w_offset=0.0) -> np.ndarray:
+    v, w = np.asarray(v, np.float64), np.asarray(w, np.float64)
+    return v / np.sqrt((v * v).mean(axis=1, keepdims=True) + eps) * (w_offset + w)
+
+
+def block_stream(y, h, post_w=None, gate=None, gate_ids=None, gate_kind="mul", stream_scale=1.0,
+                 branch_scale=1.0, eps=1e-5, w_offset=0.0) -> np.ndarray:
+    """h' [M][N] = stream_scale h + branch_scale act(gate) (.) o, with o = y or
+    RMSNorm(y; post_w); gate [rows][N], row gate_ids[m] (outside: factor one),
+    or row m, or the only row."""
+    o = np.asarray(y, np.float64)
+    if post_w is not None:
+        o = rms_norm(o, post_w, eps, w_offset)
+    if gate is not None:
+        g = np.asarray(gate, np.float64)
+        g = {"mul": lambda v: v, "tanh": np.tanh, "sigmoid": sigmoid}[gate_kind](g)
+        if gate_ids is not None:
+            rows = [g[i] if 0 <= i < len(g) else np.ones(o.shape[1]) for i in np.asarray(gate_ids).tolist()]
+            o = o * np.array(rows).reshape(o.shape)
+        else:
+            o = o * g
+    return branch_scale * o + (0.0 if h is None else stream_scale * np.asarray(h, np.float64))

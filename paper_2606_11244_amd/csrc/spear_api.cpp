@@ -1200,6 +1200,123 @@ void* device_scratch(spear_status_t* err) {
   return g_scratch_ptr[dev];
 }
 
+// the buffers of a post-EC tail; ws_bytes: what the call uses of its workspace
+spear_status_t check_tail(const spear_problem_t* prob, const void* x, const spear_tail_t* tail, const void* y,
+                          const void* workspace, size_t ws_bytes) {
+  if (tail->norm_w && !tail->y_norm) return SPEAR_E_NULL;
+  if (misaligned(tail->residual) || misaligned(tail->norm_w) || misaligned(tail->y_norm))
+    return SPEAR_E_ALIGN;
+  const size_t yb = (size_t)prob->M * prob->N * 2;
+  const size_t xb = (size_t)prob->M * prob->K * 2;
+  if (tail->residual && tail->residual != y && overlaps(tail->residual, yb, y, yb))
+    return SPEAR_E_ALIAS;
+  if (tail->norm_w &&
+      (overlaps(tail->y_norm, yb, y, yb) || overlaps(tail->y_norm, yb, x, xb) ||
+       overlaps(tail->y_norm, yb, tail->residual, yb) ||
+       overlaps(tail->y_norm, yb, tail->norm_w, (size_t)prob->N * 2) ||
+       overlaps(tail->y_norm, yb, workspace, ws_bytes)))
+    return SPEAR_E_ALIAS;
+  return SPEAR_OK;
+}
+
+// ---- adapters ---------------------------------------------------------------
+
+// The adapter data of one member in the workspace: its coordinates u and its
+// term d, the residual that its layer call adds.
+struct AdapterLayout {
+  bool on = false;  // the member has tokens, rows and adapters
+  size_t u = 0, d = 0;
+};
+
+spear_status_t adapters_layout(int32_t n, const spear_layer_call_t* calls, const spear_adapters_t* const* ads,
+                               AdapterLayout* al, size_t* total) {
+  size_t off = std::max(*total, kDataBase);
+  bool any = false;
+  for (int i = 0; i < n; ++i) {
+    const spear_problem_t* p = calls[i].prob;
+    const spear_adapters_t* a = ads[i];
+    if (!a) continue;
+    if (a->n_adapters < 0 || a->rank < 0 || a->rank > 256) return SPEAR_E_SHAPE;
+    const int64_t lim = (int64_t)1 << 30;
+    if (p->M * a->rank >= lim || p->N * a->rank >= lim || p->K * a->rank >= lim) return SPEAR_E_SHAPE;
+    al[i].on = p->M > 0 && p->N > 0 && a->n_adapters > 0 && a->rank > 0;
+    if (!al[i].on) continue;
+    any = true;
+    al[i].u = off;
+    off += round256((size_t)p->M * a->rank * 4);
+    al[i].d = off;
+    off += round256((size_t)p->M * p->N * 2);
+  }
+  if (any) *total = off;
+  return SPEAR_OK;
+}
+
+int64_t a_stride_of(const spear_problem_t* p, const spear_adapters_t* a) {
+  return a->a_stride ? a->a_stride : (int64_t)a->rank * p->K;
+}
+int64_t b_stride_of(const spear_problem_t* p, const spear_adapters_t* a) {
+  return a->b_stride ? a->b_stride : (int64_t)a->rank * p->N;
+}
+
+// a nonempty member's adapters (none: nothing to check)
+spear_status_t check_adapters(const spear_problem_t* p, const spear_adapters_t* a) {
+  if (!a || a->n_adapters == 0 || a->rank == 0) return SPEAR_OK;
+  if (!a->A || !a->B || !a->ids) return SPEAR_E_NULL;
+  if (misaligned(a->A) || misaligned(a->B) || misaligned(a->ids) || misaligned(a->ranks) || misaligned(a->scale))
+    return SPEAR_E_ALIGN;
+  const int64_t as = a_stride_of(p, a), bs = b_stride_of(p, a), top = (int64_t)1 << 31;
+  if (as < a->rank * p->K || bs < a->rank * p->N || as >= top || bs >= top) return SPEAR_E_SHAPE;
+  return as % 8 ? SPEAR_E_ALIGN : SPEAR_OK;
+}
+
+// whether an output overlaps an adapter buffer
+bool hits_adapters(const void* y, size_t yb, const spear_problem_t* p, const spear_adapters_t* a) {
+  if (!a || a->n_adapters == 0 || a->rank == 0) return false;
+  const size_t L = (size_t)a->n_adapters, M = (size_t)p->M;
+  return overlaps(y, yb, a->A, ((L - 1) * (size_t)a_stride_of(p, a) + (size_t)a->rank * p->K) * 2) ||
+         overlaps(y, yb, a->B, ((L - 1) * (size_t)b_stride_of(p, a) + (size_t)a->rank * p->N) * 2) ||
+         overlaps(y, yb, a->ids, M * 4) || overlaps(y, yb, a->ranks, L * 4) || overlaps(y, yb, a->scale, L * 4);
+}
+
+// Forms the members' terms (plus their residuals res) in the workspace; out[i]
+// is member i's, or null where it has no adapters. Members of one activation
+// dtype share the launches.
+spear_status_t run_adapters(int32_t n, const spear_layer_call_t* calls, const spear_adapters_t* const* ads,
+                            const AdapterLayout* al, const uint16_t* const* res, char* ws, const uint16_t** out,
+                            hipStream_t s) {
+  for (int dt : {SPEAR_F16, SPEAR_BF16}) {
+    AdapterGroup g;
+    std::memset(&g, 0, sizeof(g));
+    for (int i = 0; i < n; ++i) {
+      const spear_problem_t* p = calls[i].prob;
+      if (!al[i].on || p->act_dtype != dt) continue;
+      const spear_adapters_t* a = ads[i];
+      AdapterParams& q = g.p[g.n++];
+      q.x = (const uint16_t*)calls[i].x;
+      q.A = (const uint16_t*)a->A;
+      q.B = (const uint16_t*)a->B;
+      q.a_stride = a_stride_of(p, a);
+      q.b_stride = b_stride_of(p, a);
+      q.ids = a->ids;
+      q.ranks = a->ranks;
+      q.scale = a->scale;
+      q.res = res[i];
+      q.u = (float*)(ws + al[i].u);
+      q.d = (uint16_t*)(ws + al[i].d);
+      q.M = (int)p->M;
+      q.N = (int)p->N;
+      q.K = (int)p->K;
+      q.L = a->n_adapters;
+      q.R = a->rank;
+      out[i] = q.d;
+    }
+    if (g.n == 0) continue;
+    const spear_status_t st = hip_status(SPEAR_BY_DT(launch_adapters, dt)(g, s));
+    if (st != SPEAR_OK) return st;
+  }
+  return SPEAR_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -1264,19 +1381,7 @@ spear_status_t spear_w4ec_linear_tail(const spear_problem_t* prob, const void* x
   if (prob->M == 0 || prob->N == 0) return SPEAR_OK;
   if ((st = check_w4(prob, x, w, y)) != SPEAR_OK) return st;
   if (ec && (st = check_ec(prob, z, ec, y)) != SPEAR_OK) return st;
-  if (tail->norm_w && !tail->y_norm) return SPEAR_E_NULL;
-  if (misaligned(tail->residual) || misaligned(tail->norm_w) || misaligned(tail->y_norm))
-    return SPEAR_E_ALIGN;
-  const size_t yb = (size_t)prob->M * prob->N * 2;
-  const size_t xb = (size_t)prob->M * prob->K * 2;
-  if (tail->residual && tail->residual != y && overlaps(tail->residual, yb, y, yb))
-    return SPEAR_E_ALIAS;
-  if (tail->norm_w &&
-      (overlaps(tail->y_norm, yb, y, yb) || overlaps(tail->y_norm, yb, x, xb) ||
-       overlaps(tail->y_norm, yb, tail->residual, yb) ||
-       overlaps(tail->y_norm, yb, tail->norm_w, (size_t)prob->N * 2) ||
-       overlaps(tail->y_norm, yb, workspace, z.plan.workspace_bytes)))
-    return SPEAR_E_ALIAS;
+  if ((st = check_tail(prob, x, tail, y, workspace, z.plan.workspace_bytes)) != SPEAR_OK) return st;
   if ((st = check_ws(prob, z, y, workspace, workspace_bytes)) != SPEAR_OK) return st;
   hipStream_t s = (hipStream_t)hip_stream;
   st = run_layer(prob, z, x, w, ec, y, (const uint16_t*)tail->residual, (char*)workspace, s);
@@ -1467,12 +1572,17 @@ spear_status_t spear_group_launches(int32_t n, const spear_layer_call_t* calls, 
   return SPEAR_OK;
 }
 
-spear_status_t spear_w4ec_linear_group(int32_t n, const spear_layer_call_t* calls, void* workspace,
-                                       size_t workspace_bytes, void* hip_stream) {
+// The grouped call; ads: the members' adapters (the array or any member may be
+// NULL), whose terms are formed first and enter the members as residuals.
+static spear_status_t group_call(int32_t n, const spear_layer_call_t* calls,
+                                 const spear_adapters_t* const* ads, void* workspace,
+                                 size_t workspace_bytes, void* hip_stream) {
   Resolved z[SPEAR_GROUP_MAX];
   size_t off[SPEAR_GROUP_MAX], total = 0;
   spear_status_t st = group_resolve(n, calls, z, off, &total);
   if (st != SPEAR_OK) return st;
+  AdapterLayout al[SPEAR_GROUP_MAX];
+  if (ads && (st = adapters_layout(n, calls, ads, al, &total)) != SPEAR_OK) return st;
   if (total > 0) {
     if (!workspace || workspace_bytes < total) return SPEAR_E_WORKSPACE;
     if (misaligned(workspace)) return SPEAR_E_ALIGN;
@@ -1486,6 +1596,7 @@ spear_status_t spear_w4ec_linear_group(int32_t n, const spear_layer_call_t* call
     if (p->M == 0 || p->N == 0) continue;
     if ((st = check_w4(p, c.x, c.w, c.y)) != SPEAR_OK) return st;
     if (c.ec && (st = check_ec(p, z[i], c.ec, c.y)) != SPEAR_OK) return st;
+    if (ads && (st = check_adapters(p, ads[i])) != SPEAR_OK) return st;
   }
   for (int i = 0; i < n; ++i) {
     const spear_layer_call_t& c = calls[i];
@@ -1496,8 +1607,16 @@ spear_status_t spear_w4ec_linear_group(int32_t n, const spear_layer_call_t* call
     for (int j = 0; j < n; ++j)
       if (j != i && calls[j].prob->M > 0 && calls[j].prob->N > 0 && hits_member(c.y, yb, calls[j]))
         return SPEAR_E_ALIAS;
+    for (int j = 0; ads && j < n; ++j)
+      if (calls[j].prob->M > 0 && calls[j].prob->N > 0 && hits_adapters(c.y, yb, calls[j].prob, ads[j]))
+        return SPEAR_E_ALIAS;
   }
   hipStream_t s = (hipStream_t)hip_stream;
+  const uint16_t* res[SPEAR_GROUP_MAX] = {};
+  if (ads) {
+    const uint16_t* none[SPEAR_GROUP_MAX] = {};
+    if ((st = run_adapters(n, calls, ads, al, none, (char*)workspace, res, s)) != SPEAR_OK) return st;
+  }
   // Members of one single-launch GEMV variant share one launch; the other
   // members run one after another on the same stream, as their own calls
   // would. Every member's output is the one its own call writes.
@@ -1511,7 +1630,7 @@ spear_status_t spear_w4ec_linear_group(int32_t n, const spear_layer_call_t* call
   for (int i = 0; i < n; ++i) {
     const spear_layer_call_t& c = calls[i];
     if (in[i] || set[i] >= 0 || ec_set[i] >= 0 || c.prob->M == 0 || c.prob->N == 0) continue;
-    st = run_layer(c.prob, z[i], c.x, c.w, c.ec, c.y, nullptr, ws, s);
+    st = run_layer(c.prob, z[i], c.x, c.w, c.ec, c.y, res[i], ws, s);
     if (st != SPEAR_OK) return st;
   }
   // the shared EC pre-kernels, then the 4-bit products that add their
@@ -1549,6 +1668,7 @@ spear_status_t spear_w4ec_linear_group(int32_t n, const spear_layer_call_t* call
         const spear_layer_call_t& m = calls[i];
         GemvParams& q = g.p[g.n];
         q = make_gemv(m.prob, z[i], m.x, m.w, m.y, m.ec, ws + off[i]);
+        q.res = res[i];
         q.ec = ecp[i];
         if (z[i].S > 1) {
           q.rb_ctr = (uint32_t*)(ws + kCtrRows) + ctr;
@@ -1563,7 +1683,7 @@ spear_status_t spear_w4ec_linear_group(int32_t n, const spear_layer_call_t* call
       if (st != SPEAR_OK) return st;
     }
     if (set[k] < 0 && gv_set[k] < 0 && ec_set[k] >= 0) {
-      st = run_2k_main(c.prob, z[k], c.x, c.w, c.ec, ecp[k], c.y, nullptr, ws + off[k], s, ws);
+      st = run_2k_main(c.prob, z[k], c.x, c.w, c.ec, ecp[k], c.y, res[k], ws + off[k], s, ws);
       if (st != SPEAR_OK) return st;
     }
     if (set[k] != k) continue;
@@ -1575,6 +1695,7 @@ spear_status_t spear_w4ec_linear_group(int32_t n, const spear_layer_call_t* call
       const spear_layer_call_t& m = calls[i];
       GemmParams& q = g.p[g.n];
       q = make_gemm(m.prob, z[i], m.x, m.w, m.y, z[i].ec ? m.ec : nullptr, ws ? ws + off[i] : nullptr);
+      q.res = res[i];
       const int tiles = mid_tiles(z[i].gmid, (int)m.prob->M, (int)m.prob->N);
       if (z[i].Sg > 1) {
         q.ctr = (uint32_t*)(ws + kCtrRows) + ctr;
@@ -1626,6 +1747,7 @@ spear_status_t spear_w4ec_linear_group(int32_t n, const spear_layer_call_t* call
     g.start[k + 1] = g.start[k] + z[i].nrg * z[i].S;
     GemvParams& q = g.p[k];
     q = make_gemv(c.prob, z[i], c.x, c.w, c.y, z[i].ec ? c.ec : nullptr, wsi);
+    q.res = res[i];
     if (z[i].ec) {
       q.ec = make_ec(c.prob, z[i], c.x, c.ec, wsi);
       if (z[i].S > 1) q.eupart = (float*)(wsi + z[i].off_eupart);
@@ -1640,6 +1762,130 @@ spear_status_t spear_w4ec_linear_group(int32_t n, const spear_layer_call_t* call
   g.n = k;
   const Resolved& z0 = z[first];
   return hip_status(SPEAR_BY_WB(launch_gemv_group, z0.wb, z0.dt)(z0.MT, z0.RT, epi, g, 64 * z0.NW, lds, s));
+}
+
+spear_status_t spear_w4ec_linear_group(int32_t n, const spear_layer_call_t* calls, void* workspace,
+                                       size_t workspace_bytes, void* hip_stream) {
+  return group_call(n, calls, nullptr, workspace, workspace_bytes, hip_stream);
+}
+
+spear_status_t spear_adapters_workspace(int32_t n, const spear_layer_call_t* calls,
+                                        const spear_adapters_t* const* adapters, size_t* out_bytes) {
+  if (!adapters) return SPEAR_E_NULL;
+  Resolved z[SPEAR_GROUP_MAX];
+  size_t off[SPEAR_GROUP_MAX], total = 0;
+  if (!out_bytes) return SPEAR_E_NULL;
+  spear_status_t st = group_resolve(n, calls, z, off, &total);
+  if (st != SPEAR_OK) return st;
+  AdapterLayout al[SPEAR_GROUP_MAX];
+  if ((st = adapters_layout(n, calls, adapters, al, &total)) != SPEAR_OK) return st;
+  *out_bytes = total;
+  return SPEAR_OK;
+}
+
+spear_status_t spear_w4ec_linear_adapters_group(int32_t n, const spear_layer_call_t* calls,
+                                                const spear_adapters_t* const* adapters,
+                                                void* workspace, size_t workspace_bytes,
+                                                void* hip_stream) {
+  if (!adapters) return SPEAR_E_NULL;
+  return group_call(n, calls, adapters, workspace, workspace_bytes, hip_stream);
+}
+
+spear_status_t spear_w4ec_linear_adapters(const spear_problem_t* prob, const void* x,
+                                          const spear_w4_t* w, const spear_ec_t* ec,
+                                          const spear_adapters_t* adapters, const spear_tail_t* tail,
+                                          void* y, void* workspace, size_t workspace_bytes,
+                                          void* hip_stream) {
+  if (!prob || !adapters) return SPEAR_E_NULL;
+  const spear_layer_call_t call = {prob, x, w, ec, y};
+  Resolved z[SPEAR_GROUP_MAX];
+  size_t off[SPEAR_GROUP_MAX], total = 0;
+  spear_status_t st = group_resolve(1, &call, z, off, &total);
+  if (st != SPEAR_OK) return st;
+  AdapterLayout al[SPEAR_GROUP_MAX];
+  if ((st = adapters_layout(1, &call, &adapters, al, &total)) != SPEAR_OK) return st;
+  if (tail && (!std::isfinite(tail->eps) || tail->eps < 0.f)) return SPEAR_E_SHAPE;
+  if (prob->M == 0 || prob->N == 0) return SPEAR_OK;
+  if ((st = check_w4(prob, x, w, y)) != SPEAR_OK) return st;
+  if (ec && (st = check_ec(prob, z[0], ec, y)) != SPEAR_OK) return st;
+  if ((st = check_adapters(prob, adapters)) != SPEAR_OK) return st;
+  if (tail && (st = check_tail(prob, x, tail, y, workspace, total)) != SPEAR_OK) return st;
+  const size_t yb = (size_t)prob->M * prob->N * 2;
+  if (hits_adapters(y, yb, prob, adapters) ||
+      (tail && tail->norm_w && hits_adapters(tail->y_norm, yb, prob, adapters)))
+    return SPEAR_E_ALIAS;
+  if (total > 0) {
+    if (!workspace || workspace_bytes < total) return SPEAR_E_WORKSPACE;
+    if (misaligned(workspace)) return SPEAR_E_ALIGN;
+    if (overlaps(y, yb, workspace, total)) return SPEAR_E_ALIAS;
+  }
+  hipStream_t s = (hipStream_t)hip_stream;
+  const uint16_t* res = tail ? (const uint16_t*)tail->residual : nullptr;
+  const uint16_t* term = nullptr;
+  if ((st = run_adapters(1, &call, &adapters, al, &res, (char*)workspace, &term, s)) != SPEAR_OK) return st;
+  st = run_layer(prob, z[0], x, w, ec, y, term ? term : res, (char*)workspace, s);
+  if (st != SPEAR_OK || !tail || !tail->norm_w) return st;
+  return hip_status(SPEAR_BY_DT(launch_rmsnorm, z[0].dt)((const uint16_t*)y, (const uint16_t*)tail->norm_w,
+                                   tail->eps, (uint16_t*)tail->y_norm, (int)prob->M, (int)prob->N, s));
+}
+
+spear_status_t spear_block_norm(const spear_block_norm_t* a, void* hip_stream) {
+  if (!a) return SPEAR_E_NULL;
+  const int64_t M = a->M, N = a->N;
+  if (M < 0 || N < 0 || M >= ((int64_t)1 << 31) || N >= ((int64_t)1 << 30)) return SPEAR_E_SHAPE;
+  if (a->act_dtype != SPEAR_F16 && a->act_dtype != SPEAR_BF16) return SPEAR_E_DTYPE;
+  if (a->stream_dtype != SPEAR_STREAM_ACT && a->stream_dtype != SPEAR_STREAM_F32) return SPEAR_E_DTYPE;
+  if (a->gate_kind < SPEAR_BLOCK_GATE_MUL || a->gate_kind > SPEAR_BLOCK_GATE_SIGMOID) return SPEAR_E_UNSUPPORTED;
+  if (!std::isfinite(a->stream_scale) || !std::isfinite(a->branch_scale) || !std::isfinite(a->w_offset) ||
+      !std::isfinite(a->eps) || a->eps < 0.f)
+    return SPEAR_E_SHAPE;
+  // a row stride may not let an extent leave 62 bits
+  bool ld_ok = true;
+  auto ld = [&](int64_t v) {
+    const int64_t l = v == 0 ? N : v;
+    ld_ok = ld_ok && l >= N && l < ((int64_t)1 << 30);
+    return l;
+  };
+  const int64_t yl = ld(a->y_ld), gl = ld(a->gate_ld), hl = ld(a->h_ld), ol = ld(a->h_out_ld), xl = ld(a->x_ld);
+  if (!ld_ok) return SPEAR_E_SHAPE;
+  if (a->gate && (a->n_gates < 1 || (!a->gate_ids && a->n_gates != 1 && a->n_gates != M))) return SPEAR_E_SHAPE;
+  if (M == 0 || N == 0) return SPEAR_OK;
+  if (!a->y || !a->h_out || (a->pre_w && !a->x)) return SPEAR_E_NULL;
+  if (misaligned(a->y) || misaligned(a->post_w) || misaligned(a->gate) || misaligned(a->gate_ids) ||
+      misaligned(a->h) || misaligned(a->h_out) || misaligned(a->pre_w) || (a->pre_w && misaligned(a->x)))
+    return SPEAR_E_ALIGN;
+  const size_t hb = a->stream_dtype == SPEAR_STREAM_F32 ? 4 : 2;
+  auto bytes = [&](int64_t rows, int64_t l, size_t e) { return ((size_t)(rows - 1) * l + N) * e; };
+  const size_t ob = bytes(M, ol, hb), xb = bytes(M, xl, 2), hbytes = bytes(M, hl, hb), row = (size_t)N * 2;
+  auto hits = [&](const void* o, size_t b) {
+    return overlaps(o, b, a->y, bytes(M, yl, 2)) || overlaps(o, b, a->post_w, row) || overlaps(o, b, a->pre_w, row) ||
+           (a->gate && overlaps(o, b, a->gate, bytes(a->n_gates, gl, 2))) ||
+           (a->gate && overlaps(o, b, a->gate_ids, (size_t)M * 4));
+  };
+  if (hits(a->h_out, ob) || ((a->h_out != a->h || hl != ol) && overlaps(a->h_out, ob, a->h, hbytes)))
+    return SPEAR_E_ALIAS;
+  if (a->pre_w && (hits(a->x, xb) || overlaps(a->x, xb, a->h, hbytes) || overlaps(a->x, xb, a->h_out, ob)))
+    return SPEAR_E_ALIAS;
+  BlockNormParams p;
+  std::memset(&p, 0, sizeof(p));
+  p.y = (const uint16_t*)a->y;
+  p.post_w = (const uint16_t*)a->post_w;
+  p.gate = (const uint16_t*)a->gate;
+  p.gate_ids = a->gate_ids;
+  p.h = a->h;
+  p.h_out = a->h_out;
+  p.pre_w = (const uint16_t*)a->pre_w;
+  p.x = (uint16_t*)a->x;
+  p.y_ld = yl, p.gate_ld = gl, p.h_ld = hl, p.h_out_ld = ol, p.x_ld = xl;
+  p.stream_scale = a->stream_scale;
+  p.branch_scale = a->branch_scale;
+  p.w_offset = a->w_offset;
+  p.eps = a->eps;
+  p.M = (int)M, p.N = (int)N;
+  p.n_gates = a->n_gates;
+  p.gate_kind = a->gate_kind;
+  p.f32 = a->stream_dtype == SPEAR_STREAM_F32;
+  return hip_status(SPEAR_BY_DT(launch_block_norm, a->act_dtype)(p, (hipStream_t)hip_stream));
 }
 
 spear_status_t spear_w4_dequant(const spear_problem_t* prob, const spear_w4_t* w, void* w_out,

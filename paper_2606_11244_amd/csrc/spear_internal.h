@@ -215,6 +215,42 @@ struct EcGroup {
   int start[kGroupMax + 1];
   int n;
 };
+// The adapters' term of up to kGroupMax layers, in shared launches.
+struct AdapterParams {
+  const uint16_t* x;      // [M][K]
+  const uint16_t* A;      // slots of [R][K], a_stride elements apart
+  const uint16_t* B;      // slots of [N][R], b_stride elements apart
+  const int32_t* ids;     // [M] slot of each token, outside [0, L): none
+  const int32_t* ranks;   // [L] or null (all R)
+  const float* scale;     // [L] or null (all 1)
+  const uint16_t* res;    // [M][N] residual, or null
+  uint16_t* d;            // [M][N] the term plus the residual, act dtype
+  float* u;               // [M][R] scaled coordinates
+  int64_t a_stride, b_stride;
+  int M, N, K, L, R;
+};
+struct AdapterGroup {
+  AdapterParams p[kGroupMax];
+  int shrink_start[kGroupMax + 1], expand_start[kGroupMax + 1];  // first workgroups
+  int n;
+};
+
+// The norms around a block.
+enum { BGATE_MUL = 0, BGATE_TANH = 1, BGATE_SIGMOID = 2 };
+struct BlockNormParams {
+  const uint16_t* y;
+  const uint16_t* post_w;  // or null
+  const uint16_t* gate;    // or null
+  const int32_t* gate_ids; // or null
+  const void* h;           // or null; fp32 or act dtype
+  void* h_out;
+  const uint16_t* pre_w;   // or null
+  uint16_t* x;
+  int64_t y_ld, gate_ld, h_ld, h_out_ld, x_ld;
+  float stream_scale, branch_scale, w_offset, eps;
+  int M, N, n_gates, gate_kind, f32;
+};
+
 // EPI_LOCAL GEMM: the EC stage tile holds A's 16 rows and w_g (row 16)
 constexpr int kGemmEcRows = 17;
 
@@ -273,6 +309,8 @@ __host__ __device__ inline size_t ec_block_lds(int NW, int R1p, int h, int r) {
   hipError_t launch_ec_up_acc_##D(const float* v, const uint16_t* B, const int8_t* B8,           \
                                   const float* sb, uint16_t* y, int M, int N, int r,             \
                                   hipStream_t st);                                               \
+  hipError_t launch_adapters_##D(AdapterGroup& g, hipStream_t st);                               \
+  hipError_t launch_block_norm_##D(const BlockNormParams& p, hipStream_t st);                    \
   SPEAR_WEIGHT_LAUNCHERS(w4_##D)                                                                 \
   SPEAR_WEIGHT_LAUNCHERS(w3_##D)
 SPEAR_ACT_LAUNCHERS(f16)

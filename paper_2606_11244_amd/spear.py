@@ -36,7 +36,8 @@ EXPORTED = ("spear_dispatch_plan", "spear_w4_linear", "spear_w4ec_linear", "spea
             "spear_group_launches", "spear_set_wait_polls", "spear_set_gemv_shape",
             "spear_set_gemm_slices",
             "spear_set_gemm_tile", "spear_set_gemm_roles", "spear_workspace_regions",
-            "spear_w4ec_linear_noalloc",
+            "spear_w4ec_linear_noalloc", "spear_adapters_workspace", "spear_w4ec_linear_adapters",
+            "spear_w4ec_linear_adapters_group", "spear_block_norm",
             "spear_set_gemv_stages",
             "spear_status_string", "spear_version", "spear_sched_latency", "spear_sched_chunk")
 
@@ -77,6 +78,30 @@ class LayerCall(ctypes.Structure):
 
 
 GROUP_MAX = 4
+
+
+class Adapters(ctypes.Structure):
+    _fields_ = [("n_adapters", ctypes.c_int32), ("rank", ctypes.c_int32), ("A", ctypes.c_void_p),
+                ("B", ctypes.c_void_p), ("a_stride", ctypes.c_int64), ("b_stride", ctypes.c_int64),
+                ("ranks", ctypes.c_void_p), ("scale", ctypes.c_void_p), ("ids", ctypes.c_void_p)]
+
+
+BLOCK_GATE_MUL, BLOCK_GATE_TANH, BLOCK_GATE_SIGMOID = 0, 1, 2
+BLOCK_GATES = {"mul": BLOCK_GATE_MUL, "tanh": BLOCK_GATE_TANH, "sigmoid": BLOCK_GATE_SIGMOID}
+STREAM_ACT, STREAM_F32 = 0, 1
+
+
+class BlockNorm(ctypes.Structure):
+    _fields_ = [("M", ctypes.c_int64), ("N", ctypes.c_int64), ("act_dtype", ctypes.c_int32),
+                ("stream_dtype", ctypes.c_int32), ("y", ctypes.c_void_p),
+                ("post_w", ctypes.c_void_p), ("gate", ctypes.c_void_p),
+                ("gate_ids", ctypes.c_void_p), ("h", ctypes.c_void_p), ("h_out", ctypes.c_void_p),
+                ("pre_w", ctypes.c_void_p), ("x", ctypes.c_void_p), ("y_ld", ctypes.c_int64),
+                ("gate_ld", ctypes.c_int64), ("h_ld", ctypes.c_int64), ("h_out_ld", ctypes.c_int64),
+                ("x_ld", ctypes.c_int64), ("n_gates", ctypes.c_int32),
+                ("gate_kind", ctypes.c_int32), ("stream_scale", ctypes.c_float),
+                ("branch_scale", ctypes.c_float), ("w_offset", ctypes.c_float),
+                ("eps", ctypes.c_float)]
 
 
 class Plan(ctypes.Structure):
@@ -128,6 +153,15 @@ def _load():
     lib.spear_group_launches.argtypes = [ctypes.c_int32, P(LayerCall), P(ctypes.c_int32)]
     lib.spear_w4ec_linear_group.argtypes = [ctypes.c_int32, P(LayerCall), ctypes.c_void_p,
                                             ctypes.c_size_t, ctypes.c_void_p]
+    lib.spear_adapters_workspace.argtypes = [ctypes.c_int32, P(LayerCall), P(P(Adapters)),
+                                             P(ctypes.c_size_t)]
+    lib.spear_w4ec_linear_adapters.argtypes = [P(Problem), ctypes.c_void_p, P(W4), P(EC),
+                                               P(Adapters), P(Tail), ctypes.c_void_p,
+                                               ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]
+    lib.spear_w4ec_linear_adapters_group.argtypes = [ctypes.c_int32, P(LayerCall), P(P(Adapters)),
+                                                     ctypes.c_void_p, ctypes.c_size_t,
+                                                     ctypes.c_void_p]
+    lib.spear_block_norm.argtypes = [P(BlockNorm), ctypes.c_void_p]
     lib.spear_set_wait_polls.argtypes = [ctypes.c_int32]
     lib.spear_workspace_regions.argtypes = [P(Problem), ctypes.c_int32] + [P(ctypes.c_size_t)] * 4
     lib.spear_set_gemv_shape.argtypes = [ctypes.c_int32] * 3
@@ -151,7 +185,9 @@ def _load():
     for f in ("spear_dispatch_plan", "spear_w4_linear", "spear_w4ec_linear", "spear_w4_dequant",
               "spear_w4ec_linear_tail", "spear_group_workspace", "spear_w4ec_linear_group",
               "spear_group_launches", "spear_set_wait_polls", "spear_workspace_regions",
-              "spear_w4ec_linear_noalloc"):
+              "spear_w4ec_linear_noalloc", "spear_adapters_workspace",
+              "spear_w4ec_linear_adapters", "spear_w4ec_linear_adapters_group",
+              "spear_block_norm"):
         getattr(lib, f).restype = ctypes.c_int32
     return lib
 
@@ -349,6 +385,161 @@ def w4ec_linear_group(members, workspace=None, stream=None):
                                      _stream(stream))
     if st != 0:
         raise SpearError(st, "spear_w4ec_linear_group")
+
+
+def adapters(A, B, ids, ranks=None, scale=None) -> Adapters:
+    """Adapters of a batch's tokens (include/spear.h): A [L][r][K] and B
+    [L][N][r] in the activation dtype, whose slots may lie further apart than
+    their size (dense within a slot); ids [M] int32, ranks [L] int32, scale [L]
+    fp32. The struct keeps its tensors alive."""
+    if A.dim() != 3 or B.dim() != 3 or A.shape[0] != B.shape[0] or A.shape[1] != B.shape[2]:
+        raise ValueError("adapters: A [L][r][K] and B [L][N][r]")
+    if A.dtype != B.dtype:
+        raise TypeError("adapters: A and B differ in dtype")
+    for t, dt in ((ids, torch.int32), (ranks, torch.int32), (scale, torch.float32)):
+        if t is not None and (t.dtype != dt or not t.is_contiguous()):
+            raise TypeError(f"adapters: ids and ranks int32, scale fp32, contiguous (got {t.dtype})")
+    L, r, K = A.shape
+    for t in (ranks, scale):
+        if t is not None and t.numel() != L:
+            raise ValueError("adapters: ranks and scale have one entry a slot")
+    for t in (A, B):
+        if t.numel() and not t[0].is_contiguous():
+            raise ValueError("adapters: a slot is dense")
+
+    def p(t):
+        return None if t is None else t.data_ptr()
+
+    far = L > 1 and r > 0
+    a = Adapters(L, r, p(A), p(B), A.stride(0) if far else 0, B.stride(0) if far else 0, p(ranks),
+                 p(scale), p(ids))
+    a._keep = (A, B, ids, ranks, scale)
+    return a
+
+
+def _same_device(first, *tensors):
+    """Every tensor on the current GPU: a kernel reads what it is given, and the
+    stream is the current device's."""
+    if not first.is_cuda or first.device.index != torch.cuda.current_device():
+        raise ValueError(f"tensors on the current GPU are needed (got {first.device})")
+    for t in tensors:
+        if t is not None and t.device != first.device:
+            raise ValueError(f"tensors on one device are needed (got {t.device} beside {first.device})")
+
+
+def _adapters_array(members):
+    ptrs = [m.get("adapters") for m in members]
+    return (ctypes.POINTER(Adapters) * max(len(ptrs), 1))(
+        *[ctypes.pointer(a) if a is not None else None for a in ptrs])
+
+
+def _check_adapters(prob, x, adapters):
+    """What only the tensors know: the slots' sizes, the tokens' count, the device."""
+    if adapters is None:
+        return
+    A, B, ids = adapters._keep[:3]
+    _same_device(x, *adapters._keep)
+    if A.shape[2] != prob.K or B.shape[1] != prob.N or ids.numel() < prob.M:
+        raise ValueError("adapters: A [L][r][K], B [L][N][r] and ids [M] of the problem's sizes")
+    if _dtype_code(A) != prob.act_dtype:
+        raise TypeError("adapters: A and B are in the activation dtype")
+
+
+def adapters_workspace(members) -> int:
+    """Workspace bytes of a call with adapters, single (one member) or grouped;
+    members as in w4ec_linear_adapters_group."""
+    arr, keep = _group_array(members)
+    out = ctypes.c_size_t(0)
+    st = LIB.spear_adapters_workspace(len(members), arr, _adapters_array(members), ctypes.byref(out))
+    if st != 0:
+        raise SpearError(st, "spear_adapters_workspace")
+    return out.value
+
+
+def w4ec_linear_adapters(prob: Problem, x, qweight, scales, zeros, adapters, y, *, ec_args=None,
+                         residual=None, norm_w=None, eps=1e-5, y_norm=None, workspace=None,
+                         stream=None):
+    """The layer with its tokens' adapters (include/spear.h), and with the
+    post-EC tail where a residual or norm_w is given; ec_args as in
+    w4ec_linear_tail."""
+    _check_adapters(prob, x, adapters)
+    w = W4(qweight.data_ptr(), scales.data_ptr(), zeros.data_ptr())
+    ec = ctypes.byref(_ec_from_args(ec_args)) if ec_args is not None else None
+    tail = None
+    if residual is not None or norm_w is not None:
+        tail = ctypes.byref(Tail(None if residual is None else residual.data_ptr(),
+                                 None if norm_w is None else norm_w.data_ptr(), float(eps),
+                                 None if y_norm is None else y_norm.data_ptr()))
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    st = LIB.spear_w4ec_linear_adapters(ctypes.byref(prob), x.data_ptr(), ctypes.byref(w), ec,
+                                        ctypes.byref(adapters), tail, y.data_ptr(), _ptr(workspace),
+                                        ws_bytes, _stream(stream))
+    if st != 0:
+        raise SpearError(st, "spear_w4ec_linear_adapters")
+    return y
+
+
+def w4ec_linear_adapters_group(members, workspace=None, stream=None):
+    """w4ec_linear_group with the adapters of each member's "adapters" entry
+    (None: none)."""
+    for m in members:
+        _check_adapters(m["prob"], m["x"], m.get("adapters"))
+    arr, keep = _group_array(members)
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    st = LIB.spear_w4ec_linear_adapters_group(len(members), arr, _adapters_array(members),
+                                              _ptr(workspace), ws_bytes, _stream(stream))
+    if st != 0:
+        raise SpearError(st, "spear_w4ec_linear_adapters_group")
+
+
+def _rows(t, M, N, dtypes, what):
+    """Row stride of a [M][N] tensor of dense rows."""
+    if t.dtype not in dtypes:
+        raise TypeError(f"block_norm: {what} is {t.dtype}")
+    if t.dim() != 2 or t.shape[0] != M or t.shape[1] != N or (N > 1 and M > 0 and t.stride(1) != 1):
+        raise ValueError(f"block_norm: {what} is [{M}][{N}] with dense rows")
+    return t.stride(0) if M > 1 else 0
+
+
+def block_norm(y, h, h_out, x=None, *, post_w=None, pre_w=None, gate=None, gate_ids=None,
+               gate_kind="mul", stream_scale=1.0, branch_scale=1.0, w_offset=0.0, eps=1e-5,
+               stream=None):
+    """The norms around a block (include/spear.h): h_out = stream_scale h +
+    branch_scale act(gate) (.) RMSNorm(y; post_w), x = RMSNorm(h_out; pre_w).
+    y, h, h_out, x: [M][N], rows of any stride; h (or None) and h_out in the
+    activation dtype or fp32; gate [N], [rows][N]; gate_ids [M] int32."""
+    _same_device(y, h, h_out, x, post_w, pre_w, gate, gate_ids)
+    M, N = y.shape
+    dt = _dtype_code(y)
+    f32 = h_out.dtype == torch.float32
+    act, stm = (y.dtype,), (h_out.dtype,)
+    if not f32 and h_out.dtype != y.dtype:
+        raise TypeError(f"block_norm: h_out is {h_out.dtype}")
+    for t, what in ((post_w, "post_w"), (pre_w, "pre_w")):
+        if t is not None and (t.dtype != y.dtype or t.numel() != N or not t.is_contiguous()):
+            raise ValueError(f"block_norm: {what} is [{N}] in the activation dtype")
+    n_gates, gate_ld = 0, 0
+    if gate is not None:
+        gate = gate.view(1, -1) if gate.dim() == 1 else gate
+        n_gates = gate.shape[0]
+        gate_ld = _rows(gate, n_gates, N, act, "gate")
+        if gate_ids is not None and (gate_ids.dtype != torch.int32 or gate_ids.numel() != M or
+                                     not gate_ids.is_contiguous()):
+            raise ValueError(f"block_norm: gate_ids is [{M}] int32")
+
+    def p(t):
+        return None if t is None else t.data_ptr()
+
+    a = BlockNorm(M, N, dt, STREAM_F32 if f32 else STREAM_ACT, p(y), p(post_w), p(gate),
+                  p(gate_ids), p(h), p(h_out), p(pre_w), p(x), _rows(y, M, N, act, "y"), gate_ld,
+                  _rows(h, M, N, stm, "h") if h is not None else 0, _rows(h_out, M, N, stm, "h_out"),
+                  _rows(x, M, N, act, "x") if x is not None else 0, n_gates,
+                  BLOCK_GATES[gate_kind], float(stream_scale), float(branch_scale),
+                  float(w_offset), float(eps))
+    st = LIB.spear_block_norm(ctypes.byref(a), _stream(stream))
+    if st != 0:
+        raise SpearError(st, "spear_block_norm")
+    return h_out
 
 
 def w4_dequant(prob: Problem, qweight, scales, zeros, w_out, stream=None):
