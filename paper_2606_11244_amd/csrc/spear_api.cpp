@@ -1225,13 +1225,55 @@ spear_status_t check_tail(const spear_problem_t* prob, const void* x, const spea
 // term d, the residual that its layer call adds.
 struct AdapterLayout {
   bool on = false;  // the member has tokens, rows and adapters
-  size_t u = 0, d = 0;
+  size_t upart = 0, uh = 0, ul = 0, us = 0, d = 0;
+  int ctr = 0, nctr = 0;  // first arrival counter, counters
+  AdapterParams p;        // the launch shape
 };
+
+constexpr int64_t kAdapterDecodeM = 64;  // tokens whose ids one wave holds, a lane each
+
+// The launch shape of one member, by its own sizes alone.
+void adapters_shape(const spear_problem_t* p, const spear_adapters_t* a, AdapterParams* q) {
+  const int IT = (int)(p->K / kIterK);
+  const int64_t M = p->M;
+  q->RG = (int)cdiv(a->rank, 32);
+  q->tile = M > kAdapterDecodeM;
+  if (!q->tile) {
+    // one workgroup of four waves for each token (those that lead no slot's
+    // tokens end at once), rank group and K-slice; K-slices of at least two
+    // passes of the waves while the leaders alone leave CUs idle
+    q->PA = 1;
+    int P = 1;
+    while (M * q->RG * P < 256 && IT / (2 * P) >= 8) P *= 2;
+    q->ips = (int)cdiv(IT, P);
+    q->P = (int)cdiv(IT, q->ips);
+    q->rpw = 1;
+    while (M * cdiv(p->N, 128 * q->rpw) > 1024 && q->rpw < 8) q->rpw *= 2;
+    q->chunks = (int)cdiv(p->N, 128 * q->rpw);
+    return;
+  }
+  const int64_t tiles = cdiv(M, 64);
+  int P = 1;
+  while (tiles * q->RG * P < 512 && IT / (2 * P) >= 4) P *= 2;
+  q->ips = (int)cdiv(IT, P);
+  q->P = (int)cdiv(IT, q->ips);
+  q->rpw = 1;
+  while (tiles * cdiv(p->N, 128 * q->rpw) > 2048 && q->rpw < 16) q->rpw *= 2;
+  q->chunks = (int)cdiv(p->N, 128 * q->rpw);
+  // few tiles: their slots, as many as their tokens at worst, are shared out
+  q->PA = 1;
+  while (q->PA < 16 && tiles * q->PA < 32) q->PA *= 2;
+  if (tiles * q->RG > kMaxEcCounters / SPEAR_GROUP_MAX) {  // (many tiles: no split)
+    q->P = 1;
+    q->ips = IT;
+  }
+}
 
 spear_status_t adapters_layout(int32_t n, const spear_layer_call_t* calls, const spear_adapters_t* const* ads,
                                AdapterLayout* al, size_t* total) {
   size_t off = std::max(*total, kDataBase);
   bool any = false;
+  int ctr = 0;
   for (int i = 0; i < n; ++i) {
     const spear_problem_t* p = calls[i].prob;
     const spear_adapters_t* a = ads[i];
@@ -1242,10 +1284,25 @@ spear_status_t adapters_layout(int32_t n, const spear_layer_call_t* calls, const
     al[i].on = p->M > 0 && p->N > 0 && a->n_adapters > 0 && a->rank > 0;
     if (!al[i].on) continue;
     any = true;
-    al[i].u = off;
-    off += round256((size_t)p->M * a->rank * 4);
-    al[i].d = off;
-    off += round256((size_t)p->M * p->N * 2);
+    std::memset(&al[i].p, 0, sizeof(al[i].p));
+    adapters_shape(p, a, &al[i].p);
+    const AdapterParams& q = al[i].p;
+    const size_t uw = (size_t)p->M * 32 * q.RG;
+    auto take = [&](size_t bytes) {
+      const size_t o = off;
+      off += round256(bytes);
+      return o;
+    };
+    al[i].upart = take(q.P > 1 ? (size_t)q.P * uw * 4 : 0);
+    al[i].uh = take(uw * 2);
+    al[i].ul = take(uw * 2);
+    al[i].us = take((size_t)p->M * q.RG * 4);
+    al[i].d = take((size_t)p->M * p->N * 2);
+    // (the EC projection's counters: its launches come later on the stream)
+    al[i].ctr = ctr;
+    al[i].nctr = q.P > 1 ? (int)(q.tile ? cdiv(p->M, 64) : p->M) * q.RG : 0;
+    ctr += al[i].nctr;
+    if (ctr > kMaxEcCounters) return SPEAR_E_SHAPE;  // (cannot happen: at most 1024 a member)
   }
   if (any) *total = off;
   return SPEAR_OK;
@@ -1292,6 +1349,7 @@ spear_status_t run_adapters(int32_t n, const spear_layer_call_t* calls, const sp
       if (!al[i].on || p->act_dtype != dt) continue;
       const spear_adapters_t* a = ads[i];
       AdapterParams& q = g.p[g.n++];
+      q = al[i].p;
       q.x = (const uint16_t*)calls[i].x;
       q.A = (const uint16_t*)a->A;
       q.B = (const uint16_t*)a->B;
@@ -1301,7 +1359,11 @@ spear_status_t run_adapters(int32_t n, const spear_layer_call_t* calls, const sp
       q.ranks = a->ranks;
       q.scale = a->scale;
       q.res = res[i];
-      q.u = (float*)(ws + al[i].u);
+      q.upart = (float*)(ws + al[i].upart);
+      q.ctr = (uint32_t*)(ws + kCtrEc) + al[i].ctr;
+      q.uh = (uint16_t*)(ws + al[i].uh);
+      q.ul = (uint16_t*)(ws + al[i].ul);
+      q.us = (float*)(ws + al[i].us);
       q.d = (uint16_t*)(ws + al[i].d);
       q.M = (int)p->M;
       q.N = (int)p->N;

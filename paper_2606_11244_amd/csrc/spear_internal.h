@@ -225,9 +225,21 @@ struct AdapterParams {
   const float* scale;     // [L] or null (all 1)
   const uint16_t* res;    // [M][N] residual, or null
   uint16_t* d;            // [M][N] the term plus the residual, act dtype
-  float* u;               // [M][R] scaled coordinates
+  // coordinates u = s_a A_a x, ranks padded to 32 RG: the K-slices' fp32 sums
+  // [P][M][32 RG] and their arrival counters (P > 1), the two act-dtype parts
+  // [M][32 RG], and per token and rank group the factor that undoes their
+  // scaling [M][RG] (fp16)
+  float* upart;
+  uint32_t* ctr;
+  uint16_t *uh, *ul;
+  float* us;
   int64_t a_stride, b_stride;
   int M, N, K, L, R;
+  int RG;                 // rank groups of 32
+  int tile;               // 0: decode (a leader's tokens), 1: 64 consecutive tokens
+  int P, ips;             // K-slices of u, iterations (128 K) per slice
+  int PA;                 // tile: parts that share a tile's slots
+  int chunks, rpw;        // row chunks of the term, row pairs (32 rows) a wave in each
 };
 struct AdapterGroup {
   AdapterParams p[kGroupMax];
@@ -309,7 +321,7 @@ __host__ __device__ inline size_t ec_block_lds(int NW, int R1p, int h, int r) {
   hipError_t launch_ec_up_acc_##D(const float* v, const uint16_t* B, const int8_t* B8,           \
                                   const float* sb, uint16_t* y, int M, int N, int r,             \
                                   hipStream_t st);                                               \
-  hipError_t launch_adapters_##D(AdapterGroup& g, hipStream_t st);                               \
+  hipError_t launch_adapters_##D(const AdapterGroup& g, hipStream_t st);                         \
   hipError_t launch_block_norm_##D(const BlockNormParams& p, hipStream_t st);                    \
   SPEAR_WEIGHT_LAUNCHERS(w4_##D)                                                                 \
   SPEAR_WEIGHT_LAUNCHERS(w3_##D)
