@@ -387,16 +387,19 @@ typedef struct {
  * what spear_group_workspace gives, then each member's adapter data. Of calls[i]
  * prob and whether ec is NULL are read, of adapters[i] (NULL: a member without
  * adapters) n_adapters and rank. Host-only. Errors as in spear_group_workspace,
- * and SPEAR_E_SHAPE for n_adapters < 0, rank outside 0..256 or a product of
- * rank with M, N or K of 2^30 elements or more. */
+ * and SPEAR_E_SHAPE for n_adapters < 0, rank outside 0..256, a product of rank
+ * with N or K of 2^30 elements or more, or of M with the rank rounded up to 32
+ * of 2^29 or more. */
 spear_status_t spear_adapters_workspace(int32_t n, const spear_layer_call_t* calls,
                                         const spear_adapters_t* const* adapters, size_t* out_bytes);
 
 /* spear_w4ec_linear (ec NULL: spear_w4_linear) with adapters, followed by the
  * post-EC tail if tail is not NULL. Y = the layer + the adapters' term + the
- * tail's residual: the term and the residual are summed in fp32, rounded once
- * to the act dtype and added to the layer's fp32 sums before Y's rounding. A
- * token without an adapter gets what the call without adapters writes, and no
+ * tail's residual, each summed in fp32, with one rounding to the act dtype
+ * before Y's own: of the term plus the residual, which the layer then adds to
+ * its sums, or (where the layer runs on 256 x 256 tiles) of the layer's sums,
+ * to which both are then added. A token without an adapter gets, but for that
+ * rounding of its residual, what the call without adapters writes, and no
  * token's result depends on another token's adapter or values. The workspace
  * follows the rules of the other calls and may be shared with them in stream
  * order. Errors as for spear_w4ec_linear_tail and spear_adapters_workspace,

@@ -1,6 +1,7 @@
 // gfx950 (MI355X) kernels of the low-rank adapters of many requests: the term
 //   d[m] = res[m] + s_a B_a (A_a x[m]),   a = ids[m] (d[m] = res[m] without one)
-// that the 4-bit product's final store adds in place of a residual.
+// that the 4-bit product's final store adds in place of a residual, or that is
+// added to its output.
 //
 // Two steps, the coordinates u[m] = s_a A_a x[m] (bound by reading x and the
 // slots' A) and the term B_a u[m] (bound by reading B and writing d). Both are
@@ -29,7 +30,7 @@ __device__ __forceinline__ int slot_of(const AdapterParams& p, int m) {
   const int a = p.ids[m];
   return a >= 0 && a < p.L ? a : -1;
 }
-__device__ __forceinline__ int rank_of(const AdapterParams& p, int a) {  // a uniform
+__device__ __forceinline__ int rank_of(const AdapterParams& p, int a) {
   if (a < 0) return 0;
   return p.ranks ? min(max(p.ranks[a], 0), p.R) : p.R;
 }
@@ -123,48 +124,85 @@ __device__ __forceinline__ int scale_exp(float maxabs) {  // k: the values times
 }
 __device__ __forceinline__ float exp2i(int k) { return __uint_as_float((uint32_t)(k + 127) << 23); }
 
-// u [cnt][32] of a rank group in LDS (row stride us) to parts at hi, lo (row
-// stride hs) and the scale of each token to undo at sc (stride ss); 32 lanes
-// per token. tok(t): where token t's row goes (negative: nowhere).
-template <int DT, class Row>
-__device__ __forceinline__ void store_parts(int cnt, const float* u, int us, uint16_t* hi, uint16_t* lo, int hs,
-                                            float* sc, int ss, Row row) {
-  for (int i = threadIdx.x; i < cnt * 32; i += blockDim.x) {  // (whole waves stay together: cnt * 32 in steps of 64 or a half wave)
-    const int t = i >> 5, j = i & 31;
-    float v = u[t * us + j];
-    const int m = row(t);
+// The parts of u for the term, in LDS: [T tokens][32 RG + 8] high, the same low,
+// [T][RG] scales.
+struct Parts {
+  uint16_t *hi, *lo;
+  float* sc;
+  int ld, RG;
+  __device__ __forceinline__ Parts(char* lds, int T, int RG_) : ld(32 * RG_ + 8), RG(RG_) {
+    hi = (uint16_t*)lds;
+    lo = hi + T * ld;
+    sc = (float*)(lo + T * ld);
+  }
+  // this lane's fragment of token t, rank group kk
+  __device__ __forceinline__ void get(int t, int kk, u32x4& h, u32x4& l, float& f) const {
+    const int o = t * ld + 32 * kk + 8 * ((threadIdx.x & 63) >> 4);
+    h = *(const u32x4*)(hi + o);
+    l = *(const u32x4*)(lo + o);
+    f = sc[t * RG + kk];
+  }
+};
+// Fills them for T tokens: val(t, j) gives u of token t, ranks j .. j + 4. Eight
+// threads hold a token's rank group. Ends with a barrier.
+template <int DT, class Val>
+__device__ __forceinline__ void build_parts(const Parts& o, int T, Val val) {
+  const int G = 8 * o.RG;  // threads a token
+  for (int i = threadIdx.x; i < T * G; i += blockDim.x) {  // (T G is a multiple of 64)
+    const int t = i / G, q = i - t * G;
+    f32x4 v = val(t, 4 * q);
     if constexpr (DT == DT_F16) {
-      float mx = __builtin_fabsf(v);
+      float mx = fmaxf(fmaxf(__builtin_fabsf(v[0]), __builtin_fabsf(v[1])), fmaxf(__builtin_fabsf(v[2]), __builtin_fabsf(v[3])));
 #pragma unroll
-      for (int h = 16; h > 0; h >>= 1) mx = fmaxf(mx, __shfl_xor(mx, h));
+      for (int h = 4; h > 0; h >>= 1) mx = fmaxf(mx, __shfl_xor(mx, h));
       const int k = scale_exp(mx);
       v *= exp2i(k);
-      if (j == 0 && m >= 0) sc[(size_t)m * ss] = exp2i(-k);
+      if ((q & 7) == 0) o.sc[t * o.RG + (q >> 3)] = exp2i(-k);
     }
-    uint16_t h, l;
-    split_parts<DT>(v, &h, &l);
-    if (m >= 0) {
-      hi[(size_t)m * hs + j] = h;
-      lo[(size_t)m * hs + j] = l;
-    }
+    uint16_t h[4], l[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) split_parts<DT>(v[e], &h[e], &l[e]);
+    const int at = t * o.ld + 4 * q;
+    *(u32x2*)(o.hi + at) = u32x2{h[0] | ((uint32_t)h[1] << 16), h[2] | ((uint32_t)h[3] << 16)};
+    *(u32x2*)(o.lo + at) = u32x2{l[0] | ((uint32_t)l[1] << 16), l[2] | ((uint32_t)l[3] << 16)};
   }
+  __syncthreads();
+}
+// u of token m, ranks j .. j + 4, from the K-slices' sums: scaled, zero from
+// rank r on (whose sums were never written)
+__device__ __forceinline__ f32x4 sum_u(const AdapterParams& p, int m, int j, int r, float scale) {
+  const int W = 32 * p.RG;
+  const rsrc_t ru = make_rsrc(p.upart, (uint32_t)p.P * p.M * W * 4);
+  f32x4 s = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int q0 = 0; q0 < p.P; q0 += 8) {
+    f32x4 w[8];
+#pragma unroll
+    for (int q = 0; q < 8; ++q)
+      w[q] = __builtin_bit_cast(f32x4, bld128(ru, q0 + q < p.P ? (uint32_t)(((q0 + q) * p.M + m) * W + j) * 4u : kOOB));
+#pragma unroll
+    for (int q = 0; q < 8; ++q) s += w[q];  // (slices past the last read as zero)
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) s[e] = j + e < r ? scale * s[e] : 0.f;
+  return s;
 }
 
 // ---------------------------------------------------------------------------
 // the term
 // ---------------------------------------------------------------------------
 
-// Row pair: 32 rows of B_a as two MFMA row tiles whose row q of tile t is row 8
-// (q / 4) + 4 t + q % 4, so that a lane's eight results are consecutive rows.
-// Its fragments of rank group kk; ranks from r on read as zero.
+// 64 rows of B_a from n0, rank group kk, as four MFMA row tiles: row q of tile
+// t is row 32 (t / 2) + 8 (q / 4) + 4 (t % 2) + q % 4, so that a lane's results
+// are two runs of eight consecutive rows. Ranks from r on are not used (of a
+// whole chunk of eight they are read and put to zero).
 template <int DT>
-__device__ __forceinline__ void load_pair(const AdapterParams& p, rsrc_t rb, int n0, int kk, int r, bool vec,
-                                          u32x4 (&bf)[2]) {
+__device__ __forceinline__ void load_rows(const AdapterParams& p, rsrc_t rb, int n0, int kk, int r, bool vec,
+                                          u32x4 (&bf)[4]) {
   const int lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4;
   const int j0 = 32 * kk + 8 * lg;
 #pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    const int n = n0 + 8 * (lr >> 2) + 4 * t + (lr & 3);
+  for (int t = 0; t < 4; ++t) {
+    const int n = n0 + 32 * (t >> 1) + 8 * (lr >> 2) + 4 * (t & 1) + (lr & 3);
     const uint32_t off = ((uint32_t)n * p.R + j0) * 2;
     if (vec) {
       bf[t] = bld128(rb, n < p.N && j0 < r ? off : kOOB);
@@ -178,72 +216,104 @@ __device__ __forceinline__ void load_pair(const AdapterParams& p, rsrc_t rb, int
     }
   }
 }
-// (the ranks past r of a whole chunk of eight, read with it: to zero)
-__device__ __forceinline__ void mask_pair(int kk, int r, u32x4 (&bf)[2]) {
+__device__ __forceinline__ void mask_rows(int kk, int r, u32x4 (&bf)[4]) {
   const int j0 = 32 * kk + 8 * ((threadIdx.x & 63) >> 4);
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
     const uint32_t keep = (j0 + 2 * q < r ? 0xFFFFu : 0u) | (j0 + 2 * q + 1 < r ? 0xFFFF0000u : 0u);
-    bf[0][q] &= keep;
-    bf[1][q] &= keep;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) bf[t][q] &= keep;
   }
 }
-
-// A lane's eight rows n .. n + 8 of token m: v plus the residual, rounded once.
+// v += the rank group's product with the parts of u at hi, lo (undone by sc)
 template <int DT>
-__device__ __forceinline__ void store_term(const AdapterParams& p, int m, int n, const f32x4 (&v)[2]) {
-  const size_t o = (size_t)m * p.N + n;
-  if ((p.N & 7) == 0) {
-    if (n >= p.N) return;
-    u32x4 rv = u32x4{0, 0, 0, 0}, w;
-    if (p.res) rv = ldg16(p.res + o);
+__device__ __forceinline__ void add_product(const u32x4 (&bf)[4], u32x4 hi, u32x4 lo, float sc, f32x4 (&v)[4]) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const float a = v[q >> 1][2 * (q & 1)] + act2f<DT>(rv[q] & 0xFFFFu);
-      const float b = v[q >> 1][2 * (q & 1) + 1] + act2f<DT>(rv[q] >> 16);
-      w[q] = (uint32_t)f2act<DT>(a) | ((uint32_t)f2act<DT>(b) << 16);
+  for (int t = 0; t < 4; ++t) {
+    if constexpr (DT == DT_F16) {
+      f32x4 q = f32x4{0.f, 0.f, 0.f, 0.f};
+      q = mfma16<DT>(bf[t], hi, q);
+      q = mfma16<DT>(bf[t], lo, q);
+      v[t] += sc * q;
+    } else {
+      v[t] = mfma16<DT>(bf[t], hi, v[t]);
+      v[t] = mfma16<DT>(bf[t], lo, v[t]);
     }
-    *(u32x4*)(p.d + o) = w;
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (n + e < p.N) p.d[o + e] = f2act<DT>(v[e >> 2][e & 3] + (p.res ? act2f<DT>(p.res[o + e]) : 0.f));
   }
 }
 
-// The rows [n0, n1) of the term for a group of up to 16 tokens of one slot, by
-// the workgroup; part(kk, hi, lo, sc): this lane's fragments of u (token lane %
-// 16, ranks 32 kk + 8 (lane / 16) .. +8) and its scale.
-template <int DT, class Part>
-__device__ __forceinline__ void expand_group(const AdapterParams& p, const TokenGroup& g, int n0, int n1, Part part) {
-  const int lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), NW = blockDim.x >> 6;
-  const rsrc_t rb = make_rsrc(p.B + (size_t)max(g.a, 0) * p.b_stride, (uint32_t)p.N * p.R * 2);
-  const int nkk = (g.r + 31) >> 5;
-  const bool vec = (p.R & 7) == 0 && (p.b_stride & 7) == 0;
-  const bool cut = vec && (g.r & 7) != 0;
-  for (int n = n0 + 32 * wave; n < n1; n += 32 * NW) {
-    f32x4 v[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
-    for (int kk = 0; kk < nkk; ++kk) {
-      u32x4 bf[2], hi, lo;
-      float sc = 1.f;
-      load_pair<DT>(p, rb, n, kk, g.r, vec, bf);
-      part(kk, hi, lo, sc);
-      if (cut) mask_pair(kk, g.r, bf);
+// What the term of a lane's token is added to, its rows n + 8 lg and n + 32 + 8
+// lg (eight each): the residual, and in place (p.add) what d holds.
+struct Base {
+  u32x4 res[2], old[2];
+};
+__device__ __forceinline__ void load_base(const AdapterParams& p, bool live, int m, int n, Base& b) {
+  const int lg = (threadIdx.x & 63) >> 4;
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        if constexpr (DT == DT_F16) {
-          f32x4 q = f32x4{0.f, 0.f, 0.f, 0.f};
-          q = mfma16<DT>(bf[t], hi, q);
-          q = mfma16<DT>(bf[t], lo, q);
-          v[t] += sc * q;
-        } else {
-          v[t] = mfma16<DT>(bf[t], hi, v[t]);
-          v[t] = mfma16<DT>(bf[t], lo, v[t]);
-        }
-      }
+  for (int h = 0; h < 2; ++h) {
+    const int nn = n + 32 * h + 8 * lg;
+    b.res[h] = b.old[h] = u32x4{0, 0, 0, 0};
+    if ((p.N & 7) == 0 && live && nn < p.N) {
+      if (p.res) b.res[h] = ldg16(p.res + (size_t)m * p.N + nn);
+      if (p.add) b.old[h] = ldg16(p.d + (size_t)m * p.N + nn);
     }
-    if (lr < g.cnt) store_term<DT>(p, g.tok, n + 8 * lg, v);
+  }
+}
+// d of those rows: one rounding of the sum
+template <int DT>
+__device__ __forceinline__ void store_term(const AdapterParams& p, bool live, int m, int n, const Base& b,
+                                           const f32x4 (&v)[4]) {
+  const int lg = (threadIdx.x & 63) >> 4;
+  if (!live) return;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int nn = n + 32 * h + 8 * lg;
+    if (nn >= p.N) continue;
+    const size_t o = (size_t)m * p.N + nn;
+    if ((p.N & 7) == 0) {
+      u32x4 w;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const f32x4& f = v[2 * h + (q >> 1)];
+        const float x = f[2 * (q & 1)] + act2f<DT>(b.res[h][q] & 0xFFFFu) + act2f<DT>(b.old[h][q] & 0xFFFFu);
+        const float y = f[2 * (q & 1) + 1] + act2f<DT>(b.res[h][q] >> 16) + act2f<DT>(b.old[h][q] >> 16);
+        w[q] = (uint32_t)f2act<DT>(x) | ((uint32_t)f2act<DT>(y) << 16);
+      }
+      *(u32x4*)(p.d + o) = w;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (nn + e < p.N)
+          p.d[o + e] = f2act<DT>(v[2 * h + (e >> 2)][e & 3] + (p.res ? act2f<DT>(p.res[o + e]) : 0.f) +
+                                 (p.add ? act2f<DT>(p.d[o + e]) : 0.f));
+    }
+  }
+}
+
+// Rows [n0, n1) of the term of up to 16 tokens of one slot (lane's token tok,
+// live), every `step` rows from n0; part(kk, hi, lo, sc): this lane's fragments
+// of u (ranks 32 kk + 8 (lane / 16) .. +8) and its scale.
+template <int DT, class Part>
+__device__ __forceinline__ void expand_slot(const AdapterParams& p, int a, int r, bool live, int tok, int n0, int n1,
+                                            int step, Part part) {
+  const rsrc_t rb = make_rsrc(p.B + (size_t)max(a, 0) * p.b_stride, (uint32_t)p.N * p.R * 2);
+  const int nkk = (r + 31) >> 5;
+  const bool vec = (p.R & 7) == 0 && (p.b_stride & 7) == 0;
+  for (int n = n0; n < n1; n += step) {
+    Base base;
+    f32x4 v[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) v[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    load_base(p, live, tok, n, base);
+    for (int kk = 0; kk < nkk; ++kk) {
+      u32x4 bf[4], hi, lo;
+      float sc = 1.f;
+      load_rows<DT>(p, rb, n, kk, r, vec, bf);
+      part(kk, hi, lo, sc);
+      if (vec && (r & 7)) mask_rows(kk, r, bf);
+      add_product<DT>(bf, hi, lo, sc, v);
+    }
+    store_term<DT>(p, live, tok, n, base, v);
   }
 }
 
@@ -252,9 +322,8 @@ __device__ __forceinline__ void expand_group(const AdapterParams& p, const Token
 // ---------------------------------------------------------------------------
 template <int DT>
 __device__ __forceinline__ void shrink_group(const AdapterParams& p, int b) {
-  __shared__ float red[4][2][256];
-  __shared__ float u[16][33];
-  __shared__ int stok[16], s_last;
+  __shared__ __attribute__((aligned(16))) float red[4][2][256];
+  __shared__ int stok[16];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int per = p.P * p.RG, m = b / per, rem = b - m * per, rg = rem / p.P, ks = rem - rg * p.P;
   const TokenGroup g = token_group(p, m, stok);
@@ -273,66 +342,49 @@ __device__ __forceinline__ void shrink_group(const AdapterParams& p, int b) {
 #pragma unroll
   for (int t = 0; t < 2; ++t) *(f32x4*)(red[wave][t] + 4 * lane) = acc[t];
   __syncthreads();
-  // lane l of a tile holds token l % 16, ranks 4 (l / 16) .. +4
-  const float sc = p.scale ? p.scale[g.a] : 1.f;
-  float* part = p.upart + (size_t)ks * p.M * (32 * p.RG);
-  for (int i = threadIdx.x; i < 512; i += 256) {
-    const int t = i >> 8, l = (i & 255) >> 2, e = i & 3, tok = l & 15, j = 16 * t + 4 * (l >> 4) + e;
-    float s = 0.f;
+  // lane l of a tile holds token l % 16, ranks 4 (l / 16) .. +4: thread (t, l)
+  // sums and stores those four
+  if (threadIdx.x < 128) {
+    const int t = threadIdx.x >> 6, tok = lane & 15, j = 32 * rg + 16 * t + 4 * (lane >> 4);
+    f32x4 s = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int w = 0; w < 4; ++w) s += red[w][t][4 * l + e];
-    s = 32 * rg + j < g.r ? s : 0.f;
-    if (p.P == 1) u[tok][j] = sc * s;
-    else if (tok < g.cnt) st_agent(part + (size_t)stok[tok] * (32 * p.RG) + 32 * rg + j, s);
+    for (int w = 0; w < 4; ++w) s += *(const f32x4*)(red[w][t] + 4 * lane);
+    if (tok < g.cnt) *(f32x4*)(p.upart + ((size_t)ks * p.M + stok[tok]) * (32 * p.RG) + j) = s;
   }
-  if (p.P > 1) {
-    complete_and_sync();
-    if (threadIdx.x == 0) s_last = arrive_last(p.ctr + m * p.RG + rg, (uint32_t)p.P) ? 1 : 0;
-    __syncthreads();
-    if (!s_last) return;
-    const int W = 32 * p.RG;
-    const rsrc_t rp = make_rsrc(p.upart, (uint32_t)p.P * p.M * W * 4);
-    sum_slices(rp, p.P, g.cnt * 32,
-               [&](int q, int i) { return (uint32_t)((q * p.M + stok[i >> 5]) * W + 32 * rg + (i & 31)) * 4u; },
-               [&](int i, float v) { u[i >> 5][i & 31] = sc * v; });
-  }
-  __syncthreads();
-  const int W = 32 * p.RG;
-  store_parts<DT>(g.cnt, &u[0][0], 33, p.uh + 32 * rg, p.ul + 32 * rg, W, p.us + rg, p.RG,
-                  [&](int t) { return stok[t]; });
 }
 
 // ---------------------------------------------------------------------------
 // beyond: 64 consecutive tokens
 // ---------------------------------------------------------------------------
 
-// The slots that the 64 tokens from m0 name, one after another: next() gives the
-// tokens of the next one this part owns (the i-th with i % PA == pa).
+// The slots that consecutive tokens name, one after another: each lane holds
+// one token's slot and rank (-1: none, and ranks of zero, count as none).
+// next() gives the tokens of the next slot, of those left in `left`.
 struct TileSlots {
-  int id;         // this lane's token's slot (-1: none, -2: no token)
-  uint64_t left;  // tokens of slots not yet given
-  int i, pa, PA;
-  __device__ __forceinline__ TileSlots(const AdapterParams& p, int m0, int pa_, int PA_) : i(0), pa(pa_), PA(PA_) {
-    const int m = m0 + (threadIdx.x & 63);
-    id = m < p.M ? slot_of(p, m) : -2;
-    left = __ballot(id >= 0);
-  }
-  __device__ __forceinline__ bool next(int* a, uint64_t* toks) {
-    while (left) {
-      *a = __builtin_amdgcn_readlane(id, __builtin_ctzll(left));
-      *toks = __ballot(id == *a);
-      left &= ~*toks;
-      if (i++ % PA == pa) return true;
-    }
-    return false;
+  int id, rank;
+  uint64_t left;
+  __device__ __forceinline__ bool next(int* a, int* r, uint64_t* toks) {
+    if (!left) return false;
+    const int l = __builtin_ctzll(left);
+    *a = __builtin_amdgcn_readlane(id, l);
+    *r = __builtin_amdgcn_readlane(rank, l);
+    *toks = __ballot(id == *a) & left;
+    left &= ~*toks;
+    return true;
   }
 };
+__device__ __forceinline__ TileSlots tile_slots(const AdapterParams& p, int m0) {
+  TileSlots t;
+  const int m = m0 + (threadIdx.x & 63);
+  t.id = m < p.M ? slot_of(p, m) : -1;
+  t.rank = rank_of(p, t.id);
+  t.left = __ballot(t.rank > 0);
+  return t;
+}
 
 template <int DT>
 __device__ __forceinline__ void shrink_tile(const AdapterParams& p, int b) {
-  __shared__ float red[4][2][4][256];
-  __shared__ float u[64][33];
-  __shared__ int s_last;
+  __shared__ __attribute__((aligned(16))) float red[4][2][4][256];
   const int lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int per = p.P * p.RG * p.PA, tb = b / per;
@@ -340,16 +392,27 @@ __device__ __forceinline__ void shrink_tile(const AdapterParams& p, int b) {
   const int rg = rem / (p.P * p.PA);
   rem -= rg * p.P * p.PA;
   const int ks = rem / p.PA, pa = rem - ks * p.PA;
-  const int m0 = 64 * tb, cnt = min(64, p.M - m0), W = 32 * p.RG;
+  const int m0 = 64 * tb, W = 32 * p.RG;
   const rsrc_t rx = make_rsrc(p.x, (uint32_t)p.M * p.K * 2);
   const int it_beg = ks * p.ips, it_end = min(p.K / kIterK, it_beg + p.ips);
+  TileSlots slots = tile_slots(p, m0);
+  // this part's slots: the i-th with i % PA == pa, of those that reach the rank group
+  uint64_t owned = slots.left;
+  if (p.PA > 1) {
+    TileSlots t = slots;
+    owned = 0;
+    int a, r;
+    uint64_t toks;
+    for (int i = 0; t.next(&a, &r, &toks); ++i)
+      if (i % p.PA == pa) owned |= toks;
+  }
+  owned &= __ballot(slots.rank > 32 * rg);
+  if (!owned) return;
   f32x4 acc[2][4];
 #pragma unroll
   for (int t = 0; t < 2; ++t)
 #pragma unroll
     for (int s = 0; s < 4; ++s) acc[t][s] = f32x4{0.f, 0.f, 0.f, 0.f};
-  uint64_t owned = 0;  // tokens of this part's slots
-  const TileSlots slots0(p, m0, pa, p.PA);
   uint32_t xoff[4];
 #pragma unroll
   for (int s = 0; s < 4; ++s) xoff[s] = (uint32_t)min(m0 + 16 * s + lr, p.M - 1) * p.K * 2 + 16 * lg;
@@ -360,12 +423,12 @@ __device__ __forceinline__ void shrink_tile(const AdapterParams& p, int b) {
     for (int s = 0; s < 4; ++s)
 #pragma unroll
       for (int jj = 0; jj < 4; ++jj) xv[s][jj] = bld128(rx, xoff[s] + kb + 64 * jj);
-    TileSlots slots = slots0;
-    int a;
+    TileSlots t0 = slots;
+    t0.left = owned;
+    int a, r;
     uint64_t toks;
-    while (slots.next(&a, &toks)) {
-      const int r = rank_of(p, a) - 32 * rg;  // ranks of this group
-      if (r <= 0) continue;
+    while (t0.next(&a, &r, &toks)) {
+      r -= 32 * rg;
       const rsrc_t ra = make_rsrc(p.A + (size_t)a * p.a_stride, (uint32_t)p.R * p.K * 2);
       u32x4 av[2][4];
 #pragma unroll
@@ -380,6 +443,7 @@ __device__ __forceinline__ void shrink_tile(const AdapterParams& p, int b) {
         const bool in = (st >> lr) & 1;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
+          if (16 * t >= r) continue;  // uniform
           f32x4 q = acc[t][s];
 #pragma unroll
           for (int jj = 0; jj < 4; ++jj) q = mfma16<DT>(av[t][jj], xv[s][jj], q);
@@ -389,143 +453,202 @@ __device__ __forceinline__ void shrink_tile(const AdapterParams& p, int b) {
       }
     }
   }
-  {
-    TileSlots slots = slots0;
-    int a;
-    uint64_t toks;
-    while (slots.next(&a, &toks)) owned |= toks;
-  }
 #pragma unroll
   for (int t = 0; t < 2; ++t)
 #pragma unroll
     for (int s = 0; s < 4; ++s) *(f32x4*)(red[wave][t][s] + 4 * lane) = acc[t][s];
   __syncthreads();
-  const auto scale_of = [&](int tok) {
-    const int a = slot_of(p, m0 + tok);
-    return p.scale && a >= 0 ? p.scale[a] : 1.f;
-  };
-  for (int i = threadIdx.x; i < 2048; i += 256) {
-    const int ts = i >> 8, t = ts >> 2, s = ts & 3, l = (i & 255) >> 2, e = i & 3;
-    const int tok = 16 * s + (l & 15), j = 16 * t + 4 * (l >> 4) + e;
-    if (!((owned >> tok) & 1)) continue;
-    float v = 0.f;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) v += red[w][t][s][4 * l + e];
-    // (ranks past the slot's: zero even where the token holds an infinity)
-    if (32 * rg + j >= rank_of(p, slot_of(p, m0 + tok))) v = 0.f;
-    if (p.P == 1) u[tok][j] = scale_of(tok) * v;
-    else st_agent(p.upart + ((size_t)ks * p.M + m0 + tok) * W + 32 * rg + j, v);
+  for (int i = 0; i < 2; ++i) {  // eight tiles of results, 64 threads each
+    const int ts = 4 * i + wave, t = ts >> 2, s = ts & 3, tok = 16 * s + lr;
+    f32x4 v = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < 4; ++w) v += *(const f32x4*)(red[w][t][s] + 4 * lane);
+    if ((owned >> tok) & 1)
+      *(f32x4*)(p.upart + ((size_t)ks * p.M + m0 + tok) * W + 32 * rg + 16 * t + 4 * lg) = v;
   }
-  if (p.P > 1) {
-    complete_and_sync();
-    if (threadIdx.x == 0) s_last = arrive_last(p.ctr + tb * p.RG + rg, (uint32_t)(p.P * p.PA)) ? 1 : 0;
-    __syncthreads();
-    if (!s_last) return;
-    // (tokens without a slot: whatever lies there, never used)
-    const rsrc_t rp = make_rsrc(p.upart, (uint32_t)p.P * p.M * W * 4);
-    sum_slices(rp, p.P, cnt * 32,
-               [&](int q, int i) { return (uint32_t)((q * p.M + m0 + (i >> 5)) * W + 32 * rg + (i & 31)) * 4u; },
-               [&](int i, float v) { u[i >> 5][i & 31] = scale_of(i >> 5) * v; });
-    owned = ~0ull;
-  }
-  __syncthreads();
-  store_parts<DT>(cnt, &u[0][0], 33, p.uh + 32 * rg, p.ul + 32 * rg, W, p.us + rg, p.RG,
-                  [&](int t) { return (owned >> t) & 1 ? m0 + t : -1; });
 }
 
-// The term of 64 tokens and 32 rpw rows a wave, part pa of PA (the tokens
-// without a slot belong to part 0). NKK: rank groups whose parts of u stay in
-// registers (0: read again for each slot and row pair).
-template <int DT, int NKK>
-__device__ __forceinline__ void expand_tile(const AdapterParams& p, int b) {
-  const int lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4;
+// The term of 64 tokens, 16 a wave (the waves walk the same rows, so that B
+// comes from memory once for the four), over 64 rpw rows. A wave walks (64
+// rows, slot, rank group) with the fragments of B one item ahead.
+template <int DT>
+__device__ __forceinline__ void expand_tile(const AdapterParams& p, int b, char* smem) {
+  const int lane = threadIdx.x & 63, lr = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int per = p.chunks * p.PA, tb = b / per, rem = b - tb * per, chunk = rem / p.PA, pa = rem - chunk * p.PA;
-  const int m0 = 64 * tb, W = 32 * p.RG;
-  const TileSlots slots0(p, m0, pa, p.PA);
-  const bool vec = (p.R & 7) == 0 && (p.b_stride & 7) == 0;
-  uint64_t owned = pa == 0 ? __ballot(slots0.id == -1) : 0;
+  const int tb = b / p.chunks, chunk = b - tb * p.chunks;
+  const int m0 = 64 * tb + 16 * wave;
+  const Parts parts(smem, 64, p.RG);
+  build_parts<DT>(parts, 64, [&](int t, int j) {
+    const int m = 64 * tb + t, mm = min(m, p.M - 1), a = m < p.M ? slot_of(p, mm) : -1;
+    return sum_u(p, mm, j, rank_of(p, a), p.scale && a >= 0 ? p.scale[a] : 1.f);
+  });
+  if (m0 >= p.M) return;
+  TileSlots all;
   {
-    TileSlots slots = slots0;
-    int a;
-    uint64_t toks;
-    while (slots.next(&a, &toks)) owned |= toks;
+    const int m = m0 + lr;  // (four lanes a token; lanes 0 to 15 count)
+    all.id = m < p.M ? slot_of(p, m) : -1;
+    all.rank = rank_of(p, all.id);
+    all.left = __ballot(all.rank > 0) & 0xFFFFu;
   }
-  if (!owned) return;
-  auto part = [&](int s, int kk, u32x4& hi, u32x4& lo, float& sc) {
-    const size_t m = (size_t)min(m0 + 16 * s + lr, p.M - 1);
-    hi = ldg16(p.uh + m * W + 32 * kk + 8 * lg);
-    lo = ldg16(p.ul + m * W + 32 * kk + 8 * lg);
-    sc = DT == DT_F16 ? p.us[m * p.RG + kk] : 1.f;
+  const int m = min(m0 + lr, p.M - 1);
+  // in place with no residual, only the tokens of a slot change
+  const bool live = m0 + lr < p.M && (!p.add || p.res || all.rank > 0);
+  if (p.add && !p.res && !all.left) return;
+  const bool vec = (p.R & 7) == 0 && (p.b_stride & 7) == 0;
+  const int n_beg = chunk * 64 * p.rpw, n_end = min(p.N, n_beg + 64 * p.rpw);
+
+  struct Item {
+    int n, a, r, kk;
+    uint32_t toks;
   };
-  constexpr int H = NKK > 0 ? NKK : 1;
-  u32x4 hi[H][4], lo[H][4];
-  float sc[H][4];
-  if constexpr (NKK > 0) {
+  TileSlots left = all;
+  auto first_slot = [&](Item& t) {
+    left.left = all.left;
+    uint64_t m64 = 0;
+    t.kk = 0;
+    t.r = 0;
+    t.a = 0;
+    left.next(&t.a, &t.r, &m64);
+    t.toks = (uint32_t)m64;
+  };
+  auto advance = [&](Item& t) {
+    if (32 * (t.kk + 1) < t.r) {
+      ++t.kk;
+      return;
+    }
+    uint64_t m64 = 0;
+    if (left.next(&t.a, &t.r, &m64)) {
+      t.toks = (uint32_t)m64;
+      t.kk = 0;
+      return;
+    }
+    t.n += 64;
+    first_slot(t);
+  };
+  auto load = [&](const Item& t, u32x4 (&bf)[4]) {
+    const rsrc_t rb = make_rsrc(p.B + (size_t)t.a * p.b_stride, t.r > 0 ? (uint32_t)p.N * p.R * 2 : 0u);
+    load_rows<DT>(p, rb, t.n, t.kk, t.r, vec, bf);
+  };
+  Item cur;
+  cur.n = n_beg;
+  first_slot(cur);
+  u32x4 bf[4], nx[4];
+  load(cur, bf);
+  f32x4 acc[4], v[4];
+  Base base;
 #pragma unroll
-    for (int kk = 0; kk < H; ++kk)
+  for (int t = 0; t < 4; ++t) acc[t] = v[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  load_base(p, live, m, cur.n, base);
+  while (cur.n < n_end) {
+    Item nxt = cur;
+    advance(nxt);
+    if (nxt.n < n_end) load(nxt, nx);
+    if (cur.r > 0) {
+      if (vec && (cur.r & 7)) mask_rows(cur.kk, cur.r, bf);
+      u32x4 hi, lo;
+      float sc;
+      parts.get(16 * wave + lr, cur.kk, hi, lo, sc);
+      add_product<DT>(bf, hi, lo, sc, v);
+    }
+    if (nxt.kk == 0) {  // the slot's last rank group
+      const bool in = (cur.toks >> lr) & 1;
 #pragma unroll
-      for (int s = 0; s < 4; ++s)
-        if (kk < p.RG) part(s, kk, hi[kk][s], lo[kk][s], sc[kk][s]);
-  }
-  const int rows = 128 * p.rpw;
-  for (int n = chunk * rows + 32 * wave; n < min(p.N, (chunk + 1) * rows); n += 128) {
-    f32x4 acc[4][2];
+      for (int t = 0; t < 4; ++t) {
 #pragma unroll
-    for (int s = 0; s < 4; ++s) acc[s][0] = acc[s][1] = f32x4{0.f, 0.f, 0.f, 0.f};
-    TileSlots slots = slots0;
-    int a;
-    uint64_t toks;
-    while (slots.next(&a, &toks)) {
-      const int r = rank_of(p, a), nkk = (r + 31) >> 5;
-      const rsrc_t rb = make_rsrc(p.B + (size_t)a * p.b_stride, (uint32_t)p.N * p.R * 2);
-      f32x4 v[4][2];
-#pragma unroll
-      for (int s = 0; s < 4; ++s) v[s][0] = v[s][1] = f32x4{0.f, 0.f, 0.f, 0.f};
-      auto group = [&](int kk, const u32x4 (&h)[4], const u32x4 (&l)[4], const float (&c)[4]) {
-        u32x4 bf[2];
-        load_pair<DT>(p, rb, n, kk, r, vec, bf);
-        if (vec && (r & 7)) mask_pair(kk, r, bf);
-#pragma unroll
-        for (int s = 0; s < 4; ++s) {
-          if (((toks >> (16 * s)) & 0xFFFFu) == 0) continue;  // uniform
-#pragma unroll
-          for (int t = 0; t < 2; ++t) {
-            if constexpr (DT == DT_F16) {
-              f32x4 q = f32x4{0.f, 0.f, 0.f, 0.f};
-              q = mfma16<DT>(bf[t], h[s], q);
-              q = mfma16<DT>(bf[t], l[s], q);
-              v[s][t] += c[s] * q;
-            } else {
-              v[s][t] = mfma16<DT>(bf[t], h[s], v[s][t]);
-              v[s][t] = mfma16<DT>(bf[t], l[s], v[s][t]);
-            }
-          }
-        }
-      };
-      if constexpr (NKK > 0) {
-#pragma unroll
-        for (int kk = 0; kk < H; ++kk)
-          if (kk < nkk) group(kk, hi[kk], lo[kk], sc[kk]);
-      } else {
-        for (int kk = 0; kk < nkk; ++kk) {
-#pragma unroll
-          for (int s = 0; s < 4; ++s) part(s, kk, hi[0][s], lo[0][s], sc[0][s]);
-          group(kk, hi[0], lo[0], sc[0]);
-        }
-      }
-#pragma unroll
-      for (int s = 0; s < 4; ++s) {
-        const bool in = (toks >> (16 * s + lr)) & 1;
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) acc[s][t][e] = in ? v[s][t][e] : acc[s][t][e];
+        for (int e = 0; e < 4; ++e) acc[t][e] = in ? v[t][e] : acc[t][e];
+        v[t] = f32x4{0.f, 0.f, 0.f, 0.f};
       }
     }
+    if (nxt.n != cur.n) {
+      store_term<DT>(p, live, m, cur.n, base, acc);
 #pragma unroll
-    for (int s = 0; s < 4; ++s)
-      if ((owned >> (16 * s + lr)) & 1) store_term<DT>(p, m0 + 16 * s + lr, n + 8 * lg, acc[s]);
+      for (int t = 0; t < 4; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (nxt.n < n_end) load_base(p, live, m, nxt.n, base);
+    }
+    cur = nxt;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) bf[t] = nx[t];
+  }
+}
+
+// ---------------------------------------------------------------------------
+// decode, slots of few ranks: u and the term in one launch
+// ---------------------------------------------------------------------------
+
+// Every workgroup of a leader forms u over all of K (eight waves, K shared out)
+// and then its own rows of the term: A is read once per row chunk, from L2
+// after the first, in place of a second launch and the slices' round trip. The
+// chain of dependent accesses is ids, then the slot's A, B, rank and scale all
+// together (rows and columns past the slot's rank are read and dropped).
+template <int DT>
+__device__ __forceinline__ void adapt_local(const AdapterParams& p, int b, char* smem) {
+  __shared__ __attribute__((aligned(16))) float red[8][2][256];
+  __shared__ __attribute__((aligned(16))) float u[16][kAdapterLocalR + 4];
+  __shared__ int stok[16];
+  const int lane = threadIdx.x & 63, lr = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int m = b / p.chunks, chunk = b - m * p.chunks;
+  const TokenGroup g = token_group(p, m, stok);
+  if (g.cnt == 0) return;
+  const int a = max(g.a, 0), n0 = chunk * 512 * p.rpw, n1 = min(p.N, n0 + 512 * p.rpw), n = n0 + 64 * wave;
+  const bool live = lr < g.cnt, vec = (p.R & 7) == 0 && (p.b_stride & 7) == 0;
+  const rsrc_t rx = make_rsrc(p.x, (uint32_t)p.M * p.K * 2);
+  const rsrc_t ra = make_rsrc(p.A + (size_t)a * p.a_stride, (uint32_t)p.R * p.K * 2);
+  const rsrc_t rb = make_rsrc(p.B + (size_t)a * p.b_stride, (uint32_t)p.N * p.R * 2);
+  const int r = rank_of(p, g.a);
+  const float sc = p.scale ? p.scale[a] : 1.f;
+  const int IT = p.K / kIterK;
+  u32x4 bf[4];
+  Base base;
+  load_rows<DT>(p, rb, n, 0, p.R, vec, bf);
+  load_base(p, live, g.tok, n, base);
+  const int top = g.a < 0 ? 0 : p.R;  // no rank in the addresses: nothing waits for it
+  for (int j0 = 0; j0 < top; j0 += 32) {
+    f32x4 acc[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+    if (top - j0 > 16) {
+      project<DT, 2>(rx, (uint32_t)g.tok * p.K * 2, ra, p.K, j0, top, 0, IT, wave, 8, acc);
+    } else {
+      f32x4 a1[1] = {acc[0]};
+      project<DT, 1>(rx, (uint32_t)g.tok * p.K * 2, ra, p.K, j0, top, 0, IT, wave, 8, a1);
+      acc[0] = a1[0];
+    }
+    if (j0 > 0) __syncthreads();
+#pragma unroll
+    for (int t = 0; t < 2; ++t) *(f32x4*)(red[wave][t] + 4 * lane) = acc[t];
+    __syncthreads();
+    // thread (t, l) sums one token's four ranks over half of the waves
+    const int t = (threadIdx.x >> 6) & 1, half = threadIdx.x >> 7;
+    if (half < 1) {
+      f32x4 s = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < 8; ++w) s += *(const f32x4*)(red[w][t] + 4 * lane);
+      const int j = j0 + 16 * t + 4 * (lane >> 4);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[e] = j + e < r ? sc * s[e] : 0.f;
+      *(f32x4*)&u[lr][j] = s;
+    }
+  }
+  const Parts parts(smem, 16, p.RG);
+  if (r > 0) {  // uniform
+    __syncthreads();
+    build_parts<DT>(parts, 16, [&](int t, int j) { return *(const f32x4*)&u[t][j]; });
+  }
+  const int nkk = (r + 31) >> 5;
+  for (int nn = n; nn < n1; nn += 512) {
+    f32x4 v[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) v[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (nn != n) load_base(p, live, g.tok, nn, base);
+    for (int kk = 0; kk < nkk; ++kk) {
+      if (nn != n || kk > 0) load_rows<DT>(p, rb, nn, kk, p.R, vec, bf);
+      u32x4 hi, lo;
+      float f;
+      parts.get(lr, kk, hi, lo, f);
+      if (r < 32 * kk + 32) mask_rows(kk, r, bf);
+      add_product<DT>(bf, hi, lo, f, v);
+    }
+    store_term<DT>(p, live, g.tok, nn, base, v);
   }
 }
 
@@ -540,70 +663,98 @@ __device__ __forceinline__ int member(const int (&start)[kGroupMax + 1], int n, 
   return i;
 }
 
-template <int DT, bool TILE>
-__global__ __launch_bounds__(256) void k_adapter_shrink(AdapterGroup g) {
-  const int i = member(g.shrink_start, g.n, blockIdx.x), b = blockIdx.x - g.shrink_start[i];
-  if constexpr (TILE) shrink_tile<DT>(g.p[i], b);
-  else shrink_group<DT>(g.p[i], b);
+// (a single member's call passes its parameters alone: the table's lookup is a
+// dependent load ahead of everything else)
+template <int DT, int KIND>
+__device__ __forceinline__ void shrink_body(const AdapterParams& p, int b) {
+  if constexpr (KIND == ADAPT_TILES) shrink_tile<DT>(p, b);
+  else shrink_group<DT>(p, b);
 }
-
-template <int DT, int NKK>
-__global__ __launch_bounds__(256) void k_adapter_expand_tile(AdapterGroup g) {
+template <int DT, int KIND>
+__device__ __forceinline__ void expand_body(const AdapterParams& p, int b, char* smem) {
+  if constexpr (KIND == ADAPT_LOCAL) {
+    adapt_local<DT>(p, b, smem);
+  } else if constexpr (KIND == ADAPT_TILES) {
+    expand_tile<DT>(p, b, smem);
+  } else {
+    __shared__ int stok[16];
+    const int m = b / p.chunks, chunk = b - m * p.chunks;
+    TokenGroup t = token_group(p, m, stok);
+    if (t.cnt == 0) return;
+    const Parts parts(smem, 16, p.RG);
+    if (t.r > 0) {
+      const float sc = p.scale ? p.scale[t.a] : 1.f;
+      build_parts<DT>(parts, 16, [&](int i, int j) { return sum_u(p, stok[min(i, t.cnt - 1)], j, t.r, sc); });
+    }
+    const int lane = threadIdx.x & 63, rows = 256 * p.rpw, n0 = chunk * rows;
+    expand_slot<DT>(p, t.a, t.r, (lane & 15) < t.cnt, t.tok, n0 + 64 * (threadIdx.x >> 6), min(p.N, n0 + rows), 256,
+                    [&](int kk, u32x4& hi, u32x4& lo, float& sc) { parts.get(lane & 15, kk, hi, lo, sc); });
+  }
+}
+template <int DT, int KIND>
+__global__ __launch_bounds__(256) void k_adapter_shrink(AdapterParams p) {
+  shrink_body<DT, KIND>(p, blockIdx.x);
+}
+template <int DT, int KIND>
+__global__ __launch_bounds__(256) void k_adapter_shrink_group(AdapterGroup g) {
+  const int i = member(g.shrink_start, g.n, blockIdx.x);
+  shrink_body<DT, KIND>(g.p[i], blockIdx.x - g.shrink_start[i]);
+}
+template <int DT, int KIND>
+__global__ __launch_bounds__(KIND == ADAPT_LOCAL ? 512 : 256) void k_adapter_expand(AdapterParams p) {
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  expand_body<DT, KIND>(p, blockIdx.x, smem);
+}
+template <int DT, int KIND>
+__global__ __launch_bounds__(KIND == ADAPT_LOCAL ? 512 : 256) void k_adapter_expand_group(AdapterGroup g) {
+  extern __shared__ __attribute__((aligned(16))) char smem[];
   const int i = member(g.expand_start, g.n, blockIdx.x);
-  expand_tile<DT, NKK>(g.p[i], blockIdx.x - g.expand_start[i]);
-}
-
-template <int DT>
-__global__ __launch_bounds__(256) void k_adapter_expand(AdapterGroup g) {
-  __shared__ int stok[16];
-  const int i = member(g.expand_start, g.n, blockIdx.x), b = blockIdx.x - g.expand_start[i];
-  const AdapterParams& p = g.p[i];
-  const int m = b / p.chunks, chunk = b - m * p.chunks;
-  const TokenGroup t = token_group(p, m, stok);
-  if (t.cnt == 0) return;
-  const int lg = (threadIdx.x & 63) >> 4, W = 32 * p.RG, rows = 128 * p.rpw;
-  expand_group<DT>(p, t, chunk * rows, min(p.N, (chunk + 1) * rows), [&](int kk, u32x4& hi, u32x4& lo, float& sc) {
-    hi = ldg16(p.uh + (size_t)t.tok * W + 32 * kk + 8 * lg);
-    lo = ldg16(p.ul + (size_t)t.tok * W + 32 * kk + 8 * lg);
-    sc = DT == DT_F16 ? p.us[(size_t)t.tok * p.RG + kk] : 1.f;
-  });
+  expand_body<DT, KIND>(g.p[i], blockIdx.x - g.expand_start[i], smem);
 }
 
 // ---------------------------------------------------------------------------
 // launcher
 // ---------------------------------------------------------------------------
-hipError_t SPEAR_D(launch_adapters)(const AdapterGroup& all, hipStream_t st) {
-  // members of the decode kind and of the other kind in launches of their own
-  for (int tile = 0; tile < 2; ++tile) {
-    AdapterGroup g;
-    g.n = 0;
-    g.shrink_start[0] = g.expand_start[0] = 0;
-    int rg = 0;
-    for (int i = 0; i < all.n; ++i) {
-      const AdapterParams& p = all.p[i];
-      if (p.tile != tile) continue;
-      const int units = tile ? (p.M + 63) / 64 * p.PA : p.M;
-      g.p[g.n] = p;
-      g.shrink_start[g.n + 1] = g.shrink_start[g.n] + units * p.P * p.RG;
-      g.expand_start[g.n + 1] = g.expand_start[g.n] + units * p.chunks;
-      rg = std::max(rg, p.RG);
-      ++g.n;
-    }
-    if (g.n == 0) continue;
-    const auto go = [&](auto kern, int grid) {
-      hipLaunchKernelGGL(kern, dim3(grid), dim3(256), 0, st, g);
-      return hipGetLastError();
-    };
-    const int gs = g.shrink_start[g.n], ge = g.expand_start[g.n];
-    hipError_t err = tile ? go(k_adapter_shrink<DTC, true>, gs) : go(k_adapter_shrink<DTC, false>, gs);
+template <int KIND>
+static hipError_t launch_kind(const AdapterGroup& all, hipStream_t st) {
+  AdapterGroup g;
+  g.n = 0;
+  g.shrink_start[0] = g.expand_start[0] = 0;
+  size_t lds = 0;
+  for (int i = 0; i < all.n; ++i) {
+    const AdapterParams& p = all.p[i];
+    if (p.kind != KIND) continue;
+    const int units = KIND == ADAPT_TILES ? (p.M + 63) / 64 : p.M, T = KIND == ADAPT_TILES ? 64 : 16;
+    g.p[g.n] = p;
+    g.shrink_start[g.n + 1] = g.shrink_start[g.n] + units * p.PA * p.P * p.RG;
+    g.expand_start[g.n + 1] = g.expand_start[g.n] + units * p.chunks;
+    lds = std::max(lds, (size_t)T * ((32 * p.RG + 8) * 4 + p.RG * 4));
+    ++g.n;
+  }
+  if (g.n == 0) return hipSuccess;
+  const auto go = [&](auto kern, const auto& p, int grid, int block, size_t bytes) {
+    hipError_t err = allow_lds(kern, bytes);
     if (err != hipSuccess) return err;
-    if (!tile) err = go(k_adapter_expand<DTC>, ge);
-    else if (rg == 1) err = go(k_adapter_expand_tile<DTC, 1>, ge);
-    else if (rg == 2) err = go(k_adapter_expand_tile<DTC, 2>, ge);
-    else err = go(k_adapter_expand_tile<DTC, 0>, ge);
+    hipLaunchKernelGGL(kern, dim3(grid), dim3(block), bytes, st, p);
+    return hipGetLastError();
+  };
+  const int gs = g.shrink_start[g.n], ge = g.expand_start[g.n];
+  if constexpr (KIND != ADAPT_LOCAL) {
+    const hipError_t err = g.n == 1 ? go(k_adapter_shrink<DTC, KIND>, g.p[0], gs, 256, 0)
+                                    : go(k_adapter_shrink_group<DTC, KIND>, g, gs, 256, 0);
     if (err != hipSuccess) return err;
   }
-  return hipSuccess;
+  constexpr int block = KIND == ADAPT_LOCAL ? 512 : 256;
+  return g.n == 1 ? go(k_adapter_expand<DTC, KIND>, g.p[0], ge, block, lds)
+                  : go(k_adapter_expand_group<DTC, KIND>, g, ge, block, lds);
+}
+
+hipError_t SPEAR_D(launch_adapters)(const AdapterGroup& all, hipStream_t st) {
+  // members of one kind share its launches
+  hipError_t err = launch_kind<ADAPT_LOCAL>(all, st);
+  if (err == hipSuccess) err = launch_kind<ADAPT_SLOTS>(all, st);
+  if (err == hipSuccess) err = launch_kind<ADAPT_TILES>(all, st);
+  return err;
 }
 
 }  // namespace spear

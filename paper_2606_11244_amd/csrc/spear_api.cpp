@@ -1221,88 +1221,89 @@ spear_status_t check_tail(const spear_problem_t* prob, const void* x, const spea
 
 // ---- adapters ---------------------------------------------------------------
 
-// The adapter data of one member in the workspace: its coordinates u and its
-// term d, the residual that its layer call adds.
+// The adapter data of one member in the workspace: the K-slices of its
+// coordinates and its term d, the residual that its layer call adds. `post`: the
+// term is added to the layer's output instead, in place. That is where the
+// layer runs k_gemm_ws on 256 x 256 tiles, whose epilogue with a residual costs
+// more than another pass over the output (8B gate, 14336 x 4096 at 2048 tokens,
+// fp16: 282 us with one, 240 without; the pass reads and writes 117 MB).
 struct AdapterLayout {
   bool on = false;  // the member has tokens, rows and adapters
-  size_t upart = 0, uh = 0, ul = 0, us = 0, d = 0;
-  int ctr = 0, nctr = 0;  // first arrival counter, counters
+  bool post = false;
+  size_t upart = 0, d = 0;
   AdapterParams p;        // the launch shape
 };
 
 constexpr int64_t kAdapterDecodeM = 64;  // tokens whose ids one wave holds, a lane each
+constexpr int64_t kAdapterLocalA = 512 << 10;   // ADAPT_LOCAL: bytes of a slot's A
+constexpr int64_t kAdapterRestage = 64 << 20;   // and of A over all workgroups
 
 // The launch shape of one member, by its own sizes alone.
 void adapters_shape(const spear_problem_t* p, const spear_adapters_t* a, AdapterParams* q) {
   const int IT = (int)(p->K / kIterK);
   const int64_t M = p->M;
   q->RG = (int)cdiv(a->rank, 32);
-  q->tile = M > kAdapterDecodeM;
-  if (!q->tile) {
+  q->P = q->PA = 1;
+  q->ips = IT;
+  if (M <= kAdapterDecodeM) {
+    // one launch, eight waves and 512 rows (or more) a workgroup, while the
+    // slots' A, read again for each row chunk, stay small
+    const int64_t a_bytes = 2 * a->rank * p->K;
+    q->rpw = 1;
+    while (M * cdiv(p->N, 512 * q->rpw) > 512 && q->rpw < 8) q->rpw *= 2;
+    q->chunks = (int)cdiv(p->N, 512 * q->rpw);
+    q->kind = a->rank <= kAdapterLocalR && a_bytes <= kAdapterLocalA && M * q->chunks * a_bytes <= kAdapterRestage
+                  ? ADAPT_LOCAL
+                  : ADAPT_SLOTS;
+    if (q->kind == ADAPT_LOCAL) return;
     // one workgroup of four waves for each token (those that lead no slot's
-    // tokens end at once), rank group and K-slice; K-slices of at least two
-    // passes of the waves while the leaders alone leave CUs idle
-    q->PA = 1;
+    // tokens end at once), rank group and K-slice; K-slices of at least one
+    // pass of the waves while the leaders alone leave CUs idle
     int P = 1;
     while (M * q->RG * P < 256 && IT / (2 * P) >= 8) P *= 2;
     q->ips = (int)cdiv(IT, P);
     q->P = (int)cdiv(IT, q->ips);
     q->rpw = 1;
-    while (M * cdiv(p->N, 128 * q->rpw) > 1024 && q->rpw < 8) q->rpw *= 2;
-    q->chunks = (int)cdiv(p->N, 128 * q->rpw);
+    while (M * cdiv(p->N, 256 * q->rpw) > 1024 && q->rpw < 8) q->rpw *= 2;
+    q->chunks = (int)cdiv(p->N, 256 * q->rpw);
     return;
   }
+  q->kind = ADAPT_TILES;
   const int64_t tiles = cdiv(M, 64);
+  q->rpw = 1;
+  while (tiles * cdiv(p->N, 64 * q->rpw) > 2048 && q->rpw < 32) q->rpw *= 2;
+  q->chunks = (int)cdiv(p->N, 64 * q->rpw);
   int P = 1;
-  while (tiles * q->RG * P < 512 && IT / (2 * P) >= 4) P *= 2;
+  while (tiles * q->RG * P < 256 && IT / (2 * P) >= 4) P *= 2;
   q->ips = (int)cdiv(IT, P);
   q->P = (int)cdiv(IT, q->ips);
-  q->rpw = 1;
-  while (tiles * cdiv(p->N, 128 * q->rpw) > 2048 && q->rpw < 16) q->rpw *= 2;
-  q->chunks = (int)cdiv(p->N, 128 * q->rpw);
   // few tiles: their slots, as many as their tokens at worst, are shared out
-  q->PA = 1;
   while (q->PA < 16 && tiles * q->PA < 32) q->PA *= 2;
-  if (tiles * q->RG > kMaxEcCounters / SPEAR_GROUP_MAX) {  // (many tiles: no split)
-    q->P = 1;
-    q->ips = IT;
-  }
 }
 
 spear_status_t adapters_layout(int32_t n, const spear_layer_call_t* calls, const spear_adapters_t* const* ads,
-                               AdapterLayout* al, size_t* total) {
+                               const Resolved* z, AdapterLayout* al, size_t* total) {
   size_t off = std::max(*total, kDataBase);
   bool any = false;
-  int ctr = 0;
   for (int i = 0; i < n; ++i) {
     const spear_problem_t* p = calls[i].prob;
     const spear_adapters_t* a = ads[i];
     if (!a) continue;
     if (a->n_adapters < 0 || a->rank < 0 || a->rank > 256) return SPEAR_E_SHAPE;
     const int64_t lim = (int64_t)1 << 30;
-    if (p->M * a->rank >= lim || p->N * a->rank >= lim || p->K * a->rank >= lim) return SPEAR_E_SHAPE;
+    // (M with the rank in whole groups of 32: fp32 sums, 32-bit byte offsets)
+    if (p->M * cdiv(a->rank, 32) * 64 >= lim || p->N * a->rank >= lim || p->K * a->rank >= lim) return SPEAR_E_SHAPE;
     al[i].on = p->M > 0 && p->N > 0 && a->n_adapters > 0 && a->rank > 0;
     if (!al[i].on) continue;
     any = true;
     std::memset(&al[i].p, 0, sizeof(al[i].p));
     adapters_shape(p, a, &al[i].p);
     const AdapterParams& q = al[i].p;
-    const size_t uw = (size_t)p->M * 32 * q.RG;
-    auto take = [&](size_t bytes) {
-      const size_t o = off;
-      off += round256(bytes);
-      return o;
-    };
-    al[i].upart = take(q.P > 1 ? (size_t)q.P * uw * 4 : 0);
-    al[i].uh = take(uw * 2);
-    al[i].ul = take(uw * 2);
-    al[i].us = take((size_t)p->M * q.RG * 4);
-    al[i].d = take((size_t)p->M * p->N * 2);
-    // (the EC projection's counters: its launches come later on the stream)
-    al[i].ctr = ctr;
-    al[i].nctr = q.P > 1 ? (int)(q.tile ? cdiv(p->M, 64) : p->M) * q.RG : 0;
-    ctr += al[i].nctr;
-    if (ctr > kMaxEcCounters) return SPEAR_E_SHAPE;  // (cannot happen: at most 1024 a member)
+    al[i].upart = off;
+    if (q.kind != ADAPT_LOCAL) off += round256((size_t)q.P * p->M * 32 * q.RG * 4);
+    al[i].post = q.kind == ADAPT_TILES && !z[i].gemv && z[i].groles == 3;
+    al[i].d = off;
+    if (!al[i].post) off += round256((size_t)p->M * p->N * 2);
   }
   if (any) *total = off;
   return SPEAR_OK;
@@ -1335,18 +1336,19 @@ bool hits_adapters(const void* y, size_t yb, const spear_problem_t* p, const spe
          overlaps(y, yb, a->ids, M * 4) || overlaps(y, yb, a->ranks, L * 4) || overlaps(y, yb, a->scale, L * 4);
 }
 
-// Forms the members' terms (plus their residuals res) in the workspace; out[i]
-// is member i's, or null where it has no adapters. Members of one activation
-// dtype share the launches.
+// The adapters' launches of the members before (post false) or after their
+// layers: the term plus the residual res[i] in the workspace, out[i] (untouched
+// for the others); or both added to y. Members of one activation dtype share
+// launches.
 spear_status_t run_adapters(int32_t n, const spear_layer_call_t* calls, const spear_adapters_t* const* ads,
-                            const AdapterLayout* al, const uint16_t* const* res, char* ws, const uint16_t** out,
-                            hipStream_t s) {
+                            const AdapterLayout* al, bool post, const uint16_t* const* res, char* ws,
+                            const uint16_t** out, hipStream_t s) {
   for (int dt : {SPEAR_F16, SPEAR_BF16}) {
     AdapterGroup g;
     std::memset(&g, 0, sizeof(g));
     for (int i = 0; i < n; ++i) {
       const spear_problem_t* p = calls[i].prob;
-      if (!al[i].on || p->act_dtype != dt) continue;
+      if (!al[i].on || al[i].post != post || p->act_dtype != dt) continue;
       const spear_adapters_t* a = ads[i];
       AdapterParams& q = g.p[g.n++];
       q = al[i].p;
@@ -1360,17 +1362,14 @@ spear_status_t run_adapters(int32_t n, const spear_layer_call_t* calls, const sp
       q.scale = a->scale;
       q.res = res[i];
       q.upart = (float*)(ws + al[i].upart);
-      q.ctr = (uint32_t*)(ws + kCtrEc) + al[i].ctr;
-      q.uh = (uint16_t*)(ws + al[i].uh);
-      q.ul = (uint16_t*)(ws + al[i].ul);
-      q.us = (float*)(ws + al[i].us);
-      q.d = (uint16_t*)(ws + al[i].d);
+      q.d = post ? (uint16_t*)calls[i].y : (uint16_t*)(ws + al[i].d);
+      q.add = post;
       q.M = (int)p->M;
       q.N = (int)p->N;
       q.K = (int)p->K;
       q.L = a->n_adapters;
       q.R = a->rank;
-      out[i] = q.d;
+      if (!post) out[i] = q.d;
     }
     if (g.n == 0) continue;
     const spear_status_t st = hip_status(SPEAR_BY_DT(launch_adapters, dt)(g, s));
@@ -1634,51 +1633,10 @@ spear_status_t spear_group_launches(int32_t n, const spear_layer_call_t* calls, 
   return SPEAR_OK;
 }
 
-// The grouped call; ads: the members' adapters (the array or any member may be
-// NULL), whose terms are formed first and enter the members as residuals.
-static spear_status_t group_call(int32_t n, const spear_layer_call_t* calls,
-                                 const spear_adapters_t* const* ads, void* workspace,
-                                 size_t workspace_bytes, void* hip_stream) {
-  Resolved z[SPEAR_GROUP_MAX];
-  size_t off[SPEAR_GROUP_MAX], total = 0;
-  spear_status_t st = group_resolve(n, calls, z, off, &total);
-  if (st != SPEAR_OK) return st;
-  AdapterLayout al[SPEAR_GROUP_MAX];
-  if (ads && (st = adapters_layout(n, calls, ads, al, &total)) != SPEAR_OK) return st;
-  if (total > 0) {
-    if (!workspace || workspace_bytes < total) return SPEAR_E_WORKSPACE;
-    if (misaligned(workspace)) return SPEAR_E_ALIGN;
-  }
-  char* ws = (char*)workspace;
-  // every member's own checks first: the cross-member checks below read the
-  // other members' pointers
-  for (int i = 0; i < n; ++i) {
-    const spear_layer_call_t& c = calls[i];
-    const spear_problem_t* p = c.prob;
-    if (p->M == 0 || p->N == 0) continue;
-    if ((st = check_w4(p, c.x, c.w, c.y)) != SPEAR_OK) return st;
-    if (c.ec && (st = check_ec(p, z[i], c.ec, c.y)) != SPEAR_OK) return st;
-    if (ads && (st = check_adapters(p, ads[i])) != SPEAR_OK) return st;
-  }
-  for (int i = 0; i < n; ++i) {
-    const spear_layer_call_t& c = calls[i];
-    const spear_problem_t* p = c.prob;
-    if (p->M == 0 || p->N == 0) continue;
-    const size_t yb = (size_t)p->M * p->N * 2;
-    if (overlaps(c.y, yb, workspace, total)) return SPEAR_E_ALIAS;
-    for (int j = 0; j < n; ++j)
-      if (j != i && calls[j].prob->M > 0 && calls[j].prob->N > 0 && hits_member(c.y, yb, calls[j]))
-        return SPEAR_E_ALIAS;
-    for (int j = 0; ads && j < n; ++j)
-      if (calls[j].prob->M > 0 && calls[j].prob->N > 0 && hits_adapters(c.y, yb, calls[j].prob, ads[j]))
-        return SPEAR_E_ALIAS;
-  }
-  hipStream_t s = (hipStream_t)hip_stream;
-  const uint16_t* res[SPEAR_GROUP_MAX] = {};
-  if (ads) {
-    const uint16_t* none[SPEAR_GROUP_MAX] = {};
-    if ((st = run_adapters(n, calls, ads, al, none, (char*)workspace, res, s)) != SPEAR_OK) return st;
-  }
+// The launches of a grouped call after its checks; res: the members' residuals.
+static spear_status_t run_group(int32_t n, const spear_layer_call_t* calls, Resolved* z, const size_t* off,
+                                const uint16_t* const* res, char* ws, hipStream_t s) {
+  spear_status_t st = SPEAR_OK;
   // Members of one single-launch GEMV variant share one launch; the other
   // members run one after another on the same stream, as their own calls
   // would. Every member's output is the one its own call writes.
@@ -1826,6 +1784,52 @@ static spear_status_t group_call(int32_t n, const spear_layer_call_t* calls,
   return hip_status(SPEAR_BY_WB(launch_gemv_group, z0.wb, z0.dt)(z0.MT, z0.RT, epi, g, 64 * z0.NW, lds, s));
 }
 
+// The grouped call; ads: the members' adapters (the array or any member may be
+// NULL), whose terms are formed first and enter the members as residuals.
+static spear_status_t group_call(int32_t n, const spear_layer_call_t* calls,
+                                 const spear_adapters_t* const* ads, void* workspace,
+                                 size_t workspace_bytes, void* hip_stream) {
+  Resolved z[SPEAR_GROUP_MAX];
+  size_t off[SPEAR_GROUP_MAX], total = 0;
+  spear_status_t st = group_resolve(n, calls, z, off, &total);
+  if (st != SPEAR_OK) return st;
+  AdapterLayout al[SPEAR_GROUP_MAX];
+  if (ads && (st = adapters_layout(n, calls, ads, z, al, &total)) != SPEAR_OK) return st;
+  if (total > 0) {
+    if (!workspace || workspace_bytes < total) return SPEAR_E_WORKSPACE;
+    if (misaligned(workspace)) return SPEAR_E_ALIGN;
+  }
+  char* ws = (char*)workspace;
+  // every member's own checks first: the cross-member checks below read the
+  // other members' pointers
+  for (int i = 0; i < n; ++i) {
+    const spear_layer_call_t& c = calls[i];
+    const spear_problem_t* p = c.prob;
+    if (p->M == 0 || p->N == 0) continue;
+    if ((st = check_w4(p, c.x, c.w, c.y)) != SPEAR_OK) return st;
+    if (c.ec && (st = check_ec(p, z[i], c.ec, c.y)) != SPEAR_OK) return st;
+    if (ads && (st = check_adapters(p, ads[i])) != SPEAR_OK) return st;
+  }
+  for (int i = 0; i < n; ++i) {
+    const spear_layer_call_t& c = calls[i];
+    const spear_problem_t* p = c.prob;
+    if (p->M == 0 || p->N == 0) continue;
+    const size_t yb = (size_t)p->M * p->N * 2;
+    if (overlaps(c.y, yb, workspace, total)) return SPEAR_E_ALIAS;
+    for (int j = 0; j < n; ++j)
+      if (j != i && calls[j].prob->M > 0 && calls[j].prob->N > 0 && hits_member(c.y, yb, calls[j]))
+        return SPEAR_E_ALIAS;
+    for (int j = 0; ads && j < n; ++j)
+      if (calls[j].prob->M > 0 && calls[j].prob->N > 0 && hits_adapters(c.y, yb, calls[j].prob, ads[j]))
+        return SPEAR_E_ALIAS;
+  }
+  hipStream_t s = (hipStream_t)hip_stream;
+  const uint16_t* res[SPEAR_GROUP_MAX] = {};
+  const uint16_t* none[SPEAR_GROUP_MAX] = {};
+  if (ads && (st = run_adapters(n, calls, ads, al, false, none, (char*)workspace, res, s)) != SPEAR_OK) return st;
+  if ((st = run_group(n, calls, z, off, res, ws, s)) != SPEAR_OK) return st;
+  return ads ? run_adapters(n, calls, ads, al, true, none, (char*)workspace, res, s) : SPEAR_OK;
+}
 spear_status_t spear_w4ec_linear_group(int32_t n, const spear_layer_call_t* calls, void* workspace,
                                        size_t workspace_bytes, void* hip_stream) {
   return group_call(n, calls, nullptr, workspace, workspace_bytes, hip_stream);
@@ -1840,7 +1844,7 @@ spear_status_t spear_adapters_workspace(int32_t n, const spear_layer_call_t* cal
   spear_status_t st = group_resolve(n, calls, z, off, &total);
   if (st != SPEAR_OK) return st;
   AdapterLayout al[SPEAR_GROUP_MAX];
-  if ((st = adapters_layout(n, calls, adapters, al, &total)) != SPEAR_OK) return st;
+  if ((st = adapters_layout(n, calls, adapters, z, al, &total)) != SPEAR_OK) return st;
   *out_bytes = total;
   return SPEAR_OK;
 }
@@ -1865,7 +1869,7 @@ spear_status_t spear_w4ec_linear_adapters(const spear_problem_t* prob, const voi
   spear_status_t st = group_resolve(1, &call, z, off, &total);
   if (st != SPEAR_OK) return st;
   AdapterLayout al[SPEAR_GROUP_MAX];
-  if ((st = adapters_layout(1, &call, &adapters, al, &total)) != SPEAR_OK) return st;
+  if ((st = adapters_layout(1, &call, &adapters, z, al, &total)) != SPEAR_OK) return st;
   if (tail && (!std::isfinite(tail->eps) || tail->eps < 0.f)) return SPEAR_E_SHAPE;
   if (prob->M == 0 || prob->N == 0) return SPEAR_OK;
   if ((st = check_w4(prob, x, w, y)) != SPEAR_OK) return st;
@@ -1883,9 +1887,12 @@ spear_status_t spear_w4ec_linear_adapters(const spear_problem_t* prob, const voi
   }
   hipStream_t s = (hipStream_t)hip_stream;
   const uint16_t* res = tail ? (const uint16_t*)tail->residual : nullptr;
-  const uint16_t* term = nullptr;
-  if ((st = run_adapters(1, &call, &adapters, al, &res, (char*)workspace, &term, s)) != SPEAR_OK) return st;
-  st = run_layer(prob, z[0], x, w, ec, y, term ? term : res, (char*)workspace, s);
+  const uint16_t *none = nullptr, *in = res;  // what the layer adds
+  if ((st = run_adapters(1, &call, &adapters, al, false, &res, (char*)workspace, &in, s)) != SPEAR_OK) return st;
+  // (the residual goes with the term added afterwards, unless y itself holds it)
+  const bool later = al[0].on && al[0].post && res != y;
+  st = run_layer(prob, z[0], x, w, ec, y, later ? nullptr : in, (char*)workspace, s);
+  if (st == SPEAR_OK) st = run_adapters(1, &call, &adapters, al, true, later ? &res : &none, (char*)workspace, &in, s);
   if (st != SPEAR_OK || !tail || !tail->norm_w) return st;
   return hip_status(SPEAR_BY_DT(launch_rmsnorm, z[0].dt)((const uint16_t*)y, (const uint16_t*)tail->norm_w,
                                    tail->eps, (uint16_t*)tail->y_norm, (int)prob->M, (int)prob->N, s));

@@ -225,22 +225,21 @@ struct AdapterParams {
   const float* scale;     // [L] or null (all 1)
   const uint16_t* res;    // [M][N] residual, or null
   uint16_t* d;            // [M][N] the term plus the residual, act dtype
-  // coordinates u = s_a A_a x, ranks padded to 32 RG: the K-slices' fp32 sums
-  // [P][M][32 RG] and their arrival counters (P > 1), the two act-dtype parts
-  // [M][32 RG], and per token and rank group the factor that undoes their
-  // scaling [M][RG] (fp16)
-  float* upart;
-  uint32_t* ctr;
-  uint16_t *uh, *ul;
-  float* us;
+  int add;                // d += that instead (in place: the layer's output)
+  float* upart;           // [P][M][32 RG] K-slices of the coordinates A_a x (all but ADAPT_LOCAL)
   int64_t a_stride, b_stride;
   int M, N, K, L, R;
   int RG;                 // rank groups of 32
-  int tile;               // 0: decode (a leader's tokens), 1: 64 consecutive tokens
+  int kind;               // ADAPT_*
   int P, ips;             // K-slices of u, iterations (128 K) per slice
-  int PA;                 // tile: parts that share a tile's slots
-  int chunks, rpw;        // row chunks of the term, row pairs (32 rows) a wave in each
+  int PA;                 // ADAPT_TILES: parts that share a tile's slots (u)
+  int chunks, rpw;        // row chunks of the term, runs of 64 rows a wave in each
 };
+enum { ADAPT_LOCAL = 0,  // a leader's tokens, u and the term in one launch
+       ADAPT_SLOTS = 1,  // a leader's tokens, u and the term in two
+       ADAPT_TILES = 2   // 64 consecutive tokens, in two
+};
+constexpr int kAdapterLocalR = 64;  // ADAPT_LOCAL: the largest rank
 struct AdapterGroup {
   AdapterParams p[kGroupMax];
   int shrink_start[kGroupMax + 1], expand_start[kGroupMax + 1];  // first workgroups
