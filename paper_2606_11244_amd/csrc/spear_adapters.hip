@@ -67,44 +67,86 @@ __device__ __forceinline__ TokenGroup token_group(const AdapterParams& p, int m,
 // u, up to 16 tokens of one slot
 // ---------------------------------------------------------------------------
 
-// acc[t] += rows j0 + 16 t .. +16 of A_a times the tokens at xoff (per lane: byte
-// offset of its token's row), over the wave's share of iterations [it_beg,
-// it_end) of 128 K. K order within an iteration: MFMA jj, lane group lg takes
-// K [8 lg + 32 jj, +8) for both operands (64 contiguous bytes per row and
-// load). Rows from r on are not read.
-template <int DT, int RT>
-__device__ __forceinline__ void project(rsrc_t rx, uint32_t xoff, rsrc_t ra, int K, int j0, int r, int it_beg,
-                                        int it_end, int wave, int NW, f32x4 (&acc)[RT]) {
+// acc[t] += rows j0 + 16 t .. +16 of A_a times the group's tokens, over the
+// wave's iterations [it, it_end) of 128 K. K order within an iteration: MFMA jj,
+// lane group lg takes K [8 lg + 32 jj, +8) for both operands (64 contiguous
+// bytes per row and load). Rows from r on are not read.
+//
+// In the MFMA's layout (lane: column lane % 16) the tokens cost 16 loads for
+// 512 K however few they are, as many as 16 rows of the slot, and the loads'
+// rate is the bound. So up to four tokens (the usual case at decode) come in
+// whole, one load each, and through the wave's own part of the LDS, xs
+// [4][kXRow].
+constexpr int kXRow = 512 + 8;  // halves
+template <int DT, int RT, bool FEW>
+__device__ __forceinline__ void project_part(rsrc_t rx, const TokenGroup& g, const int* stok, uint16_t* xs, rsrc_t ra,
+                                             int K, int j0, int r, int it, int it_end, f32x4 (&acc)[RT]) {
+  constexpr int I = RT == 1 && FEW ? 4 : 2;  // iterations whose loads are in flight together
   const int lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4;
-  constexpr int IPP = 2;  // iterations whose loads are in flight together
   uint32_t aoff[RT];
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
     const int j = j0 + 16 * t + lr;
     aoff[t] = j < r ? (uint32_t)j * K * 2 + 16 * lg : kOOB;
   }
-  const uint32_t xo = xoff + 16 * lg;
-  for (int it0 = it_beg + wave * IPP; it0 < it_end; it0 += NW * IPP) {
-    u32x4 xv[IPP][4], av[IPP][RT][4];
+  const uint16_t* xr = xs + min(lr, g.cnt - 1) * kXRow + 8 * lg;
+  const uint32_t xo = (uint32_t)g.tok * K * 2 + 16 * lg;
+  uint32_t xw[4];  // FEW: this lane's 16 bytes of each token's run
 #pragma unroll
-    for (int h = 0; h < IPP; ++h) {
-      const bool ok = it0 + h < it_end;  // uniform
-      const uint32_t kb = (uint32_t)(it0 + h) * (kIterK * 2);
+  for (int t = 0; t < 4; ++t) xw[t] = FEW ? (uint32_t)stok[min(t, g.cnt - 1)] * K * 2 + 16 * lane : 0u;
+  for (; it < it_end; it += I) {
+    const int n = min(I, it_end - it);  // uniform
+    const uint32_t kb = (uint32_t)it * (kIterK * 2);
+    u32x4 av[I][RT][4], xv[FEW ? 1 : I][4];
+    if constexpr (FEW) {
 #pragma unroll
-      for (int jj = 0; jj < 4; ++jj) xv[h][jj] = bld128(rx, ok ? xo + kb + 64 * jj : kOOB);
+      for (int t = 0; t < 4; ++t)
+        if (t == 0 || t < g.cnt) xv[0][t] = bld128(rx, lane < 16 * n ? xw[t] + kb : kOOB);  // (uniform)
+    } else {
+#pragma unroll
+      for (int h = 0; h < I; ++h)
+#pragma unroll
+        for (int jj = 0; jj < 4; ++jj) xv[h][jj] = bld128(rx, h < n ? xo + kb + 256 * h + 64 * jj : kOOB);
+    }
+#pragma unroll
+    for (int h = 0; h < I; ++h)
 #pragma unroll
       for (int t = 0; t < RT; ++t)
 #pragma unroll
         for (int jj = 0; jj < 4; ++jj)
-          av[h][t][jj] = bld128(ra, ok && aoff[t] != kOOB ? aoff[t] + kb + 64 * jj : kOOB);
-    }
+          av[h][t][jj] = bld128(ra, h < n && aoff[t] != kOOB ? aoff[t] + kb + 256 * h + 64 * jj : kOOB);
     __builtin_amdgcn_sched_barrier(0);
+    if constexpr (FEW) {
 #pragma unroll
-    for (int h = 0; h < IPP; ++h)
+      for (int t = 0; t < 4; ++t)
+        if (t == 0 || t < g.cnt) *(u32x4*)(xs + t * kXRow + 8 * lane) = xv[0][t];
+      __builtin_amdgcn_wave_barrier();  // the wave's own LDS, in program order
+    }
 #pragma unroll
-      for (int jj = 0; jj < 4; ++jj)
+    for (int h = 0; h < I; ++h)
 #pragma unroll
-        for (int t = 0; t < RT; ++t) acc[t] = mfma16<DT>(av[h][t][jj], xv[h][jj], acc[t]);
+      for (int jj = 0; jj < 4; ++jj) {
+        u32x4 xf;
+        if constexpr (FEW) xf = *(const u32x4*)(xr + 128 * h + 32 * jj);
+        else xf = xv[h][jj];
+#pragma unroll
+        for (int t = 0; t < RT; ++t) acc[t] = mfma16<DT>(av[h][t][jj], xf, acc[t]);
+      }
+    if constexpr (FEW) __builtin_amdgcn_wave_barrier();
+  }
+}
+// (the second half of acc stays as it is where the ranks fit one row tile)
+template <int DT>
+__device__ __forceinline__ void project(rsrc_t rx, const TokenGroup& g, const int* stok, uint16_t* xs, rsrc_t ra, int K,
+                                        int j0, int r, int it, int it_end, f32x4 (&acc)[2]) {
+  if (r - j0 > 16) {
+    if (g.cnt <= 4) project_part<DT, 2, true>(rx, g, stok, xs, ra, K, j0, r, it, it_end, acc);
+    else project_part<DT, 2, false>(rx, g, stok, xs, ra, K, j0, r, it, it_end, acc);
+  } else {
+    f32x4 a1[1] = {acc[0]};
+    if (g.cnt <= 4) project_part<DT, 1, true>(rx, g, stok, xs, ra, K, j0, r, it, it_end, a1);
+    else project_part<DT, 1, false>(rx, g, stok, xs, ra, K, j0, r, it, it_end, a1);
+    acc[0] = a1[0];
   }
 }
 
@@ -291,31 +333,43 @@ __device__ __forceinline__ void store_term(const AdapterParams& p, bool live, in
 }
 
 // Rows [n0, n1) of the term of up to 16 tokens of one slot (lane's token tok,
-// live), every `step` rows from n0; part(kk, hi, lo, sc): this lane's fragments
-// of u (ranks 32 kk + 8 (lane / 16) .. +8) and its scale.
-template <int DT, class Part>
-__device__ __forceinline__ void expand_slot(const AdapterParams& p, int a, int r, bool live, int tok, int n0, int n1,
-                                            int step, Part part) {
-  const rsrc_t rb = make_rsrc(p.B + (size_t)max(a, 0) * p.b_stride, (uint32_t)p.N * p.R * 2);
-  const int nkk = (r + 31) >> 5;
-  const bool vec = (p.R & 7) == 0 && (p.b_stride & 7) == 0;
-  for (int n = n0; n < n1; n += step) {
-    Base base;
-    f32x4 v[4];
-#pragma unroll
-    for (int t = 0; t < 4; ++t) v[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+// live), 64 at a time, every `step` from the wave's first; the first 64 rows'
+// operands are requested by the constructor, before u is there.
+template <int DT>
+struct SlotTerm {
+  const AdapterParams& p;
+  rsrc_t rb;
+  int tok, n0;
+  bool live, vec;
+  u32x4 bf[4];
+  Base base;
+  // (columns past the slot's rank are read and dropped: nothing waits for it)
+  __device__ __forceinline__ SlotTerm(const AdapterParams& p_, int a, bool live_, int tok_, int n)
+      : p(p_), tok(tok_), n0(n), live(live_) {
+    rb = make_rsrc(p.B + (size_t)max(a, 0) * p.b_stride, a < 0 ? 0u : (uint32_t)p.N * p.R * 2);
+    vec = (p.R & 7) == 0 && (p.b_stride & 7) == 0;
+    load_rows<DT>(p, rb, n, 0, p.R, vec, bf);
     load_base(p, live, tok, n, base);
-    for (int kk = 0; kk < nkk; ++kk) {
-      u32x4 bf[4], hi, lo;
-      float sc = 1.f;
-      load_rows<DT>(p, rb, n, kk, r, vec, bf);
-      part(kk, hi, lo, sc);
-      if (vec && (r & 7)) mask_rows(kk, r, bf);
-      add_product<DT>(bf, hi, lo, sc, v);
-    }
-    store_term<DT>(p, live, tok, n, base, v);
   }
-}
+  __device__ __forceinline__ void rows(int n1, int step, int r, const Parts& parts) {
+    const int nkk = (r + 31) >> 5;
+    for (int n = n0; n < n1; n += step) {
+      f32x4 v[4];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) v[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (n != n0) load_base(p, live, tok, n, base);
+      for (int kk = 0; kk < nkk; ++kk) {
+        if (n != n0 || kk > 0) load_rows<DT>(p, rb, n, kk, r, vec, bf);
+        u32x4 hi, lo;
+        float f;
+        parts.get(threadIdx.x & 15, kk, hi, lo, f);
+        if (r < 32 * kk + 32) mask_rows(kk, r, bf);
+        add_product<DT>(bf, hi, lo, f, v);
+      }
+      store_term<DT>(p, live, tok, n, base, v);
+    }
+  }
+};
 
 // ---------------------------------------------------------------------------
 // decode: u in slices over K, then the term
@@ -323,6 +377,7 @@ __device__ __forceinline__ void expand_slot(const AdapterParams& p, int a, int r
 template <int DT>
 __device__ __forceinline__ void shrink_group(const AdapterParams& p, int b) {
   __shared__ __attribute__((aligned(16))) float red[4][2][256];
+  __shared__ __attribute__((aligned(16))) uint16_t xs[4][4 * kXRow];
   __shared__ int stok[16];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int per = p.P * p.RG, m = b / per, rem = b - m * per, rg = rem / p.P, ks = rem - rg * p.P;
@@ -331,14 +386,10 @@ __device__ __forceinline__ void shrink_group(const AdapterParams& p, int b) {
   const rsrc_t rx = make_rsrc(p.x, (uint32_t)p.M * p.K * 2);
   const rsrc_t ra = make_rsrc(p.A + (size_t)g.a * p.a_stride, (uint32_t)p.R * p.K * 2);
   f32x4 acc[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
-  const int it0 = ks * p.ips, it1 = min(p.K / kIterK, it0 + p.ips);
-  if (g.r - 32 * rg > 16) {
-    project<DT, 2>(rx, (uint32_t)g.tok * p.K * 2, ra, p.K, 32 * rg, g.r, it0, it1, wave, 4, acc);
-  } else {
-    f32x4 a1[1] = {acc[0]};
-    project<DT, 1>(rx, (uint32_t)g.tok * p.K * 2, ra, p.K, 32 * rg, g.r, it0, it1, wave, 4, a1);
-    acc[0] = a1[0];
-  }
+  // the slice's iterations, shared out in runs
+  const int it0 = ks * p.ips, it1 = min(p.K / kIterK, it0 + p.ips), iw = (it1 - it0 + 3) >> 2;
+  const int ib = min(it1, it0 + wave * iw), ie = min(it1, ib + iw);
+  project<DT>(rx, g, stok, xs[wave], ra, p.K, 32 * rg, g.r, ib, ie, acc);
 #pragma unroll
   for (int t = 0; t < 2; ++t) *(f32x4*)(red[wave][t] + 4 * lane) = acc[t];
   __syncthreads();
@@ -585,34 +636,24 @@ template <int DT>
 __device__ __forceinline__ void adapt_local(const AdapterParams& p, int b, char* smem) {
   __shared__ __attribute__((aligned(16))) float red[8][2][256];
   __shared__ __attribute__((aligned(16))) float u[16][kAdapterLocalR + 4];
+  __shared__ __attribute__((aligned(16))) uint16_t xs[8][4 * kXRow];
   __shared__ int stok[16];
   const int lane = threadIdx.x & 63, lr = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int m = b / p.chunks, chunk = b - m * p.chunks;
   const TokenGroup g = token_group(p, m, stok);
   if (g.cnt == 0) return;
-  const int a = max(g.a, 0), n0 = chunk * 512 * p.rpw, n1 = min(p.N, n0 + 512 * p.rpw), n = n0 + 64 * wave;
-  const bool live = lr < g.cnt, vec = (p.R & 7) == 0 && (p.b_stride & 7) == 0;
+  const int a = max(g.a, 0), n0 = chunk * 512 * p.rpw, n1 = min(p.N, n0 + 512 * p.rpw);
   const rsrc_t rx = make_rsrc(p.x, (uint32_t)p.M * p.K * 2);
   const rsrc_t ra = make_rsrc(p.A + (size_t)a * p.a_stride, (uint32_t)p.R * p.K * 2);
-  const rsrc_t rb = make_rsrc(p.B + (size_t)a * p.b_stride, (uint32_t)p.N * p.R * 2);
   const int r = rank_of(p, g.a);
   const float sc = p.scale ? p.scale[a] : 1.f;
-  const int IT = p.K / kIterK;
-  u32x4 bf[4];
-  Base base;
-  load_rows<DT>(p, rb, n, 0, p.R, vec, bf);
-  load_base(p, live, g.tok, n, base);
+  const int IT = p.K / kIterK, iw = (IT + 7) >> 3, ib = min(IT, wave * iw), ie = min(IT, ib + iw);
+  SlotTerm<DT> term(p, g.a, lr < g.cnt, g.tok, n0 + 64 * wave);
   const int top = g.a < 0 ? 0 : p.R;  // no rank in the addresses: nothing waits for it
   for (int j0 = 0; j0 < top; j0 += 32) {
     f32x4 acc[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
-    if (top - j0 > 16) {
-      project<DT, 2>(rx, (uint32_t)g.tok * p.K * 2, ra, p.K, j0, top, 0, IT, wave, 8, acc);
-    } else {
-      f32x4 a1[1] = {acc[0]};
-      project<DT, 1>(rx, (uint32_t)g.tok * p.K * 2, ra, p.K, j0, top, 0, IT, wave, 8, a1);
-      acc[0] = a1[0];
-    }
+    project<DT>(rx, g, stok, xs[wave], ra, p.K, j0, top, ib, ie, acc);
     if (j0 > 0) __syncthreads();
 #pragma unroll
     for (int t = 0; t < 2; ++t) *(f32x4*)(red[wave][t] + 4 * lane) = acc[t];
@@ -634,22 +675,7 @@ __device__ __forceinline__ void adapt_local(const AdapterParams& p, int b, char*
     __syncthreads();
     build_parts<DT>(parts, 16, [&](int t, int j) { return *(const f32x4*)&u[t][j]; });
   }
-  const int nkk = (r + 31) >> 5;
-  for (int nn = n; nn < n1; nn += 512) {
-    f32x4 v[4];
-#pragma unroll
-    for (int t = 0; t < 4; ++t) v[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-    if (nn != n) load_base(p, live, g.tok, nn, base);
-    for (int kk = 0; kk < nkk; ++kk) {
-      if (nn != n || kk > 0) load_rows<DT>(p, rb, nn, kk, p.R, vec, bf);
-      u32x4 hi, lo;
-      float f;
-      parts.get(lr, kk, hi, lo, f);
-      if (r < 32 * kk + 32) mask_rows(kk, r, bf);
-      add_product<DT>(bf, hi, lo, f, v);
-    }
-    store_term<DT>(p, live, g.tok, nn, base, v);
-  }
+  term.rows(n1, 512, r, parts);
 }
 
 // ---------------------------------------------------------------------------
@@ -679,16 +705,16 @@ __device__ __forceinline__ void expand_body(const AdapterParams& p, int b, char*
   } else {
     __shared__ int stok[16];
     const int m = b / p.chunks, chunk = b - m * p.chunks;
-    TokenGroup t = token_group(p, m, stok);
+    const TokenGroup t = token_group(p, m, stok);
     if (t.cnt == 0) return;
+    const int rows = 256 * p.rpw, n0 = chunk * rows;
+    SlotTerm<DT> term(p, t.a, (threadIdx.x & 15) < t.cnt, t.tok, n0 + 64 * (threadIdx.x >> 6));
     const Parts parts(smem, 16, p.RG);
     if (t.r > 0) {
       const float sc = p.scale ? p.scale[t.a] : 1.f;
       build_parts<DT>(parts, 16, [&](int i, int j) { return sum_u(p, stok[min(i, t.cnt - 1)], j, t.r, sc); });
     }
-    const int lane = threadIdx.x & 63, rows = 256 * p.rpw, n0 = chunk * rows;
-    expand_slot<DT>(p, t.a, t.r, (lane & 15) < t.cnt, t.tok, n0 + 64 * (threadIdx.x >> 6), min(p.N, n0 + rows), 256,
-                    [&](int kk, u32x4& hi, u32x4& lo, float& sc) { parts.get(lane & 15, kk, hi, lo, sc); });
+    term.rows(min(p.N, n0 + rows), 256, t.r, parts);
   }
 }
 template <int DT, int KIND>
