@@ -12,143 +12,27 @@
 // product with zero, so that no token meets another's values. u is held in
 // fp32 and enters the second MFMA as two activation-dtype parts.
 //
-// Decode (up to 64 tokens): the tokens of one slot, up to 16 of them, belong
-// to the workgroups of the first of them ("leader"); the other tokens'
-// workgroups end at once. Nothing needs sorting, and the ids are read on the
-// device. Beyond, a workgroup owns 64 consecutive tokens and walks the slots
-// they name.
-#include "spear_device.h"
+// Decode (up to 64 tokens; its coordinates in spear_adapters.h): the tokens of
+// one slot, up to 16 of them, belong to the workgroups of the first of them
+// ("leader"); the other tokens' workgroups end at once. Nothing needs sorting,
+// and the ids are read on the device. Beyond, a workgroup owns 64 consecutive
+// tokens and walks the slots they name.
+//
+// The coordinates leave as sums over K-slices, which every workgroup of the
+// second step adds up for its own tokens: a few KB from L2 each, in place of a
+// last arriver that sums them alone (8B down, K = 14336, 300 tokens: 32 us for
+// the first step that way, 18 and 3 more in the second this way). One launch
+// that forms u anew in each workgroup of the term was slower wherever A is not
+// tiny: a CU draws about 12 bytes a cycle from its L2 (8B gate and up at eight
+// requests 17.8 us against 12.0 for the two, o 14.0 against 10.2; 8B q, k, v at 16
+// requests 9.4 against 10.1; 1B q at one token, rank 8, 6.1 against 8.2).
+#include "spear_adapters.h"
 
 namespace spear {
 
 // ---------------------------------------------------------------------------
-// tokens and slots
+// the parts of u
 // ---------------------------------------------------------------------------
-
-// the slot of token m, or -1 (none) for any id outside [0, L)
-__device__ __forceinline__ int slot_of(const AdapterParams& p, int m) {
-  const int a = p.ids[m];
-  return a >= 0 && a < p.L ? a : -1;
-}
-__device__ __forceinline__ int rank_of(const AdapterParams& p, int a) {
-  if (a < 0) return 0;
-  return p.ranks ? min(max(p.ranks[a], 0), p.R) : p.R;
-}
-
-// The tokens of one slot that a leader's workgroups own.
-struct TokenGroup {
-  int a, r;    // slot (-1: none) and its rank
-  int cnt;     // tokens, 0: this token leads none
-  int tok;     // this lane's: token lane % 16 of the group (past cnt: the leader)
-};
-// M <= 64; every wave of the workgroup calls it. stok: 16 ints of LDS.
-__device__ __forceinline__ TokenGroup token_group(const AdapterParams& p, int m, int* stok) {
-  const int lane = threadIdx.x & 63;
-  const int id = lane < p.M ? slot_of(p, lane) : -2;
-  TokenGroup g;
-  g.a = __builtin_amdgcn_readlane(id, m);
-  const uint64_t same = __ballot(id == g.a);
-  const int before = __popcll(same & ((1ull << m) - 1));
-  g.cnt = 0;
-  g.r = 0;
-  g.tok = m;
-  if (before & 15) return g;  // uniform
-  const uint64_t mine = same & ~((1ull << m) - 1);
-  g.cnt = min(16, (int)__popcll(mine));
-  const int pos = __popcll(mine & ((1ull << lane) - 1));
-  if (((mine >> lane) & 1) && pos < 16) stok[pos] = lane;  // every wave writes the same
-  __syncthreads();
-  g.tok = stok[min(lane & 15, g.cnt - 1)];
-  g.r = rank_of(p, g.a);
-  return g;
-}
-
-// ---------------------------------------------------------------------------
-// u, up to 16 tokens of one slot
-// ---------------------------------------------------------------------------
-
-// acc[t] += rows j0 + 16 t .. +16 of A_a times the group's tokens, over the
-// wave's iterations [it, it_end) of 128 K. K order within an iteration: MFMA jj,
-// lane group lg takes K [8 lg + 32 jj, +8) for both operands (64 contiguous
-// bytes per row and load). Rows from r on are not read.
-//
-// In the MFMA's layout (lane: column lane % 16) the tokens cost 16 loads for
-// 512 K however few they are, as many as 16 rows of the slot, and the loads'
-// rate is the bound. So up to four tokens (the usual case at decode) come in
-// whole, one load each, and through the wave's own part of the LDS, xs
-// [4][kXRow].
-constexpr int kXRow = 512 + 8;  // halves
-template <int DT, int RT, bool FEW>
-__device__ __forceinline__ void project_part(rsrc_t rx, const TokenGroup& g, const int* stok, uint16_t* xs, rsrc_t ra,
-                                             int K, int j0, int r, int it, int it_end, f32x4 (&acc)[RT]) {
-  constexpr int I = RT == 1 && FEW ? 4 : 2;  // iterations whose loads are in flight together
-  const int lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4;
-  uint32_t aoff[RT];
-#pragma unroll
-  for (int t = 0; t < RT; ++t) {
-    const int j = j0 + 16 * t + lr;
-    aoff[t] = j < r ? (uint32_t)j * K * 2 + 16 * lg : kOOB;
-  }
-  const uint16_t* xr = xs + min(lr, g.cnt - 1) * kXRow + 8 * lg;
-  const uint32_t xo = (uint32_t)g.tok * K * 2 + 16 * lg;
-  uint32_t xw[4];  // FEW: this lane's 16 bytes of each token's run
-#pragma unroll
-  for (int t = 0; t < 4; ++t) xw[t] = FEW ? (uint32_t)stok[min(t, g.cnt - 1)] * K * 2 + 16 * lane : 0u;
-  for (; it < it_end; it += I) {
-    const int n = min(I, it_end - it);  // uniform
-    const uint32_t kb = (uint32_t)it * (kIterK * 2);
-    u32x4 av[I][RT][4], xv[FEW ? 1 : I][4];
-    if constexpr (FEW) {
-#pragma unroll
-      for (int t = 0; t < 4; ++t)
-        if (t == 0 || t < g.cnt) xv[0][t] = bld128(rx, lane < 16 * n ? xw[t] + kb : kOOB);  // (uniform)
-    } else {
-#pragma unroll
-      for (int h = 0; h < I; ++h)
-#pragma unroll
-        for (int jj = 0; jj < 4; ++jj) xv[h][jj] = bld128(rx, h < n ? xo + kb + 256 * h + 64 * jj : kOOB);
-    }
-#pragma unroll
-    for (int h = 0; h < I; ++h)
-#pragma unroll
-      for (int t = 0; t < RT; ++t)
-#pragma unroll
-        for (int jj = 0; jj < 4; ++jj)
-          av[h][t][jj] = bld128(ra, h < n && aoff[t] != kOOB ? aoff[t] + kb + 256 * h + 64 * jj : kOOB);
-    __builtin_amdgcn_sched_barrier(0);
-    if constexpr (FEW) {
-#pragma unroll
-      for (int t = 0; t < 4; ++t)
-        if (t == 0 || t < g.cnt) *(u32x4*)(xs + t * kXRow + 8 * lane) = xv[0][t];
-      __builtin_amdgcn_wave_barrier();  // the wave's own LDS, in program order
-    }
-#pragma unroll
-    for (int h = 0; h < I; ++h)
-#pragma unroll
-      for (int jj = 0; jj < 4; ++jj) {
-        u32x4 xf;
-        if constexpr (FEW) xf = *(const u32x4*)(xr + 128 * h + 32 * jj);
-        else xf = xv[h][jj];
-#pragma unroll
-        for (int t = 0; t < RT; ++t) acc[t] = mfma16<DT>(av[h][t][jj], xf, acc[t]);
-      }
-    if constexpr (FEW) __builtin_amdgcn_wave_barrier();
-  }
-}
-// (the second half of acc stays as it is where the ranks fit one row tile)
-template <int DT>
-__device__ __forceinline__ void project(rsrc_t rx, const TokenGroup& g, const int* stok, uint16_t* xs, rsrc_t ra, int K,
-                                        int j0, int r, int it, int it_end, f32x4 (&acc)[2]) {
-  if (r - j0 > 16) {
-    if (g.cnt <= 4) project_part<DT, 2, true>(rx, g, stok, xs, ra, K, j0, r, it, it_end, acc);
-    else project_part<DT, 2, false>(rx, g, stok, xs, ra, K, j0, r, it, it_end, acc);
-  } else {
-    f32x4 a1[1] = {acc[0]};
-    if (g.cnt <= 4) project_part<DT, 1, true>(rx, g, stok, xs, ra, K, j0, r, it, it_end, a1);
-    else project_part<DT, 1, false>(rx, g, stok, xs, ra, K, j0, r, it, it_end, a1);
-    acc[0] = a1[0];
-  }
-}
 
 // The two activation-dtype parts of a coordinate. fp16 has neither the range
 // nor, for small values, the precision: there the 32 coordinates of a token and
@@ -177,6 +61,15 @@ struct Parts {
     lo = hi + T * ld;
     sc = (float*)(lo + T * ld);
   }
+  // the parts of token t's ranks j .. j + 4
+  template <int DT>
+  __device__ __forceinline__ void put(int t, int j, const f32x4& v) const {
+    uint16_t h[4], l[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) split_parts<DT>(v[e], &h[e], &l[e]);
+    *(u32x2*)(hi + t * ld + j) = u32x2{h[0] | ((uint32_t)h[1] << 16), h[2] | ((uint32_t)h[3] << 16)};
+    *(u32x2*)(lo + t * ld + j) = u32x2{l[0] | ((uint32_t)l[1] << 16), l[2] | ((uint32_t)l[3] << 16)};
+  }
   // this lane's fragment of token t, rank group kk
   __device__ __forceinline__ void get(int t, int kk, u32x4& h, u32x4& l, float& f) const {
     const int o = t * ld + 32 * kk + 8 * ((threadIdx.x & 63) >> 4);
@@ -201,12 +94,7 @@ __device__ __forceinline__ void build_parts(const Parts& o, int T, Val val) {
       v *= exp2i(k);
       if ((q & 7) == 0) o.sc[t * o.RG + (q >> 3)] = exp2i(-k);
     }
-    uint16_t h[4], l[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) split_parts<DT>(v[e], &h[e], &l[e]);
-    const int at = t * o.ld + 4 * q;
-    *(u32x2*)(o.hi + at) = u32x2{h[0] | ((uint32_t)h[1] << 16), h[2] | ((uint32_t)h[3] << 16)};
-    *(u32x2*)(o.lo + at) = u32x2{l[0] | ((uint32_t)l[1] << 16), l[2] | ((uint32_t)l[3] << 16)};
+    o.template put<DT>(t, 4 * q, v);
   }
   __syncthreads();
 }
@@ -237,27 +125,38 @@ __device__ __forceinline__ f32x4 sum_u(const AdapterParams& p, int m, int j, int
 // t is row 32 (t / 2) + 8 (q / 4) + 4 (t % 2) + q % 4, so that a lane's results
 // are two runs of eight consecutive rows. Ranks from r on are not used (of a
 // whole chunk of eight they are read and put to zero).
-template <int DT>
-__device__ __forceinline__ void load_rows(const AdapterParams& p, rsrc_t rb, int n0, int kk, int r, bool vec,
-                                          u32x4 (&bf)[4]) {
-  const int lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4;
-  const int j0 = 32 * kk + 8 * lg;
+struct RowLanes {
+  uint32_t off[4];  // this lane's row of each tile at n0 = 0, ranks 8 lg
+  bool vec;         // rows of whole, aligned chunks of eight ranks
+  __device__ __forceinline__ explicit RowLanes(const AdapterParams& p) {
+    const int lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4;
 #pragma unroll
-  for (int t = 0; t < 4; ++t) {
-    const int n = n0 + 32 * (t >> 1) + 8 * (lr >> 2) + 4 * (t & 1) + (lr & 3);
-    const uint32_t off = ((uint32_t)n * p.R + j0) * 2;
-    if (vec) {
-      bf[t] = bld128(rb, n < p.N && j0 < r ? off : kOOB);
-    } else {
+    for (int t = 0; t < 4; ++t)
+      off[t] = (uint32_t)((32 * (t >> 1) + 8 * (lr >> 2) + 4 * (t & 1) + (lr & 3)) * p.R + 8 * lg) * 2;
+    vec = (p.R & 7) == 0 && (p.b_stride & 7) == 0;
+  }
+};
+// (rows from N on lie past the buffer rb of the slot's N R values: zero)
+__device__ __forceinline__ void load_rows(const AdapterParams& p, const RowLanes& o, rsrc_t rb, int n0, int kk, int r,
+                                          u32x4 (&bf)[4]) {
+  const int lg = (threadIdx.x & 63) >> 4, j0 = 32 * kk + 8 * lg;
+  const uint32_t base = ((uint32_t)n0 * p.R + 32 * kk) * 2;  // (past the slot where n0 >= N: not a scalar offset)
+  if (o.vec) {
+    const bool ok = j0 < r;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) bf[t] = bld128(rb, ok ? o.off[t] + base : kOOB);
+  } else {
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         const int j = j0 + 2 * q;
-        bf[t][q] = bld16(rb, n < p.N && j < r ? off + 4 * q : kOOB) |
-                   (bld16(rb, n < p.N && j + 1 < r ? off + 4 * q + 2 : kOOB) << 16);
+        bf[t][q] = bld16(rb, j < r ? o.off[t] + base + 4 * q : kOOB) |
+                   (bld16(rb, j + 1 < r ? o.off[t] + base + 4 * q + 2 : kOOB) << 16);
       }
-    }
   }
 }
+// ranks from r on to zero (where they were read: of the slot's R)
 __device__ __forceinline__ void mask_rows(int kk, int r, u32x4 (&bf)[4]) {
   const int j0 = 32 * kk + 8 * ((threadIdx.x & 63) >> 4);
 #pragma unroll
@@ -294,7 +193,6 @@ __device__ __forceinline__ void load_base(const AdapterParams& p, bool live, int
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const int nn = n + 32 * h + 8 * lg;
-    b.res[h] = b.old[h] = u32x4{0, 0, 0, 0};
     if ((p.N & 7) == 0 && live && nn < p.N) {
       if (p.res) b.res[h] = ldg16(p.res + (size_t)m * p.N + nn);
       if (p.add) b.old[h] = ldg16(p.d + (size_t)m * p.N + nn);
@@ -313,13 +211,19 @@ __device__ __forceinline__ void store_term(const AdapterParams& p, bool live, in
     if (nn >= p.N) continue;
     const size_t o = (size_t)m * p.N + nn;
     if ((p.N & 7) == 0) {
+      f32x4 f[2] = {v[2 * h], v[2 * h + 1]};
+      auto add = [&](const u32x4& w) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e >> 2][e & 3] += act2f<DT>((w[e >> 1] >> (16 * (e & 1))) & 0xFFFFu);
+      };
+      if (p.res) add(b.res[h]);  // (uniform)
+      if (p.add) add(b.old[h]);
       u32x4 w;
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const f32x4& f = v[2 * h + (q >> 1)];
-        const float x = f[2 * (q & 1)] + act2f<DT>(b.res[h][q] & 0xFFFFu) + act2f<DT>(b.old[h][q] & 0xFFFFu);
-        const float y = f[2 * (q & 1) + 1] + act2f<DT>(b.res[h][q] >> 16) + act2f<DT>(b.old[h][q] >> 16);
-        w[q] = (uint32_t)f2act<DT>(x) | ((uint32_t)f2act<DT>(y) << 16);
+        const float x = f[q >> 1][2 * (q & 1)], y = f[q >> 1][2 * (q & 1) + 1];
+        if constexpr (DT == DT_BF16) w[q] = pack_bf16(x, y);
+        else w[q] = (uint32_t)f2act<DT>(x) | ((uint32_t)f2act<DT>(y) << 16);
       }
       *(u32x4*)(p.d + o) = w;
     } else {
@@ -338,17 +242,17 @@ __device__ __forceinline__ void store_term(const AdapterParams& p, bool live, in
 template <int DT>
 struct SlotTerm {
   const AdapterParams& p;
+  const RowLanes lanes;
   rsrc_t rb;
   int tok, n0;
-  bool live, vec;
+  bool live;
   u32x4 bf[4];
   Base base;
   // (columns past the slot's rank are read and dropped: nothing waits for it)
   __device__ __forceinline__ SlotTerm(const AdapterParams& p_, int a, bool live_, int tok_, int n)
-      : p(p_), tok(tok_), n0(n), live(live_) {
+      : p(p_), lanes(p_), tok(tok_), n0(n), live(live_) {
     rb = make_rsrc(p.B + (size_t)max(a, 0) * p.b_stride, a < 0 ? 0u : (uint32_t)p.N * p.R * 2);
-    vec = (p.R & 7) == 0 && (p.b_stride & 7) == 0;
-    load_rows<DT>(p, rb, n, 0, p.R, vec, bf);
+    load_rows(p, lanes, rb, n, 0, p.R, bf);
     load_base(p, live, tok, n, base);
   }
   __device__ __forceinline__ void rows(int n1, int step, int r, const Parts& parts) {
@@ -359,50 +263,17 @@ struct SlotTerm {
       for (int t = 0; t < 4; ++t) v[t] = f32x4{0.f, 0.f, 0.f, 0.f};
       if (n != n0) load_base(p, live, tok, n, base);
       for (int kk = 0; kk < nkk; ++kk) {
-        if (n != n0 || kk > 0) load_rows<DT>(p, rb, n, kk, r, vec, bf);
+        if (n != n0 || kk > 0) load_rows(p, lanes, rb, n, kk, p.R, bf);
         u32x4 hi, lo;
         float f;
         parts.get(threadIdx.x & 15, kk, hi, lo, f);
-        if (r < 32 * kk + 32) mask_rows(kk, r, bf);
+        if (r < min(p.R, 32 * kk + 32)) mask_rows(kk, r, bf);
         add_product<DT>(bf, hi, lo, f, v);
       }
       store_term<DT>(p, live, tok, n, base, v);
     }
   }
 };
-
-// ---------------------------------------------------------------------------
-// decode: u in slices over K, then the term
-// ---------------------------------------------------------------------------
-template <int DT>
-__device__ __forceinline__ void shrink_group(const AdapterParams& p, int b) {
-  __shared__ __attribute__((aligned(16))) float red[4][2][256];
-  __shared__ __attribute__((aligned(16))) uint16_t xs[4][4 * kXRow];
-  __shared__ int stok[16];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int per = p.P * p.RG, m = b / per, rem = b - m * per, rg = rem / p.P, ks = rem - rg * p.P;
-  const TokenGroup g = token_group(p, m, stok);
-  if (g.cnt == 0 || 32 * rg >= g.r) return;
-  const rsrc_t rx = make_rsrc(p.x, (uint32_t)p.M * p.K * 2);
-  const rsrc_t ra = make_rsrc(p.A + (size_t)g.a * p.a_stride, (uint32_t)p.R * p.K * 2);
-  f32x4 acc[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
-  // the slice's iterations, shared out in runs
-  const int it0 = ks * p.ips, it1 = min(p.K / kIterK, it0 + p.ips), iw = (it1 - it0 + 3) >> 2;
-  const int ib = min(it1, it0 + wave * iw), ie = min(it1, ib + iw);
-  project<DT>(rx, g, stok, xs[wave], ra, p.K, 32 * rg, g.r, ib, ie, acc);
-#pragma unroll
-  for (int t = 0; t < 2; ++t) *(f32x4*)(red[wave][t] + 4 * lane) = acc[t];
-  __syncthreads();
-  // lane l of a tile holds token l % 16, ranks 4 (l / 16) .. +4: thread (t, l)
-  // sums and stores those four
-  if (threadIdx.x < 128) {
-    const int t = threadIdx.x >> 6, tok = lane & 15, j = 32 * rg + 16 * t + 4 * (lane >> 4);
-    f32x4 s = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int w = 0; w < 4; ++w) s += *(const f32x4*)(red[w][t] + 4 * lane);
-    if (tok < g.cnt) *(f32x4*)(p.upart + ((size_t)ks * p.M + stok[tok]) * (32 * p.RG) + j) = s;
-  }
-}
 
 // ---------------------------------------------------------------------------
 // beyond: 64 consecutive tokens
@@ -467,13 +338,14 @@ __device__ __forceinline__ void shrink_tile(const AdapterParams& p, int b) {
   uint32_t xoff[4];
 #pragma unroll
   for (int s = 0; s < 4; ++s) xoff[s] = (uint32_t)min(m0 + 16 * s + lr, p.M - 1) * p.K * 2 + 16 * lg;
+  const uint32_t aoff = (uint32_t)(32 * rg + lr) * p.K * 2 + 16 * lg;
   for (int it = it_beg + wave; it < it_end; it += 4) {
     const uint32_t kb = (uint32_t)it * (kIterK * 2);
     u32x4 xv[4][4];
 #pragma unroll
     for (int s = 0; s < 4; ++s)
 #pragma unroll
-      for (int jj = 0; jj < 4; ++jj) xv[s][jj] = bld128(rx, xoff[s] + kb + 64 * jj);
+      for (int jj = 0; jj < 4; ++jj) xv[s][jj] = bld128s(rx, xoff[s] + 64 * jj, kb);
     TileSlots t0 = slots;
     t0.left = owned;
     int a, r;
@@ -483,10 +355,11 @@ __device__ __forceinline__ void shrink_tile(const AdapterParams& p, int b) {
       const rsrc_t ra = make_rsrc(p.A + (size_t)a * p.a_stride, (uint32_t)p.R * p.K * 2);
       u32x4 av[2][4];
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
+      for (int t = 0; t < 2; ++t) {
+        const uint32_t ao = 16 * t + lr < r ? aoff + (uint32_t)t * 32 * p.K : kOOB;
 #pragma unroll
-        for (int jj = 0; jj < 4; ++jj)
-          av[t][jj] = bld128(ra, 16 * t + lr < r ? (uint32_t)(32 * rg + 16 * t + lr) * p.K * 2 + 16 * lg + kb + 64 * jj : kOOB);
+        for (int jj = 0; jj < 4; ++jj) av[t][jj] = bld128s(ra, ao + 64 * jj, kb);
+      }
 #pragma unroll
       for (int s = 0; s < 4; ++s) {
         const uint32_t st = (uint32_t)(toks >> (16 * s)) & 0xFFFFu;
@@ -546,7 +419,7 @@ __device__ __forceinline__ void expand_tile(const AdapterParams& p, int b, char*
   // in place with no residual, only the tokens of a slot change
   const bool live = m0 + lr < p.M && (!p.add || p.res || all.rank > 0);
   if (p.add && !p.res && !all.left) return;
-  const bool vec = (p.R & 7) == 0 && (p.b_stride & 7) == 0;
+  const RowLanes lanes(p);
   const int n_beg = chunk * 64 * p.rpw, n_end = min(p.N, n_beg + 64 * p.rpw);
 
   struct Item {
@@ -579,7 +452,7 @@ __device__ __forceinline__ void expand_tile(const AdapterParams& p, int b, char*
   };
   auto load = [&](const Item& t, u32x4 (&bf)[4]) {
     const rsrc_t rb = make_rsrc(p.B + (size_t)t.a * p.b_stride, t.r > 0 ? (uint32_t)p.N * p.R * 2 : 0u);
-    load_rows<DT>(p, rb, t.n, t.kk, t.r, vec, bf);
+    load_rows(p, lanes, rb, t.n, t.kk, t.r, bf);
   };
   Item cur;
   cur.n = n_beg;
@@ -596,7 +469,7 @@ __device__ __forceinline__ void expand_tile(const AdapterParams& p, int b, char*
     advance(nxt);
     if (nxt.n < n_end) load(nxt, nx);
     if (cur.r > 0) {
-      if (vec && (cur.r & 7)) mask_rows(cur.kk, cur.r, bf);
+      if (lanes.vec && (cur.r & 7)) mask_rows(cur.kk, cur.r, bf);
       u32x4 hi, lo;
       float sc;
       parts.get(16 * wave + lr, cur.kk, hi, lo, sc);
@@ -624,61 +497,6 @@ __device__ __forceinline__ void expand_tile(const AdapterParams& p, int b, char*
 }
 
 // ---------------------------------------------------------------------------
-// decode, slots of few ranks: u and the term in one launch
-// ---------------------------------------------------------------------------
-
-// Every workgroup of a leader forms u over all of K (eight waves, K shared out)
-// and then its own rows of the term: A is read once per row chunk, from L2
-// after the first, in place of a second launch and the slices' round trip. The
-// chain of dependent accesses is ids, then the slot's A, B, rank and scale all
-// together (rows and columns past the slot's rank are read and dropped).
-template <int DT>
-__device__ __forceinline__ void adapt_local(const AdapterParams& p, int b, char* smem) {
-  __shared__ __attribute__((aligned(16))) float red[8][2][256];
-  __shared__ __attribute__((aligned(16))) float u[16][kAdapterLocalR + 4];
-  __shared__ __attribute__((aligned(16))) uint16_t xs[8][4 * kXRow];
-  __shared__ int stok[16];
-  const int lane = threadIdx.x & 63, lr = lane & 15;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int m = b / p.chunks, chunk = b - m * p.chunks;
-  const TokenGroup g = token_group(p, m, stok);
-  if (g.cnt == 0) return;
-  const int a = max(g.a, 0), n0 = chunk * 512 * p.rpw, n1 = min(p.N, n0 + 512 * p.rpw);
-  const rsrc_t rx = make_rsrc(p.x, (uint32_t)p.M * p.K * 2);
-  const rsrc_t ra = make_rsrc(p.A + (size_t)a * p.a_stride, (uint32_t)p.R * p.K * 2);
-  const int r = rank_of(p, g.a);
-  const float sc = p.scale ? p.scale[a] : 1.f;
-  const int IT = p.K / kIterK, iw = (IT + 7) >> 3, ib = min(IT, wave * iw), ie = min(IT, ib + iw);
-  SlotTerm<DT> term(p, g.a, lr < g.cnt, g.tok, n0 + 64 * wave);
-  const int top = g.a < 0 ? 0 : p.R;  // no rank in the addresses: nothing waits for it
-  for (int j0 = 0; j0 < top; j0 += 32) {
-    f32x4 acc[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
-    project<DT>(rx, g, stok, xs[wave], ra, p.K, j0, top, ib, ie, acc);
-    if (j0 > 0) __syncthreads();
-#pragma unroll
-    for (int t = 0; t < 2; ++t) *(f32x4*)(red[wave][t] + 4 * lane) = acc[t];
-    __syncthreads();
-    // thread (t, l) sums one token's four ranks over half of the waves
-    const int t = (threadIdx.x >> 6) & 1, half = threadIdx.x >> 7;
-    if (half < 1) {
-      f32x4 s = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int w = 0; w < 8; ++w) s += *(const f32x4*)(red[w][t] + 4 * lane);
-      const int j = j0 + 16 * t + 4 * (lane >> 4);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) s[e] = j + e < r ? sc * s[e] : 0.f;
-      *(f32x4*)&u[lr][j] = s;
-    }
-  }
-  const Parts parts(smem, 16, p.RG);
-  if (r > 0) {  // uniform
-    __syncthreads();
-    build_parts<DT>(parts, 16, [&](int t, int j) { return *(const f32x4*)&u[t][j]; });
-  }
-  term.rows(n1, 512, r, parts);
-}
-
-// ---------------------------------------------------------------------------
 // kernels: up to kGroupMax layers a launch, each with workgroups of its own
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ int member(const int (&start)[kGroupMax + 1], int n, int b) {
@@ -693,14 +511,13 @@ __device__ __forceinline__ int member(const int (&start)[kGroupMax + 1], int n, 
 // dependent load ahead of everything else)
 template <int DT, int KIND>
 __device__ __forceinline__ void shrink_body(const AdapterParams& p, int b) {
+  extern __shared__ __attribute__((aligned(16))) char smem[];
   if constexpr (KIND == ADAPT_TILES) shrink_tile<DT>(p, b);
-  else shrink_group<DT>(p, b);
+  else shrink_slot<DT>(p, b, smem);
 }
 template <int DT, int KIND>
 __device__ __forceinline__ void expand_body(const AdapterParams& p, int b, char* smem) {
-  if constexpr (KIND == ADAPT_LOCAL) {
-    adapt_local<DT>(p, b, smem);
-  } else if constexpr (KIND == ADAPT_TILES) {
+  if constexpr (KIND == ADAPT_TILES) {
     expand_tile<DT>(p, b, smem);
   } else {
     __shared__ int stok[16];
@@ -727,12 +544,12 @@ __global__ __launch_bounds__(256) void k_adapter_shrink_group(AdapterGroup g) {
   shrink_body<DT, KIND>(g.p[i], blockIdx.x - g.shrink_start[i]);
 }
 template <int DT, int KIND>
-__global__ __launch_bounds__(KIND == ADAPT_LOCAL ? 512 : 256) void k_adapter_expand(AdapterParams p) {
+__global__ __launch_bounds__(256) void k_adapter_expand(AdapterParams p) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
   expand_body<DT, KIND>(p, blockIdx.x, smem);
 }
 template <int DT, int KIND>
-__global__ __launch_bounds__(KIND == ADAPT_LOCAL ? 512 : 256) void k_adapter_expand_group(AdapterGroup g) {
+__global__ __launch_bounds__(256) void k_adapter_expand_group(AdapterGroup g) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
   const int i = member(g.expand_start, g.n, blockIdx.x);
   expand_body<DT, KIND>(g.p[i], blockIdx.x - g.expand_start[i], smem);
@@ -741,12 +558,13 @@ __global__ __launch_bounds__(KIND == ADAPT_LOCAL ? 512 : 256) void k_adapter_exp
 // ---------------------------------------------------------------------------
 // launcher
 // ---------------------------------------------------------------------------
+// the members of one kind (they share its launches), their workgroups placed
 template <int KIND>
-static hipError_t launch_kind(const AdapterGroup& all, hipStream_t st) {
+static AdapterGroup of_kind(const AdapterGroup& all, size_t* parts_lds) {
   AdapterGroup g;
   g.n = 0;
   g.shrink_start[0] = g.expand_start[0] = 0;
-  size_t lds = 0;
+  *parts_lds = 0;
   for (int i = 0; i < all.n; ++i) {
     const AdapterParams& p = all.p[i];
     if (p.kind != KIND) continue;
@@ -754,33 +572,43 @@ static hipError_t launch_kind(const AdapterGroup& all, hipStream_t st) {
     g.p[g.n] = p;
     g.shrink_start[g.n + 1] = g.shrink_start[g.n] + units * p.PA * p.P * p.RG;
     g.expand_start[g.n + 1] = g.expand_start[g.n] + units * p.chunks;
-    lds = std::max(lds, (size_t)T * ((32 * p.RG + 8) * 4 + p.RG * 4));
+    *parts_lds = std::max(*parts_lds, (size_t)T * ((32 * p.RG + 8) * 4 + p.RG * 4));
     ++g.n;
   }
+  return g;
+}
+template <class F, class P>
+static hipError_t go(F kern, const P& p, int grid, size_t lds, hipStream_t st) {
+  hipError_t err = allow_lds(kern, lds);
+  if (err != hipSuccess) return err;
+  hipLaunchKernelGGL(kern, dim3(grid), dim3(256), lds, st, p);
+  return hipGetLastError();
+}
+template <int KIND>
+static hipError_t shrink_kind(const AdapterGroup& all, hipStream_t st) {
+  size_t lds;
+  const AdapterGroup g = of_kind<KIND>(all, &lds);
   if (g.n == 0) return hipSuccess;
-  const auto go = [&](auto kern, const auto& p, int grid, int block, size_t bytes) {
-    hipError_t err = allow_lds(kern, bytes);
-    if (err != hipSuccess) return err;
-    hipLaunchKernelGGL(kern, dim3(grid), dim3(block), bytes, st, p);
-    return hipGetLastError();
-  };
-  const int gs = g.shrink_start[g.n], ge = g.expand_start[g.n];
-  if constexpr (KIND != ADAPT_LOCAL) {
-    const hipError_t err = g.n == 1 ? go(k_adapter_shrink<DTC, KIND>, g.p[0], gs, 256, 0)
-                                    : go(k_adapter_shrink_group<DTC, KIND>, g, gs, 256, 0);
-    if (err != hipSuccess) return err;
-  }
-  constexpr int block = KIND == ADAPT_LOCAL ? 512 : 256;
-  return g.n == 1 ? go(k_adapter_expand<DTC, KIND>, g.p[0], ge, block, lds)
-                  : go(k_adapter_expand_group<DTC, KIND>, g, ge, block, lds);
+  lds = KIND == ADAPT_TILES ? 0 : shrink_slot_lds(4);
+  return g.n == 1 ? go(k_adapter_shrink<DTC, KIND>, g.p[0], g.shrink_start[1], lds, st)
+                  : go(k_adapter_shrink_group<DTC, KIND>, g, g.shrink_start[g.n], lds, st);
+}
+template <int KIND>
+static hipError_t expand_kind(const AdapterGroup& all, hipStream_t st) {
+  size_t lds;
+  const AdapterGroup g = of_kind<KIND>(all, &lds);
+  if (g.n == 0) return hipSuccess;
+  return g.n == 1 ? go(k_adapter_expand<DTC, KIND>, g.p[0], g.expand_start[1], lds, st)
+                  : go(k_adapter_expand_group<DTC, KIND>, g, g.expand_start[g.n], lds, st);
 }
 
-hipError_t SPEAR_D(launch_adapters)(const AdapterGroup& all, hipStream_t st) {
-  // members of one kind share its launches
-  hipError_t err = launch_kind<ADAPT_LOCAL>(all, st);
-  if (err == hipSuccess) err = launch_kind<ADAPT_SLOTS>(all, st);
-  if (err == hipSuccess) err = launch_kind<ADAPT_TILES>(all, st);
-  return err;
+hipError_t SPEAR_D(launch_adapter_shrink)(const AdapterGroup& all, hipStream_t st) {
+  const hipError_t err = shrink_kind<ADAPT_SLOTS>(all, st);
+  return err != hipSuccess ? err : shrink_kind<ADAPT_TILES>(all, st);
+}
+hipError_t SPEAR_D(launch_adapter_expand)(const AdapterGroup& all, hipStream_t st) {
+  const hipError_t err = expand_kind<ADAPT_SLOTS>(all, st);
+  return err != hipSuccess ? err : expand_kind<ADAPT_TILES>(all, st);
 }
 
 }  // namespace spear

@@ -1223,20 +1223,21 @@ spear_status_t check_tail(const spear_problem_t* prob, const void* x, const spea
 
 // The adapter data of one member in the workspace: the K-slices of its
 // coordinates and its term d, the residual that its layer call adds. `post`: the
-// term is added to the layer's output instead, in place. That is where the
-// layer runs k_gemm_ws on 256 x 256 tiles, whose epilogue with a residual costs
-// more than another pass over the output (8B gate, 14336 x 4096 at 2048 tokens,
-// fp16: 282 us with one, 240 without; the pass reads and writes 117 MB).
+// term is added to the layer's output instead, in place. That is where
+// - the layer runs k_gemm_ws on 256 x 256 tiles, whose epilogue with a residual
+//   costs more than another pass over the output (8B gate, 14336 x 4096 at 2048
+//   tokens, fp16: 282 us with one, 240 without; the pass reads and writes 117 MB);
+// - the layer is one GEMV launch that can carry the coordinates along as further
+//   workgroups (`rides`): decode calls are latency, and this takes the first of
+//   the adapters' two launches off their path.
 struct AdapterLayout {
   bool on = false;  // the member has tokens, rows and adapters
-  bool post = false;
+  bool post = false, rides = false;
   size_t upart = 0, d = 0;
   AdapterParams p;        // the launch shape
 };
 
 constexpr int64_t kAdapterDecodeM = 64;  // tokens whose ids one wave holds, a lane each
-constexpr int64_t kAdapterLocalA = 512 << 10;   // ADAPT_LOCAL: bytes of a slot's A
-constexpr int64_t kAdapterRestage = 64 << 20;   // and of A over all workgroups
 
 // The launch shape of one member, by its own sizes alone.
 void adapters_shape(const spear_problem_t* p, const spear_adapters_t* a, AdapterParams* q) {
@@ -1246,19 +1247,10 @@ void adapters_shape(const spear_problem_t* p, const spear_adapters_t* a, Adapter
   q->P = q->PA = 1;
   q->ips = IT;
   if (M <= kAdapterDecodeM) {
-    // one launch, eight waves and 512 rows (or more) a workgroup, while the
-    // slots' A, read again for each row chunk, stay small
-    const int64_t a_bytes = 2 * a->rank * p->K;
-    q->rpw = 1;
-    while (M * cdiv(p->N, 512 * q->rpw) > 512 && q->rpw < 8) q->rpw *= 2;
-    q->chunks = (int)cdiv(p->N, 512 * q->rpw);
-    q->kind = a->rank <= kAdapterLocalR && a_bytes <= kAdapterLocalA && M * q->chunks * a_bytes <= kAdapterRestage
-                  ? ADAPT_LOCAL
-                  : ADAPT_SLOTS;
-    if (q->kind == ADAPT_LOCAL) return;
-    // one workgroup of four waves for each token (those that lead no slot's
-    // tokens end at once), rank group and K-slice; K-slices of at least one
-    // pass of the waves while the leaders alone leave CUs idle
+    q->kind = ADAPT_SLOTS;
+    // one workgroup for each token (those that lead no slot's tokens end at
+    // once), rank group and K-slice; K-slices of at
+    // least eight iterations while the leaders alone leave CUs idle
     int P = 1;
     while (M * q->RG * P < 256 && IT / (2 * P) >= 8) P *= 2;
     q->ips = (int)cdiv(IT, P);
@@ -1300,8 +1292,9 @@ spear_status_t adapters_layout(int32_t n, const spear_layer_call_t* calls, const
     adapters_shape(p, a, &al[i].p);
     const AdapterParams& q = al[i].p;
     al[i].upart = off;
-    if (q.kind != ADAPT_LOCAL) off += round256((size_t)q.P * p->M * 32 * q.RG * 4);
-    al[i].post = q.kind == ADAPT_TILES && !z[i].gemv && z[i].groles == 3;
+    off += round256((size_t)q.P * p->M * 32 * q.RG * 4);
+    al[i].rides = q.kind == ADAPT_SLOTS && group_epi(z[i], calls[i].ec) >= 0 && z[i].MT <= 2 && z[i].nst == 2;
+    al[i].post = al[i].rides || (q.kind == ADAPT_TILES && !z[i].gemv && z[i].groles == 3);
     al[i].d = off;
     if (!al[i].post) off += round256((size_t)p->M * p->N * 2);
   }
@@ -1336,47 +1329,69 @@ bool hits_adapters(const void* y, size_t yb, const spear_problem_t* p, const spe
          overlaps(y, yb, a->ids, M * 4) || overlaps(y, yb, a->ranks, L * 4) || overlaps(y, yb, a->scale, L * 4);
 }
 
-// The adapters' launches of the members before (post false) or after their
-// layers: the term plus the residual res[i] in the workspace, out[i] (untouched
-// for the others); or both added to y. Members of one activation dtype share
-// launches.
-spear_status_t run_adapters(int32_t n, const spear_layer_call_t* calls, const spear_adapters_t* const* ads,
-                            const AdapterLayout* al, bool post, const uint16_t* const* res, char* ws,
-                            const uint16_t** out, hipStream_t s) {
-  for (int dt : {SPEAR_F16, SPEAR_BF16}) {
-    AdapterGroup g;
-    std::memset(&g, 0, sizeof(g));
-    for (int i = 0; i < n; ++i) {
-      const spear_problem_t* p = calls[i].prob;
-      if (!al[i].on || al[i].post != post || p->act_dtype != dt) continue;
-      const spear_adapters_t* a = ads[i];
-      AdapterParams& q = g.p[g.n++];
-      q = al[i].p;
-      q.x = (const uint16_t*)calls[i].x;
-      q.A = (const uint16_t*)a->A;
-      q.B = (const uint16_t*)a->B;
-      q.a_stride = a_stride_of(p, a);
-      q.b_stride = b_stride_of(p, a);
-      q.ids = a->ids;
-      q.ranks = a->ranks;
-      q.scale = a->scale;
-      q.res = res[i];
-      q.upart = (float*)(ws + al[i].upart);
-      q.d = post ? (uint16_t*)calls[i].y : (uint16_t*)(ws + al[i].d);
-      q.add = post;
-      q.M = (int)p->M;
-      q.N = (int)p->N;
-      q.K = (int)p->K;
-      q.L = a->n_adapters;
-      q.R = a->rank;
-      if (!post) out[i] = q.d;
-    }
-    if (g.n == 0) continue;
-    const spear_status_t st = hip_status(SPEAR_BY_DT(launch_adapters, dt)(g, s));
-    if (st != SPEAR_OK) return st;
-  }
-  return SPEAR_OK;
+// One member's adapters; res: the residual that goes with its term, or null.
+AdapterParams make_adapters(const spear_layer_call_t& c, const spear_adapters_t* a, const AdapterLayout& al,
+                            const uint16_t* res, char* ws) {
+  AdapterParams q = al.p;
+  q.x = (const uint16_t*)c.x;
+  q.A = (const uint16_t*)a->A;
+  q.B = (const uint16_t*)a->B;
+  q.a_stride = a_stride_of(c.prob, a);
+  q.b_stride = b_stride_of(c.prob, a);
+  q.ids = a->ids;
+  q.ranks = a->ranks;
+  q.scale = a->scale;
+  q.res = res;
+  q.upart = (float*)(ws + al.upart);
+  q.d = al.post ? (uint16_t*)c.y : (uint16_t*)(ws + al.d);
+  q.add = al.post;
+  q.M = (int)c.prob->M;
+  q.N = (int)c.prob->N;
+  q.K = (int)c.prob->K;
+  q.L = a->n_adapters;
+  q.R = a->rank;
+  return q;
 }
+
+// The adapters of a call's members: their launches around those of the layers.
+struct AdapterCall {
+  int32_t n = 0;  // members (0: a call without adapters)
+  const spear_layer_call_t* calls = nullptr;
+  AdapterLayout al[SPEAR_GROUP_MAX];
+  AdapterParams p[SPEAR_GROUP_MAX];  // of the members that are on
+
+  // members by `pick`, those of one activation dtype in one launch each
+  template <class Pick, class Launch>
+  spear_status_t each(Pick pick, Launch launch) const {
+    for (int dt : {SPEAR_F16, SPEAR_BF16}) {
+      AdapterGroup g;
+      std::memset(&g, 0, sizeof(g));
+      for (int i = 0; i < n; ++i)
+        if (al[i].on && calls[i].prob->act_dtype == dt && pick(i)) g.p[g.n++] = p[i];
+      if (g.n == 0) continue;
+      const spear_status_t st = hip_status(launch(dt, g));
+      if (st != SPEAR_OK) return st;
+    }
+    return SPEAR_OK;
+  }
+  spear_status_t expand(bool post, hipStream_t s) const {
+    return each([&](int i) { return al[i].post == post; }, [&](int dt, const AdapterGroup& g) {
+      return SPEAR_BY_DT(launch_adapter_expand, dt)(g, s);
+    });
+  }
+  // before the layers: the coordinates of all members but those that ride, and
+  // the terms that enter the layers as residuals, res[i]
+  spear_status_t before(const bool* rides, const uint16_t** res, hipStream_t s) const {
+    const spear_status_t st = each([&](int i) { return !rides[i]; }, [&](int dt, const AdapterGroup& g) {
+      return SPEAR_BY_DT(launch_adapter_shrink, dt)(g, s);
+    });
+    if (st != SPEAR_OK) return st;
+    for (int i = 0; i < n; ++i)
+      if (al[i].on && !al[i].post) res[i] = p[i].d;
+    return expand(false, s);
+  }
+  spear_status_t after(hipStream_t s) const { return expand(true, s); }
+};
 
 }  // namespace
 
@@ -1633,9 +1648,9 @@ spear_status_t spear_group_launches(int32_t n, const spear_layer_call_t* calls, 
   return SPEAR_OK;
 }
 
-// The launches of a grouped call after its checks; res: the members' residuals.
+// The launches of a grouped call after its checks.
 static spear_status_t run_group(int32_t n, const spear_layer_call_t* calls, Resolved* z, const size_t* off,
-                                const uint16_t* const* res, char* ws, hipStream_t s) {
+                                const AdapterCall& ad, char* ws, hipStream_t s) {
   spear_status_t st = SPEAR_OK;
   // Members of one single-launch GEMV variant share one launch; the other
   // members run one after another on the same stream, as their own calls
@@ -1645,6 +1660,13 @@ static spear_status_t run_group(int32_t n, const spear_layer_call_t* calls, Reso
   const int n_in = group_select(n, calls, z, in, &epi, &first);
   int set[SPEAR_GROUP_MAX], ec_set[SPEAR_GROUP_MAX], gv_set[SPEAR_GROUP_MAX];
   shared_sets(n, calls, z, in, set, ec_set, gv_set);
+  // the coordinates of adapters go with the shared GEMV launch, or first
+  const uint16_t* res[SPEAR_GROUP_MAX] = {};
+  if (ad.n > 0) {
+    bool rides[SPEAR_GROUP_MAX];
+    for (int i = 0; i < n; ++i) rides[i] = in[i] && ad.al[i].rides;
+    if ((st = ad.before(rides, res, s)) != SPEAR_OK) return st;
+  }
   // members that share nothing: each as its own call would run, in the
   // workspace a single call would use
   for (int i = 0; i < n; ++i) {
@@ -1781,6 +1803,12 @@ static spear_status_t run_group(int32_t n, const spear_layer_call_t* calls, Reso
   }
   g.n = k;
   const Resolved& z0 = z[first];
+  AdapterGroup a;
+  a.n = 0;
+  for (int i = 0; i < ad.n; ++i)
+    if (in[i] && ad.al[i].on && ad.al[i].rides) a.p[a.n++] = ad.p[i];
+  if (a.n > 0)
+    return hip_status(SPEAR_BY_WB(launch_gemv_adapt, z0.wb, z0.dt)(z0.MT, z0.RT, epi, g, a, 64 * z0.NW, lds, s));
   return hip_status(SPEAR_BY_WB(launch_gemv_group, z0.wb, z0.dt)(z0.MT, z0.RT, epi, g, 64 * z0.NW, lds, s));
 }
 
@@ -1793,8 +1821,8 @@ static spear_status_t group_call(int32_t n, const spear_layer_call_t* calls,
   size_t off[SPEAR_GROUP_MAX], total = 0;
   spear_status_t st = group_resolve(n, calls, z, off, &total);
   if (st != SPEAR_OK) return st;
-  AdapterLayout al[SPEAR_GROUP_MAX];
-  if (ads && (st = adapters_layout(n, calls, ads, z, al, &total)) != SPEAR_OK) return st;
+  AdapterCall ad;
+  if (ads && (st = adapters_layout(n, calls, ads, z, ad.al, &total)) != SPEAR_OK) return st;
   if (total > 0) {
     if (!workspace || workspace_bytes < total) return SPEAR_E_WORKSPACE;
     if (misaligned(workspace)) return SPEAR_E_ALIGN;
@@ -1824,12 +1852,16 @@ static spear_status_t group_call(int32_t n, const spear_layer_call_t* calls,
         return SPEAR_E_ALIAS;
   }
   hipStream_t s = (hipStream_t)hip_stream;
-  const uint16_t* res[SPEAR_GROUP_MAX] = {};
-  const uint16_t* none[SPEAR_GROUP_MAX] = {};
-  if (ads && (st = run_adapters(n, calls, ads, al, false, none, (char*)workspace, res, s)) != SPEAR_OK) return st;
-  if ((st = run_group(n, calls, z, off, res, ws, s)) != SPEAR_OK) return st;
-  return ads ? run_adapters(n, calls, ads, al, true, none, (char*)workspace, res, s) : SPEAR_OK;
+  if (ads) {
+    ad.n = n;
+    ad.calls = calls;
+    for (int i = 0; i < n; ++i)
+      if (ad.al[i].on) ad.p[i] = make_adapters(calls[i], ads[i], ad.al[i], nullptr, ws);
+  }
+  st = run_group(n, calls, z, off, ad, ws, s);
+  return st != SPEAR_OK ? st : ad.after(s);
 }
+
 spear_status_t spear_w4ec_linear_group(int32_t n, const spear_layer_call_t* calls, void* workspace,
                                        size_t workspace_bytes, void* hip_stream) {
   return group_call(n, calls, nullptr, workspace, workspace_bytes, hip_stream);
@@ -1868,8 +1900,8 @@ spear_status_t spear_w4ec_linear_adapters(const spear_problem_t* prob, const voi
   size_t off[SPEAR_GROUP_MAX], total = 0;
   spear_status_t st = group_resolve(1, &call, z, off, &total);
   if (st != SPEAR_OK) return st;
-  AdapterLayout al[SPEAR_GROUP_MAX];
-  if ((st = adapters_layout(1, &call, &adapters, z, al, &total)) != SPEAR_OK) return st;
+  AdapterCall ad;
+  if ((st = adapters_layout(1, &call, &adapters, z, ad.al, &total)) != SPEAR_OK) return st;
   if (tail && (!std::isfinite(tail->eps) || tail->eps < 0.f)) return SPEAR_E_SHAPE;
   if (prob->M == 0 || prob->N == 0) return SPEAR_OK;
   if ((st = check_w4(prob, x, w, y)) != SPEAR_OK) return st;
@@ -1887,12 +1919,38 @@ spear_status_t spear_w4ec_linear_adapters(const spear_problem_t* prob, const voi
   }
   hipStream_t s = (hipStream_t)hip_stream;
   const uint16_t* res = tail ? (const uint16_t*)tail->residual : nullptr;
-  const uint16_t *none = nullptr, *in = res;  // what the layer adds
-  if ((st = run_adapters(1, &call, &adapters, al, false, &res, (char*)workspace, &in, s)) != SPEAR_OK) return st;
-  // (the residual goes with the term added afterwards, unless y itself holds it)
-  const bool later = al[0].on && al[0].post && res != y;
-  st = run_layer(prob, z[0], x, w, ec, y, later ? nullptr : in, (char*)workspace, s);
-  if (st == SPEAR_OK) st = run_adapters(1, &call, &adapters, al, true, later ? &res : &none, (char*)workspace, &in, s);
+  char* ws = (char*)workspace;
+  ad.n = 1;
+  ad.calls = &call;
+  const AdapterLayout& al = ad.al[0];
+  // the residual goes with the term, except where that comes after the layer and
+  // y itself holds the residual
+  const bool with_term = al.on && (!al.post || res != y);
+  if (al.on) ad.p[0] = make_adapters(call, adapters, al, with_term ? res : nullptr, ws);
+  const uint16_t* in = with_term ? nullptr : res;  // what the layer adds
+  const bool rides = al.on && al.rides;
+  if ((st = ad.before(&rides, &in, s)) != SPEAR_OK) return st;
+  if (rides) {
+    const int epi = group_epi(z[0], ec);
+    GemvGroup g;
+    std::memset(&g, 0, sizeof(g));
+    g.p[0] = make_gemv(prob, z[0], x, w, y, z[0].ec ? ec : nullptr, ws);
+    g.p[0].res = in;
+    if (z[0].ec) {
+      g.p[0].ec = make_ec(prob, z[0], x, ec, ws);
+      if (z[0].S > 1) g.p[0].eupart = (float*)(ws + z[0].off_eupart);
+    }
+    g.start[1] = z[0].nrg * z[0].S;
+    g.n = 1;
+    AdapterGroup a;
+    a.p[0] = ad.p[0];
+    a.n = 1;
+    st = hip_status(SPEAR_BY_WB(launch_gemv_adapt, z[0].wb, z[0].dt)(z[0].MT, z[0].RT, epi, g, a, 64 * z[0].NW,
+                                                                     z[0].lds_gemv, s));
+  } else {
+    st = run_layer(prob, z[0], x, w, ec, y, in, ws, s);
+  }
+  if (st == SPEAR_OK) st = ad.after(s);
   if (st != SPEAR_OK || !tail || !tail->norm_w) return st;
   return hip_status(SPEAR_BY_DT(launch_rmsnorm, z[0].dt)((const uint16_t*)y, (const uint16_t*)tail->norm_w,
                                    tail->eps, (uint16_t*)tail->y_norm, (int)prob->M, (int)prob->N, s));

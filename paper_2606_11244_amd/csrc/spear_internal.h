@@ -226,7 +226,7 @@ struct AdapterParams {
   const uint16_t* res;    // [M][N] residual, or null
   uint16_t* d;            // [M][N] the term plus the residual, act dtype
   int add;                // d += that instead (in place: the layer's output)
-  float* upart;           // [P][M][32 RG] K-slices of the coordinates A_a x (all but ADAPT_LOCAL)
+  float* upart;           // [P][M][32 RG] K-slices of the coordinates A_a x
   int64_t a_stride, b_stride;
   int M, N, K, L, R;
   int RG;                 // rank groups of 32
@@ -235,11 +235,9 @@ struct AdapterParams {
   int PA;                 // ADAPT_TILES: parts that share a tile's slots (u)
   int chunks, rpw;        // row chunks of the term, runs of 64 rows a wave in each
 };
-enum { ADAPT_LOCAL = 0,  // a leader's tokens, u and the term in one launch
-       ADAPT_SLOTS = 1,  // a leader's tokens, u and the term in two
-       ADAPT_TILES = 2   // 64 consecutive tokens, in two
+enum { ADAPT_SLOTS = 0,  // the tokens of one slot (up to 64 tokens)
+       ADAPT_TILES = 1   // 64 consecutive tokens
 };
-constexpr int kAdapterLocalR = 64;  // ADAPT_LOCAL: the largest rank
 struct AdapterGroup {
   AdapterParams p[kGroupMax];
   int shrink_start[kGroupMax + 1], expand_start[kGroupMax + 1];  // first workgroups
@@ -309,6 +307,8 @@ __host__ __device__ inline size_t ec_block_lds(int NW, int R1p, int h, int r) {
                              int block, size_t lds, hipStream_t st);                            \
   hipError_t launch_gemv_group_##W(int MT, int RT, int epi, const GemvGroup& g, int block,      \
                                    size_t lds, hipStream_t st);                                 \
+  hipError_t launch_gemv_adapt_##W(int MT, int RT, int epi, const GemvGroup& g,                 \
+                                   const AdapterGroup& a, int block, size_t lds, hipStream_t st); \
   hipError_t launch_gemm_##W(int epi, const GemmParams& p, hipStream_t st);                      \
   hipError_t launch_mid_##W(int MT, const GemmGroup& g, hipStream_t st);
 #define SPEAR_ACT_LAUNCHERS(D)                                                                    \
@@ -320,7 +320,8 @@ __host__ __device__ inline size_t ec_block_lds(int NW, int R1p, int h, int r) {
   hipError_t launch_ec_up_acc_##D(const float* v, const uint16_t* B, const int8_t* B8,           \
                                   const float* sb, uint16_t* y, int M, int N, int r,             \
                                   hipStream_t st);                                               \
-  hipError_t launch_adapters_##D(const AdapterGroup& g, hipStream_t st);                         \
+  hipError_t launch_adapter_shrink_##D(const AdapterGroup& g, hipStream_t st);                   \
+  hipError_t launch_adapter_expand_##D(const AdapterGroup& g, hipStream_t st);                   \
   hipError_t launch_block_norm_##D(const BlockNormParams& p, hipStream_t st);                    \
   SPEAR_WEIGHT_LAUNCHERS(w4_##D)                                                                 \
   SPEAR_WEIGHT_LAUNCHERS(w3_##D)

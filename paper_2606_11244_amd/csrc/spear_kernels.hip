@@ -15,7 +15,7 @@
 //   k_gate, k_ec_up_acc   the naive split chain's separate gate and
 //              reprojection+accumulate launches
 //   k_rmsnorm  post-EC tail
-#include "spear_device.h"
+#include "spear_adapters.h"
 
 namespace spear {
 
@@ -1432,6 +1432,29 @@ __global__ __launch_bounds__(kGemvMaxThreads, gemv_min_waves(MT, RT, EPI)) void 
   gemv_body<DT, MT, RT, EPI, WB, 2, SPLIT>(g.p[i], b - g.start[i], 0u, smem);
 }
 
+// The same with the coordinates of decode adapters (spear_adapters.h) as the
+// grid's first workgroups: the two read the same x, neither waits for the
+// other, and the term is formed from both by a later launch.
+template <int DT, int MT, int RT, int EPI, int WB, bool SPLIT>
+__global__ __launch_bounds__(kGemvMaxThreads, gemv_min_waves(MT, RT, EPI)) void k_gemv_adapt(GemvGroup g,
+                                                                                            AdapterGroup a) {
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  int b = blockIdx.x, i = 0;
+  const int na = a.shrink_start[a.n];
+  if (b < na) {
+#pragma unroll
+    for (int j = 1; j < kGroupMax; ++j)
+      if (j < a.n && b >= a.shrink_start[j]) i = j;
+    shrink_slot<DT>(a.p[i], b - a.shrink_start[i], smem);
+    return;
+  }
+  b -= na;
+#pragma unroll
+  for (int j = 1; j < kGroupMax; ++j)
+    if (j < g.n && b >= g.start[j]) i = j;
+  gemv_body<DT, MT, RT, EPI, WB, 2, SPLIT>(g.p[i], b - g.start[i], 0u, smem);
+}
+
 // ---------------------------------------------------------------------------
 // launchers
 // ---------------------------------------------------------------------------
@@ -1583,23 +1606,75 @@ static hipError_t gemv_group_launch(int epi, const GemvGroup& g, int block, size
 #undef SPEAR_GEMV_GROUP_GO
 }
 
-hipError_t SPEAR_W(launch_gemv_group)(int MT, int RT, int epi, const GemvGroup& g,
-                                      int block, size_t lds, hipStream_t st) {
-  if (g.n < 1 || g.n > kGroupMax || g.start[0] != 0) return hipErrorInvalidValue;
+static bool gemv_group_ok(int epi, const GemvGroup& g) {
+  if (g.n < 1 || g.n > kGroupMax || g.start[0] != 0) return false;
   const bool loc = epi == EPI_LOCAL || epi == EPI_LOCAL_I8;
   for (int i = 0; i < g.n; ++i) {
     const GemvParams& p = g.p[i];
     if (g.start[i + 1] < g.start[i] || p.S < 1 ||
         (p.S > 1 && (!p.ypart || !p.rb_ctr || (loc && !p.eupart))) ||
         (epi == EPI_LOCAL_I8 && (!p.ec.A8 || !p.ec.sa || !p.B8 || !p.sb)))
-      return hipErrorInvalidValue;
+      return false;
   }
+  return true;
+}
+
+hipError_t SPEAR_W(launch_gemv_group)(int MT, int RT, int epi, const GemvGroup& g,
+                                      int block, size_t lds, hipStream_t st) {
+  if (!gemv_group_ok(epi, g)) return hipErrorInvalidValue;
   if (g.start[g.n] == 0) return hipSuccess;
 #define SPEAR_GEMV_GROUP_CASE(mt, rt) \
   if (MT == mt && RT == rt)  \
     return gemv_group_launch<DTC, mt, rt>(epi, g, block, lds, st);
   SPEAR_GEMV_SHAPES(SPEAR_GEMV_GROUP_CASE)
 #undef SPEAR_GEMV_GROUP_CASE
+  return hipErrorInvalidValue;
+}
+
+// The GEMV with adapters' coordinates: up to two token tiles, the product alone
+// and the local EC variants.
+template <int DT, int MT, int RT>
+static hipError_t gemv_adapt_launch(int epi, const GemvGroup& g, const AdapterGroup& a, int block, size_t lds,
+                                    hipStream_t st) {
+  constexpr int WB = SPEAR_WB;
+  bool split = MT > 1;
+  for (int i = 0; i < g.n; ++i) split |= g.p[i].S > 1;
+  lds = std::max(lds, shrink_slot_lds(block / 64));
+  const auto go = [&](auto kern) {
+    hipError_t err = allow_lds(kern, lds);
+    if (err != hipSuccess) return err;
+    hipLaunchKernelGGL(kern, dim3(a.shrink_start[a.n] + g.start[g.n]), dim3(block), lds, st, g, a);
+    return hipGetLastError();
+  };
+#define SPEAR_GEMV_ADAPT_GO(E) \
+  case E: return split ? go(k_gemv_adapt<DT, MT, RT, E, WB, true>) : go(k_gemv_adapt<DT, MT, RT, E, WB, MT != 1>);
+  switch (epi) {
+    SPEAR_GEMV_ADAPT_GO(EPI_NONE)
+    SPEAR_GEMV_ADAPT_GO(EPI_LOCAL)
+    SPEAR_GEMV_ADAPT_GO(EPI_LOCAL_I8)
+    default: return hipErrorInvalidValue;
+  }
+#undef SPEAR_GEMV_ADAPT_GO
+}
+
+hipError_t SPEAR_W(launch_gemv_adapt)(int MT, int RT, int epi, const GemvGroup& g, const AdapterGroup& all,
+                                      int block, size_t lds, hipStream_t st) {
+  if (!gemv_group_ok(epi, g) || all.n < 1 || all.n > kGroupMax) return hipErrorInvalidValue;
+  AdapterGroup a = all;
+  a.shrink_start[0] = 0;
+  for (int i = 0; i < a.n; ++i) {
+    if (a.p[i].kind != ADAPT_SLOTS || a.p[i].M > 64) return hipErrorInvalidValue;
+    a.shrink_start[i + 1] = a.shrink_start[i] + a.p[i].M * a.p[i].P * a.p[i].RG;
+  }
+#define SPEAR_GEMV_ADAPT_CASE(mt, rt) \
+  if (MT == mt && RT == rt) return gemv_adapt_launch<DTC, mt, rt>(epi, g, a, block, lds, st);
+  SPEAR_GEMV_ADAPT_CASE(1, 1)
+  SPEAR_GEMV_ADAPT_CASE(1, 2)
+  SPEAR_GEMV_ADAPT_CASE(1, 4)
+  SPEAR_GEMV_ADAPT_CASE(2, 1)
+  SPEAR_GEMV_ADAPT_CASE(2, 2)
+  SPEAR_GEMV_ADAPT_CASE(2, 4)
+#undef SPEAR_GEMV_ADAPT_CASE
   return hipErrorInvalidValue;
 }
 
