@@ -1433,22 +1433,22 @@ __global__ __launch_bounds__(kGemvMaxThreads, gemv_min_waves(MT, RT, EPI)) void 
 }
 
 // The same with the coordinates of decode adapters (spear_adapters.h) as the
-// grid's first workgroups: the two read the same x, neither waits for the
+// grid's last workgroups: the two read the same x, neither waits for the
 // other, and the term is formed from both by a later launch.
 template <int DT, int MT, int RT, int EPI, int WB, bool SPLIT>
 __global__ __launch_bounds__(kGemvMaxThreads, gemv_min_waves(MT, RT, EPI)) void k_gemv_adapt(GemvGroup g,
                                                                                             AdapterGroup a) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
   int b = blockIdx.x, i = 0;
-  const int na = a.shrink_start[a.n];
-  if (b < na) {
+  const int ng = g.start[g.n];
+  if (b >= ng) {
+    b -= ng;
 #pragma unroll
     for (int j = 1; j < kGroupMax; ++j)
       if (j < a.n && b >= a.shrink_start[j]) i = j;
     shrink_slot<DT>(a.p[i], b - a.shrink_start[i], smem);
     return;
   }
-  b -= na;
 #pragma unroll
   for (int j = 1; j < kGroupMax; ++j)
     if (j < g.n && b >= g.start[j]) i = j;
