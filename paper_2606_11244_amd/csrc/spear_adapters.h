@@ -1,5 +1,6 @@
-// The coordinates of the decode adapters (spear_adapters.hip), which a GEMV
-// launch may carry along as further workgroups.
+// What other kernels share with the adapters' own (spear_adapters.hip): tokens and
+// slots, the decode coordinates, which a GEMV launch may carry along as further
+// workgroups, and the two parts in which the coordinates enter an MFMA.
 #pragma once
 
 #include "spear_device.h"
@@ -192,5 +193,26 @@ __device__ __forceinline__ void shrink_slot(const AdapterParams& p, int b, char*
     if (tok < g.cnt) *(f32x4*)(p.upart + ((size_t)ks * p.M + stok[tok]) * (32 * p.RG) + j) = s;
   }
 }
+
+// ---------------------------------------------------------------------------
+// the parts of u
+// ---------------------------------------------------------------------------
+
+// The two activation-dtype parts of a coordinate. fp16 has neither the range
+// nor, for small values, the precision: where the largest of the 32 coordinates
+// of a token and rank group is not between 1/2 and 2^15, they are first scaled
+// by a power of two that brings it near 2^14, undone on the fp32 result of
+// their MFMA.
+template <int DT>
+__device__ __forceinline__ void split_parts(float v, uint16_t* hi, uint16_t* lo) {
+  *hi = f2act<DT>(v);
+  const float h = act2f<DT>(*hi);
+  *lo = __builtin_fabsf(h) < __builtin_inff() ? f2act<DT>(v - h) : (uint16_t)0;
+}
+__device__ __forceinline__ int scale_exp(float maxabs) {  // k: the values times 2^k
+  const int e = (int)((__float_as_uint(maxabs) >> 23) & 255) - 127;
+  return e == 128 || (e >= -1 && e <= 14) ? 0 : min(max(14 - e, -113), 100);
+}
+__device__ __forceinline__ float exp2i(int k) { return __uint_as_float((uint32_t)(k + 127) << 23); }
 
 }  // namespace spear

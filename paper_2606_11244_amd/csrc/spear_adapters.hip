@@ -31,24 +31,8 @@
 namespace spear {
 
 // ---------------------------------------------------------------------------
-// the parts of u
+// u for the term
 // ---------------------------------------------------------------------------
-
-// The two activation-dtype parts of a coordinate. fp16 has neither the range
-// nor, for small values, the precision: there the 32 coordinates of a token and
-// rank group are first scaled by a power of two that brings the largest near
-// 2^14, undone on the fp32 result of their MFMA.
-template <int DT>
-__device__ __forceinline__ void split_parts(float v, uint16_t* hi, uint16_t* lo) {
-  *hi = f2act<DT>(v);
-  const float h = act2f<DT>(*hi);
-  *lo = __builtin_fabsf(h) < __builtin_inff() ? f2act<DT>(v - h) : (uint16_t)0;
-}
-__device__ __forceinline__ int scale_exp(float maxabs) {  // k: the values times 2^k
-  const int e = (int)((__float_as_uint(maxabs) >> 23) & 255) - 127;
-  return e == 128 ? 0 : min(max(14 - e, -113), 100);
-}
-__device__ __forceinline__ float exp2i(int k) { return __uint_as_float((uint32_t)(k + 127) << 23); }
 
 // The parts of u for the term, in LDS: [T tokens][32 RG + 8] high, the same low,
 // [T][RG] scales.
@@ -507,6 +491,44 @@ __device__ __forceinline__ int member(const int (&start)[kGroupMax + 1], int n, 
   return i;
 }
 
+// The parts of u once, for a GEMM whose tiles each read them: 16 threads a token,
+// four ranks of each 64. The GEMM adds them to the product's own sums, so that
+// small coordinates need no scaling (a part is off by at most 2^-25); large ones
+// in fp16 are divided by a power of two that its weight tile is multiplied by.
+template <int DT>
+__global__ __launch_bounds__(256) void k_adapter_parts(AdapterParams p) {
+  const int m = blockIdx.x * 16 + (threadIdx.x >> 4), q = threadIdx.x & 15, W = 32 * p.RG;
+  const int mm = min(m, p.M - 1), a = slot_of(p, mm), r = rank_of(p, a);
+  const float sc = p.scale && a >= 0 ? p.scale[a] : 1.f;
+  int k = 0;
+  f32x4 v = sum_u(p, mm, min(4 * q, W - 4), r, sc);
+  if constexpr (DT == DT_F16) {
+    float mx = 0.f;
+    f32x4 w = v;
+    for (int j = 4 * q;;) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) mx = __builtin_fabsf(w[e]) < __builtin_inff() ? fmaxf(mx, __builtin_fabsf(w[e])) : mx;
+      j += 64;
+      if (j >= W) break;
+      w = sum_u(p, mm, j, r, sc);
+    }
+#pragma unroll
+    for (int h = 8; h > 0; h >>= 1) mx = fmaxf(mx, __shfl_xor(mx, h));
+    k = max(0, (int)(__float_as_uint(mx) >> 23) - 127 - 14);
+  }
+  if (m >= p.M) return;
+  if (q == 0) p.ukx[m] = k;
+  for (int j = 4 * q; j < W; j += 64) {
+    if (j >= 64) v = sum_u(p, mm, j, r, sc);
+    uint16_t h[4], l[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) split_parts<DT>(v[e] * exp2i(-k), &h[e], &l[e]);
+    const size_t at = (size_t)m * W + j;
+    *(u32x2*)(p.uh + at) = u32x2{h[0] | ((uint32_t)h[1] << 16), h[2] | ((uint32_t)h[3] << 16)};
+    *(u32x2*)(p.ul + at) = u32x2{l[0] | ((uint32_t)l[1] << 16), l[2] | ((uint32_t)l[3] << 16)};
+  }
+}
+
 // (a single member's call passes its parameters alone: the table's lookup is a
 // dependent load ahead of everything else)
 template <int DT, int KIND>
@@ -605,6 +627,10 @@ static hipError_t expand_kind(const AdapterGroup& all, hipStream_t st) {
 hipError_t SPEAR_D(launch_adapter_shrink)(const AdapterGroup& all, hipStream_t st) {
   const hipError_t err = shrink_kind<ADAPT_SLOTS>(all, st);
   return err != hipSuccess ? err : shrink_kind<ADAPT_TILES>(all, st);
+}
+hipError_t SPEAR_D(launch_adapter_parts)(const AdapterParams& p, hipStream_t st) {
+  hipLaunchKernelGGL(k_adapter_parts<DTC>, dim3((p.M + 15) / 16), dim3(256), 0, st, p);
+  return hipGetLastError();
 }
 hipError_t SPEAR_D(launch_adapter_expand)(const AdapterGroup& all, hipStream_t st) {
   const hipError_t err = expand_kind<ADAPT_SLOTS>(all, st);

@@ -1221,20 +1221,26 @@ spear_status_t check_tail(const spear_problem_t* prob, const void* x, const spea
 
 // ---- adapters ---------------------------------------------------------------
 
+// How a member's term joins its layer:
+// - ADAPT_BEFORE: formed first, in the workspace (d), with the tail's residual,
+//   it enters the layer as the residual of its final store;
+// - ADAPT_RIDES: the coordinates go with the layer's GEMV launch as further
+//   workgroups, and a launch after it adds the term to y. Where the layer is one
+//   GEMV launch: decode calls are latency, and this takes the first of the
+//   adapters' two launches off their path (8B q, k, v at 16 requests: 13.2 us for
+//   the launch, 12.9 without adapters, 4.8 for the coordinates alone);
+// - ADAPT_EPILOGUE: k_gemm_ws on 256 x 256 tiles forms it. Its epilogue with a
+//   residual costs as much as another pass over the output (8B gate and up,
+//   14336 x 4096 at 2048 tokens, fp16: 617 us with the term first, 574 with a pass
+//   after it that also rounds y once more).
+enum { ADAPT_BEFORE = 0, ADAPT_RIDES = 1, ADAPT_EPILOGUE = 2 };
 // The adapter data of one member in the workspace: the K-slices of its
-// coordinates and its term d, the residual that its layer call adds. `post`: the
-// term is added to the layer's output instead, in place. That is where
-// - the layer runs k_gemm_ws on 256 x 256 tiles, whose epilogue with a residual
-//   costs more than another pass over the output (8B gate, 14336 x 4096 at 2048
-//   tokens, fp16: 282 us with one, 240 without; the pass reads and writes 117 MB);
-// - the layer is one GEMV launch that can carry the coordinates along as further
-//   workgroups (`rides`): decode calls are latency, and this takes the first of
-//   the adapters' two launches off their path.
+// coordinates, their parts (ADAPT_EPILOGUE), its term d (ADAPT_BEFORE).
 struct AdapterLayout {
   bool on = false;  // the member has tokens, rows and adapters
-  bool post = false, rides = false;
-  size_t upart = 0, d = 0;
-  AdapterParams p;        // the launch shape
+  int join = ADAPT_BEFORE;
+  size_t upart = 0, uh = 0, ul = 0, ukx = 0, d = 0;
+  AdapterParams p;  // the launch shape
 };
 
 constexpr int64_t kAdapterDecodeM = 64;  // tokens whose ids one wave holds, a lane each
@@ -1291,12 +1297,22 @@ spear_status_t adapters_layout(int32_t n, const spear_layer_call_t* calls, const
     std::memset(&al[i].p, 0, sizeof(al[i].p));
     adapters_shape(p, a, &al[i].p);
     const AdapterParams& q = al[i].p;
-    al[i].upart = off;
-    off += round256((size_t)q.P * p->M * 32 * q.RG * 4);
-    al[i].rides = q.kind == ADAPT_SLOTS && group_epi(z[i], calls[i].ec) >= 0 && z[i].MT <= 2 && z[i].nst == 2;
-    al[i].post = al[i].rides || (q.kind == ADAPT_TILES && !z[i].gemv && z[i].groles == 3);
-    al[i].d = off;
-    if (!al[i].post) off += round256((size_t)p->M * p->N * 2);
+    auto take = [&](size_t bytes) {
+      const size_t o = off;
+      off += round256(bytes);
+      return o;
+    };
+    al[i].join = q.kind == ADAPT_SLOTS && group_epi(z[i], calls[i].ec) >= 0 && z[i].MT <= 2 && z[i].nst == 2 ? ADAPT_RIDES
+                 : q.kind == ADAPT_TILES && !z[i].gemv && !z[i].ec && z[i].groles == 3                      ? ADAPT_EPILOGUE
+                                                                                                           : ADAPT_BEFORE;
+    const size_t uw = (size_t)p->M * 32 * q.RG;
+    al[i].upart = take(q.P * uw * 4);
+    if (al[i].join == ADAPT_EPILOGUE) {
+      al[i].uh = take(uw * 2);
+      al[i].ul = take(uw * 2);
+      al[i].ukx = take((size_t)p->M * 4);
+    }
+    if (al[i].join == ADAPT_BEFORE) al[i].d = take((size_t)p->M * p->N * 2);
   }
   if (any) *total = off;
   return SPEAR_OK;
@@ -1343,8 +1359,13 @@ AdapterParams make_adapters(const spear_layer_call_t& c, const spear_adapters_t*
   q.scale = a->scale;
   q.res = res;
   q.upart = (float*)(ws + al.upart);
-  q.d = al.post ? (uint16_t*)c.y : (uint16_t*)(ws + al.d);
-  q.add = al.post;
+  q.add = al.join == ADAPT_RIDES;
+  q.d = q.add ? (uint16_t*)c.y : (uint16_t*)(ws + al.d);
+  if (al.join == ADAPT_EPILOGUE) {
+    q.uh = (uint16_t*)(ws + al.uh);
+    q.ul = (uint16_t*)(ws + al.ul);
+    q.ukx = (int*)(ws + al.ukx);
+  }
   q.M = (int)c.prob->M;
   q.N = (int)c.prob->N;
   q.K = (int)c.prob->K;
@@ -1374,23 +1395,34 @@ struct AdapterCall {
     }
     return SPEAR_OK;
   }
-  spear_status_t expand(bool post, hipStream_t s) const {
-    return each([&](int i) { return al[i].post == post; }, [&](int dt, const AdapterGroup& g) {
+  spear_status_t expand(int join, hipStream_t s) const {
+    return each([&](int i) { return al[i].join == join; }, [&](int dt, const AdapterGroup& g) {
       return SPEAR_BY_DT(launch_adapter_expand, dt)(g, s);
     });
   }
-  // before the layers: the coordinates of all members but those that ride, and
-  // the terms that enter the layers as residuals, res[i]
+  // before the layers: the coordinates of all members but those that ride along,
+  // and the terms that enter the layers as residuals, res[i]
   spear_status_t before(const bool* rides, const uint16_t** res, hipStream_t s) const {
-    const spear_status_t st = each([&](int i) { return !rides[i]; }, [&](int dt, const AdapterGroup& g) {
+    spear_status_t st = each([&](int i) { return !rides[i]; }, [&](int dt, const AdapterGroup& g) {
       return SPEAR_BY_DT(launch_adapter_shrink, dt)(g, s);
     });
+    for (int i = 0; i < n && st == SPEAR_OK; ++i)
+      if (al[i].on && al[i].join == ADAPT_EPILOGUE)
+        st = hip_status(SPEAR_BY_DT(launch_adapter_parts, calls[i].prob->act_dtype)(p[i], s));
     if (st != SPEAR_OK) return st;
     for (int i = 0; i < n; ++i)
-      if (al[i].on && !al[i].post) res[i] = p[i].d;
-    return expand(false, s);
+      if (al[i].on && al[i].join == ADAPT_BEFORE) res[i] = p[i].d;
+    return expand(ADAPT_BEFORE, s);
   }
-  spear_status_t after(hipStream_t s) const { return expand(true, s); }
+  spear_status_t after(hipStream_t s) const { return expand(ADAPT_RIDES, s); }
+  // the layer of a member that shares no launch
+  spear_status_t layer(int i, const Resolved& z, const uint16_t* res, char* ws, hipStream_t s) const {
+    const spear_layer_call_t& c = calls[i];
+    if (!al[i].on || al[i].join != ADAPT_EPILOGUE) return run_layer(c.prob, z, c.x, c.w, c.ec, c.y, res, ws, s);
+    GemmParams g = make_gemm(c.prob, z, c.x, c.w, c.y, nullptr, ws);
+    g.res = res;
+    return hip_status(SPEAR_BY_WB(launch_gemm_adapt, z.wb, z.dt)(g, p[i], s));
+  }
 };
 
 }  // namespace
@@ -1664,7 +1696,7 @@ static spear_status_t run_group(int32_t n, const spear_layer_call_t* calls, Reso
   const uint16_t* res[SPEAR_GROUP_MAX] = {};
   if (ad.n > 0) {
     bool rides[SPEAR_GROUP_MAX];
-    for (int i = 0; i < n; ++i) rides[i] = in[i] && ad.al[i].rides;
+    for (int i = 0; i < n; ++i) rides[i] = in[i] && ad.al[i].join == ADAPT_RIDES;
     if ((st = ad.before(rides, res, s)) != SPEAR_OK) return st;
   }
   // members that share nothing: each as its own call would run, in the
@@ -1672,7 +1704,7 @@ static spear_status_t run_group(int32_t n, const spear_layer_call_t* calls, Reso
   for (int i = 0; i < n; ++i) {
     const spear_layer_call_t& c = calls[i];
     if (in[i] || set[i] >= 0 || ec_set[i] >= 0 || c.prob->M == 0 || c.prob->N == 0) continue;
-    st = run_layer(c.prob, z[i], c.x, c.w, c.ec, c.y, res[i], ws, s);
+    st = ad.n > 0 ? ad.layer(i, z[i], res[i], ws, s) : run_layer(c.prob, z[i], c.x, c.w, c.ec, c.y, nullptr, ws, s);
     if (st != SPEAR_OK) return st;
   }
   // the shared EC pre-kernels, then the 4-bit products that add their
@@ -1806,7 +1838,7 @@ static spear_status_t run_group(int32_t n, const spear_layer_call_t* calls, Reso
   AdapterGroup a;
   a.n = 0;
   for (int i = 0; i < ad.n; ++i)
-    if (in[i] && ad.al[i].on && ad.al[i].rides) a.p[a.n++] = ad.p[i];
+    if (in[i] && ad.al[i].on && ad.al[i].join == ADAPT_RIDES) a.p[a.n++] = ad.p[i];
   if (a.n > 0)
     return hip_status(SPEAR_BY_WB(launch_gemv_adapt, z0.wb, z0.dt)(z0.MT, z0.RT, epi, g, a, 64 * z0.NW, lds, s));
   return hip_status(SPEAR_BY_WB(launch_gemv_group, z0.wb, z0.dt)(z0.MT, z0.RT, epi, g, 64 * z0.NW, lds, s));
@@ -1923,12 +1955,12 @@ spear_status_t spear_w4ec_linear_adapters(const spear_problem_t* prob, const voi
   ad.n = 1;
   ad.calls = &call;
   const AdapterLayout& al = ad.al[0];
-  // the residual goes with the term, except where that comes after the layer and
-  // y itself holds the residual
-  const bool with_term = al.on && (!al.post || res != y);
+  // the residual goes with the term, except where the layer's epilogue forms that,
+  // or where it comes after the layer and y itself holds the residual
+  const bool rides = al.on && al.join == ADAPT_RIDES;
+  const bool with_term = al.on && (al.join == ADAPT_BEFORE || (rides && res != y));
   if (al.on) ad.p[0] = make_adapters(call, adapters, al, with_term ? res : nullptr, ws);
   const uint16_t* in = with_term ? nullptr : res;  // what the layer adds
-  const bool rides = al.on && al.rides;
   if ((st = ad.before(&rides, &in, s)) != SPEAR_OK) return st;
   if (rides) {
     const int epi = group_epi(z[0], ec);
@@ -1948,7 +1980,7 @@ spear_status_t spear_w4ec_linear_adapters(const spear_problem_t* prob, const voi
     st = hip_status(SPEAR_BY_WB(launch_gemv_adapt, z[0].wb, z[0].dt)(z[0].MT, z[0].RT, epi, g, a, 64 * z[0].NW,
                                                                      z[0].lds_gemv, s));
   } else {
-    st = run_layer(prob, z[0], x, w, ec, y, in, ws, s);
+    st = ad.layer(0, z[0], in, ws, s);
   }
   if (st == SPEAR_OK) st = ad.after(s);
   if (st != SPEAR_OK || !tail || !tail->norm_w) return st;

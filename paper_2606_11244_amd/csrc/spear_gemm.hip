@@ -5,7 +5,7 @@
 //              epilogue adding B v from the EC pre-kernel, or with the EC
 //              projected by its own waves
 //   k_gemm_ws  the same product with loading and multiplying waves
-#include "spear_device.h"
+#include "spear_adapters.h"
 
 namespace spear {
 
@@ -516,9 +516,19 @@ __global__ __launch_bounds__(128 * TMW, TMW == 2 ? 2 : 1) void k_gemm(GemmParams
 // tokens 70.4 us against 75.3, at 4096 136 against 149, but with a residual 94
 // against 77; 4096 x 4096 at 2048 tokens on 256 x 128 tiles 81 against 79).
 // ---------------------------------------------------------------------------
+//
+// EPI_ADAPT: the tokens' adapters are further steps of the same loop, so that the
+// multiplying waves have no code of their own for them (accumulators that live
+// through another loop spilled, 672 bytes a lane): for each slot that the tile's
+// tokens name and each 64 of its ranks, the loading waves store the high and then
+// the low parts of the tokens' coordinates (zero for the other tokens) as the
+// activation tile and the slot's rows of B as the weight tile. What is not finite
+// in B is kept out, since zero times it would reach the other tokens; a further
+// step then has one rank, with the largest finite value as the factor of the
+// slot's tokens and of the rows of B in question: infinite in y.
 template <int DT, int EPI, int TNB, int WB, bool PLAIN>
-__global__ __launch_bounds__(256 * (1 + TNB), 1) void k_gemm_ws(GemmParams a) {
-  static_assert(EPI == EPI_NONE || EPI == EPI_READY, "plain and semi-fused epilogues");
+__device__ __forceinline__ void gemm_ws_body(const GemmParams& a, const AdapterParams& ad) {
+  static_assert(EPI == EPI_NONE || EPI == EPI_READY || EPI == EPI_ADAPT, "plain, semi-fused and adapter epilogues");
   extern __shared__ __attribute__((aligned(16))) char smem[];
   constexpr int TM = 256, TN = kGemmTN * TNB, LR = kGemmLdsRow;
   constexpr int TILEX = TM * kGemmTK, TILEW = TN * LR;
@@ -601,6 +611,14 @@ __global__ __launch_bounds__(256 * (1 + TNB), 1) void k_gemm_ws(GemmParams a) {
     }
   };
 
+  // EPI_ADAPT, after the stages: the tokens' slots (-1: none) and the power of two
+  // that their coordinates were divided by, the steps at which a row of B was not
+  // finite ([TN]: any row's), and whether buffer b holds a further step
+  int* sid = (int*)(Ws + 2 * TILEW);  // [TM]
+  int* skx = sid + TM;                // [TM]
+  int* sbad = skx + TM;               // [TN + 1]
+  int* smore = sbad + TN + 1;         // [2]
+
   if (wave >= NCW) {
     // ---- loading waves: thread pt stages, of each 64-wide step, the codes
     // of K half pt % 2 of row pt / 2 (TNB = 1) or both halves of row pt
@@ -652,6 +670,115 @@ __global__ __launch_bounds__(256 * (1 + TNB), 1) void k_gemm_ws(GemmParams a) {
         }
       }
     };
+    // EPI_ADAPT: the next further step into buffer buf; false: there is none
+    int id[4], kx[4];
+    uint64_t left[4] = {0, 0, 0, 0};
+    int slot = -1, k2 = 0, r = 0, kr0 = 0, part = 0, astep = 0;
+    bool more = false;
+    if constexpr (EPI == EPI_ADAPT) {
+      const int m = m0 + pt, s = m < M ? slot_of(ad, m) : -1;  // (TM loading threads)
+      const bool on = rank_of(ad, s) > 0;
+      sid[pt] = on ? s : -1;
+      skx[pt] = on && DT == DT_F16 ? ad.ukx[m] : 0;
+      for (int t = pt; t <= TN; t += 256) sbad[t] = -1;
+    }
+    auto adapt_begin = [&]() {  // (a barrier after the above)
+      const int ln = pt & 63;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        id[q] = sid[64 * q + ln];
+        kx[q] = skx[64 * q + ln];
+        left[q] = __ballot(id[q] >= 0);
+      }
+    };
+    auto adapt_step = [&](int buf) -> bool {
+      constexpr uint32_t kExp = DT == DT_F16 ? 0x7C00u : 0x7F80u, kMax = kExp - 1;  // the largest finite value
+      uint16_t* xs = Xs + buf * TILEX;
+      uint16_t* ws = Ws + buf * TILEW;
+      if (part == 2) {  // both parts of these ranks are done
+        if (sbad[TN] == astep) {  // (uniform) the factors of what is not finite
+          for (int c = pt; c < TM * 8; c += 256) {
+            const int t = c >> 3;
+            *(u32x4*)(xs + t * kGemmTK + 8 * ((c & 7) ^ (t & 7))) =
+                u32x4{(c & 7) == 0 && sid[t] == slot && skx[t] == k2 ? kMax : 0u, 0u, 0u, 0u};
+          }
+          for (int c = pt; c < TN * 8; c += 256)
+            *(u32x4*)(ws + (c >> 3) * LR + 8 * (c & 7)) = u32x4{(c & 7) == 0 && sbad[c >> 3] == astep ? kMax : 0u, 0u, 0u, 0u};
+          part = 3;
+          return true;
+        }
+        part = 3;
+      }
+      if (part == 3) {
+        part = 0;
+        kr0 += 64;
+        ++astep;
+      }
+      if (part == 0 && kr0 >= r) {  // the next slot
+        if (!(left[0] | left[1] | left[2] | left[3])) return false;
+#pragma unroll
+        for (int q = 3; q >= 0; --q)
+          if (left[q]) {
+            const int l = __builtin_ctzll(left[q]);
+            slot = __builtin_amdgcn_readlane(id[q], l);
+            k2 = __builtin_amdgcn_readlane(kx[q], l);
+          }
+#pragma unroll
+        for (int q = 0; q < 4; ++q) left[q] &= ~__ballot(id[q] == slot && kx[q] == k2);
+        r = rank_of(ad, slot);
+        kr0 = 0;
+      }
+      const int W = 32 * ad.RG;
+      const uint16_t* u = part ? ad.ul : ad.uh;
+      const uint16_t* B = ad.B + (size_t)slot * ad.b_stride;
+      const bool vec = (ad.R & 7) == 0 && (ad.b_stride & 7) == 0;
+      u32x4 xv[8], wv[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int c = pt + 256 * i, t = c >> 3, col = kr0 + 8 * (c & 7);
+        xv[i] = u32x4{0, 0, 0, 0};
+        if (sid[t] == slot && skx[t] == k2 && col < W) xv[i] = ldg16(u + (size_t)(m0 + t) * W + col);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int c = pt + 256 * i, n = n0 + (c >> 3), col = kr0 + 8 * (c & 7);
+        wv[i] = u32x4{0, 0, 0, 0};
+        if (n < N && col < r) {
+          const uint16_t* br = B + (size_t)n * ad.R + col;
+          if (vec && col + 8 <= r) {
+            wv[i] = ldg16(br);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              if (col + e < r) wv[i][e >> 1] |= (uint32_t)br[e] << (16 * (e & 1));
+          }
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int c = pt + 256 * i, t = c >> 3;
+        *(u32x4*)(xs + t * kGemmTK + 8 * ((c & 7) ^ (t & 7))) = xv[i];
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int c = pt + 256 * i, row = c >> 3;
+        bool bad = false;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          if (DT == DT_F16 && k2 > 0) {  // (uniform) what the coordinates were divided by
+            const float f = exp2i(k2);
+            wv[i][q] = (uint32_t)f2act<DT>(f * act2f<DT>(wv[i][q] & 0xFFFFu)) |
+                       ((uint32_t)f2act<DT>(f * act2f<DT>(wv[i][q] >> 16)) << 16);
+          }
+          if ((wv[i][q] & kExp) == kExp) bad = true, wv[i][q] &= 0xFFFF0000u;
+          if ((wv[i][q] >> 16 & kExp) == kExp) bad = true, wv[i][q] &= 0xFFFFu;
+        }
+        if (bad) sbad[row] = sbad[TN] = astep;
+        *(u32x4*)(ws + row * LR + 8 * (c & 7)) = wv[i];
+      }
+      ++part;
+      return true;
+    };
     // step kt stores step kt + 1 (loaded two steps earlier) and then loads
     // step kt + 3 into the same registers; loads past the end re-read the
     // last step (never stored), so that every load is unconditional
@@ -670,8 +797,19 @@ __global__ __launch_bounds__(256 * (1 + TNB), 1) void k_gemm_ws(GemmParams a) {
       if (kt + 2 < KT) {
         lstore(g0, 0);
         gload(g0, min(kt + 4, kl));
+      } else if constexpr (EPI == EPI_ADAPT) {
+        adapt_begin();
+        more = adapt_step(0);
+        if (pt == 0) smore[0] = more;
       }
       __syncthreads();
+    }
+    if constexpr (EPI == EPI_ADAPT) {
+      for (int b = 1; more; b ^= 1) {
+        more = adapt_step(b);
+        if (pt == 0) smore[b] = more;
+        __syncthreads();
+      }
     }
     if constexpr (EPI == EPI_READY) {
       for (int kr0 = 0; kr0 < a.vstride; kr0 += 64) {
@@ -751,7 +889,8 @@ __global__ __launch_bounds__(256 * (1 + TNB), 1) void k_gemm_ws(GemmParams a) {
   __syncthreads();
   // one copy of the step's MFMAs in the loop (two copies, one per buffer,
   // make the register allocator shuffle accumulators between them)
-  for (int kt = 0; kt < KT; ++kt) {
+  int end = KT;  // (EPI_ADAPT: moves on while the loading waves have further steps)
+  for (int kt = 0; kt < end; ++kt) {
     if (kt + 1 < KT) xdma(kt + 1, (kt + 1) & 1);
     const uint16_t* xs = Xs + (kt & 1) * TILEX;
     const uint16_t* ws = Ws + (kt & 1) * TILEW;
@@ -759,6 +898,8 @@ __global__ __launch_bounds__(256 * (1 + TNB), 1) void k_gemm_ws(GemmParams a) {
     for (int kk = 0; kk < kGemmTK; kk += 16) mma(xs, ws, wm * 128, wn * 64, LR, kk, true);
     __builtin_amdgcn_s_waitcnt(0);  // this wave's share of the next tile is in LDS
     __syncthreads();
+    if constexpr (EPI == EPI_ADAPT)
+      if (kt + 1 >= KT && __builtin_amdgcn_readfirstlane(smore[(kt + 1) & 1])) end = kt + 2;
   }
 
   if constexpr (EPI == EPI_READY) {
@@ -808,9 +949,33 @@ __global__ __launch_bounds__(256 * (1 + TNB), 1) void k_gemm_ws(GemmParams a) {
   }
 }
 
+template <int DT, int EPI, int TNB, int WB, bool PLAIN>
+__global__ __launch_bounds__(256 * (1 + TNB), 1) void k_gemm_ws(GemmParams a) {
+  gemm_ws_body<DT, EPI, TNB, WB, PLAIN>(a, AdapterParams{});
+}
+template <int DT, int WB, bool PLAIN>
+__global__ __launch_bounds__(768, 1) void k_gemm_ws_adapt(GemmParams a, AdapterParams ad) {
+  gemm_ws_body<DT, EPI_ADAPT, 2, WB, PLAIN>(a, ad);
+}
+
 // ---------------------------------------------------------------------------
 // launchers
 // ---------------------------------------------------------------------------
+hipError_t SPEAR_W(launch_gemm_adapt)(const GemmParams& p, const AdapterParams& ad, hipStream_t st) {
+  if (p.tmw != 4 || p.S != 1 || p.roles != 3 || !ad.uh || !ad.ul || !ad.ukx || ad.M != p.M || ad.N != p.N)
+    return hipErrorInvalidValue;
+  const unsigned grid = (unsigned)(((p.M + 255) / 256) * ((p.N + 255) / 256));
+  if (grid == 0) return hipSuccess;
+  const size_t lds = (size_t)2 * 256 * kGemmTK * 2 + (size_t)2 * 256 * kGemmLdsRow * 2 + (3 * 256 + 4) * 4;
+  const auto go = [&](auto kern) {
+    hipError_t err = allow_lds(kern, lds);
+    if (err != hipSuccess) return err;
+    hipLaunchKernelGGL(kern, dim3(grid), dim3(768), lds, st, p, ad);
+    return hipGetLastError();
+  };
+  return p.res ? go(k_gemm_ws_adapt<DTC, SPEAR_WB, false>) : go(k_gemm_ws_adapt<DTC, SPEAR_WB, true>);
+}
+
 hipError_t SPEAR_W(launch_dequant)(const uint32_t* qw, const uint16_t* sc, const uint8_t* zr,
                                    uint16_t* out, int N, int K, int G, hipStream_t st) {
   const long long nunits = (long long)N * (K / (SPEAR_WB == 4 ? 8 : 32));

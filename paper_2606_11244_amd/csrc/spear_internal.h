@@ -18,6 +18,7 @@ enum { EPI_NONE = 0,   // Y = X W^T
        EPI_LOCAL_I8 = 4  // EPI_LOCAL with INT8 A and B (per-channel fp32 scales)
                        // over their K chunks (small rank), v from it per block
 };
+constexpr int EPI_ADAPT = 5;  // k_gemm_ws: Y = X W^T + the tokens' adapters
 // How the EC projection's K-slices are combined.
 enum { EC_LAST = 0,    // the last slice to arrive sums the partials, applies
                        // the gate and publishes v
@@ -227,6 +228,10 @@ struct AdapterParams {
   uint16_t* d;            // [M][N] the term plus the residual, act dtype
   int add;                // d += that instead (in place: the layer's output)
   float* upart;           // [P][M][32 RG] K-slices of the coordinates A_a x
+  // where the GEMM forms the term: the two act-dtype parts of s_a A_a x [M][32 RG],
+  // and the power of two >= 0 that a token's were divided by [M] (fp16)
+  uint16_t *uh, *ul;
+  int* ukx;
   int64_t a_stride, b_stride;
   int M, N, K, L, R;
   int RG;                 // rank groups of 32
@@ -310,6 +315,7 @@ __host__ __device__ inline size_t ec_block_lds(int NW, int R1p, int h, int r) {
   hipError_t launch_gemv_adapt_##W(int MT, int RT, int epi, const GemvGroup& g,                 \
                                    const AdapterGroup& a, int block, size_t lds, hipStream_t st); \
   hipError_t launch_gemm_##W(int epi, const GemmParams& p, hipStream_t st);                      \
+  hipError_t launch_gemm_adapt_##W(const GemmParams& p, const AdapterParams& ad, hipStream_t st); \
   hipError_t launch_mid_##W(int MT, const GemmGroup& g, hipStream_t st);
 #define SPEAR_ACT_LAUNCHERS(D)                                                                    \
   hipError_t launch_ec_##D(const EcGroup& g, int block, int ipp, size_t lds, hipStream_t st);     \
@@ -322,6 +328,7 @@ __host__ __device__ inline size_t ec_block_lds(int NW, int R1p, int h, int r) {
                                   hipStream_t st);                                               \
   hipError_t launch_adapter_shrink_##D(const AdapterGroup& g, hipStream_t st);                   \
   hipError_t launch_adapter_expand_##D(const AdapterGroup& g, hipStream_t st);                   \
+  hipError_t launch_adapter_parts_##D(const AdapterParams& p, hipStream_t st);                   \
   hipError_t launch_block_norm_##D(const BlockNormParams& p, hipStream_t st);                    \
   SPEAR_WEIGHT_LAUNCHERS(w4_##D)                                                                 \
   SPEAR_WEIGHT_LAUNCHERS(w3_##D)

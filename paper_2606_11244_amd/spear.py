@@ -213,6 +213,12 @@ def _stream(stream):
     return ctypes.c_void_p(stream.cuda_stream)
 
 
+def _raw_stream(stream, device: int) -> int:
+    """The same as an integer: a decode call is a few microseconds, and the
+    current stream's object takes two of them to make."""
+    return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
+
+
 def problem(M, N, K, group_size=0, act_dtype=F16, rank=0, gate_kind=GATE_SIGMOID_LINEAR,
             gate_hidden=0, force_path=PATH_AUTO, weight_bits=0) -> Problem:
     return Problem(int(M), int(N), int(K), int(group_size), int(act_dtype), int(rank),
@@ -345,7 +351,7 @@ def _group_array(members):
     arr = (LayerCall * max(n, 1))()
     keep = []
     for i, m in enumerate(members):
-        w = W4(_ptr(m["qweight"]).value, _ptr(m["scales"]).value, _ptr(m["zeros"]).value)
+        w = W4(m["qweight"].data_ptr(), m["scales"].data_ptr(), m["zeros"].data_ptr())
         ec = _ec_from_args(m["ec_args"]) if m.get("ec_args") is not None else None
         keep += [m["prob"], w, ec]
         arr[i].prob = ctypes.pointer(m["prob"])
@@ -414,17 +420,23 @@ def adapters(A, B, ids, ranks=None, scale=None) -> Adapters:
     a = Adapters(L, r, p(A), p(B), A.stride(0) if far else 0, B.stride(0) if far else 0, p(ranks),
                  p(scale), p(ids))
     a._keep = (A, B, ids, ranks, scale)
+    devs = {t.get_device() for t in a._keep if t is not None}
+    # what a call has to match: K, N, dtype, device, and the tokens there are
+    a._sig = (K, B.shape[1], _dtype_code(A), devs.pop() if len(devs) == 1 else -1)
+    a._tokens = ids.numel()
     return a
 
 
-def _same_device(first, *tensors):
-    """Every tensor on the current GPU: a kernel reads what it is given, and the
-    stream is the current device's."""
-    if not first.is_cuda or first.device.index != torch.cuda.current_device():
+def _device_of(first, *tensors) -> int:
+    """The current GPU, which holds every tensor: a kernel reads what it is
+    given, and the stream is the current device's."""
+    dev = first.get_device()
+    if dev < 0 or dev != torch.cuda.current_device():
         raise ValueError(f"tensors on the current GPU are needed (got {first.device})")
     for t in tensors:
-        if t is not None and t.device != first.device:
+        if t is not None and t.get_device() != dev:
             raise ValueError(f"tensors on one device are needed (got {t.device} beside {first.device})")
+    return dev
 
 
 def _adapters_array(members):
@@ -433,16 +445,13 @@ def _adapters_array(members):
         *[ctypes.pointer(a) if a is not None else None for a in ptrs])
 
 
-def _check_adapters(prob, x, adapters):
+def _check_adapters(prob, dev, adapters):
     """What only the tensors know: the slots' sizes, the tokens' count, the device."""
     if adapters is None:
         return
-    A, B, ids = adapters._keep[:3]
-    _same_device(x, *adapters._keep)
-    if A.shape[2] != prob.K or B.shape[1] != prob.N or ids.numel() < prob.M:
-        raise ValueError("adapters: A [L][r][K], B [L][N][r] and ids [M] of the problem's sizes")
-    if _dtype_code(A) != prob.act_dtype:
-        raise TypeError("adapters: A and B are in the activation dtype")
+    if adapters._sig != (prob.K, prob.N, prob.act_dtype, dev) or adapters._tokens < prob.M:
+        raise ValueError("adapters: A [L][r][K], B [L][N][r] in the activation dtype and ids [M] of the "
+                         f"problem's sizes, on its GPU (K, N, dtype, device: {adapters._sig})")
 
 
 def adapters_workspace(members) -> int:
@@ -462,7 +471,8 @@ def w4ec_linear_adapters(prob: Problem, x, qweight, scales, zeros, adapters, y, 
     """The layer with its tokens' adapters (include/spear.h), and with the
     post-EC tail where a residual or norm_w is given; ec_args as in
     w4ec_linear_tail."""
-    _check_adapters(prob, x, adapters)
+    dev = _device_of(x, qweight, scales, zeros, y)
+    _check_adapters(prob, dev, adapters)
     w = W4(qweight.data_ptr(), scales.data_ptr(), zeros.data_ptr())
     ec = ctypes.byref(_ec_from_args(ec_args)) if ec_args is not None else None
     tail = None
@@ -472,8 +482,9 @@ def w4ec_linear_adapters(prob: Problem, x, qweight, scales, zeros, adapters, y, 
                                  None if y_norm is None else y_norm.data_ptr()))
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     st = LIB.spear_w4ec_linear_adapters(ctypes.byref(prob), x.data_ptr(), ctypes.byref(w), ec,
-                                        ctypes.byref(adapters), tail, y.data_ptr(), _ptr(workspace),
-                                        ws_bytes, _stream(stream))
+                                        ctypes.byref(adapters), tail, y.data_ptr(),
+                                        None if workspace is None else workspace.data_ptr(), ws_bytes,
+                                        _raw_stream(stream, dev))
     if st != 0:
         raise SpearError(st, "spear_w4ec_linear_adapters")
     return y
@@ -482,23 +493,29 @@ def w4ec_linear_adapters(prob: Problem, x, qweight, scales, zeros, adapters, y, 
 def w4ec_linear_adapters_group(members, workspace=None, stream=None):
     """w4ec_linear_group with the adapters of each member's "adapters" entry
     (None: none)."""
+    dev = torch.cuda.current_device()
     for m in members:
-        _check_adapters(m["prob"], m["x"], m.get("adapters"))
+        _device_of(m["x"], m["qweight"], m["scales"], m["zeros"], m["y"])
+        _check_adapters(m["prob"], dev, m.get("adapters"))
     arr, keep = _group_array(members)
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     st = LIB.spear_w4ec_linear_adapters_group(len(members), arr, _adapters_array(members),
-                                              _ptr(workspace), ws_bytes, _stream(stream))
+                                              None if workspace is None else workspace.data_ptr(), ws_bytes,
+                                              _raw_stream(stream, dev))
     if st != 0:
         raise SpearError(st, "spear_w4ec_linear_adapters_group")
 
 
-def _rows(t, M, N, dtypes, what):
-    """Row stride of a [M][N] tensor of dense rows."""
-    if t.dtype not in dtypes:
+def _rows(t, shape, dtype, what):
+    """Row stride of a [M][N] tensor of dense rows (0: M or N tells it)."""
+    if t.dtype is not dtype:
         raise TypeError(f"block_norm: {what} is {t.dtype}")
-    if t.dim() != 2 or t.shape[0] != M or t.shape[1] != N or (N > 1 and M > 0 and t.stride(1) != 1):
-        raise ValueError(f"block_norm: {what} is [{M}][{N}] with dense rows")
-    return t.stride(0) if M > 1 else 0
+    if t.shape != shape:
+        raise ValueError(f"block_norm: {what} is {tuple(shape)}")
+    ld, one = t.stride()
+    if one != 1 and shape[1] > 1 and shape[0] > 0:
+        raise ValueError(f"block_norm: {what} has dense rows")
+    return ld if shape[0] > 1 else 0
 
 
 def block_norm(y, h, h_out, x=None, *, post_w=None, pre_w=None, gate=None, gate_ids=None,
@@ -508,35 +525,33 @@ def block_norm(y, h, h_out, x=None, *, post_w=None, pre_w=None, gate=None, gate_
     branch_scale act(gate) (.) RMSNorm(y; post_w), x = RMSNorm(h_out; pre_w).
     y, h, h_out, x: [M][N], rows of any stride; h (or None) and h_out in the
     activation dtype or fp32; gate [N], [rows][N]; gate_ids [M] int32."""
-    _same_device(y, h, h_out, x, post_w, pre_w, gate, gate_ids)
-    M, N = y.shape
-    dt = _dtype_code(y)
-    f32 = h_out.dtype == torch.float32
-    act, stm = (y.dtype,), (h_out.dtype,)
-    if not f32 and h_out.dtype != y.dtype:
-        raise TypeError(f"block_norm: h_out is {h_out.dtype}")
-    for t, what in ((post_w, "post_w"), (pre_w, "pre_w")):
-        if t is not None and (t.dtype != y.dtype or t.numel() != N or not t.is_contiguous()):
-            raise ValueError(f"block_norm: {what} is [{N}] in the activation dtype")
+    dev = _device_of(y, h, h_out, x, post_w, pre_w, gate, gate_ids)
+    shape, act, stm = y.shape, y.dtype, h_out.dtype
+    M, N = shape
+    f32 = stm is torch.float32
+    if not f32 and stm is not act:
+        raise TypeError(f"block_norm: h_out is {stm}")
+    for t in (post_w, pre_w):
+        if t is not None and (t.dtype is not act or t.numel() != N or not t.is_contiguous()):
+            raise ValueError(f"block_norm: post_w and pre_w are [{N}] in the activation dtype")
     n_gates, gate_ld = 0, 0
     if gate is not None:
         gate = gate.view(1, -1) if gate.dim() == 1 else gate
         n_gates = gate.shape[0]
-        gate_ld = _rows(gate, n_gates, N, act, "gate")
-        if gate_ids is not None and (gate_ids.dtype != torch.int32 or gate_ids.numel() != M or
+        gate_ld = _rows(gate, (n_gates, N), act, "gate")
+        if gate_ids is not None and (gate_ids.dtype is not torch.int32 or gate_ids.numel() != M or
                                      not gate_ids.is_contiguous()):
             raise ValueError(f"block_norm: gate_ids is [{M}] int32")
 
     def p(t):
         return None if t is None else t.data_ptr()
 
-    a = BlockNorm(M, N, dt, STREAM_F32 if f32 else STREAM_ACT, p(y), p(post_w), p(gate),
-                  p(gate_ids), p(h), p(h_out), p(pre_w), p(x), _rows(y, M, N, act, "y"), gate_ld,
-                  _rows(h, M, N, stm, "h") if h is not None else 0, _rows(h_out, M, N, stm, "h_out"),
-                  _rows(x, M, N, act, "x") if x is not None else 0, n_gates,
-                  BLOCK_GATES[gate_kind], float(stream_scale), float(branch_scale),
-                  float(w_offset), float(eps))
-    st = LIB.spear_block_norm(ctypes.byref(a), _stream(stream))
+    a = BlockNorm(M, N, _dtype_code(y), STREAM_F32 if f32 else STREAM_ACT, y.data_ptr(), p(post_w), p(gate),
+                  p(gate_ids), p(h), h_out.data_ptr(), p(pre_w), p(x), _rows(y, shape, act, "y"), gate_ld,
+                  0 if h is None else _rows(h, shape, stm, "h"), _rows(h_out, shape, stm, "h_out"),
+                  0 if x is None else _rows(x, shape, act, "x"), n_gates, BLOCK_GATES[gate_kind],
+                  stream_scale, branch_scale, w_offset, eps)
+    st = LIB.spear_block_norm(ctypes.byref(a), _raw_stream(stream, dev))
     if st != 0:
         raise SpearError(st, "spear_block_norm")
     return h_out
