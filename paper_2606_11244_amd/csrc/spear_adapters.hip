@@ -496,8 +496,10 @@ __device__ __forceinline__ int member(const int (&start)[kGroupMax + 1], int n, 
 // small coordinates need no scaling (a part is off by at most 2^-25); large ones
 // in fp16 are divided by a power of two that its weight tile is multiplied by.
 template <int DT>
-__global__ __launch_bounds__(256) void k_adapter_parts(AdapterParams p) {
-  const int m = blockIdx.x * 16 + (threadIdx.x >> 4), q = threadIdx.x & 15, W = 32 * p.RG;
+__global__ __launch_bounds__(256) void k_adapter_parts(AdapterGroup g) {
+  const int b = member(g.expand_start, g.n, blockIdx.x);
+  const AdapterParams& p = g.p[b];
+  const int m = (blockIdx.x - g.expand_start[b]) * 16 + (threadIdx.x >> 4), q = threadIdx.x & 15, W = 32 * p.RG;
   const int mm = min(m, p.M - 1), a = slot_of(p, mm), r = rank_of(p, a);
   const float sc = p.scale && a >= 0 ? p.scale[a] : 1.f;
   int k = 0;
@@ -628,9 +630,11 @@ hipError_t SPEAR_D(launch_adapter_shrink)(const AdapterGroup& all, hipStream_t s
   const hipError_t err = shrink_kind<ADAPT_SLOTS>(all, st);
   return err != hipSuccess ? err : shrink_kind<ADAPT_TILES>(all, st);
 }
-hipError_t SPEAR_D(launch_adapter_parts)(const AdapterParams& p, hipStream_t st) {
-  hipLaunchKernelGGL(k_adapter_parts<DTC>, dim3((p.M + 15) / 16), dim3(256), 0, st, p);
-  return hipGetLastError();
+hipError_t SPEAR_D(launch_adapter_parts)(const AdapterGroup& all, hipStream_t st) {
+  AdapterGroup g = all;
+  g.expand_start[0] = 0;
+  for (int i = 0; i < g.n; ++i) g.expand_start[i + 1] = g.expand_start[i] + (g.p[i].M + 15) / 16;
+  return go(k_adapter_parts<DTC>, g, g.expand_start[g.n], 0, st);
 }
 hipError_t SPEAR_D(launch_adapter_expand)(const AdapterGroup& all, hipStream_t st) {
   const hipError_t err = expand_kind<ADAPT_SLOTS>(all, st);

@@ -1406,9 +1406,10 @@ struct AdapterCall {
     spear_status_t st = each([&](int i) { return !rides[i]; }, [&](int dt, const AdapterGroup& g) {
       return SPEAR_BY_DT(launch_adapter_shrink, dt)(g, s);
     });
-    for (int i = 0; i < n && st == SPEAR_OK; ++i)
-      if (al[i].on && al[i].join == ADAPT_EPILOGUE)
-        st = hip_status(SPEAR_BY_DT(launch_adapter_parts, calls[i].prob->act_dtype)(p[i], s));
+    if (st == SPEAR_OK)
+      st = each([&](int i) { return al[i].join == ADAPT_EPILOGUE; }, [&](int dt, const AdapterGroup& g) {
+        return SPEAR_BY_DT(launch_adapter_parts, dt)(g, s);
+      });
     if (st != SPEAR_OK) return st;
     for (int i = 0; i < n; ++i)
       if (al[i].on && al[i].join == ADAPT_BEFORE) res[i] = p[i].d;

@@ -520,12 +520,13 @@ __global__ __launch_bounds__(128 * TMW, TMW == 2 ? 2 : 1) void k_gemm(GemmParams
 // EPI_ADAPT: the tokens' adapters are further steps of the same loop, so that the
 // multiplying waves have no code of their own for them (accumulators that live
 // through another loop spilled, 672 bytes a lane): for each slot that the tile's
-// tokens name and each 64 of its ranks, the loading waves store the high and then
-// the low parts of the tokens' coordinates (zero for the other tokens) as the
-// activation tile and the slot's rows of B as the weight tile. What is not finite
-// in B is kept out, since zero times it would reach the other tokens; a further
-// step then has one rank, with the largest finite value as the factor of the
-// slot's tokens and of the rows of B in question: infinite in y.
+// tokens name and each 32 of its ranks, the loading waves store the high and the
+// low parts of the tokens' coordinates side by side (zero for the other tokens)
+// as the activation tile, and the slot's rows of B twice as the weight tile,
+// requested a step ahead. What is not finite in B is kept out, since zero times
+// it would reach the other tokens; a further step then has one rank, with the
+// largest finite value as the factor of the slot's tokens and of the rows of B
+// in question: infinite in y.
 template <int DT, int EPI, int TNB, int WB, bool PLAIN>
 __device__ __forceinline__ void gemm_ws_body(const GemmParams& a, const AdapterParams& ad) {
   static_assert(EPI == EPI_NONE || EPI == EPI_READY || EPI == EPI_ADAPT, "plain, semi-fused and adapter epilogues");
@@ -611,11 +612,12 @@ __device__ __forceinline__ void gemm_ws_body(const GemmParams& a, const AdapterP
     }
   };
 
-  // EPI_ADAPT, after the stages: the tokens' slots (-1: none) and the power of two
-  // that their coordinates were divided by, the steps at which a row of B was not
-  // finite ([TN]: any row's), and whether buffer b holds a further step
+  // EPI_ADAPT, after the stages: the tokens' slots (-1: none), their ranks and the
+  // power of two that their coordinates were divided by; the step at which a row
+  // of B was not finite ([TN]: any row's); whether buffer b holds a further step
   int* sid = (int*)(Ws + 2 * TILEW);  // [TM]
-  int* skx = sid + TM;                // [TM]
+  int* srk = sid + TM;                // [TM]
+  int* skx = srk + TM;                // [TM]
   int* sbad = skx + TM;               // [TN + 1]
   int* smore = sbad + TN + 1;         // [2]
 
@@ -670,81 +672,68 @@ __device__ __forceinline__ void gemm_ws_body(const GemmParams& a, const AdapterP
         }
       }
     };
-    // EPI_ADAPT: the next further step into buffer buf; false: there is none
-    int id[4], kx[4];
+    // EPI_ADAPT: the walk over slots and ranks, the operands of the next step and
+    // what the last one stored was
+    int id[4], rk[4], kx[4];
     uint64_t left[4] = {0, 0, 0, 0};
-    int slot = -1, k2 = 0, r = 0, kr0 = 0, part = 0, astep = 0;
-    bool more = false;
-    if constexpr (EPI == EPI_ADAPT) {
+    int slot = -1, k2 = 0, r = 0, kr0 = 0, pslot = -1, pk2 = 0, nstep = 0;
+    bool have = false;
+    u32x4 xv[8], wv[4];
+    auto adapt_tokens = [&]() {
       const int m = m0 + pt, s = m < M ? slot_of(ad, m) : -1;  // (TM loading threads)
-      const bool on = rank_of(ad, s) > 0;
-      sid[pt] = on ? s : -1;
-      skx[pt] = on && DT == DT_F16 ? ad.ukx[m] : 0;
+      const int n = rank_of(ad, s);
+      sid[pt] = n > 0 ? s : -1;
+      srk[pt] = n;
+      skx[pt] = n > 0 && DT == DT_F16 ? ad.ukx[m] : 0;
       for (int t = pt; t <= TN; t += 256) sbad[t] = -1;
-    }
+    };
     auto adapt_begin = [&]() {  // (a barrier after the above)
       const int ln = pt & 63;
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         id[q] = sid[64 * q + ln];
+        rk[q] = srk[64 * q + ln];
         kx[q] = skx[64 * q + ln];
         left[q] = __ballot(id[q] >= 0);
       }
     };
-    auto adapt_step = [&](int buf) -> bool {
-      constexpr uint32_t kExp = DT == DT_F16 ? 0x7C00u : 0x7F80u, kMax = kExp - 1;  // the largest finite value
-      uint16_t* xs = Xs + buf * TILEX;
-      uint16_t* ws = Ws + buf * TILEW;
-      if (part == 2) {  // both parts of these ranks are done
-        if (sbad[TN] == astep) {  // (uniform) the factors of what is not finite
-          for (int c = pt; c < TM * 8; c += 256) {
-            const int t = c >> 3;
-            *(u32x4*)(xs + t * kGemmTK + 8 * ((c & 7) ^ (t & 7))) =
-                u32x4{(c & 7) == 0 && sid[t] == slot && skx[t] == k2 ? kMax : 0u, 0u, 0u, 0u};
-          }
-          for (int c = pt; c < TN * 8; c += 256)
-            *(u32x4*)(ws + (c >> 3) * LR + 8 * (c & 7)) = u32x4{(c & 7) == 0 && sbad[c >> 3] == astep ? kMax : 0u, 0u, 0u, 0u};
-          part = 3;
-          return true;
-        }
-        part = 3;
-      }
-      if (part == 3) {
-        part = 0;
-        kr0 += 64;
-        ++astep;
-      }
-      if (part == 0 && kr0 >= r) {  // the next slot
-        if (!(left[0] | left[1] | left[2] | left[3])) return false;
+    // requests the next step's operands: thread pt has, of the activation tile,
+    // chunk pt % 8 (parts high: 0 to 3, low: 4 to 7) of rows pt / 8 + 32 i, and, of
+    // the weight tile, chunk pt % 4 (and + 4) of rows pt / 4 + 64 i
+    auto adapt_load = [&]() {
+      kr0 += 32;
+      if (kr0 >= r) {  // the next slot
+        have = (left[0] | left[1] | left[2] | left[3]) != 0;
+        if (!have) return;
 #pragma unroll
         for (int q = 3; q >= 0; --q)
           if (left[q]) {
             const int l = __builtin_ctzll(left[q]);
             slot = __builtin_amdgcn_readlane(id[q], l);
+            r = __builtin_amdgcn_readlane(rk[q], l);
             k2 = __builtin_amdgcn_readlane(kx[q], l);
           }
 #pragma unroll
         for (int q = 0; q < 4; ++q) left[q] &= ~__ballot(id[q] == slot && kx[q] == k2);
-        r = rank_of(ad, slot);
         kr0 = 0;
       }
       const int W = 32 * ad.RG;
-      const uint16_t* u = part ? ad.ul : ad.uh;
-      const uint16_t* B = ad.B + (size_t)slot * ad.b_stride;
-      const bool vec = (ad.R & 7) == 0 && (ad.b_stride & 7) == 0;
-      u32x4 xv[8], wv[8];
+      const uint16_t* u = ((pt & 4) ? ad.ul : ad.uh) + kr0 + 8 * (pt & 3);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const int c = pt + 256 * i, t = c >> 3, col = kr0 + 8 * (c & 7);
+        const int t = (pt >> 3) + 32 * i;
         xv[i] = u32x4{0, 0, 0, 0};
-        if (sid[t] == slot && skx[t] == k2 && col < W) xv[i] = ldg16(u + (size_t)(m0 + t) * W + col);
+        if (sid[t] == slot && skx[t] == k2) xv[i] = ldg16(u + (size_t)(m0 + t) * W);
       }
+      const bool vec = (ad.R & 7) == 0 && (ad.b_stride & 7) == 0;
+      const int col = kr0 + 8 * (pt & 3);
+      const uint16_t* B = ad.B + (size_t)slot * ad.b_stride + col;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int c = pt + 256 * i, n = n0 + (c >> 3), col = kr0 + 8 * (c & 7);
+      for (int i = 0; i < 4; ++i) {
+        const int n = n0 + (pt >> 2) + 64 * i;
         wv[i] = u32x4{0, 0, 0, 0};
         if (n < N && col < r) {
-          const uint16_t* br = B + (size_t)n * ad.R + col;
+          const uint16_t* br = B + (size_t)n * ad.R;
           if (vec && col + 8 <= r) {
             wv[i] = ldg16(br);
           } else {
@@ -754,14 +743,34 @@ __device__ __forceinline__ void gemm_ws_body(const GemmParams& a, const AdapterP
           }
         }
       }
+    };
+    // stores a further step into buffer buf; false: there is none
+    auto adapt_step = [&](int buf) -> bool {
+      constexpr uint32_t kExp = DT == DT_F16 ? 0x7C00u : 0x7F80u, kMax = kExp - 1;  // the largest finite value
+      uint16_t* xs = Xs + buf * TILEX;
+      uint16_t* ws = Ws + buf * TILEW;
+      if (nstep > 0 && sbad[TN] == nstep) {  // (uniform) what the last step kept out
+        for (int c = pt; c < TM * 8; c += 256) {
+          const int t = c >> 3;
+          const bool f = (c & 7) == 0 && sid[t] == pslot && skx[t] == pk2;
+          *(u32x4*)(xs + t * kGemmTK + 8 * ((c & 7) ^ (t & 7))) = u32x4{f ? kMax : 0u, 0u, 0u, 0u};
+        }
+        for (int c = pt; c < TN * 8; c += 256)
+          *(u32x4*)(ws + (c >> 3) * LR + 8 * (c & 7)) =
+              u32x4{(c & 7) == 0 && sbad[c >> 3] == nstep ? kMax : 0u, 0u, 0u, 0u};
+        ++nstep;
+        return true;
+      }
+      if (!have) return false;
+      ++nstep;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const int c = pt + 256 * i, t = c >> 3;
-        *(u32x4*)(xs + t * kGemmTK + 8 * ((c & 7) ^ (t & 7))) = xv[i];
+        const int t = (pt >> 3) + 32 * i;
+        *(u32x4*)(xs + t * kGemmTK + 8 * ((pt & 7) ^ (t & 7))) = xv[i];
       }
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int c = pt + 256 * i, row = c >> 3;
+      for (int i = 0; i < 4; ++i) {
+        const int row = (pt >> 2) + 64 * i;
         bool bad = false;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
@@ -773,10 +782,13 @@ __device__ __forceinline__ void gemm_ws_body(const GemmParams& a, const AdapterP
           if ((wv[i][q] & kExp) == kExp) bad = true, wv[i][q] &= 0xFFFF0000u;
           if ((wv[i][q] >> 16 & kExp) == kExp) bad = true, wv[i][q] &= 0xFFFFu;
         }
-        if (bad) sbad[row] = sbad[TN] = astep;
-        *(u32x4*)(ws + row * LR + 8 * (c & 7)) = wv[i];
+        if (bad) sbad[row] = sbad[TN] = nstep;
+        *(u32x4*)(ws + row * LR + 8 * (pt & 3)) = wv[i];
+        *(u32x4*)(ws + row * LR + 8 * (pt & 3) + 32) = wv[i];
       }
-      ++part;
+      pslot = slot;
+      pk2 = k2;
+      adapt_load();
       return true;
     };
     // step kt stores step kt + 1 (loaded two steps earlier) and then loads
@@ -790,25 +802,32 @@ __device__ __forceinline__ void gemm_ws_body(const GemmParams& a, const AdapterP
     lstore(g0, 0);
     gload(g0, min(2, kl));
     __syncthreads();
-    for (int kt = 0; kt < KT; kt += 2) {
+    // (EPI_ADAPT: the last round apart, with the first further step; inside the
+    // loop its addresses cost the loading waves registers they do not have)
+    constexpr int kApart = EPI == EPI_ADAPT ? 2 : 0;
+    for (int kt = 0; kt < KT - kApart; kt += 2) {
       lstore(g1, 1);
       gload(g1, min(kt + 3, kl));
       __syncthreads();
-      if (kt + 2 < KT) {
+      // (where no branch keeps the second stage's wait behind the barrier)
+      if constexpr (kApart > 0) __builtin_amdgcn_sched_barrier(0);
+      if (kApart || kt + 2 < KT) {
         lstore(g0, 0);
         gload(g0, min(kt + 4, kl));
-      } else if constexpr (EPI == EPI_ADAPT) {
-        adapt_begin();
-        more = adapt_step(0);
-        if (pt == 0) smore[0] = more;
       }
       __syncthreads();
     }
     if constexpr (EPI == EPI_ADAPT) {
-      for (int b = 1; more; b ^= 1) {
-        more = adapt_step(b);
+      lstore(g1, 1);
+      adapt_tokens();
+      __syncthreads();
+      adapt_begin();
+      adapt_load();
+      for (int b = 0;; b ^= 1) {
+        const bool more = adapt_step(b);
         if (pt == 0) smore[b] = more;
         __syncthreads();
+        if (!more) break;
       }
     }
     if constexpr (EPI == EPI_READY) {
@@ -899,7 +918,8 @@ __device__ __forceinline__ void gemm_ws_body(const GemmParams& a, const AdapterP
     __builtin_amdgcn_s_waitcnt(0);  // this wave's share of the next tile is in LDS
     __syncthreads();
     if constexpr (EPI == EPI_ADAPT)
-      if (kt + 1 >= KT && __builtin_amdgcn_readfirstlane(smore[(kt + 1) & 1])) end = kt + 2;
+      // (volatile: not to be read in every step)
+      if (kt + 1 >= KT && __builtin_amdgcn_readfirstlane(*(volatile __attribute__((address_space(3))) int*)(smore + ((kt + 1) & 1)))) end = kt + 2;
   }
 
   if constexpr (EPI == EPI_READY) {
@@ -966,7 +986,7 @@ hipError_t SPEAR_W(launch_gemm_adapt)(const GemmParams& p, const AdapterParams& 
     return hipErrorInvalidValue;
   const unsigned grid = (unsigned)(((p.M + 255) / 256) * ((p.N + 255) / 256));
   if (grid == 0) return hipSuccess;
-  const size_t lds = (size_t)2 * 256 * kGemmTK * 2 + (size_t)2 * 256 * kGemmLdsRow * 2 + (3 * 256 + 4) * 4;
+  const size_t lds = (size_t)2 * 256 * kGemmTK * 2 + (size_t)2 * 256 * kGemmLdsRow * 2 + (4 * 256 + 4) * 4;
   const auto go = [&](auto kern) {
     hipError_t err = allow_lds(kern, lds);
     if (err != hipSuccess) return err;

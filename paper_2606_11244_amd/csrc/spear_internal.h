@@ -328,7 +328,7 @@ __host__ __device__ inline size_t ec_block_lds(int NW, int R1p, int h, int r) {
                                   hipStream_t st);                                               \
   hipError_t launch_adapter_shrink_##D(const AdapterGroup& g, hipStream_t st);                   \
   hipError_t launch_adapter_expand_##D(const AdapterGroup& g, hipStream_t st);                   \
-  hipError_t launch_adapter_parts_##D(const AdapterParams& p, hipStream_t st);                   \
+  hipError_t launch_adapter_parts_##D(const AdapterGroup& g, hipStream_t st);                    \
   hipError_t launch_block_norm_##D(const BlockNormParams& p, hipStream_t st);                    \
   SPEAR_WEIGHT_LAUNCHERS(w4_##D)                                                                 \
   SPEAR_WEIGHT_LAUNCHERS(w3_##D)
