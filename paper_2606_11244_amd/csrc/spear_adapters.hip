@@ -288,9 +288,14 @@ __device__ __forceinline__ TileSlots tile_slots(const AdapterParams& p, int m0) 
   return t;
 }
 
+// The activations come into LDS by direct loads of whole 256-byte pieces of four
+// rows each (in the MFMA's layout a load takes 64 bytes of each of 16 rows, twice
+// the requests, and the requests in flight are the bound), each wave's own 16 KB,
+// chunk c of row t at c ^ (t % 16).
 template <int DT>
 __device__ __forceinline__ void shrink_tile(const AdapterParams& p, int b) {
-  __shared__ __attribute__((aligned(16))) float red[4][2][4][256];
+  __shared__ __attribute__((aligned(16))) uint16_t xs[4][64 * kIterK];
+  float (*red)[2][4][256] = (float (*)[2][4][256])&xs[0][0];  // (after the last iteration)
   const int lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int per = p.P * p.RG * p.PA, tb = b / per;
@@ -321,15 +326,16 @@ __device__ __forceinline__ void shrink_tile(const AdapterParams& p, int b) {
     for (int s = 0; s < 4; ++s) acc[t][s] = f32x4{0.f, 0.f, 0.f, 0.f};
   uint32_t xoff[4];
 #pragma unroll
-  for (int s = 0; s < 4; ++s) xoff[s] = (uint32_t)min(m0 + 16 * s + lr, p.M - 1) * p.K * 2 + 16 * lg;
+  for (int u = 0; u < 4; ++u) xoff[u] = (uint32_t)(m0 + 4 * u + lg) * p.K * 2 + 16 * (lr ^ (4 * u + lg));
+  const uint32_t xlast = (uint32_t)(p.M - 1) * p.K * 2 + 240;  // (for tokens past the last: no slot owns them)
+  uint16_t* xw = xs[wave];
   const uint32_t aoff = (uint32_t)(32 * rg + lr) * p.K * 2 + 16 * lg;
   for (int it = it_beg + wave; it < it_end; it += 4) {
     const uint32_t kb = (uint32_t)it * (kIterK * 2);
-    u32x4 xv[4][4];
 #pragma unroll
-    for (int s = 0; s < 4; ++s)
-#pragma unroll
-      for (int jj = 0; jj < 4; ++jj) xv[s][jj] = bld128s(rx, xoff[s] + 64 * jj, kb);
+    for (int u = 0; u < 16; ++u)
+      bld128_lds(rx, xw + u * 512, min(xoff[u & 3] + (uint32_t)(16 * (u >> 2)) * p.K * 2, xlast) + kb);
+    bool landed = false;
     TileSlots t0 = slots;
     t0.left = owned;
     int a, r;
@@ -344,23 +350,40 @@ __device__ __forceinline__ void shrink_tile(const AdapterParams& p, int b) {
 #pragma unroll
         for (int jj = 0; jj < 4; ++jj) av[t][jj] = bld128s(ra, ao + 64 * jj, kb);
       }
+      if (!landed) {  // (uniform) with the first slot's rows requested
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        landed = true;
+      }
 #pragma unroll
       for (int s = 0; s < 4; ++s) {
         const uint32_t st = (uint32_t)(toks >> (16 * s)) & 0xFFFFu;
         if (st == 0) continue;  // uniform
         const bool in = (st >> lr) & 1;
+        u32x4 xv[4];
+#pragma unroll
+        for (int jj = 0; jj < 4; ++jj)
+          xv[jj] = *(const u32x4*)(xw + (16 * s + lr) * kIterK + 8 * ((lg + 4 * jj) ^ lr));
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
           if (16 * t >= r) continue;  // uniform
           f32x4 q = acc[t][s];
 #pragma unroll
-          for (int jj = 0; jj < 4; ++jj) q = mfma16<DT>(av[t][jj], xv[s][jj], q);
+          for (int jj = 0; jj < 4; ++jj) q = mfma16<DT>(av[t][jj], xv[jj], q);
 #pragma unroll
           for (int e = 0; e < 4; ++e) acc[t][s][e] = in ? q[e] : acc[t][s][e];
         }
       }
     }
+    // the reads are done before the next iteration's loads write there
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
   }
+  __syncthreads();
 #pragma unroll
   for (int t = 0; t < 2; ++t)
 #pragma unroll
