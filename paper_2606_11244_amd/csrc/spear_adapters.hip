@@ -335,28 +335,40 @@ __device__ __forceinline__ void shrink_tile(const AdapterParams& p, int b) {
 #pragma unroll
     for (int u = 0; u < 16; ++u)
       bld128_lds(rx, xw + u * 512, min(xoff[u & 3] + (uint32_t)(16 * (u >> 2)) * p.K * 2, xlast) + kb);
-    bool landed = false;
+    // a slot's rows of A, requested one slot ahead
     TileSlots t0 = slots;
     t0.left = owned;
-    int a, r;
-    uint64_t toks;
-    while (t0.next(&a, &r, &toks)) {
-      r -= 32 * rg;
+    int r = 0, rn = 0;
+    uint64_t toks = 0, tn = 0;
+    u32x4 av[2][4], nv[2][4];
+    auto request = [&]() {
+      int a;
+      if (!t0.next(&a, &rn, &tn)) {
+        tn = 0;
+        return;
+      }
+      rn -= 32 * rg;
       const rsrc_t ra = make_rsrc(p.A + (size_t)a * p.a_stride, (uint32_t)p.R * p.K * 2);
-      u32x4 av[2][4];
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        const uint32_t ao = 16 * t + lr < r ? aoff + (uint32_t)t * 32 * p.K : kOOB;
+        const uint32_t ao = 16 * t + lr < rn ? aoff + (uint32_t)t * 32 * p.K : kOOB;
 #pragma unroll
-        for (int jj = 0; jj < 4; ++jj) av[t][jj] = bld128s(ra, ao + 64 * jj, kb);
+        for (int jj = 0; jj < 4; ++jj) nv[t][jj] = bld128s(ra, ao + 64 * jj, kb);
       }
-      if (!landed) {  // (uniform) with the first slot's rows requested
-        __builtin_amdgcn_sched_barrier(0);
-        __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
-        asm volatile("" ::: "memory");
-        __builtin_amdgcn_sched_barrier(0);
-        landed = true;
-      }
+    };
+    request();
+    // the activations, with the first slot's rows
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    while (tn) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int jj = 0; jj < 4; ++jj) av[t][jj] = nv[t][jj];
+      r = rn, toks = tn;
+      request();
 #pragma unroll
       for (int s = 0; s < 4; ++s) {
         const uint32_t st = (uint32_t)(toks >> (16 * s)) & 0xFFFFu;
