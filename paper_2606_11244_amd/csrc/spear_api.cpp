@@ -1272,11 +1272,17 @@ void adapters_shape(const spear_problem_t* p, const spear_adapters_t* a, Adapter
   while (tiles * cdiv(p->N, 64 * q->rpw) > 2048 && q->rpw < 32) q->rpw *= 2;
   q->chunks = (int)cdiv(p->N, 64 * q->rpw);
   int P = 1;
-  while (tiles * q->RG * P < 256 && IT / (2 * P) >= 4) P *= 2;
+  // K-slices of two iterations or more while the tiles leave CUs idle, no more than
+  // 16, which the coordinates' readers add up (5000 x 2944, 77 tokens: slices of
+  // two 4.7 us, of four 6.0; 4096 x 14336, 300 tokens: 28 slices take 2.1 us
+  // longer to add than 16 and save nothing)
+  while (tiles * q->RG * P < 256 && P < 16 && IT / (2 * P) >= 2) P *= 2;
   q->ips = (int)cdiv(IT, P);
   q->P = (int)cdiv(IT, q->ips);
-  // few tiles: their slots, as many as their tokens at worst, are shared out
-  while (q->PA < 16 && tiles * q->PA < 32) q->PA *= 2;
+  // few tiles: their slots, as many as their tokens at worst, are shared out over
+  // workgroups that would be idle (every part reads its tile again: 300 tokens of
+  // 14336, 80 workgroups: in 1, 2, 4, 8 parts 9.1, 8.2, 10.4, 16.0 us)
+  while (q->PA < 16 && tiles * q->PA < 32 && 2 * tiles * q->RG * q->P * q->PA <= 256) q->PA *= 2;
 }
 
 spear_status_t adapters_layout(int32_t n, const spear_layer_call_t* calls, const spear_adapters_t* const* ads,
