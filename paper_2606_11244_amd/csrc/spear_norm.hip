@@ -5,10 +5,23 @@
 
 namespace spear {
 
+// sum over a wave, the same in every lane: exchanges in registers within 16 lanes
+template <int CTRL>
+__device__ __forceinline__ float dpp_add(float v) {
+  return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, true));
+}
+__device__ __forceinline__ float wave_sum(float v) {
+  v = dpp_add<0xB1>(v);   // pairs
+  v = dpp_add<0x4E>(v);   // pairs of a four
+  v = dpp_add<0x141>(v);  // fours of an eight (mirrored)
+  v = dpp_add<0x140>(v);  // eights of a sixteen (mirrored)
+  v += __shfl_xor(v, 16);
+  return v + __shfl_xor(v, 32);
+}
+
 // sum over the workgroup (a multiple of 64 threads), the same in every thread
 __device__ __forceinline__ float block_sum(float v, float* red) {
-#pragma unroll
-  for (int h = 32; h > 0; h >>= 1) v += __shfl_xor(v, h);
+  v = wave_sum(v);
   __syncthreads();
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
   __syncthreads();
@@ -157,6 +170,9 @@ __device__ __forceinline__ float elem(const u32x4& v, int e) {
 // 64, no barrier), else a row per workgroup. Up to two chunks the weights are
 // loaded once and serve all rows that the workgroup takes. AL: rows of whole
 // 16-byte aligned chunks; else any length and stride.
+// Bound by memory for many rows: 4096 x 8192 fp16 with both norms and a gate row
+// for each token moves 336 MB in 71 us, 4.7 TB/s (a copy of 1 GiB: 5.2); by
+// latency for few: 3.4 us for one row of 4096, two dependent sums behind one load.
 template <int DT, bool F32, int C, bool WAVE, bool AL>
 __global__ __launch_bounds__(WAVE ? 256 : 1024) void k_block_norm_v(BlockNormParams p) {
   __shared__ float red[2][16];
@@ -174,8 +190,7 @@ __global__ __launch_bounds__(WAVE ? 256 : 1024) void k_block_norm_v(BlockNormPar
   };
   if constexpr (HOLD) weights(pw, p.post_w), weights(nw, p.pre_w);
   auto row_sum = [&](float v, int k) {
-#pragma unroll
-    for (int h = 32; h > 0; h >>= 1) v += __shfl_xor(v, h);
+    v = wave_sum(v);
     if constexpr (WAVE) return v;
     if ((threadIdx.x & 63) == 0) red[k][threadIdx.x >> 6] = v;
     __syncthreads();
@@ -185,7 +200,7 @@ __global__ __launch_bounds__(WAVE ? 256 : 1024) void k_block_norm_v(BlockNormPar
   };
   const float inv_n = 1.f / (float)N;
   for (long long m0 = (long long)blockIdx.x * per; m0 < p.M; m0 += (long long)gridDim.x * per) {
-    const long long m = WAVE ? m0 + (threadIdx.x >> 6) : m0;
+    const long long m = WAVE ? m0 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : m0;
     if (WAVE && m >= p.M) break;
     const uint16_t* y = p.y + (size_t)m * p.y_ld;
     u32x4 yv[C], gv[C];
@@ -288,6 +303,13 @@ static hipError_t norm_launch(const BlockNormParams& p, hipStream_t st) {
   if (n8 <= 64) return go(k_block_norm_v<DTC, F32, 1, true, AL>, 4, 256);
   if (n8 <= 128) return go(k_block_norm_v<DTC, F32, 2, true, AL>, 4, 256);
   if (n8 <= 256) return go(k_block_norm_v<DTC, F32, 1, false, AL>, 1, 256);
+  // Up to a row for each CU a row's latency is all: one chunk a thread (kernel
+  // times with two and with one: one row of 4096 4.1 and 3.4 us, 24 of 8192 in 32
+  // bits 7.2 and 6.7). More rows share a CU, and the wider workgroups cost: 301 of
+  // 5003 8.8 and 11.3.
+  const bool few = p.M <= 256;
+  if (few && n8 <= 512) return go(k_block_norm_v<DTC, F32, 1, false, AL>, 1, 512);
+  if (few && n8 <= 1024) return go(k_block_norm_v<DTC, F32, 1, false, AL>, 1, 1024);
   if (n8 <= 512) return go(k_block_norm_v<DTC, F32, 2, false, AL>, 1, 256);
   if (n8 <= 1024) return go(k_block_norm_v<DTC, F32, 2, false, AL>, 1, 512);
   if (n8 <= 2048) return go(k_block_norm_v<DTC, F32, 2, false, AL>, 1, 1024);
