@@ -396,11 +396,9 @@ spear_status_t spear_adapters_workspace(int32_t n, const spear_layer_call_t* cal
 /* spear_w4ec_linear (ec NULL: spear_w4_linear) with adapters, followed by the
  * post-EC tail if tail is not NULL. Y = the layer + the adapters' term + the
  * tail's residual, each summed in fp32. Where the layer is one decode GEMV
- * launch, its sums are rounded to the act dtype once before the others are
- * added; where the layer runs on 256 x 256 tiles, nothing is rounded before Y
- * itself; elsewhere the term plus the residual is, once. A token without an
- * adapter gets, but for that rounding, what the call without adapters writes,
- * and no
+ * launch or runs on 256 x 256 tiles, nothing is rounded before Y itself;
+ * elsewhere the term plus the residual is, once, to the act dtype. A token
+ * without an adapter gets what the call without adapters writes, and no
  * token's result depends on another token's adapter or values. The workspace
  * follows the rules of the other calls and may be shared with them in stream
  * order. Errors as for spear_w4ec_linear_tail and spear_adapters_workspace,

@@ -1,7 +1,7 @@
 // gfx950 (MI355X) kernels of the low-rank adapters of many requests: the term
 //   d[m] = res[m] + s_a B_a (A_a x[m]),   a = ids[m] (d[m] = res[m] without one)
-// that the 4-bit product's final store adds in place of a residual, or that is
-// added to its output.
+// that the 4-bit product's final store adds in place of a residual, or that
+// takes the product's sums (yf, fp32) up and is the layer's output.
 //
 // Two steps, the coordinates u[m] = s_a A_a x[m] (bound by reading x and the
 // slots' A) and the term B_a u[m] (bound by reading B and writing d). Both are
@@ -168,9 +168,10 @@ __device__ __forceinline__ void add_product(const u32x4 (&bf)[4], u32x4 hi, u32x
 }
 
 // What the term of a lane's token is added to, its rows n + 8 lg and n + 32 + 8
-// lg (eight each): the residual, and in place (p.add) what d holds.
+// lg (eight each): the residual and the layer's sums.
 struct Base {
-  u32x4 res[2], old[2];
+  u32x4 res[2];
+  f32x4 yf[4];
 };
 __device__ __forceinline__ void load_base(const AdapterParams& p, bool live, int m, int n, Base& b) {
   const int lg = (threadIdx.x & 63) >> 4;
@@ -179,7 +180,10 @@ __device__ __forceinline__ void load_base(const AdapterParams& p, bool live, int
     const int nn = n + 32 * h + 8 * lg;
     if ((p.N & 7) == 0 && live && nn < p.N) {
       if (p.res) b.res[h] = ldg16(p.res + (size_t)m * p.N + nn);
-      if (p.add) b.old[h] = ldg16(p.d + (size_t)m * p.N + nn);
+      if (p.yf) {
+        const f32x4* y = (const f32x4*)(p.yf + (size_t)m * p.N + nn);
+        b.yf[2 * h] = y[0], b.yf[2 * h + 1] = y[1];
+      }
     }
   }
 }
@@ -196,12 +200,11 @@ __device__ __forceinline__ void store_term(const AdapterParams& p, bool live, in
     const size_t o = (size_t)m * p.N + nn;
     if ((p.N & 7) == 0) {
       f32x4 f[2] = {v[2 * h], v[2 * h + 1]};
-      auto add = [&](const u32x4& w) {
+      if (p.yf) f[0] += b.yf[2 * h], f[1] += b.yf[2 * h + 1];  // (uniform)
+      if (p.res) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) f[e >> 2][e & 3] += act2f<DT>((w[e >> 1] >> (16 * (e & 1))) & 0xFFFFu);
-      };
-      if (p.res) add(b.res[h]);  // (uniform)
-      if (p.add) add(b.old[h]);
+        for (int e = 0; e < 8; ++e) f[e >> 2][e & 3] += act2f<DT>((b.res[h][e >> 1] >> (16 * (e & 1))) & 0xFFFFu);
+      }
       u32x4 w;
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
@@ -215,7 +218,7 @@ __device__ __forceinline__ void store_term(const AdapterParams& p, bool live, in
       for (int e = 0; e < 8; ++e)
         if (nn + e < p.N)
           p.d[o + e] = f2act<DT>(v[2 * h + (e >> 2)][e & 3] + (p.res ? act2f<DT>(p.res[o + e]) : 0.f) +
-                                 (p.add ? act2f<DT>(p.d[o + e]) : 0.f));
+                                 (p.yf ? p.yf[o + e] : 0.f));
     }
   }
 }
@@ -435,9 +438,7 @@ __device__ __forceinline__ void expand_tile(const AdapterParams& p, int b, char*
     all.left = __ballot(all.rank > 0) & 0xFFFFu;
   }
   const int m = min(m0 + lr, p.M - 1);
-  // in place with no residual, only the tokens of a slot change
-  const bool live = m0 + lr < p.M && (!p.add || p.res || all.rank > 0);
-  if (p.add && !p.res && !all.left) return;
+  const bool live = m0 + lr < p.M;
   const RowLanes lanes(p);
   const int n_beg = chunk * 64 * p.rpw, n_end = min(p.N, n_beg + 64 * p.rpw);
 

@@ -1225,21 +1225,24 @@ spear_status_t check_tail(const spear_problem_t* prob, const void* x, const spea
 // - ADAPT_BEFORE: formed first, in the workspace (d), with the tail's residual,
 //   it enters the layer as the residual of its final store;
 // - ADAPT_RIDES: the coordinates go with the layer's GEMV launch as further
-//   workgroups, and a launch after it adds the term to y. Where the layer is one
-//   GEMV launch: decode calls are latency, and this takes the first of the
-//   adapters' two launches off their path (8B q, k, v at 16 requests: 13.2 us for
-//   the launch, 12.9 without adapters, 4.8 for the coordinates alone);
-// - ADAPT_EPILOGUE: k_gemm_ws on 256 x 256 tiles forms it. Its epilogue with a
-//   residual costs as much as another pass over the output (8B gate and up,
-//   14336 x 4096 at 2048 tokens, fp16: 617 us with the term first, 574 with a pass
-//   after it that also rounds y once more).
+//   workgroups; its sums stay in fp32 (yf), and a launch after it adds the term
+//   and the tail's residual and writes y. Where the layer is one GEMV launch:
+//   decode calls are latency, and this takes the first of the adapters' two
+//   launches off their path (8B q, k, v at 16 requests: 13.3 us for the launch, 12.9
+//   without adapters, 4.8 for the coordinates alone);
+// - ADAPT_EPILOGUE: k_gemm_ws on 256 x 256 tiles forms it, as further steps of its
+//   loop. Its epilogue with a residual costs as much as another pass over the
+//   output (8B gate and up, 14336 x 4096 at 2048 tokens, fp16: 617 us with the term
+//   first, 574 with a pass after it that also rounds y once more, 482 this way,
+//   449 without adapters).
 enum { ADAPT_BEFORE = 0, ADAPT_RIDES = 1, ADAPT_EPILOGUE = 2 };
 // The adapter data of one member in the workspace: the K-slices of its
-// coordinates, their parts (ADAPT_EPILOGUE), its term d (ADAPT_BEFORE).
+// coordinates, their parts (ADAPT_EPILOGUE), its term d (ADAPT_BEFORE), the
+// layer's sums yf (ADAPT_RIDES).
 struct AdapterLayout {
   bool on = false;  // the member has tokens, rows and adapters
   int join = ADAPT_BEFORE;
-  size_t upart = 0, uh = 0, ul = 0, ukx = 0, d = 0;
+  size_t upart = 0, uh = 0, ul = 0, ukx = 0, d = 0, yf = 0;
   AdapterParams p;  // the launch shape
 };
 
@@ -1319,6 +1322,7 @@ spear_status_t adapters_layout(int32_t n, const spear_layer_call_t* calls, const
       al[i].ukx = take((size_t)p->M * 4);
     }
     if (al[i].join == ADAPT_BEFORE) al[i].d = take((size_t)p->M * p->N * 2);
+    if (al[i].join == ADAPT_RIDES) al[i].yf = take((size_t)p->M * p->N * 4);
   }
   if (any) *total = off;
   return SPEAR_OK;
@@ -1365,8 +1369,8 @@ AdapterParams make_adapters(const spear_layer_call_t& c, const spear_adapters_t*
   q.scale = a->scale;
   q.res = res;
   q.upart = (float*)(ws + al.upart);
-  q.add = al.join == ADAPT_RIDES;
-  q.d = q.add ? (uint16_t*)c.y : (uint16_t*)(ws + al.d);
+  if (al.join == ADAPT_RIDES) q.yf = (const float*)(ws + al.yf);
+  q.d = q.yf ? (uint16_t*)c.y : (uint16_t*)(ws + al.d);
   if (al.join == ADAPT_EPILOGUE) {
     q.uh = (uint16_t*)(ws + al.uh);
     q.ul = (uint16_t*)(ws + al.ul);
@@ -1408,8 +1412,8 @@ struct AdapterCall {
   }
   // before the layers: the coordinates of all members but those that ride along,
   // and the terms that enter the layers as residuals, res[i]
-  spear_status_t before(const bool* rides, const uint16_t** res, hipStream_t s) const {
-    spear_status_t st = each([&](int i) { return !rides[i]; }, [&](int dt, const AdapterGroup& g) {
+  spear_status_t before(const uint16_t** res, hipStream_t s) const {
+    spear_status_t st = each([&](int i) { return al[i].join != ADAPT_RIDES; }, [&](int dt, const AdapterGroup& g) {
       return SPEAR_BY_DT(launch_adapter_shrink, dt)(g, s);
     });
     if (st == SPEAR_OK)
@@ -1425,7 +1429,26 @@ struct AdapterCall {
   // the layer of a member that shares no launch
   spear_status_t layer(int i, const Resolved& z, const uint16_t* res, char* ws, hipStream_t s) const {
     const spear_layer_call_t& c = calls[i];
-    if (!al[i].on || al[i].join != ADAPT_EPILOGUE) return run_layer(c.prob, z, c.x, c.w, c.ec, c.y, res, ws, s);
+    if (!al[i].on || al[i].join == ADAPT_BEFORE) return run_layer(c.prob, z, c.x, c.w, c.ec, c.y, res, ws, s);
+    if (al[i].join == ADAPT_RIDES) {
+      const bool ec = z.ec;
+      GemvGroup g;
+      std::memset(&g, 0, sizeof(g));
+      g.p[0] = make_gemv(c.prob, z, c.x, c.w, c.y, ec ? c.ec : nullptr, ws);
+      g.p[0].res = res;
+      g.p[0].yf = const_cast<float*>(p[i].yf);
+      if (ec) {
+        g.p[0].ec = make_ec(c.prob, z, c.x, c.ec, ws);
+        if (z.S > 1) g.p[0].eupart = (float*)(ws + z.off_eupart);
+      }
+      g.start[1] = z.nrg * z.S;
+      g.n = 1;
+      AdapterGroup a;
+      a.p[0] = p[i];
+      a.n = 1;
+      return hip_status(SPEAR_BY_WB(launch_gemv_adapt, z.wb, z.dt)(z.MT, z.RT, group_epi(z, c.ec), g, a, 64 * z.NW,
+                                                                   z.lds_gemv, s));
+    }
     GemmParams g = make_gemm(c.prob, z, c.x, c.w, c.y, nullptr, ws);
     g.res = res;
     return hip_status(SPEAR_BY_WB(launch_gemm_adapt, z.wb, z.dt)(g, p[i], s));
@@ -1701,11 +1724,7 @@ static spear_status_t run_group(int32_t n, const spear_layer_call_t* calls, Reso
   shared_sets(n, calls, z, in, set, ec_set, gv_set);
   // the coordinates of adapters go with the shared GEMV launch, or first
   const uint16_t* res[SPEAR_GROUP_MAX] = {};
-  if (ad.n > 0) {
-    bool rides[SPEAR_GROUP_MAX];
-    for (int i = 0; i < n; ++i) rides[i] = in[i] && ad.al[i].join == ADAPT_RIDES;
-    if ((st = ad.before(rides, res, s)) != SPEAR_OK) return st;
-  }
+  if (ad.n > 0 && (st = ad.before(res, s)) != SPEAR_OK) return st;
   // members that share nothing: each as its own call would run, in the
   // workspace a single call would use
   for (int i = 0; i < n; ++i) {
@@ -1844,8 +1863,14 @@ static spear_status_t run_group(int32_t n, const spear_layer_call_t* calls, Reso
   const Resolved& z0 = z[first];
   AdapterGroup a;
   a.n = 0;
-  for (int i = 0; i < ad.n; ++i)
-    if (in[i] && ad.al[i].on && ad.al[i].join == ADAPT_RIDES) a.p[a.n++] = ad.p[i];
+  for (int i = 0, m = 0; i < ad.n; ++i) {
+    if (!in[i]) continue;
+    if (ad.al[i].on && ad.al[i].join == ADAPT_RIDES) {
+      g.p[m].yf = const_cast<float*>(ad.p[i].yf);
+      a.p[a.n++] = ad.p[i];
+    }
+    ++m;
+  }
   if (a.n > 0)
     return hip_status(SPEAR_BY_WB(launch_gemv_adapt, z0.wb, z0.dt)(z0.MT, z0.RT, epi, g, a, 64 * z0.NW, lds, s));
   return hip_status(SPEAR_BY_WB(launch_gemv_group, z0.wb, z0.dt)(z0.MT, z0.RT, epi, g, 64 * z0.NW, lds, s));
@@ -1962,33 +1987,12 @@ spear_status_t spear_w4ec_linear_adapters(const spear_problem_t* prob, const voi
   ad.n = 1;
   ad.calls = &call;
   const AdapterLayout& al = ad.al[0];
-  // the residual goes with the term, except where the layer's epilogue forms that,
-  // or where it comes after the layer and y itself holds the residual
-  const bool rides = al.on && al.join == ADAPT_RIDES;
-  const bool with_term = al.on && (al.join == ADAPT_BEFORE || (rides && res != y));
+  // the residual goes with the term, except where the layer's epilogue forms that
+  const bool with_term = al.on && al.join != ADAPT_EPILOGUE;
   if (al.on) ad.p[0] = make_adapters(call, adapters, al, with_term ? res : nullptr, ws);
   const uint16_t* in = with_term ? nullptr : res;  // what the layer adds
-  if ((st = ad.before(&rides, &in, s)) != SPEAR_OK) return st;
-  if (rides) {
-    const int epi = group_epi(z[0], ec);
-    GemvGroup g;
-    std::memset(&g, 0, sizeof(g));
-    g.p[0] = make_gemv(prob, z[0], x, w, y, z[0].ec ? ec : nullptr, ws);
-    g.p[0].res = in;
-    if (z[0].ec) {
-      g.p[0].ec = make_ec(prob, z[0], x, ec, ws);
-      if (z[0].S > 1) g.p[0].eupart = (float*)(ws + z[0].off_eupart);
-    }
-    g.start[1] = z[0].nrg * z[0].S;
-    g.n = 1;
-    AdapterGroup a;
-    a.p[0] = ad.p[0];
-    a.n = 1;
-    st = hip_status(SPEAR_BY_WB(launch_gemv_adapt, z[0].wb, z[0].dt)(z[0].MT, z[0].RT, epi, g, a, 64 * z[0].NW,
-                                                                     z[0].lds_gemv, s));
-  } else {
-    st = ad.layer(0, z[0], in, ws, s);
-  }
+  if ((st = ad.before(&in, s)) != SPEAR_OK) return st;
+  st = ad.layer(0, z[0], in, ws, s);
   if (st == SPEAR_OK) st = ad.after(s);
   if (st != SPEAR_OK || !tail || !tail->norm_w) return st;
   return hip_status(SPEAR_BY_DT(launch_rmsnorm, z[0].dt)((const uint16_t*)y, (const uint16_t*)tail->norm_w,

@@ -128,6 +128,7 @@ struct GemvParams {
   const int8_t* B8;       // [N][r] INT8 codes, or null
   const float* sb;        // [N] INT8 per-channel scales
   const uint16_t* res;    // [M][N] residual added before the output's rounding, or null
+  float* yf;              // k_gemv_adapt: [M][N] the sums, in place of y (or null)
   int M, N, K, G, ngroups, r;
   int S, ips, iw;         // K-slices per row group, iterations per slice and per wave
   int n_prod;             // EC workgroups at the head of the grid (fused)
@@ -225,8 +226,8 @@ struct AdapterParams {
   const int32_t* ranks;   // [L] or null (all R)
   const float* scale;     // [L] or null (all 1)
   const uint16_t* res;    // [M][N] residual, or null
-  uint16_t* d;            // [M][N] the term plus the residual, act dtype
-  int add;                // d += that instead (in place: the layer's output)
+  const float* yf;        // [M][N] the layer's sums, or null
+  uint16_t* d;            // [M][N] the sum of these and the term, act dtype
   float* upart;           // [P][M][32 RG] K-slices of the coordinates A_a x
   // where the GEMM forms the term: the two act-dtype parts of s_a A_a x [M][32 RG],
   // and the power of two >= 0 that a token's were divided by [M] (fp16)

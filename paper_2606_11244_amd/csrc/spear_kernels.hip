@@ -760,7 +760,8 @@ __device__ void ec_wave(const GemvParams& a, uint32_t gen, char* smem, int n0, b
 // 16, bf16, one token: 8.4 us with it, 7.4 without; 4-bit product 8192 x 8192 at
 // one token 12.0 and 11.5; producer-fused 8192 x 8192, rank 32, 18.0 and 17.3).
 // ---------------------------------------------------------------------------
-template <int DT, int MT, int RT, int EPI, int WB, int NST, bool SPLIT>
+// F32: with a.yf the sums leave in fp32, in place of y.
+template <int DT, int MT, int RT, int EPI, int WB, int NST, bool SPLIT, bool F32 = false>
 __device__ __forceinline__ void gemv_body(const GemvParams& a, int bid, uint32_t gen, char* smem) {
   __shared__ int s_flag;
   constexpr bool kEC = EPI == EPI_READY || EPI == EPI_FUSED;  // with an EC wave
@@ -1382,7 +1383,8 @@ __device__ __forceinline__ void gemv_body(const GemvParams& a, int bid, uint32_t
         v += ev;
       }
       if (a.res) v += act2f<DT>(res_pre ? resv : a.res[(size_t)m * N + n0 + row]);
-      a.y[(size_t)m * N + n0 + row] = f2act<DT>(v);
+      if (F32 && a.yf) a.yf[(size_t)m * N + n0 + row] = v;  // (uniform)
+      else a.y[(size_t)m * N + n0 + row] = f2act<DT>(v);
     }
   }
   if constexpr (EPI == EPI_FUSED) fused_exit(a);
@@ -1434,7 +1436,8 @@ __global__ __launch_bounds__(kGemvMaxThreads, gemv_min_waves(MT, RT, EPI)) void 
 
 // The same with the coordinates of decode adapters (spear_adapters.h) as the
 // grid's last workgroups: the two read the same x, neither waits for the
-// other, and the term is formed from both by a later launch.
+// other, and the output is formed from both by a later launch (the layer's sums
+// wait in fp32, so that y is rounded once).
 template <int DT, int MT, int RT, int EPI, int WB, bool SPLIT>
 __global__ __launch_bounds__(kGemvMaxThreads, gemv_min_waves(MT, RT, EPI)) void k_gemv_adapt(GemvGroup g,
                                                                                             AdapterGroup a) {
@@ -1452,7 +1455,7 @@ __global__ __launch_bounds__(kGemvMaxThreads, gemv_min_waves(MT, RT, EPI)) void 
 #pragma unroll
   for (int j = 1; j < kGroupMax; ++j)
     if (j < g.n && b >= g.start[j]) i = j;
-  gemv_body<DT, MT, RT, EPI, WB, 2, SPLIT>(g.p[i], b - g.start[i], 0u, smem);
+  gemv_body<DT, MT, RT, EPI, WB, 2, SPLIT, true>(g.p[i], b - g.start[i], 0u, smem);
 }
 
 // ---------------------------------------------------------------------------
