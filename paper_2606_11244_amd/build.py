@@ -31,6 +31,10 @@ COMMON = ["-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
 UNITS = tuple((src, f"w{wb}_{'bf16' if bf else 'f16'}",
                [f"--offload-arch={ARCH}", "-x", "hip", f"-DSPEAR_WB={wb}", f"-DSPEAR_BF16_UNIT={bf}"])
               for src in ("spear_kernels.hip", "spear_gemm.hip", "spear_mid.hip") for wb in (4, 3) for bf in (0, 1)) + tuple(
+    # the decode GEMV of calls with adapters, apart from the other kernels
+    ("spear_kernels.hip", f"adapt_w{wb}_{'bf16' if bf else 'f16'}",
+     [f"--offload-arch={ARCH}", "-x", "hip", f"-DSPEAR_WB={wb}", f"-DSPEAR_BF16_UNIT={bf}", "-DSPEAR_ADAPT_UNIT=1"])
+    for wb in (4, 3) for bf in (0, 1)) + tuple(
     # and those that read no codes once per activation dtype
     (src, "bf16" if bf else "f16", [f"--offload-arch={ARCH}", "-x", "hip", f"-DSPEAR_BF16_UNIT={bf}"])
     for src in ("spear_adapters.hip", "spear_norm.hip") for bf in (0, 1)) + (

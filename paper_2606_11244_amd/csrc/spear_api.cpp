@@ -1436,7 +1436,6 @@ struct AdapterCall {
       std::memset(&g, 0, sizeof(g));
       g.p[0] = make_gemv(c.prob, z, c.x, c.w, c.y, ec ? c.ec : nullptr, ws);
       g.p[0].res = res;
-      g.p[0].yf = const_cast<float*>(p[i].yf);
       if (ec) {
         g.p[0].ec = make_ec(c.prob, z, c.x, c.ec, ws);
         if (z.S > 1) g.p[0].eupart = (float*)(ws + z.off_eupart);
@@ -1444,7 +1443,9 @@ struct AdapterCall {
       g.start[1] = z.nrg * z.S;
       g.n = 1;
       AdapterGroup a;
+      std::memset(&a, 0, sizeof(a));
       a.p[0] = p[i];
+      a.yf[0] = const_cast<float*>(p[i].yf);
       a.n = 1;
       return hip_status(SPEAR_BY_WB(launch_gemv_adapt, z.wb, z.dt)(z.MT, z.RT, group_epi(z, c.ec), g, a, 64 * z.NW,
                                                                    z.lds_gemv, s));
@@ -1862,11 +1863,11 @@ static spear_status_t run_group(int32_t n, const spear_layer_call_t* calls, Reso
   g.n = k;
   const Resolved& z0 = z[first];
   AdapterGroup a;
-  a.n = 0;
+  std::memset(&a, 0, sizeof(a));
   for (int i = 0, m = 0; i < ad.n; ++i) {
     if (!in[i]) continue;
     if (ad.al[i].on && ad.al[i].join == ADAPT_RIDES) {
-      g.p[m].yf = const_cast<float*>(ad.p[i].yf);
+      a.yf[m] = const_cast<float*>(ad.p[i].yf);
       a.p[a.n++] = ad.p[i];
     }
     ++m;

@@ -25,6 +25,9 @@
 #ifndef SPEAR_WB
 #define SPEAR_WB 4
 #endif
+#ifndef SPEAR_ADAPT_UNIT  // spear_kernels.hip: the kernels of calls with adapters
+#define SPEAR_ADAPT_UNIT 0
+#endif
 #ifndef SPEAR_BF16_UNIT
 #define SPEAR_BF16_UNIT 0
 #endif

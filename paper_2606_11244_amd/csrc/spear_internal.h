@@ -128,7 +128,6 @@ struct GemvParams {
   const int8_t* B8;       // [N][r] INT8 codes, or null
   const float* sb;        // [N] INT8 per-channel scales
   const uint16_t* res;    // [M][N] residual added before the output's rounding, or null
-  float* yf;              // k_gemv_adapt: [M][N] the sums, in place of y (or null)
   int M, N, K, G, ngroups, r;
   int S, ips, iw;         // K-slices per row group, iterations per slice and per wave
   int n_prod;             // EC workgroups at the head of the grid (fused)
@@ -247,6 +246,7 @@ enum { ADAPT_SLOTS = 0,  // the tokens of one slot (up to 64 tokens)
 struct AdapterGroup {
   AdapterParams p[kGroupMax];
   int shrink_start[kGroupMax + 1], expand_start[kGroupMax + 1];  // first workgroups
+  float* yf[kGroupMax];  // k_gemv_adapt, by GEMV member: [M][N] the sums, in place of y (or null)
   int n;
 };
 

@@ -760,9 +760,10 @@ __device__ void ec_wave(const GemvParams& a, uint32_t gen, char* smem, int n0, b
 // 16, bf16, one token: 8.4 us with it, 7.4 without; 4-bit product 8192 x 8192 at
 // one token 12.0 and 11.5; producer-fused 8192 x 8192, rank 32, 18.0 and 17.3).
 // ---------------------------------------------------------------------------
-// F32: with a.yf the sums leave in fp32, in place of y.
+// F32: with yf the sums leave in fp32, in place of y.
 template <int DT, int MT, int RT, int EPI, int WB, int NST, bool SPLIT, bool F32 = false>
-__device__ __forceinline__ void gemv_body(const GemvParams& a, int bid, uint32_t gen, char* smem) {
+__device__ __forceinline__ void gemv_body(const GemvParams& a, int bid, uint32_t gen, char* smem,
+                                          float* yf = nullptr) {
   __shared__ int s_flag;
   constexpr bool kEC = EPI == EPI_READY || EPI == EPI_FUSED;  // with an EC wave
   constexpr bool kLoc = EPI == EPI_LOCAL || EPI == EPI_LOCAL_I8;
@@ -1383,7 +1384,7 @@ __device__ __forceinline__ void gemv_body(const GemvParams& a, int bid, uint32_t
         v += ev;
       }
       if (a.res) v += act2f<DT>(res_pre ? resv : a.res[(size_t)m * N + n0 + row]);
-      if (F32 && a.yf) a.yf[(size_t)m * N + n0 + row] = v;  // (uniform)
+      if (F32 && yf) yf[(size_t)m * N + n0 + row] = v;  // (uniform)
       else a.y[(size_t)m * N + n0 + row] = f2act<DT>(v);
     }
   }
@@ -1455,12 +1456,29 @@ __global__ __launch_bounds__(kGemvMaxThreads, gemv_min_waves(MT, RT, EPI)) void 
 #pragma unroll
   for (int j = 1; j < kGroupMax; ++j)
     if (j < g.n && b >= g.start[j]) i = j;
-  gemv_body<DT, MT, RT, EPI, WB, 2, SPLIT, true>(g.p[i], b - g.start[i], 0u, smem);
+  gemv_body<DT, MT, RT, EPI, WB, 2, SPLIT, true>(g.p[i], b - g.start[i], 0u, smem, a.yf[i]);
 }
 
 // ---------------------------------------------------------------------------
 // launchers
 // ---------------------------------------------------------------------------
+static bool gemv_group_ok(int epi, const GemvGroup& g) {
+  if (g.n < 1 || g.n > kGroupMax || g.start[0] != 0) return false;
+  const bool loc = epi == EPI_LOCAL || epi == EPI_LOCAL_I8;
+  for (int i = 0; i < g.n; ++i) {
+    const GemvParams& p = g.p[i];
+    if (g.start[i + 1] < g.start[i] || p.S < 1 ||
+        (p.S > 1 && (!p.ypart || !p.rb_ctr || (loc && !p.eupart))) ||
+        (epi == EPI_LOCAL_I8 && (!p.ec.A8 || !p.ec.sa || !p.B8 || !p.sb)))
+      return false;
+  }
+  return true;
+}
+
+// The calls with adapters compile to a code object of their own: among them, the
+// kernels of the calls without were unchanged instruction for instruction and yet
+// 1 % slower (2048-wide decode block at 24 tokens, INT8 factors: 333 and 337 us).
+#if !SPEAR_ADAPT_UNIT
 #if SPEAR_WB == 4
 
 hipError_t SPEAR_D(launch_ec)(const EcGroup& g, int block, int ipp, size_t lds, hipStream_t st) {
@@ -1609,19 +1627,6 @@ static hipError_t gemv_group_launch(int epi, const GemvGroup& g, int block, size
 #undef SPEAR_GEMV_GROUP_GO
 }
 
-static bool gemv_group_ok(int epi, const GemvGroup& g) {
-  if (g.n < 1 || g.n > kGroupMax || g.start[0] != 0) return false;
-  const bool loc = epi == EPI_LOCAL || epi == EPI_LOCAL_I8;
-  for (int i = 0; i < g.n; ++i) {
-    const GemvParams& p = g.p[i];
-    if (g.start[i + 1] < g.start[i] || p.S < 1 ||
-        (p.S > 1 && (!p.ypart || !p.rb_ctr || (loc && !p.eupart))) ||
-        (epi == EPI_LOCAL_I8 && (!p.ec.A8 || !p.ec.sa || !p.B8 || !p.sb)))
-      return false;
-  }
-  return true;
-}
-
 hipError_t SPEAR_W(launch_gemv_group)(int MT, int RT, int epi, const GemvGroup& g,
                                       int block, size_t lds, hipStream_t st) {
   if (!gemv_group_ok(epi, g)) return hipErrorInvalidValue;
@@ -1633,6 +1638,8 @@ hipError_t SPEAR_W(launch_gemv_group)(int MT, int RT, int epi, const GemvGroup& 
 #undef SPEAR_GEMV_GROUP_CASE
   return hipErrorInvalidValue;
 }
+
+#else  // SPEAR_ADAPT_UNIT
 
 // The GEMV with adapters' coordinates: up to two token tiles, the product alone
 // and the local EC variants.
@@ -1680,5 +1687,7 @@ hipError_t SPEAR_W(launch_gemv_adapt)(int MT, int RT, int epi, const GemvGroup& 
 #undef SPEAR_GEMV_ADAPT_CASE
   return hipErrorInvalidValue;
 }
+
+#endif  // SPEAR_ADAPT_UNIT
 
 }  // namespace spear
