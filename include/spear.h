@@ -404,7 +404,7 @@ spear_status_t spear_adapters_workspace(int32_t n, const spear_layer_call_t* cal
  * order. Errors as for spear_w4ec_linear_tail and spear_adapters_workspace,
  * plus SPEAR_E_NULL for missing adapters, A, B or ids, SPEAR_E_ALIGN for a
  * misaligned pointer or a_stride, SPEAR_E_SHAPE for a stride smaller than its
- * slot, SPEAR_E_ALIAS for an output overlapping an adapter buffer. */
+ * slot or of 2^31 or more, SPEAR_E_ALIAS for an output overlapping an adapter buffer. */
 spear_status_t spear_w4ec_linear_adapters(const spear_problem_t* prob, const void* x,
                                           const spear_w4_t* w, const spear_ec_t* ec,
                                           const spear_adapters_t* adapters, const spear_tail_t* tail,

@@ -417,6 +417,8 @@ def adapters(A, B, ids, ranks=None, scale=None) -> Adapters:
         return None if t is None else t.data_ptr()
 
     far = L > 1 and r > 0
+    if far and min(A.stride(0) - r * K, B.stride(0) - r * B.shape[1]) < 0:
+        raise ValueError("adapters: slots may not overlap")  # (a stride of zero would mean dense slots)
     a = Adapters(L, r, p(A), p(B), A.stride(0) if far else 0, B.stride(0) if far else 0, p(ranks),
                  p(scale), p(ids))
     a._keep = (A, B, ids, ranks, scale)
@@ -471,7 +473,7 @@ def w4ec_linear_adapters(prob: Problem, x, qweight, scales, zeros, adapters, y, 
     """The layer with its tokens' adapters (include/spear.h), and with the
     post-EC tail where a residual or norm_w is given; ec_args as in
     w4ec_linear_tail."""
-    dev = _device_of(x, qweight, scales, zeros, y)
+    dev = _device_of(x, qweight, scales, zeros, y, residual, norm_w, y_norm, workspace)
     _check_adapters(prob, dev, adapters)
     w = W4(qweight.data_ptr(), scales.data_ptr(), zeros.data_ptr())
     ec = ctypes.byref(_ec_from_args(ec_args)) if ec_args is not None else None
@@ -495,7 +497,7 @@ def w4ec_linear_adapters_group(members, workspace=None, stream=None):
     (None: none)."""
     dev = torch.cuda.current_device()
     for m in members:
-        _device_of(m["x"], m["qweight"], m["scales"], m["zeros"], m["y"])
+        _device_of(m["x"], m["qweight"], m["scales"], m["zeros"], m["y"], workspace)
         _check_adapters(m["prob"], dev, m.get("adapters"))
     arr, keep = _group_array(members)
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
@@ -515,6 +517,8 @@ def _rows(t, shape, dtype, what):
     ld, one = t.stride()
     if one != 1 and shape[1] > 1 and shape[0] > 0:
         raise ValueError(f"block_norm: {what} has dense rows")
+    if shape[0] > 1 and ld < shape[1]:  # (zero would mean N)
+        raise ValueError(f"block_norm: the rows of {what} overlap")
     return ld if shape[0] > 1 else 0
 
 

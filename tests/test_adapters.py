@@ -209,6 +209,35 @@ def test_binding_refuses_what_the_library_cannot_see():
         sp.block_norm(x, x, x.clone(), None)
 
 
+def test_binding_refuses_overlapping_slots_and_rows():
+    """Strides of zero (an expanded tensor) mean dense to the library."""
+    A, B = torch.zeros(1, 8, 256, dtype=torch.float16), torch.zeros(3, 64, 8, dtype=torch.float16)
+    ids = torch.zeros(5, dtype=torch.int32)
+    with pytest.raises(ValueError, match="overlap"):
+        sp.adapters(A.expand(3, 8, 256), B, ids)
+    with pytest.raises(ValueError, match="overlap"):
+        sp.adapters(A.repeat(3, 1, 1), B[:1].expand(3, 64, 8), ids)
+    flat = torch.zeros(8 * 256 * 3, dtype=torch.float16)
+    with pytest.raises(ValueError, match="overlap"):
+        sp.adapters(flat.as_strided((3, 8, 256), (256, 256, 1)), B, ids)
+    sp.adapters(A, B[:1], ids)
+    rows = torch.zeros(1, 64, dtype=torch.float16)
+    with pytest.raises(ValueError, match="overlap"):
+        sp._rows(rows.expand(4, 64), (4, 64), torch.float16, "y")
+    with pytest.raises(ValueError, match="overlap"):
+        sp._rows(flat.as_strided((4, 64), (8, 1)), (4, 64), torch.float16, "h_out")
+    assert sp._rows(rows, (1, 64), torch.float16, "y") == 0
+    assert sp._rows(flat.as_strided((4, 64), (80, 1)), (4, 64), torch.float16, "y") == 80
+
+
+def test_products_past_32_bits_refused():
+    big = sp.problem(1 << 21, 128, 256)
+    assert _call(_ad(r=256), prob=big, ec=False) == -2  # 2^21 tokens, 256 ranks
+    assert _call(_ad(r=224), prob=big, ec=False, ws=None) == -5  # fits: the workspace is asked for
+    assert _call(_ad(r=256), prob=sp.problem(1, 1 << 22, 128), ec=False) == -2
+    assert _call(_ad(r=256), prob=sp.problem(1, 16, 1 << 22), ec=False) == -2
+
+
 def test_oracle_against_loops():
     rng = np.random.default_rng(0)
     x, A, B = rng.normal(size=(5, 6)), rng.normal(size=(3, 4, 6)), rng.normal(size=(3, 7, 4))

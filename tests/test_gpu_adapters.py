@@ -426,3 +426,159 @@ def test_another_stream_and_far_slots():
     sp.w4ec_linear_adapters(m["prob"], dl.x, dl.qweight, dl.scales, dl.zeros, ad, dl.y, workspace=ws, stream=st)
     st.synchronize()
     assert np.all(np.abs(dl.y.double().cpu().numpy() - ref) <= s.bound(_x(dl), ref, ref))
+
+
+@pytest.mark.parametrize("M,N,K,L,R", [(1, 520, 1152, 3, 16), (16, 256, 1024, 16, 16), (27, 1000, 512, 5, 40), (32, 130, 256, 40, 8)])
+@pytest.mark.parametrize("dt", [S.F16, S.BF16])
+def test_one_rounding_at_decode(M, N, K, L, R, dt):
+    """The layer, the term and the residual meet before y is rounded. Small integers
+    and powers of two: every sum is exact in fp32 (up to 2^22 in steps of one before
+    the powers), u in two parts too, and y is the exact sum rounded once; from 17
+    tokens on, where the layer is a GEMM, the term with the residual is rounded too."""
+    from paper_2606_11244_amd import spear as sp
+    lay, dl = _layer(M, N, K, dt, seed=M)
+    g = torch.Generator().manual_seed(K)
+    dl.x.copy_(torch.randint(-2, 3, (M, K), generator=g))
+    bits = np.full_like(lay.scales, np.float16(2.0 ** -6).view(np.uint16))
+    dl.scales.copy_(torch.from_numpy(bits.view(np.int16)).view(dl.scales.dtype))
+    s = Slots(M, N, K, L, R, dt, ids="turn", seed=5)
+    s.A.copy_(torch.randint(-1, 2, s.A.shape, generator=g))
+    s.B.copy_(torch.randint(-3, 4, s.B.shape, generator=g) * 2.0 ** -7)
+    s.scale = 2.0 ** torch.randint(-1, 2, (L,), generator=g).float()
+    res = (torch.randint(-99, 100, (M, N), generator=g) * 2.0 ** -6).to(DT[dt])
+    log(f"one rounding M={M} N={N} K={K} L={L} R={R} dt={dt}")
+    y = _call(dl, s.device(), residual=res.cuda())
+    W = O.dequant(lay.qweight, bits, lay.zeros, lay.group_size)
+    assert np.abs(W).max() >= 2.0 ** -4
+
+    def rounded(v):
+        assert np.array_equal(v, np.float32(v))
+        return torch.from_numpy(v).float().to(DT[dt]).double().numpy()
+    rest = s.term(_x(dl)) + res.double().numpy()
+    gemv = sp.dispatch_plan(dl.problem(), with_ec=False).path == sp.PATH_FUSED_GEMV
+    assert gemv or M > 16
+    assert np.array_equal(y, rounded(O.w4_linear(_x(dl), W) + (rest if gemv else rounded(rest))))
+
+
+MIXED = [
+    # (M, N, K, EC rank, weight bits, INT8 factors, dtype, adapters (L, R)) of each member
+    [(4, 256, 512, 16, 4, False, S.F16, (3, 8)), (4, 256, 512, 16, 4, False, S.BF16, (3, 8)),
+     (4, 128, 512, 0, 3, False, S.F16, (2, 16)), (20, 64, 256, 0, 4, False, S.F16, None)],
+    [(8, 512, 1024, 16, 4, True, S.F16, (8, 16)), (8, 512, 1024, 16, 4, True, S.F16, None),
+     (8, 512, 1024, 0, 4, False, S.F16, (8, 24)), (40, 512, 1024, 0, 3, False, S.BF16, (8, 16))],
+    [(1, 4096, 1024, 0, 4, False, S.F16, (2, 8)), (30, 128, 1024, 0, 4, False, S.F16, (30, 8)),
+     (64, 128, 1024, 32, 4, False, S.F16, (5, 8)), (65, 128, 1024, 0, 4, False, S.F16, (5, 8))],
+]
+
+
+def _mixed(spec, seed=0):
+    from paper_2606_11244_amd import spear as sp
+    members = []
+    for i, (M, N, K, rank, bits, i8, dt, lr) in enumerate(spec):
+        kw = dict(weight_bits=bits) if bits != 4 else {}
+        if i8:
+            kw["ab_int8"] = True
+        _, dl = _layer(M, N, K, dt, seed=seed + i, rank=rank, **kw)
+        m = dl.member(dl.problem(), with_ec=rank > 0)
+        m["y"] = torch.full((M, N), 7.0, dtype=DT[dt], device="cuda")
+        m["adapters"] = Slots(M, N, K, *lr, dt, seed=i).device() if lr else None
+        members.append(m)
+    return sp, members
+
+
+def _singly(sp, m, ws=None):
+    M, K, N = m["prob"].M, m["prob"].K, m["prob"].N
+    t = m["y"].dtype
+    ad = m["adapters"] or sp.adapters(torch.empty(0, 1, K, dtype=t, device="cuda"), torch.empty(0, N, 1, dtype=t, device="cuda"),
+                                      torch.zeros(M, dtype=torch.int32, device="cuda"))
+    if ws is None:
+        ws = torch.zeros(sp.adapters_workspace([dict(m, adapters=ad)]), dtype=torch.uint8, device="cuda")
+    y = torch.empty_like(m["y"])
+    sp.w4ec_linear_adapters(m["prob"], m["x"], m["qweight"], m["scales"], m["zeros"], ad, y, ec_args=m["ec_args"], workspace=ws)
+    torch.cuda.synchronize()
+    return y
+
+
+@pytest.mark.parametrize("spec", MIXED)
+def test_groups_of_unlike_members(spec):
+    """Code widths, activation dtypes, INT8 factors, members that share no launch."""
+    sp, members = _mixed(spec)
+    want = [_singly(sp, m) for m in members]
+    ws = torch.zeros(sp.adapters_workspace(members), dtype=torch.uint8, device="cuda")
+    for order in ([0, 1, 2, 3], [3, 1, 0, 2], [2, 3, 1, 0]):
+        log(f"mixed group {spec} order {order}")
+        for m in members:
+            m["y"].fill_(7.0)
+        group = [members[i] for i in order]
+        assert sp.adapters_workspace(group) == ws.numel()
+        sp.w4ec_linear_adapters_group(group, ws)
+        torch.cuda.synchronize()
+        for m, y in zip(members, want):
+            assert torch.equal(m["y"], y)
+
+
+@pytest.mark.parametrize("stages,shape", [(4, None), (2, (2, 2, 4)), (None, (1, 3, 8))])
+@pytest.mark.parametrize("dt", [S.F16, S.BF16])
+def test_other_launch_shapes_of_the_layer(stages, shape, dt):
+    """K-slices, row tiles and pipelines of the decode GEMV other than the planner's."""
+    from paper_2606_11244_amd import spear as sp
+    M, N, K = 9, 520, 2048
+    lay, dl = _layer(M, N, K, dt, seed=4)
+    s = Slots(M, N, K, 4, 16, dt, seed=4)
+    log(f"adapters stages {stages} shape {shape} dt={dt}")
+    try:
+        if stages:
+            sp.set_gemv_stages(stages)
+        if shape:
+            sp.set_gemv_shape(*shape)
+        y = _call(dl, s.device())
+    finally:
+        sp.set_gemv_stages(0)
+        sp.set_gemv_shape(0, 0, 0)
+    x = _x(dl)
+    assert_parity(y, O.w4_linear(x, O.dequant(lay.qweight, lay.scales, lay.zeros, lay.group_size)) + s.term(x), "launch shapes")
+
+
+def test_two_graphs_share_a_workspace():
+    """Captured calls of different shapes on one workspace, replayed in turn."""
+    from paper_2606_11244_amd import spear as sp
+    sets = [_mixed(spec, seed=20 * k)[1] for k, spec in enumerate(MIXED)]
+    want = [[_singly(sp, m) for m in ms] for ms in sets]
+    ws = torch.zeros(max(sp.adapters_workspace(ms) for ms in sets), dtype=torch.uint8, device="cuda")
+    graphs = []
+    for ms in sets:
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            sp.w4ec_linear_adapters_group(ms, ws)
+        torch.cuda.current_stream().wait_stream(side)
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            sp.w4ec_linear_adapters_group(ms, ws)
+        graphs.append(g)
+    for k in (0, 1, 2, 1, 0, 0, 2, 1):
+        log(f"two graphs: {k}")
+        for m in sets[k]:
+            m["y"].fill_(7.0)
+        graphs[k].replay()
+        torch.cuda.synchronize()
+        for m, y in zip(sets[k], want[k]):
+            assert torch.equal(m["y"], y)
+
+
+def test_two_calls_at_once():
+    """Two streams, the same weights and adapters, a workspace each."""
+    sp, members = _mixed(MIXED[2])
+    want = [_singly(sp, m) for m in members]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    other = [dict(m, y=torch.empty_like(m["y"])) for m in members]
+    ws = [torch.zeros(sp.adapters_workspace(members), dtype=torch.uint8, device="cuda") for _ in range(2)]
+    torch.cuda.synchronize()
+    log("two calls at once")
+    for _ in range(5):
+        for ms, w, st in zip((members, other), ws, streams):
+            sp.w4ec_linear_adapters_group(ms, w, stream=st)
+    torch.cuda.synchronize()
+    for ms in (members, other):
+        for m, y in zip(ms, want):
+            assert torch.equal(m["y"], y)

@@ -258,3 +258,53 @@ def test_a_block_of_both():
         c = dict(M=M, N=D, dt=torch.float16, f32=False, kind="mul", rho=1.0, beta=beta, off=0.0, eps=1e-5, y=y.cpu(),
                  h=hin.cpu(), post_w=w[i].cpu(), pre_w=w[i + 1].cpu(), gate=None, gate_ids=None)
         _check(c, hn.double().cpu().numpy(), xn.double().cpu().numpy())
+
+
+@pytest.mark.parametrize("N", [264, 5003])
+@pytest.mark.parametrize("f32", [False, True])
+def test_rows_past_32_bits(N, f32):
+    """The last rows lie past 2^32 bytes: the same values as dense rows."""
+    from paper_2606_11244_amd import spear as sp
+    M, ld = 5, (1 << 29) + 8
+    g = torch.Generator().manual_seed(N)
+    y, h = (torch.randn(M, N, generator=g).half().cuda() for _ in range(2))
+    w = torch.randn(N, generator=g).half().cuda()
+    h = h.float() if f32 else h
+    want, x = torch.empty_like(h), torch.empty_like(y)
+    sp.block_norm(y, h, want, x, post_w=w, pre_w=w, stream_scale=0.5)
+
+    def far(t):
+        big = torch.empty((M - 1) * ld + N, dtype=t.dtype, device="cuda").as_strided((M, N), (ld, 1))
+        return big.copy_(t)
+    log(f"block norm rows past 32 bits N={N} f32={f32}")
+    fy, fh, fx = far(y), far(h), far(torch.zeros_like(y))
+    sp.block_norm(fy, fh, fh, fx, post_w=w, pre_w=w, stream_scale=0.5)
+    torch.cuda.synchronize()
+    assert torch.equal(fh, want) and torch.equal(fx, x) and torch.equal(fy, y)
+
+
+def test_two_calls_at_once():
+    """Two streams read the same input and weights."""
+    from paper_2606_11244_amd import spear as sp
+    y, h = torch.randn(300, 4096, device="cuda").half(), torch.randn(300, 4096, device="cuda").half()
+    w = torch.randn(4096, device="cuda").half()
+    outs = [(torch.empty_like(y), torch.empty_like(y)) for _ in range(3)]
+    sp.block_norm(y, h, *outs[2], post_w=w, pre_w=w)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(5):
+        for st, o in zip(streams, outs):
+            sp.block_norm(y, h, *o, post_w=w, pre_w=w, stream=st)
+    torch.cuda.synchronize()
+    for o in outs[:2]:
+        assert torch.equal(o[0], outs[2][0]) and torch.equal(o[1], outs[2][1])
+
+
+@pytest.mark.parametrize("M,N", [(256, 4096), (257, 4096), (300, 2064), (260, 5003), (3000, 8192), (513, 8200)])
+@pytest.mark.parametrize("dt", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("f32", [False, True])
+def test_more_rows_than_cus(M, N, dt, f32):
+    """Rows of several chunks a thread, and workgroups that take several rows."""
+    log(f"block norm M={M} N={N} dt={dt} f32={f32}")
+    c = _case(M, N, dt, f32=f32, gates="ids", kind="sigmoid", rho=0.7, beta=-1.5, pad=0 if N % 8 else 8)
+    _check(c, *_run(c))
