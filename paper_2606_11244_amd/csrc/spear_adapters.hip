@@ -529,8 +529,8 @@ __device__ __forceinline__ int member(const int (&start)[kGroupMax + 1], int n, 
 
 // The parts of u once, for a GEMM whose tiles each read them: 16 threads a token,
 // four ranks of each 64. The GEMM adds them to the product's own sums, so that
-// small coordinates need no scaling (a part is off by at most 2^-25); large ones
-// in fp16 are divided by a power of two that its weight tile is multiplied by.
+// small coordinates need no scaling (a part is off by at most 2^-25); those past
+// fp16's range are divided by a power of two that its weight tile is multiplied by.
 template <int DT>
 __global__ __launch_bounds__(256) void k_adapter_parts(AdapterGroup g) {
   const int b = member(g.expand_start, g.n, blockIdx.x);
@@ -552,7 +552,7 @@ __global__ __launch_bounds__(256) void k_adapter_parts(AdapterGroup g) {
     }
 #pragma unroll
     for (int h = 8; h > 0; h >>= 1) mx = fmaxf(mx, __shfl_xor(mx, h));
-    k = max(0, (int)(__float_as_uint(mx) >> 23) - 127 - 14);
+    k = mx > 65504.f ? (int)(__float_as_uint(mx) >> 23) - 127 - 14 : 0;
   }
   if (m >= p.M) return;
   if (q == 0) p.ukx[m] = k;

@@ -274,6 +274,24 @@ def test_bad_values_stay_with_their_request(M, gemm, dt):
         _bad_values(M, dt)
 
 
+@pytest.mark.parametrize("M,N,K", [(70, 264, 512), (300, 513, 384), (600, 4096, 256)])
+@pytest.mark.parametrize("dt", [S.F16, S.BF16])
+def test_tokens_without_an_adapter_in_the_gemm(M, N, K, dt):
+    """They get what the plain call writes there."""
+    from paper_2606_11244_amd import spear as sp
+    log(f"without an adapter in the GEMM M={M} N={N} K={K} dt={dt}")
+    _, dl = _layer(M, N, K, dt, seed=M)
+    prob, plain = dl.problem(), torch.empty_like(dl.y)
+    with in_the_gemm():
+        dl.run_w4(prob, sp.allocate_workspace(prob, False), y=plain)
+        torch.cuda.synchronize()
+        plain = plain.double().cpu().numpy()
+        for ids in ("random", "none"):
+            s = Slots(M, N, K, 5, 24, dt, ids=ids, seed=9)
+            out = ((s.ids < 0) | (s.ids >= 5)).numpy()
+            assert out.any() and np.array_equal(_call(dl, s.device())[out], plain[out])
+
+
 def _bad_values(M, dt):
     N, K, L, R = 144, 256, 4, 16
     _, dl = _layer(M, N, K, dt, seed=1)
