@@ -974,13 +974,20 @@ hipError_t launch_gemm_wb(const Resolved& z, int epi, const GemmParams& p, hipSt
   return SPEAR_BY_WB(launch_gemm, z.wb, z.dt)(epi, p, st);
 }
 
-// the EC pre-kernel of one layer
-spear_status_t run_ec(const Resolved& z, const EcParams& e, hipStream_t st) {
+// the EC pre-kernel of one layer, with its adapters' coordinates or null
+spear_status_t run_ec(const Resolved& z, const EcParams& e, hipStream_t st, const AdapterParams* ad = nullptr) {
   EcGroup g;
   std::memset(&g, 0, sizeof(g));
   g.p[0] = e;
   g.start[1] = z.ntb * z.P * z.PG;
   g.n = 1;
+  if (ad) {
+    AdapterGroup a;
+    std::memset(&a, 0, sizeof(a));
+    a.p[0] = *ad;
+    a.n = 1;
+    return hip_status(SPEAR_BY_DT(launch_ec_adapt, z.dt)(g, a, z.ec_block, z.ec_ipp, z.lds_prod, st));
+  }
   return hip_status(SPEAR_BY_DT(launch_ec, z.dt)(g, z.ec_block, z.ec_ipp, z.lds_prod, st));
 }
 
@@ -1223,7 +1230,10 @@ spear_status_t check_tail(const spear_problem_t* prob, const void* x, const spea
 
 // How a member's term joins its layer:
 // - ADAPT_BEFORE: formed first, in the workspace (d), with the tail's residual,
-//   it enters the layer as the residual of its final store;
+//   it enters the layer as the residual of its final store. Up to 64 tokens the
+//   coordinates go with the EC pre-kernel's launch where the layer has one (3584 x
+//   8192, rank 64, 48 tokens: 12.2 us for that launch, 10.4 without and 7.2 for the
+//   coordinates alone; the call 43.1 and 37.9);
 // - ADAPT_RIDES: the coordinates go with the layer's GEMV launch as further
 //   workgroups; its sums stay in fp32 (yf), and a launch after it adds the term
 //   and the tail's residual and writes y. Where the layer is one GEMV launch:
@@ -1390,6 +1400,7 @@ struct AdapterCall {
   const spear_layer_call_t* calls = nullptr;
   AdapterLayout al[SPEAR_GROUP_MAX];
   AdapterParams p[SPEAR_GROUP_MAX];  // of the members that are on
+  bool with_ec[SPEAR_GROUP_MAX] = {};  // the coordinates go with the EC pre-kernel
 
   // members by `pick`, those of one activation dtype in one launch each
   template <class Pick, class Launch>
@@ -1405,15 +1416,19 @@ struct AdapterCall {
     }
     return SPEAR_OK;
   }
-  spear_status_t expand(int join, hipStream_t s) const {
-    return each([&](int i) { return al[i].join == join; }, [&](int dt, const AdapterGroup& g) {
-      return SPEAR_BY_DT(launch_adapter_expand, dt)(g, s);
-    });
+  template <class Pick>
+  spear_status_t expand(Pick pick, hipStream_t s) const {
+    return each(pick, [&](int dt, const AdapterGroup& g) { return SPEAR_BY_DT(launch_adapter_expand, dt)(g, s); });
   }
-  // before the layers: the coordinates of all members but those that ride along,
-  // and the terms that enter the layers as residuals, res[i]
+  // member i's coordinates go with its layer's EC pre-kernel
+  bool ec_takes(int i, const Resolved& z) const {
+    return al[i].on && al[i].join == ADAPT_BEFORE && al[i].p.kind == ADAPT_SLOTS && z.ec &&
+           z.plan.path == SPEAR_PATH_UNFUSED_2K;
+  }
+  // before the layers: the coordinates of all members but those that go with
+  // another launch, and the terms that enter the layers as residuals, res[i]
   spear_status_t before(const uint16_t** res, hipStream_t s) const {
-    spear_status_t st = each([&](int i) { return al[i].join != ADAPT_RIDES; }, [&](int dt, const AdapterGroup& g) {
+    spear_status_t st = each([&](int i) { return al[i].join != ADAPT_RIDES && !with_ec[i]; }, [&](int dt, const AdapterGroup& g) {
       return SPEAR_BY_DT(launch_adapter_shrink, dt)(g, s);
     });
     if (st == SPEAR_OK)
@@ -1423,12 +1438,20 @@ struct AdapterCall {
     if (st != SPEAR_OK) return st;
     for (int i = 0; i < n; ++i)
       if (al[i].on && al[i].join == ADAPT_BEFORE) res[i] = p[i].d;
-    return expand(ADAPT_BEFORE, s);
+    return expand([&](int i) { return al[i].join == ADAPT_BEFORE && !with_ec[i]; }, s);
   }
-  spear_status_t after(hipStream_t s) const { return expand(ADAPT_RIDES, s); }
+  spear_status_t after(hipStream_t s) const {
+    return expand([&](int i) { return al[i].join == ADAPT_RIDES; }, s);
+  }
   // the layer of a member that shares no launch
   spear_status_t layer(int i, const Resolved& z, const uint16_t* res, char* ws, hipStream_t s) const {
     const spear_layer_call_t& c = calls[i];
+    if (with_ec[i]) {
+      const EcParams e = ec_for_2k(c.prob, z, c.x, c.ec, ws);
+      spear_status_t st = run_ec(z, e, s, &p[i]);
+      if (st == SPEAR_OK) st = expand([&](int j) { return j == i; }, s);
+      return st != SPEAR_OK ? st : run_2k_main(c.prob, z, c.x, c.w, c.ec, e, c.y, res, ws, s);
+    }
     if (!al[i].on || al[i].join == ADAPT_BEFORE) return run_layer(c.prob, z, c.x, c.w, c.ec, c.y, res, ws, s);
     if (al[i].join == ADAPT_RIDES) {
       const bool ec = z.ec;
@@ -1713,7 +1736,7 @@ spear_status_t spear_group_launches(int32_t n, const spear_layer_call_t* calls, 
 
 // The launches of a grouped call after its checks.
 static spear_status_t run_group(int32_t n, const spear_layer_call_t* calls, Resolved* z, const size_t* off,
-                                const AdapterCall& ad, char* ws, hipStream_t s) {
+                                AdapterCall& ad, char* ws, hipStream_t s) {
   spear_status_t st = SPEAR_OK;
   // Members of one single-launch GEMV variant share one launch; the other
   // members run one after another on the same stream, as their own calls
@@ -1722,9 +1745,12 @@ static spear_status_t run_group(int32_t n, const spear_layer_call_t* calls, Reso
   int epi = -1, first = -1;
   const int n_in = group_select(n, calls, z, in, &epi, &first);
   int set[SPEAR_GROUP_MAX], ec_set[SPEAR_GROUP_MAX], gv_set[SPEAR_GROUP_MAX];
-  shared_sets(n, calls, z, in, set, ec_set, gv_set);
-  // the coordinates of adapters go with the shared GEMV launch, or first
+  // the coordinates of adapters go with the GEMV or EC launches, or first (as in
+  // the member's own call, also where the group has an EC pre-kernel for it that
+  // the call has not: the sums' order follows the launch)
   const uint16_t* res[SPEAR_GROUP_MAX] = {};
+  for (int i = 0; i < ad.n; ++i) ad.with_ec[i] = ad.ec_takes(i, z[i]);
+  shared_sets(n, calls, z, in, set, ec_set, gv_set);
   if (ad.n > 0 && (st = ad.before(res, s)) != SPEAR_OK) return st;
   // members that share nothing: each as its own call would run, in the
   // workspace a single call would use
@@ -1742,10 +1768,13 @@ static spear_status_t run_group(int32_t n, const spear_layer_call_t* calls, Reso
     if (ec_set[k] != k) continue;
     EcGroup g;
     std::memset(&g, 0, sizeof(g));
+    AdapterGroup a;
+    std::memset(&a, 0, sizeof(a));
     size_t lds = 0;
     int ctr = 0;
     for (int i = k; i < n; ++i) {
       if (ec_set[i] != k) continue;
+      if (ad.with_ec[i]) a.p[a.n++] = ad.p[i];
       ecp[i] = ec_for_2k(calls[i].prob, z[i], calls[i].x, calls[i].ec, ws + off[i]);
       ecp[i].ctr = (uint32_t*)(ws + kCtrEc) + ctr;
       ctr += z[i].ntb;
@@ -1754,7 +1783,12 @@ static spear_status_t run_group(int32_t n, const spear_layer_call_t* calls, Reso
       lds = std::max(lds, z[i].lds_prod);
       ++g.n;
     }
-    st = hip_status(SPEAR_BY_DT(launch_ec, z[k].dt)(g, z[k].ec_block, z[k].ec_ipp, lds, s));
+    if (a.n > 0) {
+      st = hip_status(SPEAR_BY_DT(launch_ec_adapt, z[k].dt)(g, a, z[k].ec_block, z[k].ec_ipp, lds, s));
+      if (st == SPEAR_OK) st = ad.expand([&](int i) { return ad.with_ec[i] && ec_set[i] == k; }, s);
+    } else {
+      st = hip_status(SPEAR_BY_DT(launch_ec, z[k].dt)(g, z[k].ec_block, z[k].ec_ipp, lds, s));
+    }
     if (st != SPEAR_OK) return st;
   }
   for (int k = 0; k < n; ++k) {
@@ -1992,6 +2026,7 @@ spear_status_t spear_w4ec_linear_adapters(const spear_problem_t* prob, const voi
   const bool with_term = al.on && al.join != ADAPT_EPILOGUE;
   if (al.on) ad.p[0] = make_adapters(call, adapters, al, with_term ? res : nullptr, ws);
   const uint16_t* in = with_term ? nullptr : res;  // what the layer adds
+  ad.with_ec[0] = ad.ec_takes(0, z[0]);
   if ((st = ad.before(&in, s)) != SPEAR_OK) return st;
   st = ad.layer(0, z[0], in, ws, s);
   if (st == SPEAR_OK) st = ad.after(s);

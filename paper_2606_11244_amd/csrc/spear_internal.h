@@ -320,6 +320,8 @@ __host__ __device__ inline size_t ec_block_lds(int NW, int R1p, int h, int r) {
   hipError_t launch_mid_##W(int MT, const GemmGroup& g, hipStream_t st);
 #define SPEAR_ACT_LAUNCHERS(D)                                                                    \
   hipError_t launch_ec_##D(const EcGroup& g, int block, int ipp, size_t lds, hipStream_t st);     \
+  hipError_t launch_ec_adapt_##D(const EcGroup& g, const AdapterGroup& all, int block, int ipp,   \
+                                 size_t lds, hipStream_t st);                                     \
   hipError_t launch_gate_##D(const EcParams& e, int ntb, size_t lds, hipStream_t st);            \
   /* y_norm[m] = RMSNorm(y[m]) * w (one workgroup per token row) */                              \
   hipError_t launch_rmsnorm_##D(const uint16_t* y, const uint16_t* w, float eps,                 \

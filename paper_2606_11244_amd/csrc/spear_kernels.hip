@@ -1459,6 +1459,27 @@ __global__ __launch_bounds__(kGemvMaxThreads, gemv_min_waves(MT, RT, EPI)) void 
   gemv_body<DT, MT, RT, EPI, WB, 2, SPLIT, true>(g.p[i], b - g.start[i], 0u, smem, a.yf[i]);
 }
 
+// The EC pre-kernel with the coordinates, in the same way: the term is formed
+// between it and the product, whose residual it is.
+template <int DT, int IPP>
+__global__ __launch_bounds__(512) void k_ec_adapt(EcGroup g, AdapterGroup a) {
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  int b = blockIdx.x, i = 0;
+  const int ng = g.start[g.n];
+  if (b >= ng) {
+    b -= ng;
+#pragma unroll
+    for (int j = 1; j < kGroupMax; ++j)
+      if (j < a.n && b >= a.shrink_start[j]) i = j;
+    shrink_slot<DT>(a.p[i], b - a.shrink_start[i], smem);
+    return;
+  }
+#pragma unroll
+  for (int j = 1; j < kGroupMax; ++j)
+    if (j < g.n && b >= g.start[j]) i = j;
+  ec_producer<DT, IPP, true>(g.p[i], b - g.start[i], 0u, smem);
+}
+
 // ---------------------------------------------------------------------------
 // launchers
 // ---------------------------------------------------------------------------
@@ -1667,15 +1688,37 @@ static hipError_t gemv_adapt_launch(int epi, const GemvGroup& g, const AdapterGr
 #undef SPEAR_GEMV_ADAPT_GO
 }
 
-hipError_t SPEAR_W(launch_gemv_adapt)(int MT, int RT, int epi, const GemvGroup& g, const AdapterGroup& all,
-                                      int block, size_t lds, hipStream_t st) {
-  if (!gemv_group_ok(epi, g) || all.n < 1 || all.n > kGroupMax) return hipErrorInvalidValue;
-  AdapterGroup a = all;
+// the workgroups of the coordinates, by member; false: not those of a decode call
+static bool place_slots(AdapterGroup& a) {
+  if (a.n < 1 || a.n > kGroupMax) return false;
   a.shrink_start[0] = 0;
   for (int i = 0; i < a.n; ++i) {
-    if (a.p[i].kind != ADAPT_SLOTS || a.p[i].M > 64) return hipErrorInvalidValue;
+    if (a.p[i].kind != ADAPT_SLOTS || a.p[i].M > 64) return false;
     a.shrink_start[i + 1] = a.shrink_start[i] + a.p[i].M * a.p[i].P * a.p[i].RG;
   }
+  return true;
+}
+
+#if SPEAR_WB == 4
+hipError_t SPEAR_D(launch_ec_adapt)(const EcGroup& g, const AdapterGroup& all, int block, int ipp, size_t lds,
+                                    hipStream_t st) {
+  AdapterGroup a = all;
+  if (g.n < 1 || g.n > kGroupMax || g.start[0] != 0 || !place_slots(a)) return hipErrorInvalidValue;
+  lds = std::max(lds, shrink_slot_lds(block / 64));
+  const auto go = [&](auto kern) {
+    hipError_t err = allow_lds(kern, lds);
+    if (err != hipSuccess) return err;
+    hipLaunchKernelGGL(kern, dim3(g.start[g.n] + a.shrink_start[a.n]), dim3(block), lds, st, g, a);
+    return hipGetLastError();
+  };
+  return ipp == 1 ? go(k_ec_adapt<DTC, 1>) : go(k_ec_adapt<DTC, 2>);
+}
+#endif
+
+hipError_t SPEAR_W(launch_gemv_adapt)(int MT, int RT, int epi, const GemvGroup& g, const AdapterGroup& all,
+                                      int block, size_t lds, hipStream_t st) {
+  AdapterGroup a = all;
+  if (!gemv_group_ok(epi, g) || !place_slots(a)) return hipErrorInvalidValue;
 #define SPEAR_GEMV_ADAPT_CASE(mt, rt) \
   if (MT == mt && RT == rt) return gemv_adapt_launch<DTC, mt, rt>(epi, g, a, block, lds, st);
   SPEAR_GEMV_ADAPT_CASE(1, 1)

@@ -351,6 +351,9 @@ GROUPS = [
     [(24, 512, 4096, 64, (9, 32)), (24, 512, 4096, 64, (9, 32))],
     [(48, 1024, 2048, 0, (6, 16)), (48, 1024, 2048, 32, (6, 24)), (3, 136, 256, 0, (2, 5))],
     [(2048, 8192, 128, 0, (3, 16)), (2048, 8200, 128, 0, (4, 40)), (70, 64, 128, 0, (3, 8))],
+    [(48, 520, 1024, 32, (6, 16)), (48, 264, 1024, 32, (48, 24)), (48, 136, 1024, 24, None), (40, 520, 1024, 32, (2, 8))],
+    [(1, 4096, 4096, 64, (2, 16)), (1, 1024, 4096, 64, (2, 16)), (1, 1024, 4096, 64, None)],
+    [(12, 1024, 4096, 64, (5, 16)), (12, 4096, 4096, 64, (5, 40))],
     [(200, 520, 512, 0, (3, 16)), (0, 64, 256, 0, (2, 4)), (200, 264, 512, 16, None), (70, 64, 256, 0, (9, 12))],
 ]
 
