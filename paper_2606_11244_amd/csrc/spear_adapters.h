@@ -27,22 +27,23 @@ struct TokenGroup {
   int cnt;     // tokens, 0: this token leads none
   int tok;     // this lane's: token lane % 16 of the group (past cnt: the leader)
 };
-// M <= 64; every wave of the workgroup calls it. stok: 16 ints of LDS.
+// Among the 64 tokens around m; every wave of the workgroup calls it. stok: 16
+// ints of LDS.
 __device__ __forceinline__ TokenGroup token_group(const AdapterParams& p, int m, int* stok) {
-  const int lane = threadIdx.x & 63;
-  const int id = lane < p.M ? slot_of(p, lane) : -2;
+  const int lane = threadIdx.x & 63, ml = m & 63, m0 = m - ml;
+  const int id = m0 + lane < p.M ? slot_of(p, m0 + lane) : -2;
   TokenGroup g;
-  g.a = __builtin_amdgcn_readlane(id, m);
+  g.a = __builtin_amdgcn_readlane(id, ml);
   const uint64_t same = __ballot(id == g.a);
-  const int before = __popcll(same & ((1ull << m) - 1));
+  const int before = __popcll(same & ((1ull << ml) - 1));
   g.cnt = 0;
   g.r = 0;
   g.tok = m;
   if (before & 15) return g;  // uniform
-  const uint64_t mine = same & ~((1ull << m) - 1);
+  const uint64_t mine = same & ~((1ull << ml) - 1);
   g.cnt = min(16, (int)__popcll(mine));
   const int pos = __popcll(mine & ((1ull << lane) - 1));
-  if (((mine >> lane) & 1) && pos < 16) stok[pos] = lane;  // every wave writes the same
+  if (((mine >> lane) & 1) && pos < 16) stok[pos] = m0 + lane;  // every wave writes the same
   __syncthreads();
   g.tok = stok[min(lane & 15, g.cnt - 1)];
   g.r = rank_of(p, g.a);
@@ -161,7 +162,7 @@ __device__ __forceinline__ void project(rsrc_t rx, const TokenGroup& g, const in
 }
 
 // ---------------------------------------------------------------------------
-// decode: u in slices over K
+// few tokens: u in slices over K
 // ---------------------------------------------------------------------------
 
 // Workgroup b of a member: the sums of one token's slot over a K-slice for one

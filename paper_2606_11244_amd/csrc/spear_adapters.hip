@@ -12,8 +12,8 @@
 // product with zero, so that no token meets another's values. u is held in
 // fp32 and enters the second MFMA as two activation-dtype parts.
 //
-// Decode (up to 64 tokens; its coordinates in spear_adapters.h): the tokens of
-// one slot, up to 16 of them, belong to the workgroups of the first of them
+// Up to 128 tokens (their coordinates in spear_adapters.h) the tokens of one slot
+// among 64, up to 16 of them, belong to the workgroups of the first of them
 // ("leader"); the other tokens' workgroups end at once. Nothing needs sorting,
 // and the ids are read on the device. Beyond, a workgroup owns 64 consecutive
 // tokens and walks the slots they name.

@@ -1230,7 +1230,7 @@ spear_status_t check_tail(const spear_problem_t* prob, const void* x, const spea
 
 // How a member's term joins its layer:
 // - ADAPT_BEFORE: formed first, in the workspace (d), with the tail's residual,
-//   it enters the layer as the residual of its final store. Up to 64 tokens the
+//   it enters the layer as the residual of its final store. Up to 128 tokens the
 //   coordinates go with the EC pre-kernel's launch where the layer has one (3584 x
 //   8192, rank 64, 48 tokens: 12.2 us for that launch, 10.4 without and 7.2 for the
 //   coordinates alone; the call 43.1 and 37.9);
@@ -1256,7 +1256,12 @@ struct AdapterLayout {
   AdapterParams p;  // the launch shape
 };
 
-constexpr int64_t kAdapterDecodeM = 64;  // tokens whose ids one wave holds, a lane each
+// Up to here the workgroups belong to slots, beyond to tiles of 64 tokens, which
+// walk their slots one after another (4096 x 4096, us, by slots and by tiles: 65
+// tokens of 64 slots, rank 64, 43.6 and 68.5, of 4, rank 16, 30.1 and 33.1; 128 of
+// 64 50.6 and 54.8, of 8 40.2 and 39.1; 256 of 8 45.1 and 43.5; 512 of 64 90 and
+// 66, of 4 59 and 53: there each 16 tokens of a slot read its factors again).
+constexpr int64_t kAdapterSlotsM = 128;
 
 // The launch shape of one member, by its own sizes alone.
 void adapters_shape(const spear_problem_t* p, const spear_adapters_t* a, AdapterParams* q) {
@@ -1265,17 +1270,21 @@ void adapters_shape(const spear_problem_t* p, const spear_adapters_t* a, Adapter
   q->RG = (int)cdiv(a->rank, 32);
   q->P = q->PA = 1;
   q->ips = IT;
-  if (M <= kAdapterDecodeM) {
+  if (M <= kAdapterSlotsM) {
     q->kind = ADAPT_SLOTS;
     // one workgroup for each token (those that lead no slot's tokens end at
-    // once), rank group and K-slice; K-slices of at
-    // least eight iterations while the leaders alone leave CUs idle
+    // once), rank group and K-slice. Up to 64 tokens K-slices of at least eight
+    // iterations while the tokens alone leave CUs idle (8B q, k, v at 16 requests:
+    // slices of eight 13.3 us, of four 15.1). Beyond, a slot usually has many
+    // tokens and few lead, so more and shorter slices, and more chunks of the term
+    // (4096 x 14336, 65 tokens of 8 slots, rank 64: 51.3 us, by the other rule 70)
+    const bool runs = M > 64;
     int P = 1;
-    while (M * q->RG * P < 256 && IT / (2 * P) >= 8) P *= 2;
+    while (M * q->RG * P < (runs ? 4096 : 256) && IT / (2 * P) >= (runs ? 4 : 8)) P *= 2;
     q->ips = (int)cdiv(IT, P);
     q->P = (int)cdiv(IT, q->ips);
     q->rpw = 1;
-    while (M * cdiv(p->N, 256 * q->rpw) > 1024 && q->rpw < 8) q->rpw *= 2;
+    while (M * cdiv(p->N, 256 * q->rpw) > (runs ? 4096 : 1024) && q->rpw < 8) q->rpw *= 2;
     q->chunks = (int)cdiv(p->N, 256 * q->rpw);
     return;
   }

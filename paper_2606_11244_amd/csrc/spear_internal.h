@@ -240,7 +240,7 @@ struct AdapterParams {
   int PA;                 // ADAPT_TILES: parts that share a tile's slots (u)
   int chunks, rpw;        // row chunks of the term, runs of 64 rows a wave in each
 };
-enum { ADAPT_SLOTS = 0,  // the tokens of one slot (up to 64 tokens)
+enum { ADAPT_SLOTS = 0,  // the tokens of one slot
        ADAPT_TILES = 1   // 64 consecutive tokens
 };
 struct AdapterGroup {

@@ -1693,7 +1693,7 @@ static bool place_slots(AdapterGroup& a) {
   if (a.n < 1 || a.n > kGroupMax) return false;
   a.shrink_start[0] = 0;
   for (int i = 0; i < a.n; ++i) {
-    if (a.p[i].kind != ADAPT_SLOTS || a.p[i].M > 64) return false;
+    if (a.p[i].kind != ADAPT_SLOTS) return false;
     a.shrink_start[i + 1] = a.shrink_start[i] + a.p[i].M * a.p[i].P * a.p[i].RG;
   }
   return true;

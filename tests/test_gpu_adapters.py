@@ -133,6 +133,8 @@ SHAPES = [
     (520, 640, 512, 9, 128, dict(ids="runs", mixed=True)), (1030, 72, 128, 5, 16, dict(ids="random")),
     (40, 64, 256, 3, 16, dict(ids="none")), (9, 33, 14336, 4, 32, dict(ids="turn")),
     (12, 7000, 128, 5, 20, {}), (100, 8, 8192, 8, 16, dict(ids="turn")),
+    (128, 520, 1152, 40, 24, dict(ids="turn", mixed=True)), (128, 1000, 256, 2, 72, dict(ids="runs")),
+    (129, 264, 512, 5, 16, dict(ids="runs")),
 ]
 
 
@@ -157,7 +159,7 @@ def test_term_alone(M, N, K, L, R, opt, dt):
 @contextlib.contextmanager
 def in_the_gemm():
     """Every call above 64 tokens without an EC on the 256 x 256 tiles, whose GEMM
-    forms the term itself."""
+    forms the term itself (above 128 tokens)."""
     from paper_2606_11244_amd import spear as sp
     sp.set_gemm_tile(256)
     sp.set_gemm_slices(1)
@@ -170,7 +172,7 @@ def in_the_gemm():
         sp.set_gemm_tile(0)
 
 
-TILED = [s for s in SHAPES if s[0] > 64] + [
+TILED = [s for s in SHAPES if s[0] > 64] + [(135, 264, 384, 5, 20, dict(ids="turn")), (190, 129, 128, 90, 7, dict(mixed=True)),
     (513, 300, 256, 6, 64, dict(ids="turn")), (256, 256, 128, 1, 16, dict(ids="one")), (300, 520, 384, 3, 72, dict(gap=3 * 8)),
     (270, 250, 128, 20, 130, dict(ids="runs", mixed=True)), (700, 257, 256, 4, 65, dict(ids="runs", scale=False)),
     (260, 512, 128, 2, 16, dict(ids="none"))]
@@ -265,7 +267,7 @@ def test_beside_the_layer(M, N, K, rank, dt):
     assert np.array_equal(_call(dl, zero.device(), ec=rank > 0), plain.double().cpu().numpy())
 
 
-@pytest.mark.parametrize("M,gemm", [(5, False), (20, False), (70, False), (200, False), (70, True), (300, True)])
+@pytest.mark.parametrize("M,gemm", [(5, False), (20, False), (70, False), (200, False), (70, True), (150, True), (300, True)])
 @pytest.mark.parametrize("dt", [S.F16, S.BF16])
 def test_bad_values_stay_with_their_request(M, gemm, dt):
     """Infinities and NaN of one adapter, and of one token, reach no other
@@ -274,7 +276,7 @@ def test_bad_values_stay_with_their_request(M, gemm, dt):
         _bad_values(M, dt)
 
 
-@pytest.mark.parametrize("M,N,K", [(70, 264, 512), (300, 513, 384), (600, 4096, 256)])
+@pytest.mark.parametrize("M,N,K", [(70, 264, 512), (140, 264, 512), (300, 513, 384), (600, 4096, 256)])
 @pytest.mark.parametrize("dt", [S.F16, S.BF16])
 def test_tokens_without_an_adapter_in_the_gemm(M, N, K, dt):
     """They get what the plain call writes there."""
