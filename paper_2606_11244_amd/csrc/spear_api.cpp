@@ -1290,15 +1290,17 @@ void adapters_shape(const spear_problem_t* p, const spear_adapters_t* a, Adapter
   }
   q->kind = ADAPT_TILES;
   const int64_t tiles = cdiv(M, 64);
+  // 512 workgroups for the term: each adds up its tokens' coordinates, so that more
+  // of them read more (8192 x 1024, 1024 tokens of 64 slots, rank 64: 2048 67.6 us,
+  // 1024 61.7, 512 56.8, 256 57.8)
   q->rpw = 1;
-  while (tiles * cdiv(p->N, 64 * q->rpw) > 2048 && q->rpw < 32) q->rpw *= 2;
+  while (tiles * cdiv(p->N, 64 * q->rpw) > 512 && q->rpw < 32) q->rpw *= 2;
   q->chunks = (int)cdiv(p->N, 64 * q->rpw);
   int P = 1;
-  // K-slices of two iterations or more while the tiles leave CUs idle, no more than
-  // 16, which the coordinates' readers add up (5000 x 2944, 77 tokens: slices of
-  // two 4.7 us, of four 6.0; 4096 x 14336, 300 tokens: 28 slices take 2.1 us
-  // longer to add than 16 and save nothing)
-  while (tiles * q->RG * P < 256 && P < 16 && IT / (2 * P) >= 2) P *= 2;
+  // K-slices of four iterations or more while the tiles leave CUs idle (4096 x 4096,
+  // 160 tokens of 64 slots, rank 64: slices of two 55.7 us, of four 51.8), no more
+  // than 16 (4096 x 14336, 300 tokens: 28 slices took 2.1 us longer to add up)
+  while (tiles * q->RG * P < 256 && P < 16 && IT / (2 * P) >= 4) P *= 2;
   q->ips = (int)cdiv(IT, P);
   q->P = (int)cdiv(IT, q->ips);
   // few tiles: their slots, as many as their tokens at worst, are shared out over
