@@ -396,10 +396,10 @@ spear_status_t spear_adapters_workspace(int32_t n, const spear_layer_call_t* cal
 /* spear_w4ec_linear (ec NULL: spear_w4_linear) with adapters, followed by the
  * post-EC tail if tail is not NULL. Y = the layer + the adapters' term + the
  * tail's residual, each summed in fp32. Where the layer is one decode GEMV
- * launch or runs on 256 x 256 tiles, nothing is rounded before Y itself;
- * elsewhere the term plus the residual is, once, to the act dtype. A token
+ * launch, or runs on tiles of 256 tokens and has at least 32 tokens a slot,
+ * nothing is rounded before Y itself; elsewhere the term plus the residual is, once, to the act dtype. A token
  * without an adapter gets what the call without adapters writes. In fp16 a
- * coordinate s_a A_a x may pass 65504; on 256 x 256 tiles Y[n] is then infinite
+ * coordinate s_a A_a x may pass 65504; on those tiles Y[n] is then infinite
  * where an entry of B_a's row n times (the token's largest coordinate / 2^14)
  * passes it too, and coordinates are held to 2^-25 there. No
  * token's result depends on another token's adapter or values. The workspace

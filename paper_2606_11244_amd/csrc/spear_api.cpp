@@ -1240,8 +1240,8 @@ spear_status_t check_tail(const spear_problem_t* prob, const void* x, const spea
 //   decode calls are latency, and this takes the first of the adapters' two
 //   launches off their path (8B q, k, v at 16 requests: 13.3 us for the launch, 12.9
 //   without adapters, 4.8 for the coordinates alone);
-// - ADAPT_EPILOGUE: k_gemm_ws on 256 x 256 tiles forms it, as further steps of its
-//   loop. Its epilogue with a residual costs as much as another pass over the
+// - ADAPT_EPILOGUE: k_gemm_ws (tiles of 256 tokens) forms it, as further steps of
+//   its loop. Its epilogue with a residual costs as much as another pass over the
 //   output (8B gate and up, 14336 x 4096 at 2048 tokens, fp16: 617 us with the term
 //   first, 574 with a pass after it that also rounds y once more, 482 this way,
 //   449 without adapters).
@@ -1332,9 +1332,17 @@ spear_status_t adapters_layout(int32_t n, const spear_layer_call_t* calls, const
       off += round256(bytes);
       return o;
     };
+    // A further step of the GEMM's loop for each slot and 32 ranks costs as much as
+    // one of K: it pays while a tile of 256 tokens meets few slots, about 8 where
+    // they come in runs and every slot is in use (8192 x 1024, us, in the GEMM and
+    // before it: 1024 tokens of 4 slots, rank 16, 37.6 and 49.6, of 16 42.9 and 49.0,
+    // of 64 68 and 47; 2048 of 64 71.0 and 70.8, in random order 262 and 180; 4096
+    // of 64 107 and 121). The hook that asks for these tiles asks for this too.
+    const bool ws = !z[i].gemv && !z[i].ec && (z[i].groles == 2 || z[i].groles == 3);
+    const bool few_slots = (int64_t)a->n_adapters * 32 <= p->M || g_ov_gr.load() >= 2;
     al[i].join = q.kind == ADAPT_SLOTS && group_epi(z[i], calls[i].ec) >= 0 && z[i].MT <= 2 && z[i].nst == 2 ? ADAPT_RIDES
-                 : q.kind == ADAPT_TILES && !z[i].gemv && !z[i].ec && z[i].groles == 3                      ? ADAPT_EPILOGUE
-                                                                                                           : ADAPT_BEFORE;
+                 : q.kind == ADAPT_TILES && ws && few_slots                                                 ? ADAPT_EPILOGUE
+                                                                                                            : ADAPT_BEFORE;
     const size_t uw = (size_t)p->M * 32 * q.RG;
     al[i].upart = take(q.P * uw * 4);
     if (al[i].join == ADAPT_EPILOGUE) {

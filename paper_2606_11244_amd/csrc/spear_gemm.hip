@@ -678,7 +678,8 @@ __device__ __forceinline__ void gemm_ws_body(const GemmParams& a, const AdapterP
     uint64_t left[4] = {0, 0, 0, 0};
     int slot = -1, k2 = 0, r = 0, kr0 = 0, pslot = -1, pk2 = 0, nstep = 0;
     bool have = false;
-    u32x4 xv[8], wv[4];
+    constexpr int WR = TN / 64;  // weight rows of a thread
+    u32x4 xv[8], wv[WR];
     auto adapt_tokens = [&]() {
       const int m = m0 + pt, s = m < M ? slot_of(ad, m) : -1;  // (TM loading threads)
       const int n = rank_of(ad, s);
@@ -729,7 +730,7 @@ __device__ __forceinline__ void gemm_ws_body(const GemmParams& a, const AdapterP
       const int col = kr0 + 8 * (pt & 3);
       const uint16_t* B = ad.B + (size_t)slot * ad.b_stride + col;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < WR; ++i) {
         const int n = n0 + (pt >> 2) + 64 * i;
         wv[i] = u32x4{0, 0, 0, 0};
         if (n < N && col < r) {
@@ -769,7 +770,7 @@ __device__ __forceinline__ void gemm_ws_body(const GemmParams& a, const AdapterP
         *(u32x4*)(xs + t * kGemmTK + 8 * ((pt & 7) ^ (t & 7))) = xv[i];
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < WR; ++i) {
         const int row = (pt >> 2) + 64 * i;
         bool bad = false;
 #pragma unroll
@@ -973,27 +974,30 @@ template <int DT, int EPI, int TNB, int WB, bool PLAIN>
 __global__ __launch_bounds__(256 * (1 + TNB), 1) void k_gemm_ws(GemmParams a) {
   gemm_ws_body<DT, EPI, TNB, WB, PLAIN>(a, AdapterParams{});
 }
-template <int DT, int WB, bool PLAIN>
-__global__ __launch_bounds__(768, 1) void k_gemm_ws_adapt(GemmParams a, AdapterParams ad) {
-  gemm_ws_body<DT, EPI_ADAPT, 2, WB, PLAIN>(a, ad);
+template <int DT, int TNB, int WB, bool PLAIN>
+__global__ __launch_bounds__(256 * (1 + TNB), 1) void k_gemm_ws_adapt(GemmParams a, AdapterParams ad) {
+  gemm_ws_body<DT, EPI_ADAPT, TNB, WB, PLAIN>(a, ad);
 }
 
 // ---------------------------------------------------------------------------
 // launchers
 // ---------------------------------------------------------------------------
 hipError_t SPEAR_W(launch_gemm_adapt)(const GemmParams& p, const AdapterParams& ad, hipStream_t st) {
-  if (p.tmw != 4 || p.S != 1 || p.roles != 3 || !ad.uh || !ad.ul || !ad.ukx || ad.M != p.M || ad.N != p.N)
+  if (p.tmw != 4 || p.S != 1 || (p.roles != 2 && p.roles != 3) || !ad.uh || !ad.ul || !ad.ukx || ad.M != p.M ||
+      ad.N != p.N)
     return hipErrorInvalidValue;
-  const unsigned grid = (unsigned)(((p.M + 255) / 256) * ((p.N + 255) / 256));
+  const int tnb = p.roles == 3 ? 2 : 1, tn = kGemmTN * tnb;
+  const unsigned grid = (unsigned)(((p.M + 255) / 256) * ((p.N + tn - 1) / tn));
   if (grid == 0) return hipSuccess;
-  const size_t lds = (size_t)2 * 256 * kGemmTK * 2 + (size_t)2 * 256 * kGemmLdsRow * 2 + (4 * 256 + 4) * 4;
+  const size_t lds = (size_t)2 * 256 * kGemmTK * 2 + (size_t)2 * tn * kGemmLdsRow * 2 + (3 * 256 + tn + 4) * 4;
   const auto go = [&](auto kern) {
     hipError_t err = allow_lds(kern, lds);
     if (err != hipSuccess) return err;
-    hipLaunchKernelGGL(kern, dim3(grid), dim3(768), lds, st, p, ad);
+    hipLaunchKernelGGL(kern, dim3(grid), dim3(256 * (1 + tnb)), lds, st, p, ad);
     return hipGetLastError();
   };
-  return p.res ? go(k_gemm_ws_adapt<DTC, SPEAR_WB, false>) : go(k_gemm_ws_adapt<DTC, SPEAR_WB, true>);
+  if (tnb == 1) return go(k_gemm_ws_adapt<DTC, 1, SPEAR_WB, false>);
+  return p.res ? go(k_gemm_ws_adapt<DTC, 2, SPEAR_WB, false>) : go(k_gemm_ws_adapt<DTC, 2, SPEAR_WB, true>);
 }
 
 hipError_t SPEAR_W(launch_dequant)(const uint32_t* qw, const uint16_t* sc, const uint8_t* zr,

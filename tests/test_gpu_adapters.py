@@ -157,13 +157,13 @@ def test_term_alone(M, N, K, L, R, opt, dt):
 
 
 @contextlib.contextmanager
-def in_the_gemm():
-    """Every call above 64 tokens without an EC on the 256 x 256 tiles, whose GEMM
-    forms the term itself (above 128 tokens)."""
+def in_the_gemm(roles=3):
+    """Every call above 64 tokens without an EC on tiles of 256 tokens (by 128 rows:
+    roles 2, by 256: roles 3), whose GEMM forms the term itself above 128 tokens."""
     from paper_2606_11244_amd import spear as sp
     sp.set_gemm_tile(256)
     sp.set_gemm_slices(1)
-    sp.set_gemm_roles(3)
+    sp.set_gemm_roles(roles)
     try:
         yield
     finally:
@@ -180,14 +180,15 @@ TILED = [s for s in SHAPES if s[0] > 64] + [(135, 264, 384, 5, 20, dict(ids="tur
 
 @pytest.mark.parametrize("M,N,K,L,R,opt", TILED)
 @pytest.mark.parametrize("dt", [S.F16, S.BF16])
-def test_term_in_the_gemm(M, N, K, L, R, opt, dt):
-    log(f"adapters in the GEMM M={M} N={N} K={K} L={L} R={R} {opt} dt={dt}")
+@pytest.mark.parametrize("roles", [2, 3])
+def test_term_in_the_gemm(M, N, K, L, R, opt, dt, roles):
+    log(f"adapters in the GEMM roles={roles} M={M} N={N} K={K} L={L} R={R} {opt} dt={dt}")
     _, dl = _layer(M, N, K, dt, seed=M + N)
     dl.scales.zero_()
     s = Slots(M, N, K, L, R, dt, seed=R, **opt)
     buf = torch.full((M + 2, N), 7.0, dtype=DT[dt], device="cuda")
     res = torch.randn(M, N, generator=torch.Generator().manual_seed(3)).to(DT[dt])
-    with in_the_gemm():
+    with in_the_gemm(roles):
         ad = s.device()
         y = _call(dl, ad, y=buf[:M])
         assert torch.all(buf[M:] == 7.0)
@@ -202,7 +203,7 @@ def test_term_in_the_gemm(M, N, K, L, R, opt, dt):
     assert np.all(np.abs(yr - ref) <= s.bound(x, ref, ref))
 
 
-@pytest.mark.parametrize("M,N,K", [(2049, 8200, 256), (4100, 4104, 128)])
+@pytest.mark.parametrize("M,N,K", [(2049, 8200, 256), (4100, 4104, 128), (1025, 8200, 256)])
 def test_large_tiles_by_themselves(M, N, K):
     """The GEMM that AUTO takes there, on sampled tokens."""
     L, R, dt = 5, 24, S.F16
@@ -267,24 +268,25 @@ def test_beside_the_layer(M, N, K, rank, dt):
     assert np.array_equal(_call(dl, zero.device(), ec=rank > 0), plain.double().cpu().numpy())
 
 
-@pytest.mark.parametrize("M,gemm", [(5, False), (20, False), (70, False), (200, False), (70, True), (150, True), (300, True)])
+@pytest.mark.parametrize("M,gemm", [(5, 0), (20, 0), (70, 0), (200, 0), (70, 3), (150, 3), (300, 3), (150, 2), (300, 2)])
 @pytest.mark.parametrize("dt", [S.F16, S.BF16])
 def test_bad_values_stay_with_their_request(M, gemm, dt):
     """Infinities and NaN of one adapter, and of one token, reach no other
     token, and reach their own."""
-    with in_the_gemm() if gemm else contextlib.nullcontext():
+    with in_the_gemm(gemm) if gemm else contextlib.nullcontext():
         _bad_values(M, dt)
 
 
 @pytest.mark.parametrize("M,N,K", [(70, 264, 512), (140, 264, 512), (300, 513, 384), (600, 4096, 256)])
 @pytest.mark.parametrize("dt", [S.F16, S.BF16])
-def test_tokens_without_an_adapter_in_the_gemm(M, N, K, dt):
+@pytest.mark.parametrize("roles", [2, 3])
+def test_tokens_without_an_adapter_in_the_gemm(M, N, K, dt, roles):
     """They get what the plain call writes there."""
     from paper_2606_11244_amd import spear as sp
     log(f"without an adapter in the GEMM M={M} N={N} K={K} dt={dt}")
     _, dl = _layer(M, N, K, dt, seed=M)
     prob, plain = dl.problem(), torch.empty_like(dl.y)
-    with in_the_gemm():
+    with in_the_gemm(roles):
         dl.run_w4(prob, sp.allocate_workspace(prob, False), y=plain)
         torch.cuda.synchronize()
         plain = plain.double().cpu().numpy()
@@ -318,11 +320,11 @@ def _bad_values(M, dt):
     assert np.array_equal(got[rest], want[rest])
 
 
-@pytest.mark.parametrize("M,gemm", [(3, False), (40, False), (150, False), (150, True)])
+@pytest.mark.parametrize("M,gemm", [(3, 0), (40, 0), (150, 0), (150, 3), (150, 2)])
 def test_large_coordinates_in_fp16(M, gemm):
     """Coordinates past the largest fp16 number, and far below the smallest,
     with factors that bring the term back into range."""
-    with in_the_gemm() if gemm else contextlib.nullcontext():
+    with in_the_gemm(gemm) if gemm else contextlib.nullcontext():
         _large_coordinates(M, gemm)
 
 
