@@ -21,7 +21,8 @@
 // The coordinates leave as sums over K-slices, which every workgroup of the
 // second step adds up for its own tokens: a few KB from L2 each, in place of a
 // last arriver that sums them alone (8B down, K = 14336, 300 tokens: 32 us for
-// the first step that way, 18 and 3 more in the second this way). One launch
+// the first step that way, 18 and 3 more in the second this way, as both were
+// built then; now 8.3 and 8.1). One launch
 // that forms u anew in each workgroup of the term was slower wherever A is not
 // tiny: a CU draws about 12 bytes a cycle from its L2 (8B gate and up at eight
 // requests 17.8 us against 12.0 for the two, o 14.0 against 10.2; 8B q, k, v at 16

@@ -156,6 +156,18 @@ def test_term_alone(M, N, K, L, R, opt, dt):
     assert not y[out.numpy()].any()
 
 
+@pytest.mark.parametrize("M,N,K,rank", [(4, 512, 1024, 16), (9, 1000, 4096, 48), (48, 520, 1024, 32), (77, 1000, 1408, 24),
+                                        (128, 264, 2048, 32), (200, 520, 1024, 16)])
+@pytest.mark.parametrize("dt", [S.F16, S.BF16])
+@pytest.mark.parametrize("int8,gate", [(True, S.GATE_SIGMOID_LINEAR), (False, S.GATE_TANH_MLP), (True, S.GATE_TANH_MLP)])
+def test_beside_other_compensators(M, N, K, rank, dt, int8, gate):
+    """INT8 factors and the tanh-MLP gate, on decode and prefill paths."""
+    L, dl = _layer(M, N, K, dt, seed=M, rank=rank, ab_int8=int8, gate_kind=gate)
+    s = Slots(M, N, K, 7, 16, dt, seed=9, mixed=True)
+    log(f"adapters beside M={M} N={N} K={K} rank={rank} dt={dt} int8={int8} gate={gate}")
+    assert_parity(_call(dl, s.device(), ec=True), O.w4ec_linear(L) + s.term(_x(dl)), "with adapters")
+
+
 @contextlib.contextmanager
 def in_the_gemm(roles=3):
     """Every call above 64 tokens without an EC on tiles of 256 tokens (by 128 rows:
@@ -493,6 +505,8 @@ MIXED = [
      (8, 512, 1024, 0, 4, False, S.F16, (8, 24)), (40, 512, 1024, 0, 3, False, S.BF16, (8, 16))],
     [(1, 4096, 1024, 0, 4, False, S.F16, (2, 8)), (30, 128, 1024, 0, 4, False, S.F16, (30, 8)),
      (64, 128, 1024, 32, 4, False, S.F16, (5, 8)), (65, 128, 1024, 0, 4, False, S.F16, (5, 8))],
+    [(48, 520, 1024, 32, 4, True, S.F16, (6, 16)), (100, 264, 1024, 32, 4, True, S.F16, (100, 8)),
+     (128, 264, 1024, 32, 3, False, S.F16, (3, 40)), (129, 264, 1024, 32, 4, False, S.BF16, (3, 40))],
 ]
 
 
