@@ -66,10 +66,12 @@ __device__ __forceinline__ TokenGroup token_group(const AdapterParams& p, int m,
 // whole, one load each, and through the wave's own part of the LDS, xs
 // [4][kXRow].
 //
-// The wave's iterations lie NW apart, from one that differs between the leaders:
+// The wave's iterations lie NW apart, from one that differs between the slots:
 // the slot's rows are a multiple of 4 KB apart on the usual layers, so that a
 // load's 16 rows lie in one L2 channel, and waves that walked K in step would
-// queue at a few channels at a time.
+// queue at a few channels at a time. (Between the slots, not the leaders: a
+// token's sums are in the order that its own slot gives, whichever tokens share
+// the slot and whichever row is the first of them.)
 //
 // At these sizes a workgroup's time is its instructions as much as its loads (a
 // SIMD issues one every four cycles): every load takes its place in K from a
@@ -182,7 +184,7 @@ __device__ __forceinline__ void shrink_slot(const AdapterParams& p, int b, char*
   const rsrc_t ra = make_rsrc(p.A + (size_t)g.a * p.a_stride, (uint32_t)p.R * p.K * 2);
   f32x4 acc[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
   const int it0 = ks * p.ips, nit = min(p.K / kIterK - it0, p.ips);
-  project<DT>(rx, g, stok, xs + wave * 4 * kXRow, ra, p.K, 32 * rg, g.r, it0, nit, m % nit, wave, NW, acc);
+  project<DT>(rx, g, stok, xs + wave * 4 * kXRow, ra, p.K, 32 * rg, g.r, it0, nit, g.a % nit, wave, NW, acc);
 #pragma unroll
   for (int t = 0; t < 2; ++t) *(f32x4*)(red + (2 * wave + t) * 256 + 4 * lane) = acc[t];
   __syncthreads();
