@@ -395,16 +395,20 @@ spear_status_t spear_adapters_workspace(int32_t n, const spear_layer_call_t* cal
 
 /* spear_w4ec_linear (ec NULL: spear_w4_linear) with adapters, followed by the
  * post-EC tail if tail is not NULL. Y = the layer + the adapters' term + the
- * tail's residual, each summed in fp32. Where the layer is one decode GEMV
- * launch, or runs on tiles of 256 tokens and has at least 32 tokens a slot,
- * nothing is rounded before Y itself; elsewhere the term plus the residual is, once, to the act dtype. A token
+ * tail's residual, each summed in fp32. Where the layer's product is a decode
+ * GEMV (AUTO: up to 16 tokens, and from 17 to 32 where it is not a GEMM), or
+ * runs on tiles of 256 tokens, without an EC, and has at least 32 tokens a slot,
+ * nothing is rounded before Y itself; elsewhere (a GEMM otherwise, a GEMV forced
+ * above 32 tokens or with spear_set_gemv_stages(4), the naive chain, the
+ * overlapped pair) the term plus the residual is, once, to the act dtype, whose
+ * range it has to keep: past 65504 in fp16 Y is infinite. A token
  * without an adapter gets what the call without adapters writes. In fp16 a
  * coordinate s_a A_a x may pass 65504; on those tiles Y[n] is then infinite
  * where an entry of B_a's row n times (the token's largest coordinate / 2^14)
  * passes it too, and coordinates are held to 2^-25 there. No
- * token's result depends on another token's adapter or values. The workspace
- * follows the rules of the other calls and may be shared with them in stream
- * order. Errors as for spear_w4ec_linear_tail and spear_adapters_workspace,
+ * token's result depends on another token's adapter or values. The
+ * workspace follows the rules of the other calls and may be shared with them in
+ * stream order. Errors as for spear_w4ec_linear_tail and spear_adapters_workspace,
  * plus SPEAR_E_NULL for missing adapters, A, B or ids, SPEAR_E_ALIGN for a
  * misaligned pointer or a_stride, SPEAR_E_SHAPE for a stride smaller than its
  * slot or of 2^31 or more, SPEAR_E_ALIAS for an output overlapping an adapter buffer. */

@@ -962,6 +962,15 @@ hipError_t launch_gemv_wb(const Resolved& z, int epi, const GemvParams& p, int g
   const int nst = epi == EPI_NONE || epi == EPI_READY || epi == EPI_FUSED ? z.nst : 2;
   return SPEAR_BY_WB(launch_gemv, z.wb, z.dt)(z.MT, z.RT, epi, nst, p, grid, block, lds, st);
 }
+// The GEMV with an EC wave, one layer's, its sums to yf in fp32 in place of y.
+hipError_t launch_gemv_sums_wb(const Resolved& z, int epi, const GemvParams& p, float* yf, size_t lds, hipStream_t st) {
+  GemvGroup g;
+  std::memset(&g, 0, sizeof(g));
+  g.p[0] = p;
+  g.start[1] = z.nrg * z.S;
+  g.n = 1;
+  return SPEAR_BY_WB(launch_gemv_sums, z.wb, z.dt)(z.MT, z.RT, epi, g, GemvSums{{yf}}, 64 * (z.NW + 1), lds, st);
+}
 hipError_t launch_gemm_wb(const Resolved& z, int epi, const GemmParams& p, hipStream_t st) {
   if (z.groles == 4) {
     GemmGroup g;
@@ -1006,7 +1015,8 @@ spear_status_t run_w4(const spear_problem_t* p, const Resolved& z, const void* x
 
 // The semi-fused path: the EC pre-kernel's parameters, and the 4-bit product
 // with the epilogue that adds its result (its counters lie at `base`, the
-// workspace itself where `ws` is a member's part of a group's).
+// workspace itself where `ws` is a member's part of a group's). yf: a decode
+// GEMV's sums go there in fp32, in place of y.
 EcParams ec_for_2k(const spear_problem_t* prob, const Resolved& z, const void* x, const spear_ec_t* ec,
                    char* ws) {
   EcParams e = make_ec(prob, z, x, ec, ws);
@@ -1019,13 +1029,14 @@ EcParams ec_for_2k(const spear_problem_t* prob, const Resolved& z, const void* x
 }
 spear_status_t run_2k_main(const spear_problem_t* prob, const Resolved& z, const void* x,
                            const spear_w4_t* w, const spear_ec_t* ec, const EcParams& e, void* y,
-                           const uint16_t* res, char* ws, hipStream_t s, char* base = nullptr) {
+                           const uint16_t* res, char* ws, hipStream_t s, char* base = nullptr, float* yf = nullptr) {
   if (!base) base = ws;
   if (z.gemv) {
     GemvParams g = make_gemv(prob, z, x, w, y, ec, ws);
     if (z.S > 1) g.rb_ctr = (uint32_t*)(base + kCtrRows);
     g.res = res;
     g.ec = e;
+    if (yf) return hip_status(launch_gemv_sums_wb(z, EPI_READY, g, yf, z.lds_gemv, s));
     return hip_status(launch_gemv_wb(z, EPI_READY, g, z.nrg * z.S, 64 * (z.NW + 1), z.lds_gemv, s));
   }
   GemmParams g = make_gemm(prob, z, x, w, y, ec, ws);
@@ -1035,10 +1046,11 @@ spear_status_t run_2k_main(const spear_problem_t* prob, const Resolved& z, const
 }
 
 // The layer on its planned path, after validation; res as in run_w4 (the
-// chain adds it in its 4-bit kernel, every other path in its final store).
+// chain adds it in its 4-bit kernel, every other path in its final store); yf
+// as in run_2k_main, on the producer-fused and the semi-fused path.
 spear_status_t run_layer(const spear_problem_t* prob, const Resolved& z, const void* x,
                          const spear_w4_t* w, const spear_ec_t* ec, void* y, const uint16_t* res,
-                         char* ws, hipStream_t s) {
+                         char* ws, hipStream_t s, float* yf = nullptr) {
   spear_status_t st = SPEAR_OK;
   if (!z.ec) return run_w4(prob, z, x, w, y, ws, s, res);
 
@@ -1070,12 +1082,13 @@ spear_status_t run_layer(const spear_problem_t* prob, const Resolved& z, const v
     g.n_prod = z.n_prod;
     g.grid_total = z.n_prod + z.nrg * z.S;
     const size_t lds = std::max(z.lds_gemv, z.lds_prod);
+    if (yf) return hip_status(launch_gemv_sums_wb(z, EPI_FUSED, g, yf, lds, s));
     return hip_status(launch_gemv_wb(z, EPI_FUSED, g, g.grid_total, 64 * (z.NW + 1), lds, s));
   }
   if (path == SPEAR_PATH_UNFUSED_2K) {
     e = ec_for_2k(prob, z, x, ec, ws);
     st = run_ec(z, e, s);
-    return st != SPEAR_OK ? st : run_2k_main(prob, z, x, w, ec, e, y, res, ws, s);
+    return st != SPEAR_OK ? st : run_2k_main(prob, z, x, w, ec, e, y, res, ws, s, nullptr, yf);
   }
   if (path == SPEAR_PATH_OVERLAP_2K) {
     // fork: the EC pre-kernel (A x, gate, v in fp32) on the side stream,
@@ -1240,18 +1253,21 @@ spear_status_t check_tail(const spear_problem_t* prob, const void* x, const spea
 //   decode calls are latency, and this takes the first of the adapters' two
 //   launches off their path (8B q, k, v at 16 requests: 13.3 us for the launch, 12.9
 //   without adapters, 4.8 for the coordinates alone);
+// - ADAPT_AFTER: the layer is a GEMV with an EC wave (producer-fused, or behind its
+//   pre-kernel); its sums stay in fp32 as above, so that y is rounded once;
 // - ADAPT_EPILOGUE: k_gemm_ws (tiles of 256 tokens) forms it, as further steps of
 //   its loop. Its epilogue with a residual costs as much as another pass over the
 //   output (8B gate and up, 14336 x 4096 at 2048 tokens, fp16: 617 us with the term
 //   first, 574 with a pass after it that also rounds y once more, 482 this way,
 //   449 without adapters).
-enum { ADAPT_BEFORE = 0, ADAPT_RIDES = 1, ADAPT_EPILOGUE = 2 };
+enum { ADAPT_BEFORE = 0, ADAPT_RIDES = 1, ADAPT_EPILOGUE = 2, ADAPT_AFTER = 3 };
 // The adapter data of one member in the workspace: the K-slices of its
 // coordinates, their parts (ADAPT_EPILOGUE), its term d (ADAPT_BEFORE), the
-// layer's sums yf (ADAPT_RIDES).
+// layer's sums yf (ADAPT_RIDES, ADAPT_AFTER).
 struct AdapterLayout {
   bool on = false;  // the member has tokens, rows and adapters
   int join = ADAPT_BEFORE;
+  bool sums() const { return on && (join == ADAPT_RIDES || join == ADAPT_AFTER); }
   size_t upart = 0, uh = 0, ul = 0, ukx = 0, d = 0, yf = 0;
   AdapterParams p;  // the launch shape
 };
@@ -1340,9 +1356,14 @@ spear_status_t adapters_layout(int32_t n, const spear_layer_call_t* calls, const
     // of 64 107 and 121). The hook that asks for these tiles asks for this too.
     const bool ws = !z[i].gemv && !z[i].ec && (z[i].groles == 2 || z[i].groles == 3);
     const bool few_slots = (int64_t)a->n_adapters * 32 <= p->M || g_ov_gr.load() >= 2;
-    al[i].join = q.kind == ADAPT_SLOTS && group_epi(z[i], calls[i].ec) >= 0 && z[i].MT <= 2 && z[i].nst == 2 ? ADAPT_RIDES
-                 : q.kind == ADAPT_TILES && ws && few_slots                                                 ? ADAPT_EPILOGUE
-                                                                                                            : ADAPT_BEFORE;
+    // (the GEMV variants compiled with fp32 sums; others only a forced path above 32
+    // tokens and the pipeline's hook reach)
+    const bool gemv = q.kind == ADAPT_SLOTS && z[i].gemv && z[i].MT <= 2 && z[i].nst == 2;
+    const bool ec_wave = z[i].ec && (z[i].plan.path == SPEAR_PATH_FUSED_GEMV || z[i].plan.path == SPEAR_PATH_UNFUSED_2K);
+    al[i].join = gemv && group_epi(z[i], calls[i].ec) >= 0        ? ADAPT_RIDES
+                 : gemv && ec_wave                                ? ADAPT_AFTER
+                 : q.kind == ADAPT_TILES && ws && few_slots       ? ADAPT_EPILOGUE
+                                                                  : ADAPT_BEFORE;
     const size_t uw = (size_t)p->M * 32 * q.RG;
     al[i].upart = take(q.P * uw * 4);
     if (al[i].join == ADAPT_EPILOGUE) {
@@ -1351,7 +1372,7 @@ spear_status_t adapters_layout(int32_t n, const spear_layer_call_t* calls, const
       al[i].ukx = take((size_t)p->M * 4);
     }
     if (al[i].join == ADAPT_BEFORE) al[i].d = take((size_t)p->M * p->N * 2);
-    if (al[i].join == ADAPT_RIDES) al[i].yf = take((size_t)p->M * p->N * 4);
+    if (al[i].sums()) al[i].yf = take((size_t)p->M * p->N * 4);
   }
   if (any) *total = off;
   return SPEAR_OK;
@@ -1398,7 +1419,7 @@ AdapterParams make_adapters(const spear_layer_call_t& c, const spear_adapters_t*
   q.scale = a->scale;
   q.res = res;
   q.upart = (float*)(ws + al.upart);
-  if (al.join == ADAPT_RIDES) q.yf = (const float*)(ws + al.yf);
+  if (al.sums()) q.yf = (const float*)(ws + al.yf);
   q.d = q.yf ? (uint16_t*)c.y : (uint16_t*)(ws + al.d);
   if (al.join == ADAPT_EPILOGUE) {
     q.uh = (uint16_t*)(ws + al.uh);
@@ -1441,8 +1462,8 @@ struct AdapterCall {
   }
   // member i's coordinates go with its layer's EC pre-kernel
   bool ec_takes(int i, const Resolved& z) const {
-    return al[i].on && al[i].join == ADAPT_BEFORE && al[i].p.kind == ADAPT_SLOTS && z.ec &&
-           z.plan.path == SPEAR_PATH_UNFUSED_2K;
+    return al[i].on && (al[i].join == ADAPT_BEFORE || al[i].join == ADAPT_AFTER) && al[i].p.kind == ADAPT_SLOTS &&
+           z.ec && z.plan.path == SPEAR_PATH_UNFUSED_2K;
   }
   // before the layers: the coordinates of all members but those that go with
   // another launch, and the terms that enter the layers as residuals, res[i]
@@ -1460,18 +1481,21 @@ struct AdapterCall {
     return expand([&](int i) { return al[i].join == ADAPT_BEFORE && !with_ec[i]; }, s);
   }
   spear_status_t after(hipStream_t s) const {
-    return expand([&](int i) { return al[i].join == ADAPT_RIDES; }, s);
+    return expand([&](int i) { return al[i].sums(); }, s);
   }
+  // where member i's layer leaves its sums, or null
+  float* sums(int i) const { return i < n && al[i].sums() ? const_cast<float*>(p[i].yf) : nullptr; }
   // the layer of a member that shares no launch
   spear_status_t layer(int i, const Resolved& z, const uint16_t* res, char* ws, hipStream_t s) const {
     const spear_layer_call_t& c = calls[i];
     if (with_ec[i]) {
       const EcParams e = ec_for_2k(c.prob, z, c.x, c.ec, ws);
       spear_status_t st = run_ec(z, e, s, &p[i]);
-      if (st == SPEAR_OK) st = expand([&](int j) { return j == i; }, s);
-      return st != SPEAR_OK ? st : run_2k_main(c.prob, z, c.x, c.w, c.ec, e, c.y, res, ws, s);
+      if (st == SPEAR_OK) st = expand([&](int j) { return j == i && al[j].join == ADAPT_BEFORE; }, s);
+      return st != SPEAR_OK ? st : run_2k_main(c.prob, z, c.x, c.w, c.ec, e, c.y, res, ws, s, nullptr, sums(i));
     }
-    if (!al[i].on || al[i].join == ADAPT_BEFORE) return run_layer(c.prob, z, c.x, c.w, c.ec, c.y, res, ws, s);
+    if (!al[i].on || al[i].join == ADAPT_BEFORE || al[i].join == ADAPT_AFTER)
+      return run_layer(c.prob, z, c.x, c.w, c.ec, c.y, res, ws, s, sums(i));
     if (al[i].join == ADAPT_RIDES) {
       const bool ec = z.ec;
       GemvGroup g;
@@ -1487,7 +1511,7 @@ struct AdapterCall {
       AdapterGroup a;
       std::memset(&a, 0, sizeof(a));
       a.p[0] = p[i];
-      a.yf[0] = const_cast<float*>(p[i].yf);
+      a.yf[0] = sums(i);
       a.n = 1;
       return hip_status(SPEAR_BY_WB(launch_gemv_adapt, z.wb, z.dt)(z.MT, z.RT, group_epi(z, c.ec), g, a, 64 * z.NW,
                                                                    z.lds_gemv, s));
@@ -1804,7 +1828,8 @@ static spear_status_t run_group(int32_t n, const spear_layer_call_t* calls, Reso
     }
     if (a.n > 0) {
       st = hip_status(SPEAR_BY_DT(launch_ec_adapt, z[k].dt)(g, a, z[k].ec_block, z[k].ec_ipp, lds, s));
-      if (st == SPEAR_OK) st = ad.expand([&](int i) { return ad.with_ec[i] && ec_set[i] == k; }, s);
+      if (st == SPEAR_OK)
+        st = ad.expand([&](int i) { return ad.with_ec[i] && ec_set[i] == k && ad.al[i].join == ADAPT_BEFORE; }, s);
     } else {
       st = hip_status(SPEAR_BY_DT(launch_ec, z[k].dt)(g, z[k].ec_block, z[k].ec_ipp, lds, s));
     }
@@ -1815,6 +1840,8 @@ static spear_status_t run_group(int32_t n, const spear_layer_call_t* calls, Reso
     if (gv_set[k] == k) {
       GemvGroup g;
       std::memset(&g, 0, sizeof(g));
+      GemvSums sums = {};
+      bool any_sums = false;
       size_t lds = 0;
       int ctr = 0;
       for (int i = k; i < n; ++i) {
@@ -1830,14 +1857,17 @@ static spear_status_t run_group(int32_t n, const spear_layer_call_t* calls, Reso
         }
         g.start[g.n + 1] = g.start[g.n] + z[i].nrg * z[i].S;
         lds = std::max(lds, z[i].lds_gemv);
+        sums.yf[g.n] = ad.sums(i);
+        any_sums = any_sums || sums.yf[g.n];
         ++g.n;
       }
-      st = hip_status(SPEAR_BY_WB(launch_gemv_group, z[k].wb, z[k].dt)(z[k].MT, z[k].RT, EPI_READY, g,
-                                                                       64 * (z[k].NW + 1), lds, s));
+      const int block = 64 * (z[k].NW + 1);
+      st = hip_status(any_sums ? SPEAR_BY_WB(launch_gemv_sums, z[k].wb, z[k].dt)(z[k].MT, z[k].RT, EPI_READY, g, sums, block, lds, s)
+                               : SPEAR_BY_WB(launch_gemv_group, z[k].wb, z[k].dt)(z[k].MT, z[k].RT, EPI_READY, g, block, lds, s));
       if (st != SPEAR_OK) return st;
     }
     if (set[k] < 0 && gv_set[k] < 0 && ec_set[k] >= 0) {
-      st = run_2k_main(c.prob, z[k], c.x, c.w, c.ec, ecp[k], c.y, res[k], ws + off[k], s, ws);
+      st = run_2k_main(c.prob, z[k], c.x, c.w, c.ec, ecp[k], c.y, res[k], ws + off[k], s, ws, ad.sums(k));
       if (st != SPEAR_OK) return st;
     }
     if (set[k] != k) continue;
@@ -1920,7 +1950,7 @@ static spear_status_t run_group(int32_t n, const spear_layer_call_t* calls, Reso
   for (int i = 0, m = 0; i < ad.n; ++i) {
     if (!in[i]) continue;
     if (ad.al[i].on && ad.al[i].join == ADAPT_RIDES) {
-      a.yf[m] = const_cast<float*>(ad.p[i].yf);
+      a.yf[m] = ad.sums(i);
       a.p[a.n++] = ad.p[i];
     }
     ++m;

@@ -250,6 +250,11 @@ struct AdapterGroup {
   int n;
 };
 
+// [M][N] where a GEMV member's sums go in fp32, in place of y (or null).
+struct GemvSums {
+  float* yf[kGroupMax];
+};
+
 // The norms around a block.
 enum { BGATE_MUL = 0, BGATE_TANH = 1, BGATE_SIGMOID = 2 };
 struct BlockNormParams {
@@ -315,6 +320,8 @@ __host__ __device__ inline size_t ec_block_lds(int NW, int R1p, int h, int r) {
                                    size_t lds, hipStream_t st);                                 \
   hipError_t launch_gemv_adapt_##W(int MT, int RT, int epi, const GemvGroup& g,                 \
                                    const AdapterGroup& a, int block, size_t lds, hipStream_t st); \
+  hipError_t launch_gemv_sums_##W(int MT, int RT, int epi, const GemvGroup& g, const GemvSums& s, \
+                                  int block, size_t lds, hipStream_t st);                       \
   hipError_t launch_gemm_##W(int epi, const GemmParams& p, hipStream_t st);                      \
   hipError_t launch_gemm_adapt_##W(const GemmParams& p, const AdapterParams& ad, hipStream_t st); \
   hipError_t launch_mid_##W(int MT, const GemmGroup& g, hipStream_t st);

@@ -1459,8 +1459,39 @@ __global__ __launch_bounds__(kGemvMaxThreads, gemv_min_waves(MT, RT, EPI)) void 
   gemv_body<DT, MT, RT, EPI, WB, 2, SPLIT, true>(g.p[i], b - g.start[i], 0u, smem, a.yf[i]);
 }
 
+// The variants with an EC wave with their sums in fp32, for the same reason; they
+// carry no coordinates. A grouped call runs producer-fused members as semi-fused
+// ones, and its results are those of the members' own calls, so that both have it.
+template <int DT, int MT, int RT, int EPI, int WB, bool SPLIT>
+__global__ __launch_bounds__(kGemvMaxThreads, gemv_min_waves(MT, RT, EPI)) void k_gemv_sums(GemvParams a, float* yf) {
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  int bid = blockIdx.x;
+  uint32_t gen = 0;
+  if constexpr (EPI == EPI_FUSED) {
+    gen = (uint32_t)(__hip_atomic_load(gen_counter(a, bid), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) >> 32);
+    if (bid < a.n_prod) {
+      ec_producer<DT, 1, false>(a.ec, bid, gen, smem);
+      fused_exit(a);
+      return;
+    }
+    bid -= a.n_prod;
+  }
+  gemv_body<DT, MT, RT, EPI, WB, 2, SPLIT, true>(a, bid, gen, smem, yf);
+}
+template <int DT, int MT, int RT, int WB, bool SPLIT>
+__global__ __launch_bounds__(kGemvMaxThreads, gemv_min_waves(MT, RT, EPI_READY)) void k_gemv_group_sums(GemvGroup g,
+                                                                                                       GemvSums s) {
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  const int b = blockIdx.x;
+  int i = 0;
+#pragma unroll
+  for (int j = 1; j < kGroupMax; ++j)
+    if (j < g.n && b >= g.start[j]) i = j;
+  gemv_body<DT, MT, RT, EPI_READY, WB, 2, SPLIT, true>(g.p[i], b - g.start[i], 0u, smem, s.yf[i]);
+}
+
 // The EC pre-kernel with the coordinates, in the same way: the term is formed
-// between it and the product, whose residual it is.
+// after it, before a GEMM whose residual it is, or after a GEMV's sums.
 template <int DT, int IPP>
 __global__ __launch_bounds__(512) void k_ec_adapt(EcGroup g, AdapterGroup a) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -1662,8 +1693,8 @@ hipError_t SPEAR_W(launch_gemv_group)(int MT, int RT, int epi, const GemvGroup& 
 
 #else  // SPEAR_ADAPT_UNIT
 
-// The GEMV with adapters' coordinates: up to two token tiles, the product alone
-// and the local EC variants.
+// The GEMV of calls with adapters: up to two token tiles; with their coordinates
+// the product alone and the local EC variants, without them the others.
 template <int DT, int MT, int RT>
 static hipError_t gemv_adapt_launch(int epi, const GemvGroup& g, const AdapterGroup& a, int block, size_t lds,
                                     hipStream_t st) {
@@ -1728,6 +1759,47 @@ hipError_t SPEAR_W(launch_gemv_adapt)(int MT, int RT, int epi, const GemvGroup& 
   SPEAR_GEMV_ADAPT_CASE(2, 2)
   SPEAR_GEMV_ADAPT_CASE(2, 4)
 #undef SPEAR_GEMV_ADAPT_CASE
+  return hipErrorInvalidValue;
+}
+
+template <int DT, int MT, int RT>
+static hipError_t gemv_sums_launch(int epi, const GemvGroup& g, const GemvSums& s, int block, size_t lds,
+                                   hipStream_t st) {
+  constexpr int WB = SPEAR_WB;
+  bool split = MT > 1;
+  for (int i = 0; i < g.n; ++i) split |= g.p[i].S > 1;
+  const auto go = [&](auto kern, int grid, const auto& p, const auto& yf) {
+    hipError_t err = allow_lds(kern, lds);
+    if (err != hipSuccess) return err;
+    hipLaunchKernelGGL(kern, dim3(grid), dim3(block), lds, st, p, yf);
+    return hipGetLastError();
+  };
+  // (one member: its parameters alone, as in a call without adapters; in a group's
+  // table 8192 x 28672, rank 64, at one token took 42.3 us, this way 40.9)
+  const GemvParams& p = g.p[0];
+  if (epi == EPI_FUSED && g.n == 1)
+    return split ? go(k_gemv_sums<DT, MT, RT, EPI_FUSED, WB, true>, p.grid_total, p, s.yf[0])
+                 : go(k_gemv_sums<DT, MT, RT, EPI_FUSED, WB, MT != 1>, p.grid_total, p, s.yf[0]);
+  if (epi != EPI_READY) return hipErrorInvalidValue;
+  if (g.n == 1)
+    return split ? go(k_gemv_sums<DT, MT, RT, EPI_READY, WB, true>, g.start[1], p, s.yf[0])
+                 : go(k_gemv_sums<DT, MT, RT, EPI_READY, WB, MT != 1>, g.start[1], p, s.yf[0]);
+  return split ? go(k_gemv_group_sums<DT, MT, RT, WB, true>, g.start[g.n], g, s)
+               : go(k_gemv_group_sums<DT, MT, RT, WB, MT != 1>, g.start[g.n], g, s);
+}
+
+hipError_t SPEAR_W(launch_gemv_sums)(int MT, int RT, int epi, const GemvGroup& g, const GemvSums& s, int block,
+                                     size_t lds, hipStream_t st) {
+  if (!gemv_group_ok(epi, g)) return hipErrorInvalidValue;
+#define SPEAR_GEMV_SUMS_CASE(mt, rt) \
+  if (MT == mt && RT == rt) return gemv_sums_launch<DTC, mt, rt>(epi, g, s, block, lds, st);
+  SPEAR_GEMV_SUMS_CASE(1, 1)
+  SPEAR_GEMV_SUMS_CASE(1, 2)
+  SPEAR_GEMV_SUMS_CASE(1, 4)
+  SPEAR_GEMV_SUMS_CASE(2, 1)
+  SPEAR_GEMV_SUMS_CASE(2, 2)
+  SPEAR_GEMV_SUMS_CASE(2, 4)
+#undef SPEAR_GEMV_SUMS_CASE
   return hipErrorInvalidValue;
 }
 
