@@ -403,9 +403,11 @@ spear_status_t spear_adapters_workspace(int32_t n, const spear_layer_call_t* cal
  * overlapped pair) the term plus the residual is, once, to the act dtype, whose
  * range it has to keep: past 65504 in fp16 Y is infinite. A token
  * without an adapter gets what the call without adapters writes. In fp16 a
- * coordinate s_a A_a x may pass 65504; on those tiles Y[n] is then infinite
- * where an entry of B_a's row n times (the token's largest coordinate / 2^14)
- * passes it too, and coordinates are held to 2^-25 there. No
+ * coordinate s_a A_a x may pass 65504; on those tiles Y[n] is then rounded once
+ * more where an entry of B_a's row n times (the token's largest coordinate / 2^14)
+ * passes it too, and coordinates are held to 2^-25 there. Infinities and NaN in A_a
+ * or the scale make the Y of its tokens not finite, in B_a's row n only Y[n] (NaN
+ * may stand where the formula gives an infinity). No
  * token's result depends on another token's adapter or values. The
  * workspace follows the rules of the other calls and may be shared with them in
  * stream order. Errors as for spear_w4ec_linear_tail and spear_adapters_workspace,

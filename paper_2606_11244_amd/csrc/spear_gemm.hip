@@ -523,10 +523,10 @@ __global__ __launch_bounds__(128 * TMW, TMW == 2 ? 2 : 1) void k_gemm(GemmParams
 // tokens name and each 32 of its ranks, the loading waves store the high and the
 // low parts of the tokens' coordinates side by side (zero for the other tokens)
 // as the activation tile, and the slot's rows of B twice as the weight tile,
-// requested a step ahead. What is not finite in B is kept out, since zero times
-// it would reach the other tokens; a further step then has one rank, with the
-// largest finite value as the factor of the slot's tokens and of the rows of B
-// in question: infinite in y.
+// requested a step ahead. What is not finite in B (or, in fp16, would not be once
+// multiplied by what the coordinates were divided by) is kept out, since zero
+// times it would reach the other tokens; where there was such an entry, the loading
+// waves add its products in fp32 to y of its slot's tokens after the final store.
 template <int DT, int EPI, int TNB, int WB, bool PLAIN>
 __device__ __forceinline__ void gemm_ws_body(const GemmParams& a, const AdapterParams& ad) {
   static_assert(EPI == EPI_NONE || EPI == EPI_READY || EPI == EPI_ADAPT, "plain, semi-fused and adapter epilogues");
@@ -613,8 +613,8 @@ __device__ __forceinline__ void gemm_ws_body(const GemmParams& a, const AdapterP
   };
 
   // EPI_ADAPT, after the stages: the tokens' slots (-1: none), their ranks and the
-  // power of two that their coordinates were divided by; the step at which a row
-  // of B was not finite ([TN]: any row's); whether buffer b holds a further step
+  // power of two that their coordinates were divided by; whether an entry of a row
+  // of B was kept out ([TN]: of any row); whether buffer b holds a further step
   int* sid = (int*)(Ws + 2 * TILEW);  // [TM]
   int* srk = sid + TM;                // [TM]
   int* skx = srk + TM;                // [TM]
@@ -672,11 +672,11 @@ __device__ __forceinline__ void gemm_ws_body(const GemmParams& a, const AdapterP
         }
       }
     };
-    // EPI_ADAPT: the walk over slots and ranks, the operands of the next step and
-    // what the last one stored was
+    // EPI_ADAPT: the walk over slots and ranks, and the operands of the next step
+    constexpr uint32_t kExp = DT == DT_F16 ? 0x7C00u : 0x7F80u;  // all ones: not finite
     int id[4], rk[4], kx[4];
     uint64_t left[4] = {0, 0, 0, 0};
-    int slot = -1, k2 = 0, r = 0, kr0 = 0, pslot = -1, pk2 = 0, nstep = 0;
+    int slot = -1, k2 = 0, r = 0, kr0 = 0;
     bool have = false;
     constexpr int WR = TN / 64;  // weight rows of a thread
     u32x4 xv[8], wv[WR];
@@ -686,7 +686,7 @@ __device__ __forceinline__ void gemm_ws_body(const GemmParams& a, const AdapterP
       sid[pt] = n > 0 ? s : -1;
       srk[pt] = n;
       skx[pt] = n > 0 && DT == DT_F16 ? ad.ukx[m] : 0;
-      for (int t = pt; t <= TN; t += 256) sbad[t] = -1;
+      for (int t = pt; t <= TN; t += 256) sbad[t] = 0;
     };
     auto adapt_begin = [&]() {  // (a barrier after the above)
       const int ln = pt & 63;
@@ -747,23 +747,9 @@ __device__ __forceinline__ void gemm_ws_body(const GemmParams& a, const AdapterP
     };
     // stores a further step into buffer buf; false: there is none
     auto adapt_step = [&](int buf) -> bool {
-      constexpr uint32_t kExp = DT == DT_F16 ? 0x7C00u : 0x7F80u, kMax = kExp - 1;  // the largest finite value
+      if (!have) return false;
       uint16_t* xs = Xs + buf * TILEX;
       uint16_t* ws = Ws + buf * TILEW;
-      if (nstep > 0 && sbad[TN] == nstep) {  // (uniform) what the last step kept out
-        for (int c = pt; c < TM * 8; c += 256) {
-          const int t = c >> 3;
-          const bool f = (c & 7) == 0 && sid[t] == pslot && skx[t] == pk2;
-          *(u32x4*)(xs + t * kGemmTK + 8 * ((c & 7) ^ (t & 7))) = u32x4{f ? kMax : 0u, 0u, 0u, 0u};
-        }
-        for (int c = pt; c < TN * 8; c += 256)
-          *(u32x4*)(ws + (c >> 3) * LR + 8 * (c & 7)) =
-              u32x4{(c & 7) == 0 && sbad[c >> 3] == nstep ? kMax : 0u, 0u, 0u, 0u};
-        ++nstep;
-        return true;
-      }
-      if (!have) return false;
-      ++nstep;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const int t = (pt >> 3) + 32 * i;
@@ -783,14 +769,34 @@ __device__ __forceinline__ void gemm_ws_body(const GemmParams& a, const AdapterP
           if ((wv[i][q] & kExp) == kExp) bad = true, wv[i][q] &= 0xFFFF0000u;
           if ((wv[i][q] >> 16 & kExp) == kExp) bad = true, wv[i][q] &= 0xFFFFu;
         }
-        if (bad) sbad[row] = sbad[TN] = nstep;
+        if (bad) sbad[row] = sbad[TN] = 1;
         *(u32x4*)(ws + row * LR + 8 * (pt & 3)) = wv[i];
         *(u32x4*)(ws + row * LR + 8 * (pt & 3) + 32) = wv[i];
       }
-      pslot = slot;
-      pk2 = k2;
       adapt_load();
       return true;
+    };
+    // the products that the steps kept out, into the stored y: a token a thread
+    auto adapt_kept_out = [&]() {
+      const int s = sid[pt], rank = srk[pt];
+      if (s < 0) return;
+      const float f = exp2i(skx[pt]);
+      const size_t m = m0 + pt;
+      const uint16_t *uh = ad.uh + m * 32 * ad.RG, *ul = ad.ul + m * 32 * ad.RG;
+      for (int row = 0; row < TN; ++row) {
+        if (!sbad[row]) continue;
+        const uint16_t* br = ad.B + (size_t)s * ad.b_stride + (size_t)(n0 + row) * ad.R;
+        bool any = false;
+        float add = 0.f;
+        for (int j = 0; j < rank; ++j) {
+          const float v = act2f<DT>(br[j]);
+          if ((f2act<DT>(f * v) & kExp) != kExp) continue;
+          add += f * (act2f<DT>(uh[j]) + act2f<DT>(ul[j])) * v;
+          any = true;
+        }
+        uint16_t* y = a.y + m * N + n0 + row;
+        if (any) *y = f2act<DT>(act2f<DT>(*y) + add);
+      }
     };
     // step kt stores step kt + 1 (loaded two steps earlier) and then loads
     // step kt + 3 into the same registers; loads past the end re-read the
@@ -829,6 +835,10 @@ __device__ __forceinline__ void gemm_ws_body(const GemmParams& a, const AdapterP
         if (pt == 0) smore[b] = more;
         __syncthreads();
         if (!more) break;
+      }
+      if (sbad[TN]) {     // (as the multiplying waves read it)
+        __syncthreads();  // y is stored
+        adapt_kept_out();
       }
     }
     if constexpr (EPI == EPI_READY) {
@@ -968,6 +978,8 @@ __device__ __forceinline__ void gemm_ws_body(const GemmParams& a, const AdapterP
             },
             [&](int e) { return acc[i][j][e]; });
   }
+  if constexpr (EPI == EPI_ADAPT)
+    if (sbad[TN]) __syncthreads();
 }
 
 template <int DT, int EPI, int TNB, int WB, bool PLAIN>

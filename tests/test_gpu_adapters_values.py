@@ -13,7 +13,7 @@ from oracle import spear_oracle as O
 from paper_2606_11244_amd import synth as S
 
 from gpu_util import log
-from test_gpu_adapters import DT, Slots, _call, _gpu, _layer, in_the_gemm  # noqa: F401 (a fixture)
+from test_gpu_adapters import DT, HALF, Slots, _call, _gpu, _layer, _x, in_the_gemm  # noqa: F401 (a fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -132,3 +132,65 @@ def test_decode_sums_pass_the_range_of_fp16(M, N, K, rank, path):
     want = 80000.0 - 8.0 * K * step.item()
     # half a step of fp16 there, and a rounding of 2^-24 a step of the sums over K
     assert np.all(np.abs(y - want) <= 16.0 + K * 2.0 ** -24 * 110000.0)
+
+
+def _kind(v):
+    return np.where(np.isnan(v), 2.0, np.where(np.isinf(v), np.sign(v), 0.0))
+
+
+@pytest.mark.parametrize("M,N,roles", [(150, 144, 2), (150, 144, 3), (300, 520, 2), (300, 520, 3)])
+@pytest.mark.parametrize("dt", [S.F16, S.BF16])
+@pytest.mark.parametrize("residual", [False, True])
+def test_what_is_not_finite_in_b_keeps_its_kind_in_the_gemm(M, N, roles, dt, residual):
+    """NaN, infinities of both signs and of both on one row, where the GEMM forms the
+    term: as the formula gives them, on their own rows and tokens only."""
+    K, L, R = 256, 4, 40
+    _, dl = _layer(M, N, K, dt, seed=1)
+    dl.scales.zero_()
+    s = Slots(M, N, K, L, R, dt, ids="turn", seed=6)
+    res = torch.randn(M, N, generator=torch.Generator().manual_seed(3)).to(DT[dt]) if residual else None
+    kw = dict(residual=res.cuda()) if residual else {}
+    with in_the_gemm(roles):
+        want = _call(dl, s.device(), **kw).copy()
+        s.B[1, 3, 35], s.B[1, 130, 2], s.B[2, 7, 5] = np.nan, np.inf, -np.inf
+        s.B[2, N - 1, 1], s.B[2, N - 1, 39], s.B[3, 0, 0], s.B[3, 0, 1] = np.inf, -np.inf, np.inf, np.nan
+        log(f"not finite M={M} N={N} roles={roles} dt={dt} residual={residual}")
+        inplace = kw["residual"] if residual else None
+        got = _call(dl, s.device(), y=inplace, **kw) if residual else _call(dl, s.device())
+    A, B, x = s.A.double().numpy(), s.B.double().numpy(), _x(dl)
+    with np.errstate(invalid="ignore"):
+        ref = np.stack([(float(s.scale[a]) * (x[m] @ A[a].T) * B[a]).sum(1) for m, a in enumerate(s.ids.tolist())])
+    assert (_kind(ref) != 0).sum() >= M and {2.0, 1.0, -1.0} <= set(_kind(ref).ravel())
+    assert np.array_equal(_kind(got), _kind(ref))
+    fine = np.isfinite(ref)
+    assert np.array_equal(got[fine], want[fine])
+
+
+@pytest.mark.parametrize("M,N,roles", [(150, 144, 2), (150, 144, 3), (300, 520, 3)])
+def test_entries_past_the_range_of_fp16_in_the_gemm(M, N, roles):
+    """A coordinate of 2^20 is divided by 2^6 there and the slot's B multiplied by it,
+    which entries of 2000 do not bear: y is finite all the same, either sign. Powers of
+    two and small integers: but for two roundings of y, and one for the pair of an
+    entry that was kept out, everything is exact."""
+    K, R = 256, 8
+    _, dl = _layer(M, N, K, S.F16, seed=1)
+    dl.scales.zero_()
+    dl.x.fill_(1.0)
+    s = Slots(M, N, K, 2, R, S.F16, ids="turn", scale=False)
+    s.A.zero_()
+    s.A[:, 0], s.A[:, 1, :2], s.A[:, 2, 0] = 4096.0, 1.0, -1.0  # coordinates 2^20, 2, -1
+    s.B.zero_()
+    s.B[:, :, 0] = 2.0 ** -8 * (1 + torch.arange(N) % 3)  # the term 4096, 8192, 12288
+    s.B[0, 5::16, 1] = 2000.0                              # + 4000
+    s.B[1, 6::16, 2] = 1504.0                              # - 1504
+    s.B[1, 7::16, 2] = -2000.0                             # + 2000
+    log(f"past fp16 in the GEMM M={M} N={N} roles={roles}")
+    with in_the_gemm(roles):
+        y = _call(dl, s.device())
+    ref = s.term(_x(dl))
+    assert np.abs(ref).max() < 2.0 ** 15 and (ref != ref[0]).any()
+    # half a step of fp16 for each rounding: of the partial sum and of y
+    assert np.all(np.abs(y - ref) <= HALF[S.F16] * (np.abs(ref) + 4000.0 + np.abs(ref)))
+    alone = np.ones(N, bool)
+    alone[5::16] = alone[6::16] = alone[7::16] = False
+    assert np.array_equal(y[:, alone], ref[:, alone])
