@@ -1258,7 +1258,7 @@ spear_status_t check_tail(const spear_problem_t* prob, const void* x, const spea
 // - ADAPT_EPILOGUE: k_gemm_ws (tiles of 256 tokens) forms it, as further steps of
 //   its loop. Its epilogue with a residual costs as much as another pass over the
 //   output (8B gate and up, 14336 x 4096 at 2048 tokens, fp16: 617 us with the term
-//   first, 574 with a pass after it that also rounds y once more, 482 this way,
+//   first, 574 with a pass after it that also rounds y once more, 481 this way,
 //   449 without adapters).
 enum { ADAPT_BEFORE = 0, ADAPT_RIDES = 1, ADAPT_EPILOGUE = 2, ADAPT_AFTER = 3 };
 // The adapter data of one member in the workspace: the K-slices of its
@@ -1350,10 +1350,13 @@ spear_status_t adapters_layout(int32_t n, const spear_layer_call_t* calls, const
     };
     // A further step of the GEMM's loop for each slot and 32 ranks costs as much as
     // one of K: it pays while a tile of 256 tokens meets few slots, about 8 where
-    // they come in runs and every slot is in use (8192 x 1024, us, in the GEMM and
-    // before it: 1024 tokens of 4 slots, rank 16, 37.6 and 49.6, of 16 42.9 and 49.0,
-    // of 64 68 and 47; 2048 of 64 71.0 and 70.8, in random order 262 and 180; 4096
-    // of 64 107 and 121). The hook that asks for these tiles asks for this too.
+    // they come in runs and every slot is in use (us, rank 16, in the GEMM and before
+    // it: 8192 x 1024, 1024 tokens of 4 slots 37.2 and 48.0, of 16 41.4 and 47.5, of
+    // 64 61.5 and 45.6; 2048 of 64 66.9 and 68.6; 4096 of 64 104 and 140, in random
+    // order 400 and 301; 14336 x 4096, 2048 of 4 slots 234 and 279, of 64 in random
+    // order 560 and 457). The ids are on the device: the slots that exist stand for
+    // those in use, so that a large pool takes the other way however few are. The
+    // hook that asks for these tiles asks for this too.
     const bool ws = !z[i].gemv && !z[i].ec && (z[i].groles == 2 || z[i].groles == 3);
     const bool few_slots = (int64_t)a->n_adapters * 32 <= p->M || g_ov_gr.load() >= 2;
     // (the GEMV variants compiled with fp32 sums; others only a forced path above 32
@@ -1961,7 +1964,7 @@ static spear_status_t run_group(int32_t n, const spear_layer_call_t* calls, Reso
 }
 
 // The grouped call; ads: the members' adapters (the array or any member may be
-// NULL), whose terms are formed first and enter the members as residuals.
+// NULL), whose terms join the members as the ADAPT_* values say.
 static spear_status_t group_call(int32_t n, const spear_layer_call_t* calls,
                                  const spear_adapters_t* const* ads, void* workspace,
                                  size_t workspace_bytes, void* hip_stream) {
