@@ -12,7 +12,7 @@ import torch
 from oracle import spear_oracle as O
 from paper_2606_11244_amd import synth as S
 
-from gpu_util import log
+from gpu_util import assert_parity, log
 from test_gpu_adapters import DT, HALF, Slots, _call, _gpu, _layer, _x, in_the_gemm  # noqa: F401 (a fixture)
 
 pytestmark = pytest.mark.gpu
@@ -108,6 +108,59 @@ def test_one_rounding_at_decode_with_an_ec(M, N, K, rank, path, dt):
     assert np.array_equal(want, np.float32(want)) and np.abs(want).max() < 2.0 ** 15
     assert np.array_equal(y, torch.from_numpy(want).float().to(DT[dt]).double().numpy())
     assert np.array_equal(_call(dl, s.device(), ec=True, residual=res.cuda()), y)  # (the workspace's counters go on)
+
+
+@pytest.mark.parametrize("M,N,K,rank,path", [(1, 264, 1152, 48, "GEMV"), (9, 264, 4608, 40, "GEMV"), (6, 264, 1024, 32, "2K"),
+                                             (20, 130, 4608, 64, "GEMV")])
+@pytest.mark.parametrize("dt", [S.F16, S.BF16])
+@pytest.mark.parametrize("bits,int8,gate", [(3, False, S.GATE_SIGMOID_LINEAR), (4, True, S.GATE_SIGMOID_LINEAR), (3, True, S.GATE_TANH_MLP)])
+def test_an_ec_wave_of_other_kinds(M, N, K, rank, path, dt, bits, int8, gate):
+    """Three-bit codes, INT8 factors and the tanh-MLP gate beside adapters at decode."""
+    L, dl = _layer(M, N, K, dt, seed=M, rank=rank, weight_bits=bits, ab_int8=int8, gate_kind=gate)
+    assert _path(dl) == path
+    s = Slots(M, N, K, 5, 16, dt, seed=9, mixed=True)
+    log(f"EC wave M={M} N={N} K={K} rank={rank} bits={bits} int8={int8} gate={gate} dt={dt}")
+    assert_parity(_call(dl, s.device(), ec=True), O.w4ec_linear(L) + s.term(_x(dl)), "an EC wave")
+
+
+@pytest.mark.parametrize("M,K,rank,path", [(1, 1152, 64, "GEMV"), (8, 4608, 48, "GEMV"), (4, 1024, 32, "2K")])
+def test_replays_with_an_ec_wave(M, K, rank, path):
+    """A captured call and group, replayed with other inputs between eager calls of
+    the same and of another layer on the same workspace."""
+    from paper_2606_11244_amd import spear as sp
+    N, dt = 264, S.F16
+    dls = [_layer(M, N, K, dt, seed=i, rank=rank)[1] for i in range(3)]
+    assert _path(dls[0]) == path
+    members = [dict(d.member(d.problem()), adapters=Slots(M, N, K, 4, 24, dt, seed=i).device()) for i, d in enumerate(dls)]
+    ws = torch.zeros(sp.adapters_workspace(members), dtype=torch.uint8, device="cuda")
+
+    def single(m, y):
+        sp.w4ec_linear_adapters(m["prob"], m["x"], m["qweight"], m["scales"], m["zeros"], m["adapters"], y,
+                                ec_args=m["ec_args"], workspace=ws)
+
+    def run():
+        single(members[0], members[0]["y"])
+        sp.w4ec_linear_adapters_group(members[1:], ws)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        run()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    for j in range(4):
+        log(f"replay {j} with an EC wave M={M} K={K} rank={rank}")
+        for d in dls:
+            d.x.copy_(torch.randn(M, K, generator=torch.Generator().manual_seed(j)))
+        graph.replay()
+        torch.cuda.synchronize()
+        for m in members:
+            eager = torch.empty_like(m["y"])
+            single(m, eager)
+            torch.cuda.synchronize()
+            assert torch.equal(eager, m["y"])
+            m["y"].zero_()
 
 
 @pytest.mark.parametrize("M,N,K,rank,path", DECODE_EC + [(3, 264, 1152, 0, None)])
