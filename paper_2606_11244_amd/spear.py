@@ -215,8 +215,13 @@ def _stream(stream):
 
 def _raw_stream(stream, device: int) -> int:
     """The same as an integer: a decode call is a few microseconds, and the
-    current stream's object takes two of them to make."""
-    return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
+    current stream's object takes two of them to make. A stream of another
+    device than the tensors' would run their kernels there."""
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(device)
+    if stream.device.index != device:
+        raise ValueError(f"a stream of the tensors' device is needed (got one of {stream.device})")
+    return stream.cuda_stream
 
 
 def problem(M, N, K, group_size=0, act_dtype=F16, rank=0, gate_kind=GATE_SIGMOID_LINEAR,
