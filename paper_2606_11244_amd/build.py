@@ -37,8 +37,9 @@ UNITS = tuple((src, f"w{wb}_{'bf16' if bf else 'f16'}",
     for wb in (4, 3) for bf in (0, 1)) + tuple(
     # and those that read no codes once per activation dtype
     (src, "bf16" if bf else "f16", [f"--offload-arch={ARCH}", "-x", "hip", f"-DSPEAR_BF16_UNIT={bf}"])
-    for src in ("spear_adapters.hip", "spear_norm.hip") for bf in (0, 1)) + (
+    for src in ("spear_adapters.hip", "spear_norm.hip", "spear_kv.hip", "spear_attn.hip") for bf in (0, 1)) + (
     ("spear_api.cpp", "", [f"--offload-arch={ARCH}", "-x", "hip"]),
+    ("spear_kv_api.cpp", "", [f"--offload-arch={ARCH}", "-x", "hip"]),
     ("spear_sched.cpp", "", [f"--offload-arch={ARCH}"]))
 
 

@@ -1,0 +1,277 @@
+// Host side of spear_kv.h: checks of the arguments, launch shapes.
+#include "spear_kv_internal.h"
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+
+#include "spear_kv.h"
+
+using namespace spear;
+
+namespace {
+
+bool off16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
+bool off4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) != 0; }
+bool overlaps(const void* a, size_t na, const void* b, size_t nb) {
+  if (!a || !b || na == 0 || nb == 0) return false;
+  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+  return x < y + nb && y < x + na;
+}
+spear_status_t hip_status(hipError_t e) { return e == hipSuccess ? SPEAR_OK : SPEAR_E_HIP; }
+bool page_size(int p) { return p == 16 || p == 32 || p == 64 || p == 128; }
+
+// a buffer; where row is given, only the first `row` of each `ld` bytes of it
+struct Span {
+  const void* p;
+  size_t bytes, row = 0, ld = 0;
+};
+bool hits(const Span& a, const Span& b) {
+  if (!overlaps(a.p, a.bytes, b.p, b.bytes)) return false;
+  if (!a.row || !b.row || a.ld != b.ld) return true;
+  // rows of one stride, as the parts of a packed projection: apart within the stride
+  const uintptr_t x = (uintptr_t)a.p, y = (uintptr_t)b.p;
+  const size_t d = x <= y ? (y - x) % a.ld : (a.ld - (x - y) % a.ld) % a.ld;
+  return d < a.row || a.ld - d < b.row;
+}
+// whether one of outs overlaps another of them or one of ins
+bool clash(const Span* outs, int n_outs, const Span* ins, int n_ins) {
+  for (int i = 0; i < n_outs; ++i) {
+    for (int j = i + 1; j < n_outs; ++j)
+      if (hits(outs[i], outs[j])) return true;
+    for (int j = 0; j < n_ins; ++j)
+      if (hits(outs[i], ins[j])) return true;
+  }
+  return false;
+}
+// `rows` rows of `row` elements, `ld` apart, to the end of the last
+Span rows_of(const void* p, int64_t rows, int64_t ld, int64_t row) {
+  return {p, rows > 0 ? ((size_t)(rows - 1) * ld + row) * 2 : 0, (size_t)row * 2, (size_t)ld * 2};
+}
+
+spear_status_t check_cache(const spear_kv_cache_t* c, bool buffers = true) {
+  if (!c) return SPEAR_E_NULL;
+  if (c->format != SPEAR_KV_INT8 && c->format != SPEAR_KV_E4M3) return SPEAR_E_DTYPE;
+  if (c->act_dtype != SPEAR_F16 && c->act_dtype != SPEAR_BF16) return SPEAR_E_DTYPE;
+  if (c->kv_heads < 1 || c->kv_heads > 1024 || (c->head_dim != 64 && c->head_dim != 128) ||
+      !page_size(c->page_tokens) || c->reserved != 0 || c->pages < 0 ||
+      c->pages >= ((int64_t)1 << 31) / c->page_tokens)
+    return SPEAR_E_SHAPE;
+  if (!buffers) return SPEAR_OK;
+  if (c->pages && (!c->k || !c->v || !c->k_scale || !c->v_scale)) return SPEAR_E_NULL;
+  if (off16(c->k) || off16(c->v) || off16(c->k_scale) || off16(c->v_scale)) return SPEAR_E_ALIGN;
+  return SPEAR_OK;
+}
+KvCache cache_of(const spear_kv_cache_t* c) {
+  return {(uint8_t*)c->k, (uint8_t*)c->v, c->k_scale, c->v_scale, c->kv_heads, c->head_dim, c->page_tokens, (int)c->pages};
+}
+// the cache's four buffers
+void cache_spans(const spear_kv_cache_t* c, Span (&s)[4]) {
+  const size_t heads = (size_t)c->pages * c->kv_heads, codes = heads * c->page_tokens * c->head_dim;
+  s[0] = {c->k, codes}, s[1] = {c->v, codes}, s[2] = {c->k_scale, heads * 4}, s[3] = {c->v_scale, heads * 4};
+}
+
+spear_status_t check_batch(const spear_kv_batch_t* b, bool buffers = true) {
+  if (!b) return SPEAR_E_NULL;
+  if (b->requests < 0 || b->requests > kKvRequests || b->tokens < 0 || b->tokens > kKvTokens || b->max_new < 1 ||
+      (b->tokens && b->max_new > b->tokens) || b->width < 1 || b->width > (1 << 26) ||
+      (b->table_ld != 0 && b->table_ld < b->width) || b->reserved != 0)
+    return SPEAR_E_SHAPE;
+  if (!buffers) return SPEAR_OK;
+  if (!b->starts || (b->requests && (!b->lens || !b->table))) return SPEAR_E_NULL;
+  if (off4(b->starts) || off4(b->lens) || off4(b->table)) return SPEAR_E_ALIGN;
+  return SPEAR_OK;
+}
+int64_t table_ld(const spear_kv_batch_t* b) { return b->table_ld ? b->table_ld : b->width; }
+size_t table_bytes(const spear_kv_batch_t* b) {
+  return b->requests ? ((size_t)(b->requests - 1) * table_ld(b) + b->width) * 4 : 0;
+}
+
+}  // namespace
+
+spear_status_t spear_kv_pages(const spear_kv_batch_t* b, const spear_kv_pages_t* a, void* hip_stream) {
+  if (!b || !a) return SPEAR_E_NULL;
+  const spear_status_t st = check_batch(b);
+  if (st != SPEAR_OK) return st;
+  if (!page_size(a->page_tokens) || a->n_free < 0) return SPEAR_E_SHAPE;
+  if (!a->taken || (b->requests && (!a->held || !a->fresh)) || (a->n_free && !a->free_pages) ||
+      (b->tokens && (!a->slots || !a->positions)))
+    return SPEAR_E_NULL;
+  if (off4(a->held) || off4(a->fresh) || off4(a->free_pages) || off4(a->slots) || off4(a->positions) || off4(a->taken))
+    return SPEAR_E_ALIGN;
+  const size_t R = b->requests, T = b->tokens;
+  const Span outs[] = {{b->starts, (R + 1) * 4}, {b->lens, R * 4},      {b->table, table_bytes(b)},
+                       {a->slots, T * 4},        {a->positions, T * 4}, {a->taken, 8}};
+  const Span ins[] = {{a->held, R * 4}, {a->fresh, R * 4}, {a->free_pages, (size_t)a->n_free * 4}};
+  if (clash(outs, 6, ins, 3)) return SPEAR_E_ALIAS;
+  KvPagesParams p;
+  p.R = b->requests, p.T = b->tokens, p.P = a->page_tokens, p.width = b->width, p.n_free = a->n_free;
+  p.ld = table_ld(b);
+  p.held = a->held, p.fresh = a->fresh, p.free_pages = a->free_pages;
+  p.starts = b->starts, p.lens = b->lens, p.table = b->table;
+  p.slots = a->slots, p.positions = a->positions, p.taken = a->taken;
+  return hip_status(launch_kv_pages(p, (hipStream_t)hip_stream));
+}
+
+spear_status_t spear_rope_frequencies(int32_t rotary_dim, double base, double factor, double context,
+                                      double low_turns, double high_turns, uint64_t* freqs) {
+  if (rotary_dim < 0 || rotary_dim % 2 || rotary_dim > 1 << 20 || !(base > 1.0) || !std::isfinite(base) ||
+      !(factor >= 1.0) || !std::isfinite(factor) || !(context >= 0.0) || !std::isfinite(context))
+    return SPEAR_E_SHAPE;
+  const bool parts = factor > 1.0 && context > 0.0;
+  if (parts && !(high_turns > low_turns && std::isfinite(high_turns) && std::isfinite(low_turns))) return SPEAR_E_SHAPE;
+  if (rotary_dim && !freqs) return SPEAR_E_NULL;
+  for (int i = 0; i < rotary_dim / 2; ++i) {
+    // turns a position, at most 0.16
+    long double f = std::pow((long double)base, -2.0L * i / rotary_dim) / 6.283185307179586476925286766559L;
+    long double share = factor > 1.0 ? 0.0L : 1.0L;
+    if (parts)
+      share = std::min(1.0L, std::max(0.0L, (f * context - low_turns) / ((long double)high_turns - low_turns)));
+    f *= share + (1.0L - share) / factor;
+    freqs[i] = (uint64_t)std::llround(f * 18446744073709551616.0L);
+  }
+  return SPEAR_OK;
+}
+
+spear_status_t spear_kv_append(const spear_kv_cache_t* c, const spear_kv_append_t* a, void* hip_stream) {
+  if (!a) return SPEAR_E_NULL;
+  spear_status_t st = check_cache(c);
+  if (st != SPEAR_OK) return st;
+  const int64_t T = a->tokens, kv = (int64_t)c->kv_heads * c->head_dim;
+  const int64_t qd = a->q ? (int64_t)a->heads * c->head_dim : 0;
+  if (T < 0 || T > kKvTokens || (a->q && (a->heads < 1 || a->heads > 1024))) return SPEAR_E_SHAPE;
+  const spear_rope_t& r = a->rope;
+  if (r.rotary_dim < 0 || r.rotary_dim > c->head_dim || r.rotary_dim % 2 || r.interleaved < 0 || r.interleaved > 1 ||
+      r.reserved != 0 || (r.rotary_dim && !std::isfinite(r.magnitude)))
+    return SPEAR_E_SHAPE;
+  bool ld_ok = true;
+  auto ld = [&](int64_t v, int64_t row) {
+    const int64_t l = v == 0 ? row : v;
+    ld_ok = ld_ok && l >= row && l % 8 == 0 && l < ((int64_t)1 << 30);
+    return l;
+  };
+  const int64_t kl = ld(a->k_ld, kv), vl = ld(a->v_ld, kv);
+  const int64_t ql = a->q ? ld(a->q_ld, qd) : 0, ol = a->q ? ld(a->q_out_ld, qd) : 0;
+  if (!ld_ok) return SPEAR_E_SHAPE;
+  if (T == 0) return SPEAR_OK;
+  if (!a->k || !a->v || !a->slots || (a->q && !a->q_out) || (r.rotary_dim && (!r.freqs || !a->positions)))
+    return SPEAR_E_NULL;
+  if (off16(a->k) || off16(a->v) || off16(a->q) || (a->q && off16(a->q_out)) || off4(a->slots) || off4(a->positions) ||
+      (r.rotary_dim && (reinterpret_cast<uintptr_t>(r.freqs) & 7u)))
+    return SPEAR_E_ALIGN;
+  Span outs[5];
+  cache_spans(c, reinterpret_cast<Span(&)[4]>(outs));
+  outs[4] = rows_of(a->q ? a->q_out : nullptr, T, ol, qd);
+  const bool in_place = a->q && a->q == a->q_out && ql == ol;
+  const Span ins[] = {rows_of(a->k, T, kl, kv),
+                      rows_of(a->v, T, vl, kv),
+                      {a->slots, (size_t)T * 4},
+                      {a->positions, r.rotary_dim ? (size_t)T * 4 : 0},
+                      {r.freqs, (size_t)r.rotary_dim / 2 * 8},
+                      rows_of(in_place ? nullptr : a->q, T, ql, qd)};
+  if (clash(outs, 5, ins, 6) || (in_place && clash(outs, 4, outs + 4, 1))) return SPEAR_E_ALIAS;
+  if (c->pages == 0) return SPEAR_OK;  // every slot is outside
+  KvAppendParams p;
+  p.c = cache_of(c);
+  p.r = {r.freqs, r.rotary_dim, r.interleaved, r.magnitude};
+  p.T = (int)T, p.H = a->q ? a->heads : 0;
+  p.q = (const uint16_t*)a->q, p.k = (const uint16_t*)a->k, p.v = (const uint16_t*)a->v;
+  p.q_out = (uint16_t*)a->q_out;
+  p.q_ld = ql, p.k_ld = kl, p.v_ld = vl, p.qo_ld = ol;
+  p.slots = a->slots, p.positions = a->positions;
+  p.window = T <= 1024 ? 1 : 4;
+  p.q_tokens = T <= 1024 ? 1 : 4;
+  p.kv_blocks = (uint32_t)((T + p.window - 1) / p.window * c->kv_heads * 2);
+  p.q_blocks = a->q ? (uint32_t)((T + p.q_tokens - 1) / p.q_tokens) : 0;
+  const auto launch = c->act_dtype == SPEAR_F16 ? launch_kv_append_f16 : launch_kv_append_bf16;
+  return hip_status(launch(p, c->format, (hipStream_t)hip_stream));
+}
+
+spear_status_t spear_kv_read(const spear_kv_cache_t* c, int64_t n, const int32_t* slots, void* k_out, void* v_out,
+                             void* hip_stream) {
+  const spear_status_t st = check_cache(c);
+  if (st != SPEAR_OK) return st;
+  if (n < 0 || n >= ((int64_t)1 << 31) || (n + 15) / 16 * c->kv_heads >= ((int64_t)1 << 31)) return SPEAR_E_SHAPE;
+  if (n == 0) return SPEAR_OK;
+  if (!slots || !k_out || !v_out) return SPEAR_E_NULL;
+  if (off4(slots) || off16(k_out) || off16(v_out)) return SPEAR_E_ALIGN;
+  const size_t row = (size_t)n * c->kv_heads * c->head_dim * 2;
+  const Span outs[] = {{k_out, row}, {v_out, row}};
+  Span ins[5];
+  cache_spans(c, reinterpret_cast<Span(&)[4]>(ins));
+  ins[4] = {slots, (size_t)n * 4};
+  if (clash(outs, 2, ins, 5)) return SPEAR_E_ALIAS;
+  if (c->pages == 0) return SPEAR_OK;
+  const KvReadParams p{cache_of(c), n, slots, (uint16_t*)k_out, (uint16_t*)v_out};
+  const auto launch = c->act_dtype == SPEAR_F16 ? launch_kv_read_f16 : launch_kv_read_bf16;
+  return hip_status(launch(p, c->format, (hipStream_t)hip_stream));
+}
+
+namespace {
+
+spear_status_t check_attention(const spear_attention_t* a, bool buffers) {
+  if (!a) return SPEAR_E_NULL;
+  spear_status_t st = check_cache(a->cache, buffers);
+  if (st == SPEAR_OK) st = check_batch(a->batch, buffers);
+  if (st != SPEAR_OK) return st;
+  if (a->heads < 1 || a->heads > 1024 || a->heads % a->cache->kv_heads || a->window < 0) return SPEAR_E_SHAPE;
+  if (!buffers) return SPEAR_OK;
+  if (!a->plan) return SPEAR_E_NULL;
+  if (off16(a->plan) || off4(a->prefix)) return SPEAR_E_ALIGN;
+  return SPEAR_OK;
+}
+
+}  // namespace
+
+spear_status_t spear_attention_sizes(const spear_attention_t* a, size_t* plan_bytes, size_t* workspace_bytes) {
+  if (!a || !plan_bytes || !workspace_bytes) return SPEAR_E_NULL;
+  const spear_status_t st = check_attention(a, false);
+  if (st != SPEAR_OK) return st;
+  *plan_bytes = 256;
+  *workspace_bytes = 256;
+  return SPEAR_OK;
+}
+
+spear_status_t spear_attention_plan(const spear_attention_t* a, void*) {
+  const spear_status_t st = check_attention(a, true);
+  if (st != SPEAR_OK) return st;
+  size_t plan = 0, work = 0;
+  spear_attention_sizes(a, &plan, &work);
+  return a->plan_bytes < plan ? SPEAR_E_WORKSPACE : SPEAR_OK;
+}
+
+spear_status_t spear_attention(const spear_attention_t* a, void* hip_stream) {
+  const spear_status_t st = check_attention(a, true);
+  if (st != SPEAR_OK) return st;
+  const spear_kv_cache_t* c = a->cache;
+  const spear_kv_batch_t* b = a->batch;
+  const int64_t T = b->tokens, row = (int64_t)a->heads * c->head_dim;
+  const int64_t ql = a->q_ld ? a->q_ld : row, ol = a->out_ld ? a->out_ld : row;
+  if (ql < row || ol < row || ql % 8 || ol % 8 || ql >= ((int64_t)1 << 30) || ol >= ((int64_t)1 << 30) ||
+      !std::isfinite(a->scale) || !std::isfinite(a->softcap) || a->softcap < 0.f)
+    return SPEAR_E_SHAPE;
+  if (T == 0 || b->requests == 0) return SPEAR_OK;
+  if (!a->q || !a->out) return SPEAR_E_NULL;
+  if (off16(a->q) || off16(a->out) || off4(a->slopes) || off16(a->workspace)) return SPEAR_E_ALIGN;
+  size_t plan = 0, work = 0;
+  spear_attention_sizes(a, &plan, &work);
+  if (a->plan_bytes < plan || a->workspace_bytes < work || !a->workspace) return SPEAR_E_WORKSPACE;
+  const size_t R = b->requests;
+  const Span outs[] = {rows_of(a->out, T, ol, row), {a->workspace, work}};
+  Span ins[11];
+  cache_spans(c, reinterpret_cast<Span(&)[4]>(ins));
+  ins[4] = {b->starts, (R + 1) * 4}, ins[5] = {b->lens, R * 4}, ins[6] = {b->table, table_bytes(b)};
+  ins[7] = {a->prefix, R * 4}, ins[8] = {a->slopes, (size_t)a->heads * 4}, ins[9] = {a->plan, plan};
+  ins[10] = rows_of(a->q, T, ql, row);
+  if (clash(outs, 2, ins, 11)) return SPEAR_E_ALIAS;
+  KvAttendParams p;
+  p.c = cache_of(c);
+  p.R = b->requests, p.T = b->tokens, p.H = a->heads, p.group = a->heads / c->kv_heads;
+  p.max_new = b->max_new, p.width = b->width, p.window_tokens = a->window ? a->window : kKvLength;
+  p.ld = table_ld(b), p.q_ld = ql, p.out_ld = ol;
+  p.starts = b->starts, p.lens = b->lens, p.table = b->table, p.prefix = a->prefix;
+  p.q = (const uint16_t*)a->q, p.out = (uint16_t*)a->out;
+  p.slopes = a->slopes, p.scale = a->scale, p.softcap = a->softcap;
+  const auto launch = c->act_dtype == SPEAR_F16 ? launch_kv_attend_f16 : launch_kv_attend_bf16;
+  return hip_status(launch(p, c->format, (hipStream_t)hip_stream));
+}

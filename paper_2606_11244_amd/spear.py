@@ -38,7 +38,8 @@ EXPORTED = ("spear_dispatch_plan", "spear_w4_linear", "spear_w4ec_linear", "spea
             "spear_set_gemm_tile", "spear_set_gemm_roles", "spear_workspace_regions",
             "spear_w4ec_linear_noalloc", "spear_adapters_workspace", "spear_w4ec_linear_adapters",
             "spear_w4ec_linear_adapters_group", "spear_block_norm",
-            "spear_set_gemv_stages",
+            "spear_set_gemv_stages", "spear_kv_pages", "spear_rope_frequencies", "spear_kv_append",
+            "spear_kv_read", "spear_attention_sizes", "spear_attention_plan", "spear_attention",
             "spear_status_string", "spear_version", "spear_sched_latency", "spear_sched_chunk")
 
 

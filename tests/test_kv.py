@@ -1,0 +1,276 @@
+"""The cache's and attention's calls (include/spear_kv.h) on the host: what they
+refuse, their sizes, the rotary frequencies."""
+from __future__ import annotations
+
+import ctypes
+import math
+from fractions import Fraction
+
+import pytest
+import torch
+
+from paper_2606_11244_amd import kv
+from paper_2606_11244_amd import spear as sp
+
+NULL, SHAPE, DTYPE, ALIGN, WORKSPACE, ALIAS = -1, -2, -3, -4, -5, -8
+MB = 1 << 20
+
+
+def _at(i):
+    """A made-up address, 64 MB from the next: nothing is read or written on the host."""
+    return (1 << 40) + i * 64 * MB
+
+
+def cache(**kw):
+    a = dict(format=0, act_dtype=0, kv_heads=2, head_dim=64, page_tokens=16, reserved=0, pages=10, k=_at(0), v=_at(1),
+             k_scale=_at(2), v_scale=_at(3))
+    a.update(kw)
+    return kv._Cache(**a)
+
+
+def batch(**kw):
+    a = dict(requests=3, tokens=5, max_new=2, width=4, table_ld=0, reserved=0, starts=_at(4), lens=_at(5), table=_at(6))
+    a.update(kw)
+    return kv._Batch(**a)
+
+
+BAD_CACHE = [(dict(format=2), DTYPE), (dict(act_dtype=2), DTYPE), (dict(kv_heads=0), SHAPE), (dict(kv_heads=1025), SHAPE),
+             (dict(head_dim=96), SHAPE), (dict(head_dim=0), SHAPE), (dict(page_tokens=24), SHAPE),
+             (dict(page_tokens=256), SHAPE), (dict(pages=-1), SHAPE), (dict(pages=1 << 27), SHAPE), (dict(reserved=1), SHAPE),
+             (dict(k=None), NULL), (dict(v_scale=None), NULL), (dict(v=_at(1) + 8), ALIGN), (dict(k_scale=_at(2) + 4), ALIGN)]
+BAD_BATCH = [(dict(requests=-1), SHAPE), (dict(requests=4097), SHAPE), (dict(tokens=-1), SHAPE),
+             (dict(tokens=(1 << 22) + 1), SHAPE), (dict(max_new=0), SHAPE), (dict(max_new=6), SHAPE), (dict(width=0), SHAPE),
+             (dict(table_ld=3), SHAPE), (dict(reserved=1), SHAPE), (dict(starts=None), NULL), (dict(lens=None), NULL),
+             (dict(table=None), NULL), (dict(starts=_at(4) + 2), ALIGN), (dict(table=_at(6) + 1), ALIGN)]
+
+
+def pages(b=None, **kw):
+    a = dict(page_tokens=16, n_free=7, held=_at(10), fresh=_at(11), free_pages=_at(12), slots=_at(13), positions=_at(14),
+             taken=_at(15))
+    a.update(kw)
+    return sp.LIB.spear_kv_pages(ctypes.byref(b or batch()), ctypes.byref(kv._Pages(**a)), None)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(page_tokens=8), SHAPE), (dict(n_free=-1), SHAPE), (dict(held=None), NULL), (dict(fresh=None), NULL),
+    (dict(free_pages=None), NULL), (dict(slots=None), NULL), (dict(positions=None), NULL), (dict(taken=None), NULL),
+    (dict(slots=_at(13) + 2), ALIGN), (dict(slots=_at(10)), ALIAS), (dict(taken=_at(12) + 24), ALIAS),
+    (dict(positions=_at(13) + 16), ALIAS), (dict(free_pages=_at(6) + 44), ALIAS), (dict(held=_at(4) + 12), ALIAS)])
+def test_pages_refusals(kw, code):
+    assert pages(**kw) == code
+
+
+@pytest.mark.parametrize("kw,code", BAD_BATCH)
+def test_pages_refuse_batches(kw, code):
+    assert pages(batch(**kw)) == code
+
+
+def append(c=None, **kw):
+    a = dict(tokens=5, heads=4, q=_at(20), k=_at(21), v=_at(22), q_out=_at(23), q_ld=0, k_ld=0, v_ld=0, q_out_ld=0,
+             slots=_at(24), positions=_at(25))
+    rope = dict(rotary_dim=64, interleaved=0, magnitude=1.0, reserved=0, freqs=_at(26))
+    for d in (a, rope):
+        d.update({k: v for k, v in kw.items() if k in d})
+    return sp.LIB.spear_kv_append(ctypes.byref(c or cache()), ctypes.byref(kv._Append(**a, rope=kv._Rope(**rope))), None)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(tokens=-1), SHAPE), (dict(tokens=(1 << 22) + 1), SHAPE), (dict(heads=0), SHAPE), (dict(heads=1025), SHAPE),
+    (dict(k_ld=120), SHAPE), (dict(k_ld=132), SHAPE), (dict(v_ld=-128), SHAPE), (dict(q_ld=248), SHAPE),
+    (dict(q_out_ld=260), SHAPE), (dict(q_ld=1 << 30), SHAPE), (dict(rotary_dim=65), SHAPE), (dict(rotary_dim=66), SHAPE),
+    (dict(rotary_dim=-2), SHAPE), (dict(interleaved=2), SHAPE), (dict(magnitude=math.inf), SHAPE),
+    (dict(magnitude=math.nan), SHAPE), (dict(reserved=3), SHAPE), (dict(k=None), NULL), (dict(v=None), NULL),
+    (dict(q_out=None), NULL), (dict(slots=None), NULL), (dict(positions=None), NULL), (dict(freqs=None), NULL),
+    (dict(k=_at(21) + 8), ALIGN), (dict(q_out=_at(23) + 2), ALIGN), (dict(slots=_at(24) + 1), ALIGN),
+    (dict(freqs=_at(26) + 4), ALIGN), (dict(q_out=_at(21)), ALIAS), (dict(q_out=_at(20) + 512), ALIAS),
+    (dict(q_out=_at(20), q_out_ld=512), ALIAS), (dict(q_out=_at(0)), ALIAS), (dict(q=_at(1), q_out=_at(1)), ALIAS),
+    (dict(k=_at(1)), ALIAS), (dict(slots=_at(2)), ALIAS)])
+def test_append_refusals(kw, code):
+    assert append(**kw) == code
+
+
+def test_parts_of_a_packed_projection_do_not_overlap():
+    row = (4 + 2 + 2) * 64  # q, k, v of a token beside each other
+    ld = dict(q_ld=row, q_out_ld=row, k_ld=row, v_ld=row)
+    at = lambda f: _at(20) + 2 * f  # noqa: E731
+    none = cache(pages=0, k=None, v=None, k_scale=None, v_scale=None)
+    assert append(none, q=at(0), q_out=at(0), k=at(256), v=at(384), **ld) == 0
+    assert append(none, q=at(256), q_out=at(256), k=at(0), v=at(128), **ld) == 0
+    assert append(none, q=at(0), q_out=at(0), k=at(248), v=at(384), **ld) == ALIAS
+    assert append(none, q=at(256), q_out=at(256), k=at(136), v=at(0), **ld) == ALIAS
+    assert append(none, q=at(0), q_out=at(0), k=at(256), v=at(384 + row), **ld) == 0
+    assert append(none, q=at(0), q_out=at(0), k=at(256), v=at(392 + row), **ld) == ALIAS
+    assert append(none, q=at(0), q_out=at(0), k=at(256), v=at(384), **dict(ld, k_ld=row + 8)) == ALIAS
+
+
+@pytest.mark.parametrize("kw,code", BAD_CACHE)
+def test_append_and_read_refuse_caches(kw, code):
+    c = cache(**kw)
+    assert append(c) == code
+    assert sp.LIB.spear_kv_read(ctypes.byref(c), 4, _at(30), _at(31), _at(32), None) == code
+
+
+@pytest.mark.parametrize("n,slots,k,v,code", [
+    (-1, _at(30), _at(31), _at(32), SHAPE), (1 << 31, _at(30), _at(31), _at(32), SHAPE), (4, None, _at(31), _at(32), NULL),
+    (4, _at(30), None, _at(32), NULL), (4, _at(30), _at(31), None, NULL), (4, _at(30) + 2, _at(31), _at(32), ALIGN),
+    (4, _at(30), _at(31) + 8, _at(32), ALIGN), (4, _at(30), _at(31), _at(31) + 512, ALIAS),
+    (4, _at(31) + 64, _at(31), _at(32), ALIAS), (4, _at(30), _at(0), _at(32), ALIAS), (0, None, None, None, 0)])
+def test_read_refusals(n, slots, k, v, code):
+    assert sp.LIB.spear_kv_read(ctypes.byref(cache()), n, slots, k, v, None) == code
+
+
+def test_buffers_of_one_cache_may_not_overlap():
+    assert append(cache(v=_at(0) + 128)) == ALIAS
+    assert append(cache(v_scale=_at(2) + 16)) == ALIAS
+
+
+def attention(c=None, b=None, call="spear_attention", sizes=False, **kw):
+    c, b = c or cache(), b or batch()
+    a = dict(heads=4, window=0, prefix=None, plan=_at(40), plan_bytes=32 * MB, q=_at(41), out=_at(42), q_ld=0, out_ld=0,
+             slopes=None, scale=0.1, softcap=0.0, workspace=_at(43), workspace_bytes=32 * MB)
+    a.update(kw)
+    s = kv._Attention(cache=ctypes.pointer(c), batch=ctypes.pointer(b), **a)
+    if sizes:
+        p, w = ctypes.c_size_t(), ctypes.c_size_t()
+        return sp.LIB.spear_attention_sizes(ctypes.byref(s), ctypes.byref(p), ctypes.byref(w)), p.value, w.value
+    return getattr(sp.LIB, call)(ctypes.byref(s), None)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(heads=0), SHAPE), (dict(heads=3), SHAPE), (dict(heads=1026), SHAPE), (dict(window=-1), SHAPE),
+    (dict(plan=None), NULL), (dict(plan=_at(40) + 8), ALIGN), (dict(prefix=_at(44) + 2), ALIGN), (dict(plan_bytes=0), WORKSPACE)])
+def test_plan_and_attention_refusals(kw, code):
+    for call in ("spear_attention_plan", "spear_attention"):
+        assert attention(call=call, **kw) == code
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(q_ld=248), SHAPE), (dict(out_ld=260), SHAPE), (dict(q_ld=1 << 30), SHAPE), (dict(scale=math.nan), SHAPE),
+    (dict(scale=math.inf), SHAPE), (dict(softcap=-1.0), SHAPE), (dict(softcap=math.inf), SHAPE), (dict(q=None), NULL),
+    (dict(out=None), NULL), (dict(q=_at(41) + 2), ALIGN), (dict(out=_at(42) + 8), ALIGN), (dict(slopes=_at(44) + 2), ALIGN),
+    (dict(workspace=_at(43) + 8), ALIGN), (dict(workspace=None), WORKSPACE), (dict(workspace_bytes=0), WORKSPACE),
+    (dict(out=_at(41)), ALIAS), (dict(out=_at(1) + 64), ALIAS), (dict(out=_at(6)), ALIAS), (dict(out=_at(43)), ALIAS),
+    (dict(workspace=_at(40)), ALIAS), (dict(workspace=_at(2)), ALIAS), (dict(slopes=_at(42)), ALIAS),
+    (dict(prefix=_at(42)), ALIAS)])
+def test_attention_refusals(kw, code):
+    assert attention(**kw) == code
+
+
+@pytest.mark.parametrize("kw,code", BAD_CACHE)
+def test_attention_refuses_caches(kw, code):
+    assert attention(c=cache(**kw)) == code
+
+
+@pytest.mark.parametrize("kw,code", BAD_BATCH)
+def test_attention_refuses_batches(kw, code):
+    assert attention(b=batch(**kw)) == code
+
+
+def test_null_arguments():
+    c, b, n = ctypes.byref(cache()), ctypes.byref(batch()), None
+    assert sp.LIB.spear_kv_pages(n, n, n) == NULL and sp.LIB.spear_kv_pages(b, n, n) == NULL
+    assert sp.LIB.spear_kv_append(n, n, n) == NULL and sp.LIB.spear_kv_append(c, n, n) == NULL
+    assert sp.LIB.spear_kv_read(n, 1, n, n, n, n) == NULL
+    assert sp.LIB.spear_attention(n, n) == NULL and sp.LIB.spear_attention_plan(n, n) == NULL
+    assert sp.LIB.spear_attention_sizes(n, n, n) == NULL
+
+
+def test_nothing_to_do_is_no_error():
+    assert append(tokens=0) == 0
+    assert append(cache(pages=0, k=None, v=None, k_scale=None, v_scale=None)) == 0
+    assert attention(b=batch(tokens=0)) == 0
+    assert attention(b=batch(requests=0)) == 0
+
+
+def test_sizes_take_no_buffers_and_do_not_shrink():
+    none = dict(k=None, v=None, k_scale=None, v_scale=None)
+    last = (0, 0)
+    for R, T in ((0, 0), (1, 1), (4, 9), (64, 64), (64, 5000), (4096, 1 << 22)):
+        st, plan, work = attention(cache(**none), batch(requests=R, tokens=T, max_new=1, starts=None, lens=None, table=None),
+                                   plan=None, workspace=None, sizes=True)
+        assert st == 0 and plan >= last[0] and work >= last[1]
+        last = (plan, work)
+    assert attention(sizes=True, heads=5)[0] == SHAPE
+
+
+def _freqs(rot, base=10000.0, factor=1.0, context=0.0, low=1.0, high=4.0):
+    f = torch.zeros(max(rot, 0) // 2 + 1, dtype=torch.int64)
+    return sp.LIB.spear_rope_frequencies(rot, base, factor, context, low, high, f.data_ptr()), f.tolist()
+
+
+@pytest.mark.parametrize("rot,base", [(64, 10000.0), (128, 500000.0), (2, 10.0), (6, 1e6), (256, 10000.0)])
+def test_rope_frequencies(rot, base):
+    st, f = _freqs(rot, base)
+    assert st == 0 and f[-1] == 0
+    for i in range(rot // 2):
+        want = base ** (-2.0 * i / rot) / (2 * math.pi)
+        # 64-bit floats of the formula are right to 2^-50; whole numbers of 2^-64 turns to half a step
+        assert abs(Fraction(f[i], 2 ** 64) - Fraction(want)) <= Fraction(want) / 2 ** 48 + Fraction(1, 2 ** 65)
+
+
+def test_rope_frequencies_for_longer_contexts():
+    _, plain = _freqs(64)
+    _, slow = _freqs(64, factor=8.0)
+    _, parts = _freqs(64, factor=8.0, context=4096.0, low=2.0, high=32.0)
+    for p, s, m in zip(plain[:32], slow, parts):
+        assert abs(s - p / 8) <= 2 ** -48 * p + 1
+        turns = p / 2 ** 64 * 4096
+        share = min(1.0, max(0.0, (turns - 2.0) / 30.0))
+        assert abs(m - p * (share + (1 - share) / 8)) <= 2 ** -45 * p + 1
+    assert parts[0] == plain[0] and parts[31] == slow[31]
+
+
+@pytest.mark.parametrize("kw", [dict(rot=3), dict(rot=-2), dict(rot=8, base=1.0), dict(rot=8, base=math.nan),
+                                dict(rot=8, factor=0.5), dict(rot=8, factor=math.inf), dict(rot=8, context=-1.0),
+                                dict(rot=8, factor=2.0, context=10.0, low=4.0, high=4.0),
+                                dict(rot=8, factor=2.0, context=10.0, low=math.nan)])
+def test_rope_frequencies_refusals(kw):
+    assert _freqs(**kw)[0] == SHAPE
+
+
+def test_rope_frequencies_need_memory():
+    assert sp.LIB.spear_rope_frequencies(8, 10000.0, 1.0, 0.0, 1.0, 4.0, None) == NULL
+    assert sp.LIB.spear_rope_frequencies(0, 10000.0, 1.0, 0.0, 1.0, 4.0, None) == 0
+
+
+# ---- the binding's own checks: what only the tensors know ------------------
+
+def _tensors(P=16, D=64, codes=torch.int8):
+    return (torch.zeros(3, 2, P, D).to(codes), torch.zeros(3, 2, D, P).to(codes), torch.ones(3, 2), torch.ones(3, 2))
+
+
+def test_binding_refuses_caches():
+    k, v, ks, vs = _tensors()
+    kv.Cache(k, v, ks, vs, torch.float16)
+    with pytest.raises(TypeError):
+        kv.Cache(k, v, ks, vs, torch.float32)
+    with pytest.raises(TypeError):
+        kv.Cache(k, v.view(torch.uint8), ks, vs, torch.float16)
+    with pytest.raises(ValueError):
+        kv.Cache(k, v.transpose(2, 3), ks, vs, torch.float16)
+    with pytest.raises(ValueError):
+        kv.Cache(k, v, ks[:, :1], vs, torch.float16)
+    with pytest.raises(ValueError):
+        kv.Cache(k[:, :, :, ::2], v[:, :, ::2], ks, vs, torch.float16)
+
+
+def test_binding_refuses_batches_and_tensors_off_the_gpu():
+    t = torch.zeros(4, 8, dtype=torch.int32)
+    b = kv.Batch(t, 5)
+    assert b.max_new == 5 and kv.Batch(t[:, :3], 5, 2).c.table_ld == 8
+    for bad in (t.long(), t[:, ::2], t[0], t[:1].expand(4, 8)):
+        with pytest.raises(ValueError):
+            kv.Batch(bad, 5)
+    with pytest.raises(ValueError):
+        kv.Batch(t, 5, starts=torch.zeros(4, dtype=torch.int32))
+    x = torch.zeros(5, dtype=torch.int32)
+    with pytest.raises(ValueError, match="current GPU"):
+        kv.pages(b, x[:4], x[:4], x, x.clone(), x.clone(), x[:2].clone(), page_tokens=16)
+    c = kv.Cache(*_tensors(), torch.float16)
+    rows = torch.zeros(5, 2, 64, dtype=torch.float16)
+    with pytest.raises(ValueError, match="current GPU"):
+        kv.append(c, rows, rows, x)
+    with pytest.raises(ValueError, match="current GPU"):
+        kv.read(c, x, rows, rows)
+    with pytest.raises(ValueError, match="GPU"):
+        kv.attention_plan(kv.AttentionPlan(c, b, 2))
