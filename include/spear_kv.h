@@ -183,7 +183,8 @@ spear_status_t spear_kv_read(const spear_kv_cache_t* cache, int64_t n, const int
 typedef struct {
   const spear_kv_cache_t* cache;
   const spear_kv_batch_t* batch;
-  int32_t heads;         /* a multiple of kv_heads, 1..1024                     */
+  int32_t heads;         /* a multiple of kv_heads, 1..1024; tokens * heads /
+                            kv_heads < 2^30                                     */
   int32_t window;        /* >= 0; 0: none                                       */
   const int32_t* prefix; /* [requests]; NULL: none                              */
   void* plan;            /* spear_attention_sizes' plan_bytes                   */
@@ -207,8 +208,9 @@ spear_status_t spear_attention_sizes(const spear_attention_t* args, size_t* plan
 /* Writes the plan: which rows and stretches of the cache go to which workgroup,
  * from starts, lens, window and prefix. It serves every spear_attention whose
  * cache, batch, heads, window and prefix are the same in size and content (the
- * layers of a step), until one of them changes. Errors as for spear_attention; q,
- * out and the workspace are not looked at. */
+ * layers of a step), until one of them changes. Where sizes differ the attention
+ * writes nothing. Errors as for spear_attention; q, out and the workspace are not
+ * looked at. */
 spear_status_t spear_attention_plan(const spear_attention_t* args, void* hip_stream);
 
 /* Errors: SPEAR_E_NULL, SPEAR_E_DTYPE, SPEAR_E_SHAPE, SPEAR_E_ALIGN; SPEAR_E_WORKSPACE

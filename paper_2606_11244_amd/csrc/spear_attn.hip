@@ -4,84 +4,714 @@
 
 namespace spear {
 
-template <int FMT>
-__device__ __forceinline__ float code_value(uint8_t b) {
-  if constexpr (FMT == KV_INT8) return (float)(int8_t)b;
-  else return __builtin_amdgcn_cvt_f32_fp8((int)b, 0);
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLowest = -3.402823466e38f;  // running maximum of a row that has seen nothing
+
+#if !SPEAR_BF16_UNIT
+// ---------------------------------------------------------------------------
+// The plan. One workgroup: requests are told apart by their rows, all steps are
+// summed, and each request's (or tile's) steps are cut into stretches of equal
+// length near all steps / goal, so that workgroups have like shares whatever the
+// lengths; heavy tiles (late positions) come first. Latency, once for all layers.
+// ---------------------------------------------------------------------------
+constexpr int kPlanThreads = 1024;
+
+// sum over the workgroup before this thread, and in all
+__device__ __forceinline__ int64_t plan_scan(int64_t v, int64_t* red, int64_t* total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int64_t s = v;
+  for (int d = 1; d < 64; d <<= 1) {
+    const int64_t o = __shfl_up(s, d);
+    if (lane >= d) s += o;
+  }
+  __syncthreads();
+  if (lane == 63) red[wave] = s;
+  __syncthreads();
+  int64_t before = 0, all = 0;
+  for (int i = 0; i < (int)(blockDim.x >> 6); ++i) {
+    if (i < wave) before += red[i];
+    all += red[i];
+  }
+  *total = all;
+  return before + s - v;
 }
 
-// One wave a row and head: 64 tokens a step, a token a lane for the scores, then
-// two (or one) features a lane for the sum.
-template <int DT, int FMT, int D>
-__global__ __launch_bounds__(64) void k_kv_attend(KvAttendParams p) {
-  const int lane = threadIdx.x, h = blockIdx.x % p.H, t = blockIdx.x / p.H, hk = h / p.group;
-  if (t >= p.starts[p.R]) return;
-  int r = 0, hi = p.R;
-  while (hi - r > 1) {
-    const int mid = (r + hi) >> 1;
-    if (p.starts[mid] <= t) r = mid;
+__device__ __forceinline__ int plan_find(const int32_t* a, int n, int x) {
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (a[mid] <= x) lo = mid;
     else hi = mid;
   }
-  const int rows = p.starts[r + 1] - p.starts[r], i = t - p.starts[r];
-  if (i < 0 || i >= rows || i >= p.max_new) return;
-  const int len = (int)min((int64_t)p.lens[r], (int64_t)p.width * p.c.P), pos = p.lens[r] - rows + i;
-  const int first = p.prefix ? p.prefix[r] : 0;
-  const uint16_t* q = p.q + (int64_t)t * p.q_ld + h * D;
-  const float slope = p.slopes ? p.slopes[h] : 0.f;
-  float m = -__builtin_inff(), l = 0.f, o[D / 64] = {};
-  for (int j0 = 0; j0 < len; j0 += 64) {
-    const int j = j0 + lane;
-    bool seen = j < len && ((j <= pos && pos - j < p.window_tokens) || j < first);
-    int page = -1;
-    if (seen) page = p.table[r * p.ld + j / p.c.P];
-    seen = seen && page >= 0 && page < p.c.pages;
-    float s = -__builtin_inff(), vs = 0.f;
-    int64_t ph = 0;
-    if (seen) {
-      ph = (int64_t)page * p.c.Hkv + hk;
-      const uint8_t* k = p.c.k + (ph * p.c.P + j % p.c.P) * D;
-      float dot = 0.f;
-      for (int d = 0; d < D; ++d) dot += act2f<DT>(q[d]) * code_value<FMT>(k[d]);
-      s = dot * p.c.k_scale[ph] * p.scale;
-      if (p.softcap > 0.f) s = p.softcap * tanhf(s / p.softcap);
-      s -= slope * (float)abs(pos - j);
-      vs = p.c.v_scale[ph];
-    }
-    float top = s;
-    for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-    if (top == -__builtin_inff()) continue;
-    const float now = fmaxf(m, top), fade = m == now ? 1.f : expf(m - now);
-    const float e = seen ? expf(s - now) : 0.f;
-    m = now;
-    float sum = e;
-    for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
-    l = l * fade + sum;
-#pragma unroll
-    for (int c = 0; c < D / 64; ++c) o[c] *= fade;
-    for (int x = 0; x < 64; ++x) {
-      const float w = __shfl(e, x);
-      if (w == 0.f) continue;
-      const int64_t at = __shfl(ph, x);
-      const float sc = __shfl(vs, x);
-#pragma unroll
-      for (int c = 0; c < D / 64; ++c)
-        o[c] += w * sc * code_value<FMT>(p.c.v[(at * D + 64 * c + lane) * p.c.P + (j0 + x) % p.c.P]);
-    }
-  }
-#pragma unroll
-  for (int c = 0; c < D / 64; ++c)
-    p.out[(int64_t)t * p.out_ld + h * D + 64 * c + lane] = f2act<DT>(l > 0.f ? o[c] / l : 0.f);
+  return lo;
 }
 
-template <int FMT>
-static hipError_t attend_launch(const KvAttendParams& p, hipStream_t st) {
-  const dim3 grid((uint32_t)p.T * p.H);
-  if (p.c.D == 64) hipLaunchKernelGGL((k_kv_attend<DTC, FMT, 64>), grid, dim3(64), 0, st, p);
-  else hipLaunchKernelGGL((k_kv_attend<DTC, FMT, 128>), grid, dim3(64), 0, st, p);
+// request r: its rows and positions; whatever the arrays hold, rows lie within the step
+__device__ __forceinline__ AttnItem plan_request(const AttnPlanParams& p, int r) {
+  AttnItem it = {};
+  const int a = min(max(p.starts[r], 0), p.T), b = min(max(p.starts[r + 1], a), p.T);
+  const int len = max(p.lens[r], 0);
+  it.r = r;
+  it.row0 = a;
+  it.rows = min(b - a, p.max_new);
+  it.pos0 = len - (b - a);
+  it.end = p.pages ? (int)min(min((int64_t)len, (int64_t)p.width * p.P), (int64_t)kKvLength) : 0;  // (tokens that have a place)
+  it.prefix = p.prefix ? min(max(p.prefix[r], 0), it.end) : 0;
+  return it;
+}
+// the tokens and steps that rows i0..i1-1 of the request see; the steps' count
+__device__ __forceinline__ int plan_range(const AttnPlanParams& p, AttnItem& it, int i0, int i1) {
+  const int lo = it.pos0 + i0, hi = it.pos0 + i1;
+  it.first = max(0, min(lo, kKvLength) - p.window + 1);
+  it.end = min(it.end, max(min(hi, kKvLength), it.prefix));
+  it.s0 = it.prefix > 0 ? 0 : it.first / kStep;
+  it.s1 = max(it.s0, (it.end + kStep - 1) / kStep);
+  return it.s1 - it.s0;
+}
+__device__ __forceinline__ int plan_splits(int steps, int c) { return steps > c ? (steps + c - 1) / c : 1; }
+// stretch x of it's splits
+__device__ __forceinline__ AttnItem plan_stretch(AttnItem it, int splits, int x, int part) {
+  const int s0 = it.s0, n = it.s1 - it.s0;
+  it.splits = splits, it.split = x, it.part = part;
+  it.s0 = s0 + (int)((int64_t)n * x / splits);
+  it.s1 = s0 + (int)((int64_t)n * (x + 1) / splits);
+  return it;
+}
+
+__global__ __launch_bounds__(kPlanThreads) void k_attention_plan(AttnPlanParams p) {
+  __shared__ int32_t s_item[kKvRequests + 1], s_part[kKvRequests], s_tile[kKvRequests + 1];
+  __shared__ int64_t red[kPlanThreads / 64];
+  constexpr int kEach = kKvRequests / kPlanThreads;
+  const int tid = threadIdx.x, each = (p.R + blockDim.x - 1) / blockDim.x;
+  // requests: steps of those of few rows, tiles of the others
+  int steps[kEach], tiles[kEach];
+  int64_t sum = 0, tile_sum = 0, total, at;
+#pragma unroll
+  for (int e = 0; e < kEach; ++e) {
+    const int r = tid * each + e;
+    steps[e] = -1, tiles[e] = 0;
+    if (e >= each || r >= p.R) continue;
+    AttnItem it = plan_request(p, r);
+    if (it.rows == 0) continue;
+    const int64_t rows = (int64_t)it.rows * p.group;
+    if (rows <= kRows) sum += steps[e] = plan_range(p, it, 0, it.rows);
+    else tile_sum += tiles[e] = (int)((rows + kTileRows - 1) / kTileRows);
+  }
+  plan_scan(sum, red, &total);
+  const int c = max(p.z.least_rows, (int)((total + p.z.goal_rows - 1) / p.z.goal_rows));
+  int64_t items = 0, parts = 0, n_items, n_tiles;
+#pragma unroll
+  for (int e = 0; e < kEach; ++e)
+    if (steps[e] >= 0) {
+      const int k = plan_splits(steps[e], c);
+      items += k;
+      parts += k > 1 ? k : 0;
+    }
+  int64_t item_at = plan_scan(items, red, &n_items), part_at = plan_scan(parts, red, &total);
+  at = plan_scan(tile_sum, red, &n_tiles);
+  n_items = min(n_items, (int64_t)p.z.max_rows);
+  n_tiles = min(n_tiles, (int64_t)p.z.max_tile);
+#pragma unroll
+  for (int e = 0; e < kEach; ++e) {
+    const int r = tid * each + e;
+    if (e >= each || r >= p.R) continue;
+    s_item[r] = (int)min(item_at, n_items);
+    s_part[r] = (int)part_at;
+    s_tile[r] = (int)min(at, n_tiles);
+    at += tiles[e];
+    if (steps[e] >= 0) {
+      const int k = plan_splits(steps[e], c);
+      item_at += k;
+      part_at += k > 1 ? k : 0;
+    }
+  }
+  if (tid == 0) s_item[p.R] = (int)n_items, s_tile[p.R] = (int)n_tiles, p.head->n_rows = (int)n_items, p.head->key = p.key;
+  __syncthreads();
+  for (int i = tid; i < n_items; i += blockDim.x) {
+    const int r = plan_find(s_item, p.R, i), x = i - s_item[r];
+    AttnItem it = plan_request(p, r);
+    const int k = plan_splits(plan_range(p, it, 0, it.rows), c);
+    const bool room = s_part[r] + k <= p.z.part_rows;
+    if (k > 1 && !room) it.s1 = it.s0;  // (arrays that contradict themselves)
+    p.items_rows[i] = plan_stretch(it, k > 1 && !room ? 1 : k, k > 1 && !room ? 0 : x, s_part[r]);
+  }
+  // tiles, the last first
+  auto tile_of = [&](int t, AttnItem& it) {
+    const int r = plan_find(s_tile, p.R, t);
+    it = plan_request(p, r);
+    it.tile = t - s_tile[r];
+    const int i0 = it.tile * kTileRows / p.group;
+    return plan_range(p, it, i0, min(it.rows, (it.tile * kTileRows + kTileRows - 1) / p.group + 1));
+  };
+  if (n_tiles == 0) {
+    if (tid == 0) p.head->n_tile = 0;
+    return;
+  }
+  sum = 0;
+  AttnItem it;
+  for (int t = tid; t < n_tiles; t += blockDim.x) sum += tile_of(t, it);
+  plan_scan(sum, red, &total);
+  const int ct = max(p.z.least_tile, (int)((total + p.z.goal_tile - 1) / p.z.goal_tile));
+  int64_t base_item = 0, base_part = 0;
+  for (int t0 = 0; t0 < n_tiles; t0 += blockDim.x) {
+    const int t = (int)n_tiles - 1 - t0 - tid;
+    int k = 0;
+    if (t >= 0) k = plan_splits(tile_of(t, it), ct);
+    int64_t all_items, all_parts;
+    int64_t i = base_item + plan_scan(k, red, &all_items);
+    const int64_t part = base_part + plan_scan(k > 1 ? k : 0, red, &all_parts);
+    base_item += all_items, base_part += all_parts;
+    const bool room = k <= 1 || part + k <= p.z.part_tile;
+    if (!room) it.s1 = it.s0;
+    for (int x = 0; x < k && i < p.z.max_tile; ++x, ++i)
+      p.items_tile[i] = plan_stretch(it, room ? k : 1, room ? x : 0, (int)part);
+  }
+  if (tid == 0) p.head->n_tile = (int)min(base_item, (int64_t)p.z.max_tile);
+}
+
+hipError_t launch_attention_plan(const AttnPlanParams& p, hipStream_t st) {
+  const int64_t tiles = p.z.max_tile;
+  const int want = (int)std::min<int64_t>(kPlanThreads, std::max<int64_t>({p.R, p.z.max_rows, tiles}));
+  hipLaunchKernelGGL(k_attention_plan, dim3(1), dim3((want + 63) / 64 * 64), 0, st, p);
   return hipGetLastError();
 }
-hipError_t SPEAR_D(launch_kv_attend)(const KvAttendParams& p, int format, hipStream_t st) {
-  return format == KV_INT8 ? attend_launch<KV_INT8>(p, st) : attend_launch<KV_E4M3>(p, st);
+#endif
+
+// ---------------------------------------------------------------------------
+// Codes as operands: eight codes in the activation type. K's scale goes on the
+// fp32 score. V's goes on V (exact: a power of two; fp16 codes times a scale from
+// 2^-14 on, what is below on the weight) or, where a code of INT8 becomes bf16
+// and a product more would be a rounding and an instruction, on the weight.
+// ---------------------------------------------------------------------------
+typedef _Float16 h16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 b16x2 __attribute__((ext_vector_type(2)));
+
+template <int DT, int FMT>
+__device__ __forceinline__ u32x4 operand8(uint32_t w0, uint32_t w1, float scale) {
+  if constexpr (FMT == KV_E4M3) {
+    if constexpr (DT == DT_F16)
+      return u32x4{__builtin_bit_cast(uint32_t, (h16x2)__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w0, scale, false)),
+                   __builtin_bit_cast(uint32_t, (h16x2)__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w0, scale, true)),
+                   __builtin_bit_cast(uint32_t, (h16x2)__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w1, scale, false)),
+                   __builtin_bit_cast(uint32_t, (h16x2)__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w1, scale, true))};
+    else
+      return u32x4{__builtin_bit_cast(uint32_t, (b16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, scale, false)),
+                   __builtin_bit_cast(uint32_t, (b16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, scale, true)),
+                   __builtin_bit_cast(uint32_t, (b16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, scale, false)),
+                   __builtin_bit_cast(uint32_t, (b16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, scale, true))};
+  } else {
+    return i8x8_exact<DT>(w0, w1);
+  }
+}
+template <int DT, int FMT>
+__device__ __forceinline__ u32x4 v_operand8(uint32_t w0, uint32_t w1, float scale) {
+  u32x4 x = operand8<DT, FMT>(w0, w1, scale);
+  if constexpr (DT == DT_F16 && FMT == KV_INT8) {
+    const h16x2 s = h16x2{(_Float16)scale, (_Float16)scale};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t e = x[i];  // (a bit_cast of the element itself is taken as the first one's)
+      x[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(h16x2, e) * s);
+    }
+  }
+  return x;
+}
+// V's scale as (factor of V, factor of the weight)
+template <int DT, int FMT>
+__device__ __forceinline__ float2 v_factors(float s) {
+  if constexpr (DT == DT_F16) return make_float2(fmaxf(s, 6.103515625e-5f), fminf(s * 16384.f, 1.f));
+  else if constexpr (FMT == KV_INT8) return make_float2(1.f, s);
+  else return make_float2(s, 1.f);
+}
+
+template <int DT>
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+  if constexpr (DT == DT_F16)
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, h16x2));
+  else
+    return pack_bf16(a, b);
+}
+
+// A score in powers of two. OPT: capped, or biased by distance.
+struct ScoreOptions {
+  float scale, cap, slope2;  // slope2: slope times log2 e
+};
+template <bool OPT>
+__device__ __forceinline__ float score2(float dot, float k_scale, const ScoreOptions& o, int pos, int j) {
+  if constexpr (!OPT) return dot * (k_scale * (o.scale * kLog2e));
+  float t = dot * (k_scale * o.scale);
+  if (o.cap > 0.f) {  // cap tanh(t / cap) = cap (1 - 2 / (e^(2 t / cap) + 1))
+    const float e = __builtin_amdgcn_exp2f(t * (2.f * kLog2e / o.cap));
+    t = o.cap * (1.f - 2.f / (e + 1.f));
+  }
+  return t * kLog2e - o.slope2 * (float)abs(pos - j);
+}
+
+// which of the 16 tokens from j0 on some row of the item sees, as bytes of four dwords
+__device__ __forceinline__ u32x4 seen_bytes(int j0, const AttnItem& it) {
+  u32x4 m;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    uint32_t b = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int j = j0 + 4 * w + e;
+      b |= j < it.end && (j >= it.first || j < it.prefix) ? 0xFFu << (8 * e) : 0u;
+    }
+    m[w] = b;
+  }
+  return m;
+}
+
+// ---------------------------------------------------------------------------
+// At most 16 rows (decode): four waves, each a step of 64 tokens in turn, its
+// codes in registers and those of the next step in flight. S^T = K Q^T and
+// O^T = V^T P^T on 16 x 16 x 32 MFMAs: with the tokens as rows of S^T a lane holds
+// 16 scores of one row, of 16 tokens that lie side by side, so that the weights
+// are V's operand as they are, a page's scale is one number a lane, and K and V
+// come in pieces of 16 bytes. The waves' and then the stretches' results are
+// joined in order, the latter by the stretch that ends last.
+// Bound: the codes' bytes (long caches), latency (short ones).
+// ---------------------------------------------------------------------------
+template <int DT, int FMT, int D, bool OPT>
+__global__ __launch_bounds__(256, 2) void k_attend_rows(AttnParams p) {
+  constexpr int KS = D / 64, DTILES = D / 16, PITCH = D + 4;
+  __shared__ float s_o[4 * kRows * PITCH], s_m[4 * kRows], s_l[4 * kRows];
+  __shared__ int s_last;
+  const int head = blockIdx.x % p.c.Hkv, idx = blockIdx.x / p.c.Hkv;
+  if (p.head->key != p.key || idx >= p.head->n_rows) return;
+  AttnItem it = p.items_rows[idx];
+  if (p.c.pages == 0) it.s1 = it.s0;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, c = lane & 15, g = lane >> 4;
+  const int P = p.c.P, live_rows = it.rows * p.group;
+  const bool mine = c < live_rows;
+  const int i = mine ? c / p.group : 0, hq = head * p.group + (mine ? c % p.group : 0);
+  u32x4 q[2 * KS];
+  {
+    const uint16_t* qp = p.q + (int64_t)(it.row0 + i) * p.q_ld + hq * D + 16 * g;
+#pragma unroll
+    for (int s = 0; s < 2 * KS; ++s) q[s] = ldg16(qp + 64 * (s >> 1) + 8 * (s & 1));
+    if (!mine)
+#pragma unroll
+      for (int s = 0; s < 2 * KS; ++s) q[s] = u32x4{0, 0, 0, 0};
+  }
+  const int pos = it.pos0 + i, pos_max = it.pos0 + it.rows - 1;
+  const ScoreOptions opt{p.scale, p.softcap, OPT && p.slopes ? p.slopes[hq] * kLog2e : 0.f};
+  const int32_t* table = p.table + it.r * p.ld;
+  const int64_t page_bytes = (int64_t)P * D;
+
+  // the page of the run of 16 tokens that this lane reads of K (run c / 4) or of V (run g)
+  auto page_at = [&](int s, int run) {
+    const int j = s * kStep + 16 * run;
+    const int page = s < it.s1 && j < it.end ? table[j >> p.log2_page] : -1;
+    return page >= 0 && page < p.c.pages ? page : -1;
+  };
+  u32x4 kr[4][KS], vr[DTILES];
+  auto load_k = [&](int s, int page) {
+    const int at = (s * kStep + 16 * (c >> 2)) & (P - 1);
+    const uint8_t* k = p.c.k + ((int64_t)max(page, 0) * p.c.Hkv + head) * page_bytes + (at + (c & 3)) * D + 16 * g;
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int x = 0; x < KS; ++x) kr[t][x] = ldg16(k + t * 4 * D + 64 * x);
+  };
+  auto load_v = [&](int s, int page) {
+    const int at = (s * kStep + 16 * g) & (P - 1);
+    const uint8_t* v = p.c.v + ((int64_t)max(page, 0) * p.c.Hkv + head) * page_bytes + c * P + at;
+#pragma unroll
+    for (int d = 0; d < DTILES; ++d) vr[d] = ldg16(v + d * 16 * P);
+  };
+  auto scales = [&](int page) {
+    const int64_t ph = (int64_t)max(page, 0) * p.c.Hkv + head;
+    return make_float2(p.c.k_scale[ph], p.c.v_scale[ph]);
+  };
+
+  f32x4 o[DTILES] = {};
+  float m = kLowest, l = 0.f;
+  int s = it.s0 + wave;
+  if (s < it.s1) {
+    int page_v = page_at(s, g), next_k = page_at(s, c >> 2), next_v;
+    float2 sc = scales(page_v);
+    load_k(s, next_k);
+    load_v(s, page_v);
+    next_k = page_at(s + 4, c >> 2), next_v = page_at(s + 4, g);
+    for (; s < it.s1; s += 4) {
+      f32x4 st[4] = {};
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int x = 0; x < KS; ++x) {
+          st[t] = mfma16<DT>(operand8<DT, FMT>(kr[t][x][0], kr[t][x][1], 1.f), q[2 * x], st[t]);
+          st[t] = mfma16<DT>(operand8<DT, FMT>(kr[t][x][2], kr[t][x][3], 1.f), q[2 * x + 1], st[t]);
+        }
+      const bool more = s + 4 < it.s1;
+      if (more) load_k(s + 4, next_k);
+      const int j0 = s * kStep + 16 * g;
+      // every row sees every token of the step, all pages are there
+      const bool whole = s * kStep + kStep <= min(it.end, it.pos0 + 1) && pos_max - s * kStep < p.window &&
+                         __all(page_v >= 0);
+      float2 f = v_factors<DT, FMT>(sc.y);
+      float w[16];
+      if (whole) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) w[e] = score2<OPT>(st[e >> 2][e & 3], sc.x, opt, pos, j0 + e);
+      } else {
+        const u32x4 seen = page_v >= 0 ? seen_bytes(j0, it) : u32x4{0, 0, 0, 0};
+        if (!(seen[0] | seen[1] | seen[2] | seen[3])) f = make_float2(1.f, 1.f);
+#pragma unroll
+        for (int d = 0; d < DTILES; ++d) vr[d] &= seen;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int j = j0 + e;
+          const bool sees = ((seen[e >> 2] >> (8 * (e & 3))) & 1) && ((j <= pos && pos - j < p.window) || j < it.prefix);
+          w[e] = sees ? score2<OPT>(st[e >> 2][e & 3], sc.x, opt, pos, j) : -__builtin_inff();
+        }
+      }
+      float top = w[0];
+#pragma unroll
+      for (int e = 1; e < 16; ++e) top = fmaxf(top, w[e]);
+      top = fmaxf(top, __shfl_xor(top, 16));
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const float now = fmaxf(m, top), fade = __builtin_amdgcn_exp2f(m - now);
+      m = now;
+      float sum = 0.f;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        w[e] = __builtin_amdgcn_exp2f(w[e] - now);
+        sum += w[e];
+      }
+      l = l * fade + sum;
+      if (__any(fade != 1.f)) {
+#pragma unroll
+        for (int d = 0; d < DTILES; ++d) o[d] *= fade;
+      }
+      if ((DT != DT_F16 && FMT == KV_INT8) || (DT == DT_F16 && __any(f.y != 1.f))) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) w[e] *= f.y;
+      }
+      u32x4 pw[2];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) pw[e >> 2][e & 3] = pack2<DT>(w[2 * e], w[2 * e + 1]);
+#pragma unroll
+      for (int d = 0; d < DTILES; ++d) {
+        o[d] = mfma16<DT>(v_operand8<DT, FMT>(vr[d][0], vr[d][1], f.x), pw[0], o[d]);
+        o[d] = mfma16<DT>(v_operand8<DT, FMT>(vr[d][2], vr[d][3], f.x), pw[1], o[d]);
+      }
+      if (more) {
+        page_v = next_v;
+        load_v(s + 4, page_v);
+        sc = scales(page_v);
+        next_k = page_at(s + 8, c >> 2), next_v = page_at(s + 8, g);
+      }
+    }
+  }
+  l += __shfl_xor(l, 16);
+  l += __shfl_xor(l, 32);
+#pragma unroll
+  for (int d = 0; d < DTILES; ++d) *(f32x4*)&s_o[(wave * kRows + c) * PITCH + 16 * d + 4 * g] = o[d];
+  if (g == 0) s_m[wave * kRows + c] = m, s_l[wave * kRows + c] = l;
+  __syncthreads();
+  // a thread: row tid / 16, D / 16 features of it
+  constexpr int F = D / 16;
+  const int row = tid >> 4, d0 = (tid & 15) * F;
+  float top = s_m[row], x[F] = {}, total = 0.f;
+#pragma unroll
+  for (int v = 1; v < 4; ++v) top = fmaxf(top, s_m[v * kRows + row]);
+#pragma unroll
+  for (int v = 0; v < 4; ++v) {
+    const float f = __builtin_amdgcn_exp2f(s_m[v * kRows + row] - top);
+    total += f * s_l[v * kRows + row];
+#pragma unroll
+    for (int e = 0; e < F; ++e) x[e] += f * s_o[(v * kRows + row) * PITCH + d0 + e];
+  }
+  if (it.splits > 1) {
+    const uint32_t size = kRows * (D + 2) * 4, slot = (uint32_t)it.part * p.c.Hkv + head;
+    const rsrc_t r = make_rsrc((const char*)p.parts_rows + (size_t)slot * size, (uint32_t)((it.splits - 1) * p.c.Hkv + 1) * size);
+    const uint32_t at = (uint32_t)it.split * p.c.Hkv * size;
+#pragma unroll
+    for (int e = 0; e < F; e += 4) bst128c(r, at + (row * D + d0 + e) * 4, f32x4{x[e], x[e + 1], x[e + 2], x[e + 3]});
+    float* ml = p.parts_rows + ((size_t)slot * size + at) / 4 + kRows * D;
+    if ((tid & 15) == 0) st_agent(ml + row, top), st_agent(ml + kRows + row, total);
+    complete_and_sync();
+    if (tid == 0) s_last = arrive_last(p.counters + slot, it.splits);
+    __syncthreads();
+    if (!s_last) return;
+    // the stretches in order, four in flight
+    total = 0.f;
+    top = kLowest;
+#pragma unroll
+    for (int e = 0; e < F; ++e) x[e] = 0.f;
+    const uint32_t stride = p.c.Hkv * size, own = (row * D + d0) * 4, own_m = (kRows * D + row) * 4;
+    for (int b = 0; b < it.splits; b += 4) {
+      f32x4 v[4][F / 4];
+      float pm[4], pl[4];
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
+        const uint32_t off = b + y < it.splits ? (b + y) * stride : kOOB;
+        pm[y] = __uint_as_float(bld32c(r, off + own_m));
+        pl[y] = __uint_as_float(bld32c(r, off + own_m + kRows * 4));
+#pragma unroll
+        for (int e = 0; e < F / 4; ++e) v[y][e] = bld128cf(r, off + own + 16 * e);
+      }
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
+        if (b + y >= it.splits) continue;
+        const float now = fmaxf(top, pm[y]), f0 = __builtin_amdgcn_exp2f(top - now), f1 = __builtin_amdgcn_exp2f(pm[y] - now);
+        top = now;
+        total = total * f0 + pl[y] * f1;
+#pragma unroll
+        for (int e = 0; e < F; ++e) x[e] = x[e] * f0 + v[y][e >> 2][e & 3] * f1;
+      }
+    }
+  }
+  if (row >= live_rows) return;
+  const float inv = total > 0.f ? 1.f / total : 0.f;
+  uint16_t* out = p.out + (int64_t)(it.row0 + row / p.group) * p.out_ld + (head * p.group + row % p.group) * D + d0;
+#pragma unroll
+  for (int e = 0; e < F; e += 4) *(u32x2*)(out + e) = u32x2{pack2<DT>(x[e] * inv, x[e + 1] * inv), pack2<DT>(x[e + 2] * inv, x[e + 3] * inv)};
+}
+
+// ---------------------------------------------------------------------------
+// Tiles of 256 rows (prompts, chunks): eight waves of 32 rows. All waves bring a
+// step's codes to LDS as operands (each code converted once for 256 rows), two
+// steps in LDS and one in registers, and multiply on 32 x 32 x 16 MFMAs, again
+// S^T = K Q^T and O^T = V^T P^T: a lane holds half the scores of one row, and its
+// weights are V's operand once V's tokens stand in LDS in the order in which the
+// MFMA leaves the scores (the middle quads of every sixteen exchanged).
+// Bound: the MFMAs and the exponentials beside them.
+// ---------------------------------------------------------------------------
+template <int DT, int FMT, int D, bool OPT>
+__global__ __launch_bounds__(512) void k_attend_tile(AttnParams p) {
+  constexpr int KP = D * 2 + 16, VP = kStep * 2 + 16, PIECES = D / 16;  // pitches in bytes; pieces of a row of K
+  constexpr int KBYTES = kStep * KP, BUF = KBYTES + D * VP;
+  __shared__ __attribute__((aligned(16))) char lds[2 * BUF];
+  __shared__ float s_ks[2][4], s_vf[2][4];
+  __shared__ int s_last;
+  const int head = blockIdx.x % p.c.Hkv, idx = blockIdx.x / p.c.Hkv;
+  if (p.head->key != p.key || idx >= p.head->n_tile) return;
+  AttnItem it = p.items_tile[idx];
+  if (p.c.pages == 0) it.s1 = it.s0;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, c = lane & 31, h = lane >> 5;
+  const int P = p.c.P, live_rows = it.rows * p.group, wave_row = it.tile * kTileRows + 32 * wave;
+  const int row = wave_row + c;
+  const bool active = wave_row < live_rows, mine = row < live_rows;
+  const int i = mine ? row / p.group : it.rows - 1, hq = head * p.group + (mine ? row % p.group : 0);
+  u32x4 q[D / 16];
+  {
+    const uint16_t* qp = p.q + (int64_t)(it.row0 + i) * p.q_ld + hq * D + 8 * h;
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) q[s] = ldg16(qp + 16 * s);
+    if (!mine)
+#pragma unroll
+      for (int s = 0; s < D / 16; ++s) q[s] = u32x4{0, 0, 0, 0};
+  }
+  const int pos = it.pos0 + i;
+  // positions of the wave's first and last row
+  const int pos_lo = it.pos0 + min(wave_row / p.group, it.rows - 1), pos_hi = it.pos0 + min((wave_row + 31) / p.group, it.rows - 1);
+  const ScoreOptions opt{p.scale, p.softcap, OPT && p.slopes ? p.slopes[hq] * kLog2e : 0.f};
+  const int32_t* table = p.table + it.r * p.ld;
+  const int64_t page_bytes = (int64_t)P * D;
+
+  // staging: K by threads of (token, piece), V by threads of (feature, run); D = 64
+  // has half as many pieces, K's in the first half of the workgroup, V's in the other
+  const bool does_k = D == 128 || tid < 256, does_v = D == 128 || tid >= 256;
+  const int k_token = (tid / PIECES) & 63, k_piece = tid % PIECES, v_feature = (tid >> 2) % D, v_run = tid & 3;
+  auto page_at = [&](int s, int run) {
+    const int j = s * kStep + 16 * run;
+    const int page = s < it.s1 && j < it.end ? table[j >> p.log2_page] : -1;
+    return page >= 0 && page < p.c.pages ? page : -1;
+  };
+  u32x4 kr, vr;
+  float2 sc;  // scales of this thread's run of V
+  int page_k = 0, page_v = 0, held_v = 0;
+  auto fetch = [&](int s) {  // pages of s are in page_k, page_v; those of s + 1 follow
+    if (does_k)
+      kr = ldg16(p.c.k + ((int64_t)max(page_k, 0) * p.c.Hkv + head) * page_bytes + ((s * kStep + k_token) & (P - 1)) * D + 16 * k_piece);
+    if (does_v)
+      vr = ldg16(p.c.v + ((int64_t)max(page_v, 0) * p.c.Hkv + head) * page_bytes + v_feature * P + ((s * kStep + 16 * v_run) & (P - 1)));
+    const int64_t ph = (int64_t)max(page_v, 0) * p.c.Hkv + head;
+    sc = make_float2(p.c.k_scale[ph], p.c.v_scale[ph]);
+    held_v = page_v;
+    page_k = page_at(s + 1, k_token >> 4), page_v = page_at(s + 1, v_run);
+  };
+  auto stage = [&](int s) {
+    char* buf = lds + (s & 1) * BUF;
+    if (does_k) {
+      u32x4* k = (u32x4*)(buf + k_token * KP + 32 * k_piece);
+      k[0] = operand8<DT, FMT>(kr[0], kr[1], 1.f);
+      k[1] = operand8<DT, FMT>(kr[2], kr[3], 1.f);
+    }
+    float2 f = make_float2(sc.y, 1.f);
+    if constexpr (DT == DT_F16) f = v_factors<DT, FMT>(sc.y);
+    const int j0 = s * kStep + 16 * v_run;
+    if (held_v < 0 || j0 + 16 > it.end || j0 < it.first) {
+      const u32x4 seen = held_v >= 0 ? seen_bytes(j0, it) : u32x4{0, 0, 0, 0};
+      vr &= seen;
+      if (!(seen[0] | seen[1] | seen[2] | seen[3])) f = make_float2(1.f, 1.f);
+    }
+    if (does_v) {
+      u32x4* v = (u32x4*)(buf + KBYTES + v_feature * VP + 32 * v_run);
+      u32x4 a, b;
+      if constexpr (DT != DT_F16 && FMT == KV_INT8) {
+        a = i8x8_to_act<DT>(vr[0], vr[2], f.x), b = i8x8_to_act<DT>(vr[1], vr[3], f.x);
+      } else {
+        a = v_operand8<DT, FMT>(vr[0], vr[2], f.x), b = v_operand8<DT, FMT>(vr[1], vr[3], f.x);
+      }
+      v[0] = a, v[1] = b;
+    }
+    if (tid >= 256 && tid < 260) {  // (runs 0..3) no page: a scale that is no number, for the waves to see
+      s_ks[s & 1][v_run] = held_v >= 0 ? sc.x : __builtin_nanf("");
+      s_vf[s & 1][v_run] = f.y;
+    }
+  };
+
+  f32x16 o[D / 32] = {};
+  float m = kLowest, l = 0.f;
+  if (it.s0 < it.s1) {
+    page_k = page_at(it.s0, k_token >> 4), page_v = page_at(it.s0, v_run);
+    fetch(it.s0);
+    stage(it.s0);
+    if (it.s0 + 1 < it.s1) fetch(it.s0 + 1);
+    __syncthreads();
+  }
+  for (int s = it.s0; s < it.s1; ++s) {
+    // (the other buffer's readers have passed the last barrier)
+    if (s + 1 < it.s1) {
+      stage(s + 1);
+      if (s + 2 < it.s1) fetch(s + 2);
+    }
+    const int j0 = s * kStep;
+    const bool sees_any = active && ((j0 <= pos_hi && j0 + kStep > pos_lo - p.window + 1) || j0 < it.prefix);
+    if (sees_any) {
+      const char* buf = lds + (s & 1) * BUF;
+      f32x16 st[2] = {};
+#pragma unroll
+      for (int x = 0; x < D / 16; ++x)
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+          st[t] = mfma32<DT>(*(const u32x4*)(buf + (32 * t + c) * KP + 32 * x + 16 * h), q[x], st[t]);
+      float ks[4], vf[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) ks[r] = s_ks[s & 1][r], vf[r] = s_vf[s & 1][r];
+      const bool pages_there = ks[0] == ks[0] && ks[1] == ks[1] && ks[2] == ks[2] && ks[3] == ks[3];
+      const bool whole = j0 + kStep <= min(it.end, pos_lo + 1) && pos_hi - j0 < p.window && pages_there;
+      float w[2][16];
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int run = 2 * t + (e >> 3), j = j0 + 32 * t + 8 * (e >> 2) + 4 * h + (e & 3);
+          w[t][e] = score2<OPT>(st[t][e], ks[run], opt, pos, j);
+          if (!whole) {
+            const bool sees = j < it.end && ((j <= pos && pos - j < p.window) || j < it.prefix) && ks[run] == ks[run];
+            w[t][e] = sees ? w[t][e] : -__builtin_inff();
+          }
+        }
+      float top = w[0][0];
+#pragma unroll
+      for (int e = 1; e < 32; ++e) top = fmaxf(top, w[e >> 4][e & 15]);
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const float now = fmaxf(m, top), fade = __builtin_amdgcn_exp2f(m - now);
+      m = now;
+      float sum = 0.f;
+#pragma unroll
+      for (int e = 0; e < 32; ++e) {
+        float& x = w[e >> 4][e & 15];
+        x = __builtin_amdgcn_exp2f(x - now);
+        sum += x;
+      }
+      l = l * fade + sum;
+      if (__any(fade != 1.f)) {
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d) o[d] *= fade;
+      }
+      if (DT == DT_F16 && !(vf[0] == 1.f && vf[1] == 1.f && vf[2] == 1.f && vf[3] == 1.f)) {
+#pragma unroll
+        for (int e = 0; e < 32; ++e) w[e >> 4][e & 15] *= vf[e >> 3];
+      }
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {  // sixteen tokens
+        u32x4 pw;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) pw[e] = pack2<DT>(w[y >> 1][8 * (y & 1) + 2 * e], w[y >> 1][8 * (y & 1) + 2 * e + 1]);
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d)
+          o[d] = mfma32<DT>(*(const u32x4*)(buf + KBYTES + (32 * d + c) * VP + 32 * y + 16 * h), pw, o[d]);
+      }
+    }
+    __syncthreads();
+  }
+  l += __shfl_xor(l, 32);
+  if (it.splits > 1) {
+    const uint32_t size = kTileRows * (D + 2) * 4, slot = (uint32_t)it.part * p.c.Hkv + head;
+    const rsrc_t r = make_rsrc((const char*)p.parts_tile + (size_t)slot * size, (uint32_t)((it.splits - 1) * p.c.Hkv + 1) * size);
+    const uint32_t at = (uint32_t)it.split * p.c.Hkv * size, own = ((32 * wave + c) * D + 4 * h) * 4;
+    const uint32_t own_m = (kTileRows * D + 32 * wave + c) * 4;
+    if (active) {
+#pragma unroll
+      for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+          bst128c(r, at + own + (32 * d + 8 * x) * 4, f32x4{o[d][4 * x], o[d][4 * x + 1], o[d][4 * x + 2], o[d][4 * x + 3]});
+      float* ml = p.parts_tile + ((size_t)slot * size + at + own_m) / 4;
+      if (h == 0) st_agent(ml, m), st_agent(ml + kTileRows, l);
+    }
+    complete_and_sync();
+    if (tid == 0) s_last = arrive_last(p.counters + (size_t)p.z.part_rows * p.c.Hkv + slot, it.splits);
+    __syncthreads();
+    if (!s_last) return;
+    if (active) {
+      m = kLowest, l = 0.f;
+#pragma unroll
+      for (int d = 0; d < D / 32; ++d) o[d] = f32x16{};
+      for (int b = 0; b < it.splits; ++b) {
+        const uint32_t off = b * p.c.Hkv * size;
+        const float pm = __uint_as_float(bld32c(r, off + own_m)), pl = __uint_as_float(bld32c(r, off + own_m + kTileRows * 4));
+        const float now = fmaxf(m, pm), f0 = __builtin_amdgcn_exp2f(m - now), f1 = __builtin_amdgcn_exp2f(pm - now);
+        m = now;
+        l = l * f0 + pl * f1;
+        f32x4 v[D / 8];
+#pragma unroll
+        for (int x = 0; x < D / 8; ++x) v[x] = bld128cf(r, off + own + 8 * x * 4);
+#pragma unroll
+        for (int x = 0; x < D / 8; ++x)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[x >> 2][4 * (x & 3) + e] = o[x >> 2][4 * (x & 3) + e] * f0 + v[x][e] * f1;
+      }
+    }
+  }
+  if (!mine) return;
+  const float inv = l > 0.f ? 1.f / l : 0.f;
+  uint16_t* out = p.out + (int64_t)(it.row0 + i) * p.out_ld + hq * D + 4 * h;
+#pragma unroll
+  for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+      *(u32x2*)(out + 32 * d + 8 * x) = u32x2{pack2<DT>(o[d][4 * x] * inv, o[d][4 * x + 1] * inv),
+                                              pack2<DT>(o[d][4 * x + 2] * inv, o[d][4 * x + 3] * inv)};
+}
+
+template <int FMT, int D>
+static hipError_t rows_launch(const AttnParams& p, hipStream_t st) {
+  const dim3 grid((uint32_t)p.z.max_rows * p.c.Hkv);
+  if (p.slopes || p.softcap > 0.f) hipLaunchKernelGGL((k_attend_rows<DTC, FMT, D, true>), grid, dim3(256), 0, st, p);
+  else hipLaunchKernelGGL((k_attend_rows<DTC, FMT, D, false>), grid, dim3(256), 0, st, p);
+  return hipGetLastError();
+}
+template <int FMT, int D>
+static hipError_t tile_launch(const AttnParams& p, hipStream_t st) {
+  const dim3 grid((uint32_t)p.z.max_tile * p.c.Hkv);
+  if (p.slopes || p.softcap > 0.f) hipLaunchKernelGGL((k_attend_tile<DTC, FMT, D, true>), grid, dim3(512), 0, st, p);
+  else hipLaunchKernelGGL((k_attend_tile<DTC, FMT, D, false>), grid, dim3(512), 0, st, p);
+  return hipGetLastError();
+}
+hipError_t SPEAR_D(launch_attend_rows)(const AttnParams& p, int format, hipStream_t st) {
+  if (p.c.D == 64) return format == KV_INT8 ? rows_launch<KV_INT8, 64>(p, st) : rows_launch<KV_E4M3, 64>(p, st);
+  return format == KV_INT8 ? rows_launch<KV_INT8, 128>(p, st) : rows_launch<KV_E4M3, 128>(p, st);
+}
+hipError_t SPEAR_D(launch_attend_tile)(const AttnParams& p, int format, hipStream_t st) {
+  if (p.c.D == 64) return format == KV_INT8 ? tile_launch<KV_INT8, 64>(p, st) : tile_launch<KV_E4M3, 64>(p, st);
+  return format == KV_INT8 ? tile_launch<KV_INT8, 128>(p, st) : tile_launch<KV_E4M3, 128>(p, st);
 }
 
 }  // namespace spear

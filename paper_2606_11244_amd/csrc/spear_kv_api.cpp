@@ -214,11 +214,61 @@ spear_status_t check_attention(const spear_attention_t* a, bool buffers) {
   spear_status_t st = check_cache(a->cache, buffers);
   if (st == SPEAR_OK) st = check_batch(a->batch, buffers);
   if (st != SPEAR_OK) return st;
-  if (a->heads < 1 || a->heads > 1024 || a->heads % a->cache->kv_heads || a->window < 0) return SPEAR_E_SHAPE;
+  if (a->heads < 1 || a->heads > 1024 || a->heads % a->cache->kv_heads || a->window < 0 ||
+      (int64_t)a->batch->tokens * (a->heads / a->cache->kv_heads) >= (1 << 30))
+    return SPEAR_E_SHAPE;
   if (!buffers) return SPEAR_OK;
   if (!a->plan) return SPEAR_E_NULL;
   if (off16(a->plan) || off4(a->prefix)) return SPEAR_E_ALIGN;
   return SPEAR_OK;
+}
+
+
+// Stretches wanted of each kernel, over all kv heads, and a stretch's least steps.
+constexpr int kRowsGoal = 512, kRowsLeast = 4, kTileGoal = 256, kTileLeast = 8;
+
+// Where the plan's and the workspace's parts lie, from sizes alone.
+struct AttnLayout {
+  AttnShape z;
+  size_t items_rows, items_tile, plan_bytes;
+  size_t parts_rows, parts_tile, work_bytes;
+};
+// the sizes that a plan and the calls it serves have in common, as one number
+uint64_t plan_key(const spear_attention_t* a) {
+  const spear_kv_cache_t* c = a->cache;
+  const spear_kv_batch_t* b = a->batch;
+  uint64_t h = 0xcbf29ce484222325ull;
+  for (const int64_t v : {(int64_t)c->kv_heads, (int64_t)c->page_tokens, (int64_t)b->requests, (int64_t)b->tokens,
+                          (int64_t)b->max_new, (int64_t)b->width, (int64_t)a->heads, (int64_t)a->window,
+                          (int64_t)(a->prefix != nullptr)})
+    for (int i = 0; i < 32; i += 8) h = (h ^ ((v >> i) & 255)) * 0x100000001b3ull;
+  return h;
+}
+AttnLayout attention_layout(const spear_attention_t* a) {
+  const spear_kv_cache_t* c = a->cache;
+  const spear_kv_batch_t* b = a->batch;
+  const int64_t hkv = c->kv_heads, group = a->heads / c->kv_heads, T = b->tokens, R = b->requests;
+  const int64_t served = std::min(R, T);  // requests with a row
+  const bool rows = group <= kRows, tile = (int64_t)b->max_new * group > kRows;
+  AttnLayout l;
+  AttnShape& z = l.z;
+  z.goal_rows = (int)((kRowsGoal + hkv - 1) / hkv);
+  z.goal_tile = (int)((kTileGoal + hkv - 1) / hkv);
+  z.least_rows = kRowsLeast, z.least_tile = kTileLeast;
+  // sum over tiles of max(1, ceil(steps / c)) with c >= all steps / goal
+  z.max_rows = rows ? (int)served + z.goal_rows : 0;
+  z.max_tile = tile ? (int)(T * group / kTileRows + served) + z.goal_tile : 0;
+  // and over those of more than one, ceil(steps / c) <= 2 steps / c
+  z.part_rows = rows && z.goal_rows > 1 ? 2 * z.goal_rows : 0;
+  z.part_tile = tile && z.goal_tile > 1 ? 2 * z.goal_tile : 0;
+  l.items_rows = sizeof(AttnHeader);
+  l.items_tile = l.items_rows + (size_t)z.max_rows * sizeof(AttnItem);
+  l.plan_bytes = l.items_tile + (size_t)z.max_tile * sizeof(AttnItem);
+  const size_t counters = ((size_t)(z.part_rows + z.part_tile) * hkv * 4 + 255) / 256 * 256;
+  l.parts_rows = counters;
+  l.parts_tile = l.parts_rows + (size_t)z.part_rows * hkv * kRows * (c->head_dim + 2) * 4;
+  l.work_bytes = std::max<size_t>(256, l.parts_tile + (size_t)z.part_tile * hkv * kTileRows * (c->head_dim + 2) * 4);
+  return l;
 }
 
 }  // namespace
@@ -227,17 +277,35 @@ spear_status_t spear_attention_sizes(const spear_attention_t* a, size_t* plan_by
   if (!a || !plan_bytes || !workspace_bytes) return SPEAR_E_NULL;
   const spear_status_t st = check_attention(a, false);
   if (st != SPEAR_OK) return st;
-  *plan_bytes = 256;
-  *workspace_bytes = 256;
+  const AttnLayout l = attention_layout(a);
+  *plan_bytes = l.plan_bytes;
+  *workspace_bytes = l.work_bytes;
   return SPEAR_OK;
 }
 
-spear_status_t spear_attention_plan(const spear_attention_t* a, void*) {
+spear_status_t spear_attention_plan(const spear_attention_t* a, void* hip_stream) {
   const spear_status_t st = check_attention(a, true);
   if (st != SPEAR_OK) return st;
-  size_t plan = 0, work = 0;
-  spear_attention_sizes(a, &plan, &work);
-  return a->plan_bytes < plan ? SPEAR_E_WORKSPACE : SPEAR_OK;
+  const spear_kv_cache_t* c = a->cache;
+  const spear_kv_batch_t* b = a->batch;
+  const AttnLayout l = attention_layout(a);
+  if (a->plan_bytes < l.plan_bytes) return SPEAR_E_WORKSPACE;
+  const size_t R = b->requests;
+  const Span outs[] = {{a->plan, l.plan_bytes}};
+  const Span ins[] = {{b->starts, (R + 1) * 4}, {b->lens, R * 4}, {b->table, table_bytes(b)}, {a->prefix, R * 4}};
+  if (clash(outs, 1, ins, 4)) return SPEAR_E_ALIAS;
+  if (b->tokens == 0 || R == 0) return SPEAR_OK;
+  AttnPlanParams p;
+  p.R = b->requests, p.T = b->tokens, p.P = c->page_tokens, p.Hkv = c->kv_heads, p.group = a->heads / c->kv_heads;
+  p.max_new = b->max_new, p.width = b->width, p.window = a->window ? std::min(a->window, kKvLength) : kKvLength;
+  p.pages = (int)c->pages;
+  p.key = plan_key(a);
+  p.starts = b->starts, p.lens = b->lens, p.prefix = a->prefix;
+  p.z = l.z;
+  p.head = (AttnHeader*)a->plan;
+  p.items_rows = (AttnItem*)((char*)a->plan + l.items_rows);
+  p.items_tile = (AttnItem*)((char*)a->plan + l.items_tile);
+  return hip_status(launch_attention_plan(p, (hipStream_t)hip_stream));
 }
 
 spear_status_t spear_attention(const spear_attention_t* a, void* hip_stream) {
@@ -250,28 +318,41 @@ spear_status_t spear_attention(const spear_attention_t* a, void* hip_stream) {
   if (ql < row || ol < row || ql % 8 || ol % 8 || ql >= ((int64_t)1 << 30) || ol >= ((int64_t)1 << 30) ||
       !std::isfinite(a->scale) || !std::isfinite(a->softcap) || a->softcap < 0.f)
     return SPEAR_E_SHAPE;
+  const AttnLayout l = attention_layout(a);
+  if (a->plan_bytes < l.plan_bytes) return SPEAR_E_WORKSPACE;
   if (T == 0 || b->requests == 0) return SPEAR_OK;
   if (!a->q || !a->out) return SPEAR_E_NULL;
   if (off16(a->q) || off16(a->out) || off4(a->slopes) || off16(a->workspace)) return SPEAR_E_ALIGN;
-  size_t plan = 0, work = 0;
-  spear_attention_sizes(a, &plan, &work);
-  if (a->plan_bytes < plan || a->workspace_bytes < work || !a->workspace) return SPEAR_E_WORKSPACE;
+  if (a->workspace_bytes < l.work_bytes || !a->workspace) return SPEAR_E_WORKSPACE;
   const size_t R = b->requests;
-  const Span outs[] = {rows_of(a->out, T, ol, row), {a->workspace, work}};
+  const Span outs[] = {rows_of(a->out, T, ol, row), {a->workspace, l.work_bytes}};
   Span ins[11];
   cache_spans(c, reinterpret_cast<Span(&)[4]>(ins));
   ins[4] = {b->starts, (R + 1) * 4}, ins[5] = {b->lens, R * 4}, ins[6] = {b->table, table_bytes(b)};
-  ins[7] = {a->prefix, R * 4}, ins[8] = {a->slopes, (size_t)a->heads * 4}, ins[9] = {a->plan, plan};
+  ins[7] = {a->prefix, R * 4}, ins[8] = {a->slopes, (size_t)a->heads * 4}, ins[9] = {a->plan, l.plan_bytes};
   ins[10] = rows_of(a->q, T, ql, row);
   if (clash(outs, 2, ins, 11)) return SPEAR_E_ALIAS;
-  KvAttendParams p;
+  AttnParams p;
   p.c = cache_of(c);
-  p.R = b->requests, p.T = b->tokens, p.H = a->heads, p.group = a->heads / c->kv_heads;
-  p.max_new = b->max_new, p.width = b->width, p.window_tokens = a->window ? a->window : kKvLength;
+  p.group = a->heads / c->kv_heads;
+  p.window = a->window ? std::min(a->window, kKvLength) : kKvLength;
+  p.key = plan_key(a);
+  p.log2_page = __builtin_ctz((unsigned)c->page_tokens);
   p.ld = table_ld(b), p.q_ld = ql, p.out_ld = ol;
-  p.starts = b->starts, p.lens = b->lens, p.table = b->table, p.prefix = a->prefix;
+  p.table = b->table;
   p.q = (const uint16_t*)a->q, p.out = (uint16_t*)a->out;
   p.slopes = a->slopes, p.scale = a->scale, p.softcap = a->softcap;
-  const auto launch = c->act_dtype == SPEAR_F16 ? launch_kv_attend_f16 : launch_kv_attend_bf16;
-  return hip_status(launch(p, c->format, (hipStream_t)hip_stream));
+  p.z = l.z;
+  p.head = (const AttnHeader*)a->plan;
+  p.items_rows = (const AttnItem*)((const char*)a->plan + l.items_rows);
+  p.items_tile = (const AttnItem*)((const char*)a->plan + l.items_tile);
+  p.counters = (uint32_t*)a->workspace;
+  p.parts_rows = (float*)((char*)a->workspace + l.parts_rows);
+  p.parts_tile = (float*)((char*)a->workspace + l.parts_tile);
+  const bool f16 = c->act_dtype == SPEAR_F16;
+  hipError_t e = hipSuccess;
+  if (l.z.max_tile) e = (f16 ? launch_attend_tile_f16 : launch_attend_tile_bf16)(p, c->format, (hipStream_t)hip_stream);
+  if (e == hipSuccess && l.z.max_rows)
+    e = (f16 ? launch_attend_rows_f16 : launch_attend_rows_bf16)(p, c->format, (hipStream_t)hip_stream);
+  return hip_status(e);
 }

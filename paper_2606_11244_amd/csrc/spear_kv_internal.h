@@ -52,22 +52,67 @@ struct KvReadParams {
   uint16_t *k_out, *v_out;
 };
 
-struct KvAttendParams {
+// ---- attention ----
+// A request's rows (its new tokens, each with the query heads of one kv head) go
+// to k_attend_rows where they are at most kRows, else to k_attend_tile in tiles of
+// kTileRows. Either walks the cache in steps of kStep tokens.
+constexpr int kRows = 16, kTileRows = 256, kStep = 64;
+
+// one workgroup's share (of each kv head): some rows over some steps
+struct AttnItem {
+  int32_t r, row0, rows, pos0;    // request, its first row of the step, its rows, position of the first
+  int32_t tile, s0, s1, splits;   // tile of its rows; steps; stretches the tile's steps are cut into
+  int32_t split, part, first, end;  // which; the first one's place among the partial results (splits > 1);
+                                  // tokens some row sees: first..end-1 and 0..prefix-1
+  int32_t prefix, pad[3];
+};
+struct AttnHeader {
+  uint64_t key;            // of the sizes that it was made for: a call of others does nothing
+  int32_t n_rows, n_tile;  // items of each kernel
+  int32_t pad[12];
+};
+
+// sizes that the host fixes from the batch's and the heads' sizes alone
+struct AttnShape {
+  int goal_rows, goal_tile;    // stretches wanted: enough workgroups to fill the GPU
+  int least_rows, least_tile;  // least steps of a stretch
+  int max_rows, max_tile;      // items there can be
+  int part_rows, part_tile;    // partial results there can be, a kv head
+};
+
+struct AttnPlanParams {
+  int R, T, P, Hkv, group, max_new, width, window, pages;
+  uint64_t key;
+  const int32_t *starts, *lens, *prefix;
+  AttnShape z;
+  AttnHeader* head;
+  AttnItem *items_rows, *items_tile;
+};
+
+struct AttnParams {
   KvCache c;
-  int R, T, H, group, max_new, width, window_tokens;  // window_tokens: kKvLength: none
+  int group, window, log2_page;  // window: kKvLength for none
+  uint64_t key;
   int64_t ld, q_ld, out_ld;
-  const int32_t *starts, *lens, *table, *prefix;
+  const int32_t* table;
   const uint16_t* q;
   uint16_t* out;
   const float* slopes;
   float scale, softcap;
+  AttnShape z;
+  const AttnHeader* head;
+  const AttnItem *items_rows, *items_tile;
+  uint32_t* counters;            // [part_rows + part_tile][Hkv]
+  float *parts_rows, *parts_tile;  // [part][Hkv][rows of O, their maxima, their sums]
 };
 
+hipError_t launch_attention_plan(const AttnPlanParams& p, hipStream_t st);
 hipError_t launch_kv_pages(const KvPagesParams& p, hipStream_t st);
 #define SPEAR_KV_LAUNCHERS(D)                                                      \
   hipError_t launch_kv_append_##D(const KvAppendParams& p, int format, hipStream_t st); \
   hipError_t launch_kv_read_##D(const KvReadParams& p, int format, hipStream_t st); \
-  hipError_t launch_kv_attend_##D(const KvAttendParams& p, int format, hipStream_t st);
+  hipError_t launch_attend_rows_##D(const AttnParams& p, int format, hipStream_t st); \
+  hipError_t launch_attend_tile_##D(const AttnParams& p, int format, hipStream_t st);
 SPEAR_KV_LAUNCHERS(f16)
 SPEAR_KV_LAUNCHERS(bf16)
 #undef SPEAR_KV_LAUNCHERS
