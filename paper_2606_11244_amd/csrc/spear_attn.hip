@@ -6,6 +6,9 @@ namespace spear {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLowest = -3.402823466e38f;  // running maximum of a row that has seen nothing
+// How far scores may pass a row's maximum, in powers of two, before it is moved and
+// what was summed is scaled: weights up to 2^8 keep their precision in either type.
+constexpr float kSlack = 8.f;
 
 #if !SPEAR_BF16_UNIT
 // ---------------------------------------------------------------------------
@@ -14,7 +17,7 @@ constexpr float kLowest = -3.402823466e38f;  // running maximum of a row that ha
 // length near all steps / goal, so that workgroups have like shares whatever the
 // lengths; heavy tiles (late positions) come first. Latency, once for all layers.
 // ---------------------------------------------------------------------------
-constexpr int kPlanThreads = 1024;
+constexpr int kPlanThreads = 1024, kSizes = 32;
 
 // sum over the workgroup before this thread, and in all
 __device__ __forceinline__ int64_t plan_scan(int64_t v, int64_t* red, int64_t* total) {
@@ -49,6 +52,7 @@ __device__ __forceinline__ int plan_find(const int32_t* a, int n, int x) {
 // request r: its rows and positions; whatever the arrays hold, rows lie within the step
 __device__ __forceinline__ AttnItem plan_request(const AttnPlanParams& p, int r) {
   AttnItem it = {};
+  it.key = p.key;
   const int a = min(max(p.starts[r], 0), p.T), b = min(max(p.starts[r + 1], a), p.T);
   const int len = max(p.lens[r], 0);
   it.r = r;
@@ -81,6 +85,7 @@ __device__ __forceinline__ AttnItem plan_stretch(AttnItem it, int splits, int x,
 __global__ __launch_bounds__(kPlanThreads) void k_attention_plan(AttnPlanParams p) {
   __shared__ int32_t s_item[kKvRequests + 1], s_part[kKvRequests], s_tile[kKvRequests + 1];
   __shared__ int64_t red[kPlanThreads / 64];
+  __shared__ int s_size[kSizes];
   constexpr int kEach = kKvRequests / kPlanThreads;
   const int tid = threadIdx.x, each = (p.R + blockDim.x - 1) / blockDim.x;
   // requests: steps of those of few rows, tiles of the others
@@ -125,16 +130,40 @@ __global__ __launch_bounds__(kPlanThreads) void k_attention_plan(AttnPlanParams 
       part_at += k > 1 ? k : 0;
     }
   }
-  if (tid == 0) s_item[p.R] = (int)n_items, s_tile[p.R] = (int)n_tiles, p.head->n_rows = (int)n_items, p.head->key = p.key;
+  if (tid == 0) s_item[p.R] = (int)n_items, s_tile[p.R] = (int)n_tiles;
+  if (tid < kSizes) s_size[tid] = 0;
   __syncthreads();
-  for (int i = tid; i < n_items; i += blockDim.x) {
+  // Long stretches first: by size in kSizes classes (where one stands in its class is
+  // left to chance, and makes no difference to what is computed).
+  auto stretch = [&](int i, int* size) {
     const int r = plan_find(s_item, p.R, i), x = i - s_item[r];
     AttnItem it = plan_request(p, r);
-    const int k = plan_splits(plan_range(p, it, 0, it.rows), c);
-    const bool room = s_part[r] + k <= p.z.part_rows;
-    if (k > 1 && !room) it.s1 = it.s0;  // (arrays that contradict themselves)
-    p.items_rows[i] = plan_stretch(it, k > 1 && !room ? 1 : k, k > 1 && !room ? 0 : x, s_part[r]);
+    int k = plan_splits(plan_range(p, it, 0, it.rows), c);
+    if (k > 1 && s_part[r] + k > p.z.part_rows) it.s1 = it.s0, k = 1;  // (arrays that contradict themselves)
+    it = plan_stretch(it, k, k > 1 ? x : 0, s_part[r]);
+    *size = kSizes - 1 - min((int)((int64_t)(it.s1 - it.s0) * (kSizes - 1) / c), kSizes - 1);
+    return it;
+  };
+  int size;
+  for (int i = tid; i < n_items; i += blockDim.x) {
+    stretch(i, &size);
+    atomicAdd(&s_size[size], 1);
   }
+  __syncthreads();
+  if (tid < 64) {
+    int v = tid < kSizes ? s_size[tid] : 0, s = v;
+    for (int d = 1; d < 64; d <<= 1) {
+      const int o = __shfl_up(s, d);
+      if (tid >= d) s += o;
+    }
+    if (tid < kSizes) s_size[tid] = s - v;
+  }
+  __syncthreads();
+  for (int i = tid; i < n_items; i += blockDim.x) {
+    const AttnItem it = stretch(i, &size);
+    p.items_rows[atomicAdd(&s_size[size], 1)] = it;
+  }
+  for (int i = (int)n_items + tid; i < p.z.max_rows; i += blockDim.x) p.items_rows[i].key = 0;
   // tiles, the last first
   auto tile_of = [&](int t, AttnItem& it) {
     const int r = plan_find(s_tile, p.R, t);
@@ -143,10 +172,6 @@ __global__ __launch_bounds__(kPlanThreads) void k_attention_plan(AttnPlanParams 
     const int i0 = it.tile * kTileRows / p.group;
     return plan_range(p, it, i0, min(it.rows, (it.tile * kTileRows + kTileRows - 1) / p.group + 1));
   };
-  if (n_tiles == 0) {
-    if (tid == 0) p.head->n_tile = 0;
-    return;
-  }
   sum = 0;
   AttnItem it;
   for (int t = tid; t < n_tiles; t += blockDim.x) sum += tile_of(t, it);
@@ -166,7 +191,7 @@ __global__ __launch_bounds__(kPlanThreads) void k_attention_plan(AttnPlanParams 
     for (int x = 0; x < k && i < p.z.max_tile; ++x, ++i)
       p.items_tile[i] = plan_stretch(it, room ? k : 1, room ? x : 0, (int)part);
   }
-  if (tid == 0) p.head->n_tile = (int)min(base_item, (int64_t)p.z.max_tile);
+  for (int i = (int)min(base_item, (int64_t)p.z.max_tile) + tid; i < p.z.max_tile; i += blockDim.x) p.items_tile[i].key = 0;
 }
 
 hipError_t launch_attention_plan(const AttnPlanParams& p, hipStream_t st) {
@@ -256,7 +281,7 @@ __device__ __forceinline__ u32x4 seen_bytes(int j0, const AttnItem& it) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int j = j0 + 4 * w + e;
-      b |= j < it.end && (j >= it.first || j < it.prefix) ? 0xFFu << (8 * e) : 0u;
+      b |= (j < it.end) & ((j >= it.first) | (j < it.prefix)) ? 0xFFu << (8 * e) : 0u;
     }
     m[w] = b;
   }
@@ -273,53 +298,70 @@ __device__ __forceinline__ u32x4 seen_bytes(int j0, const AttnItem& it) {
 // joined in order, the latter by the stretch that ends last.
 // Bound: the codes' bytes (long caches), latency (short ones).
 // ---------------------------------------------------------------------------
-template <int DT, int FMT, int D, bool OPT>
-__global__ __launch_bounds__(256, 2) void k_attend_rows(AttnParams p) {
-  constexpr int KS = D / 64, DTILES = D / 16, PITCH = D + 4;
-  __shared__ float s_o[4 * kRows * PITCH], s_m[4 * kRows], s_l[4 * kRows];
+#ifndef XW
+#define XW 4
+#define XN 8
+#endif
+template <int DT, int FMT, int D, bool OPT, int W = XW>
+__global__ __launch_bounds__(64 * W, 2) void k_attend_rows(AttnParams p) {
+  constexpr int KS = D / 64, DTILES = D / 16, PITCH = D + 4, KBYTES = kStep * D;
+  constexpr int LDS = std::max(W * KBYTES, W * kRows * PITCH * 4);
+  __shared__ __attribute__((aligned(16))) char lds[LDS];  // K of each wave's step; then each wave's O
+  __shared__ float s_m[W * kRows], s_l[W * kRows];
   __shared__ int s_last;
+  float* s_o = (float*)lds;
   const int head = blockIdx.x % p.c.Hkv, idx = blockIdx.x / p.c.Hkv;
-  if (p.head->key != p.key || idx >= p.head->n_rows) return;
   AttnItem it = p.items_rows[idx];
+  if (it.key != p.key) return;
   if (p.c.pages == 0) it.s1 = it.s0;
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, c = lane & 15, g = lane >> 4;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c = lane & 15, g = lane >> 4;
   const int P = p.c.P, live_rows = it.rows * p.group;
   const bool mine = c < live_rows;
   const int i = mine ? c / p.group : 0, hq = head * p.group + (mine ? c % p.group : 0);
+  const uint32_t sign = p.scale < 0.f ? 0x80008000u : 0u;  // (a scale below zero: of q)
   u32x4 q[2 * KS];
   {
     const uint16_t* qp = p.q + (int64_t)(it.row0 + i) * p.q_ld + hq * D + 16 * g;
 #pragma unroll
-    for (int s = 0; s < 2 * KS; ++s) q[s] = ldg16(qp + 64 * (s >> 1) + 8 * (s & 1));
+    for (int s = 0; s < 2 * KS; ++s) q[s] = ldg16(qp + 64 * (s >> 1) + 8 * (s & 1)) ^ sign;
     if (!mine)
 #pragma unroll
       for (int s = 0; s < 2 * KS; ++s) q[s] = u32x4{0, 0, 0, 0};
   }
   const int pos = it.pos0 + i, pos_max = it.pos0 + it.rows - 1;
-  const ScoreOptions opt{p.scale, p.softcap, OPT && p.slopes ? p.slopes[hq] * kLog2e : 0.f};
+  const ScoreOptions opt{fabsf(p.scale), p.softcap, OPT && p.slopes ? p.slopes[hq] * kLog2e : 0.f};
   const int32_t* table = p.table + it.r * p.ld;
   const int64_t page_bytes = (int64_t)P * D;
 
-  // the page of the run of 16 tokens that this lane reads of K (run c / 4) or of V (run g)
-  auto page_at = [&](int s, int run) {
-    const int j = s * kStep + 16 * run;
+  // the page of the lane's run of 16 tokens, run g
+  auto page_at = [&](int s) {
+    const int j = s * kStep + 16 * g;
     const int page = s < it.s1 && j < it.end ? table[j >> p.log2_page] : -1;
     return page >= 0 && page < p.c.pages ? page : -1;
   };
-  u32x4 kr[4][KS], vr[DTILES];
+  // K straight to LDS, a KB an instruction from tokens that lie side by side; the
+  // pieces of token t stand in the order piece ^ turn(t), so that the sixteen tokens
+  // that a sixteen of lanes reads lie in different banks
+  auto turn = [](int t) { return D == 128 ? ((t >> 4) & 3) | ((t >> 1) & 1) << 2 : (t >> 4) & 3; };
+  char* const s_k = lds + wave * KBYTES;
+  constexpr int PIECES = D / 16, TOKENS = 64 / PIECES;  // of a token; tokens an instruction
   auto load_k = [&](int s, int page) {
-    const int at = (s * kStep + 16 * (c >> 2)) & (P - 1);
-    const uint8_t* k = p.c.k + ((int64_t)max(page, 0) * p.c.Hkv + head) * page_bytes + (at + (c & 3)) * D + 16 * g;
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
-#pragma unroll
-      for (int x = 0; x < KS; ++x) kr[t][x] = ldg16(k + t * 4 * D + 64 * x);
+    for (int x = 0; x < kStep / TOKENS; ++x) {
+      const int run = x * TOKENS / 16, in_run = x * TOKENS % 16 + lane / PIECES;
+      const int pg = max(__builtin_amdgcn_readlane(page, 16 * run), 0);
+      const uint8_t* k = p.c.k + ((int64_t)pg * p.c.Hkv + head) * page_bytes + ((s * kStep + 16 * run) & (P - 1)) * D;
+      const uint8_t* from = k + (in_run * D + 16 * ((lane % PIECES) ^ turn(16 * run + in_run)));
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
+                                       (__attribute__((address_space(3))) void*)(s_k + 1024 * x), 16, 0, 2);
+    }
   };
-  auto load_v = [&](int s, int page) {
+  u32x4 vr[DTILES], vn[DTILES];  // V of this step, and of the next
+  auto load_v = [&](u32x4 (&vr)[DTILES], int s, int page) {
     const int at = (s * kStep + 16 * g) & (P - 1);
     const uint8_t* v = p.c.v + ((int64_t)max(page, 0) * p.c.Hkv + head) * page_bytes + c * P + at;
 #pragma unroll
-    for (int d = 0; d < DTILES; ++d) vr[d] = ldg16(v + d * 16 * P);
+    for (int d = 0; d < DTILES; ++d) vr[d] = __builtin_nontemporal_load((const u32x4*)(v + d * 16 * P));
   };
   auto scales = [&](int page) {
     const int64_t ph = (int64_t)max(page, 0) * p.c.Hkv + head;
@@ -330,41 +372,52 @@ __global__ __launch_bounds__(256, 2) void k_attend_rows(AttnParams p) {
   float m = kLowest, l = 0.f;
   int s = it.s0 + wave;
   if (s < it.s1) {
-    int page_v = page_at(s, g), next_k = page_at(s, c >> 2), next_v;
-    float2 sc = scales(page_v);
-    load_k(s, next_k);
-    load_v(s, page_v);
-    next_k = page_at(s + 4, c >> 2), next_v = page_at(s + 4, g);
-    for (; s < it.s1; s += 4) {
+    int page = page_at(s), next, after = -1;
+    float2 sn = {};
+    load_k(s, page);
+    float2 sc = scales(page);
+    load_v(vr, s, page);
+    next = page_at(s + W);
+    for (; s < it.s1; s += W) {
       f32x4 st[4] = {};
 #pragma unroll
-      for (int t = 0; t < 4; ++t)
+      for (int t = 0; t < 4; ++t) {
+        const int token = 16 * (c >> 2) + 4 * t + (c & 3);
 #pragma unroll
         for (int x = 0; x < KS; ++x) {
-          st[t] = mfma16<DT>(operand8<DT, FMT>(kr[t][x][0], kr[t][x][1], 1.f), q[2 * x], st[t]);
-          st[t] = mfma16<DT>(operand8<DT, FMT>(kr[t][x][2], kr[t][x][3], 1.f), q[2 * x + 1], st[t]);
+          const u32x4 k = *(const u32x4*)(s_k + token * D + 16 * ((g + 4 * x) ^ turn(token)));
+          st[t] = mfma16<DT>(operand8<DT, FMT>(k[0], k[1], 1.f), q[2 * x], st[t]);
+          st[t] = mfma16<DT>(operand8<DT, FMT>(k[2], k[3], 1.f), q[2 * x + 1], st[t]);
         }
-      const bool more = s + 4 < it.s1;
-      if (more) load_k(s + 4, next_k);
+      }
+      const bool more = s + W < it.s1;
+      if (more) {
+        __builtin_amdgcn_s_waitcnt(0xC07F);  // this wave's reads of K have left LDS (lgkmcnt 0)
+        load_k(s + W, next);
+        load_v(vn, s + W, next);
+        sn = scales(next);
+        after = page_at(s + 2 * W);
+      }
       const int j0 = s * kStep + 16 * g;
       // every row sees every token of the step, all pages are there
       const bool whole = s * kStep + kStep <= min(it.end, it.pos0 + 1) && pos_max - s * kStep < p.window &&
-                         __all(page_v >= 0);
+                         __all(page >= 0);
       float2 f = v_factors<DT, FMT>(sc.y);
       float w[16];
       if (whole) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) w[e] = score2<OPT>(st[e >> 2][e & 3], sc.x, opt, pos, j0 + e);
       } else {
-        const u32x4 seen = page_v >= 0 ? seen_bytes(j0, it) : u32x4{0, 0, 0, 0};
+        const u32x4 seen = page >= 0 ? seen_bytes(j0, it) : u32x4{0, 0, 0, 0};
         if (!(seen[0] | seen[1] | seen[2] | seen[3])) f = make_float2(1.f, 1.f);
 #pragma unroll
         for (int d = 0; d < DTILES; ++d) vr[d] &= seen;
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           const int j = j0 + e;
-          const bool sees = ((seen[e >> 2] >> (8 * (e & 3))) & 1) && ((j <= pos && pos - j < p.window) || j < it.prefix);
-          w[e] = sees ? score2<OPT>(st[e >> 2][e & 3], sc.x, opt, pos, j) : -__builtin_inff();
+          const bool sees = ((seen[e >> 2] >> (8 * (e & 3))) & 1) & (((j <= pos) & (pos - j < p.window)) | (j < it.prefix));
+          const float x = score2<OPT>(st[e >> 2][e & 3], sc.x, opt, pos, j);
+          w[e] = sees ? x : -__builtin_inff();
         }
       }
       float top = w[0];
@@ -372,19 +425,20 @@ __global__ __launch_bounds__(256, 2) void k_attend_rows(AttnParams p) {
       for (int e = 1; e < 16; ++e) top = fmaxf(top, w[e]);
       top = fmaxf(top, __shfl_xor(top, 16));
       top = fmaxf(top, __shfl_xor(top, 32));
-      const float now = fmaxf(m, top), fade = __builtin_amdgcn_exp2f(m - now);
-      m = now;
-      float sum = 0.f;
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        w[e] = __builtin_amdgcn_exp2f(w[e] - now);
-        sum += w[e];
-      }
-      l = l * fade + sum;
-      if (__any(fade != 1.f)) {
+      if (__any(top > m + kSlack)) {
+        const float now = fmaxf(m, top), fade = __builtin_amdgcn_exp2f(m - now);
+        m = now;
+        l *= fade;
 #pragma unroll
         for (int d = 0; d < DTILES; ++d) o[d] *= fade;
       }
+      float sum = 0.f;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        w[e] = __builtin_amdgcn_exp2f(w[e] - m);
+        sum += w[e];
+      }
+      l += sum;
       if ((DT != DT_F16 && FMT == KV_INT8) || (DT == DT_F16 && __any(f.y != 1.f))) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) w[e] *= f.y;
@@ -397,78 +451,105 @@ __global__ __launch_bounds__(256, 2) void k_attend_rows(AttnParams p) {
         o[d] = mfma16<DT>(v_operand8<DT, FMT>(vr[d][0], vr[d][1], f.x), pw[0], o[d]);
         o[d] = mfma16<DT>(v_operand8<DT, FMT>(vr[d][2], vr[d][3], f.x), pw[1], o[d]);
       }
-      if (more) {
-        page_v = next_v;
-        load_v(s + 4, page_v);
-        sc = scales(page_v);
-        next_k = page_at(s + 8, c >> 2), next_v = page_at(s + 8, g);
-      }
+      page = next, next = after, sc = sn;
+#pragma unroll
+      for (int d = 0; d < DTILES; ++d) vr[d] = vn[d];
     }
   }
   l += __shfl_xor(l, 16);
   l += __shfl_xor(l, 32);
+  __syncthreads();
 #pragma unroll
   for (int d = 0; d < DTILES; ++d) *(f32x4*)&s_o[(wave * kRows + c) * PITCH + 16 * d + 4 * g] = o[d];
   if (g == 0) s_m[wave * kRows + c] = m, s_l[wave * kRows + c] = l;
   __syncthreads();
-  // a thread: row tid / 16, D / 16 features of it
-  constexpr int F = D / 16;
-  const int row = tid >> 4, d0 = (tid & 15) * F;
-  float top = s_m[row], x[F] = {}, total = 0.f;
+  // Eight features a thread: D / 8 threads a row, the rows that are there, and so
+  // many groups of threads as the workgroup holds, which share the partial results.
+  constexpr int F = 8, CHUNKS = D / F;
+  const int per = live_rows * CHUNKS, groups = 64 * W / per, part = tid / per;
+  const int row = tid % per / CHUNKS, d0 = tid % CHUNKS * F;
+  float top = kLowest, x[F] = {}, total = 0.f;
+  // one more result of maximum pm and sum pl, its features v
+  auto add = [&](float pm, float pl, const float (&v)[F]) {
+    const float now = fmaxf(top, pm), f0 = __builtin_amdgcn_exp2f(top - now), f1 = __builtin_amdgcn_exp2f(pm - now);
+    top = now;
+    total = total * f0 + pl * f1;
 #pragma unroll
-  for (int v = 1; v < 4; ++v) top = fmaxf(top, s_m[v * kRows + row]);
+    for (int e = 0; e < F; ++e) x[e] = x[e] * f0 + v[e] * f1;
+  };
+  if (part == 0) {
 #pragma unroll
-  for (int v = 0; v < 4; ++v) {
-    const float f = __builtin_amdgcn_exp2f(s_m[v * kRows + row] - top);
-    total += f * s_l[v * kRows + row];
+    for (int v = 0; v < W; ++v) {
+      float y[F];
 #pragma unroll
-    for (int e = 0; e < F; ++e) x[e] += f * s_o[(v * kRows + row) * PITCH + d0 + e];
+      for (int e = 0; e < F; ++e) y[e] = s_o[(v * kRows + row) * PITCH + d0 + e];
+      add(s_m[v * kRows + row], s_l[v * kRows + row], y);
+    }
   }
   if (it.splits > 1) {
     const uint32_t size = kRows * (D + 2) * 4, slot = (uint32_t)it.part * p.c.Hkv + head;
     const rsrc_t r = make_rsrc((const char*)p.parts_rows + (size_t)slot * size, (uint32_t)((it.splits - 1) * p.c.Hkv + 1) * size);
     const uint32_t at = (uint32_t)it.split * p.c.Hkv * size;
+    if (part == 0) {
 #pragma unroll
-    for (int e = 0; e < F; e += 4) bst128c(r, at + (row * D + d0 + e) * 4, f32x4{x[e], x[e + 1], x[e + 2], x[e + 3]});
-    float* ml = p.parts_rows + ((size_t)slot * size + at) / 4 + kRows * D;
-    if ((tid & 15) == 0) st_agent(ml + row, top), st_agent(ml + kRows + row, total);
+      for (int e = 0; e < F; e += 4) bst128c(r, at + (row * D + d0 + e) * 4, f32x4{x[e], x[e + 1], x[e + 2], x[e + 3]});
+      float* ml = p.parts_rows + ((size_t)slot * size + at) / 4 + kRows * D;
+      if (d0 == 0) st_agent(ml + row, top), st_agent(ml + kRows + row, total);
+    }
     complete_and_sync();
-    if (tid == 0) s_last = arrive_last(p.counters + slot, it.splits);
+    if (tid == 0) s_last = arrive_last(p.counters_rows + slot, it.splits);
     __syncthreads();
     if (!s_last) return;
-    // the stretches in order, four in flight
+    // group `part` takes every groups-th stretch in order, N in flight; then the groups in order
+    constexpr int N = XN;
     total = 0.f;
     top = kLowest;
 #pragma unroll
     for (int e = 0; e < F; ++e) x[e] = 0.f;
     const uint32_t stride = p.c.Hkv * size, own = (row * D + d0) * 4, own_m = (kRows * D + row) * 4;
-    for (int b = 0; b < it.splits; b += 4) {
-      f32x4 v[4][F / 4];
-      float pm[4], pl[4];
+    for (int b = part < groups ? part : it.splits; b < it.splits; b += N * groups) {
+      f32x4 v[N][F / 4];
+      float pm[N], pl[N];
 #pragma unroll
-      for (int y = 0; y < 4; ++y) {
-        const uint32_t off = b + y < it.splits ? (b + y) * stride : kOOB;
+      for (int y = 0; y < N; ++y) {
+        const uint32_t off = b + y * groups < it.splits ? (b + y * groups) * stride : kOOB;
         pm[y] = __uint_as_float(bld32c(r, off + own_m));
         pl[y] = __uint_as_float(bld32c(r, off + own_m + kRows * 4));
 #pragma unroll
         for (int e = 0; e < F / 4; ++e) v[y][e] = bld128cf(r, off + own + 16 * e);
       }
 #pragma unroll
-      for (int y = 0; y < 4; ++y) {
-        if (b + y >= it.splits) continue;
-        const float now = fmaxf(top, pm[y]), f0 = __builtin_amdgcn_exp2f(top - now), f1 = __builtin_amdgcn_exp2f(pm[y] - now);
-        top = now;
-        total = total * f0 + pl[y] * f1;
+      for (int y = 0; y < N; ++y) {
+        if (b + y * groups >= it.splits) continue;
+        const float z[F] = {v[y][0][0], v[y][0][1], v[y][0][2], v[y][0][3], v[y][1][0], v[y][1][1], v[y][1][2], v[y][1][3]};
+        add(pm[y], pl[y], z);
+      }
+    }
+    static_assert(64 * W / CHUNKS <= W * kRows, "a place in s_o for each row of each group");
+    if (part < groups) {
 #pragma unroll
-        for (int e = 0; e < F; ++e) x[e] = x[e] * f0 + v[y][e >> 2][e & 3] * f1;
+      for (int e = 0; e < F; ++e) s_o[(part * live_rows + row) * PITCH + d0 + e] = x[e];
+      if (d0 == 0) s_m[part * live_rows + row] = top, s_l[part * live_rows + row] = total;
+    }
+    __syncthreads();
+    if (part == 0) {
+      total = 0.f;
+      top = kLowest;
+#pragma unroll
+      for (int e = 0; e < F; ++e) x[e] = 0.f;
+      for (int b = 0; b < groups; ++b) {
+        float y[F];
+#pragma unroll
+        for (int e = 0; e < F; ++e) y[e] = s_o[(b * live_rows + row) * PITCH + d0 + e];
+        add(s_m[b * live_rows + row], s_l[b * live_rows + row], y);
       }
     }
   }
-  if (row >= live_rows) return;
+  if (part) return;
   const float inv = total > 0.f ? 1.f / total : 0.f;
   uint16_t* out = p.out + (int64_t)(it.row0 + row / p.group) * p.out_ld + (head * p.group + row % p.group) * D + d0;
-#pragma unroll
-  for (int e = 0; e < F; e += 4) *(u32x2*)(out + e) = u32x2{pack2<DT>(x[e] * inv, x[e + 1] * inv), pack2<DT>(x[e + 2] * inv, x[e + 3] * inv)};
+  *(u32x4*)out = u32x4{pack2<DT>(x[0] * inv, x[1] * inv), pack2<DT>(x[2] * inv, x[3] * inv),
+                       pack2<DT>(x[4] * inv, x[5] * inv), pack2<DT>(x[6] * inv, x[7] * inv)};
 }
 
 // ---------------------------------------------------------------------------
@@ -488,19 +569,20 @@ __global__ __launch_bounds__(512) void k_attend_tile(AttnParams p) {
   __shared__ float s_ks[2][4], s_vf[2][4];
   __shared__ int s_last;
   const int head = blockIdx.x % p.c.Hkv, idx = blockIdx.x / p.c.Hkv;
-  if (p.head->key != p.key || idx >= p.head->n_tile) return;
   AttnItem it = p.items_tile[idx];
+  if (it.key != p.key) return;
   if (p.c.pages == 0) it.s1 = it.s0;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, c = lane & 31, h = lane >> 5;
   const int P = p.c.P, live_rows = it.rows * p.group, wave_row = it.tile * kTileRows + 32 * wave;
   const int row = wave_row + c;
   const bool active = wave_row < live_rows, mine = row < live_rows;
   const int i = mine ? row / p.group : it.rows - 1, hq = head * p.group + (mine ? row % p.group : 0);
+  const uint32_t sign = p.scale < 0.f ? 0x80008000u : 0u;  // (a scale below zero: of q)
   u32x4 q[D / 16];
   {
     const uint16_t* qp = p.q + (int64_t)(it.row0 + i) * p.q_ld + hq * D + 8 * h;
 #pragma unroll
-    for (int s = 0; s < D / 16; ++s) q[s] = ldg16(qp + 16 * s);
+    for (int s = 0; s < D / 16; ++s) q[s] = ldg16(qp + 16 * s) ^ sign;
     if (!mine)
 #pragma unroll
       for (int s = 0; s < D / 16; ++s) q[s] = u32x4{0, 0, 0, 0};
@@ -508,7 +590,7 @@ __global__ __launch_bounds__(512) void k_attend_tile(AttnParams p) {
   const int pos = it.pos0 + i;
   // positions of the wave's first and last row
   const int pos_lo = it.pos0 + min(wave_row / p.group, it.rows - 1), pos_hi = it.pos0 + min((wave_row + 31) / p.group, it.rows - 1);
-  const ScoreOptions opt{p.scale, p.softcap, OPT && p.slopes ? p.slopes[hq] * kLog2e : 0.f};
+  const ScoreOptions opt{fabsf(p.scale), p.softcap, OPT && p.slopes ? p.slopes[hq] * kLog2e : 0.f};
   const int32_t* table = p.table + it.r * p.ld;
   const int64_t page_bytes = (int64_t)P * D;
 
@@ -595,36 +677,51 @@ __global__ __launch_bounds__(512) void k_attend_tile(AttnParams p) {
       for (int r = 0; r < 4; ++r) ks[r] = s_ks[s & 1][r], vf[r] = s_vf[s & 1][r];
       const bool pages_there = ks[0] == ks[0] && ks[1] == ks[1] && ks[2] == ks[2] && ks[3] == ks[3];
       const bool whole = j0 + kStep <= min(it.end, pos_lo + 1) && pos_hi - j0 < p.window && pages_there;
-      float w[2][16];
+      // scores in powers of two; where every row sees every token, still without K's scale
+      float w[2][16], f[4], top;
+      const bool plain = whole && !OPT;
+      if (plain) {
+        top = kLowest;
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
+        for (int r = 0; r < 4; ++r) {
+          f[r] = ks[r] * (opt.scale * kLog2e);
+          float x = st[r >> 1][8 * (r & 1)];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int run = 2 * t + (e >> 3), j = j0 + 32 * t + 8 * (e >> 2) + 4 * h + (e & 3);
-          w[t][e] = score2<OPT>(st[t][e], ks[run], opt, pos, j);
-          if (!whole) {
-            const bool sees = j < it.end && ((j <= pos && pos - j < p.window) || j < it.prefix) && ks[run] == ks[run];
-            w[t][e] = sees ? w[t][e] : -__builtin_inff();
-          }
+          for (int e = 0; e < 8; ++e) x = fmaxf(x, w[r >> 1][8 * (r & 1) + e] = st[r >> 1][8 * (r & 1) + e]);
+          top = fmaxf(top, x * f[r]);
         }
-      float top = w[0][0];
+      } else {
 #pragma unroll
-      for (int e = 1; e < 32; ++e) top = fmaxf(top, w[e >> 4][e & 15]);
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int run = 2 * t + (e >> 3), j = j0 + 32 * t + 8 * (e >> 2) + 4 * h + (e & 3);
+            const bool sees = (j < it.end) & (((j <= pos) & (pos - j < p.window)) | (j < it.prefix)) & (ks[run] == ks[run]);
+            const float x = score2<OPT>(st[t][e], ks[run], opt, pos, j);
+            w[t][e] = whole | sees ? x : -__builtin_inff();
+          }
+        top = w[0][0];
+#pragma unroll
+        for (int e = 1; e < 32; ++e) top = fmaxf(top, w[e >> 4][e & 15]);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) f[r] = 1.f;
+      }
       top = fmaxf(top, __shfl_xor(top, 32));
-      const float now = fmaxf(m, top), fade = __builtin_amdgcn_exp2f(m - now);
-      m = now;
+      if (__any(top > m + kSlack)) {
+        const float now = fmaxf(m, top), fade = __builtin_amdgcn_exp2f(m - now);
+        m = now;
+        l *= fade;
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d) o[d] *= fade;
+      }
       float sum = 0.f;
 #pragma unroll
       for (int e = 0; e < 32; ++e) {
         float& x = w[e >> 4][e & 15];
-        x = __builtin_amdgcn_exp2f(x - now);
+        x = __builtin_amdgcn_exp2f(__builtin_fmaf(x, f[e >> 3], -m));
         sum += x;
       }
-      l = l * fade + sum;
-      if (__any(fade != 1.f)) {
-#pragma unroll
-        for (int d = 0; d < D / 32; ++d) o[d] *= fade;
-      }
+      l += sum;
       if (DT == DT_F16 && !(vf[0] == 1.f && vf[1] == 1.f && vf[2] == 1.f && vf[3] == 1.f)) {
 #pragma unroll
         for (int e = 0; e < 32; ++e) w[e >> 4][e & 15] *= vf[e >> 3];
@@ -657,7 +754,7 @@ __global__ __launch_bounds__(512) void k_attend_tile(AttnParams p) {
       if (h == 0) st_agent(ml, m), st_agent(ml + kTileRows, l);
     }
     complete_and_sync();
-    if (tid == 0) s_last = arrive_last(p.counters + (size_t)p.z.part_rows * p.c.Hkv + slot, it.splits);
+    if (tid == 0) s_last = arrive_last(p.counters_tile + slot, it.splits);
     __syncthreads();
     if (!s_last) return;
     if (active) {
@@ -694,8 +791,8 @@ __global__ __launch_bounds__(512) void k_attend_tile(AttnParams p) {
 template <int FMT, int D>
 static hipError_t rows_launch(const AttnParams& p, hipStream_t st) {
   const dim3 grid((uint32_t)p.z.max_rows * p.c.Hkv);
-  if (p.slopes || p.softcap > 0.f) hipLaunchKernelGGL((k_attend_rows<DTC, FMT, D, true>), grid, dim3(256), 0, st, p);
-  else hipLaunchKernelGGL((k_attend_rows<DTC, FMT, D, false>), grid, dim3(256), 0, st, p);
+  if (p.slopes || p.softcap > 0.f) hipLaunchKernelGGL((k_attend_rows<DTC, FMT, D, true>), grid, dim3(64 * XW), 0, st, p);
+  else hipLaunchKernelGGL((k_attend_rows<DTC, FMT, D, false>), grid, dim3(64 * XW), 0, st, p);
   return hipGetLastError();
 }
 template <int FMT, int D>

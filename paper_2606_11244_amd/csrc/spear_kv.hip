@@ -174,6 +174,12 @@ __device__ __forceinline__ void decode4(uint32_t w, float (&x)[4]) {
     x[0] = a[0], x[1] = a[1], x[2] = b[0], x[3] = b[1];
   }
 }
+typedef _Float16 h16x2 __attribute__((ext_vector_type(2)));
+template <int DT>
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+  if constexpr (DT == DT_F16) return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, h16x2));
+  else return pack_bf16(a, b);
+}
 // a value over its scale, NaN as zero, what passes the largest code as that
 __device__ __forceinline__ float to_code(float x, float inv, float most) {
   const float c = x == x ? x * inv : 0.f;
@@ -251,185 +257,273 @@ __device__ __forceinline__ void turn(const Unit& u, int interleaved, float (&a)[
 
 // ---------------------------------------------------------------------------
 // New tokens. A workgroup of the cache's part owns the runs of tokens (those of
-// one page that follow each other) that begin in its window of rows, for one head
-// and K or V: it brings the run to LDS in fp32 (K turned), takes the largest
-// magnitude, settles the page's scale with the one before, divides the codes
-// already there if it grew, and writes the run's. One page and head is one
-// workgroup's alone: no atomics, the same codes on every run. A workgroup of the
-// queries' part takes whole tokens, its cosines and sines in LDS for all heads.
+// one page that follow each other) that begin in its share of a window of 64 rows,
+// for one head and K or V: it takes the run to registers (K turned), the largest magnitude,
+// settles the page's scale with the one before, divides the codes already there
+// if it grew, and writes the run's. One page and head is one workgroup's alone: no
+// atomics, the same codes on every run. A workgroup of the queries' part takes
+// a token, its cosines and sines in LDS for all heads.
 // Bound: the bytes of q, k and v (long prompts), latency (decode).
 // ---------------------------------------------------------------------------
-template <int DT, int FMT, int W>
-__device__ void append_run(const KvAppendParams& p, int t, int slot, int n, int h, bool is_v, float* x, float* red) {
-  const int tid = threadIdx.x, D = p.c.D, P = p.c.P, page = slot / P, off = slot % P;
-  const int pitch = is_v ? D + 1 : D;
-  float top = 0.f;
-  if (is_v) {
-    for (int i = tid; i < n * (D / 8); i += 256) {
-      const int m = i / (D / 8), d = 8 * (i % (D / 8));
-      float a[8];
-      load_run<DT, 8>(p.v + (int64_t)(t + m) * p.v_ld + h * D + d, a);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        x[m * pitch + d + e] = a[e];
-        top = fmaxf(top, finite_size(a[e]));
-      }
-    }
-  } else {
-    const int units = D / (2 * W);
-    for (int i = tid; i < n * units; i += 256) {
-      const int m = i / units;
-      const Unit u = unit_at<W>(i % units, p.r.rot, p.r.interleaved);
-      const uint16_t* k = p.k + (int64_t)(t + m) * p.k_ld + h * D;
-      float a[W], b[W];
-      load_run<DT, W>(k + u.p0, a);
-      load_run<DT, W>(k + u.p1, b);
-      const uint64_t pos = p.r.rot ? (uint64_t)(int64_t)p.positions[t + m] : 0;
-      turn<W>(u, p.r.interleaved, a, b, [&](int i) { return cos_sin(pos * p.r.freqs[i], p.r.magnitude); });
-#pragma unroll
-      for (int e = 0; e < W; ++e) {
-        x[m * pitch + u.p0 + e] = a[e];
-        x[m * pitch + u.p1 + e] = b[e];
-        top = fmaxf(top, fmaxf(finite_size(a[e]), finite_size(b[e])));
-      }
-    }
-  }
+
+// the scale of a page and head, from the one before and the largest magnitude given
+struct PageScale {
+  float scale, inv, ratio, most;  // ratio: what older codes are multiplied by
+  bool grew;
+};
+template <int DT, int FMT>
+__device__ __forceinline__ PageScale settle(float top, float before, float* red) {
   for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-  if ((tid & 63) == 0) red[tid >> 6] = top;
-  float* scale = (is_v ? p.c.v_scale : p.c.k_scale) + (int64_t)page * p.c.Hkv + h;
-  const float before = off ? *scale : 0.f;
+  __syncthreads();  // (red: of the run before)
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = top;
   __syncthreads();
   top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-  const float s = fmaxf(before, scale_of<FMT>(top)), inv = 1.f / s, ratio = before * inv;
-  const float most = top_code<DT, FMT>(s);
-  const bool grew = s > before;
-  if (tid == 0 && grew) *scale = s;
-  uint8_t* codes = (is_v ? p.c.v : p.c.k) + ((int64_t)page * p.c.Hkv + h) * P * D;
-  if (is_v) {  // [D][P]: dwords of four places
-    const int g0 = grew ? 0 : off / 4, groups = (off + n + 3) / 4 - g0;
-    for (int i = tid; i < D * groups; i += 256) {
-      const int d = i / groups, at = 4 * (g0 + i % groups);
-      uint32_t* w = (uint32_t*)(codes + d * P + at);
-      uint32_t old = 0;
-      float c[4];
-      const bool part = at < off || at + 4 > off + n;
-      if (part) old = *w;
-      uint32_t kept = old;
-      if (at < off && grew) {
-        decode4<FMT>(old, c);
+  PageScale s;
+  s.scale = fmaxf(before, scale_of<FMT>(top));
+  s.inv = 1.f / s.scale;
+  s.ratio = before * s.inv;
+  s.most = top_code<DT, FMT>(s.scale);
+  s.grew = s.scale > before;
+  return s;
+}
+template <int FMT>
+__device__ __forceinline__ uint32_t divide4(uint32_t w, float ratio) {
+  float c[4];
+  decode4<FMT>(w, c);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) c[e] *= ratio;
-        kept = encode4<FMT>(c);
-      }
-      uint32_t fresh = 0, before_run = 0, behind_run = 0;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int m = at + e - off;
-        c[e] = m >= 0 && m < n ? to_code(x[m * pitch + d], inv, most) : 0.f;
-        before_run |= m < 0 ? 0xFFu << (8 * e) : 0u;
-        behind_run |= m >= n ? 0xFFu << (8 * e) : 0u;
-      }
-      fresh = encode4<FMT>(c);
-      *w = (kept & before_run) | (old & behind_run) | (fresh & ~(before_run | behind_run));
-    }
-  } else {  // [P][D]
-    const int m0 = grew ? -off : 0, quads = D / 4;
-    for (int i = tid; i < (n - m0) * quads; i += 256) {
-      const int m = m0 + i / quads, d = 4 * (i % quads);
-      uint32_t* w = (uint32_t*)(codes + (off + m) * D + d);
-      float c[4];
-      if (m < 0) {
-        decode4<FMT>(*w, c);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) c[e] *= ratio;
-      } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) c[e] = to_code(x[m * pitch + d + e], inv, most);
-      }
-      *w = encode4<FMT>(c);
-    }
-  }
-  __syncthreads();  // x and red belong to the next run
+  for (int e = 0; e < 4; ++e) c[e] *= ratio;
+  return encode4<FMT>(c);
 }
 
-template <int DT, int FMT, int W>
-__global__ __launch_bounds__(256) void k_kv_append(KvAppendParams p) {
-  extern __shared__ float lds[];
-  __shared__ float red[4];
-  const int tid = threadIdx.x, D = p.c.D, P = p.c.P;
-  const int64_t capacity = (int64_t)p.c.pages * P;
-  if (blockIdx.x < p.kv_blocks) {
-    const int is_v = blockIdx.x & 1, h = (blockIdx.x >> 1) % p.c.Hkv;
-    const int t0 = (int)((blockIdx.x >> 1) / p.c.Hkv) * p.window;
-    for (int t = t0; t < min(t0 + p.window, p.T); ++t) {
-      const int slot = p.slots[t];
-      if (slot < 0 || slot >= capacity) continue;
-      if (t) {  // not the first of its page's tokens
-        const int prev = p.slots[t - 1];
-        if (prev >= 0 && prev < capacity && prev / P == slot / P) continue;
+template <int DT, int FMT, int D, int W>
+__device__ __forceinline__ void append_k(const KvAppendParams& p, int t, int slot, int n, int h, float* red) {
+  constexpr int units = D / (2 * W);
+  const int tid = threadIdx.x, P = p.c.P, page = slot >> p.log2_page, off = slot & (P - 1);
+  const int64_t ph = (int64_t)page * p.c.Hkv + h;
+  const float before = off ? p.c.k_scale[ph] : 0.f;
+  uint8_t* codes = p.c.k + ph * P * D;
+  auto unit = [&](int i, float (&a)[W], float (&b)[W]) {
+    const int m = i / units;
+    const Unit u = unit_at<W>(i % units, p.r.rot, p.r.interleaved);
+    const uint16_t* k = p.k + (int64_t)(t + m) * p.k_ld + h * D;
+    load_run<DT, W>(k + u.p0, a);
+    load_run<DT, W>(k + u.p1, b);
+    const uint64_t pos = p.r.rot ? (uint64_t)(int64_t)p.positions[t + m] : 0;
+    turn<W>(u, p.r.interleaved, a, b, [&](int x) { return cos_sin(pos * p.r.freqs[x], p.r.magnitude); });
+  };
+  auto older = [&](float ratio) {
+    for (int i = tid; i < off * D / 4; i += 256) ((uint32_t*)codes)[i] = divide4<FMT>(((uint32_t*)codes)[i], ratio);
+  };
+  float top = 0.f;
+  if constexpr (W == 8) {
+    constexpr int U = 4;  // units a thread at most: pages of 128 tokens, 128 features
+    float a[U][8], b[U][8];
+#pragma unroll
+    for (int x = 0; x < U; ++x) {
+      if (tid + 256 * x >= n * units) continue;
+      unit(tid + 256 * x, a[x], b[x]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) top = fmaxf(top, fmaxf(finite_size(a[x][e]), finite_size(b[x][e])));
+    }
+    const PageScale s = settle<DT, FMT>(top, before, red);
+    if (tid == 0 && s.grew) p.c.k_scale[ph] = s.scale;
+    if (s.grew) older(s.ratio);
+    auto put = [&](uint8_t* to, const float (&v)[8]) {
+      float c[2][4];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) c[e >> 2][e & 3] = to_code(v[e], s.inv, s.most);
+      *(u32x2*)to = u32x2{encode4<FMT>(c[0]), encode4<FMT>(c[1])};
+    };
+#pragma unroll
+    for (int x = 0; x < U; ++x) {
+      const int i = tid + 256 * x;
+      if (i >= n * units) continue;
+      const Unit u = unit_at<W>(i % units, p.r.rot, p.r.interleaved);
+      uint8_t* row = codes + (off + i / units) * D;
+      put(row + u.p0, a[x]);
+      put(row + u.p1, b[x]);
+    }
+  } else {  // (a rotation of no multiple of 16 features: turned twice, a byte a store)
+    float a[1], b[1];
+    for (int i = tid; i < n * units; i += 256) {
+      unit(i, a, b);
+      top = fmaxf(top, fmaxf(finite_size(a[0]), finite_size(b[0])));
+    }
+    const PageScale s = settle<DT, FMT>(top, before, red);
+    if (tid == 0 && s.grew) p.c.k_scale[ph] = s.scale;
+    if (s.grew) older(s.ratio);
+    for (int i = tid; i < n * units; i += 256) {
+      unit(i, a, b);
+      const float c[4] = {to_code(a[0], s.inv, s.most), to_code(b[0], s.inv, s.most), 0.f, 0.f};
+      const uint32_t w = encode4<FMT>(c);
+      const Unit u = unit_at<W>(i % units, p.r.rot, p.r.interleaved);
+      uint8_t* row = codes + (off + i / units) * D;
+      row[u.p0] = (uint8_t)w;
+      row[u.p1] = (uint8_t)(w >> 8);
+    }
+  }
+}
+
+// V: a unit is four places of a page (a dword of codes) and eight features
+template <int DT, int FMT, int D>
+__device__ __forceinline__ void append_v(const KvAppendParams& p, int t, int slot, int n, int h, float* red) {
+  const int tid = threadIdx.x, P = p.c.P, page = slot >> p.log2_page, off = slot & (P - 1);
+  const int64_t ph = (int64_t)page * p.c.Hkv + h;
+  const float before = off ? p.c.v_scale[ph] : 0.f;
+  uint8_t* codes = p.c.v + ph * P * D;
+  constexpr int U = 2;  // units a thread at most
+  const int q0 = off / 4, quads = (off + n + 3) / 4 - q0, units = quads * (D / 8);
+  u32x4 x[U][4];
+  int quad[U], feature[U];
+  float top = 0.f;
+#pragma unroll
+  for (int y = 0; y < U; ++y) {
+    const int i = tid + 256 * y;
+    quad[y] = q0 + i % quads, feature[y] = 8 * (i / quads);
+    if (i >= units) continue;
+    const int m0 = 4 * quad[y] - off;
+    const uint16_t* v = p.v + (int64_t)t * p.v_ld + h * D + feature[y];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[y][e] = m0 + e >= 0 && m0 + e < n ? ldg16(v + (int64_t)(m0 + e) * p.v_ld) : u32x4{0, 0, 0, 0};
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int f = 0; f < 8; ++f) top = fmaxf(top, finite_size(act2f<DT>((x[y][e][f >> 1] >> (16 * (f & 1))) & 0xFFFFu)));
+  }
+  const PageScale s = settle<DT, FMT>(top, before, red);
+  if (tid == 0 && s.grew) p.c.v_scale[ph] = s.scale;
+  if (s.grew)
+    for (int i = tid; i < D * q0; i += 256) {
+      uint32_t* w = (uint32_t*)(codes + i / q0 * P + 4 * (i % q0));
+      *w = divide4<FMT>(*w, s.ratio);
+    }
+#pragma unroll
+  for (int y = 0; y < U; ++y) {
+    const int i = tid + 256 * y;
+    if (i >= units) continue;
+    const int m0 = 4 * quad[y] - off;
+    uint32_t before_run = 0, behind_run = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      before_run |= m0 + e < 0 ? 0xFFu << (8 * e) : 0u;
+      behind_run |= m0 + e >= n ? 0xFFu << (8 * e) : 0u;
+    }
+#pragma unroll
+    for (int f = 0; f < 8; ++f) {
+      uint32_t* w = (uint32_t*)(codes + (feature[y] + f) * P + 4 * quad[y]);
+      float c[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) c[e] = to_code(act2f<DT>((x[y][e][f >> 1] >> (16 * (f & 1))) & 0xFFFFu), s.inv, s.most);
+      uint32_t fresh = encode4<FMT>(c);
+      if (before_run | behind_run) {
+        const uint32_t old = *w, kept = before_run && s.grew ? divide4<FMT>(old, s.ratio) : old;
+        fresh = (kept & before_run) | (old & behind_run) | (fresh & ~(before_run | behind_run));
       }
+      *w = fresh;
+    }
+  }
+}
+
+template <int DT, int FMT, int D, int W>
+__global__ __launch_bounds__(256) void k_kv_append(KvAppendParams p) {
+  __shared__ float2 cs[64];
+  __shared__ float red[4];
+  const int tid = threadIdx.x, P = p.c.P, capacity = p.c.pages << p.log2_page;
+  if (blockIdx.x < p.kv_blocks) {
+    // (sub, window of 64 tokens, head, K or V): the sub-th of every p.subs runs that begin in the window.
+    // The subs that find none in a prompt come last: side by side with the others they would leave the
+    // work to the same few CUs (4096 tokens, 8 heads: 47 us, 35 this way).
+    uint32_t b = blockIdx.x;
+    const int is_v = b & 1, h = (b >>= 1) % p.c.Hkv, windows = (p.T + 63) / 64;
+    const int t0 = (int)((b /= p.c.Hkv) % windows) * 64, sub = (int)(b / windows);
+    const int lane = tid & 63, own = t0 + lane < p.T ? p.slots[t0 + lane] : -1;
+    const int prev = t0 + lane > 0 && t0 + lane <= p.T ? p.slots[t0 + lane - 1] : -1;
+    const bool first = own >= 0 && own < capacity && !(prev >= 0 && prev < capacity && (prev ^ own) < P);
+    uint64_t starts = __ballot(first);
+    for (int run = 0; starts; ++run, starts &= starts - 1) {
+      if (run % p.subs != sub) continue;
+      const int x = __builtin_ctzll(starts), t = t0 + x, slot = __builtin_amdgcn_readlane(own, x);
       // how many follow: the first lane whose token does not
-      const int most = min(P - slot % P, p.T - t), lane = tid & 63;
+      const int most = min(P - (slot & (P - 1)), p.T - t);
       int n = 0;
       for (int i = 0; i < most; i += 64) {
         const int m = i + lane;
         const uint64_t yes = __ballot(m < most && p.slots[t + m] == slot + m);
-        const int run = yes == ~0ull ? 64 : __builtin_ctzll(~yes);
-        n += run;
-        if (run < 64) break;
+        const int more = yes == ~0ull ? 64 : __builtin_ctzll(~yes);
+        n += more;
+        if (more < 64) break;
       }
-      append_run<DT, FMT, W>(p, t, slot, n, h, is_v, lds, red);
+      if (is_v) append_v<DT, FMT, D>(p, t, slot, n, h, red);
+      else append_k<DT, FMT, D, W>(p, t, slot, n, h, red);
     }
     return;
   }
-  // queries
-  const int t0 = (int)(blockIdx.x - p.kv_blocks) * p.q_tokens, count = min(p.q_tokens, p.T - t0);
-  float2* cs = (float2*)lds;
-  const int half = p.r.rot / 2, units = D / (2 * W), per = p.H * units;
-  for (int i = tid; i < count * half; i += 256)
-    cs[i] = cos_sin((uint64_t)(int64_t)p.positions[t0 + i / half] * p.r.freqs[i % half], p.r.magnitude);
-  __syncthreads();
-  for (int i = tid; i < count * per; i += 256) {
-    const int m = i / per, hu = i % per, h = hu / units, t = t0 + m;
-    const int slot = p.slots[t];
-    if (slot < 0 || slot >= capacity) continue;
-    const Unit u = unit_at<W>(hu % units, p.r.rot, p.r.interleaved);
-    const uint16_t* q = p.q + (int64_t)t * p.q_ld + h * D;
-    uint16_t* o = p.q_out + (int64_t)t * p.qo_ld + h * D;
-    float a[W], b[W];
-    load_run<DT, W>(q + u.p0, a);
-    load_run<DT, W>(q + u.p1, b);
-    turn<W>(u, p.r.interleaved, a, b, [&](int i) { return cs[m * half + i]; });
-    if constexpr (W == 8) {
-      u32x4 va, vb;
+  // queries: a token, N units a thread at a time, all requested before the first is turned
+  const int t = (int)(blockIdx.x - p.kv_blocks), slot = p.slots[t];
+  if (slot < 0 || slot >= capacity) return;
+  constexpr int units = D / (2 * W), N = 2;
+  const int half = p.r.rot / 2, all = p.H * units;
+  const uint64_t pos = half ? (uint64_t)(int64_t)p.positions[t] : 0;
+  const uint16_t* q = p.q + (int64_t)t * p.q_ld;
+  uint16_t* out = p.q_out + (int64_t)t * p.qo_ld;
+  typedef typename std::conditional<W == 8, u32x4, uint16_t>::type Raw;
+  Raw ra[N], rb[N];
+  auto fetch = [&](int i0) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        va[e] = (uint32_t)f2act<DT>(a[2 * e]) | ((uint32_t)f2act<DT>(a[2 * e + 1]) << 16);
-        vb[e] = (uint32_t)f2act<DT>(b[2 * e]) | ((uint32_t)f2act<DT>(b[2 * e + 1]) << 16);
-      }
-      *(u32x4*)(o + u.p0) = va;
-      *(u32x4*)(o + u.p1) = vb;
-    } else {
-      o[u.p0] = f2act<DT>(a[0]);
-      o[u.p1] = f2act<DT>(b[0]);
+    for (int x = 0; x < N; ++x) {
+      const int i = min(i0 + 256 * x, all - 1);
+      const Unit u = unit_at<W>(i % units, p.r.rot, p.r.interleaved);
+      ra[x] = *(const Raw*)(q + i / units * D + u.p0);
+      rb[x] = *(const Raw*)(q + i / units * D + u.p1);
     }
+  };
+  auto put = [&](int i0) {
+#pragma unroll
+    for (int x = 0; x < N; ++x) {
+      const int i = i0 + 256 * x;
+      if (i >= all) continue;
+      const Unit u = unit_at<W>(i % units, p.r.rot, p.r.interleaved);
+      uint16_t* o = out + i / units * D;
+      float a[W], b[W];
+      if constexpr (W == 8) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          a[e] = act2f<DT>((ra[x][e >> 1] >> (16 * (e & 1))) & 0xFFFFu);
+          b[e] = act2f<DT>((rb[x][e >> 1] >> (16 * (e & 1))) & 0xFFFFu);
+        }
+      } else {
+        a[0] = act2f<DT>(ra[x]), b[0] = act2f<DT>(rb[x]);
+      }
+      turn<W>(u, p.r.interleaved, a, b, [&](int y) { return cs[y]; });
+      if constexpr (W == 8) {
+        *(u32x4*)(o + u.p0) = u32x4{pack2<DT>(a[0], a[1]), pack2<DT>(a[2], a[3]), pack2<DT>(a[4], a[5]), pack2<DT>(a[6], a[7])};
+        *(u32x4*)(o + u.p1) = u32x4{pack2<DT>(b[0], b[1]), pack2<DT>(b[2], b[3]), pack2<DT>(b[4], b[5]), pack2<DT>(b[6], b[7])};
+      } else {
+        o[u.p0] = f2act<DT>(a[0]);
+        o[u.p1] = f2act<DT>(b[0]);
+      }
+    }
+  };
+  fetch(tid);
+  if (tid < half) cs[tid] = cos_sin(pos * p.r.freqs[tid], p.r.magnitude);
+  __syncthreads();
+  put(tid);
+  for (int i0 = tid + 256 * N; i0 < all; i0 += 256 * N) {
+    fetch(i0);
+    put(i0);
   }
 }
 
-template <int FMT>
+template <int FMT, int D>
 static hipError_t append_launch(const KvAppendParams& p, hipStream_t st) {
-  const uint32_t run = (uint32_t)std::min(p.c.P, p.T) * (p.c.D + 1) * 4;
-  const uint32_t lds = std::max(run, (uint32_t)(p.q_tokens * p.r.rot / 2 * 8));
-  const auto go = [&](auto kern) {
-    const hipError_t e = allow_lds(kern, lds);
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(kern, dim3(p.kv_blocks + p.q_blocks), dim3(256), lds, st, p);
-    return hipGetLastError();
-  };
-  return p.r.rot % 16 == 0 ? go(k_kv_append<DTC, FMT, 8>) : go(k_kv_append<DTC, FMT, 1>);
+  const dim3 grid(p.kv_blocks + p.q_blocks);
+  if (p.r.rot % 16 == 0) hipLaunchKernelGGL((k_kv_append<DTC, FMT, D, 8>), grid, dim3(256), 0, st, p);
+  else hipLaunchKernelGGL((k_kv_append<DTC, FMT, D, 1>), grid, dim3(256), 0, st, p);
+  return hipGetLastError();
 }
 hipError_t SPEAR_D(launch_kv_append)(const KvAppendParams& p, int format, hipStream_t st) {
-  return format == KV_INT8 ? append_launch<KV_INT8>(p, st) : append_launch<KV_E4M3>(p, st);
+  if (p.c.D == 64) return format == KV_INT8 ? append_launch<KV_INT8, 64>(p, st) : append_launch<KV_E4M3, 64>(p, st);
+  return format == KV_INT8 ? append_launch<KV_INT8, 128>(p, st) : append_launch<KV_E4M3, 128>(p, st);
 }
 
 // ---------------------------------------------------------------------------

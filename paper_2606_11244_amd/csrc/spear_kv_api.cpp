@@ -7,6 +7,15 @@
 
 #include "spear_kv.h"
 
+#ifndef XWIN
+#define XWIN 4
+#endif
+#ifndef XRG
+#define XRG 384
+#define XRL 8
+#define XTG 256
+#define XTL 8
+#endif
 using namespace spear;
 
 namespace {
@@ -179,10 +188,10 @@ spear_status_t spear_kv_append(const spear_kv_cache_t* c, const spear_kv_append_
   p.q_out = (uint16_t*)a->q_out;
   p.q_ld = ql, p.k_ld = kl, p.v_ld = vl, p.qo_ld = ol;
   p.slots = a->slots, p.positions = a->positions;
-  p.window = T <= 1024 ? 1 : 4;
-  p.q_tokens = T <= 1024 ? 1 : 4;
-  p.kv_blocks = (uint32_t)((T + p.window - 1) / p.window * c->kv_heads * 2);
-  p.q_blocks = a->q ? (uint32_t)((T + p.q_tokens - 1) / p.q_tokens) : 0;
+  p.subs = (int)(T <= 1024 ? std::min<int64_t>(T, 64) : XWIN);
+  p.log2_page = __builtin_ctz((unsigned)c->page_tokens);
+  p.kv_blocks = (uint32_t)((T + 63) / 64 * p.subs * c->kv_heads * 2);
+  p.q_blocks = a->q ? (uint32_t)T : 0;
   const auto launch = c->act_dtype == SPEAR_F16 ? launch_kv_append_f16 : launch_kv_append_bf16;
   return hip_status(launch(p, c->format, (hipStream_t)hip_stream));
 }
@@ -225,7 +234,10 @@ spear_status_t check_attention(const spear_attention_t* a, bool buffers) {
 
 
 // Stretches wanted of each kernel, over all kv heads, and a stretch's least steps.
-constexpr int kRowsGoal = 512, kRowsLeast = 4, kTileGoal = 256, kTileLeast = 8;
+constexpr int kRowsGoal = XRG, kRowsLeast = XRL, kTileGoal = XTG, kTileLeast = XTL;
+// (stretches are shared out among kv heads only where there are fewer heads than the
+// goal, so that counters are at most 2 (goal + heads))
+static_assert(4 * kRowsGoal <= kAttnCounters && 4 * kTileGoal <= kAttnCounters, "a counter for each shared tile and head");
 
 // Where the plan's and the workspace's parts lie, from sizes alone.
 struct AttnLayout {
@@ -234,7 +246,7 @@ struct AttnLayout {
   size_t parts_rows, parts_tile, work_bytes;
 };
 // the sizes that a plan and the calls it serves have in common, as one number
-uint64_t plan_key(const spear_attention_t* a) {
+uint32_t plan_key(const spear_attention_t* a) {
   const spear_kv_cache_t* c = a->cache;
   const spear_kv_batch_t* b = a->batch;
   uint64_t h = 0xcbf29ce484222325ull;
@@ -242,7 +254,7 @@ uint64_t plan_key(const spear_attention_t* a) {
                           (int64_t)b->max_new, (int64_t)b->width, (int64_t)a->heads, (int64_t)a->window,
                           (int64_t)(a->prefix != nullptr)})
     for (int i = 0; i < 32; i += 8) h = (h ^ ((v >> i) & 255)) * 0x100000001b3ull;
-  return h;
+  return (uint32_t)(h ^ (h >> 32)) | 1u;
 }
 AttnLayout attention_layout(const spear_attention_t* a) {
   const spear_kv_cache_t* c = a->cache;
@@ -261,13 +273,14 @@ AttnLayout attention_layout(const spear_attention_t* a) {
   // and over those of more than one, ceil(steps / c) <= 2 steps / c
   z.part_rows = rows && z.goal_rows > 1 ? 2 * z.goal_rows : 0;
   z.part_tile = tile && z.goal_tile > 1 ? 2 * z.goal_tile : 0;
-  l.items_rows = sizeof(AttnHeader);
+  l.items_rows = 0;
   l.items_tile = l.items_rows + (size_t)z.max_rows * sizeof(AttnItem);
-  l.plan_bytes = l.items_tile + (size_t)z.max_tile * sizeof(AttnItem);
-  const size_t counters = ((size_t)(z.part_rows + z.part_tile) * hkv * 4 + 255) / 256 * 256;
-  l.parts_rows = counters;
+  l.plan_bytes = std::max<size_t>(sizeof(AttnItem), l.items_tile + (size_t)z.max_tile * sizeof(AttnItem));
+  // The counters have places of their own that every call of any sizes has in
+  // common: another call's partial results never lie on them.
+  l.parts_rows = 2 * kAttnCounters * sizeof(uint32_t);
   l.parts_tile = l.parts_rows + (size_t)z.part_rows * hkv * kRows * (c->head_dim + 2) * 4;
-  l.work_bytes = std::max<size_t>(256, l.parts_tile + (size_t)z.part_tile * hkv * kTileRows * (c->head_dim + 2) * 4);
+  l.work_bytes = (l.parts_tile + (size_t)z.part_tile * hkv * kTileRows * (c->head_dim + 2) * 4);
   return l;
 }
 
@@ -302,7 +315,6 @@ spear_status_t spear_attention_plan(const spear_attention_t* a, void* hip_stream
   p.key = plan_key(a);
   p.starts = b->starts, p.lens = b->lens, p.prefix = a->prefix;
   p.z = l.z;
-  p.head = (AttnHeader*)a->plan;
   p.items_rows = (AttnItem*)((char*)a->plan + l.items_rows);
   p.items_tile = (AttnItem*)((char*)a->plan + l.items_tile);
   return hip_status(launch_attention_plan(p, (hipStream_t)hip_stream));
@@ -343,10 +355,10 @@ spear_status_t spear_attention(const spear_attention_t* a, void* hip_stream) {
   p.q = (const uint16_t*)a->q, p.out = (uint16_t*)a->out;
   p.slopes = a->slopes, p.scale = a->scale, p.softcap = a->softcap;
   p.z = l.z;
-  p.head = (const AttnHeader*)a->plan;
   p.items_rows = (const AttnItem*)((const char*)a->plan + l.items_rows);
   p.items_tile = (const AttnItem*)((const char*)a->plan + l.items_tile);
-  p.counters = (uint32_t*)a->workspace;
+  p.counters_rows = (uint32_t*)a->workspace;
+  p.counters_tile = p.counters_rows + kAttnCounters;
   p.parts_rows = (float*)((char*)a->workspace + l.parts_rows);
   p.parts_tile = (float*)((char*)a->workspace + l.parts_tile);
   const bool f16 = c->act_dtype == SPEAR_F16;

@@ -40,8 +40,8 @@ struct KvAppendParams {
   uint16_t* q_out;
   int64_t q_ld, k_ld, v_ld, qo_ld;
   const int32_t *slots, *positions;
-  int window;        // run starts a workgroup of the cache's part looks for
-  int q_tokens;      // tokens a workgroup of the queries' part takes
+  int log2_page;
+  int subs;  // workgroups that share the runs of a window of 64 tokens
   uint32_t kv_blocks, q_blocks;
 };
 
@@ -57,19 +57,16 @@ struct KvReadParams {
 // to k_attend_rows where they are at most kRows, else to k_attend_tile in tiles of
 // kTileRows. Either walks the cache in steps of kStep tokens.
 constexpr int kRows = 16, kTileRows = 256, kStep = 64;
+constexpr int kAttnCounters = 2048;  // of each kernel
 
 // one workgroup's share (of each kv head): some rows over some steps
 struct AttnItem {
+  uint32_t key;                   // of the sizes the plan was made for (0: none); a call of others does nothing
   int32_t r, row0, rows, pos0;    // request, its first row of the step, its rows, position of the first
   int32_t tile, s0, s1, splits;   // tile of its rows; steps; stretches the tile's steps are cut into
   int32_t split, part, first, end;  // which; the first one's place among the partial results (splits > 1);
                                   // tokens some row sees: first..end-1 and 0..prefix-1
-  int32_t prefix, pad[3];
-};
-struct AttnHeader {
-  uint64_t key;            // of the sizes that it was made for: a call of others does nothing
-  int32_t n_rows, n_tile;  // items of each kernel
-  int32_t pad[12];
+  int32_t prefix, pad[2];
 };
 
 // sizes that the host fixes from the batch's and the heads' sizes alone
@@ -82,17 +79,16 @@ struct AttnShape {
 
 struct AttnPlanParams {
   int R, T, P, Hkv, group, max_new, width, window, pages;
-  uint64_t key;
+  uint32_t key;
   const int32_t *starts, *lens, *prefix;
   AttnShape z;
-  AttnHeader* head;
   AttnItem *items_rows, *items_tile;
 };
 
 struct AttnParams {
   KvCache c;
   int group, window, log2_page;  // window: kKvLength for none
-  uint64_t key;
+  uint32_t key;
   int64_t ld, q_ld, out_ld;
   const int32_t* table;
   const uint16_t* q;
@@ -100,9 +96,8 @@ struct AttnParams {
   const float* slopes;
   float scale, softcap;
   AttnShape z;
-  const AttnHeader* head;
   const AttnItem *items_rows, *items_tile;
-  uint32_t* counters;            // [part_rows + part_tile][Hkv]
+  uint32_t *counters_rows, *counters_tile;  // [part][Hkv]: kAttnCounters each
   float *parts_rows, *parts_tile;  // [part][Hkv][rows of O, their maxima, their sums]
 };
 

@@ -540,6 +540,25 @@ def test_a_captured_step_serves_other_lengths():
             torch.randn(1000, device="cuda").sum().item()
 
 
+def test_calls_of_unlike_sizes_share_a_workspace():
+    """Stretches joined by both kernels, of other head counts and batches, one workspace in turn: what one
+    call leaves there is nothing to the next."""
+    act, codes = torch.bfloat16, torch.int8
+    setups = [Setup([(1, 5000)], 16, 1, 64, 64, act, codes), Setup([(70, 3000), (1, 2000)], 16, 2, 128, 64, act, codes),
+              Setup([(1, 4000)] * 3, 8, 4, 128, 64, act, codes), Setup([(300, 2500)], 4, 4, 64, 64, act, codes)]
+    ws = max((s.ws for s in setups), key=torch.Tensor.numel)
+    want = []
+    for s in setups:
+        s.check()
+        want.append(s.out.clone())
+        s.ws = ws
+    ws.zero_()
+    for order in ([0, 1, 2, 3], [3, 0, 1], [2, 1, 0], [1, 1, 3, 0]):
+        for i in order:
+            setups[i].out.fill_(9.0)
+            assert torch.equal(setups[i].run(), want[i]), i
+
+
 def test_other_streams():
     s = Server(3, 90, 40)
     stream = torch.cuda.Stream()
