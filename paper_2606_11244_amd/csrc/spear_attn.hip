@@ -257,6 +257,16 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
     return pack_bf16(a, b);
 }
 
+// the larger of the two halves of a wave, and of its four sixteens
+__device__ __forceinline__ float max_halves(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float max_sixteens(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return max_halves(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+
 // A score in powers of two. OPT: capped, or biased by distance.
 struct ScoreOptions {
   float scale, cap, slope2;  // slope2: slope times log2 e
@@ -331,14 +341,18 @@ __global__ __launch_bounds__(64 * W, 2) void k_attend_rows(AttnParams p) {
   const int pos = it.pos0 + i, pos_max = it.pos0 + it.rows - 1;
   const ScoreOptions opt{fabsf(p.scale), p.softcap, OPT && p.slopes ? p.slopes[hq] * kLog2e : 0.f};
   const int32_t* table = p.table + it.r * p.ld;
-  const int64_t page_bytes = (int64_t)P * D;
+  const uint32_t page_bytes = P * D, pool_bytes = p.c.Hkv * page_bytes;
+  const uint8_t *k_head = p.c.k + (int64_t)head * page_bytes, *v_head = p.c.v + (int64_t)head * page_bytes;
 
-  // the page of the lane's run of 16 tokens, run g
-  auto page_at = [&](int s) {
+  // the table's entry of the lane's run of 16 tokens, run g, and whether it is a page
+  // (looked at only where it is used: a comparison here would wait for the load)
+  auto entry_at = [&](int s) {
     const int j = s * kStep + 16 * g;
-    const int page = s < it.s1 && j < it.end ? table[j >> p.log2_page] : -1;
-    return page >= 0 && page < p.c.pages ? page : -1;
+    int page = -1;
+    if (s < it.s1 && j < it.end) page = table[j >> p.log2_page];
+    return page;
   };
+  auto page_of = [&](int entry) { return (uint32_t)entry < (uint32_t)p.c.pages ? entry : -1; };
   // K straight to LDS, a KB an instruction from tokens that lie side by side; the
   // pieces of token t stand in the order piece ^ turn(t), so that the sixteen tokens
   // that a sixteen of lanes reads lie in different banks
@@ -350,7 +364,7 @@ __global__ __launch_bounds__(64 * W, 2) void k_attend_rows(AttnParams p) {
     for (int x = 0; x < kStep / TOKENS; ++x) {
       const int run = x * TOKENS / 16, in_run = x * TOKENS % 16 + lane / PIECES;
       const int pg = max(__builtin_amdgcn_readlane(page, 16 * run), 0);
-      const uint8_t* k = p.c.k + ((int64_t)pg * p.c.Hkv + head) * page_bytes + ((s * kStep + 16 * run) & (P - 1)) * D;
+      const uint8_t* k = k_head + (uint64_t)pg * pool_bytes + ((s * kStep + 16 * run) & (P - 1)) * D;
       const uint8_t* from = k + (in_run * D + 16 * ((lane % PIECES) ^ turn(16 * run + in_run)));
       __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
                                        (__attribute__((address_space(3))) void*)(s_k + 1024 * x), 16, 0, 2);
@@ -359,7 +373,7 @@ __global__ __launch_bounds__(64 * W, 2) void k_attend_rows(AttnParams p) {
   u32x4 vr[DTILES], vn[DTILES];  // V of this step, and of the next
   auto load_v = [&](u32x4 (&vr)[DTILES], int s, int page) {
     const int at = (s * kStep + 16 * g) & (P - 1);
-    const uint8_t* v = p.c.v + ((int64_t)max(page, 0) * p.c.Hkv + head) * page_bytes + c * P + at;
+    const uint8_t* v = v_head + (uint64_t)(uint32_t)max(page, 0) * pool_bytes + (c * P + at);
 #pragma unroll
     for (int d = 0; d < DTILES; ++d) vr[d] = __builtin_nontemporal_load((const u32x4*)(v + d * 16 * P));
   };
@@ -372,12 +386,13 @@ __global__ __launch_bounds__(64 * W, 2) void k_attend_rows(AttnParams p) {
   float m = kLowest, l = 0.f;
   int s = it.s0 + wave;
   if (s < it.s1) {
-    int page = page_at(s), next, after = -1;
+    int page = page_of(entry_at(s)), next, entry;
     float2 sn = {};
     load_k(s, page);
     float2 sc = scales(page);
     load_v(vr, s, page);
-    next = page_at(s + W);
+    next = page;
+    entry = entry_at(s + W);
     for (; s < it.s1; s += W) {
       f32x4 st[4] = {};
 #pragma unroll
@@ -393,10 +408,11 @@ __global__ __launch_bounds__(64 * W, 2) void k_attend_rows(AttnParams p) {
       const bool more = s + W < it.s1;
       if (more) {
         __builtin_amdgcn_s_waitcnt(0xC07F);  // this wave's reads of K have left LDS (lgkmcnt 0)
+        next = page_of(entry);
         load_k(s + W, next);
         load_v(vn, s + W, next);
         sn = scales(next);
-        after = page_at(s + 2 * W);
+        entry = entry_at(s + 2 * W);
       }
       const int j0 = s * kStep + 16 * g;
       // every row sees every token of the step, all pages are there
@@ -423,8 +439,7 @@ __global__ __launch_bounds__(64 * W, 2) void k_attend_rows(AttnParams p) {
       float top = w[0];
 #pragma unroll
       for (int e = 1; e < 16; ++e) top = fmaxf(top, w[e]);
-      top = fmaxf(top, __shfl_xor(top, 16));
-      top = fmaxf(top, __shfl_xor(top, 32));
+      top = max_sixteens(top);
       if (__any(top > m + kSlack)) {
         const float now = fmaxf(m, top), fade = __builtin_amdgcn_exp2f(m - now);
         m = now;
@@ -451,7 +466,7 @@ __global__ __launch_bounds__(64 * W, 2) void k_attend_rows(AttnParams p) {
         o[d] = mfma16<DT>(v_operand8<DT, FMT>(vr[d][0], vr[d][1], f.x), pw[0], o[d]);
         o[d] = mfma16<DT>(v_operand8<DT, FMT>(vr[d][2], vr[d][3], f.x), pw[1], o[d]);
       }
-      page = next, next = after, sc = sn;
+      page = next, sc = sn;
 #pragma unroll
       for (int d = 0; d < DTILES; ++d) vr[d] = vn[d];
     }
@@ -566,13 +581,13 @@ __global__ __launch_bounds__(512) void k_attend_tile(AttnParams p) {
   constexpr int KP = D * 2 + 16, VP = kStep * 2 + 16, PIECES = D / 16;  // pitches in bytes; pieces of a row of K
   constexpr int KBYTES = kStep * KP, BUF = KBYTES + D * VP;
   __shared__ __attribute__((aligned(16))) char lds[2 * BUF];
-  __shared__ float s_ks[2][4], s_vf[2][4];
+  __shared__ float s_ks[2][4];
   __shared__ int s_last;
   const int head = blockIdx.x % p.c.Hkv, idx = blockIdx.x / p.c.Hkv;
   AttnItem it = p.items_tile[idx];
   if (it.key != p.key) return;
   if (p.c.pages == 0) it.s1 = it.s0;
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, c = lane & 31, h = lane >> 5;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c = lane & 31, h = lane >> 5;
   const int P = p.c.P, live_rows = it.rows * p.group, wave_row = it.tile * kTileRows + 32 * wave;
   const int row = wave_row + c;
   const bool active = wave_row < live_rows, mine = row < live_rows;
@@ -592,29 +607,33 @@ __global__ __launch_bounds__(512) void k_attend_tile(AttnParams p) {
   const int pos_lo = it.pos0 + min(wave_row / p.group, it.rows - 1), pos_hi = it.pos0 + min((wave_row + 31) / p.group, it.rows - 1);
   const ScoreOptions opt{fabsf(p.scale), p.softcap, OPT && p.slopes ? p.slopes[hq] * kLog2e : 0.f};
   const int32_t* table = p.table + it.r * p.ld;
-  const int64_t page_bytes = (int64_t)P * D;
+  const uint32_t page_bytes = P * D, pool_bytes = p.c.Hkv * page_bytes;
 
   // staging: K by threads of (token, piece), V by threads of (feature, run); D = 64
   // has half as many pieces, K's in the first half of the workgroup, V's in the other
   const bool does_k = D == 128 || tid < 256, does_v = D == 128 || tid >= 256;
   const int k_token = (tid / PIECES) & 63, k_piece = tid % PIECES, v_feature = (tid >> 2) % D, v_run = tid & 3;
-  auto page_at = [&](int s, int run) {
+  const uint8_t* k_head = p.c.k + (int64_t)head * page_bytes + 16 * k_piece;
+  const uint8_t* v_head = p.c.v + (int64_t)head * page_bytes + v_feature * P;
+  // table entries of a step's runs; whether they are pages is looked at where they are
+  // used (a comparison here would wait for the load)
+  auto entry_at = [&](int s, int run) {
     const int j = s * kStep + 16 * run;
-    const int page = s < it.s1 && j < it.end ? table[j >> p.log2_page] : -1;
-    return page >= 0 && page < p.c.pages ? page : -1;
+    int page = -1;
+    if (s < it.s1 && j < it.end) page = table[j >> p.log2_page];
+    return page;
   };
+  auto page_of = [&](int entry) { return (uint32_t)entry < (uint32_t)p.c.pages ? entry : -1; };
   u32x4 kr, vr;
   float2 sc;  // scales of this thread's run of V
-  int page_k = 0, page_v = 0, held_v = 0;
-  auto fetch = [&](int s) {  // pages of s are in page_k, page_v; those of s + 1 follow
-    if (does_k)
-      kr = ldg16(p.c.k + ((int64_t)max(page_k, 0) * p.c.Hkv + head) * page_bytes + ((s * kStep + k_token) & (P - 1)) * D + 16 * k_piece);
-    if (does_v)
-      vr = ldg16(p.c.v + ((int64_t)max(page_v, 0) * p.c.Hkv + head) * page_bytes + v_feature * P + ((s * kStep + 16 * v_run) & (P - 1)));
-    const int64_t ph = (int64_t)max(page_v, 0) * p.c.Hkv + head;
+  int entry_k = 0, entry_v = 0, held_v = 0;
+  auto fetch = [&](int s) {  // entries of s are there; those of s + 1 follow
+    const uint32_t page_k = max(page_of(entry_k), 0), page_v = max(held_v = page_of(entry_v), 0);
+    if (does_k) kr = ldg16(k_head + (uint64_t)page_k * pool_bytes + ((s * kStep + k_token) & (P - 1)) * D);
+    if (does_v) vr = ldg16(v_head + (uint64_t)page_v * pool_bytes + ((s * kStep + 16 * v_run) & (P - 1)));
+    const uint64_t ph = (uint64_t)page_v * p.c.Hkv + head;
     sc = make_float2(p.c.k_scale[ph], p.c.v_scale[ph]);
-    held_v = page_v;
-    page_k = page_at(s + 1, k_token >> 4), page_v = page_at(s + 1, v_run);
+    entry_k = entry_at(s + 1, k_token >> 4), entry_v = entry_at(s + 1, v_run);
   };
   auto stage = [&](int s) {
     char* buf = lds + (s & 1) * BUF;
@@ -623,34 +642,31 @@ __global__ __launch_bounds__(512) void k_attend_tile(AttnParams p) {
       k[0] = operand8<DT, FMT>(kr[0], kr[1], 1.f);
       k[1] = operand8<DT, FMT>(kr[2], kr[3], 1.f);
     }
-    float2 f = make_float2(sc.y, 1.f);
-    if constexpr (DT == DT_F16) f = v_factors<DT, FMT>(sc.y);
+    float f = sc.y;
     const int j0 = s * kStep + 16 * v_run;
     if (held_v < 0 || j0 + 16 > it.end || j0 < it.first) {
       const u32x4 seen = held_v >= 0 ? seen_bytes(j0, it) : u32x4{0, 0, 0, 0};
       vr &= seen;
-      if (!(seen[0] | seen[1] | seen[2] | seen[3])) f = make_float2(1.f, 1.f);
+      if (!(seen[0] | seen[1] | seen[2] | seen[3])) f = 1.f;
     }
     if (does_v) {
       u32x4* v = (u32x4*)(buf + KBYTES + v_feature * VP + 32 * v_run);
       u32x4 a, b;
-      if constexpr (DT != DT_F16 && FMT == KV_INT8) {
-        a = i8x8_to_act<DT>(vr[0], vr[2], f.x), b = i8x8_to_act<DT>(vr[1], vr[3], f.x);
+      if (FMT == KV_INT8 && (DT != DT_F16 || f < 6.103515625e-5f)) {  // (fp16: a scale below its normal range)
+        a = i8x8_to_act<DT>(vr[0], vr[2], f), b = i8x8_to_act<DT>(vr[1], vr[3], f);
       } else {
-        a = v_operand8<DT, FMT>(vr[0], vr[2], f.x), b = v_operand8<DT, FMT>(vr[1], vr[3], f.x);
+        a = v_operand8<DT, FMT>(vr[0], vr[2], f), b = v_operand8<DT, FMT>(vr[1], vr[3], f);
       }
       v[0] = a, v[1] = b;
     }
-    if (tid >= 256 && tid < 260) {  // (runs 0..3) no page: a scale that is no number, for the waves to see
+    if (tid >= 256 && tid < 260)  // (runs 0..3) no page: a scale that is no number, for the waves to see
       s_ks[s & 1][v_run] = held_v >= 0 ? sc.x : __builtin_nanf("");
-      s_vf[s & 1][v_run] = f.y;
-    }
   };
 
   f32x16 o[D / 32] = {};
   float m = kLowest, l = 0.f;
   if (it.s0 < it.s1) {
-    page_k = page_at(it.s0, k_token >> 4), page_v = page_at(it.s0, v_run);
+    entry_k = entry_at(it.s0, k_token >> 4), entry_v = entry_at(it.s0, v_run);
     fetch(it.s0);
     stage(it.s0);
     if (it.s0 + 1 < it.s1) fetch(it.s0 + 1);
@@ -672,10 +688,10 @@ __global__ __launch_bounds__(512) void k_attend_tile(AttnParams p) {
 #pragma unroll
         for (int t = 0; t < 2; ++t)
           st[t] = mfma32<DT>(*(const u32x4*)(buf + (32 * t + c) * KP + 32 * x + 16 * h), q[x], st[t]);
-      float ks[4], vf[4];
+      float ks[4];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) ks[r] = s_ks[s & 1][r], vf[r] = s_vf[s & 1][r];
-      const bool pages_there = ks[0] == ks[0] && ks[1] == ks[1] && ks[2] == ks[2] && ks[3] == ks[3];
+      for (int r = 0; r < 4; ++r) ks[r] = s_ks[s & 1][r];
+      const bool pages_there = __all(ks[0] == ks[0] && ks[1] == ks[1] && ks[2] == ks[2] && ks[3] == ks[3]);
       const bool whole = j0 + kStep <= min(it.end, pos_lo + 1) && pos_hi - j0 < p.window && pages_there;
       // scores in powers of two; where every row sees every token, still without K's scale
       float w[2][16], f[4], top;
@@ -706,7 +722,7 @@ __global__ __launch_bounds__(512) void k_attend_tile(AttnParams p) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) f[r] = 1.f;
       }
-      top = fmaxf(top, __shfl_xor(top, 32));
+      top = max_halves(top);
       if (__any(top > m + kSlack)) {
         const float now = fmaxf(m, top), fade = __builtin_amdgcn_exp2f(m - now);
         m = now;
@@ -722,10 +738,6 @@ __global__ __launch_bounds__(512) void k_attend_tile(AttnParams p) {
         sum += x;
       }
       l += sum;
-      if (DT == DT_F16 && !(vf[0] == 1.f && vf[1] == 1.f && vf[2] == 1.f && vf[3] == 1.f)) {
-#pragma unroll
-        for (int e = 0; e < 32; ++e) w[e >> 4][e & 15] *= vf[e >> 3];
-      }
 #pragma unroll
       for (int y = 0; y < 4; ++y) {  // sixteen tokens
         u32x4 pw;
