@@ -100,7 +100,7 @@ __global__ __launch_bounds__(kPlanThreads) void k_attention_plan(AttnPlanParams 
     if (it.rows == 0) continue;
     const int64_t rows = (int64_t)it.rows * p.group;
     if (rows <= kRows) sum += steps[e] = plan_range(p, it, 0, it.rows);
-    else tile_sum += tiles[e] = (int)((rows + kTileRows - 1) / kTileRows);
+    else tile_sum += tiles[e] = (int)((rows + p.z.tile_rows - 1) / p.z.tile_rows);
   }
   plan_scan(sum, red, &total);
   const int c = max(p.z.least_rows, (int)((total + p.z.goal_rows - 1) / p.z.goal_rows));
@@ -169,8 +169,8 @@ __global__ __launch_bounds__(kPlanThreads) void k_attention_plan(AttnPlanParams 
     const int r = plan_find(s_tile, p.R, t);
     it = plan_request(p, r);
     it.tile = t - s_tile[r];
-    const int i0 = it.tile * kTileRows / p.group;
-    return plan_range(p, it, i0, min(it.rows, (it.tile * kTileRows + kTileRows - 1) / p.group + 1));
+    const int i0 = it.tile * p.z.tile_rows / p.group;
+    return plan_range(p, it, i0, min(it.rows, (it.tile * p.z.tile_rows + p.z.tile_rows - 1) / p.group + 1));
   };
   sum = 0;
   AttnItem it;
@@ -568,6 +568,299 @@ __global__ __launch_bounds__(64 * W, 2) void k_attend_rows(AttnParams p) {
 }
 
 // ---------------------------------------------------------------------------
+// Tiles of 64 rows (some new tokens, chunks too few to fill the GPU in tiles of
+// 256): as k_attend_rows, four waves with a step each in turn, K by way of LDS, V in
+// registers, on 32 x 32 x 16 MFMAs for two halves of 32 rows that share the operands
+// made of a code. The order in which K's tokens are read from LDS is that which
+// leaves a lane the scores of sixteen tokens side by side, run 2t + h of the step.
+// Bound: the conversions and exponentials beside the MFMAs.
+// ---------------------------------------------------------------------------
+template <int DT, int FMT, int D, bool OPT>
+__global__ __launch_bounds__(256, 2) void k_attend_mid(AttnParams p) {
+  constexpr int W = 4, Y = kMidRows / 32, DTILES = D / 32, KX = D / 32, PITCH = D + 4, KBYTES = kStep * D;
+  constexpr int LDS = std::max(W * KBYTES, W * kMidRows * PITCH * 4);
+  __shared__ __attribute__((aligned(16))) char lds[LDS];  // K of each wave's step; then each wave's O
+  __shared__ float s_m[W * kMidRows], s_l[W * kMidRows];
+  __shared__ int s_last;
+  float* s_o = (float*)lds;
+  const int head = blockIdx.x % p.c.Hkv, idx = blockIdx.x / p.c.Hkv;
+  AttnItem it = p.items_tile[idx];
+  if (it.key != p.key) return;
+  if (p.c.pages == 0) it.s1 = it.s0;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c = lane & 31, h = lane >> 5;
+  const int P = p.c.P, tile_row = it.tile * kMidRows, live_rows = min(it.rows * p.group - tile_row, kMidRows);
+  const uint32_t sign = p.scale < 0.f ? 0x80008000u : 0u;  // (a scale below zero: of q)
+  const float scale = fabsf(p.scale);
+  u32x4 q[Y][2 * KX];
+  int pos[Y];
+  float slope2[Y];
+#pragma unroll
+  for (int y = 0; y < Y; ++y) {
+    const bool mine = 32 * y + c < live_rows;
+    const int row = tile_row + (mine ? 32 * y + c : 0), i = row / p.group, hq = head * p.group + row % p.group;
+    const uint16_t* qp = p.q + (int64_t)(it.row0 + i) * p.q_ld + hq * D + 16 * h;
+#pragma unroll
+    for (int x = 0; x < 2 * KX; ++x) {
+      q[y][x] = ldg16(qp + 32 * (x >> 1) + 8 * (x & 1)) ^ sign;
+      if (!mine) q[y][x] = u32x4{0, 0, 0, 0};
+    }
+    pos[y] = it.pos0 + i;
+    slope2[y] = OPT && p.slopes ? p.slopes[hq] * kLog2e : 0.f;
+  }
+  const int pos_lo = it.pos0 + tile_row / p.group, pos_hi = it.pos0 + (tile_row + live_rows - 1) / p.group;
+  const int32_t* table = p.table + it.r * p.ld;
+  const uint32_t page_bytes = P * D, pool_bytes = p.c.Hkv * page_bytes;
+  const uint8_t *k_head = p.c.k + (int64_t)head * page_bytes, *v_head = p.c.v + (int64_t)head * page_bytes;
+
+  // table entry of run lane / 16; pages of all four runs, uniform
+  auto entry_at = [&](int s) {
+    const int j = s * kStep + 16 * (lane >> 4);
+    int page = -1;
+    if (s < it.s1 && j < it.end) page = table[j >> p.log2_page];
+    return page;
+  };
+  struct Pages {
+    int at[4];
+  };
+  auto pages_of = [&](int entry) {
+    Pages r;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const int e = __builtin_amdgcn_readlane(entry, 16 * x);
+      r.at[x] = (uint32_t)e < (uint32_t)p.c.pages ? e : -1;
+    }
+    return r;
+  };
+  // K to LDS as in k_attend_rows; here the sixteen tokens that a sixteen of lanes reads
+  // are four times four, 4 and 16 apart
+  auto turn = [](int t) { return D == 128 ? ((t >> 1) & 3) | ((t >> 4) & 1) << 2 : ((t >> 2) & 1) | ((t >> 4) & 1) << 1; };
+  char* const s_k = lds + wave * KBYTES;
+  constexpr int PIECES = D / 16, TOKENS = 64 / PIECES;
+  auto load_k = [&](int s, const Pages& pg) {
+#pragma unroll
+    for (int x = 0; x < kStep / TOKENS; ++x) {
+      const int run = x * TOKENS / 16, in_run = x * TOKENS % 16 + lane / PIECES;
+      const uint8_t* k = k_head + (uint64_t)(uint32_t)max(pg.at[run], 0) * pool_bytes + ((s * kStep + 16 * run) & (P - 1)) * D;
+      const uint8_t* from = k + (in_run * D + 16 * ((lane % PIECES) ^ turn(16 * run + in_run)));
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
+                                       (__attribute__((address_space(3))) void*)(s_k + 1024 * x), 16, 0, 0);
+    }
+  };
+  u32x4 vr[2][DTILES];  // V of this step, run 2t + h
+  auto load_v = [&](int s, const Pages& pg) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int page = max(h ? pg.at[2 * t + 1] : pg.at[2 * t], 0), at = (s * kStep + 32 * t + 16 * h) & (P - 1);
+      const uint8_t* from = v_head + (uint64_t)(uint32_t)page * pool_bytes + (c * P + at);
+#pragma unroll
+      for (int d = 0; d < DTILES; ++d) vr[t][d] = ldg16(from + d * 32 * P);
+    }
+  };
+  struct Scales {
+    float2 at[2];
+  };
+  auto scales = [&](const Pages& pg) {
+    Scales r;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const uint64_t ph = (uint64_t)(uint32_t)max(h ? pg.at[2 * t + 1] : pg.at[2 * t], 0) * p.c.Hkv + head;
+      r.at[t] = make_float2(p.c.k_scale[ph], p.c.v_scale[ph]);
+    }
+    return r;
+  };
+
+  f32x16 o[Y][DTILES] = {};
+  float m[Y], l[Y];
+#pragma unroll
+  for (int y = 0; y < Y; ++y) m[y] = kLowest, l[y] = 0.f;
+  int s = it.s0 + wave;
+  if (s < it.s1) {
+    Pages page = pages_of(entry_at(s)), next = page;
+    load_k(s, page);
+    Scales sc = scales(page), sn = sc;
+    int entry = entry_at(s + W);
+    for (; s < it.s1; s += W) {
+      f32x16 st[Y][2] = {};  // [half of the rows][32 tokens]
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const int token = 32 * t + 16 * ((c >> 2) & 1) + 4 * (c >> 3) + (c & 3);
+#pragma unroll
+        for (int x = 0; x < KX; ++x) {
+          const u32x4 k = *(const u32x4*)(s_k + token * D + 16 * ((2 * x + h) ^ turn(token)));
+          const u32x4 a = operand8<DT, FMT>(k[0], k[1], 1.f), b = operand8<DT, FMT>(k[2], k[3], 1.f);
+#pragma unroll
+          for (int y = 0; y < Y; ++y) st[y][t] = mfma32<DT>(a, q[y][2 * x], st[y][t]);
+#pragma unroll
+          for (int y = 0; y < Y; ++y) st[y][t] = mfma32<DT>(b, q[y][2 * x + 1], st[y][t]);
+        }
+      }
+      load_v(s, page);
+      const bool more = s + W < it.s1;
+      if (more) {
+        __builtin_amdgcn_s_waitcnt(0xC07F);  // this wave's reads of K have left LDS (lgkmcnt 0)
+        next = pages_of(entry);
+        load_k(s + W, next);
+        sn = scales(next);
+        entry = entry_at(s + 2 * W);
+      }
+      const int j0 = s * kStep;
+      const bool whole = j0 + kStep <= min(it.end, pos_lo + 1) && pos_hi - j0 < p.window &&
+                         (page.at[0] | page.at[1] | page.at[2] | page.at[3]) >= 0;
+      float2 f[2] = {v_factors<DT, FMT>(sc.at[0].y), v_factors<DT, FMT>(sc.at[1].y)};
+      u32x4 seen[2];
+      if (!whole) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const int there = h ? page.at[2 * t + 1] : page.at[2 * t];
+          seen[t] = seen_bytes(j0 + 32 * t + 16 * h, it);
+          if (there < 0) seen[t] = u32x4{0, 0, 0, 0};
+          if (!(seen[t][0] | seen[t][1] | seen[t][2] | seen[t][3])) f[t] = make_float2(1.f, 1.f);
+#pragma unroll
+          for (int d = 0; d < DTILES; ++d) vr[t][d] &= seen[t];
+        }
+      }
+      u32x4 pw[Y][4];  // weights: [half of the rows][eight tokens of either run]
+#pragma unroll
+      for (int y = 0; y < Y; ++y) {
+        float g[2], top;
+        if (whole && !OPT) {
+          top = kLowest;
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            g[t] = sc.at[t].x * (scale * kLog2e);
+            float x = st[y][t][0];
+#pragma unroll
+            for (int e = 1; e < 16; ++e) x = fmaxf(x, st[y][t][e]);
+            top = fmaxf(top, x * g[t]);
+          }
+        } else {
+          const ScoreOptions opt{scale, p.softcap, slope2[y]};
+          top = -__builtin_inff();
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const int j = j0 + 32 * t + 16 * h + e;
+              const float x = score2<OPT>(st[y][t][e], sc.at[t].x, opt, pos[y], j);
+              const bool sees = whole || (((seen[t][e >> 2] >> (8 * (e & 3))) & 1) &
+                                          (((j <= pos[y]) & (pos[y] - j < p.window)) | (j < it.prefix)));
+              st[y][t][e] = sees ? x : -__builtin_inff();
+              top = fmaxf(top, st[y][t][e]);
+            }
+          g[0] = g[1] = 1.f;
+        }
+        top = max_halves(top);
+        if (__any(top > m[y] + kSlack)) {
+          const float now = fmaxf(m[y], top), fade = __builtin_amdgcn_exp2f(m[y] - now);
+          m[y] = now;
+          l[y] *= fade;
+#pragma unroll
+          for (int d = 0; d < DTILES; ++d) o[y][d] *= fade;
+        }
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          float w[16];
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            w[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[y][t][e], g[t], -m[y]));
+            l[y] += w[e];
+          }
+          if ((DT != DT_F16 && FMT == KV_INT8) || (DT == DT_F16 && __any(f[t].y != 1.f))) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) w[e] *= f[t].y;
+          }
+#pragma unroll
+          for (int e = 0; e < 8; ++e) pw[y][2 * t + (e >> 2)][e & 3] = pack2<DT>(w[2 * e], w[2 * e + 1]);
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int d = 0; d < DTILES; ++d) {
+          const u32x4 a = v_operand8<DT, FMT>(vr[t][d][0], vr[t][d][1], f[t].x), b = v_operand8<DT, FMT>(vr[t][d][2], vr[t][d][3], f[t].x);
+#pragma unroll
+          for (int y = 0; y < Y; ++y) o[y][d] = mfma32<DT>(a, pw[y][2 * t], o[y][d]);
+#pragma unroll
+          for (int y = 0; y < Y; ++y) o[y][d] = mfma32<DT>(b, pw[y][2 * t + 1], o[y][d]);
+        }
+      page = next, sc = sn;
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int y = 0; y < Y; ++y) {
+    l[y] += __shfl_xor(l[y], 32);
+    const int at = wave * kMidRows + 32 * y + c;
+#pragma unroll
+    for (int d = 0; d < DTILES; ++d)
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+        *(f32x4*)&s_o[at * PITCH + 32 * d + 8 * x + 4 * h] = f32x4{o[y][d][4 * x], o[y][d][4 * x + 1], o[y][d][4 * x + 2], o[y][d][4 * x + 3]};
+    if (h == 0) s_m[at] = m[y], s_l[at] = l[y];
+  }
+  __syncthreads();
+  // a thread: a row, every EACH-th of its runs of four features
+  constexpr int EACH = 256 / kMidRows, F = D / 4 / EACH;
+  const int row = tid / EACH, own = tid % EACH;
+  f32x4 x[F] = {};
+  float top = kLowest, total = 0.f;
+  auto add = [&](float pm, float pl, const f32x4 (&v)[F]) {
+    const float now = fmaxf(top, pm), f0 = __builtin_amdgcn_exp2f(top - now), f1 = __builtin_amdgcn_exp2f(pm - now);
+    top = now;
+    total = total * f0 + pl * f1;
+#pragma unroll
+    for (int e = 0; e < F; ++e) x[e] = x[e] * f0 + v[e] * f1;
+  };
+#pragma unroll
+  for (int v = 0; v < W; ++v) {
+    f32x4 y[F];
+#pragma unroll
+    for (int e = 0; e < F; ++e) y[e] = *(const f32x4*)&s_o[(v * kMidRows + row) * PITCH + 4 * (EACH * e + own)];
+    add(s_m[v * kMidRows + row], s_l[v * kMidRows + row], y);
+  }
+  if (it.splits > 1) {
+    const uint32_t size = kMidRows * (D + 2) * 4, slot = (uint32_t)it.part * p.c.Hkv + head, stride = p.c.Hkv * size;
+    const rsrc_t r = make_rsrc((const char*)p.parts_tile + (size_t)slot * size, (uint32_t)((it.splits - 1) * p.c.Hkv + 1) * size);
+    const uint32_t at = (uint32_t)it.split * stride, mine = (row * D + 4 * own) * 4, mine_m = (kMidRows * D + row) * 4;
+    if (row < live_rows) {
+#pragma unroll
+      for (int e = 0; e < F; ++e) bst128c(r, at + mine + 16 * EACH * e, x[e]);
+      float* ml = p.parts_tile + ((size_t)slot * size + at + mine_m) / 4;
+      if (own == 0) st_agent(ml, top), st_agent(ml + kMidRows, total);
+    }
+    complete_and_sync();
+    if (tid == 0) s_last = arrive_last(p.counters_tile + slot, it.splits);
+    __syncthreads();
+    if (!s_last) return;
+    top = kLowest, total = 0.f;
+#pragma unroll
+    for (int e = 0; e < F; ++e) x[e] = f32x4{};
+    constexpr int N = 4;  // stretches in flight, joined in order
+    for (int b = 0; b < it.splits; b += N) {
+      f32x4 v[N][F];
+      float pm[N], pl[N];
+#pragma unroll
+      for (int y = 0; y < N; ++y) {
+        const uint32_t off = b + y < it.splits && row < live_rows ? (b + y) * stride : kOOB;
+        pm[y] = __uint_as_float(bld32c(r, off + mine_m));
+        pl[y] = __uint_as_float(bld32c(r, off + mine_m + kMidRows * 4));
+#pragma unroll
+        for (int e = 0; e < F; ++e) v[y][e] = bld128cf(r, off + mine + 16 * EACH * e);
+      }
+#pragma unroll
+      for (int y = 0; y < N; ++y)
+        if (b + y < it.splits) add(pm[y], pl[y], v[y]);
+    }
+  }
+  if (row >= live_rows) return;
+  const float inv = total > 0.f ? 1.f / total : 0.f;
+  const int i = (tile_row + row) / p.group, hq = head * p.group + (tile_row + row) % p.group;
+  uint16_t* out = p.out + (int64_t)(it.row0 + i) * p.out_ld + hq * D + 4 * own;
+#pragma unroll
+  for (int e = 0; e < F; ++e) *(u32x2*)(out + 4 * EACH * e) = u32x2{pack2<DT>(x[e][0] * inv, x[e][1] * inv), pack2<DT>(x[e][2] * inv, x[e][3] * inv)};
+}
+
+// ---------------------------------------------------------------------------
 // Tiles of 256 rows (prompts, chunks): eight waves of 32 rows. All waves bring a
 // step's codes to LDS as operands (each code converted once for 256 rows), two
 // steps in LDS and one in registers, and multiply on 32 x 32 x 16 MFMAs, again
@@ -810,6 +1103,11 @@ static hipError_t rows_launch(const AttnParams& p, hipStream_t st) {
 template <int FMT, int D>
 static hipError_t tile_launch(const AttnParams& p, hipStream_t st) {
   const dim3 grid((uint32_t)p.z.max_tile * p.c.Hkv);
+  if (p.z.tile_rows == kMidRows) {
+    if (p.slopes || p.softcap > 0.f) hipLaunchKernelGGL((k_attend_mid<DTC, FMT, D, true>), grid, dim3(256), 0, st, p);
+    else hipLaunchKernelGGL((k_attend_mid<DTC, FMT, D, false>), grid, dim3(256), 0, st, p);
+    return hipGetLastError();
+  }
   if (p.slopes || p.softcap > 0.f) hipLaunchKernelGGL((k_attend_tile<DTC, FMT, D, true>), grid, dim3(512), 0, st, p);
   else hipLaunchKernelGGL((k_attend_tile<DTC, FMT, D, false>), grid, dim3(512), 0, st, p);
   return hipGetLastError();

@@ -15,6 +15,7 @@
 #define XRL 8
 #define XTG 256
 #define XTL 8
+#define XFT 192
 #endif
 using namespace spear;
 
@@ -233,6 +234,8 @@ spear_status_t check_attention(const spear_attention_t* a, bool buffers) {
 }
 
 
+// Tiles of 256 rows, over all kv heads, from which on these are taken.
+constexpr int kFillTiles = XFT;
 // Stretches wanted of each kernel, over all kv heads, and a stretch's least steps.
 constexpr int kRowsGoal = XRG, kRowsLeast = XRL, kTileGoal = XTG, kTileLeast = XTL;
 // (stretches are shared out among kv heads only where there are fewer heads than the
@@ -269,7 +272,8 @@ AttnLayout attention_layout(const spear_attention_t* a) {
   z.least_rows = kRowsLeast, z.least_tile = kTileLeast;
   // sum over tiles of max(1, ceil(steps / c)) with c >= all steps / goal
   z.max_rows = rows ? (int)served + z.goal_rows : 0;
-  z.max_tile = tile ? (int)(T * group / kTileRows + served) + z.goal_tile : 0;
+  z.tile_rows = (T * group + kTileRows - 1) / kTileRows * hkv < kFillTiles ? kMidRows : kTileRows;
+  z.max_tile = tile ? (int)(T * group / z.tile_rows + served) + z.goal_tile : 0;
   // and over those of more than one, ceil(steps / c) <= 2 steps / c
   z.part_rows = rows && z.goal_rows > 1 ? 2 * z.goal_rows : 0;
   z.part_tile = tile && z.goal_tile > 1 ? 2 * z.goal_tile : 0;
@@ -280,7 +284,7 @@ AttnLayout attention_layout(const spear_attention_t* a) {
   // common: another call's partial results never lie on them.
   l.parts_rows = 2 * kAttnCounters * sizeof(uint32_t);
   l.parts_tile = l.parts_rows + (size_t)z.part_rows * hkv * kRows * (c->head_dim + 2) * 4;
-  l.work_bytes = (l.parts_tile + (size_t)z.part_tile * hkv * kTileRows * (c->head_dim + 2) * 4);
+  l.work_bytes = (l.parts_tile + (size_t)z.part_tile * hkv * z.tile_rows * (c->head_dim + 2) * 4);
   return l;
 }
 
