@@ -271,9 +271,13 @@ __device__ __forceinline__ float max_sixteens(float x) {
 struct ScoreOptions {
   float scale, cap, slope2;  // slope2: slope times log2 e
 };
-template <bool OPT>
+// (of a plain score all but the dot product is one factor: at least the least float,
+// which makes no difference to a score of scale zero, and keeps what is masked, minus
+// infinity, from a product with zero and from a page's scale that is no number)
+__device__ __forceinline__ float dot_factor(float k_scale, const ScoreOptions& o) {
+  return fmaxf(k_scale * (o.scale * kLog2e), 1.17549435e-38f);
+}
 __device__ __forceinline__ float score2(float dot, float k_scale, const ScoreOptions& o, int pos, int j) {
-  if constexpr (!OPT) return dot * (k_scale * (o.scale * kLog2e));
   float t = dot * (k_scale * o.scale);
   if (o.cap > 0.f) {  // cap tanh(t / cap) = cap (1 - 2 / (e^(2 t / cap) + 1))
     const float e = __builtin_amdgcn_exp2f(t * (2.f * kLog2e / o.cap));
@@ -419,11 +423,12 @@ __global__ __launch_bounds__(64 * W, 2) void k_attend_rows(AttnParams p) {
       const bool whole = s * kStep + kStep <= min(it.end, it.pos0 + 1) && pos_max - s * kStep < p.window &&
                          __all(page >= 0);
       float2 f = v_factors<DT, FMT>(sc.y);
-      float w[16];
-      if (whole) {
+      const float fk = OPT ? 1.f : dot_factor(sc.x, opt);  // what st is of a score
+      if constexpr (OPT) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) w[e] = score2<OPT>(st[e >> 2][e & 3], sc.x, opt, pos, j0 + e);
-      } else {
+        for (int e = 0; e < 16; ++e) st[e >> 2][e & 3] = score2(st[e >> 2][e & 3], sc.x, opt, pos, j0 + e);
+      }
+      if (!whole) {
         const u32x4 seen = page >= 0 ? seen_bytes(j0, it) : u32x4{0, 0, 0, 0};
         if (!(seen[0] | seen[1] | seen[2] | seen[3])) f = make_float2(1.f, 1.f);
 #pragma unroll
@@ -432,13 +437,13 @@ __global__ __launch_bounds__(64 * W, 2) void k_attend_rows(AttnParams p) {
         for (int e = 0; e < 16; ++e) {
           const int j = j0 + e;
           const bool sees = ((seen[e >> 2] >> (8 * (e & 3))) & 1) & (((j <= pos) & (pos - j < p.window)) | (j < it.prefix));
-          const float x = score2<OPT>(st[e >> 2][e & 3], sc.x, opt, pos, j);
-          w[e] = sees ? x : -__builtin_inff();
+          st[e >> 2][e & 3] = sees ? st[e >> 2][e & 3] : -__builtin_inff();
         }
       }
-      float top = w[0];
+      float top = st[0][0];
 #pragma unroll
-      for (int e = 1; e < 16; ++e) top = fmaxf(top, w[e]);
+      for (int e = 1; e < 16; ++e) top = fmaxf(top, st[e >> 2][e & 3]);
+      top *= fk;
       top = max_sixteens(top);
       if (__any(top > m + kSlack)) {
         const float now = fmaxf(m, top), fade = __builtin_amdgcn_exp2f(m - now);
@@ -447,13 +452,12 @@ __global__ __launch_bounds__(64 * W, 2) void k_attend_rows(AttnParams p) {
 #pragma unroll
         for (int d = 0; d < DTILES; ++d) o[d] *= fade;
       }
-      float sum = 0.f;
+      float w[16];
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        w[e] = __builtin_amdgcn_exp2f(w[e] - m);
-        sum += w[e];
+        w[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[e >> 2][e & 3], fk, -m));
+        l += w[e];
       }
-      l += sum;
       if ((DT != DT_F16 && FMT == KV_INT8) || (DT == DT_F16 && __any(f.y != 1.f))) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) w[e] *= f.y;
@@ -722,32 +726,27 @@ __global__ __launch_bounds__(256, 2) void k_attend_mid(AttnParams p) {
       u32x4 pw[Y][4];  // weights: [half of the rows][eight tokens of either run]
 #pragma unroll
       for (int y = 0; y < Y; ++y) {
-        float g[2], top;
-        if (whole && !OPT) {
-          top = kLowest;
+        const ScoreOptions opt{scale, p.softcap, slope2[y]};
+        float g[2], top = kLowest;  // g: what st is of a score
 #pragma unroll
-          for (int t = 0; t < 2; ++t) {
-            g[t] = sc.at[t].x * (scale * kLog2e);
-            float x = st[y][t][0];
+        for (int t = 0; t < 2; ++t) {
+          g[t] = OPT ? 1.f : dot_factor(sc.at[t].x, opt);
+          if constexpr (OPT) {
 #pragma unroll
-            for (int e = 1; e < 16; ++e) x = fmaxf(x, st[y][t][e]);
-            top = fmaxf(top, x * g[t]);
+            for (int e = 0; e < 16; ++e) st[y][t][e] = score2(st[y][t][e], sc.at[t].x, opt, pos[y], j0 + 32 * t + 16 * h + e);
           }
-        } else {
-          const ScoreOptions opt{scale, p.softcap, slope2[y]};
-          top = -__builtin_inff();
-#pragma unroll
-          for (int t = 0; t < 2; ++t)
+          if (!whole) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
               const int j = j0 + 32 * t + 16 * h + e;
-              const float x = score2<OPT>(st[y][t][e], sc.at[t].x, opt, pos[y], j);
-              const bool sees = whole || (((seen[t][e >> 2] >> (8 * (e & 3))) & 1) &
-                                          (((j <= pos[y]) & (pos[y] - j < p.window)) | (j < it.prefix)));
-              st[y][t][e] = sees ? x : -__builtin_inff();
-              top = fmaxf(top, st[y][t][e]);
+              const bool sees = ((seen[t][e >> 2] >> (8 * (e & 3))) & 1) & (((j <= pos[y]) & (pos[y] - j < p.window)) | (j < it.prefix));
+              st[y][t][e] = sees ? st[y][t][e] : -__builtin_inff();
             }
-          g[0] = g[1] = 1.f;
+          }
+          float x = st[y][t][0];
+#pragma unroll
+          for (int e = 1; e < 16; ++e) x = fmaxf(x, st[y][t][e]);
+          top = fmaxf(top, x * g[t]);
         }
         top = max_halves(top);
         if (__any(top > m[y] + kSlack)) {
@@ -773,6 +772,7 @@ __global__ __launch_bounds__(256, 2) void k_attend_mid(AttnParams p) {
           for (int e = 0; e < 8; ++e) pw[y][2 * t + (e >> 2)][e & 3] = pack2<DT>(w[2 * e], w[2 * e + 1]);
         }
       }
+      __builtin_amdgcn_sched_barrier(0);  // (V's operands made ahead of the softmax would not fit the registers)
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -986,34 +986,28 @@ __global__ __launch_bounds__(512) void k_attend_tile(AttnParams p) {
       for (int r = 0; r < 4; ++r) ks[r] = s_ks[s & 1][r];
       const bool pages_there = __all(ks[0] == ks[0] && ks[1] == ks[1] && ks[2] == ks[2] && ks[3] == ks[3]);
       const bool whole = j0 + kStep <= min(it.end, pos_lo + 1) && pos_hi - j0 < p.window && pages_there;
-      // scores in powers of two; where every row sees every token, still without K's scale
-      float w[2][16], f[4], top;
-      const bool plain = whole && !OPT;
-      if (plain) {
-        top = kLowest;
+      float f[4], top = kLowest;  // f: what st is of a score
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          f[r] = ks[r] * (opt.scale * kLog2e);
-          float x = st[r >> 1][8 * (r & 1)];
+      for (int r = 0; r < 4; ++r) f[r] = OPT ? 1.f : dot_factor(ks[r], opt);
+      if constexpr (OPT) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) x = fmaxf(x, w[r >> 1][8 * (r & 1) + e] = st[r >> 1][8 * (r & 1) + e]);
-          top = fmaxf(top, x * f[r]);
+        for (int e = 0; e < 32; ++e)
+          st[e >> 4][e & 15] = score2(st[e >> 4][e & 15], ks[e >> 3], opt, pos, j0 + 8 * (e >> 2) + 4 * h + (e & 3));
+      }
+      if (!whole) {
+#pragma unroll
+        for (int e = 0; e < 32; ++e) {
+          const int j = j0 + 8 * (e >> 2) + 4 * h + (e & 3);
+          const bool sees = (j < it.end) & (((j <= pos) & (pos - j < p.window)) | (j < it.prefix)) & (ks[e >> 3] == ks[e >> 3]);
+          st[e >> 4][e & 15] = sees ? st[e >> 4][e & 15] : -__builtin_inff();
         }
-      } else {
+      }
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+      for (int r = 0; r < 4; ++r) {
+        float x = st[r >> 1][8 * (r & 1)];
 #pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const int run = 2 * t + (e >> 3), j = j0 + 32 * t + 8 * (e >> 2) + 4 * h + (e & 3);
-            const bool sees = (j < it.end) & (((j <= pos) & (pos - j < p.window)) | (j < it.prefix)) & (ks[run] == ks[run]);
-            const float x = score2<OPT>(st[t][e], ks[run], opt, pos, j);
-            w[t][e] = whole | sees ? x : -__builtin_inff();
-          }
-        top = w[0][0];
-#pragma unroll
-        for (int e = 1; e < 32; ++e) top = fmaxf(top, w[e >> 4][e & 15]);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) f[r] = 1.f;
+        for (int e = 1; e < 8; ++e) x = fmaxf(x, st[r >> 1][8 * (r & 1) + e]);
+        top = fmaxf(top, x * f[r]);
       }
       top = max_halves(top);
       if (__any(top > m + kSlack)) {
@@ -1023,19 +1017,17 @@ __global__ __launch_bounds__(512) void k_attend_tile(AttnParams p) {
 #pragma unroll
         for (int d = 0; d < D / 32; ++d) o[d] *= fade;
       }
-      float sum = 0.f;
-#pragma unroll
-      for (int e = 0; e < 32; ++e) {
-        float& x = w[e >> 4][e & 15];
-        x = __builtin_amdgcn_exp2f(__builtin_fmaf(x, f[e >> 3], -m));
-        sum += x;
-      }
-      l += sum;
 #pragma unroll
       for (int y = 0; y < 4; ++y) {  // sixteen tokens
+        float w[8];
         u32x4 pw;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) pw[e] = pack2<DT>(w[y >> 1][8 * (y & 1) + 2 * e], w[y >> 1][8 * (y & 1) + 2 * e + 1]);
+        for (int e = 0; e < 8; ++e) {
+          w[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[y >> 1][8 * (y & 1) + e], f[y], -m));
+          l += w[e];
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) pw[e] = pack2<DT>(w[2 * e], w[2 * e + 1]);
 #pragma unroll
         for (int d = 0; d < D / 32; ++d)
           o[d] = mfma32<DT>(*(const u32x4*)(buf + KBYTES + (32 * d + c) * VP + 32 * y + 16 * h), pw, o[d]);
