@@ -286,19 +286,28 @@ __device__ __forceinline__ float score2(float dot, float k_scale, const ScoreOpt
   return t * kLog2e - o.slope2 * (float)abs(pos - j);
 }
 
-// which of the 16 tokens from j0 on some row of the item sees, as bytes of four dwords
-__device__ __forceinline__ u32x4 seen_bytes(int j0, const AttnItem& it) {
+// Masks of tokens as bits, bit e of token j + e. (Compact code counts here: a call of
+// few steps spends its time on fetching what it runs once, and the last step of every
+// row is a masked one; compared and selected one by one this cost 3 us a call.)
+__device__ __forceinline__ uint32_t below(int x) { return (uint32_t)((1ull << min(max(x, 0), 32)) - 1); }
+// tokens that some row of the item sees
+__device__ __forceinline__ uint32_t live_tokens(int j, const AttnItem& it) {
+  return (below(it.end - j) & ~below(it.first - j)) | below(it.prefix - j);
+}
+// tokens that the row at pos sees
+__device__ __forceinline__ uint32_t seen_tokens(int j, const AttnItem& it, int pos, int window) {
+  return ((below(pos + 1 - j) & ~below(pos - window + 1 - j)) | below(it.prefix - j)) & below(it.end - j);
+}
+// x where bit e of the mask is set, else minus infinity
+__device__ __forceinline__ float where_seen(float x, uint32_t mask, int e) {
+  const uint32_t m = (uint32_t)((int)(mask << (31 - e)) >> 31);
+  return __uint_as_float((__float_as_uint(x) & m) | (0xFF800000u & ~m));
+}
+// sixteen bits as bytes of four dwords
+__device__ __forceinline__ u32x4 byte_mask(uint32_t bits) {
   u32x4 m;
 #pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    uint32_t b = 0;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int j = j0 + 4 * w + e;
-      b |= (j < it.end) & ((j >= it.first) | (j < it.prefix)) ? 0xFFu << (8 * e) : 0u;
-    }
-    m[w] = b;
-  }
+  for (int w = 0; w < 4; ++w) m[w] = ((((bits >> (4 * w)) & 15u) * 0x00204081u) & 0x01010101u) * 0xFFu;
   return m;
 }
 
@@ -312,19 +321,17 @@ __device__ __forceinline__ u32x4 seen_bytes(int j0, const AttnItem& it) {
 // joined in order, the latter by the stretch that ends last.
 // Bound: the codes' bytes (long caches), latency (short ones).
 // ---------------------------------------------------------------------------
-#ifndef XW
-#define XW 4
 #define XN 8
-#endif
-template <int DT, int FMT, int D, bool OPT, int W = XW>
-__global__ __launch_bounds__(64 * W, 2) void k_attend_rows(AttnParams p) {
-  constexpr int KS = D / 64, DTILES = D / 16, PITCH = D + 4, KBYTES = kStep * D;
-  constexpr int LDS = std::max(W * KBYTES, W * kRows * PITCH * 4);
-  __shared__ __attribute__((aligned(16))) char lds[LDS];  // K of each wave's step; then each wave's O
-  __shared__ float s_m[W * kRows], s_l[W * kRows];
-  __shared__ int s_last;
+constexpr int kWaves = 4;  // of a workgroup of k_attend_rows and k_attend_mid
+// LDS of either: K of each wave's step, then each wave's O
+template <int D, int ROWS>
+constexpr int few_lds() { return kWaves * std::max(kStep * D, ROWS * (D + 4) * 4); }
+
+template <int DT, int FMT, int D, bool OPT>
+__device__ __forceinline__ void attend_rows(const AttnParams& p, uint32_t block, char* lds, float* s_m, float* s_l, int* s_last) {
+  constexpr int W = kWaves, KS = D / 64, DTILES = D / 16, PITCH = D + 4, KBYTES = kStep * D;
   float* s_o = (float*)lds;
-  const int head = blockIdx.x % p.c.Hkv, idx = blockIdx.x / p.c.Hkv;
+  const int head = block % p.c.Hkv, idx = block / p.c.Hkv;
   AttnItem it = p.items_rows[idx];
   if (it.key != p.key) return;
   if (p.c.pages == 0) it.s1 = it.s0;
@@ -429,16 +436,14 @@ __global__ __launch_bounds__(64 * W, 2) void k_attend_rows(AttnParams p) {
         for (int e = 0; e < 16; ++e) st[e >> 2][e & 3] = score2(st[e >> 2][e & 3], sc.x, opt, pos, j0 + e);
       }
       if (!whole) {
-        const u32x4 seen = page >= 0 ? seen_bytes(j0, it) : u32x4{0, 0, 0, 0};
-        if (!(seen[0] | seen[1] | seen[2] | seen[3])) f = make_float2(1.f, 1.f);
+        const uint32_t there = page >= 0 ? 0xFFFFu : 0u, live = live_tokens(j0, it) & there;
+        const uint32_t sees = seen_tokens(j0, it, pos, p.window) & there;
+        if (!live) f = make_float2(1.f, 1.f);
+        const u32x4 bytes = byte_mask(live);
 #pragma unroll
-        for (int d = 0; d < DTILES; ++d) vr[d] &= seen;
+        for (int d = 0; d < DTILES; ++d) vr[d] &= bytes;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int j = j0 + e;
-          const bool sees = ((seen[e >> 2] >> (8 * (e & 3))) & 1) & (((j <= pos) & (pos - j < p.window)) | (j < it.prefix));
-          st[e >> 2][e & 3] = sees ? st[e >> 2][e & 3] : -__builtin_inff();
-        }
+        for (int e = 0; e < 16; ++e) st[e >> 2][e & 3] = where_seen(st[e >> 2][e & 3], sees, e);
       }
       float top = st[0][0];
 #pragma unroll
@@ -516,9 +521,9 @@ __global__ __launch_bounds__(64 * W, 2) void k_attend_rows(AttnParams p) {
       if (d0 == 0) st_agent(ml + row, top), st_agent(ml + kRows + row, total);
     }
     complete_and_sync();
-    if (tid == 0) s_last = arrive_last(p.counters_rows + slot, it.splits);
+    if (tid == 0) *s_last = arrive_last(p.counters_rows + slot, it.splits);
     __syncthreads();
-    if (!s_last) return;
+    if (!*s_last) return;
     // group `part` takes every groups-th stretch in order, N in flight; then the groups in order
     constexpr int N = XN;
     total = 0.f;
@@ -580,14 +585,10 @@ __global__ __launch_bounds__(64 * W, 2) void k_attend_rows(AttnParams p) {
 // Bound: the conversions and exponentials beside the MFMAs.
 // ---------------------------------------------------------------------------
 template <int DT, int FMT, int D, bool OPT>
-__global__ __launch_bounds__(256, 2) void k_attend_mid(AttnParams p) {
-  constexpr int W = 4, Y = kMidRows / 32, DTILES = D / 32, KX = D / 32, PITCH = D + 4, KBYTES = kStep * D;
-  constexpr int LDS = std::max(W * KBYTES, W * kMidRows * PITCH * 4);
-  __shared__ __attribute__((aligned(16))) char lds[LDS];  // K of each wave's step; then each wave's O
-  __shared__ float s_m[W * kMidRows], s_l[W * kMidRows];
-  __shared__ int s_last;
+__device__ __forceinline__ void attend_mid(const AttnParams& p, uint32_t block, char* lds, float* s_m, float* s_l, int* s_last) {
+  constexpr int W = kWaves, Y = kMidRows / 32, DTILES = D / 32, KX = D / 32, PITCH = D + 4, KBYTES = kStep * D;
   float* s_o = (float*)lds;
-  const int head = blockIdx.x % p.c.Hkv, idx = blockIdx.x / p.c.Hkv;
+  const int head = block % p.c.Hkv, idx = block / p.c.Hkv;
   AttnItem it = p.items_tile[idx];
   if (it.key != p.key) return;
   if (p.c.pages == 0) it.s1 = it.s0;
@@ -711,16 +712,16 @@ __global__ __launch_bounds__(256, 2) void k_attend_mid(AttnParams p) {
       const bool whole = j0 + kStep <= min(it.end, pos_lo + 1) && pos_hi - j0 < p.window &&
                          (page.at[0] | page.at[1] | page.at[2] | page.at[3]) >= 0;
       float2 f[2] = {v_factors<DT, FMT>(sc.at[0].y), v_factors<DT, FMT>(sc.at[1].y)};
-      u32x4 seen[2];
+      uint32_t there[2];
       if (!whole) {
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-          const int there = h ? page.at[2 * t + 1] : page.at[2 * t];
-          seen[t] = seen_bytes(j0 + 32 * t + 16 * h, it);
-          if (there < 0) seen[t] = u32x4{0, 0, 0, 0};
-          if (!(seen[t][0] | seen[t][1] | seen[t][2] | seen[t][3])) f[t] = make_float2(1.f, 1.f);
+          there[t] = (h ? page.at[2 * t + 1] : page.at[2 * t]) >= 0 ? 0xFFFFu : 0u;
+          const uint32_t live = live_tokens(j0 + 32 * t + 16 * h, it) & there[t];
+          if (!live) f[t] = make_float2(1.f, 1.f);
+          const u32x4 bytes = byte_mask(live);
 #pragma unroll
-          for (int d = 0; d < DTILES; ++d) vr[t][d] &= seen[t];
+          for (int d = 0; d < DTILES; ++d) vr[t][d] &= bytes;
         }
       }
       u32x4 pw[Y][4];  // weights: [half of the rows][eight tokens of either run]
@@ -736,12 +737,9 @@ __global__ __launch_bounds__(256, 2) void k_attend_mid(AttnParams p) {
             for (int e = 0; e < 16; ++e) st[y][t][e] = score2(st[y][t][e], sc.at[t].x, opt, pos[y], j0 + 32 * t + 16 * h + e);
           }
           if (!whole) {
+            const uint32_t sees = seen_tokens(j0 + 32 * t + 16 * h, it, pos[y], p.window) & there[t];
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              const int j = j0 + 32 * t + 16 * h + e;
-              const bool sees = ((seen[t][e >> 2] >> (8 * (e & 3))) & 1) & (((j <= pos[y]) & (pos[y] - j < p.window)) | (j < it.prefix));
-              st[y][t][e] = sees ? st[y][t][e] : -__builtin_inff();
-            }
+            for (int e = 0; e < 16; ++e) st[y][t][e] = where_seen(st[y][t][e], sees, e);
           }
           float x = st[y][t][0];
 #pragma unroll
@@ -829,9 +827,9 @@ __global__ __launch_bounds__(256, 2) void k_attend_mid(AttnParams p) {
       if (own == 0) st_agent(ml, top), st_agent(ml + kMidRows, total);
     }
     complete_and_sync();
-    if (tid == 0) s_last = arrive_last(p.counters_tile + slot, it.splits);
+    if (tid == 0) *s_last = arrive_last(p.counters_tile + slot, it.splits);
     __syncthreads();
-    if (!s_last) return;
+    if (!*s_last) return;
     top = kLowest, total = 0.f;
 #pragma unroll
     for (int e = 0; e < F; ++e) x[e] = f32x4{};
@@ -858,6 +856,24 @@ __global__ __launch_bounds__(256, 2) void k_attend_mid(AttnParams p) {
   uint16_t* out = p.out + (int64_t)(it.row0 + i) * p.out_ld + hq * D + 4 * own;
 #pragma unroll
   for (int e = 0; e < F; ++e) *(u32x2*)(out + 4 * EACH * e) = u32x2{pack2<DT>(x[e][0] * inv, x[e][1] * inv), pack2<DT>(x[e][2] * inv, x[e][3] * inv)};
+}
+
+template <int DT, int FMT, int D, bool OPT>
+__global__ __launch_bounds__(64 * kWaves, 2) void k_attend_rows(AttnParams p) {
+  __shared__ __attribute__((aligned(16))) char lds[few_lds<D, kRows>()];
+  __shared__ float s_m[kWaves * kRows], s_l[kWaves * kRows];
+  __shared__ int s_last;
+  attend_rows<DT, FMT, D, OPT>(p, blockIdx.x, lds, s_m, s_l, &s_last);
+}
+// both kinds in one launch, side by side on the GPU: those of 32 rows first
+template <int DT, int FMT, int D, bool OPT>
+__global__ __launch_bounds__(64 * kWaves, 2) void k_attend_mid(AttnParams p) {
+  __shared__ __attribute__((aligned(16))) char lds[few_lds<D, kMidRows>()];
+  __shared__ float s_m[kWaves * kMidRows], s_l[kWaves * kMidRows];
+  __shared__ int s_last;
+  const uint32_t mid = (uint32_t)p.z.max_tile * p.c.Hkv;
+  if (blockIdx.x < mid) attend_mid<DT, FMT, D, OPT>(p, blockIdx.x, lds, s_m, s_l, &s_last);
+  else attend_rows<DT, FMT, D, OPT>(p, blockIdx.x - mid, lds, s_m, s_l, &s_last);
 }
 
 // ---------------------------------------------------------------------------
@@ -938,9 +954,9 @@ __global__ __launch_bounds__(512) void k_attend_tile(AttnParams p) {
     float f = sc.y;
     const int j0 = s * kStep + 16 * v_run;
     if (held_v < 0 || j0 + 16 > it.end || j0 < it.first) {
-      const u32x4 seen = held_v >= 0 ? seen_bytes(j0, it) : u32x4{0, 0, 0, 0};
-      vr &= seen;
-      if (!(seen[0] | seen[1] | seen[2] | seen[3])) f = 1.f;
+      const uint32_t live = held_v >= 0 ? live_tokens(j0, it) & 0xFFFFu : 0u;
+      vr &= byte_mask(live);
+      if (!live) f = 1.f;
     }
     if (does_v) {
       u32x4* v = (u32x4*)(buf + KBYTES + v_feature * VP + 32 * v_run);
@@ -996,10 +1012,12 @@ __global__ __launch_bounds__(512) void k_attend_tile(AttnParams p) {
       }
       if (!whole) {
 #pragma unroll
-        for (int e = 0; e < 32; ++e) {
-          const int j = j0 + 8 * (e >> 2) + 4 * h + (e & 3);
-          const bool sees = (j < it.end) & (((j <= pos) & (pos - j < p.window)) | (j < it.prefix)) & (ks[e >> 3] == ks[e >> 3]);
-          st[e >> 4][e & 15] = sees ? st[e >> 4][e & 15] : -__builtin_inff();
+        for (int t = 0; t < 2; ++t) {
+          uint32_t sees = seen_tokens(j0 + 32 * t, it, pos, p.window);
+          sees &= (ks[2 * t] == ks[2 * t] ? 0xFFFFu : 0u) | (ks[2 * t + 1] == ks[2 * t + 1] ? 0xFFFF0000u : 0u);
+          sees >>= 4 * h;
+#pragma unroll
+          for (int e = 0; e < 16; ++e) st[t][e] = where_seen(st[t][e], sees, 8 * (e >> 2) + (e & 3));
         }
       }
 #pragma unroll
@@ -1085,32 +1103,28 @@ __global__ __launch_bounds__(512) void k_attend_tile(AttnParams p) {
                                               pack2<DT>(o[d][4 * x + 2] * inv, o[d][4 * x + 3] * inv)};
 }
 
-template <int FMT, int D>
-static hipError_t rows_launch(const AttnParams& p, hipStream_t st) {
-  const dim3 grid((uint32_t)p.z.max_rows * p.c.Hkv);
-  if (p.slopes || p.softcap > 0.f) hipLaunchKernelGGL((k_attend_rows<DTC, FMT, D, true>), grid, dim3(64 * XW), 0, st, p);
-  else hipLaunchKernelGGL((k_attend_rows<DTC, FMT, D, false>), grid, dim3(64 * XW), 0, st, p);
-  return hipGetLastError();
-}
-template <int FMT, int D>
-static hipError_t tile_launch(const AttnParams& p, hipStream_t st) {
-  const dim3 grid((uint32_t)p.z.max_tile * p.c.Hkv);
-  if (p.z.tile_rows == kMidRows) {
-    if (p.slopes || p.softcap > 0.f) hipLaunchKernelGGL((k_attend_mid<DTC, FMT, D, true>), grid, dim3(256), 0, st, p);
-    else hipLaunchKernelGGL((k_attend_mid<DTC, FMT, D, false>), grid, dim3(256), 0, st, p);
+template <int FMT, int D, bool OPT>
+static hipError_t attend_launch(const AttnParams& p, hipStream_t st) {
+  const uint32_t rows = (uint32_t)p.z.max_rows * p.c.Hkv, tiles = (uint32_t)p.z.max_tile * p.c.Hkv;
+  if (tiles && p.z.tile_rows == kMidRows) {
+    hipLaunchKernelGGL((k_attend_mid<DTC, FMT, D, OPT>), dim3(tiles + rows), dim3(64 * kWaves), 0, st, p);
     return hipGetLastError();
   }
-  if (p.slopes || p.softcap > 0.f) hipLaunchKernelGGL((k_attend_tile<DTC, FMT, D, true>), grid, dim3(512), 0, st, p);
-  else hipLaunchKernelGGL((k_attend_tile<DTC, FMT, D, false>), grid, dim3(512), 0, st, p);
+  if (tiles) {
+    hipLaunchKernelGGL((k_attend_tile<DTC, FMT, D, OPT>), dim3(tiles), dim3(512), 0, st, p);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  if (rows) hipLaunchKernelGGL((k_attend_rows<DTC, FMT, D, OPT>), dim3(rows), dim3(64 * kWaves), 0, st, p);
   return hipGetLastError();
 }
-hipError_t SPEAR_D(launch_attend_rows)(const AttnParams& p, int format, hipStream_t st) {
-  if (p.c.D == 64) return format == KV_INT8 ? rows_launch<KV_INT8, 64>(p, st) : rows_launch<KV_E4M3, 64>(p, st);
-  return format == KV_INT8 ? rows_launch<KV_INT8, 128>(p, st) : rows_launch<KV_E4M3, 128>(p, st);
+template <int FMT, int D>
+static hipError_t attend_options(const AttnParams& p, hipStream_t st) {
+  return p.slopes || p.softcap > 0.f ? attend_launch<FMT, D, true>(p, st) : attend_launch<FMT, D, false>(p, st);
 }
-hipError_t SPEAR_D(launch_attend_tile)(const AttnParams& p, int format, hipStream_t st) {
-  if (p.c.D == 64) return format == KV_INT8 ? tile_launch<KV_INT8, 64>(p, st) : tile_launch<KV_E4M3, 64>(p, st);
-  return format == KV_INT8 ? tile_launch<KV_INT8, 128>(p, st) : tile_launch<KV_E4M3, 128>(p, st);
+hipError_t SPEAR_D(launch_attend)(const AttnParams& p, int format, hipStream_t st) {
+  if (p.c.D == 64) return format == KV_INT8 ? attend_options<KV_INT8, 64>(p, st) : attend_options<KV_E4M3, 64>(p, st);
+  return format == KV_INT8 ? attend_options<KV_INT8, 128>(p, st) : attend_options<KV_E4M3, 128>(p, st);
 }
 
 }  // namespace spear

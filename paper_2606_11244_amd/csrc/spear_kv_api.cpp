@@ -15,7 +15,11 @@
 #define XRL 8
 #define XTG 256
 #define XTL 8
-#define XFT 192
+#define XFT 384
+#endif
+#ifndef XMG
+#define XMG 384
+#define XML 4
 #endif
 using namespace spear;
 
@@ -237,10 +241,11 @@ spear_status_t check_attention(const spear_attention_t* a, bool buffers) {
 // Tiles of 256 rows, over all kv heads, from which on these are taken.
 constexpr int kFillTiles = XFT;
 // Stretches wanted of each kernel, over all kv heads, and a stretch's least steps.
-constexpr int kRowsGoal = XRG, kRowsLeast = XRL, kTileGoal = XTG, kTileLeast = XTL;
+constexpr int kRowsGoal = XRG, kRowsLeast = XRL, kTileGoal = XTG, kTileLeast = XTL, kMidGoal = XMG,
+              kMidLeast = XML;
 // (stretches are shared out among kv heads only where there are fewer heads than the
 // goal, so that counters are at most 2 (goal + heads))
-static_assert(4 * kRowsGoal <= kAttnCounters && 4 * kTileGoal <= kAttnCounters, "a counter for each shared tile and head");
+static_assert(4 * kRowsGoal <= kAttnCounters && 4 * std::max(kTileGoal, kMidGoal) <= kAttnCounters, "a counter for each shared tile and head");
 
 // Where the plan's and the workspace's parts lie, from sizes alone.
 struct AttnLayout {
@@ -268,11 +273,12 @@ AttnLayout attention_layout(const spear_attention_t* a) {
   AttnLayout l;
   AttnShape& z = l.z;
   z.goal_rows = (int)((kRowsGoal + hkv - 1) / hkv);
-  z.goal_tile = (int)((kTileGoal + hkv - 1) / hkv);
-  z.least_rows = kRowsLeast, z.least_tile = kTileLeast;
   // sum over tiles of max(1, ceil(steps / c)) with c >= all steps / goal
   z.max_rows = rows ? (int)served + z.goal_rows : 0;
+  z.least_rows = kRowsLeast;
   z.tile_rows = (T * group + kTileRows - 1) / kTileRows * hkv < kFillTiles ? kMidRows : kTileRows;
+  z.goal_tile = (int)(((z.tile_rows == kMidRows ? kMidGoal : kTileGoal) + hkv - 1) / hkv);
+  z.least_tile = z.tile_rows == kMidRows ? kMidLeast : kTileLeast;
   z.max_tile = tile ? (int)(T * group / z.tile_rows + served) + z.goal_tile : 0;
   // and over those of more than one, ceil(steps / c) <= 2 steps / c
   z.part_rows = rows && z.goal_rows > 1 ? 2 * z.goal_rows : 0;
@@ -365,10 +371,6 @@ spear_status_t spear_attention(const spear_attention_t* a, void* hip_stream) {
   p.counters_tile = p.counters_rows + kAttnCounters;
   p.parts_rows = (float*)((char*)a->workspace + l.parts_rows);
   p.parts_tile = (float*)((char*)a->workspace + l.parts_tile);
-  const bool f16 = c->act_dtype == SPEAR_F16;
-  hipError_t e = hipSuccess;
-  if (l.z.max_tile) e = (f16 ? launch_attend_tile_f16 : launch_attend_tile_bf16)(p, c->format, (hipStream_t)hip_stream);
-  if (e == hipSuccess && l.z.max_rows)
-    e = (f16 ? launch_attend_rows_f16 : launch_attend_rows_bf16)(p, c->format, (hipStream_t)hip_stream);
-  return hip_status(e);
+  const auto launch = c->act_dtype == SPEAR_F16 ? launch_attend_f16 : launch_attend_bf16;
+  return hip_status(launch(p, c->format, (hipStream_t)hip_stream));
 }

@@ -54,7 +54,7 @@ struct KvReadParams {
 
 // ---- attention ----
 // A request's rows (its new tokens, each with the query heads of one kv head) go
-// to k_attend_rows where they are at most kRows, else, in tiles, to k_attend_mid
+// to attend_rows where they are at most kRows, else, in tiles, to attend_mid
 // (kMidRows) or k_attend_tile (kTileRows). All walk the cache in steps of kStep tokens.
 constexpr int kRows = 16, kMidRows = 32, kTileRows = 256, kStep = 64;
 constexpr int kAttnCounters = 2048;  // of each kernel
@@ -107,8 +107,7 @@ hipError_t launch_kv_pages(const KvPagesParams& p, hipStream_t st);
 #define SPEAR_KV_LAUNCHERS(D)                                                      \
   hipError_t launch_kv_append_##D(const KvAppendParams& p, int format, hipStream_t st); \
   hipError_t launch_kv_read_##D(const KvReadParams& p, int format, hipStream_t st); \
-  hipError_t launch_attend_rows_##D(const AttnParams& p, int format, hipStream_t st); \
-  hipError_t launch_attend_tile_##D(const AttnParams& p, int format, hipStream_t st);
+  hipError_t launch_attend_##D(const AttnParams& p, int format, hipStream_t st);
 SPEAR_KV_LAUNCHERS(f16)
 SPEAR_KV_LAUNCHERS(bf16)
 #undef SPEAR_KV_LAUNCHERS
