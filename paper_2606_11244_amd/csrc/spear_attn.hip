@@ -286,6 +286,21 @@ __device__ __forceinline__ float score2(float dot, float k_scale, const ScoreOpt
   return t * kLog2e - o.slope2 * (float)abs(pos - j);
 }
 
+// Kernel arguments are read where the compiler first needs them, and a line of them
+// not yet read is another trip to memory: what is used late is asked for at the start,
+// with the rest (one request of 500 tokens 5.84 us, 5.68 this way).
+__device__ __forceinline__ void early(const AttnParams& p) {
+  asm volatile("" ::"s"(p.window), "s"(p.out), "s"(p.out_ld), "s"(p.slopes), "s"(p.softcap), "s"(p.scale));
+  asm volatile("" ::"s"(p.counters_rows), "s"(p.counters_tile), "s"(p.parts_rows), "s"(p.parts_tile));
+}
+
+// an item of the plan, by scalar loads (a launch only reads plans)
+__device__ __forceinline__ AttnItem item_at(const AttnItem* items, int idx) {
+  typedef uint32_t u32x16 __attribute__((ext_vector_type(16)));
+  static_assert(sizeof(AttnItem) == sizeof(u32x16), "one load");
+  return __builtin_bit_cast(AttnItem, *(const __attribute__((address_space(4))) u32x16*)(uintptr_t)(items + idx));
+}
+
 // Masks of tokens as bits, bit e of token j + e. (Compact code counts here: a call of
 // few steps spends its time on fetching what it runs once, and the last step of every
 // row is a masked one; compared and selected one by one this cost 3 us a call.)
@@ -332,7 +347,7 @@ __device__ __forceinline__ void attend_rows(const AttnParams& p, uint32_t block,
   constexpr int W = kWaves, KS = D / 64, DTILES = D / 16, PITCH = D + 4, KBYTES = kStep * D;
   float* s_o = (float*)lds;
   const int head = block % p.c.Hkv, idx = block / p.c.Hkv;
-  AttnItem it = p.items_rows[idx];
+  AttnItem it = item_at(p.items_rows, idx);
   if (it.key != p.key) return;
   if (p.c.pages == 0) it.s1 = it.s0;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c = lane & 15, g = lane >> 4;
@@ -589,7 +604,7 @@ __device__ __forceinline__ void attend_mid(const AttnParams& p, uint32_t block, 
   constexpr int W = kWaves, Y = kMidRows / 32, DTILES = D / 32, KX = D / 32, PITCH = D + 4, KBYTES = kStep * D;
   float* s_o = (float*)lds;
   const int head = block % p.c.Hkv, idx = block / p.c.Hkv;
-  AttnItem it = p.items_tile[idx];
+  AttnItem it = item_at(p.items_tile, idx);
   if (it.key != p.key) return;
   if (p.c.pages == 0) it.s1 = it.s0;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c = lane & 31, h = lane >> 5;
@@ -624,17 +639,17 @@ __device__ __forceinline__ void attend_mid(const AttnParams& p, uint32_t block, 
     if (s < it.s1 && j < it.end) page = table[j >> p.log2_page];
     return page;
   };
-  struct Pages {
-    int at[4];
-  };
+  typedef int Pages __attribute__((ext_vector_type(4)));
   auto pages_of = [&](int entry) {
-    Pages r;
-#pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      const int e = __builtin_amdgcn_readlane(entry, 16 * x);
-      r.at[x] = (uint32_t)e < (uint32_t)p.c.pages ? e : -1;
-    }
-    return r;
+    auto page = [&](int e) { return (uint32_t)e < (uint32_t)p.c.pages ? e : -1; };
+    return Pages{page(__builtin_amdgcn_readlane(entry, 0)), page(__builtin_amdgcn_readlane(entry, 16)),
+                 page(__builtin_amdgcn_readlane(entry, 32)), page(__builtin_amdgcn_readlane(entry, 48))};
+  };
+  // the lane's run 2t + h. (As an array indexed by h the pages went to LDS by way of the
+  // workgroup's size, which is read from host memory: 19 us instead of 5 at 64 x 64 tokens.)
+  auto mine_of = [&](const Pages& pg, int t) {
+    const int a = t ? pg.z : pg.x, b = t ? pg.w : pg.y;
+    return h ? b : a;
   };
   // K to LDS as in k_attend_rows; here the sixteen tokens that a sixteen of lanes reads
   // are four times four, 4 and 16 apart
@@ -645,7 +660,7 @@ __device__ __forceinline__ void attend_mid(const AttnParams& p, uint32_t block, 
 #pragma unroll
     for (int x = 0; x < kStep / TOKENS; ++x) {
       const int run = x * TOKENS / 16, in_run = x * TOKENS % 16 + lane / PIECES;
-      const uint8_t* k = k_head + (uint64_t)(uint32_t)max(pg.at[run], 0) * pool_bytes + ((s * kStep + 16 * run) & (P - 1)) * D;
+      const uint8_t* k = k_head + (uint64_t)(uint32_t)max(pg[run], 0) * pool_bytes + ((s * kStep + 16 * run) & (P - 1)) * D;
       const uint8_t* from = k + (in_run * D + 16 * ((lane % PIECES) ^ turn(16 * run + in_run)));
       __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
                                        (__attribute__((address_space(3))) void*)(s_k + 1024 * x), 16, 0, 0);
@@ -655,7 +670,7 @@ __device__ __forceinline__ void attend_mid(const AttnParams& p, uint32_t block, 
   auto load_v = [&](int s, const Pages& pg) {
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      const int page = max(h ? pg.at[2 * t + 1] : pg.at[2 * t], 0), at = (s * kStep + 32 * t + 16 * h) & (P - 1);
+      const int page = max(mine_of(pg, t), 0), at = (s * kStep + 32 * t + 16 * h) & (P - 1);
       const uint8_t* from = v_head + (uint64_t)(uint32_t)page * pool_bytes + (c * P + at);
 #pragma unroll
       for (int d = 0; d < DTILES; ++d) vr[t][d] = ldg16(from + d * 32 * P);
@@ -668,7 +683,7 @@ __device__ __forceinline__ void attend_mid(const AttnParams& p, uint32_t block, 
     Scales r;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      const uint64_t ph = (uint64_t)(uint32_t)max(h ? pg.at[2 * t + 1] : pg.at[2 * t], 0) * p.c.Hkv + head;
+      const uint64_t ph = (uint64_t)(uint32_t)max(mine_of(pg, t), 0) * p.c.Hkv + head;
       r.at[t] = make_float2(p.c.k_scale[ph], p.c.v_scale[ph]);
     }
     return r;
@@ -710,13 +725,13 @@ __device__ __forceinline__ void attend_mid(const AttnParams& p, uint32_t block, 
       }
       const int j0 = s * kStep;
       const bool whole = j0 + kStep <= min(it.end, pos_lo + 1) && pos_hi - j0 < p.window &&
-                         (page.at[0] | page.at[1] | page.at[2] | page.at[3]) >= 0;
+                         (page.x | page.y | page.z | page.w) >= 0;
       float2 f[2] = {v_factors<DT, FMT>(sc.at[0].y), v_factors<DT, FMT>(sc.at[1].y)};
       uint32_t there[2];
       if (!whole) {
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-          there[t] = (h ? page.at[2 * t + 1] : page.at[2 * t]) >= 0 ? 0xFFFFu : 0u;
+          there[t] = mine_of(page, t) >= 0 ? 0xFFFFu : 0u;
           const uint32_t live = live_tokens(j0 + 32 * t + 16 * h, it) & there[t];
           if (!live) f[t] = make_float2(1.f, 1.f);
           const u32x4 bytes = byte_mask(live);
@@ -863,6 +878,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_attend_rows(AttnParams p) {
   __shared__ __attribute__((aligned(16))) char lds[few_lds<D, kRows>()];
   __shared__ float s_m[kWaves * kRows], s_l[kWaves * kRows];
   __shared__ int s_last;
+  early(p);
   attend_rows<DT, FMT, D, OPT>(p, blockIdx.x, lds, s_m, s_l, &s_last);
 }
 // both kinds in one launch, side by side on the GPU: those of 32 rows first
@@ -871,9 +887,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_attend_mid(AttnParams p) {
   __shared__ __attribute__((aligned(16))) char lds[few_lds<D, kMidRows>()];
   __shared__ float s_m[kWaves * kMidRows], s_l[kWaves * kMidRows];
   __shared__ int s_last;
-  const uint32_t mid = (uint32_t)p.z.max_tile * p.c.Hkv;
-  if (blockIdx.x < mid) attend_mid<DT, FMT, D, OPT>(p, blockIdx.x, lds, s_m, s_l, &s_last);
-  else attend_rows<DT, FMT, D, OPT>(p, blockIdx.x - mid, lds, s_m, s_l, &s_last);
+  early(p);
+  if (blockIdx.x < p.mid_blocks) attend_mid<DT, FMT, D, OPT>(p, blockIdx.x, lds, s_m, s_l, &s_last);
+  else attend_rows<DT, FMT, D, OPT>(p, blockIdx.x - p.mid_blocks, lds, s_m, s_l, &s_last);
 }
 
 // ---------------------------------------------------------------------------
@@ -892,8 +908,9 @@ __global__ __launch_bounds__(512) void k_attend_tile(AttnParams p) {
   __shared__ __attribute__((aligned(16))) char lds[2 * BUF];
   __shared__ float s_ks[2][4];
   __shared__ int s_last;
+  early(p);
   const int head = blockIdx.x % p.c.Hkv, idx = blockIdx.x / p.c.Hkv;
-  AttnItem it = p.items_tile[idx];
+  AttnItem it = item_at(p.items_tile, idx);
   if (it.key != p.key) return;
   if (p.c.pages == 0) it.s1 = it.s0;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c = lane & 31, h = lane >> 5;
@@ -1104,9 +1121,9 @@ __global__ __launch_bounds__(512) void k_attend_tile(AttnParams p) {
 }
 
 template <int FMT, int D, bool OPT>
-static hipError_t attend_launch(const AttnParams& p, hipStream_t st) {
-  const uint32_t rows = (uint32_t)p.z.max_rows * p.c.Hkv, tiles = (uint32_t)p.z.max_tile * p.c.Hkv;
-  if (tiles && p.z.tile_rows == kMidRows) {
+static hipError_t attend_launch(const AttnParams& p, const AttnShape& z, hipStream_t st) {
+  const uint32_t rows = (uint32_t)z.max_rows * p.c.Hkv, tiles = (uint32_t)z.max_tile * p.c.Hkv;
+  if (tiles && z.tile_rows == kMidRows) {
     hipLaunchKernelGGL((k_attend_mid<DTC, FMT, D, OPT>), dim3(tiles + rows), dim3(64 * kWaves), 0, st, p);
     return hipGetLastError();
   }
@@ -1119,12 +1136,12 @@ static hipError_t attend_launch(const AttnParams& p, hipStream_t st) {
   return hipGetLastError();
 }
 template <int FMT, int D>
-static hipError_t attend_options(const AttnParams& p, hipStream_t st) {
-  return p.slopes || p.softcap > 0.f ? attend_launch<FMT, D, true>(p, st) : attend_launch<FMT, D, false>(p, st);
+static hipError_t attend_options(const AttnParams& p, const AttnShape& z, hipStream_t st) {
+  return p.slopes || p.softcap > 0.f ? attend_launch<FMT, D, true>(p, z, st) : attend_launch<FMT, D, false>(p, z, st);
 }
-hipError_t SPEAR_D(launch_attend)(const AttnParams& p, int format, hipStream_t st) {
-  if (p.c.D == 64) return format == KV_INT8 ? attend_options<KV_INT8, 64>(p, st) : attend_options<KV_E4M3, 64>(p, st);
-  return format == KV_INT8 ? attend_options<KV_INT8, 128>(p, st) : attend_options<KV_E4M3, 128>(p, st);
+hipError_t SPEAR_D(launch_attend)(const AttnParams& p, const AttnShape& z, int format, hipStream_t st) {
+  if (p.c.D == 64) return format == KV_INT8 ? attend_options<KV_INT8, 64>(p, z, st) : attend_options<KV_E4M3, 64>(p, z, st);
+  return format == KV_INT8 ? attend_options<KV_INT8, 128>(p, z, st) : attend_options<KV_E4M3, 128>(p, z, st);
 }
 
 }  // namespace spear

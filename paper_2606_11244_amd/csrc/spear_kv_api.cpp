@@ -364,7 +364,7 @@ spear_status_t spear_attention(const spear_attention_t* a, void* hip_stream) {
   p.table = b->table;
   p.q = (const uint16_t*)a->q, p.out = (uint16_t*)a->out;
   p.slopes = a->slopes, p.scale = a->scale, p.softcap = a->softcap;
-  p.z = l.z;
+  p.mid_blocks = (uint32_t)l.z.max_tile * c->kv_heads;
   p.items_rows = (const AttnItem*)((const char*)a->plan + l.items_rows);
   p.items_tile = (const AttnItem*)((const char*)a->plan + l.items_tile);
   p.counters_rows = (uint32_t*)a->workspace;
@@ -372,5 +372,5 @@ spear_status_t spear_attention(const spear_attention_t* a, void* hip_stream) {
   p.parts_rows = (float*)((char*)a->workspace + l.parts_rows);
   p.parts_tile = (float*)((char*)a->workspace + l.parts_tile);
   const auto launch = c->act_dtype == SPEAR_F16 ? launch_attend_f16 : launch_attend_bf16;
-  return hip_status(launch(p, c->format, (hipStream_t)hip_stream));
+  return hip_status(launch(p, l.z, c->format, (hipStream_t)hip_stream));
 }

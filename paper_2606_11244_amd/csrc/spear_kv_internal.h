@@ -92,14 +92,14 @@ struct AttnParams {
   uint32_t key;
   int64_t ld, q_ld, out_ld;
   const int32_t* table;
+  const AttnItem *items_rows, *items_tile;
   const uint16_t* q;
   uint16_t* out;
   const float* slopes;
   float scale, softcap;
-  AttnShape z;
-  const AttnItem *items_rows, *items_tile;
   uint32_t *counters_rows, *counters_tile;  // [part][Hkv]: kAttnCounters each
   float *parts_rows, *parts_tile;  // [part][Hkv][rows of O, their maxima, their sums]
+  uint32_t mid_blocks;             // workgroups of k_attend_mid that take tiles
 };
 
 hipError_t launch_attention_plan(const AttnPlanParams& p, hipStream_t st);
@@ -107,7 +107,7 @@ hipError_t launch_kv_pages(const KvPagesParams& p, hipStream_t st);
 #define SPEAR_KV_LAUNCHERS(D)                                                      \
   hipError_t launch_kv_append_##D(const KvAppendParams& p, int format, hipStream_t st); \
   hipError_t launch_kv_read_##D(const KvReadParams& p, int format, hipStream_t st); \
-  hipError_t launch_attend_##D(const AttnParams& p, int format, hipStream_t st);
+  hipError_t launch_attend_##D(const AttnParams& p, const AttnShape& z, int format, hipStream_t st);
 SPEAR_KV_LAUNCHERS(f16)
 SPEAR_KV_LAUNCHERS(bf16)
 #undef SPEAR_KV_LAUNCHERS

@@ -86,17 +86,28 @@ def _ints(t, n, what):
     return t.data_ptr()
 
 
+def _on(holder, dev):
+    """That a cache's, batch's or rotation's tensors are on GPU `dev`."""
+    if holder.device != dev:
+        raise ValueError(f"tensors on one device are needed (GPU {dev}; those of a {type(holder).__name__} are not)")
+
+
 def _rows(t, shape, dtype, what):
     """Stride between the tokens of a [tokens][heads][head_dim] tensor of dense rows (0: dense)."""
+    st = t.stride()
+    if t.dtype is dtype and t.shape == shape and st[2] == 1 and st[1] == shape[2]:
+        if shape[0] < 2:
+            return 0
+        if st[0] >= shape[1] * shape[2]:  # (zero would mean dense)
+            return st[0]
+        raise ValueError(f"the rows of {what} overlap")
     if t.dtype is not dtype:
         raise TypeError(f"{what} is {t.dtype} beside a cache of {dtype}")
-    if tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{what} is {tuple(shape)}")
-    if t.numel() and (t.stride(2) != 1 or (shape[1] > 1 and t.stride(1) != shape[2])):
+    if t.shape != shape:
+        raise ValueError(f"{what} is {shape}")
+    if t.numel() and (st[2] != 1 or shape[1] > 1):
         raise ValueError(f"{what} has dense rows")
-    if shape[0] > 1 and t.stride(0) < shape[1] * shape[2]:  # (zero would mean dense)
-        raise ValueError(f"the rows of {what} overlap")
-    return t.stride(0) if shape[0] > 1 else 0
+    return _rows(t.as_strided(shape, (st[0], shape[2], 1)), shape, dtype, what) if t.numel() else 0
 
 
 class Cache:
@@ -117,8 +128,13 @@ class Cache:
             raise ValueError("a cache's tensors are contiguous")
         self.k, self.v, self.k_scale, self.v_scale, self.act_dtype = k, v, k_scale, v_scale, act_dtype
         self.kv_heads, self.head_dim, self.page_tokens = kv_heads, head_dim, page_tokens
+        devices = {t.get_device() for t in (k, v, k_scale, v_scale)}
+        if len(devices) != 1:
+            raise ValueError("a cache's tensors are on one device")
+        self.device = devices.pop()
         self.c = _Cache(_CODES[k.dtype], _ACTS[act_dtype], kv_heads, head_dim, page_tokens, 0, pages,
                         k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr())
+        self._ref = ctypes.byref(self.c)
 
     def tensors(self):
         return self.k, self.v, self.k_scale, self.v_scale
@@ -153,18 +169,25 @@ class Batch:
         self.table, self.tokens, self.requests = table, int(tokens), R
         self.starts, self.lens = ints(starts, R + 1, "starts"), ints(lens, R, "lens")
         self.max_new = max(1, self.tokens) if max_new is None else int(max_new)
+        self.device = table.get_device()
+        if self.starts.get_device() != self.device or self.lens.get_device() != self.device:
+            raise ValueError("a batch's tensors are on one device")
         self.c = _Batch(R, self.tokens, self.max_new, width, table.stride(0) if R > 1 else 0, 0,
                         self.starts.data_ptr(), self.lens.data_ptr(), table.data_ptr())
+        self._ref = ctypes.byref(self.c)
 
 
 def pages(batch: Batch, held, fresh, free_pages, slots, positions, taken, *, page_tokens, stream=None):
     """Block tables, slots and positions of a step (include/spear_kv.h)."""
-    dev = _device_of(batch.table, batch.starts, batch.lens, held, fresh, free_pages, slots, positions, taken)
+    dev = _device_of(held, fresh, free_pages, slots, positions, taken)
+    _on(batch, dev)
     R, T = batch.requests, batch.tokens
     a = _Pages(page_tokens, free_pages.numel(), _ints(held, R, "held"), _ints(fresh, R, "fresh"),
                _ints(free_pages, free_pages.numel(), "free_pages"), _ints(slots, T, "slots"),
                _ints(positions, T, "positions"), _ints(taken, 2, "taken"))
-    _check(LIB.spear_kv_pages(ctypes.byref(batch.c), ctypes.byref(a), _raw_stream(stream, dev)), "spear_kv_pages")
+    st = LIB.spear_kv_pages(batch._ref, ctypes.byref(a), _raw_stream(stream, dev))
+    if st != 0:
+        raise SpearError(st, "spear_kv_pages")
 
 
 class Rope:
@@ -180,36 +203,53 @@ class Rope:
             freqs = freqs.to(device)
         if freqs.dtype is not torch.int64 or freqs.numel() != rotary_dim // 2 or not freqs.is_contiguous():
             raise ValueError("freqs is [rotary_dim / 2] int64")
-        self.freqs = freqs
+        self.freqs, self.device = freqs, freqs.get_device()
         self.c = _Rope(rotary_dim, int(bool(interleaved)), magnitude, 0, freqs.data_ptr())
+
+
+_NO_ROPE = _Rope(0, 0, 1.0, 0, None)
 
 
 def append(cache: Cache, k, v, slots, positions=None, *, rope: Rope | None = None, q=None, q_out=None,
            stream=None):
     """New tokens into the cache, queries turned on the way (include/spear_kv.h):
     k, v [tokens][kv_heads][head_dim], q, q_out [tokens][heads][head_dim]."""
-    dev = _device_of(k, v, slots, positions, q, q_out, rope.freqs if rope else None, *cache.tensors())
-    T, act, kv = k.shape[0], cache.act_dtype, (k.shape[0], cache.kv_heads, cache.head_dim)
+    dev = _device_of(k, v, slots, positions, q, q_out)
+    _on(cache, dev)
+    T, D, act = k.shape[0], cache.head_dim, cache.act_dtype
+    kv = (T, cache.kv_heads, D)
     if (q is None) != (q_out is None) or (rope is not None and positions is None):
         raise ValueError("append: q and q_out go together, and a rotation takes positions")
-    qs = (T, q.shape[1], cache.head_dim) if q is not None else None
-    a = _Append(T, 0 if q is None else q.shape[1], None if q is None else q.data_ptr(), k.data_ptr(), v.data_ptr(),
-                None if q is None else q_out.data_ptr(), 0 if q is None else _rows(q, qs, act, "q"),
-                _rows(k, kv, act, "k"), _rows(v, kv, act, "v"), 0 if q is None else _rows(q_out, qs, act, "q_out"),
-                _ints(slots, T, "slots"), None if positions is None else _ints(positions, T, "positions"),
-                rope.c if rope is not None else _Rope(0, 0, 1.0, 0, None))
-    _check(LIB.spear_kv_append(ctypes.byref(cache.c), ctypes.byref(a), _raw_stream(stream, dev)), "spear_kv_append")
+    c = _NO_ROPE
+    if rope is not None:
+        c = rope.c
+        if c.rotary_dim:
+            _on(rope, dev)
+    kl, vl = _rows(k, kv, act, "k"), _rows(v, kv, act, "v")
+    at = None if positions is None else _ints(positions, T, "positions")
+    if q is None:
+        a = _Append(T, 0, None, k.data_ptr(), v.data_ptr(), None, 0, kl, vl, 0, _ints(slots, T, "slots"), at, c)
+    else:
+        qs = (T, q.shape[1], D)
+        a = _Append(T, qs[1], q.data_ptr(), k.data_ptr(), v.data_ptr(), q_out.data_ptr(), _rows(q, qs, act, "q"), kl,
+                    vl, _rows(q_out, qs, act, "q_out"), _ints(slots, T, "slots"), at, c)
+    st = LIB.spear_kv_append(cache._ref, ctypes.byref(a), _raw_stream(stream, dev))
+    if st != 0:
+        raise SpearError(st, "spear_kv_append")
 
 
 def read(cache: Cache, slots, k_out, v_out, stream=None):
     """What the tokens at `slots` stand for: k_out, v_out [n][kv_heads][head_dim]."""
-    dev = _device_of(slots, k_out, v_out, *cache.tensors())
+    dev = _device_of(slots, k_out, v_out)
+    _on(cache, dev)
     n = slots.numel()
     for t, what in ((k_out, "k_out"), (v_out, "v_out")):
         if t.dtype is not cache.act_dtype or not t.is_contiguous() or t.numel() != n * cache.kv_heads * cache.head_dim:
             raise ValueError(f"read: {what} is [{n}][kv_heads][head_dim] in the activation dtype")
-    _check(LIB.spear_kv_read(ctypes.byref(cache.c), n, _ints(slots, n, "slots"), k_out.data_ptr(), v_out.data_ptr(),
-                             _raw_stream(stream, dev)), "spear_kv_read")
+    st = LIB.spear_kv_read(cache._ref, n, _ints(slots, n, "slots"), k_out.data_ptr(), v_out.data_ptr(),
+                           _raw_stream(stream, dev))
+    if st != 0:
+        raise SpearError(st, "spear_kv_read")
 
 
 class AttentionPlan:
@@ -226,6 +266,11 @@ class AttentionPlan:
         self.workspace_bytes = work.value
         self.buffer = torch.empty(plan.value, dtype=torch.uint8, device=batch.table.device)
         self.c.plan, self.c.plan_bytes = self.buffer.data_ptr(), plan.value
+        self.device = batch.device
+        if prefix is not None and prefix.get_device() != self.device:
+            raise ValueError("a plan's tensors are on one device")
+        self._batch = ctypes.pointer(batch.c)
+        self._prefix = None if prefix is None else prefix.data_ptr()
 
 
 def attention_workspace(plan: AttentionPlan) -> int:
@@ -235,9 +280,11 @@ def attention_workspace(plan: AttentionPlan) -> int:
 
 def attention_plan(plan: AttentionPlan, stream=None):
     """Writes the plan from the batch's starts and lens, window and prefix."""
-    b = plan.batch
-    dev = _device_of(b.table, b.starts, b.lens, plan.prefix, plan.buffer)
-    _check(LIB.spear_attention_plan(ctypes.byref(plan.c), _raw_stream(stream, dev)), "spear_attention_plan")
+    dev = _device_of(plan.buffer)
+    _on(plan.batch, dev)
+    st = LIB.spear_attention_plan(ctypes.byref(plan.c), _raw_stream(stream, dev))
+    if st != 0:
+        raise SpearError(st, "spear_attention_plan")
 
 
 def attention(plan: AttentionPlan, q, out, *, workspace, cache: Cache | None = None, scale=None, softcap=0.0,
@@ -245,22 +292,22 @@ def attention(plan: AttentionPlan, q, out, *, workspace, cache: Cache | None = N
     """Attention of the batch's rows over the cache (the plan's own unless given:
     another layer's, of the same sizes): q, out [tokens][heads][head_dim]; scale
     1/sqrt(head_dim) unless given; slopes [heads] fp32."""
-    b, cache = plan.batch, plan.cache if cache is None else cache
-    dev = _device_of(q, out, workspace, slopes, plan.buffer, plan.prefix, b.table, b.starts, b.lens, *cache.tensors())
     own = plan.cache
-    if (cache.kv_heads, cache.head_dim, cache.page_tokens) != (own.kv_heads, own.head_dim, own.page_tokens):
+    cache = own if cache is None else cache
+    dev = _device_of(q, out, workspace, slopes)
+    _on(plan, dev)
+    _on(cache, dev)
+    D, heads = cache.head_dim, plan.heads
+    if cache is not own and (cache.kv_heads, D, cache.page_tokens) != (own.kv_heads, own.head_dim, own.page_tokens):
         raise ValueError("attention: a cache of the plan's sizes")
-    shape = (b.tokens, plan.heads, cache.head_dim)
-    if slopes is not None and (slopes.dtype is not torch.float32 or slopes.numel() != plan.heads or
-                               not slopes.is_contiguous()):
+    if slopes is not None and (slopes.dtype is not torch.float32 or slopes.numel() != heads or not slopes.is_contiguous()):
         raise ValueError("attention: slopes is [heads] fp32")
-    a = _Attention.from_buffer_copy(plan.c)
-    a.cache = ctypes.pointer(cache.c)
-    a.q, a.out = q.data_ptr(), out.data_ptr()
-    a.q_ld, a.out_ld = _rows(q, shape, cache.act_dtype, "q"), _rows(out, shape, cache.act_dtype, "out")
-    a.slopes = None if slopes is None else slopes.data_ptr()
-    a.scale = cache.head_dim ** -0.5 if scale is None else scale
-    a.softcap = softcap
-    a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    _check(LIB.spear_attention(ctypes.byref(a), _raw_stream(stream, dev)), "spear_attention")
+    shape, act = (plan.batch.tokens, heads, D), cache.act_dtype
+    a = _Attention(ctypes.pointer(cache.c), plan._batch, heads, plan.c.window, plan._prefix, plan.c.plan,
+                   plan.c.plan_bytes, q.data_ptr(), out.data_ptr(), _rows(q, shape, act, "q"), _rows(out, shape, act, "out"),
+                   None if slopes is None else slopes.data_ptr(), D ** -0.5 if scale is None else scale, softcap,
+                   workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    st = LIB.spear_attention(ctypes.byref(a), _raw_stream(stream, dev))
+    if st != 0:
+        raise SpearError(st, "spear_attention")
     return out
