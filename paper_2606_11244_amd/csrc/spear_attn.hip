@@ -9,6 +9,10 @@ constexpr float kLowest = -3.402823466e38f;  // running maximum of a row that ha
 // How far scores may pass a row's maximum, in powers of two, before it is moved and
 // what was summed is scaled: weights up to 2^8 keep their precision in either type.
 constexpr float kSlack = 8.f;
+// Where the maximum costs more than the weights: a step's weights are made against the
+// maximum so far, and once more against a new one only where a row's sum of them (half
+// a row's, a lane's) passes 2^12, far from fp16's end.
+constexpr float kMostSum = 4096.f;
 
 #if !SPEAR_BF16_UNIT
 // ---------------------------------------------------------------------------
@@ -265,6 +269,15 @@ __device__ __forceinline__ float max_halves(float x) {
 __device__ __forceinline__ float max_sixteens(float x) {
   const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return max_halves(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+
+// c plus both weights of a pair, as they are held
+template <int DT>
+__device__ __forceinline__ float add2(uint32_t pair, float c) {
+  if constexpr (DT == DT_F16)
+    return __builtin_amdgcn_fdot2(__builtin_bit_cast(h16x2, pair), h16x2{(_Float16)1.f, (_Float16)1.f}, c, false);
+  else
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(b16x2, pair), b16x2{(__bf16)1.f, (__bf16)1.f}, c, false);
 }
 
 // A score in powers of two. OPT: capped, or biased by distance.
@@ -902,11 +915,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_attend_mid(AttnParams p) {
 // Bound: the MFMAs and the exponentials beside them.
 // ---------------------------------------------------------------------------
 template <int DT, int FMT, int D, bool OPT>
-__global__ __launch_bounds__(512) void k_attend_tile(AttnParams p) {
+__global__ __launch_bounds__(2 * tile_rows(D), 2) void k_attend_tile(AttnParams p) {
   constexpr int KP = D * 2 + 16, VP = kStep * 2 + 16, PIECES = D / 16;  // pitches in bytes; pieces of a row of K
-  constexpr int KBYTES = kStep * KP, BUF = KBYTES + D * VP;
+  constexpr int KBYTES = kStep * KP, BUF = KBYTES + D * VP, ROWS = tile_rows(D), THREADS = 2 * ROWS;
   __shared__ __attribute__((aligned(16))) char lds[2 * BUF];
-  __shared__ float s_ks[2][4];
+  __shared__ __attribute__((aligned(16))) float s_ks[2][4];
   __shared__ int s_last;
   early(p);
   const int head = blockIdx.x % p.c.Hkv, idx = blockIdx.x / p.c.Hkv;
@@ -914,7 +927,7 @@ __global__ __launch_bounds__(512) void k_attend_tile(AttnParams p) {
   if (it.key != p.key) return;
   if (p.c.pages == 0) it.s1 = it.s0;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c = lane & 31, h = lane >> 5;
-  const int P = p.c.P, live_rows = it.rows * p.group, wave_row = it.tile * kTileRows + 32 * wave;
+  const int P = p.c.P, live_rows = it.rows * p.group, wave_row = it.tile * ROWS + 32 * wave;
   const int row = wave_row + c;
   const bool active = wave_row < live_rows, mine = row < live_rows;
   const int i = mine ? row / p.group : it.rows - 1, hq = head * p.group + (mine ? row % p.group : 0);
@@ -935,10 +948,10 @@ __global__ __launch_bounds__(512) void k_attend_tile(AttnParams p) {
   const int32_t* table = p.table + it.r * p.ld;
   const uint32_t page_bytes = P * D, pool_bytes = p.c.Hkv * page_bytes;
 
-  // staging: K by threads of (token, piece), V by threads of (feature, run); D = 64
-  // has half as many pieces, K's in the first half of the workgroup, V's in the other
-  const bool does_k = D == 128 || tid < 256, does_v = D == 128 || tid >= 256;
-  const int k_token = (tid / PIECES) & 63, k_piece = tid % PIECES, v_feature = (tid >> 2) % D, v_run = tid & 3;
+  // staging: a thread's pieces are N of K, TOKENS apart, and N of V, FEATURES apart, of one run
+  constexpr int N = kStep * PIECES / THREADS, TOKENS = THREADS / PIECES, FEATURES = THREADS / 4;
+  static_assert(N >= 1 && TOKENS % 16 == 0 && N * FEATURES == D, "whole pieces");
+  const int k_token = tid / PIECES, k_piece = tid % PIECES, v_feature = tid >> 2, v_run = tid & 3;
   const uint8_t* k_head = p.c.k + (int64_t)head * page_bytes + 16 * k_piece;
   const uint8_t* v_head = p.c.v + (int64_t)head * page_bytes + v_feature * P;
   // table entries of a step's runs; whether they are pages is looked at where they are
@@ -950,49 +963,62 @@ __global__ __launch_bounds__(512) void k_attend_tile(AttnParams p) {
     return page;
   };
   auto page_of = [&](int entry) { return (uint32_t)entry < (uint32_t)p.c.pages ? entry : -1; };
-  u32x4 kr, vr;
+  u32x4 kr[N], vr[N];
   float2 sc;  // scales of this thread's run of V
-  int entry_k = 0, entry_v = 0, held_v = 0;
+  int entry_k[N], entry_v, held_v = 0;
+  auto entries = [&](int s) {
+#pragma unroll
+    for (int x = 0; x < N; ++x) entry_k[x] = entry_at(s, (k_token + TOKENS * x) >> 4);
+    entry_v = entry_at(s, v_run);
+  };
   auto fetch = [&](int s) {  // entries of s are there; those of s + 1 follow
-    const uint32_t page_k = max(page_of(entry_k), 0), page_v = max(held_v = page_of(entry_v), 0);
-    if (does_k) kr = ldg16(k_head + (uint64_t)page_k * pool_bytes + ((s * kStep + k_token) & (P - 1)) * D);
-    if (does_v) vr = ldg16(v_head + (uint64_t)page_v * pool_bytes + ((s * kStep + 16 * v_run) & (P - 1)));
+#pragma unroll
+    for (int x = 0; x < N; ++x)
+      kr[x] = ldg16(k_head + (uint64_t)(uint32_t)max(page_of(entry_k[x]), 0) * pool_bytes + ((s * kStep + k_token + TOKENS * x) & (P - 1)) * D);
+    const uint32_t page_v = max(held_v = page_of(entry_v), 0);
+    const uint8_t* v = v_head + (uint64_t)page_v * pool_bytes + ((s * kStep + 16 * v_run) & (P - 1));
+#pragma unroll
+    for (int x = 0; x < N; ++x) vr[x] = ldg16(v + FEATURES * x * P);
     const uint64_t ph = (uint64_t)page_v * p.c.Hkv + head;
     sc = make_float2(p.c.k_scale[ph], p.c.v_scale[ph]);
-    entry_k = entry_at(s + 1, k_token >> 4), entry_v = entry_at(s + 1, v_run);
+    entries(s + 1);
   };
   auto stage = [&](int s) {
     char* buf = lds + (s & 1) * BUF;
-    if (does_k) {
-      u32x4* k = (u32x4*)(buf + k_token * KP + 32 * k_piece);
-      k[0] = operand8<DT, FMT>(kr[0], kr[1], 1.f);
-      k[1] = operand8<DT, FMT>(kr[2], kr[3], 1.f);
+#pragma unroll
+    for (int x = 0; x < N; ++x) {
+      u32x4* k = (u32x4*)(buf + (k_token + TOKENS * x) * KP + 32 * k_piece);
+      k[0] = operand8<DT, FMT>(kr[x][0], kr[x][1], 1.f);
+      k[1] = operand8<DT, FMT>(kr[x][2], kr[x][3], 1.f);
     }
     float f = sc.y;
     const int j0 = s * kStep + 16 * v_run;
     if (held_v < 0 || j0 + 16 > it.end || j0 < it.first) {
       const uint32_t live = held_v >= 0 ? live_tokens(j0, it) & 0xFFFFu : 0u;
-      vr &= byte_mask(live);
+      const u32x4 bytes = byte_mask(live);
+#pragma unroll
+      for (int x = 0; x < N; ++x) vr[x] &= bytes;
       if (!live) f = 1.f;
     }
-    if (does_v) {
-      u32x4* v = (u32x4*)(buf + KBYTES + v_feature * VP + 32 * v_run);
-      u32x4 a, b;
+#pragma unroll
+    for (int x = 0; x < N; ++x) {
+      u32x4* v = (u32x4*)(buf + KBYTES + (v_feature + FEATURES * x) * VP + 32 * v_run);
       if (FMT == KV_INT8 && (DT != DT_F16 || f < 6.103515625e-5f)) {  // (fp16: a scale below its normal range)
-        a = i8x8_to_act<DT>(vr[0], vr[2], f), b = i8x8_to_act<DT>(vr[1], vr[3], f);
+        v[0] = i8x8_to_act<DT>(vr[x][0], vr[x][2], f);
+        v[1] = i8x8_to_act<DT>(vr[x][1], vr[x][3], f);
       } else {
-        a = v_operand8<DT, FMT>(vr[0], vr[2], f), b = v_operand8<DT, FMT>(vr[1], vr[3], f);
+        v[0] = v_operand8<DT, FMT>(vr[x][0], vr[x][2], f);
+        v[1] = v_operand8<DT, FMT>(vr[x][1], vr[x][3], f);
       }
-      v[0] = a, v[1] = b;
     }
-    if (tid >= 256 && tid < 260)  // (runs 0..3) no page: a scale that is no number, for the waves to see
-      s_ks[s & 1][v_run] = held_v >= 0 ? sc.x : __builtin_nanf("");
+    // (runs 0..3) what a dot product is of a score; no page: below zero, for the waves to see
+    if (tid < 4) s_ks[s & 1][tid] = held_v < 0 ? -1.f : OPT ? sc.x : dot_factor(sc.x, opt);
   };
 
   f32x16 o[D / 32] = {};
   float m = kLowest, l = 0.f;
   if (it.s0 < it.s1) {
-    entry_k = entry_at(it.s0, k_token >> 4), entry_v = entry_at(it.s0, v_run);
+    entries(it.s0);
     fetch(it.s0);
     stage(it.s0);
     if (it.s0 + 1 < it.s1) fetch(it.s0 + 1);
@@ -1014,15 +1040,12 @@ __global__ __launch_bounds__(512) void k_attend_tile(AttnParams p) {
 #pragma unroll
         for (int t = 0; t < 2; ++t)
           st[t] = mfma32<DT>(*(const u32x4*)(buf + (32 * t + c) * KP + 32 * x + 16 * h), q[x], st[t]);
-      float ks[4];
-#pragma unroll
-      for (int r = 0; r < 4; ++r) ks[r] = s_ks[s & 1][r];
-      const bool pages_there = __all(ks[0] == ks[0] && ks[1] == ks[1] && ks[2] == ks[2] && ks[3] == ks[3]);
+      const f32x4 ks = *(const f32x4*)s_ks[s & 1];
+      const bool pages_there = __all(fminf(fminf(ks[0], ks[1]), fminf(ks[2], ks[3])) > 0.f);
       const bool whole = j0 + kStep <= min(it.end, pos_lo + 1) && pos_hi - j0 < p.window && pages_there;
-      float f[4], top = kLowest;  // f: what st is of a score
-#pragma unroll
-      for (int r = 0; r < 4; ++r) f[r] = OPT ? 1.f : dot_factor(ks[r], opt);
+      f32x4 f = ks;  // what st is of a score
       if constexpr (OPT) {
+        f = f32x4{1.f, 1.f, 1.f, 1.f};
 #pragma unroll
         for (int e = 0; e < 32; ++e)
           st[e >> 4][e & 15] = score2(st[e >> 4][e & 15], ks[e >> 3], opt, pos, j0 + 8 * (e >> 2) + 4 * h + (e & 3));
@@ -1031,51 +1054,57 @@ __global__ __launch_bounds__(512) void k_attend_tile(AttnParams p) {
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
           uint32_t sees = seen_tokens(j0 + 32 * t, it, pos, p.window);
-          sees &= (ks[2 * t] == ks[2 * t] ? 0xFFFFu : 0u) | (ks[2 * t + 1] == ks[2 * t + 1] ? 0xFFFF0000u : 0u);
+          sees &= (ks[2 * t] > 0.f ? 0xFFFFu : 0u) | (ks[2 * t + 1] > 0.f ? 0xFFFF0000u : 0u);
           sees >>= 4 * h;
 #pragma unroll
           for (int e = 0; e < 16; ++e) st[t][e] = where_seen(st[t][e], sees, 8 * (e >> 2) + (e & 3));
         }
-      }
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        float x = st[r >> 1][8 * (r & 1)];
-#pragma unroll
-        for (int e = 1; e < 8; ++e) x = fmaxf(x, st[r >> 1][8 * (r & 1) + e]);
-        top = fmaxf(top, x * f[r]);
+        for (int r = 0; r < 4; ++r) f[r] = fabsf(f[r]);
       }
-      top = max_halves(top);
-      if (__any(top > m + kSlack)) {
-        const float now = fmaxf(m, top), fade = __builtin_amdgcn_exp2f(m - now);
+      u32x4 pw[4];  // sixteen tokens each
+      float sum;
+      for (int pass = 0;; ++pass) {
+        sum = 0.f;
+#pragma unroll
+        for (int y = 0; y < 4; ++y)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int x = 8 * (y & 1) + 2 * e;
+            pw[y][e] = pack2<DT>(__builtin_amdgcn_exp2f(__builtin_fmaf(st[y >> 1][x], f[y], -m)),
+                                 __builtin_amdgcn_exp2f(__builtin_fmaf(st[y >> 1][x + 1], f[y], -m)));
+            sum = add2<DT>(pw[y][e], sum);
+          }
+        if (pass || !__any(!(sum <= kMostSum))) break;
+        float top = kLowest;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          float x = st[r >> 1][8 * (r & 1)];
+#pragma unroll
+          for (int e = 1; e < 8; ++e) x = fmaxf(x, st[r >> 1][8 * (r & 1) + e]);
+          top = fmaxf(top, x * f[r]);
+        }
+        const float now = fmaxf(m, max_halves(top)), fade = __builtin_amdgcn_exp2f(m - now);
         m = now;
         l *= fade;
 #pragma unroll
         for (int d = 0; d < D / 32; ++d) o[d] *= fade;
       }
+      l += sum;
 #pragma unroll
-      for (int y = 0; y < 4; ++y) {  // sixteen tokens
-        float w[8];
-        u32x4 pw;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          w[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[y >> 1][8 * (y & 1) + e], f[y], -m));
-          l += w[e];
-        }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) pw[e] = pack2<DT>(w[2 * e], w[2 * e + 1]);
+      for (int y = 0; y < 4; ++y)
 #pragma unroll
         for (int d = 0; d < D / 32; ++d)
-          o[d] = mfma32<DT>(*(const u32x4*)(buf + KBYTES + (32 * d + c) * VP + 32 * y + 16 * h), pw, o[d]);
-      }
+          o[d] = mfma32<DT>(*(const u32x4*)(buf + KBYTES + (32 * d + c) * VP + 32 * y + 16 * h), pw[y], o[d]);
     }
     __syncthreads();
   }
   l += __shfl_xor(l, 32);
   if (it.splits > 1) {
-    const uint32_t size = kTileRows * (D + 2) * 4, slot = (uint32_t)it.part * p.c.Hkv + head;
+    const uint32_t size = ROWS * (D + 2) * 4, slot = (uint32_t)it.part * p.c.Hkv + head;
     const rsrc_t r = make_rsrc((const char*)p.parts_tile + (size_t)slot * size, (uint32_t)((it.splits - 1) * p.c.Hkv + 1) * size);
     const uint32_t at = (uint32_t)it.split * p.c.Hkv * size, own = ((32 * wave + c) * D + 4 * h) * 4;
-    const uint32_t own_m = (kTileRows * D + 32 * wave + c) * 4;
+    const uint32_t own_m = (ROWS * D + 32 * wave + c) * 4;
     if (active) {
 #pragma unroll
       for (int d = 0; d < D / 32; ++d)
@@ -1083,7 +1112,7 @@ __global__ __launch_bounds__(512) void k_attend_tile(AttnParams p) {
         for (int x = 0; x < 4; ++x)
           bst128c(r, at + own + (32 * d + 8 * x) * 4, f32x4{o[d][4 * x], o[d][4 * x + 1], o[d][4 * x + 2], o[d][4 * x + 3]});
       float* ml = p.parts_tile + ((size_t)slot * size + at + own_m) / 4;
-      if (h == 0) st_agent(ml, m), st_agent(ml + kTileRows, l);
+      if (h == 0) st_agent(ml, m), st_agent(ml + ROWS, l);
     }
     complete_and_sync();
     if (tid == 0) s_last = arrive_last(p.counters_tile + slot, it.splits);
@@ -1095,7 +1124,7 @@ __global__ __launch_bounds__(512) void k_attend_tile(AttnParams p) {
       for (int d = 0; d < D / 32; ++d) o[d] = f32x16{};
       for (int b = 0; b < it.splits; ++b) {
         const uint32_t off = b * p.c.Hkv * size;
-        const float pm = __uint_as_float(bld32c(r, off + own_m)), pl = __uint_as_float(bld32c(r, off + own_m + kTileRows * 4));
+        const float pm = __uint_as_float(bld32c(r, off + own_m)), pl = __uint_as_float(bld32c(r, off + own_m + ROWS * 4));
         const float now = fmaxf(m, pm), f0 = __builtin_amdgcn_exp2f(m - now), f1 = __builtin_amdgcn_exp2f(pm - now);
         m = now;
         l = l * f0 + pl * f1;
@@ -1128,7 +1157,7 @@ static hipError_t attend_launch(const AttnParams& p, const AttnShape& z, hipStre
     return hipGetLastError();
   }
   if (tiles) {
-    hipLaunchKernelGGL((k_attend_tile<DTC, FMT, D, OPT>), dim3(tiles), dim3(512), 0, st, p);
+    hipLaunchKernelGGL((k_attend_tile<DTC, FMT, D, OPT>), dim3(tiles), dim3(2 * tile_rows(D)), 0, st, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }

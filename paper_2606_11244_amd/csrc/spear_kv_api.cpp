@@ -15,7 +15,7 @@
 #define XRL 8
 #define XTG 256
 #define XTL 8
-#define XFT 384
+#define XFR 98304
 #endif
 #ifndef XMG
 #define XMG 384
@@ -238,8 +238,8 @@ spear_status_t check_attention(const spear_attention_t* a, bool buffers) {
 }
 
 
-// Tiles of 256 rows, over all kv heads, from which on these are taken.
-constexpr int kFillTiles = XFT;
+// Rows, over all kv heads, from which on tiles are the large ones.
+constexpr int kFillRows = XFR;
 // Stretches wanted of each kernel, over all kv heads, and a stretch's least steps.
 constexpr int kRowsGoal = XRG, kRowsLeast = XRL, kTileGoal = XTG, kTileLeast = XTL, kMidGoal = XMG,
               kMidLeast = XML;
@@ -276,7 +276,8 @@ AttnLayout attention_layout(const spear_attention_t* a) {
   // sum over tiles of max(1, ceil(steps / c)) with c >= all steps / goal
   z.max_rows = rows ? (int)served + z.goal_rows : 0;
   z.least_rows = kRowsLeast;
-  z.tile_rows = (T * group + kTileRows - 1) / kTileRows * hkv < kFillTiles ? kMidRows : kTileRows;
+  const int big = tile_rows(c->head_dim);
+  z.tile_rows = (T * group + big - 1) / big * hkv < kFillRows / big ? kMidRows : big;
   z.goal_tile = (int)(((z.tile_rows == kMidRows ? kMidGoal : kTileGoal) + hkv - 1) / hkv);
   z.least_tile = z.tile_rows == kMidRows ? kMidLeast : kTileLeast;
   z.max_tile = tile ? (int)(T * group / z.tile_rows + served) + z.goal_tile : 0;

@@ -55,8 +55,9 @@ struct KvReadParams {
 // ---- attention ----
 // A request's rows (its new tokens, each with the query heads of one kv head) go
 // to attend_rows where they are at most kRows, else, in tiles, to attend_mid
-// (kMidRows) or k_attend_tile (kTileRows). All walk the cache in steps of kStep tokens.
-constexpr int kRows = 16, kMidRows = 32, kTileRows = 256, kStep = 64;
+// (kMidRows) or k_attend_tile (tile_rows). All walk the cache in steps of kStep tokens.
+constexpr int kRows = 16, kMidRows = 32, kStep = 64;
+constexpr int tile_rows(int head_dim) { return head_dim == 128 ? 256 : 128; }
 constexpr int kAttnCounters = 2048;  // of each kernel
 
 // one workgroup's share (of each kv head): some rows over some steps
@@ -71,7 +72,7 @@ struct AttnItem {
 
 // sizes that the host fixes from the batch's and the heads' sizes alone
 struct AttnShape {
-  int tile_rows;               // kMidRows or kTileRows
+  int tile_rows;               // kMidRows or tile_rows(head_dim)
   int goal_rows, goal_tile;    // stretches wanted: enough workgroups to fill the GPU
   int least_rows, least_tile;  // least steps of a stretch
   int max_rows, max_tile;      // items there can be
