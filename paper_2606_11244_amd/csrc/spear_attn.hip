@@ -208,9 +208,9 @@ hipError_t launch_attention_plan(const AttnPlanParams& p, hipStream_t st) {
 
 // ---------------------------------------------------------------------------
 // Codes as operands: eight codes in the activation type. K's scale goes on the
-// fp32 score. V's goes on V (exact: a power of two; fp16 codes times a scale from
-// 2^-14 on, what is below on the weight) or, where a code of INT8 becomes bf16
-// and a product more would be a rounding and an instruction, on the weight.
+// fp32 score. V's goes on V (exact: a power of two; of INT8 codes in fp16 a scale
+// from 2^-14 on, what is below on the weight) or, where a code of INT8 becomes bf16
+// and a product more would be an instruction for two codes, on the weight.
 // ---------------------------------------------------------------------------
 typedef _Float16 h16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 b16x2 __attribute__((ext_vector_type(2)));
@@ -248,9 +248,9 @@ __device__ __forceinline__ u32x4 v_operand8(uint32_t w0, uint32_t w1, float scal
 // V's scale as (factor of V, factor of the weight)
 template <int DT, int FMT>
 __device__ __forceinline__ float2 v_factors(float s) {
-  if constexpr (DT == DT_F16) return make_float2(fmaxf(s, 6.103515625e-5f), fminf(s * 16384.f, 1.f));
-  else if constexpr (FMT == KV_INT8) return make_float2(1.f, s);
-  else return make_float2(s, 1.f);
+  if constexpr (FMT == KV_E4M3) return make_float2(s, 1.f);  // (one rounding to the activation type, with the code's)
+  else if constexpr (DT == DT_F16) return make_float2(fmaxf(s, 6.103515625e-5f), fminf(s * 16384.f, 1.f));
+  else return make_float2(1.f, s);
 }
 
 template <int DT>
@@ -278,6 +278,11 @@ __device__ __forceinline__ float add2(uint32_t pair, float c) {
     return __builtin_amdgcn_fdot2(__builtin_bit_cast(h16x2, pair), h16x2{(_Float16)1.f, (_Float16)1.f}, c, false);
   else
     return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(b16x2, pair), b16x2{(__bf16)1.f, (__bf16)1.f}, c, false);
+}
+
+// a pair of fp16 weights times a power of two of at most one
+__device__ __forceinline__ uint32_t scaled2(uint32_t pair, float f) {
+  return __builtin_bit_cast(uint32_t, __builtin_bit_cast(h16x2, pair) * h16x2{(_Float16)f, (_Float16)f});
 }
 
 // A score in powers of two. OPT: capped, or biased by distance.
@@ -491,7 +496,7 @@ __device__ __forceinline__ void attend_rows(const AttnParams& p, uint32_t block,
         w[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[e >> 2][e & 3], fk, -m));
         l += w[e];
       }
-      if ((DT != DT_F16 && FMT == KV_INT8) || (DT == DT_F16 && __any(f.y != 1.f))) {
+      if (FMT == KV_INT8 && (DT != DT_F16 || __any(f.y != 1.f))) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) w[e] *= f.y;
       }
@@ -756,7 +761,7 @@ __device__ __forceinline__ void attend_mid(const AttnParams& p, uint32_t block, 
 #pragma unroll
       for (int y = 0; y < Y; ++y) {
         const ScoreOptions opt{scale, p.softcap, slope2[y]};
-        float g[2], top = kLowest;  // g: what st is of a score
+        float g[2];  // what st is of a score
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
           g[t] = OPT ? 1.f : dot_factor(sc.at[t].x, opt);
@@ -769,34 +774,42 @@ __device__ __forceinline__ void attend_mid(const AttnParams& p, uint32_t block, 
 #pragma unroll
             for (int e = 0; e < 16; ++e) st[y][t][e] = where_seen(st[y][t][e], sees, e);
           }
-          float x = st[y][t][0];
-#pragma unroll
-          for (int e = 1; e < 16; ++e) x = fmaxf(x, st[y][t][e]);
-          top = fmaxf(top, x * g[t]);
         }
-        top = max_halves(top);
-        if (__any(top > m[y] + kSlack)) {
-          const float now = fmaxf(m[y], top), fade = __builtin_amdgcn_exp2f(m[y] - now);
+        // a step's weights against the maximum so far, and once more where a sum passes
+        float sum;
+        for (int pass = 0;; ++pass) {
+          sum = 0.f;
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const float u = __builtin_amdgcn_exp2f(__builtin_fmaf(st[y][t][2 * e], g[t], -m[y]));
+              const float v = __builtin_amdgcn_exp2f(__builtin_fmaf(st[y][t][2 * e + 1], g[t], -m[y]));
+              if constexpr (DT != DT_F16 && FMT == KV_INT8) {
+                sum += u + v;
+                pw[y][2 * t + (e >> 2)][e & 3] = pack2<DT>(u * f[t].y, v * f[t].y);
+              } else {
+                const uint32_t w = pack2<DT>(u, v);
+                sum = add2<DT>(w, sum);
+                pw[y][2 * t + (e >> 2)][e & 3] = DT == DT_F16 && FMT == KV_INT8 ? scaled2(w, f[t].y) : w;
+              }
+            }
+          if (pass || !__any(!(sum <= kMostSum))) break;
+          float top = kLowest;
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            float x = st[y][t][0];
+#pragma unroll
+            for (int e = 1; e < 16; ++e) x = fmaxf(x, st[y][t][e]);
+            top = fmaxf(top, x * g[t]);
+          }
+          const float now = fmaxf(m[y], max_halves(top)), fade = __builtin_amdgcn_exp2f(m[y] - now);
           m[y] = now;
           l[y] *= fade;
 #pragma unroll
           for (int d = 0; d < DTILES; ++d) o[y][d] *= fade;
         }
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          float w[16];
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            w[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[y][t][e], g[t], -m[y]));
-            l[y] += w[e];
-          }
-          if ((DT != DT_F16 && FMT == KV_INT8) || (DT == DT_F16 && __any(f[t].y != 1.f))) {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) w[e] *= f[t].y;
-          }
-#pragma unroll
-          for (int e = 0; e < 8; ++e) pw[y][2 * t + (e >> 2)][e & 3] = pack2<DT>(w[2 * e], w[2 * e + 1]);
-        }
+        l[y] += sum;
       }
       __builtin_amdgcn_sched_barrier(0);  // (V's operands made ahead of the softmax would not fit the registers)
 #pragma unroll

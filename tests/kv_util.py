@@ -174,7 +174,10 @@ def plain_attention(q, k, v, starts, lens, heads, *, scale, softcap=0.0, slopes=
             off = 2.0 ** -24 * ((D + 16) * size + 8 * (s.masked_fill(~seen, 0).abs() + b.abs()) + 16)
             po = p * off
             e = (u + po.sum(1, keepdim=True) + L * 2.0 ** -24) * a + po @ vv.abs() + u * o.abs()
-            if act is torch.float16:  # weights below 2^-14 of the largest are held to 2^-25, outputs too
-                e = e + 2.0 ** -25 * (L * vv.abs().amax() + 1)
+            if act is torch.float16:
+                # weights below 2^-14 of the largest are held to 2^-25; so is a value of v below 2^-14, which is
+                # a code times any power of two and need not be one of fp16's multiples of 2^-24 (weights sum
+                # to one: 2^-25 in all), and so is the output: 2^-25 once more
+                e = e + 2.0 ** -25 * (L * vv.abs().amax() + 2)
             out[starts[r]:starts[r] + m, h], bound[starts[r]:starts[r] + m, h] = o, e + 1e-30
     return out, bound

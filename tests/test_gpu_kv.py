@@ -399,6 +399,23 @@ def test_attention_extreme_scores_and_values():
             s.check()
 
 
+@pytest.mark.parametrize("codes", CODES)
+@pytest.mark.parametrize("act,size", [(torch.float16, 2.0 ** -24), (torch.float16, 2.0 ** -20), (torch.float16, 2.0 ** -14),
+                                      (torch.bfloat16, 2.0 ** -90), (torch.float16, 3e4)])
+@pytest.mark.parametrize("lengths", [[(1, 200)], [(20, 200)], [(400, 400)]])
+def test_attention_of_values_at_the_ends_of_the_range(act, codes, size, lengths):
+    """V of the type's least values (in fp16 of few steps of 2^-24) and of its largest, written and read."""
+    s = Setup(lengths, 64 if lengths[0][0] == 400 else 4, 64 if lengths[0][0] == 400 else 1, 64, 16, act, codes)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    L, kvh = lengths[0][1], s.cache.kv_heads
+    slots = [s.table[0][j // 16] * 16 + j % 16 for j in range(L)]
+    k = torch.randn(L, kvh, 64, device="cuda", generator=g).to(act)
+    v = (torch.randn(L, kvh, 64, device="cuda", generator=g).clamp(-2, 2) * size).to(act)
+    s.kv.append(s.cache, k, v, _ints(slots))
+    s.check()
+    assert bool(torch.isfinite(s.out.float()).all()) and (size < 2.0 ** -20 or bool((s.out != 0).any()))
+
+
 @pytest.mark.parametrize("lengths", [[(1, 3000)] * 3, [(128, 900), (1, 50)]])
 def test_attention_is_repeatable(lengths):
     s = Setup(lengths, 8, 1, 128, 64, torch.bfloat16, torch.int8)
