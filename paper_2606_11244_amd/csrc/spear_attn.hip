@@ -86,122 +86,120 @@ __device__ __forceinline__ AttnItem plan_stretch(AttnItem it, int splits, int x,
   return it;
 }
 
+// EACH: requests a thread
+template <int EACH>
 __global__ __launch_bounds__(kPlanThreads) void k_attention_plan(AttnPlanParams p) {
-  __shared__ int32_t s_item[kKvRequests + 1], s_part[kKvRequests], s_tile[kKvRequests + 1];
+  constexpr int R = EACH * kPlanThreads;
+  __shared__ int32_t s_item[R + 1], s_part[R], s_place[R], s_tile[R + 1];
   __shared__ int64_t red[kPlanThreads / 64];
   __shared__ int s_size[kSizes];
-  constexpr int kEach = kKvRequests / kPlanThreads;
-  const int tid = threadIdx.x, each = (p.R + blockDim.x - 1) / blockDim.x;
+  const int tid = threadIdx.x, r0 = tid * EACH;
   // requests: steps of those of few rows, tiles of the others
-  int steps[kEach], tiles[kEach];
-  int64_t sum = 0, tile_sum = 0, total, at;
+  int steps[EACH], tiles[EACH];
+  int64_t sum = 0, tile_sum = 0, total;
 #pragma unroll
-  for (int e = 0; e < kEach; ++e) {
-    const int r = tid * each + e;
+  for (int e = 0; e < EACH; ++e) {
     steps[e] = -1, tiles[e] = 0;
-    if (e >= each || r >= p.R) continue;
-    AttnItem it = plan_request(p, r);
+    if (r0 + e >= p.R) continue;
+    AttnItem it = plan_request(p, r0 + e);
     if (it.rows == 0) continue;
     const int64_t rows = (int64_t)it.rows * p.group;
     if (rows <= kRows) sum += steps[e] = plan_range(p, it, 0, it.rows);
     else tile_sum += tiles[e] = (int)((rows + p.z.tile_rows - 1) / p.z.tile_rows);
   }
+  if (tid < kSizes) s_size[tid] = 0;
   plan_scan(sum, red, &total);
   const int c = max(p.z.least_rows, (int)((total + p.z.goal_rows - 1) / p.z.goal_rows));
-  int64_t items = 0, parts = 0, n_items, n_tiles;
+  // their stretches, long ones first: by size in kSizes classes (where a request stands
+  // in its class is left to chance, and makes no difference to what is computed)
+  int64_t counts = 0;  // items, and partial results in the upper half
+  int place[EACH], size[EACH];
 #pragma unroll
-  for (int e = 0; e < kEach; ++e)
+  for (int e = 0; e < EACH; ++e) {
+    place[e] = size[e] = 0;
+    if (steps[e] < 0) continue;
+    const int k = plan_splits(steps[e], c);
+    counts += k + ((int64_t)(k > 1 ? k : 0) << 32);
+    size[e] = kSizes - 1 - min((int)((int64_t)steps[e] * (kSizes - 1) / ((int64_t)c * k)), kSizes - 1);
+    place[e] = atomicAdd(&s_size[size[e]], k);
+  }
+  int64_t at = plan_scan(counts, red, &total), tile_at = 0, n_tiles = 0;
+  const int n_items = (int)(total & 0xFFFFFFFF);  // at most R + goal_rows
+  if (p.z.max_tile) tile_at = plan_scan(tile_sum, red, &n_tiles);  // (uniform)
+  // (more than the step's rows make: starts that contradict themselves, and no tile is
+  // taken rather than some, whose counters would be left over)
+  if (n_tiles > p.z.max_tile - p.z.goal_tile) n_tiles = 0;
+  int before[EACH];
+#pragma unroll
+  for (int e = 0; e < EACH; ++e) before[e] = 0;
+  for (int i = 0; i < kSizes; ++i) {
+    const int n = s_size[i];
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) before[e] += i < size[e] ? n : 0;
+  }
+#pragma unroll
+  for (int e = 0; e < EACH; ++e) {
+    if (r0 + e >= p.R) continue;
+    s_item[r0 + e] = (int)(at & 0xFFFFFFFF);
+    s_part[r0 + e] = (int)(at >> 32);
+    s_place[r0 + e] = before[e] + place[e];
+    s_tile[r0 + e] = (int)min(tile_at, n_tiles);
+    tile_at += tiles[e];
     if (steps[e] >= 0) {
       const int k = plan_splits(steps[e], c);
-      items += k;
-      parts += k > 1 ? k : 0;
-    }
-  int64_t item_at = plan_scan(items, red, &n_items), part_at = plan_scan(parts, red, &total);
-  at = plan_scan(tile_sum, red, &n_tiles);
-  n_items = min(n_items, (int64_t)p.z.max_rows);
-  n_tiles = min(n_tiles, (int64_t)p.z.max_tile);
-#pragma unroll
-  for (int e = 0; e < kEach; ++e) {
-    const int r = tid * each + e;
-    if (e >= each || r >= p.R) continue;
-    s_item[r] = (int)min(item_at, n_items);
-    s_part[r] = (int)part_at;
-    s_tile[r] = (int)min(at, n_tiles);
-    at += tiles[e];
-    if (steps[e] >= 0) {
-      const int k = plan_splits(steps[e], c);
-      item_at += k;
-      part_at += k > 1 ? k : 0;
+      at += k + ((int64_t)(k > 1 ? k : 0) << 32);
     }
   }
-  if (tid == 0) s_item[p.R] = (int)n_items, s_tile[p.R] = (int)n_tiles;
-  if (tid < kSizes) s_size[tid] = 0;
+  if (tid == 0) s_item[p.R] = n_items, s_tile[p.R] = (int)n_tiles;
   __syncthreads();
-  // Long stretches first: by size in kSizes classes (where one stands in its class is
-  // left to chance, and makes no difference to what is computed).
-  auto stretch = [&](int i, int* size) {
+  for (int i = tid; i < n_items; i += blockDim.x) {
     const int r = plan_find(s_item, p.R, i), x = i - s_item[r];
     AttnItem it = plan_request(p, r);
     int k = plan_splits(plan_range(p, it, 0, it.rows), c);
     if (k > 1 && s_part[r] + k > p.z.part_rows) it.s1 = it.s0, k = 1;  // (arrays that contradict themselves)
-    it = plan_stretch(it, k, k > 1 ? x : 0, s_part[r]);
-    *size = kSizes - 1 - min((int)((int64_t)(it.s1 - it.s0) * (kSizes - 1) / c), kSizes - 1);
-    return it;
-  };
-  int size;
-  for (int i = tid; i < n_items; i += blockDim.x) {
-    stretch(i, &size);
-    atomicAdd(&s_size[size], 1);
+    p.items_rows[s_place[r] + x] = plan_stretch(it, k, k > 1 ? x : 0, s_part[r]);
   }
-  __syncthreads();
-  if (tid < 64) {
-    int v = tid < kSizes ? s_size[tid] : 0, s = v;
-    for (int d = 1; d < 64; d <<= 1) {
-      const int o = __shfl_up(s, d);
-      if (tid >= d) s += o;
-    }
-    if (tid < kSizes) s_size[tid] = s - v;
-  }
-  __syncthreads();
-  for (int i = tid; i < n_items; i += blockDim.x) {
-    const AttnItem it = stretch(i, &size);
-    p.items_rows[atomicAdd(&s_size[size], 1)] = it;
-  }
-  for (int i = (int)n_items + tid; i < p.z.max_rows; i += blockDim.x) p.items_rows[i].key = 0;
+  for (int i = n_items + tid; i < p.z.max_rows; i += blockDim.x) p.items_rows[i].key = 0;
+  if (!p.z.max_tile) return;
   // tiles, the last first
   auto tile_of = [&](int t, AttnItem& it) {
     const int r = plan_find(s_tile, p.R, t);
     it = plan_request(p, r);
     it.tile = t - s_tile[r];
+    const int64_t row = (int64_t)it.tile * p.z.tile_rows;
+    if (row >= (int64_t)it.rows * p.group) it.key = 0, it.tile = 0;  // (arrays that contradict themselves)
     const int i0 = it.tile * p.z.tile_rows / p.group;
     return plan_range(p, it, i0, min(it.rows, (it.tile * p.z.tile_rows + p.z.tile_rows - 1) / p.group + 1));
   };
   sum = 0;
   AttnItem it;
-  for (int t = tid; t < n_tiles; t += blockDim.x) sum += tile_of(t, it);
+  int k = 0;
+  for (int t = tid; t < n_tiles; t += blockDim.x) sum += tile_of((int)n_tiles - 1 - t, it);
   plan_scan(sum, red, &total);
   const int ct = max(p.z.least_tile, (int)((total + p.z.goal_tile - 1) / p.z.goal_tile));
-  int64_t base_item = 0, base_part = 0;
+  int64_t base = 0;  // as counts
   for (int t0 = 0; t0 < n_tiles; t0 += blockDim.x) {
     const int t = (int)n_tiles - 1 - t0 - tid;
-    int k = 0;
-    if (t >= 0) k = plan_splits(tile_of(t, it), ct);
-    int64_t all_items, all_parts;
-    int64_t i = base_item + plan_scan(k, red, &all_items);
-    const int64_t part = base_part + plan_scan(k > 1 ? k : 0, red, &all_parts);
-    base_item += all_items, base_part += all_parts;
+    k = 0;
+    if (t >= 0) k = plan_splits(n_tiles <= blockDim.x ? it.s1 - it.s0 : tile_of(t, it), ct);
+    int64_t all;
+    const int64_t before_me = base + plan_scan(k + ((int64_t)(k > 1 ? k : 0) << 32), red, &all);
+    base += all;
+    int i = (int)(before_me & 0xFFFFFFFF);
+    const int part = (int)(before_me >> 32);
     const bool room = k <= 1 || part + k <= p.z.part_tile;
     if (!room) it.s1 = it.s0;
-    for (int x = 0; x < k && i < p.z.max_tile; ++x, ++i)
-      p.items_tile[i] = plan_stretch(it, room ? k : 1, room ? x : 0, (int)part);
+    for (int x = 0; x < k; ++x, ++i)
+      p.items_tile[i] = plan_stretch(it, room ? k : 1, room ? x : 0, part);
   }
-  for (int i = (int)min(base_item, (int64_t)p.z.max_tile) + tid; i < p.z.max_tile; i += blockDim.x) p.items_tile[i].key = 0;
+  for (int i = (int)(base & 0xFFFFFFFF) + tid; i < p.z.max_tile; i += blockDim.x) p.items_tile[i].key = 0;
 }
 
 hipError_t launch_attention_plan(const AttnPlanParams& p, hipStream_t st) {
-  const int64_t tiles = p.z.max_tile;
-  const int want = (int)std::min<int64_t>(kPlanThreads, std::max<int64_t>({p.R, p.z.max_rows, tiles}));
-  hipLaunchKernelGGL(k_attention_plan, dim3(1), dim3((want + 63) / 64 * 64), 0, st, p);
+  const int want = std::min(kPlanThreads, std::max({p.R, p.z.max_rows, p.z.max_tile, kSizes}));
+  const dim3 threads((want + 63) / 64 * 64);
+  if (p.R > kPlanThreads) hipLaunchKernelGGL(k_attention_plan<4>, dim3(1), threads, 0, st, p);
+  else hipLaunchKernelGGL(k_attention_plan<1>, dim3(1), threads, 0, st, p);
   return hipGetLastError();
 }
 #endif

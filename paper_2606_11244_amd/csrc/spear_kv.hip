@@ -7,31 +7,33 @@ namespace spear {
 
 #if !SPEAR_BF16_UNIT
 // ---------------------------------------------------------------------------
-// Block tables, slots and positions. One workgroup: two sums over the requests
-// (rows, then new pages of those that can be served), kept in LDS, and then the
-// new pages and the rows in flat order, each finding its request by bisection.
-// Everything is latency: a few dependent loads and four barriers a sum.
+// Block tables, slots and positions. Two sums over the requests (rows, then new
+// pages of those that can be served), kept in LDS, and then the new pages and the
+// rows in flat order, each finding its request by bisection. Everything is latency:
+// a few dependent loads and two barriers a sum.
 // ---------------------------------------------------------------------------
-constexpr int kPagesThreads = 1024, kPagesEach = kKvRequests / kPagesThreads;
+constexpr int kPagesThreads = 1024;
 
-// exclusive sum over the workgroup, and its total
-__device__ __forceinline__ int64_t scan_block(int64_t v, int64_t* red, int64_t* total) {
+// sum over the workgroup before this thread, and in all, held at 2^32 - 1
+__device__ __forceinline__ uint32_t scan_block(uint32_t v, uint32_t* red, uint32_t* total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-  int64_t s = v;
+  uint32_t s = v;
+#pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
-    const int64_t o = __shfl_up(s, d);
-    if (lane >= d) s += o;
+    const uint32_t o = __shfl_up(s, d);
+    if (lane >= d) s = __builtin_elementwise_add_sat(s, o);
   }
-  __syncthreads();
+  const uint32_t up = __shfl_up(s, 1);
   if (lane == 63) red[wave] = s;
   __syncthreads();
-  int64_t before = 0, all = 0;
+  uint32_t before = 0, all = 0;
   for (int i = 0; i < waves; ++i) {
-    if (i < wave) before += red[i];
-    all += red[i];
+    if (i < wave) before = __builtin_elementwise_add_sat(before, red[i]);
+    all = __builtin_elementwise_add_sat(all, red[i]);
   }
+  __syncthreads();
   *total = all;
-  return before + s - v;
+  return lane ? __builtin_elementwise_add_sat(before, up) : before;
 }
 
 // the last i of 0..n-1 with a[i] <= x (a ascending, a[0] <= x)
@@ -45,74 +47,73 @@ __device__ __forceinline__ int last_not_above(const int32_t* a, int n, int x) {
   return lo;
 }
 
+// EACH: requests a thread. Every workgroup makes the sums; the first writes what is
+// one a request, and all share the new pages and the rows.
+template <int EACH>
 __global__ __launch_bounds__(kPagesThreads) void k_kv_pages(KvPagesParams p) {
-  __shared__ int32_t s_start[kKvRequests + 1], s_held[kKvRequests], s_page[kKvRequests];
-  __shared__ int64_t red[kPagesThreads / 64];
+  __shared__ int32_t s_start[EACH * kPagesThreads + 1], s_held[EACH * kPagesThreads], s_page[EACH * kPagesThreads];
+  __shared__ uint32_t red[kPagesThreads / 64];
   __shared__ int s_taken, s_unserved;
-  const int tid = threadIdx.x, each = (p.R + blockDim.x - 1) / blockDim.x;
+  const int tid = threadIdx.x, r0 = tid * EACH, rows_all = p.T;
+  const bool first = blockIdx.x == 0;
   if (tid == 0) s_taken = 0, s_unserved = 0;
-  int held[kPagesEach], rows[kPagesEach], need[kPagesEach];
-  bool ok[kPagesEach];
-  int64_t sum = 0;
+  int held[EACH], fresh[EACH], need[EACH];
+  bool ok[EACH];
+  uint32_t sum = 0, total;
 #pragma unroll
-  for (int e = 0; e < kPagesEach; ++e) {
-    const int r = tid * each + e;
-    held[e] = rows[e] = need[e] = 0;
-    ok[e] = false;
-    if (e >= each || r >= p.R) continue;
-    const int h = p.held[r], f = p.fresh[r];
-    ok[e] = h >= 0 && f >= 0 && (int64_t)h + f < kKvLength;
-    held[e] = h;
-    rows[e] = f > 0 ? min(f, p.T + 1) : 0;
-    sum += rows[e];
+  for (int e = 0; e < EACH; ++e) {
+    const bool there = r0 + e < p.R;
+    held[e] = there ? p.held[r0 + e] : 0;
+    fresh[e] = there ? p.fresh[r0 + e] : 0;
+    ok[e] = there && held[e] >= 0 && fresh[e] >= 0 && (int64_t)held[e] + fresh[e] < kKvLength;
+    sum = __builtin_elementwise_add_sat(sum, (uint32_t)max(fresh[e], 0));
   }
-  int64_t total;
-  int64_t at = scan_block(sum, red, &total);
-  if (tid == 0) s_start[p.R] = p.starts[p.R] = (int)(total < p.T ? total : p.T);
-  int64_t pages = 0;
+  uint32_t at = scan_block(sum, red, &total);
+  if (tid == 0) s_start[p.R] = (int)min(total, (uint32_t)rows_all);
+  uint32_t pages = 0;
 #pragma unroll
-  for (int e = 0; e < kPagesEach; ++e) {
-    const int r = tid * each + e;
-    if (e >= each || r >= p.R) continue;
-    s_start[r] = p.starts[r] = (int)(at < p.T ? at : p.T);
-    at += rows[e];
-    const int len = ok[e] ? held[e] + p.fresh[r] : 0;
-    const int has = (len + p.P - 1) / p.P;
-    ok[e] = ok[e] && at <= p.T && has <= p.width;
+  for (int e = 0; e < EACH; ++e) {
+    if (r0 + e < p.R) s_start[r0 + e] = (int)min(at, (uint32_t)rows_all);
+    at = __builtin_elementwise_add_sat(at, (uint32_t)max(fresh[e], 0));
+    const int has = ok[e] ? (held[e] + fresh[e] + p.P - 1) / p.P : 0;
+    ok[e] = ok[e] && at <= (uint32_t)rows_all && has <= p.width;
     need[e] = ok[e] ? has - (held[e] + p.P - 1) / p.P : 0;
     pages += need[e];
   }
   at = scan_block(pages, red, &total);
   int unserved = 0, taken = 0;
 #pragma unroll
-  for (int e = 0; e < kPagesEach; ++e) {
-    const int r = tid * each + e;
-    if (e >= each || r >= p.R) continue;
-    s_page[r] = (int)(at < p.n_free ? at : p.n_free);
-    at += need[e];
-    ok[e] = ok[e] && (need[e] == 0 || at <= p.n_free);
+  for (int e = 0; e < EACH; ++e) {
+    if (r0 + e >= p.R) continue;
+    s_page[r0 + e] = (int)min(at, (uint32_t)p.n_free);
+    at = __builtin_elementwise_add_sat(at, (uint32_t)need[e]);
+    ok[e] = ok[e] && (need[e] == 0 || at <= (uint32_t)p.n_free);
     if (ok[e] && need[e]) taken = (int)at;
     unserved += !ok[e];
-    s_held[r] = ok[e] ? held[e] : -1;
-    p.lens[r] = ok[e] ? held[e] + p.fresh[r] : 0;
+    s_held[r0 + e] = ok[e] ? held[e] : -1;
+    if (first) {
+      p.starts[r0 + e] = s_start[r0 + e];
+      p.lens[r0 + e] = ok[e] ? held[e] + fresh[e] : 0;
+    }
   }
   if (taken) atomicMax(&s_taken, taken);
   if (unserved) atomicAdd(&s_unserved, unserved);
   __syncthreads();
-  if (tid == 0) p.taken[0] = s_taken, p.taken[1] = s_unserved;
+  if (first && tid == 0) p.starts[p.R] = s_start[p.R], p.taken[0] = s_taken, p.taken[1] = s_unserved;
+  const int step = gridDim.x * blockDim.x, me = blockIdx.x * blockDim.x + tid;
   // the k-th page taken goes to the last request whose pages begin at or before it
-  for (int k = tid; k < s_taken; k += blockDim.x) {
+  for (int k = me; k < s_taken; k += step) {
     const int r = last_not_above(s_page, p.R, k);
     const int j = (s_held[r] + p.P - 1) / p.P + k - s_page[r];
     p.table[r * p.ld + j] = p.free_pages[k];
   }
-  for (int t = tid; t < p.T; t += blockDim.x) {
+  for (int t = me; t < p.T; t += step) {
     int slot = -1, pos = 0;
     if (p.R && t < s_start[p.R]) {
-      const int r = last_not_above(s_start, p.R, t);
-      if (s_held[r] >= 0) {
-        pos = s_held[r] + t - s_start[r];
-        const int had = (s_held[r] + p.P - 1) / p.P, j = pos / p.P;
+      const int r = last_not_above(s_start, p.R, t), h = s_held[r];
+      if (h >= 0) {
+        pos = h + t - s_start[r];
+        const int had = (h + p.P - 1) / p.P, j = pos / p.P;
         // (a new page's entry comes from the list: the table's is being written)
         const int page = j < had ? p.table[r * p.ld + j] : p.free_pages[s_page[r] + j - had];
         const int64_t s = (int64_t)page * p.P + pos % p.P;
@@ -125,8 +126,12 @@ __global__ __launch_bounds__(kPagesThreads) void k_kv_pages(KvPagesParams p) {
 }
 
 hipError_t launch_kv_pages(const KvPagesParams& p, hipStream_t st) {
-  const int threads = std::min(kPagesThreads, std::max(64, (std::max(p.R, p.T) + 63) / 64 * 64));
-  hipLaunchKernelGGL(k_kv_pages, dim3(1), dim3(threads), 0, st, p);
+  const bool many = p.R > kPagesThreads;
+  const int threads = many ? kPagesThreads : std::min(kPagesThreads, std::max(64, (std::max(p.R, p.T) + 63) / 64 * 64));
+  // a row a thread: 5276 rows of 384 requests took 12.5 us in one workgroup
+  const int grid = std::max(1, std::min(64, (p.T + threads - 1) / threads));
+  if (many) hipLaunchKernelGGL(k_kv_pages<4>, dim3(grid), dim3(threads), 0, st, p);
+  else hipLaunchKernelGGL(k_kv_pages<1>, dim3(grid), dim3(threads), 0, st, p);
   return hipGetLastError();
 }
 #endif
@@ -530,51 +535,63 @@ hipError_t SPEAR_D(launch_kv_append)(const KvAppendParams& p, int format, hipStr
 // Values back: sixteen tokens of one head a workgroup; V, whose places of one
 // feature lie side by side, changes its order through LDS.
 // ---------------------------------------------------------------------------
-template <int DT, int FMT>
+template <int DT, int FMT, int D>
 __global__ __launch_bounds__(256) void k_kv_read(KvReadParams p) {
-  __shared__ uint16_t turned[16][128 + 2];
-  const int tid = threadIdx.x, D = p.c.D, P = p.c.P, h = blockIdx.x % p.c.Hkv;
-  const int64_t i0 = (int64_t)(blockIdx.x / p.c.Hkv) * 16, capacity = (int64_t)p.c.pages * P;
+  __shared__ uint16_t turned[16][D + 2];
+  const int tid = threadIdx.x, P = p.c.P, h = blockIdx.x % p.c.Hkv, capacity = p.c.pages << p.log2_page;
+  const int64_t i0 = (int64_t)(blockIdx.x / p.c.Hkv) * 16;
   auto slot_of = [&](int m) {
     const int s = i0 + m < p.n ? p.slots[i0 + m] : -1;
     return s < capacity ? s : -1;
   };
-  for (int i = tid; i < 16 * (D / 4); i += 256) {
-    const int m = i / (D / 4), d = 4 * (i % (D / 4)), s = slot_of(m);
-    if (s < 0) continue;
-    const int64_t ph = (int64_t)(s / P) * p.c.Hkv + h;
-    float c[4];
-    decode4<FMT>(*(const uint32_t*)(p.c.k + (ph * P + s % P) * D + d), c);
-    const float scale = p.c.k_scale[ph];
-    uint16_t* o = p.k_out + ((i0 + m) * p.c.Hkv + h) * D + d;
-    *(u32x2*)o = u32x2{(uint32_t)f2act<DT>(c[0] * scale) | ((uint32_t)f2act<DT>(c[1] * scale) << 16),
-                       (uint32_t)f2act<DT>(c[2] * scale) | ((uint32_t)f2act<DT>(c[3] * scale) << 16)};
+  // all loads before the first value: K's dwords of four features, V's bytes
+  constexpr int U = D / 64, V = D / 16;
+  uint32_t k[U], v[V];
+  float k_scale[U];
+  int k_slot[U];
+#pragma unroll
+  for (int x = 0; x < U; ++x) {
+    const int i = tid + 256 * x, m = i / (D / 4), d = 4 * (i % (D / 4)), s = k_slot[x] = slot_of(m), at = max(s, 0);
+    const int64_t ph = (int64_t)(at >> p.log2_page) * p.c.Hkv + h;
+    k[x] = *(const uint32_t*)(p.c.k + (ph * P + (at & (P - 1))) * D + d);
+    k_scale[x] = p.c.k_scale[ph];
   }
-  {
-    const int m = tid & 15, s = slot_of(m);
-    if (s >= 0) {
-      const int64_t ph = (int64_t)(s / P) * p.c.Hkv + h;
-      const float scale = p.c.v_scale[ph];
-      for (int d = tid >> 4; d < D; d += 16) {
-        float c[4];
-        decode4<FMT>(p.c.v[(ph * D + d) * P + s % P], c);
-        turned[m][d] = f2act<DT>(c[0] * scale);
-      }
-    }
+  const int m = tid & 15, d0 = tid >> 4, s = slot_of(m), at = max(s, 0);
+  const int64_t ph = (int64_t)(at >> p.log2_page) * p.c.Hkv + h;
+#pragma unroll
+  for (int x = 0; x < V; ++x) v[x] = p.c.v[(ph * D + d0 + 16 * x) * P + (at & (P - 1))];
+  const float v_scale = p.c.v_scale[ph];
+#pragma unroll
+  for (int x = 0; x < U; ++x) {
+    const int i = tid + 256 * x;
+    float c[4];
+    decode4<FMT>(k[x], c);
+    uint16_t* o = p.k_out + ((i0 + i / (D / 4)) * p.c.Hkv + h) * D + 4 * (i % (D / 4));
+    if (k_slot[x] >= 0) *(u32x2*)o = u32x2{pack2<DT>(c[0] * k_scale[x], c[1] * k_scale[x]), pack2<DT>(c[2] * k_scale[x], c[3] * k_scale[x])};
+  }
+#pragma unroll
+  for (int x = 0; x < V; ++x) {
+    float c[4];
+    decode4<FMT>(v[x], c);
+    turned[m][d0 + 16 * x] = f2act<DT>(c[0] * v_scale);
   }
   __syncthreads();
-  for (int i = tid; i < 16 * (D / 2); i += 256) {
-    const int m = i / (D / 2), d = 2 * (i % (D / 2));
-    if (slot_of(m) < 0) continue;
-    *(uint32_t*)(p.v_out + ((i0 + m) * p.c.Hkv + h) * D + d) = *(const uint32_t*)&turned[m][d];
+#pragma unroll
+  for (int x = 0; x < U; ++x) {
+    const int i = tid + 256 * x, m = i / (D / 4), d = 4 * (i % (D / 4));
+    const uint32_t* t = (const uint32_t*)&turned[m][d];
+    if (k_slot[x] >= 0) *(u32x2*)(p.v_out + ((i0 + m) * p.c.Hkv + h) * D + d) = u32x2{t[0], t[1]};
   }
 }
 
-hipError_t SPEAR_D(launch_kv_read)(const KvReadParams& p, int format, hipStream_t st) {
-  const dim3 grid((uint32_t)((p.n + 15) / 16 * p.c.Hkv));
-  if (format == KV_INT8) hipLaunchKernelGGL((k_kv_read<DTC, KV_INT8>), grid, dim3(256), 0, st, p);
-  else hipLaunchKernelGGL((k_kv_read<DTC, KV_E4M3>), grid, dim3(256), 0, st, p);
+template <int FMT, int D>
+static hipError_t read_launch(const KvReadParams& p, hipStream_t st) {
+  hipLaunchKernelGGL((k_kv_read<DTC, FMT, D>), dim3((uint32_t)((p.n + 15) / 16 * p.c.Hkv)), dim3(256), 0, st, p);
   return hipGetLastError();
+}
+hipError_t SPEAR_D(launch_kv_read)(const KvReadParams& p, int format, hipStream_t st) {
+  if (p.c.D == 64) return format == KV_INT8 ? read_launch<KV_INT8, 64>(p, st) : read_launch<KV_E4M3, 64>(p, st);
+  return format == KV_INT8 ? read_launch<KV_INT8, 128>(p, st) : read_launch<KV_E4M3, 128>(p, st);
 }
 
 }  // namespace spear

@@ -216,7 +216,7 @@ spear_status_t spear_kv_read(const spear_kv_cache_t* c, int64_t n, const int32_t
   ins[4] = {slots, (size_t)n * 4};
   if (clash(outs, 2, ins, 5)) return SPEAR_E_ALIAS;
   if (c->pages == 0) return SPEAR_OK;
-  const KvReadParams p{cache_of(c), n, slots, (uint16_t*)k_out, (uint16_t*)v_out};
+  const KvReadParams p{cache_of(c), __builtin_ctz((unsigned)c->page_tokens), n, slots, (uint16_t*)k_out, (uint16_t*)v_out};
   const auto launch = c->act_dtype == SPEAR_F16 ? launch_kv_read_f16 : launch_kv_read_bf16;
   return hip_status(launch(p, c->format, (hipStream_t)hip_stream));
 }
@@ -274,7 +274,7 @@ AttnLayout attention_layout(const spear_attention_t* a) {
   AttnShape& z = l.z;
   z.goal_rows = (int)((kRowsGoal + hkv - 1) / hkv);
   // sum over tiles of max(1, ceil(steps / c)) with c >= all steps / goal
-  z.max_rows = rows ? (int)served + z.goal_rows : 0;
+  z.max_rows = rows ? (int)R + z.goal_rows : 0;
   z.least_rows = kRowsLeast;
   const int big = tile_rows(c->head_dim);
   z.tile_rows = (T * group + big - 1) / big * hkv < kFillRows / big ? kMidRows : big;

@@ -47,6 +47,7 @@ struct KvAppendParams {
 
 struct KvReadParams {
   KvCache c;
+  int log2_page;
   int64_t n;
   const int32_t* slots;
   uint16_t *k_out, *v_out;

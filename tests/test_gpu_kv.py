@@ -372,6 +372,22 @@ def test_attention_of_more_rows_than_said():
     Setup([(300, 400), (1, 33)], 8, 2, 64, 16, torch.bfloat16, torch.int8, max_new=40).check()
 
 
+def test_attention_of_starts_that_contradict_themselves():
+    """Rows that no order makes sense of: nothing outside the step is touched, and what comes after is right."""
+    act, codes = torch.bfloat16, torch.int8
+    s = Setup([(3, 900), (40, 1200), (1, 2500), (2, 33)], 8, 1, 64, 16, act, codes, pad=4)
+    want = s.run().clone()
+    bad = [[46, 0, 46, 0, 46], [-5, 2 ** 31 - 1, 3, -2 ** 31, 50], [46, 46, 46, 46, 46], [0, 46, 46, 0, 46]]
+    for starts in bad:
+        s.batch.starts.copy_(_ints(starts))
+        s.batch.lens.copy_(_ints([2 ** 31 - 1, 1200, -7, 2 ** 30]))
+        s.run()
+        s.batch.starts.copy_(_ints(s.starts))
+        s.batch.lens.copy_(_ints(s.lens))
+        s.out.fill_(9.0)
+        assert torch.equal(s.run(), want)
+
+
 def test_attention_strides():
     for lengths in ([(1, 300), (1, 20)], [(70, 300), (1, 20)]):
         s = Setup(lengths, 4, 2, 128, 32, torch.float16, torch.int8)
