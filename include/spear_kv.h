@@ -123,10 +123,11 @@ spear_status_t spear_rope_frequencies(int32_t rotary_dim, double base, double fa
                                       double low_turns, double high_turns, uint64_t* freqs);
 
 /* New tokens into the cache, one launch: k is turned and written, v written, each
- * token at its slot, and q (unless NULL) turned into q_out. Rotations are made in
- * fp32, and rounded once. The scale of a page and head is the least power of two
- * whose multiple by 127 (INT8) or 448 (E4M3) reaches every magnitude it has been
- * given since its first place was written; it never shrinks before, and where it
+ * token at its slot, and q (unless NULL) turned into q_out. q is turned in fp32 and
+ * rounded once; a code of k is the nearest to the rotation in 64 bits. The scale of a
+ * page and head is the least power of two whose multiple by 127 (INT8) or 448 (E4M3)
+ * reaches every magnitude (in fp32) it has been given since its first place was
+ * written; it never shrinks before, and where it
  * grows the codes already there are divided to match (rounded to nearest even:
  * E4M3 codes keep their value down to the format's least steps, INT8 codes are off
  * by less than one step in all). Codes are rounded to nearest even and no code

@@ -212,6 +212,27 @@ __device__ __forceinline__ float2 cos_sin(uint64_t turn, float magnitude) {
                      quarter >= 2 ? -b * magnitude : b * magnitude);
 }
 
+// The same in 64 bits (to 5e-17), for keys whose code fp32 leaves open.
+struct CosSin64 {
+  double x, y;
+};
+__device__ __forceinline__ CosSin64 cos_sin64(uint64_t turn, double magnitude) {
+  const uint64_t quarter = (turn + 0x2000000000000000ull) >> 62;
+  const double x = (double)(int64_t)(turn - (quarter << 62)) * 3.4061215800865545e-19;  // 2 pi / 2^64
+  const double y = x * x;
+  double s = 1. / 1307674368000, c = 1. / 20922789888000;  // 15!, 16!
+  const double fs[] = {1. / 6227020800, 1. / 39916800, 1. / 362880, 1. / 5040, 1. / 120, 1. / 6, 1.};
+  const double fc[] = {1. / 87178291200, 1. / 479001600, 1. / 3628800, 1. / 40320, 1. / 720, 1. / 24, 1. / 2, 1.};
+  s = -s;
+#pragma unroll
+  for (int i = 0; i < 7; ++i) s = __builtin_fma(s, y, (i & 1) ? -fs[i] : fs[i]);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) c = __builtin_fma(c, y, (i & 1) ? fc[i] : -fc[i]);
+  s *= x;
+  const double a = quarter & 1 ? s : c, b = quarter & 1 ? c : s;
+  return {(quarter == 1 || quarter == 2) ? -a * magnitude : a * magnitude, quarter >= 2 ? -b * magnitude : b * magnitude};
+}
+
 // The features of a head as units of two runs of W features, at p0 and p1, that
 // rotate together: W = 8 where pairs of features lie rot/2 apart or side by side
 // and rot is a multiple of 16, else W = 1, the two features of a pair.
@@ -236,14 +257,14 @@ __device__ __forceinline__ void load_run(const uint16_t* p, float (&x)[W]) {
   }
 }
 // turns both runs; cs(pair) is the cosine and sine of a pair
-template <int W, class CS>
-__device__ __forceinline__ void turn(const Unit& u, int interleaved, float (&a)[W], float (&b)[W], CS cs) {
+template <int W, class T, class CS>
+__device__ __forceinline__ void turn(const Unit& u, int interleaved, T (&a)[W], T (&b)[W], CS cs) {
   if (u.pair < 0) return;
   if (W == 8 && interleaved) {
 #pragma unroll
     for (int i = 0; i < W; i += 2) {
-      const float2 s = cs(u.pair + i / 2), t = cs(u.pair + W / 2 + i / 2);
-      const float x = a[i], y = b[i];
+      const auto s = cs(u.pair + i / 2), t = cs(u.pair + W / 2 + i / 2);
+      const T x = a[i], y = b[i];
       a[i] = x * s.x - a[i + 1] * s.y;
       a[i + 1] = a[i + 1] * s.x + x * s.y;
       b[i] = y * t.x - b[i + 1] * t.y;
@@ -252,8 +273,8 @@ __device__ __forceinline__ void turn(const Unit& u, int interleaved, float (&a)[
   } else {
 #pragma unroll
     for (int i = 0; i < W; ++i) {
-      const float2 s = cs(u.pair + i);
-      const float x = a[i];
+      const auto s = cs(u.pair + i);
+      const T x = a[i];
       a[i] = x * s.x - b[i] * s.y;
       b[i] = b[i] * s.x + x * s.y;
     }
@@ -307,65 +328,124 @@ __device__ __forceinline__ void append_k(const KvAppendParams& p, int t, int slo
   const int64_t ph = (int64_t)page * p.c.Hkv + h;
   const float before = off ? p.c.k_scale[ph] : 0.f;
   uint8_t* codes = p.c.k + ph * P * D;
-  auto unit = [&](int i, float (&a)[W], float (&b)[W]) {
-    const int m = i / units;
+  typedef typename std::conditional<W == 8, u32x4, uint16_t>::type Raw;
+  struct Pair {
+    Raw a, b;
+  };
+  auto load = [&](int i) {
     const Unit u = unit_at<W>(i % units, p.r.rot, p.r.interleaved);
-    const uint16_t* k = p.k + (int64_t)(t + m) * p.k_ld + h * D;
-    load_run<DT, W>(k + u.p0, a);
-    load_run<DT, W>(k + u.p1, b);
-    const uint64_t pos = p.r.rot ? (uint64_t)(int64_t)p.positions[t + m] : 0;
+    const uint16_t* k = p.k + (int64_t)(t + i / units) * p.k_ld + h * D;
+    return Pair{*(const Raw*)(k + u.p0), *(const Raw*)(k + u.p1)};
+  };
+  auto position = [&](int i) { return p.r.rot ? (uint64_t)(int64_t)p.positions[t + i / units] : 0; };
+  auto widen = [&](const Raw& r, auto (&x)[W]) {
+    if constexpr (W == 8) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = act2f<DT>((r[e >> 1] >> (16 * (e & 1))) & 0xFFFFu);
+    } else {
+      x[0] = act2f<DT>(r);
+    }
+  };
+  // the largest magnitude of a unit, turned in fp32
+  auto largest = [&](int i, const Pair& r) {
+    const Unit u = unit_at<W>(i % units, p.r.rot, p.r.interleaved);
+    const uint64_t pos = position(i);
+    float a[W], b[W], top = 0.f;
+    widen(r.a, a), widen(r.b, b);
     turn<W>(u, p.r.interleaved, a, b, [&](int x) { return cos_sin(pos * p.r.freqs[x], p.r.magnitude); });
+#pragma unroll
+    for (int e = 0; e < W; ++e) top = fmaxf(top, fmaxf(finite_size(a[e]), finite_size(b[e])));
+    return top;
   };
-  auto older = [&](float ratio) {
-    for (int i = tid; i < off * D / 4; i += 256) ((uint32_t*)codes)[i] = divide4<FMT>(((uint32_t*)codes)[i], ratio);
-  };
-  float top = 0.f;
-  if constexpr (W == 8) {
-    constexpr int U = 4;  // units a thread at most: pages of 128 tokens, 128 features
-    float a[U][8], b[U][8];
+  // its codes, each the nearest to the rotation in 64 bits: from fp32, and the pairs one of
+  // whose values then lies nearer to the border of two codes than fp32 is off once more in
+  // 64 bits, one by one. 4096 tokens of 8 heads and 64 heads of queries: 45 us all in fp32
+  // (one code in 10^5 the neighbour of the right one), 63 all in 64 bits, 48 this way.
+  auto put = [&](int i, const Pair& r, const PageScale& s) {
+    const Unit u = unit_at<W>(i % units, p.r.rot, p.r.interleaved);
+    const uint64_t pos = position(i);
+    float a[W], b[W], reach[W];
+    widen(r.a, a), widen(r.b, b);
+    const bool side_by_side = W == 8 && p.r.interleaved;
+    // an fp32 rotation is off by at most 2^-21 of what it is made of
+    const float part = u.pair < 0 ? 0.f : fabsf(p.r.magnitude * s.inv) * 4.76837158e-7f;
 #pragma unroll
-    for (int x = 0; x < U; ++x) {
-      if (tid + 256 * x >= n * units) continue;
-      unit(tid + 256 * x, a[x], b[x]);
+    for (int e = 0; e < W; ++e)
+      reach[e] = part * (!side_by_side ? fabsf(a[e]) + fabsf(b[e])
+                         : e < W / 2   ? fabsf(a[(2 * e) % W]) + fabsf(a[(2 * e + 1) % W])
+                                       : fabsf(b[(2 * e) % W]) + fabsf(b[(2 * e + 1) % W]));
+    turn<W>(u, p.r.interleaved, a, b, [&](int x) { return cos_sin(pos * p.r.freqs[x], p.r.magnitude); });
 #pragma unroll
-      for (int e = 0; e < 8; ++e) top = fmaxf(top, fmaxf(finite_size(a[x][e]), finite_size(b[x][e])));
-    }
-    const PageScale s = settle<DT, FMT>(top, before, red);
-    if (tid == 0 && s.grew) p.c.k_scale[ph] = s.scale;
-    if (s.grew) older(s.ratio);
-    auto put = [&](uint8_t* to, const float (&v)[8]) {
-      float c[2][4];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) c[e >> 2][e & 3] = to_code(v[e], s.inv, s.most);
-      *(u32x2*)to = u32x2{encode4<FMT>(c[0]), encode4<FMT>(c[1])};
+    for (int e = 0; e < W; ++e) a[e] = to_code(a[e], s.inv, s.most), b[e] = to_code(b[e], s.inv, s.most);
+    uint8_t* row = codes + (off + i / units) * D;
+    uint32_t near = 0;  // pairs
+    auto check = [&](float c, float code, int pair) {
+      // (half the distance of two codes at c)
+      const float half = FMT == KV_INT8 ? 0.5f : __uint_as_float((max((__float_as_uint(c) >> 23) & 255u, 121u) - 4) << 23);
+      near |= fabsf(fabsf(c - code) - half) <= reach[pair] ? 1u << pair : 0u;
     };
+    auto eight = [&](const float (&c)[W], int run) {
+      u32x2 w;
 #pragma unroll
-    for (int x = 0; x < U; ++x) {
-      const int i = tid + 256 * x;
-      if (i >= n * units) continue;
-      const Unit u = unit_at<W>(i % units, p.r.rot, p.r.interleaved);
-      uint8_t* row = codes + (off + i / units) * D;
-      put(row + u.p0, a[x]);
-      put(row + u.p1, b[x]);
+      for (int q = 0; q < 2; ++q) {
+        const float x[4] = {c[4 * q % W], c[(4 * q + 1) % W], c[(4 * q + 2) % W], c[(4 * q + 3) % W]};
+        float y[4];
+        w[q] = encode4<FMT>(x);
+        decode4<FMT>(w[q], y);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (4 * q + e < W) check(x[e], y[e], side_by_side ? (W * run + 4 * q + e) / 2 : (4 * q + e) % W);
+      }
+      return w;
+    };
+    const u32x2 wa = eight(a, 0), wb = eight(b, 1);
+    if constexpr (W == 8) {
+      *(u32x2*)(row + u.p0) = wa;
+      *(u32x2*)(row + u.p1) = wb;
+    } else {  // (a rotation of no multiple of 16 features: a byte a store)
+      row[u.p0] = (uint8_t)wa[0];
+      row[u.p1] = (uint8_t)wb[0];
     }
-  } else {  // (a rotation of no multiple of 16 features: turned twice, a byte a store)
-    float a[1], b[1];
-    for (int i = tid; i < n * units; i += 256) {
-      unit(i, a, b);
-      top = fmaxf(top, fmaxf(finite_size(a[0]), finite_size(b[0])));
-    }
-    const PageScale s = settle<DT, FMT>(top, before, red);
-    if (tid == 0 && s.grew) p.c.k_scale[ph] = s.scale;
-    if (s.grew) older(s.ratio);
-    for (int i = tid; i < n * units; i += 256) {
-      unit(i, a, b);
-      const float c[4] = {to_code(a[0], s.inv, s.most), to_code(b[0], s.inv, s.most), 0.f, 0.f};
+    if (u.pair < 0) near = 0;
+    const uint16_t* k = p.k + (int64_t)(t + i / units) * p.k_ld + h * D;
+    for (; near; near &= near - 1) {
+      const int e = __builtin_ctz(near);
+      const int fa = side_by_side ? u.p0 + 2 * e : u.p0 + e, fb = side_by_side ? fa + 1 : u.p1 + e;
+      const CosSin64 cs = cos_sin64(pos * p.r.freqs[u.pair + e], p.r.magnitude);
+      const double x = act2f<DT>(k[fa]), y = act2f<DT>(k[fb]);
+      auto code = [&](double v) {
+        const double c = v == v ? v * (double)s.inv : 0.;
+        const double d = fmin(fmax(c, -(double)s.most), (double)s.most);
+        float f = (float)(FMT == KV_INT8 ? rint(d) : d);
+        if (FMT == KV_E4M3) {  // to fp32 with an odd last bit if inexact: the rounding to a code sees the side of a border
+          f = __uint_as_float(__float_as_uint(f) - (fabs((double)f) > fabs(d)));
+          f = __uint_as_float(__float_as_uint(f) | ((double)f != d));
+        }
+        return f;
+      };
+      const float c[4] = {code(x * cs.x - y * cs.y), code(y * cs.x + x * cs.y), 0.f, 0.f};
       const uint32_t w = encode4<FMT>(c);
-      const Unit u = unit_at<W>(i % units, p.r.rot, p.r.interleaved);
-      uint8_t* row = codes + (off + i / units) * D;
-      row[u.p0] = (uint8_t)w;
-      row[u.p1] = (uint8_t)(w >> 8);
+      row[fa] = (uint8_t)w;
+      row[fb] = (uint8_t)(w >> 8);
     }
+  };
+  // a thread's first unit is held between the two, others are read again
+  const int all = n * units;
+  Pair own = {};
+  float top = 0.f;
+  if (tid < all) own = load(tid);
+  if (tid < all) top = largest(tid, own);
+#pragma unroll 1
+  for (int i = tid + 256; i < all; i += 256) top = fmaxf(top, largest(i, load(i)));
+  const PageScale s = settle<DT, FMT>(top, before, red);
+  if (s.grew) {
+    if (tid == 0) p.c.k_scale[ph] = s.scale;
+    for (int i = tid; i < off * D / 4; i += 256) ((uint32_t*)codes)[i] = divide4<FMT>(((uint32_t*)codes)[i], s.ratio);
+  }
+#pragma unroll 1
+  for (int i = tid; i < all; i += 256) {
+    put(i, own, s);
+    if (i + 256 < all) own = load(i + 256);
   }
 }
 
@@ -429,8 +509,10 @@ __device__ __forceinline__ void append_v(const KvAppendParams& p, int t, int slo
   }
 }
 
+// (four workgroups a CU: at the 137 registers that INT8 took without it, three fit, and
+// the queries of a prompt came at 3560 GB/s, 3800 with it)
 template <int DT, int FMT, int D, int W>
-__global__ __launch_bounds__(256) void k_kv_append(KvAppendParams p) {
+__global__ __launch_bounds__(256, 4) void k_kv_append(KvAppendParams p) {
   __shared__ float2 cs[64];
   __shared__ float red[4];
   const int tid = threadIdx.x, P = p.c.P, capacity = p.c.pages << p.log2_page;

@@ -194,6 +194,29 @@ def test_append_of_many_tokens(act, codes):
 
 @pytest.mark.parametrize("act", ACTS)
 @pytest.mark.parametrize("codes", CODES)
+@pytest.mark.parametrize("rot,interleaved", [(64, False), (32, True), (50, True)])
+def test_keys_have_the_nearest_codes(act, codes, rot, interleaved):
+    """One rounding: a code is the nearest to the rotation in 64 bits, whose own error (that of an angle held
+    as a 64-bit fraction, Taylor's sums and a dozen roundings, less than 2^-45 of a code) is all that is allowed."""
+    kv = _kv()
+    g = torch.Generator(device="cuda").manual_seed(rot)
+    P, D, T = 64, 64, 4096
+    cache = kv.new_cache(T // P, 2, P, D, act, codes)
+    rope = _rope(kv, rot, interleaved)
+    k = torch.randn(T, 2, D, device="cuda", generator=g).to(act)
+    pos = torch.randint(0, 2 ** 30, (T,), device="cuda", generator=g, dtype=torch.int32)
+    kv.append(cache, k, k.clone(), _ints(range(T)), pos, rope=rope)
+    x = U.turned(k.cpu(), pos.tolist(), [f % 2 ** 64 for f in rope.freqs.tolist()], rot, interleaved, 1.0)
+    (have, scale), _ = _content(cache)
+    have = have.transpose(1, 2).reshape(T, 2, D)
+    c = x / scale.repeat_interleave(P, 0)[:, :, None]
+    c = c.clamp(-U.TOP[codes], U.TOP[codes])
+    step = U.step_of(c, codes)
+    assert bool(((have - c).abs() <= 0.5 * step + 2.0 ** -45 * c.abs()).all())
+
+
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("codes", CODES)
 def test_append_at_the_ends_of_the_range(act, codes):
     kv = _kv()
     P, D, inf, nan = 16, 64, float("inf"), float("nan")
