@@ -155,15 +155,16 @@ typedef struct {
 } spear_kv_append_t;
 
 /* SPEAR_E_NULL for a missing pointer; SPEAR_E_DTYPE for an unknown format or act
- * dtype; SPEAR_E_SHAPE for sizes or strides outside the above; SPEAR_E_ALIGN;
- * SPEAR_E_ALIAS where q_out overlaps an input (unless it is q with the same row
+ * dtype; SPEAR_E_SHAPE for sizes or strides outside the above, or more heads and
+ * tokens than one launch takes (2^24 workgroups: one a token with q, and kv_heads / 8
+ * a token); SPEAR_E_ALIGN; SPEAR_E_ALIAS where q_out overlaps an input (unless it is q with the same row
  * stride) or a buffer of the cache overlaps any other. */
 spear_status_t spear_kv_append(const spear_kv_cache_t* cache, const spear_kv_append_t* args,
                                void* hip_stream);
 
 /* What cached tokens stand for: k_out[i], v_out[i] [kv_heads][head_dim] in the act
  * dtype of the token at slots[i], rows of slots outside the cache left as they
- * were. n in 0..2^31-1. Errors as for spear_kv_append. */
+ * were. n in 0..2^31-1, n * kv_heads below 2^28. Errors as for spear_kv_append. */
 spear_status_t spear_kv_read(const spear_kv_cache_t* cache, int64_t n, const int32_t* slots, void* k_out,
                              void* v_out, void* hip_stream);
 
@@ -178,14 +179,14 @@ spear_status_t spear_kv_read(const spear_kv_cache_t* cache, int64_t n, const int
  *
  * and zeros for a row that sees none. q.k, the softmax and the sums over j are
  * held in fp32; the weights e^(s_j - max) are rounded to the act dtype for their
- * product with v (whose values it holds exactly, in fp16 to 2^-25), and out once. Rows behind the last request are left as they
- * were. Codes and scales of tokens that no row of a request sees may hold
- * anything; those seen are finite. */
+ * product with v (whose values it holds exactly, in fp16 to 2^-25), and out once.
+ * Rows behind the last request are left as they were. Codes and scales of tokens that
+ * no row of a request sees may hold anything; those seen are finite. */
 typedef struct {
   const spear_kv_cache_t* cache;
   const spear_kv_batch_t* batch;
   int32_t heads;         /* a multiple of kv_heads, 1..1024; tokens * heads /
-                            kv_heads < 2^30                                     */
+                            kv_heads < 2^30, tokens * heads < 2^29              */
   int32_t window;        /* >= 0; 0: none                                       */
   const int32_t* prefix; /* [requests]; NULL: none                              */
   void* plan;            /* spear_attention_sizes' plan_bytes                   */

@@ -77,6 +77,13 @@ __device__ __forceinline__ int plan_range(const AttnPlanParams& p, AttnItem& it,
   return it.s1 - it.s0;
 }
 __device__ __forceinline__ int plan_splits(int steps, int c) { return steps > c ? (steps + c - 1) / c : 1; }
+// the same of few rows, whose stretches have at least the square root of a fifth of the
+// request's steps, in fours (the waves' turns): one workgroup joins them all, and a long
+// request of few heads would be all joining (120000 tokens, one head: 35 us in stretches
+// of 8 steps, 26 of 20)
+__device__ __forceinline__ int plan_row_splits(int steps, int c) {
+  return plan_splits(steps, max(c, 4 * (int)ceilf(__builtin_amdgcn_sqrtf((float)steps * 0.0125f))));
+}
 // stretch x of it's splits
 __device__ __forceinline__ AttnItem plan_stretch(AttnItem it, int splits, int x, int part) {
   const int s0 = it.s0, n = it.s1 - it.s0;
@@ -118,7 +125,7 @@ __global__ __launch_bounds__(kPlanThreads) void k_attention_plan(AttnPlanParams 
   for (int e = 0; e < EACH; ++e) {
     place[e] = size[e] = 0;
     if (steps[e] < 0) continue;
-    const int k = plan_splits(steps[e], c);
+    const int k = plan_row_splits(steps[e], c);
     counts += k + ((int64_t)(k > 1 ? k : 0) << 32);
     size[e] = kSizes - 1 - min((int)((int64_t)steps[e] * (kSizes - 1) / ((int64_t)c * k)), kSizes - 1);
     place[e] = atomicAdd(&s_size[size[e]], k);
@@ -146,7 +153,7 @@ __global__ __launch_bounds__(kPlanThreads) void k_attention_plan(AttnPlanParams 
     s_tile[r0 + e] = (int)min(tile_at, n_tiles);
     tile_at += tiles[e];
     if (steps[e] >= 0) {
-      const int k = plan_splits(steps[e], c);
+      const int k = plan_row_splits(steps[e], c);
       at += k + ((int64_t)(k > 1 ? k : 0) << 32);
     }
   }
@@ -155,7 +162,7 @@ __global__ __launch_bounds__(kPlanThreads) void k_attention_plan(AttnPlanParams 
   for (int i = tid; i < n_items; i += blockDim.x) {
     const int r = plan_find(s_item, p.R, i), x = i - s_item[r];
     AttnItem it = plan_request(p, r);
-    int k = plan_splits(plan_range(p, it, 0, it.rows), c);
+    int k = plan_row_splits(plan_range(p, it, 0, it.rows), c);
     if (k > 1 && s_part[r] + k > p.z.part_rows) it.s1 = it.s0, k = 1;  // (arrays that contradict themselves)
     p.items_rows[s_place[r] + x] = plan_stretch(it, k, k > 1 ? x : 0, s_part[r]);
   }
@@ -352,7 +359,6 @@ __device__ __forceinline__ u32x4 byte_mask(uint32_t bits) {
 // joined in order, the latter by the stretch that ends last.
 // Bound: the codes' bytes (long caches), latency (short ones).
 // ---------------------------------------------------------------------------
-#define XN 8
 constexpr int kWaves = 4;  // of a workgroup of k_attend_rows and k_attend_mid
 // LDS of either: K of each wave's step, then each wave's O
 template <int D, int ROWS>
@@ -556,7 +562,7 @@ __device__ __forceinline__ void attend_rows(const AttnParams& p, uint32_t block,
     __syncthreads();
     if (!*s_last) return;
     // group `part` takes every groups-th stretch in order, N in flight; then the groups in order
-    constexpr int N = XN;
+    constexpr int N = 8;
     total = 0.f;
     top = kLowest;
 #pragma unroll
@@ -608,10 +614,9 @@ __device__ __forceinline__ void attend_rows(const AttnParams& p, uint32_t block,
 }
 
 // ---------------------------------------------------------------------------
-// Tiles of 64 rows (some new tokens, chunks too few to fill the GPU in tiles of
-// 256): as k_attend_rows, four waves with a step each in turn, K by way of LDS, V in
-// registers, on 32 x 32 x 16 MFMAs for two halves of 32 rows that share the operands
-// made of a code. The order in which K's tokens are read from LDS is that which
+// Tiles of 32 rows (some new tokens, chunks too few to fill the GPU in tiles of
+// 256): as attend_rows, four waves with a step each in turn, K by way of LDS, V in
+// registers, on 32 x 32 x 16 MFMAs. The order in which K's tokens are read from LDS is that which
 // leaves a lane the scores of sixteen tokens side by side, run 2t + h of the step.
 // Bound: the conversions and exponentials beside the MFMAs.
 // ---------------------------------------------------------------------------

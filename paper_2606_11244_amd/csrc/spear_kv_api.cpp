@@ -7,20 +7,6 @@
 
 #include "spear_kv.h"
 
-#ifndef XWIN
-#define XWIN 4
-#endif
-#ifndef XRG
-#define XRG 384
-#define XRL 8
-#define XTG 256
-#define XTL 8
-#define XFR 98304
-#endif
-#ifndef XMG
-#define XMG 384
-#define XML 4
-#endif
 using namespace spear;
 
 namespace {
@@ -33,6 +19,8 @@ bool overlaps(const void* a, size_t na, const void* b, size_t nb) {
   return x < y + nb && y < x + na;
 }
 spear_status_t hip_status(hipError_t e) { return e == hipSuccess ? SPEAR_OK : SPEAR_E_HIP; }
+// a launch of fewer than 2^32 threads
+bool launches(int64_t blocks, int threads) { return blocks * threads < (int64_t)1 << 32; }
 bool page_size(int p) { return p == 16 || p == 32 || p == 64 || p == 128; }
 
 // a buffer; where row is given, only the first `row` of each `ld` bytes of it
@@ -167,6 +155,12 @@ spear_status_t spear_kv_append(const spear_kv_cache_t* c, const spear_kv_append_
   const int64_t kl = ld(a->k_ld, kv), vl = ld(a->v_ld, kv);
   const int64_t ql = a->q ? ld(a->q_ld, qd) : 0, ol = a->q ? ld(a->q_out_ld, qd) : 0;
   if (!ld_ok) return SPEAR_E_SHAPE;
+  // Workgroups of a window: in a decoding step every token is a run of its own, in prompts
+  // most of the many find none and cost their start. 4096 tokens, pages of 64: 46 us with one
+  // a window, 50 with four, 55 with eight; 7 prompts of 300, pages of 32: 19, 10 and 10.
+  const int subs = (int)(T <= 1024 ? std::min<int64_t>(T, 64) : 4);
+  const int64_t kv_blocks = (T + 63) / 64 * subs * c->kv_heads * 2, q_blocks = a->q ? T : 0;
+  if (!launches(kv_blocks + q_blocks, 256)) return SPEAR_E_SHAPE;
   if (T == 0) return SPEAR_OK;
   if (!a->k || !a->v || !a->slots || (a->q && !a->q_out) || (r.rotary_dim && (!r.freqs || !a->positions)))
     return SPEAR_E_NULL;
@@ -193,10 +187,8 @@ spear_status_t spear_kv_append(const spear_kv_cache_t* c, const spear_kv_append_
   p.q_out = (uint16_t*)a->q_out;
   p.q_ld = ql, p.k_ld = kl, p.v_ld = vl, p.qo_ld = ol;
   p.slots = a->slots, p.positions = a->positions;
-  p.subs = (int)(T <= 1024 ? std::min<int64_t>(T, 64) : XWIN);
   p.log2_page = __builtin_ctz((unsigned)c->page_tokens);
-  p.kv_blocks = (uint32_t)((T + 63) / 64 * p.subs * c->kv_heads * 2);
-  p.q_blocks = a->q ? (uint32_t)T : 0;
+  p.subs = subs, p.kv_blocks = (uint32_t)kv_blocks, p.q_blocks = (uint32_t)q_blocks;
   const auto launch = c->act_dtype == SPEAR_F16 ? launch_kv_append_f16 : launch_kv_append_bf16;
   return hip_status(launch(p, c->format, (hipStream_t)hip_stream));
 }
@@ -205,7 +197,7 @@ spear_status_t spear_kv_read(const spear_kv_cache_t* c, int64_t n, const int32_t
                              void* hip_stream) {
   const spear_status_t st = check_cache(c);
   if (st != SPEAR_OK) return st;
-  if (n < 0 || n >= ((int64_t)1 << 31) || (n + 15) / 16 * c->kv_heads >= ((int64_t)1 << 31)) return SPEAR_E_SHAPE;
+  if (n < 0 || n >= ((int64_t)1 << 31) || !launches((n + 15) / 16 * c->kv_heads, 256)) return SPEAR_E_SHAPE;
   if (n == 0) return SPEAR_OK;
   if (!slots || !k_out || !v_out) return SPEAR_E_NULL;
   if (off4(slots) || off16(k_out) || off16(v_out)) return SPEAR_E_ALIGN;
@@ -229,7 +221,8 @@ spear_status_t check_attention(const spear_attention_t* a, bool buffers) {
   if (st == SPEAR_OK) st = check_batch(a->batch, buffers);
   if (st != SPEAR_OK) return st;
   if (a->heads < 1 || a->heads > 1024 || a->heads % a->cache->kv_heads || a->window < 0 ||
-      (int64_t)a->batch->tokens * (a->heads / a->cache->kv_heads) >= (1 << 30))
+      (int64_t)a->batch->tokens * (a->heads / a->cache->kv_heads) >= (1 << 30) ||
+      (int64_t)a->batch->tokens * a->heads >= (1 << 29))  // (with it any launch has fewer than 2^32 threads)
     return SPEAR_E_SHAPE;
   if (!buffers) return SPEAR_OK;
   if (!a->plan) return SPEAR_E_NULL;
@@ -237,12 +230,22 @@ spear_status_t check_attention(const spear_attention_t* a, bool buffers) {
   return SPEAR_OK;
 }
 
-
-// Rows, over all kv heads, from which on tiles are the large ones.
-constexpr int kFillRows = XFR;
+// Rows, over all kv heads, from which on tiles are the large ones, which take half the
+// time where there are enough of them. A prompt of 2048, 64 heads (131072 rows): 93 us in
+// large tiles, 137 in small ones; of 1536 (98304): 76 and 84; a chunk of 1024 behind 8000
+// tokens (65536): 414 and 418; a prompt of 1024, 32 heads (32768): 45 and 28.
+constexpr int kFillRows = 98304;
 // Stretches wanted of each kernel, over all kv heads, and a stretch's least steps.
-constexpr int kRowsGoal = XRG, kRowsLeast = XRL, kTileGoal = XTG, kTileLeast = XTL, kMidGoal = XMG,
-              kMidLeast = XML;
+// Few rows: of requests of unlike lengths one and a half a CU even out better than one (64
+// requests of up to 8192 tokens: 35 us, 37 with one a CU, 37 with two), and heads of 64
+// want more loads in flight (131000 tokens: 32 us, 35 with one); one request with heads of
+// 128 is even by itself (131000 tokens: 57 us with one a CU, 65 with one and a half).
+// Stretches of 8 steps, two turns of the waves: 13 requests 19 us, 25 in stretches of 16;
+// 500 tokens 6.4, 7.8 in stretches of 4.
+constexpr int kRowsGoal = 384, kRowsGoalOne = 256, kRowsLeast = 8;
+// Small tiles: 13 requests 19 us, 21 at stretches of 8 steps or 256 stretches. Large ones
+// have a CU each, and take all the same time between 4 and 8 steps.
+constexpr int kMidGoal = 384, kMidLeast = 4, kTileGoal = 256, kTileLeast = 8;
 // (stretches are shared out among kv heads only where there are fewer heads than the
 // goal, so that counters are at most 2 (goal + heads))
 static_assert(4 * kRowsGoal <= kAttnCounters && 4 * std::max(kTileGoal, kMidGoal) <= kAttnCounters, "a counter for each shared tile and head");
@@ -258,7 +261,7 @@ uint32_t plan_key(const spear_attention_t* a) {
   const spear_kv_cache_t* c = a->cache;
   const spear_kv_batch_t* b = a->batch;
   uint64_t h = 0xcbf29ce484222325ull;
-  for (const int64_t v : {(int64_t)c->kv_heads, (int64_t)c->page_tokens, (int64_t)b->requests, (int64_t)b->tokens,
+  for (const int64_t v : {(int64_t)c->kv_heads, (int64_t)c->head_dim, (int64_t)c->page_tokens, (int64_t)b->requests, (int64_t)b->tokens,
                           (int64_t)b->max_new, (int64_t)b->width, (int64_t)a->heads, (int64_t)a->window,
                           (int64_t)(a->prefix != nullptr)})
     for (int i = 0; i < 32; i += 8) h = (h ^ ((v >> i) & 255)) * 0x100000001b3ull;
@@ -272,7 +275,7 @@ AttnLayout attention_layout(const spear_attention_t* a) {
   const bool rows = group <= kRows, tile = (int64_t)b->max_new * group > kRows;
   AttnLayout l;
   AttnShape& z = l.z;
-  z.goal_rows = (int)((kRowsGoal + hkv - 1) / hkv);
+  z.goal_rows = (int)(((R == 1 && c->head_dim == 128 ? kRowsGoalOne : kRowsGoal) + hkv - 1) / hkv);
   // sum over tiles of max(1, ceil(steps / c)) with c >= all steps / goal
   z.max_rows = rows ? (int)R + z.goal_rows : 0;
   z.least_rows = kRowsLeast;

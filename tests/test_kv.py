@@ -193,6 +193,21 @@ def test_sizes_take_no_buffers_and_do_not_shrink():
     assert attention(sizes=True, heads=5)[0] == SHAPE
 
 
+def test_launches_have_a_size():
+    """More workgroups than one launch takes are refused, not cut."""
+    none = dict(k=None, v=None, k_scale=None, v_scale=None, pages=0)
+    assert append(cache(kv_heads=1024, **none), tokens=1 << 22) == SHAPE
+    assert append(cache(kv_heads=128, **none), tokens=1 << 20, q=None) == SHAPE  # 2^24 workgroups
+    assert append(cache(kv_heads=128, **none), tokens=(1 << 20) - 64, q=None) == 0
+    read = lambda heads, n: sp.LIB.spear_kv_read(ctypes.byref(cache(kv_heads=heads, **none)), n, _at(30),  # noqa: E731
+                                                 1 << 56, 1 << 57, None)
+    assert read(1024, 1 << 18) == SHAPE and read(1024, (1 << 18) - 16) == 0 and read(1, (1 << 28) - 16) == 0
+    big = dict(starts=None, lens=None, table=None, tokens=1 << 22, max_new=1 << 22)
+    c = dict(k=None, v=None, k_scale=None, v_scale=None)
+    assert attention(cache(**c), batch(**big), plan=None, workspace=None, sizes=True, heads=128)[0] == SHAPE
+    assert attention(cache(**c), batch(**big), plan=None, workspace=None, sizes=True, heads=126)[0] == 0
+
+
 def _freqs(rot, base=10000.0, factor=1.0, context=0.0, low=1.0, high=4.0):
     f = torch.zeros(max(rot, 0) // 2 + 1, dtype=torch.int64)
     return sp.LIB.spear_rope_frequencies(rot, base, factor, context, low, high, f.data_ptr()), f.tolist()
