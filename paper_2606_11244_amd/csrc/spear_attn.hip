@@ -19,7 +19,8 @@ constexpr float kMostSum = 4096.f;
 // The plan. One workgroup: requests are told apart by their rows, all steps are
 // summed, and each request's (or tile's) steps are cut into stretches of equal
 // length near all steps / goal, so that workgroups have like shares whatever the
-// lengths; heavy tiles (late positions) come first. Latency, once for all layers.
+// lengths; heavy tiles (late positions) come first. Bound: latency, once for all layers:
+// one request 3.6 us, 24 or 64 requests 4.2, the 128 tiles of a prompt of 4096 9.6.
 // ---------------------------------------------------------------------------
 constexpr int kPlanThreads = 1024, kSizes = 32;
 
@@ -357,7 +358,11 @@ __device__ __forceinline__ u32x4 byte_mask(uint32_t bits) {
 // are V's operand as they are, a page's scale is one number a lane, and K and V
 // come in pieces of 16 bytes. The waves' and then the stretches' results are
 // joined in order, the latter by the stretch that ends last.
-// Bound: the codes' bytes (long caches), latency (short ones).
+// Bound: the codes' bytes (long caches: one request of 131000 tokens, 8 heads of 128,
+// 268 MB in 56 us, 4.8 TB/s, where the loads alone take as long; 64 requests of up to
+// 8192 tokens, 155 MB in 34 us, 4.5 TB/s), latency (one request of 500 tokens: 5.8 us).
+// K goes through LDS so that V has the registers to be a step ahead (with both in
+// registers, and stretches in the requests' order, these 64 took 45 us).
 // ---------------------------------------------------------------------------
 constexpr int kWaves = 4;  // of a workgroup of k_attend_rows and k_attend_mid
 // LDS of either: K of each wave's step, then each wave's O
@@ -618,7 +623,10 @@ __device__ __forceinline__ void attend_rows(const AttnParams& p, uint32_t block,
 // 256): as attend_rows, four waves with a step each in turn, K by way of LDS, V in
 // registers, on 32 x 32 x 16 MFMAs. The order in which K's tokens are read from LDS is that which
 // leaves a lane the scores of sixteen tokens side by side, run 2t + h of the step.
-// Bound: the conversions and exponentials beside the MFMAs.
+// Tiles of 32 rows and not more: more workgroups, and two of them to a SIMD's registers
+// (a chunk of 512 beside 8 requests 31 us, 45 in tiles of 64).
+// Bound: the conversions and exponentials beside the MFMAs; that chunk, 12.6 GFLOP, 8
+// heads on one: 29.5 us, 427 TFLOP/s.
 // ---------------------------------------------------------------------------
 template <int DT, int FMT, int D, bool OPT>
 __device__ __forceinline__ void attend_mid(const AttnParams& p, uint32_t block, char* lds, float* s_m, float* s_l, int* s_last) {
@@ -721,7 +729,7 @@ __device__ __forceinline__ void attend_mid(const AttnParams& p, uint32_t block, 
     Scales sc = scales(page), sn = sc;
     int entry = entry_at(s + W);
     for (; s < it.s1; s += W) {
-      f32x16 st[Y][2] = {};  // [half of the rows][32 tokens]
+      f32x16 st[Y][2] = {};  // [32 rows][32 tokens]
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         const int token = 32 * t + 16 * ((c >> 2) & 1) + 4 * (c >> 3) + (c & 3);
@@ -760,7 +768,7 @@ __device__ __forceinline__ void attend_mid(const AttnParams& p, uint32_t block, 
           for (int d = 0; d < DTILES; ++d) vr[t][d] &= bytes;
         }
       }
-      u32x4 pw[Y][4];  // weights: [half of the rows][eight tokens of either run]
+      u32x4 pw[Y][4];  // weights: [32 rows][eight tokens of either run]
 #pragma unroll
       for (int y = 0; y < Y; ++y) {
         const ScoreOptions opt{scale, p.softcap, slope2[y]};
@@ -928,7 +936,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_attend_mid(AttnParams p) {
 // S^T = K Q^T and O^T = V^T P^T: a lane holds half the scores of one row, and its
 // weights are V's operand once V's tokens stand in LDS in the order in which the
 // MFMA leaves the scores (the middle quads of every sixteen exchanged).
-// Bound: the MFMAs and the exponentials beside them.
+// Bound: the MFMAs and the exponentials beside them: a prompt of 4096, 64 heads, 275 GFLOP
+// in 310 us, 884 TFLOP/s; its loads and MFMAs without a softmax take 200. Tried in its
+// place, same prompt: the weights of a step made beside the next step's scores 322, tiles
+// of 128 rows at two workgroups a CU 367, four buffers and a barrier each two steps 319.
 // ---------------------------------------------------------------------------
 template <int DT, int FMT, int D, bool OPT>
 __global__ __launch_bounds__(2 * tile_rows(D), 2) void k_attend_tile(AttnParams p) {

@@ -9,8 +9,8 @@ namespace spear {
 // ---------------------------------------------------------------------------
 // Block tables, slots and positions. Two sums over the requests (rows, then new
 // pages of those that can be served), kept in LDS, and then the new pages and the
-// rows in flat order, each finding its request by bisection. Everything is latency:
-// a few dependent loads and two barriers a sum.
+// rows in flat order, each finding its request by bisection. Bound: latency, a few
+// dependent loads and two barriers a sum: one request 3.4 us, 384 with 5276 rows 6.7.
 // ---------------------------------------------------------------------------
 constexpr int kPagesThreads = 1024;
 
@@ -289,7 +289,9 @@ __device__ __forceinline__ void turn(const Unit& u, int interleaved, T (&a)[W], 
 // if it grew, and writes the run's. One page and head is one workgroup's alone: no
 // atomics, the same codes on every run. A workgroup of the queries' part takes
 // a token, its cosines and sines in LDS for all heads.
-// Bound: the bytes of q, k and v (long prompts), latency (decode).
+// Bound: the bytes of q, k and v (long prompts: 4096 tokens with 64 heads of queries and
+// 8 of keys and values, 159 MB in 42 us, 3.8 TB/s), latency (decode: a token 6 us, slots,
+// rows, the page's scale and the maximum one after the other).
 // ---------------------------------------------------------------------------
 
 // the scale of a page and head, from the one before and the largest magnitude given
@@ -615,7 +617,8 @@ hipError_t SPEAR_D(launch_kv_append)(const KvAppendParams& p, int format, hipStr
 
 // ---------------------------------------------------------------------------
 // Values back: sixteen tokens of one head a workgroup; V, whose places of one
-// feature lie side by side, changes its order through LDS.
+// feature lie side by side, changes its order through LDS. Bound: bytes (4096 tokens of
+// 8 heads, 25 MB in 6.9 us, 3.6 TB/s), latency (a few tokens 3 us).
 // ---------------------------------------------------------------------------
 template <int DT, int FMT, int D>
 __global__ __launch_bounds__(256) void k_kv_read(KvReadParams p) {
