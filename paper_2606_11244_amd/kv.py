@@ -94,6 +94,8 @@ def _on(holder, dev):
 
 def _rows(t, shape, dtype, what):
     """Stride between the tokens of a [tokens][heads][head_dim] tensor of dense rows (0: dense)."""
+    if t.dtype is dtype and t.shape == shape and t.is_contiguous():
+        return 0
     st = t.stride()
     if t.dtype is dtype and t.shape == shape and st[2] == 1 and st[1] == shape[2]:
         if shape[0] < 2:
@@ -134,7 +136,7 @@ class Cache:
         self.device = devices.pop()
         self.c = _Cache(_CODES[k.dtype], _ACTS[act_dtype], kv_heads, head_dim, page_tokens, 0, pages,
                         k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr())
-        self._ref = ctypes.byref(self.c)
+        self._ref, self._at = ctypes.byref(self.c), ctypes.pointer(self.c)
 
     def tensors(self):
         return self.k, self.v, self.k_scale, self.v_scale
@@ -303,7 +305,7 @@ def attention(plan: AttentionPlan, q, out, *, workspace, cache: Cache | None = N
     if slopes is not None and (slopes.dtype is not torch.float32 or slopes.numel() != heads or not slopes.is_contiguous()):
         raise ValueError("attention: slopes is [heads] fp32")
     shape, act = (plan.batch.tokens, heads, D), cache.act_dtype
-    a = _Attention(ctypes.pointer(cache.c), plan._batch, heads, plan.c.window, plan._prefix, plan.c.plan,
+    a = _Attention(cache._at, plan._batch, heads, plan.c.window, plan._prefix, plan.c.plan,
                    plan.c.plan_bytes, q.data_ptr(), out.data_ptr(), _rows(q, shape, act, "q"), _rows(out, shape, act, "out"),
                    None if slopes is None else slopes.data_ptr(), D ** -0.5 if scale is None else scale, softcap,
                    workspace.data_ptr(), workspace.numel() * workspace.element_size())

@@ -439,7 +439,7 @@ def _device_of(first, *tensors) -> int:
     """The current GPU, which holds every tensor: a kernel reads what it is
     given, and the stream is the current device's."""
     dev = first.get_device()
-    if dev < 0 or dev != torch.cuda.current_device():
+    if dev < 0 or dev != torch._C._cuda_getDevice():  # (as current_device(), in a quarter of its time)
         raise ValueError(f"tensors on the current GPU are needed (got {first.device})")
     for t in tensors:
         if t is not None and t.get_device() != dev:
