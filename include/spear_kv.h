@@ -179,7 +179,8 @@ spear_status_t spear_kv_read(const spear_kv_cache_t* cache, int64_t n, const int
  *
  * and zeros for a row that sees none. q.k, the softmax and the sums over j are
  * held in fp32; the weights e^(s_j - max) are rounded to the act dtype for their
- * product with v (whose values it holds exactly, in fp16 to 2^-25), and out once.
+ * product with v (whose values it holds exactly, in fp16 to 2^-25) and, of requests
+ * of more than 16 rows a kv head, in their sum; out is rounded once.
  * Rows behind the last request are left as they were. Codes and scales of tokens that
  * no row of a request sees may hold anything; those seen are finite. */
 typedef struct {

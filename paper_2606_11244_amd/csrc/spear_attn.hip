@@ -1070,7 +1070,9 @@ __global__ __launch_bounds__(2 * tile_rows(D), 2) void k_attend_tile(AttnParams 
       const f32x4 ks = *(const f32x4*)s_ks[s & 1];
       const bool pages_there = __all(fminf(fminf(ks[0], ks[1]), fminf(ks[2], ks[3])) > 0.f);
       const bool whole = j0 + kStep <= min(it.end, pos_lo + 1) && pos_hi - j0 < p.window && pages_there;
-      f32x4 f = ks;  // what st is of a score
+      f32x4 f;  // what st is of a score (an operand's modifier; left to the masked steps it was left out of some of them)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) f[r] = fabsf(ks[r]);
       if constexpr (OPT) {
         f = f32x4{1.f, 1.f, 1.f, 1.f};
 #pragma unroll
@@ -1086,8 +1088,6 @@ __global__ __launch_bounds__(2 * tile_rows(D), 2) void k_attend_tile(AttnParams 
 #pragma unroll
           for (int e = 0; e < 16; ++e) st[t][e] = where_seen(st[t][e], sees, 8 * (e >> 2) + (e & 3));
         }
-#pragma unroll
-        for (int r = 0; r < 4; ++r) f[r] = fabsf(f[r]);
       }
       u32x4 pw[4];  // sixteen tokens each
       float sum;

@@ -173,7 +173,14 @@ def plain_attention(q, k, v, starts, lens, heads, *, scale, softcap=0.0, slopes=
             # relatively, and by its rounding; sums over L tokens by L steps of fp32 at most
             off = 2.0 ** -24 * ((D + 16) * size + 8 * (s.masked_fill(~seen, 0).abs() + b.abs()) + 16)
             po = p * off
-            e = (u + po.sum(1, keepdim=True) + L * 2.0 ** -24) * a + po @ vv.abs() + u * o.abs()
+            # The weights' roundings w (1 + d), |d| <= u: over the exact sum they put the output off by
+            # sum p d v, at most u a. Over the sum of the rounded ones, as tiles have it, by
+            # sum p (1 + d) v / sum p (1 + d) - o = sum p d (v - o) / (1 + sum p d), at most
+            # u / (1 - u) sum p |v - o|; and sum p |v - o| <= a + |o|, and <= (sum p v^2 - o^2)^(1/2)
+            # (sum p = 1, Cauchy and Schwarz).
+            spread = torch.minimum(a + o.abs(), (p @ (vv * vv) - o * o).clamp(min=0).sqrt())
+            weights = torch.maximum(u * a, u / (1 - u) * spread)
+            e = weights + (po.sum(1, keepdim=True) + L * 2.0 ** -24) * a + po @ vv.abs() + u * o.abs()
             if act is torch.float16:
                 # weights below 2^-14 of the largest are held to 2^-25; so is a value of v below 2^-14, which is
                 # a code times any power of two and need not be one of fp16's multiples of 2^-24 (weights sum

@@ -455,6 +455,91 @@ def test_attention_of_values_at_the_ends_of_the_range(act, codes, size, lengths)
     assert bool(torch.isfinite(s.out.float()).all()) and (size < 2.0 ** -20 or bool((s.out != 0).any()))
 
 
+# Steps of so many rows (padding counts: sizes alone are known to the host) that tiles are the large ones.
+LARGE = dict(heads=64, pad=1600)
+
+
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("codes", CODES)
+@pytest.mark.parametrize("what", ["chunks", "prompt", "prompt and decode"])
+@pytest.mark.parametrize("kvh,D,P", [(8, 128, 64), (4, 64, 16), (64, 128, 128), (1, 64, 32), (2, 128, 16)])
+def test_attention_in_large_tiles(act, codes, what, kvh, D, P):
+    Setup(LENGTHS[what], kvh=kvh, D=D, P=P, act=act, codes=codes, **LARGE).check()
+
+
+@pytest.mark.parametrize("D,act,codes", [(128, torch.float16, torch.float8_e4m3fn), (64, torch.bfloat16, torch.int8),
+                                         (128, torch.bfloat16, torch.float8_e4m3fn), (64, torch.float16, torch.int8)])
+@pytest.mark.parametrize("softcap,slopes,window,prefix", [
+    (15.0, False, 0, False), (0.0, True, 0, False), (0.0, False, 1, False), (0.0, False, 100, False),
+    (0.0, False, 10000, False), (0.0, False, 0, True), (5.0, True, 70, True), (0.0, False, 70, True)])
+def test_attention_options_in_large_tiles(D, act, codes, softcap, slopes, window, prefix):
+    lengths = [(200, 600), (1, 300), (33, 40)]
+    s = torch.exp2(-torch.arange(64, device="cuda").float() / 8) if slopes else None
+    first = [37, 37, 40] if prefix else None
+    Setup(lengths, kvh=8, D=D, P=32, act=act, codes=codes, window=window, prefix=first, **LARGE).check(
+        softcap=softcap, slopes=s, scale=-0.3 if softcap else None)
+
+
+@pytest.mark.parametrize("D,act,codes", [(128, torch.float16, torch.int8), (64, torch.bfloat16, torch.float8_e4m3fn)])
+def test_large_tiles_of_requests_without_keys(D, act, codes):
+    """lens 0, fewer tokens than rows, pages outside the pool; more rows than said."""
+    s = Setup([(2, 40), (30, 0), (0, 50), (50, 20), (70, 0), (9, 200), (90, 20)], kvh=4, D=D, P=16, act=act, codes=codes, **LARGE)
+    dead = [torch.zeros(max(L, 1), dtype=torch.bool) for _, L in s.lengths]
+    for r, page, bad in ((0, 1, -1), (5, 0, s.pool), (5, 3, 2 ** 31 - 1), (5, 7, -2 ** 31), (6, 1, -1)):
+        s.batch.table[r, page] = bad
+        dead[r][16 * page:16 * page + 16] = True
+    s.check(dead=dead)
+    s.batch.table[5].fill_(s.pool + 5)
+    dead[5][:] = True
+    s.check(dead=dead)
+    Setup([(300, 400), (1, 33), (3, 3)], kvh=8, D=D, P=16, act=act, codes=codes, max_new=40, **LARGE).check()
+
+
+def test_large_tiles_of_starts_that_contradict_themselves():
+    s = Setup([(3, 900), (40, 1200), (1, 2500), (2, 33)], kvh=8, D=128, P=16, act=torch.bfloat16, codes=torch.int8, **LARGE)
+    want, T = s.run().clone(), s.batch.tokens
+    for starts in ([T, 0, T, 0, T], [-5, 2 ** 31 - 1, 3, -2 ** 31, 50], [T] * 5, [0, T, T, 0, T]):
+        s.batch.starts.copy_(_ints(starts))
+        s.batch.lens.copy_(_ints([2 ** 31 - 1, 1200, -7, 2 ** 30]))
+        s.run()
+        s.batch.starts.copy_(_ints(s.starts))
+        s.batch.lens.copy_(_ints(s.lens))
+        s.out.fill_(9.0)
+        assert torch.equal(s.run(), want)
+
+
+@pytest.mark.parametrize("D,kvh,act,codes", [(128, 1, torch.float16, torch.int8), (64, 2, torch.bfloat16, torch.float8_e4m3fn),
+                                             (128, 8, torch.bfloat16, torch.int8)])
+def test_large_tiles_in_stretches(D, kvh, act, codes):
+    """Few rows of long requests: stretches of a tile, joined in order; strides of other tensors between."""
+    s = Setup([(5, 9000), (20, 3000)], kvh=kvh, D=D, P=64, act=act, codes=codes, **LARGE)
+    s.check()
+    want = s.out.clone()
+    T, H, _ = s.q.shape
+    packed = torch.full((T, H + 4, D), 3.0, dtype=s.q.dtype, device="cuda")
+    packed[:, :H] = s.q
+    wide = torch.full((T, H + 1, D), 3.0, dtype=s.q.dtype, device="cuda")
+    s.q, s.out = packed[:, :H], wide[:, :H]
+    for _ in range(5):
+        s.out.fill_(9.0)
+        assert torch.equal(s.run(), want) and bool((wide[:, H:] == 3.0).all())
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("codes", CODES)
+@pytest.mark.parametrize("act,size", [(torch.float16, 2.0 ** -24), (torch.float16, 2.0 ** -20), (torch.float16, 2.0 ** -14),
+                                      (torch.bfloat16, 2.0 ** -90), (torch.float16, 3e4)])
+def test_large_tiles_of_values_at_the_ends_of_the_range(act, codes, size, D):
+    s = Setup([(200, 200)], kvh=2, D=D, P=16, act=act, codes=codes, **LARGE)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    slots = [s.table[0][j // 16] * 16 + j % 16 for j in range(200)]
+    k = torch.randn(200, 2, D, device="cuda", generator=g).to(act)
+    v = (torch.randn(200, 2, D, device="cuda", generator=g).clamp(-2, 2) * size).to(act)
+    s.kv.append(s.cache, k, v, _ints(slots))
+    s.check()
+    assert bool(torch.isfinite(s.out.float()).all()) and (size < 2.0 ** -20 or bool((s.out != 0).any()))
+
+
 @pytest.mark.parametrize("lengths", [[(1, 3000)] * 3, [(128, 900), (1, 50)]])
 def test_attention_is_repeatable(lengths):
     s = Setup(lengths, 8, 1, 128, 64, torch.bfloat16, torch.int8)
