@@ -540,6 +540,15 @@ def test_large_tiles_of_values_at_the_ends_of_the_range(act, codes, size, D):
     assert bool(torch.isfinite(s.out.float()).all()) and (size < 2.0 ** -20 or bool((s.out != 0).any()))
 
 
+@pytest.mark.parametrize("rows", [1, 17])
+def test_attention_of_more_requests_than_threads(rows):
+    """A plan of several requests a thread, and of more tiles than threads."""
+    rng = random.Random(rows)
+    lengths = [(n, n + rng.randrange(0, 90)) for n in (rng.choice((0, 1, rows, rows)) for _ in range(1100))]
+    lengths[700] = (rows, 4000)
+    Setup(lengths, 2, 2, 64, 32, torch.bfloat16, torch.int8, pad=3).check()
+
+
 @pytest.mark.parametrize("lengths", [[(1, 3000)] * 3, [(128, 900), (1, 50)]])
 def test_attention_is_repeatable(lengths):
     s = Setup(lengths, 8, 1, 128, 64, torch.bfloat16, torch.int8)
