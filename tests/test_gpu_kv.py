@@ -540,6 +540,26 @@ def test_large_tiles_of_values_at_the_ends_of_the_range(act, codes, size, D):
     assert bool(torch.isfinite(s.out.float()).all()) and (size < 2.0 ** -20 or bool((s.out != 0).any()))
 
 
+@pytest.mark.parametrize("large", [False, True])
+@pytest.mark.parametrize("act,codes", [(torch.float16, torch.int8), (torch.bfloat16, torch.float8_e4m3fn), (torch.float16, torch.float8_e4m3fn)])
+@pytest.mark.parametrize("D,prefix,softcap", [(128, None, 0.0), (64, [37, 0, 90, 200], 0.0), (128, [1, 64, 0, 5], 9.0)])
+def test_attention_where_no_row_looks_there_may_be_anything(large, act, codes, D, prefix, softcap):
+    """Tokens between a prefix and the window: pages whose scales are NaN or infinite, codes that are NaN."""
+    lengths, window, P = [(1, 1000), (3, 900), (40, 1200), (100, 700)], 70, 32
+    more = LARGE if large else dict(heads=8)
+    s = Setup(lengths, kvh=2, D=D, P=P, act=act, codes=codes, window=window, prefix=prefix, **more)
+    for r, (n, L) in enumerate(lengths):
+        lo, hi = (prefix[r] if prefix else 0), L - n - window + 1
+        for j in range(lo, hi):
+            page, at = s.table[r][j // P], j % P
+            for t in (s.cache.k.view(torch.uint8)[page, :, at], s.cache.v.view(torch.uint8)[page, :, :, at]):
+                t.fill_(0x7F if codes is torch.float8_e4m3fn else 0x80)
+            if j % P == 0 and j + P <= hi:
+                s.cache.k_scale[page] = float("nan") if j // P % 2 else float("inf")
+                s.cache.v_scale[page] = float("inf") if j // P % 3 else float("nan")
+    s.check(softcap=softcap)
+
+
 @pytest.mark.parametrize("rows", [1, 17])
 def test_attention_of_more_requests_than_threads(rows):
     """A plan of several requests a thread, and of more tiles than threads."""
