@@ -314,12 +314,18 @@ __device__ __forceinline__ PageScale settle(float top, float before, float* red)
   s.grew = s.scale > before;
   return s;
 }
+// Older codes under a scale that grew. INT8's are held to the new scale's largest code: 127 at
+// 2^9 would become 63.5 and round to 64 at 2^10, in fp16 an infinity. E4M3's largest, 448, is at
+// most 224 under a larger scale, below the limit of 240.
 template <int FMT>
-__device__ __forceinline__ uint32_t divide4(uint32_t w, float ratio) {
+__device__ __forceinline__ uint32_t divide4(uint32_t w, const PageScale& s) {
   float c[4];
   decode4<FMT>(w, c);
 #pragma unroll
-  for (int e = 0; e < 4; ++e) c[e] *= ratio;
+  for (int e = 0; e < 4; ++e) {
+    c[e] *= s.ratio;
+    if (FMT == KV_INT8) c[e] = fminf(fmaxf(c[e], -s.most), s.most);
+  }
   return encode4<FMT>(c);
 }
 
@@ -442,7 +448,7 @@ __device__ __forceinline__ void append_k(const KvAppendParams& p, int t, int slo
   const PageScale s = settle<DT, FMT>(top, before, red);
   if (s.grew) {
     if (tid == 0) p.c.k_scale[ph] = s.scale;
-    for (int i = tid; i < off * D / 4; i += 256) ((uint32_t*)codes)[i] = divide4<FMT>(((uint32_t*)codes)[i], s.ratio);
+    for (int i = tid; i < off * D / 4; i += 256) ((uint32_t*)codes)[i] = divide4<FMT>(((uint32_t*)codes)[i], s);
   }
 #pragma unroll 1
   for (int i = tid; i < all; i += 256) {
@@ -482,7 +488,7 @@ __device__ __forceinline__ void append_v(const KvAppendParams& p, int t, int slo
   if (s.grew)
     for (int i = tid; i < D * q0; i += 256) {
       uint32_t* w = (uint32_t*)(codes + i / q0 * P + 4 * (i % q0));
-      *w = divide4<FMT>(*w, s.ratio);
+      *w = divide4<FMT>(*w, s);
     }
 #pragma unroll
   for (int y = 0; y < U; ++y) {
@@ -503,7 +509,7 @@ __device__ __forceinline__ void append_v(const KvAppendParams& p, int t, int slo
       for (int e = 0; e < 4; ++e) c[e] = to_code(act2f<DT>((x[y][e][f >> 1] >> (16 * (f & 1))) & 0xFFFFu), s.inv, s.most);
       uint32_t fresh = encode4<FMT>(c);
       if (before_run | behind_run) {
-        const uint32_t old = *w, kept = before_run && s.grew ? divide4<FMT>(old, s.ratio) : old;
+        const uint32_t old = *w, kept = before_run && s.grew ? divide4<FMT>(old, s) : old;
         fresh = (kept & before_run) | (old & behind_run) | (fresh & ~(before_run | behind_run));
       }
       *w = fresh;

@@ -1,0 +1,69 @@
+"""The cache's operators and attention at the far ends of their stated ranges, on
+the GPU, against formulas in 64 bits."""
+from __future__ import annotations
+
+import pytest
+import torch
+
+import kv_util as U
+from test_gpu_kv import ACTS, CODES, LARGE, Setup, _ints, _kv
+
+pytestmark = pytest.mark.gpu
+
+# the least power of two whose multiple by the largest code passes the activation type's end
+LAST_SCALE = {(torch.float16, torch.int8): 2.0 ** 10, (torch.bfloat16, torch.int8): 2.0 ** 122,
+              (torch.float16, torch.float8_e4m3fn): 2.0 ** 8, (torch.bfloat16, torch.float8_e4m3fn): 2.0 ** 120}
+
+
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("codes", CODES)
+@pytest.mark.parametrize("P,D,off", [(16, 64, 1), (16, 128, 4), (32, 64, 7), (128, 128, 66)])
+def test_scales_that_grow_past_the_types_end(act, codes, P, D, off):
+    """The largest codes of the last scale but one, then the type's largest value in the same page: no code,
+    old or new, stands for a value past the type's largest (INT8: 127 / 2 is held to 63)."""
+    kv = _kv()
+    last, top = LAST_SCALE[act, codes], float(torch.finfo(act).max)
+    cache = kv.new_cache(3, 2, P, D, act, codes)
+    # places 0..off-1 at half the last scale: its largest code (either sign), and smaller ones
+    x = torch.randint(-127, 128, (off, 2, D), device="cuda", generator=torch.Generator(device="cuda").manual_seed(P)).double()
+    x[:, :, 0], x[:, :, 1], x[:, :, 2], x[:, :, D - 1] = 127, -127, 126, 127
+    if codes is torch.float8_e4m3fn:
+        x = U.nearest(x.cpu() * 448 / 127, codes).cuda()
+    old = (x * (last / 2)).to(act)
+    assert torch.equal(old.double(), x * (last / 2)) and bool(torch.isfinite(old).all())
+    kv.append(cache, old, old.clone(), _ints([P + i for i in range(off)]))
+    assert cache.k_scale[1].tolist() == [last / 2] * 2 and cache.v_scale[1].tolist() == [last / 2] * 2
+    new = torch.zeros(1, 2, D, dtype=act, device="cuda")
+    new[:, :, 5], new[:, :, 6] = top, -top
+    kv.append(cache, new, new.clone(), _ints([P + off]))
+    assert cache.k_scale[1].tolist() == [last] * 2 and cache.v_scale[1].tolist() == [last] * 2
+    most = U.top_code(last, codes, act)
+    want = torch.cat([U.nearest(x.cpu() / 2, codes).clamp(-most, most), (new.cpu().double() / last).clamp(-most, most)]) * last
+    ko, vo = (torch.empty(off + 1, 2, D, dtype=act, device="cuda") for _ in range(2))
+    kv.read(cache, _ints([P + i for i in range(off + 1)]), ko, vo)
+    for got in (ko, vo):
+        assert bool(torch.isfinite(got).all())
+        assert torch.equal(got.cpu().double(), want)
+
+
+@pytest.mark.parametrize("codes", CODES)
+@pytest.mark.parametrize("lengths,more", [([(1, 200)], {}), ([(20, 200)], {}), ([(200, 200)], LARGE)])
+def test_attention_over_scales_that_grew_past_the_types_end(codes, lengths, more):
+    """Values of fp16's whole range, written so that pages' scales grow to the last one: outputs are finite, also of
+    rows whose weight for such a token is zero."""
+    act, L = torch.float16, lengths[0][1]
+    s = Setup(lengths, kvh=2, D=64, P=16, act=act, codes=codes, **{"heads": 4, **more})
+    g = torch.Generator(device="cuda").manual_seed(1)
+    last = LAST_SCALE[act, codes]
+    k = torch.randn(L, 2, 64, device="cuda", generator=g).to(act)
+    v = (torch.randint(-1, 2, (L, 2, 64), device="cuda", generator=g) * U.TOP[codes] * last / 2).to(act)
+    v[15::16, :, 3::7] = float(torch.finfo(act).max)
+    slots = [s.table[0][j // 16] * 16 + j % 16 for j in range(L)]
+    old = [j for j in range(L) if j % 16 != 15]
+    rest = [j for j in range(L) if j % 16 == 15]
+    for part in (old, rest):  # (the last place of a page comes after the others)
+        s.kv.append(s.cache, k[part], v[part], _ints([slots[j] for j in part]))
+    assert float(s.cache.v_scale[s.table[0][0]].max()) == last
+    for scale in (None, 40.0):  # (and weights that are zero but for one token)
+        s.check(scale=scale)
+        assert bool(torch.isfinite(s.out[:lengths[0][0]]).all())
