@@ -293,7 +293,7 @@ __device__ __forceinline__ uint32_t scaled2(uint32_t pair, float f) {
 
 // A score in powers of two. OPT: capped, or biased by distance.
 struct ScoreOptions {
-  float scale, cap, slope2;  // slope2: slope times log2 e
+  float scale, cap, inv_cap, slope2;  // slope2: slope times log2 e
 };
 // (of a plain score all but the dot product is one factor: at least the least float,
 // which makes no difference to a score of scale zero, and keeps what is masked, minus
@@ -301,12 +301,19 @@ struct ScoreOptions {
 __device__ __forceinline__ float dot_factor(float k_scale, const ScoreOptions& o) {
   return fmaxf(k_scale * (o.scale * kLog2e), 1.17549435e-38f);
 }
+// cap tanh(z), z = t / cap: cap (1 - 2 / (e^2z + 1)), off by some 2^-23 cap (the reciprocal
+// instruction's last place with it), which leaves nothing of a score far below the cap (at a cap
+// of 10^4 a score was off by 10^-3, at 10^8 it was gone). Below a quarter of the cap Taylor's
+// sum t (1 - z^2/3 + 2 z^4/15 - 17 z^6/315 + 62 z^8/2835), whose next term is 10^-8 at most.
+__device__ __forceinline__ float capped(float t, const ScoreOptions& o) {
+  const float z = t * o.inv_cap, y = z * z;
+  const float near = t * (1.f + y * (-1.f / 3 + y * (2.f / 15 + y * (-17.f / 315 + y * (62.f / 2835)))));
+  const float far = o.cap * (1.f - 2.f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(z * (2.f * kLog2e)) + 1.f));
+  return fabsf(z) < 0.25f ? near : far;
+}
 __device__ __forceinline__ float score2(float dot, float k_scale, const ScoreOptions& o, int pos, int j) {
   float t = dot * (k_scale * o.scale);
-  if (o.cap > 0.f) {  // cap tanh(t / cap) = cap (1 - 2 / (e^(2 t / cap) + 1))
-    const float e = __builtin_amdgcn_exp2f(t * (2.f * kLog2e / o.cap));
-    t = o.cap * (1.f - 2.f / (e + 1.f));
-  }
+  if (o.cap > 0.f) t = capped(t, o);
   return t * kLog2e - o.slope2 * (float)abs(pos - j);
 }
 
@@ -314,7 +321,7 @@ __device__ __forceinline__ float score2(float dot, float k_scale, const ScoreOpt
 // not yet read is another trip to memory: what is used late is asked for at the start,
 // with the rest (one request of 500 tokens 5.84 us, 5.68 this way).
 __device__ __forceinline__ void early(const AttnParams& p) {
-  asm volatile("" ::"s"(p.window), "s"(p.out), "s"(p.out_ld), "s"(p.slopes), "s"(p.softcap), "s"(p.scale));
+  asm volatile("" ::"s"(p.window), "s"(p.out), "s"(p.out_ld), "s"(p.slopes), "s"(p.softcap), "s"(p.inv_cap), "s"(p.scale));
   asm volatile("" ::"s"(p.counters_rows), "s"(p.counters_tile), "s"(p.parts_rows), "s"(p.parts_tile));
 }
 
@@ -392,7 +399,7 @@ __device__ __forceinline__ void attend_rows(const AttnParams& p, uint32_t block,
       for (int s = 0; s < 2 * KS; ++s) q[s] = u32x4{0, 0, 0, 0};
   }
   const int pos = it.pos0 + i, pos_max = it.pos0 + it.rows - 1;
-  const ScoreOptions opt{fabsf(p.scale), p.softcap, OPT && p.slopes ? p.slopes[hq] * kLog2e : 0.f};
+  const ScoreOptions opt{fabsf(p.scale), p.softcap, p.inv_cap, OPT && p.slopes ? p.slopes[hq] * kLog2e : 0.f};
   const int32_t* table = p.table + it.r * p.ld;
   const uint32_t page_bytes = P * D, pool_bytes = p.c.Hkv * page_bytes;
   const uint8_t *k_head = p.c.k + (int64_t)head * page_bytes, *v_head = p.c.v + (int64_t)head * page_bytes;
@@ -771,7 +778,7 @@ __device__ __forceinline__ void attend_mid(const AttnParams& p, uint32_t block, 
       u32x4 pw[Y][4];  // weights: [32 rows][eight tokens of either run]
 #pragma unroll
       for (int y = 0; y < Y; ++y) {
-        const ScoreOptions opt{scale, p.softcap, slope2[y]};
+        const ScoreOptions opt{scale, p.softcap, p.inv_cap, slope2[y]};
         float g[2];  // what st is of a score
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
@@ -971,7 +978,7 @@ __global__ __launch_bounds__(2 * tile_rows(D), 2) void k_attend_tile(AttnParams 
   const int pos = it.pos0 + i;
   // positions of the wave's first and last row
   const int pos_lo = it.pos0 + min(wave_row / p.group, it.rows - 1), pos_hi = it.pos0 + min((wave_row + 31) / p.group, it.rows - 1);
-  const ScoreOptions opt{fabsf(p.scale), p.softcap, OPT && p.slopes ? p.slopes[hq] * kLog2e : 0.f};
+  const ScoreOptions opt{fabsf(p.scale), p.softcap, p.inv_cap, OPT && p.slopes ? p.slopes[hq] * kLog2e : 0.f};
   const int32_t* table = p.table + it.r * p.ld;
   const uint32_t page_bytes = P * D, pool_bytes = p.c.Hkv * page_bytes;
 

@@ -368,6 +368,7 @@ spear_status_t spear_attention(const spear_attention_t* a, void* hip_stream) {
   p.table = b->table;
   p.q = (const uint16_t*)a->q, p.out = (uint16_t*)a->out;
   p.slopes = a->slopes, p.scale = a->scale, p.softcap = a->softcap;
+  p.inv_cap = a->softcap > 0.f ? std::min(1.f / a->softcap, 3.40282347e38f) : 0.f;
   p.mid_blocks = (uint32_t)l.z.max_tile * c->kv_heads;
   p.items_rows = (const AttnItem*)((const char*)a->plan + l.items_rows);
   p.items_tile = (const AttnItem*)((const char*)a->plan + l.items_tile);

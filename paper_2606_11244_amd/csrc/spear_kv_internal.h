@@ -98,7 +98,7 @@ struct AttnParams {
   const uint16_t* q;
   uint16_t* out;
   const float* slopes;
-  float scale, softcap;
+  float scale, softcap, inv_cap;  // inv_cap: 1 / softcap, finite
   uint32_t *counters_rows, *counters_tile;  // [part][Hkv]: kAttnCounters each
   float *parts_rows, *parts_tile;  // [part][Hkv][rows of O, their maxima, their sums]
   uint32_t mid_blocks;             // workgroups of k_attend_mid that take tiles

@@ -67,3 +67,31 @@ def test_attention_over_scales_that_grew_past_the_types_end(codes, lengths, more
     for scale in (None, 40.0):  # (and weights that are zero but for one token)
         s.check(scale=scale)
         assert bool(torch.isfinite(s.out[:lengths[0][0]]).all())
+
+
+@pytest.mark.parametrize("D,act,codes", [(64, torch.float16, torch.int8), (128, torch.bfloat16, torch.float8_e4m3fn)])
+@pytest.mark.parametrize("lengths,more", [([(1, 700), (2, 90)], dict(heads=4)), ([(20, 300), (7, 7)], dict(heads=8)),
+                                          ([(200, 300), (1, 50)], LARGE)])
+def test_caps_of_any_size(D, act, codes, lengths, more):
+    """Scores far below the cap (which then makes no difference), about it, far above it; caps whose reciprocal
+    is not a float, or is not a normal one."""
+    s = Setup(lengths, kvh=2, D=D, P=32, act=act, codes=codes, **more)
+    for cap in (3e38, 1e30, 1e8, 1e6, 1e4, 300.0, 20.0, 1.0, 1e-3, 1e-30, 1e-39, 1e-45):
+        s.check(softcap=cap, scale=0.3)
+    s.check(softcap=1e7, scale=-2.0)
+
+
+def test_caps_where_weights_are_even():
+    """Scores of at most 1 that a cap of 10^8 leaves as they are: the weights follow them."""
+    act = torch.float16
+    s = Setup([(1, 64)], 1, 1, 64, 16, act, torch.int8)
+    g = torch.Generator(device="cuda").manual_seed(4)
+    slots = _ints([s.table[0][j // 16] * 16 + j % 16 for j in range(64)])
+    k = torch.zeros(64, 1, 64, dtype=act, device="cuda")
+    k[:, 0, 0] = torch.linspace(-1, 1, 64, device="cuda").to(act)
+    v = torch.randn(64, 1, 64, device="cuda", generator=g).to(act)
+    s.kv.append(s.cache, k, v, slots)
+    s.q.zero_()
+    s.q[:, :, 0] = 1.0
+    for cap in (1e3, 1e5, 1e8, 3e38):
+        s.check(scale=1.0, softcap=cap)
