@@ -77,6 +77,11 @@ __device__ __forceinline__ int plan_range(const AttnPlanParams& p, AttnItem& it,
   it.s1 = max(it.s0, (it.end + kStep - 1) / kStep);
   return it.s1 - it.s0;
 }
+// the least steps of a stretch, so that `total` steps make about `goal` of them (no request has
+// more steps than kKvLength's, and a sum over all of them passes 32 bits)
+__device__ __forceinline__ int plan_least(int64_t total, int goal, int least) {
+  return max(least, (int)min((total + goal - 1) / goal, (int64_t)(kKvLength / kStep)));
+}
 __device__ __forceinline__ int plan_splits(int steps, int c) { return steps > c ? (steps + c - 1) / c : 1; }
 // the same of few rows, whose stretches have at least the square root of a fifth of the
 // request's steps, in fours (the waves' turns): one workgroup joins them all, and a long
@@ -117,7 +122,7 @@ __global__ __launch_bounds__(kPlanThreads) void k_attention_plan(AttnPlanParams 
   }
   if (tid < kSizes) s_size[tid] = 0;
   plan_scan(sum, red, &total);
-  const int c = max(p.z.least_rows, (int)((total + p.z.goal_rows - 1) / p.z.goal_rows));
+  const int c = plan_least(total, p.z.goal_rows, p.z.least_rows);
   // their stretches, long ones first: by size in kSizes classes (where a request stands
   // in its class is left to chance, and makes no difference to what is computed)
   int64_t counts = 0;  // items, and partial results in the upper half
@@ -165,7 +170,9 @@ __global__ __launch_bounds__(kPlanThreads) void k_attention_plan(AttnPlanParams 
     AttnItem it = plan_request(p, r);
     int k = plan_row_splits(plan_range(p, it, 0, it.rows), c);
     if (k > 1 && s_part[r] + k > p.z.part_rows) it.s1 = it.s0, k = 1;  // (arrays that contradict themselves)
-    p.items_rows[s_place[r] + x] = plan_stretch(it, k, k > 1 ? x : 0, s_part[r]);
+    const int at = s_place[r];
+    if (at + k > p.z.max_rows) it.key = 0;  // (more than the sizes allow: none of it)
+    if (at + x < p.z.max_rows) p.items_rows[at + x] = plan_stretch(it, k, k > 1 ? x : 0, s_part[r]);
   }
   for (int i = n_items + tid; i < p.z.max_rows; i += blockDim.x) p.items_rows[i].key = 0;
   if (!p.z.max_tile) return;
@@ -184,7 +191,7 @@ __global__ __launch_bounds__(kPlanThreads) void k_attention_plan(AttnPlanParams 
   int k = 0;
   for (int t = tid; t < n_tiles; t += blockDim.x) sum += tile_of((int)n_tiles - 1 - t, it);
   plan_scan(sum, red, &total);
-  const int ct = max(p.z.least_tile, (int)((total + p.z.goal_tile - 1) / p.z.goal_tile));
+  const int ct = plan_least(total, p.z.goal_tile, p.z.least_tile);
   int64_t base = 0;  // as counts
   for (int t0 = 0; t0 < n_tiles; t0 += blockDim.x) {
     const int t = (int)n_tiles - 1 - t0 - tid;
@@ -197,7 +204,8 @@ __global__ __launch_bounds__(kPlanThreads) void k_attention_plan(AttnPlanParams 
     const int part = (int)(before_me >> 32);
     const bool room = k <= 1 || part + k <= p.z.part_tile;
     if (!room) it.s1 = it.s0;
-    for (int x = 0; x < k; ++x, ++i)
+    if (k > p.z.max_tile - i) it.key = 0;  // (more than the sizes allow: none of it)
+    for (int x = 0; x < k && i < p.z.max_tile; ++x, ++i)
       p.items_tile[i] = plan_stretch(it, room ? k : 1, room ? x : 0, part);
   }
   for (int i = (int)(base & 0xFFFFFFFF) + tid; i < p.z.max_tile; i += blockDim.x) p.items_tile[i].key = 0;

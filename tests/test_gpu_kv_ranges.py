@@ -95,3 +95,48 @@ def test_caps_where_weights_are_even():
     s.q[:, :, 0] = 1.0
     for cap in (1e3, 1e5, 1e8, 3e38):
         s.check(scale=1.0, softcap=cap)
+
+
+# ---------------------------------------------------------------------------
+# plans of the longest requests: written, and only their shares counted; attention over them would take hours
+# ---------------------------------------------------------------------------
+
+def _plan_in_margins(kv, plan, margin=1 << 16):
+    """The plan's own bytes after a call, which stand between margins that have to stay as they are."""
+    n = plan.buffer.numel()
+    room = torch.full((margin + n + 16 * margin,), 0x5A, dtype=torch.uint8, device="cuda")
+    at = room[margin:margin + n]
+    plan.c.plan = at.data_ptr()
+    kv.attention_plan(plan)
+    torch.cuda.synchronize()
+    assert bool((room[:margin] == 0x5A).all()) and bool((room[margin + n:] == 0x5A).all())
+    return at.view(torch.int32).view(-1, 16).cpu()  # a share is 64 bytes: its sizes' number (0: none), its request, ...
+
+
+def test_plans_of_the_longest_requests_in_tiles():
+    """8192 tiles of 2^24 steps: a stretch's length passes 31 bits before it is held to a request's steps."""
+    kv = _kv()
+    T, P, width = 131072, 128, 1 << 23
+    cache = kv.new_cache(1, 8, P, 64, torch.float16)
+    batch = kv.Batch(torch.empty((1, width), dtype=torch.int32, device="cuda"), T, starts=_ints([0, T]), lens=_ints([2 ** 30 - 1]))
+    plan = kv.AttentionPlan(cache, batch, 64)
+    tiles = T * 8 // 128
+    shares = _plan_in_margins(kv, plan)
+    shares = shares[shares[:, 0] != 0]
+    assert shares.shape[0] == tiles and bool((shares[:, 1] == 0).all())  # one stretch each
+    # what a length out of bounds gives
+    for bad in (2 ** 31 - 1, 2 ** 30, -1):
+        batch.lens.fill_(bad)
+        _plan_in_margins(kv, plan)
+
+
+def test_plans_of_the_longest_requests_of_few_rows():
+    """160 requests of 2^24 steps and 512 kv heads, one stretch wanted in all: 2.7 10^9 steps."""
+    kv = _kv()
+    R, P, width = 160, 128, 1 << 23
+    cache = kv.new_cache(1, 512, P, 64, torch.float16)
+    table = torch.empty((R, width), dtype=torch.int32, device="cuda")
+    batch = kv.Batch(table, R, max_new=1, starts=_ints(list(range(R + 1))), lens=_ints([2 ** 30 - 1] * R))
+    shares = _plan_in_margins(kv, kv.AttentionPlan(cache, batch, 512))
+    shares = shares[shares[:, 0] != 0]
+    assert sorted(shares[:, 1].tolist()) == list(range(R))  # one stretch each
