@@ -212,8 +212,10 @@ spear_status_t spear_attention_sizes(const spear_attention_t* args, size_t* plan
  * from starts, lens, window and prefix. It serves every spear_attention whose
  * cache, batch, heads, window and prefix are the same in size and content (the
  * layers of a step), until one of them changes. Where sizes differ the attention
- * writes nothing. Errors as for spear_attention; q, out and the workspace are not
- * looked at. */
+ * writes nothing. With starts that descend or lie outside 0..tokens the step's rows
+ * of `out` hold unspecified values or what they held; nothing else is touched, and a
+ * later call is as any other. Errors as for spear_attention; q, out and the workspace
+ * are not looked at. */
 spear_status_t spear_attention_plan(const spear_attention_t* args, void* hip_stream);
 
 /* Errors: SPEAR_E_NULL, SPEAR_E_DTYPE, SPEAR_E_SHAPE, SPEAR_E_ALIGN; SPEAR_E_WORKSPACE

@@ -140,3 +140,49 @@ def test_plans_of_the_longest_requests_of_few_rows():
     shares = _plan_in_margins(kv, kv.AttentionPlan(cache, batch, 512))
     shares = shares[shares[:, 0] != 0]
     assert sorted(shares[:, 1].tolist()) == list(range(R))  # one stretch each
+
+
+# ---------------------------------------------------------------------------
+# contradicting arrays
+# ---------------------------------------------------------------------------
+
+def _between_margins(n, dtype, rows=1 << 16):
+    """(all, the n elements in the middle): the rest is a pattern."""
+    room = torch.full((n + 2 * rows,), 0x5A, dtype=torch.uint8, device="cuda") if dtype is torch.uint8 else \
+        torch.full((n + 2 * rows,), 5.0, dtype=dtype, device="cuda")
+    return room, room[rows:rows + n], rows
+
+
+@pytest.mark.parametrize("kvh,more", [(1, dict(heads=8, pad=4, D=64)), (8, dict(D=128, **LARGE))])
+def test_contradicting_starts_touch_nothing_else(kvh, more):
+    """Out, plan and workspace between margins that stay as they are, whatever starts and lens hold; rows behind the
+    step's tokens and the inputs too; and a call after it is right."""
+    s = Setup([(3, 900), (40, 1200), (1, 2500), (2, 33)], kvh=kvh, P=16, act=torch.bfloat16, codes=torch.int8, **more)
+    want, T = s.run().clone(), s.batch.tokens
+    rooms = []
+    for name, t in (("out", s.out), ("plan", s.plan.buffer), ("ws", s.ws)):
+        room, middle, rows = _between_margins(t.numel(), t.dtype)
+        rooms.append((name, room, rows, t.numel()))
+        if name == "out":
+            s.out = middle.view(t.shape)
+        elif name == "plan":
+            s.plan.buffer, s.plan.c.plan = middle, middle.data_ptr()
+        else:
+            middle.zero_()
+            s.ws = middle
+    kept = [t.clone() for t in (*s.cache.tensors(), s.q, s.batch.table)]
+    n = s.starts[-1]
+    for starts in ([n, 0, n, 0, n], [-5, 2 ** 31 - 1, 3, -2 ** 31, 50], [n] * 5, [0, n, n, 0, n], [T, 0, T, 0, T], [9, 3, 1, 0, -1]):
+        for lens in ([2 ** 31 - 1, 1200, -7, 2 ** 30], [0, 0, 0, 0], [900, 1200, 2500, 33]):
+            s.batch.starts.copy_(_ints(starts))
+            s.batch.lens.copy_(_ints(lens))
+            s.run()
+            s.batch.starts.copy_(_ints(s.starts))
+            s.batch.lens.copy_(_ints(s.lens))
+            s.out.fill_(9.0)
+            assert torch.equal(s.run(), want)
+            for name, room, rows, size in rooms:
+                fill = 0x5A if room.dtype is torch.uint8 else 5.0
+                assert bool((room[:rows] == fill).all()) and bool((room[rows + size:] == fill).all()), (name, starts, lens)
+    for before, t in zip(kept, (*s.cache.tensors(), s.q, s.batch.table)):
+        assert torch.equal(before.view(torch.uint8), t.view(torch.uint8))
