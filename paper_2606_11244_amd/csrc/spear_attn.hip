@@ -962,6 +962,10 @@ __global__ __launch_bounds__(2 * tile_rows(D), 2) void k_attend_tile(AttnParams 
   constexpr int KBYTES = kStep * KP, BUF = KBYTES + D * VP, ROWS = tile_rows(D), THREADS = 2 * ROWS;
   __shared__ __attribute__((aligned(16))) char lds[2 * BUF];
   __shared__ __attribute__((aligned(16))) float s_ks[2][4];
+  // tokens of the four runs that stand in a page. (Words of their own: as the sign of s_ks, taken
+  // off in the steps that are masked, the compiler moved that |x| to one of the two branches into
+  // them, and rows of pages outside the pool were NaN.)
+  __shared__ __attribute__((aligned(16))) uint32_t s_there[2][4];
   __shared__ int s_last;
   early(p);
   const int head = blockIdx.x % p.c.Hkv, idx = blockIdx.x / p.c.Hkv;
@@ -1053,8 +1057,8 @@ __global__ __launch_bounds__(2 * tile_rows(D), 2) void k_attend_tile(AttnParams 
         v[1] = v_operand8<DT, FMT>(vr[x][1], vr[x][3], f);
       }
     }
-    // (runs 0..3) what a dot product is of a score; no page: below zero, for the waves to see
-    if (tid < 4) s_ks[s & 1][tid] = held_v < 0 ? -1.f : OPT ? sc.x : dot_factor(sc.x, opt);
+    // (runs 0..3) what a dot product is of a score
+    if (tid < 4) s_ks[s & 1][tid] = OPT ? sc.x : dot_factor(sc.x, opt), s_there[s & 1][tid] = held_v < 0 ? 0u : 0xFFFFu;
   };
 
   f32x16 o[D / 32] = {};
@@ -1083,11 +1087,10 @@ __global__ __launch_bounds__(2 * tile_rows(D), 2) void k_attend_tile(AttnParams 
         for (int t = 0; t < 2; ++t)
           st[t] = mfma32<DT>(*(const u32x4*)(buf + (32 * t + c) * KP + 32 * x + 16 * h), q[x], st[t]);
       const f32x4 ks = *(const f32x4*)s_ks[s & 1];
-      const bool pages_there = __all(fminf(fminf(ks[0], ks[1]), fminf(ks[2], ks[3])) > 0.f);
+      const u32x4 there = *(const u32x4*)s_there[s & 1];
+      const bool pages_there = __builtin_amdgcn_readfirstlane(there[0] & there[1] & there[2] & there[3]) != 0;
       const bool whole = j0 + kStep <= min(it.end, pos_lo + 1) && pos_hi - j0 < p.window && pages_there;
-      f32x4 f;  // what st is of a score (an operand's modifier; left to the masked steps it was left out of some of them)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) f[r] = fabsf(ks[r]);
+      f32x4 f = ks;  // what st is of a score
       if constexpr (OPT) {
         f = f32x4{1.f, 1.f, 1.f, 1.f};
 #pragma unroll
@@ -1098,7 +1101,7 @@ __global__ __launch_bounds__(2 * tile_rows(D), 2) void k_attend_tile(AttnParams 
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
           uint32_t sees = seen_tokens(j0 + 32 * t, it, pos, p.window);
-          sees &= (ks[2 * t] > 0.f ? 0xFFFFu : 0u) | (ks[2 * t + 1] > 0.f ? 0xFFFF0000u : 0u);
+          sees &= there[2 * t] | there[2 * t + 1] << 16;
           sees >>= 4 * h;
 #pragma unroll
           for (int e = 0; e < 16; ++e) st[t][e] = where_seen(st[t][e], sees, 8 * (e >> 2) + (e & 3));

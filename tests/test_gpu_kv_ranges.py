@@ -186,3 +186,35 @@ def test_contradicting_starts_touch_nothing_else(kvh, more):
                 assert bool((room[:rows] == fill).all()) and bool((room[rows + size:] == fill).all()), (name, starts, lens)
     for before, t in zip(kept, (*s.cache.tensors(), s.q, s.batch.table)):
         assert torch.equal(before.view(torch.uint8), t.view(torch.uint8))
+
+
+# ---------------------------------------------------------------------------
+# pages outside the pool, in steps that every row would see whole
+# ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("codes", CODES)
+@pytest.mark.parametrize("D,P", [(64, 16), (128, 32), (128, 64), (64, 128)])
+@pytest.mark.parametrize("options", [{}, dict(softcap=7.0, slopes=True)])
+@pytest.mark.parametrize("lengths,more", [([(1, 1500), (2, 700)], dict(heads=4)), ([(20, 1500), (9, 700)], dict(heads=8)),
+                                          ([(200, 1500), (90, 700)], LARGE)])
+def test_pages_outside_the_pool(act, codes, D, P, options, lengths, more):
+    """One page in a step, the first, the last that is whole, several in a row; what stands at the pool's first page,
+    which a kernel may read in their place, is no number."""
+    s = Setup(lengths, kvh=2, D=D, P=P, act=act, codes=codes, **more)
+    kinds = (-1, s.pool, 2 ** 31 - 1, -2 ** 31)
+    dead = [torch.zeros(L, dtype=torch.bool) for _, L in lengths]
+    for r, (n, L) in enumerate(lengths):
+        last = (L - n) // P - 1  # every row sees the whole of it
+        for x, page in enumerate((0, 2, last // 2, last // 2 + 1, last // 2 + 2, last)):
+            s.batch.table[r, page] = kinds[x % 4]
+            dead[r][P * page:P * page + P] = True
+        for page in range(-(-L // P)):  # pages of the pool's first place go too
+            if s.table[r][page] == 0:
+                s.batch.table[r, page] = -1
+                dead[r][P * page:P * page + P] = True
+    for scale in (s.cache.k_scale, s.cache.v_scale):
+        scale[0] = float("nan")
+    s.cache.v.view(torch.uint8)[0] = 0x7F
+    slopes = torch.exp2(-torch.arange(s.heads, device="cuda").float() / 8) if options.get("slopes") else None
+    s.check(softcap=options.get("softcap", 0.0), slopes=slopes, dead=dead)
