@@ -6,13 +6,20 @@ namespace spear {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLowest = -3.402823466e38f;  // running maximum of a row that has seen nothing
+// Weights, the products' operands, are held in the activation type. fp16 has nothing below
+// 2^-25, where a long context's tail may have its weight (131000 tokens: up to 0.4 % of the
+// largest's): weights are made against a maximum kLift powers of two lower, so that the largest is
+// 2^7, in tiles 2^3, and 2^-32 or 2^-28 of it still counts (bf16 has fp32's range).
+template <int DT> constexpr float kLift = DT == DT_F16 ? 7.f : 0.f;
+template <int DT> constexpr float kTileLift = DT == DT_F16 ? 3.f : 0.f;
 // How far scores may pass a row's maximum, in powers of two, before it is moved and
-// what was summed is scaled: weights up to 2^8 keep their precision in either type.
+// what was summed is scaled: weights up to 2^(kLift + 8), in fp16's range.
 constexpr float kSlack = 8.f;
 // Where the maximum costs more than the weights: a step's weights are made against the
 // maximum so far, and once more against a new one only where a row's sum of them (half
-// a row's, a lane's) passes 2^12, far from fp16's end.
-constexpr float kMostSum = 4096.f;
+// a row's, a lane's) passes 2^12, in fp16 2^15: each weight is in its range. (With the largest
+// at 2^7 that comes more often: a prompt of 4096 314 us instead of 307, 309 with 2^4.)
+template <int DT> constexpr float kMostSum = DT == DT_F16 ? 32768.f : 4096.f;
 
 #if !SPEAR_BF16_UNIT
 // ---------------------------------------------------------------------------
@@ -507,8 +514,8 @@ __device__ __forceinline__ void attend_rows(const AttnParams& p, uint32_t block,
       for (int e = 1; e < 16; ++e) top = fmaxf(top, st[e >> 2][e & 3]);
       top *= fk;
       top = max_sixteens(top);
-      if (__any(top > m + kSlack)) {
-        const float now = fmaxf(m, top), fade = __builtin_amdgcn_exp2f(m - now);
+      if (__any(top > m + (kLift<DT> + kSlack))) {
+        const float now = fmaxf(m, top - kLift<DT>), fade = __builtin_amdgcn_exp2f(m - now);
         m = now;
         l *= fade;
 #pragma unroll
@@ -820,7 +827,7 @@ __device__ __forceinline__ void attend_mid(const AttnParams& p, uint32_t block, 
                 pw[y][2 * t + (e >> 2)][e & 3] = DT == DT_F16 && FMT == KV_INT8 ? scaled2(w, f[t].y) : w;
               }
             }
-          if (pass || !__any(!(sum <= kMostSum))) break;
+          if (pass || !__any(!(sum <= kMostSum<DT>))) break;
           float top = kLowest;
 #pragma unroll
           for (int t = 0; t < 2; ++t) {
@@ -829,7 +836,7 @@ __device__ __forceinline__ void attend_mid(const AttnParams& p, uint32_t block, 
             for (int e = 1; e < 16; ++e) x = fmaxf(x, st[y][t][e]);
             top = fmaxf(top, x * g[t]);
           }
-          const float now = fmaxf(m[y], max_halves(top)), fade = __builtin_amdgcn_exp2f(m[y] - now);
+          const float now = fmaxf(m[y], max_halves(top) - kTileLift<DT>), fade = __builtin_amdgcn_exp2f(m[y] - now);
           m[y] = now;
           l[y] *= fade;
 #pragma unroll
@@ -1120,7 +1127,7 @@ __global__ __launch_bounds__(2 * tile_rows(D), 2) void k_attend_tile(AttnParams 
                                  __builtin_amdgcn_exp2f(__builtin_fmaf(st[y >> 1][x + 1], f[y], -m)));
             sum = add2<DT>(pw[y][e], sum);
           }
-        if (pass || !__any(!(sum <= kMostSum))) break;
+        if (pass || !__any(!(sum <= kMostSum<DT>))) break;
         float top = kLowest;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
@@ -1129,7 +1136,7 @@ __global__ __launch_bounds__(2 * tile_rows(D), 2) void k_attend_tile(AttnParams 
           for (int e = 1; e < 8; ++e) x = fmaxf(x, st[r >> 1][8 * (r & 1) + e]);
           top = fmaxf(top, x * f[r]);
         }
-        const float now = fmaxf(m, max_halves(top)), fade = __builtin_amdgcn_exp2f(m - now);
+        const float now = fmaxf(m, max_halves(top) - kTileLift<DT>), fade = __builtin_amdgcn_exp2f(m - now);
         m = now;
         l *= fade;
 #pragma unroll

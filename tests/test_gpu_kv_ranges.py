@@ -2,6 +2,8 @@
 the GPU, against formulas in 64 bits."""
 from __future__ import annotations
 
+import math
+
 import pytest
 import torch
 
@@ -218,3 +220,36 @@ def test_pages_outside_the_pool(act, codes, D, P, options, lengths, more):
     s.cache.v.view(torch.uint8)[0] = 0x7F
     slopes = torch.exp2(-torch.arange(s.heads, device="cuda").float() / 8) if options.get("slopes") else None
     s.check(softcap=options.get("softcap", 0.0), slopes=slopes, dead=dead)
+
+
+# ---------------------------------------------------------------------------
+# weights far below the largest
+# ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("act,codes", [(torch.float16, torch.int8), (torch.float16, torch.float8_e4m3fn), (torch.bfloat16, torch.int8)])
+@pytest.mark.parametrize("lengths,more", [([(1, 60000)], dict(heads=4)), ([(20, 9000)], dict(heads=8)), ([(1600, 3000)], LARGE)])
+@pytest.mark.parametrize("D,power", [(64, 20.0), (128, 25.3), (64, 26.2)])
+def test_weights_far_below_the_largest(act, codes, lengths, more, D, power):
+    """A first token of weight 1 and value 0, all others of weight 2^-power and value 1: together they are what
+    comes out, though each is near or below the least number of fp16."""
+    n, L = lengths[0]
+    s = Setup(lengths, kvh=2, D=D, P=64, act=act, codes=codes, **more)
+    slots = [s.table[0][j // 64] * 64 + j % 64 for j in range(L)]
+    k = torch.zeros(L, 2, D, dtype=act, device="cuda")
+    k[1:, :, 0] = -1.0
+    v = torch.ones(L, 2, D, dtype=act, device="cuda")
+    v[0] = 0.0
+    s.kv.append(s.cache, k, v, _ints(slots))
+    s.q.zero_()
+    s.q[:, :, 0] = 1.0
+    scale = power * math.log(2)
+    got = s.run(scale=scale)[:n].cpu().double()
+    others = torch.arange(L - n, L).double() * math.exp(-float(torch.tensor(scale, dtype=torch.float32)))
+    want = (others / (1 + others))[:, None, None].expand_as(got)
+    # Of the weight of each: its rounding (half a step, or in fp16 half of its least number, 2^-25, to a largest
+    # weight of 2^3 at least), and its score's, a product and three roundings of a number of `power` in fp32: 2^-22 power.
+    # Of the sum over them as much, and L roundings of the sums at 2^-24 each; and that of the output.
+    u = U.U[act]
+    each = torch.maximum(torch.tensor(u), torch.tensor(2.0 ** (power - 28) if act is torch.float16 else 0.0)).double()
+    bound = want * (2 * each + 2.0 ** -22 * power + L * 2.0 ** -24 + u) + (2.0 ** -25 if act is torch.float16 else 0.0)
+    assert bool(((got - want).abs() <= bound).all()), float(((got - want).abs() / want).max())
