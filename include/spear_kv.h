@@ -181,8 +181,8 @@ spear_status_t spear_kv_read(const spear_kv_cache_t* cache, int64_t n, const int
  * held in fp32; the weights e^(s_j - max) are rounded to the act dtype, in fp16 to
  * 2^-29 of the largest at best, for their product with v (whose values it holds
  * exactly, in fp16 to 2^-25) and, of requests of more than 16 rows a kv head, in their
- * sum; out is rounded once. The sums are of weights of up to 2^12 beside a row's
- * largest: in bf16, values from 2^115 on may leave fp32's range there.
+ * sum; out is rounded once. In bf16 the sums over j may leave fp32's range where a
+ * value times the request's tokens passes 2^115.
  * Rows behind the last request are left as they were. Codes and scales of tokens that
  * no row of a request sees may hold anything; those seen are finite. */
 typedef struct {
