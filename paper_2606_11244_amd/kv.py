@@ -86,6 +86,14 @@ def _ints(t, n, what):
     return t.data_ptr()
 
 
+def _size(v, what):
+    """A size as the C structs hold it, which keep the lower 32 bits of any."""
+    v = int(v)
+    if not -(1 << 31) <= v < 1 << 31:
+        raise ValueError(f"{what} is a number of 32 bits (got {v})")
+    return v
+
+
 def _on(holder, dev):
     """That a cache's, batch's or rotation's tensors are on GPU `dev`."""
     if holder.device != dev:
@@ -168,13 +176,13 @@ class Batch:
             _ints(t, n, what)
             return t
 
-        self.table, self.tokens, self.requests = table, int(tokens), R
+        self.table, self.tokens, self.requests = table, _size(tokens, "tokens"), R
         self.starts, self.lens = ints(starts, R + 1, "starts"), ints(lens, R, "lens")
-        self.max_new = max(1, self.tokens) if max_new is None else int(max_new)
+        self.max_new = max(1, self.tokens) if max_new is None else _size(max_new, "max_new")
         self.device = table.get_device()
         if self.starts.get_device() != self.device or self.lens.get_device() != self.device:
             raise ValueError("a batch's tensors are on one device")
-        self.c = _Batch(R, self.tokens, self.max_new, width, table.stride(0) if R > 1 else 0, 0,
+        self.c = _Batch(R, self.tokens, self.max_new, width, _size(table.stride(0), "table's stride") if R > 1 else 0, 0,
                         self.starts.data_ptr(), self.lens.data_ptr(), table.data_ptr())
         self._ref = ctypes.byref(self.c)
 
@@ -184,7 +192,7 @@ def pages(batch: Batch, held, fresh, free_pages, slots, positions, taken, *, pag
     dev = _device_of(held, fresh, free_pages, slots, positions, taken)
     _on(batch, dev)
     R, T = batch.requests, batch.tokens
-    a = _Pages(page_tokens, free_pages.numel(), _ints(held, R, "held"), _ints(fresh, R, "fresh"),
+    a = _Pages(_size(page_tokens, "page_tokens"), free_pages.numel(), _ints(held, R, "held"), _ints(fresh, R, "fresh"),
                _ints(free_pages, free_pages.numel(), "free_pages"), _ints(slots, T, "slots"),
                _ints(positions, T, "positions"), _ints(taken, 2, "taken"))
     st = LIB.spear_kv_pages(batch._ref, ctypes.byref(a), _raw_stream(stream, dev))
@@ -259,8 +267,8 @@ class AttentionPlan:
     and prefix [requests] int32, and the plan buffer that attention_plan writes."""
 
     def __init__(self, cache: Cache, batch: Batch, heads, *, window=0, prefix=None):
-        self.cache, self.batch, self.heads, self.prefix = cache, batch, int(heads), prefix
-        self.c = _Attention(ctypes.pointer(cache.c), ctypes.pointer(batch.c), self.heads, int(window),
+        self.cache, self.batch, self.heads, self.prefix = cache, batch, _size(heads, "heads"), prefix
+        self.c = _Attention(ctypes.pointer(cache.c), ctypes.pointer(batch.c), self.heads, _size(window, "window"),
                             None if prefix is None else _ints(prefix, batch.requests, "prefix"))
         plan, work = ctypes.c_size_t(), ctypes.c_size_t()
         _check(LIB.spear_attention_sizes(ctypes.byref(self.c), ctypes.byref(plan), ctypes.byref(work)),
