@@ -253,3 +253,10 @@ def test_weights_far_below_the_largest(act, codes, lengths, more, D, power):
     each = torch.maximum(torch.tensor(u), torch.tensor(2.0 ** (power - 28) if act is torch.float16 else 0.0)).double()
     bound = want * (2 * each + 2.0 ** -22 * power + L * 2.0 ** -24 + u) + (2.0 ** -25 if act is torch.float16 else 0.0)
     assert bool(((got - want).abs() <= bound).all()), float(((got - want).abs() / want).max())
+
+
+@pytest.mark.parametrize("heads,kvh", [(1024, 1024), (1024, 512), (1024, 32), (1024, 1), (512, 512)])
+def test_the_most_heads(heads, kvh):
+    """More kv heads than stretches are wanted, and groups of a thousand heads."""
+    Setup([(1, 70), (2, 33)], heads, kvh, 64, 16, torch.float16, torch.int8, pad=1).check()
+    Setup([(20, 50), (1, 300)], heads, kvh, 64, 32, torch.bfloat16, torch.float8_e4m3fn).check()
