@@ -6,7 +6,11 @@ namespace spear {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLowest = -3.402823466e38f;  // running maximum of a row that has seen nothing
-// Weights, the products' operands, are held in the activation type. fp16 has nothing below
+// Weights are the second product's operand and held in the activation type as its MFMA takes
+// it: in two parts they would take V's MFMAs twice. Error of the listed calls against 64 bits,
+// with the output's own rounding: fp16 2.1e-4 with exact weights, 2.2e-4 to 2.6e-4 with these,
+// bf16 1.7e-3 and 1.9e-3 to 2.2e-3. Tiles sum them as rounded, two an instruction: what rounding
+// puts on all of a row's weights alike is then not in the quotient. fp16 has nothing below
 // 2^-25, where a long context's tail may have its weight (131000 tokens: up to 0.4 % of the
 // largest's): weights are made against a maximum kLift powers of two lower, so that the largest is
 // 2^7, in tiles 2^3, and 2^-32 or 2^-28 of it still counts (bf16 has fp32's range).
@@ -260,7 +264,7 @@ __device__ __forceinline__ u32x4 v_operand8(uint32_t w0, uint32_t w1, float scal
     const h16x2 s = h16x2{(_Float16)scale, (_Float16)scale};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const uint32_t e = x[i];  // (a bit_cast of the element itself is taken as the first one's)
+      const uint32_t e = x[i];  // (this clang's bit_cast of an element of a vector takes the first one)
       x[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(h16x2, e) * s);
     }
   }
@@ -381,8 +385,9 @@ __device__ __forceinline__ u32x4 byte_mask(uint32_t bits) {
 // come in pieces of 16 bytes. The waves' and then the stretches' results are
 // joined in order, the latter by the stretch that ends last.
 // Bound: the codes' bytes (long caches: one request of 131000 tokens, 8 heads of 128,
-// 268 MB in 56 us, 4.8 TB/s, where the loads alone take as long; 64 requests of up to
-// 8192 tokens, 155 MB in 34 us, 4.5 TB/s), latency (one request of 500 tokens: 5.8 us).
+// 268 MB in 52 us, 5.1 TB/s, in replays of a graph 55, where the loads alone take as long;
+// 64 requests of up to 8192 tokens, 155 MB in 31 us, 5.0 TB/s, and 34), latency (one request
+// of 500 tokens: 5.7 us in a graph).
 // K goes through LDS so that V has the registers to be a step ahead (with both in
 // registers, and stretches in the requests' order, these 64 took 45 us).
 // ---------------------------------------------------------------------------
@@ -648,7 +653,7 @@ __device__ __forceinline__ void attend_rows(const AttnParams& p, uint32_t block,
 // Tiles of 32 rows and not more: more workgroups, and two of them to a SIMD's registers
 // (a chunk of 512 beside 8 requests 31 us, 45 in tiles of 64).
 // Bound: the conversions and exponentials beside the MFMAs; that chunk, 12.6 GFLOP, 8
-// heads on one: 29.5 us, 427 TFLOP/s.
+// heads on one: 28.3 us, 445 TFLOP/s.
 // ---------------------------------------------------------------------------
 template <int DT, int FMT, int D, bool OPT>
 __device__ __forceinline__ void attend_mid(const AttnParams& p, uint32_t block, char* lds, float* s_m, float* s_l, int* s_last) {
@@ -959,7 +964,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_attend_mid(AttnParams p) {
 // weights are V's operand once V's tokens stand in LDS in the order in which the
 // MFMA leaves the scores (the middle quads of every sixteen exchanged).
 // Bound: the MFMAs and the exponentials beside them: a prompt of 4096, 64 heads, 275 GFLOP
-// in 310 us, 884 TFLOP/s; its loads and MFMAs without a softmax take 200. Tried in its
+// in 309 us, 890 TFLOP/s; its loads and MFMAs without a softmax take 200. Tried in its
 // place, same prompt: the weights of a step made beside the next step's scores 322, tiles
 // of 128 rows at two workgroups a CU 367, four buffers and a barrier each two steps 319.
 // ---------------------------------------------------------------------------
