@@ -290,8 +290,8 @@ __device__ __forceinline__ void turn(const Unit& u, int interleaved, T (&a)[W], 
 // atomics, the same codes on every run. A workgroup of the queries' part takes
 // a token, its cosines and sines in LDS for all heads.
 // Bound: the bytes of q, k and v (long prompts: 4096 tokens with 64 heads of queries and
-// 8 of keys and values, 159 MB in 42 us, 3.8 TB/s), latency (decode: a token 6 us, slots,
-// rows, the page's scale and the maximum one after the other).
+// 8 of keys and values, 159 MB in 42 us, 3.8 TB/s), latency (decode: a token 5.8 us, 5.4
+// without a rotation: slots, rows and the page's scale, maximum, codes one after the other).
 // ---------------------------------------------------------------------------
 
 // the scale of a page and head, from the one before and the largest magnitude given
