@@ -178,8 +178,8 @@ spear_status_t spear_kv_read(const spear_kv_cache_t* cache, int64_t n, const int
  *           j <= p and p - j < window (0: any), or j < prefix[r]; j < lens[r]
  *
  * and zeros for a row that sees none. q.k, the softmax and the sums over j are
- * held in fp32; the weights e^(s_j - max) are rounded to the act dtype, in fp16 to
- * 2^-29 of the largest at best, for their product with v (whose values it holds
+ * held in fp32; the weights e^(s_j - max) are rounded to the act dtype (in fp16 small
+ * ones to 2^-28 of the largest) for their product with v (whose values it holds
  * exactly, in fp16 to 2^-25) and, of requests of more than 16 rows a kv head, in their
  * sum; out is rounded once. In bf16 the sums over j may leave fp32's range where a
  * value times the request's tokens passes 2^115.

@@ -7,7 +7,7 @@ namespace spear {
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLowest = -3.402823466e38f;  // running maximum of a row that has seen nothing
 // Weights are the second product's operand and held in the activation type as its MFMA takes
-// it: in two parts they would take V's MFMAs twice. Error of the listed calls against 64 bits,
+// it: in two parts they would take V's MFMAs twice. Error against 64 bits of ordinary calls,
 // with the output's own rounding: fp16 2.1e-4 with exact weights, 2.2e-4 to 2.6e-4 with these,
 // bf16 1.7e-3 and 1.9e-3 to 2.2e-3. Tiles sum them as rounded, two an instruction: what rounding
 // puts on all of a row's weights alike is then not in the quotient. fp16 has nothing below
